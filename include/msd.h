@@ -358,6 +358,135 @@ typedef struct {
 msd_status msd_test_gemm_shape(int32_t m, int32_t k, int32_t o, int32_t planes, int32_t glu, int32_t sms,
                                msd_gemm_shape *out);
 
+/* ---------------------------------------------------------------------------
+ * The paged cache: operators for programs that serve many multimodal requests
+ * from one pool of K/V pages (models of their own, run through msd_linear or
+ * otherwise; the contexts above keep their own caches). One pass of a model:
+ * msd_pages_reserve for the new rows of a batch, per layer msd_rope_append (q, k
+ * and v of the rows, rotated; K and V into the pages) and msd_pages_attention,
+ * then, for drafted trees, msd_pages_compact keeps the accepted path.
+ *
+ * All arrays are caller-owned device memory; calls are asynchronous on `stream`,
+ * read lengths and tables on the device and never synchronise. Argument errors
+ * are returned at once. What only the device can see sets the pool's status word;
+ * the first later call that observes it returns MSD_ERR_CAPACITY (too few free
+ * pages) or MSD_ERR_DEVICE (anything else), launches nothing, and clears it. A
+ * page operation that cannot be carried out changes nothing. A pool is used from
+ * one host thread and one stream at a time (or streams that are ordered by
+ * events), on the device that was current when it was created. Calls can be
+ * captured into a CUDA graph.
+ * ------------------------------------------------------------------------- */
+typedef struct msd_pages msd_pages;
+
+typedef struct {
+    int32_t dtype;              /* MSD_F32 or MSD_BF16: cache, q and attention output */
+    int32_t n_layers;
+    int32_t n_heads, n_kv_heads;/* query heads, a multiple (at most 64) of the K/V heads: query
+                                   head j reads K/V head j / (n_heads / n_kv_heads) */
+    int32_t head_dim;           /* 64 or 128 */
+    int32_t page_size;          /* tokens of a page: 16, 32, 64 or 128 */
+    int32_t n_pages;            /* pages of the pool */
+    int32_t max_seqs;           /* rows of the table: sequences that can live at once */
+    int32_t max_pages;          /* pages of one sequence; max_pages * page_size <= 2^30 */
+    int32_t rot_dim;            /* leading elements of a head that rotate: even, 0 .. head_dim;
+                                   element i pairs with i + rot_dim / 2 */
+    int32_t rot_section[3];     /* pairs that turn by time, height and width; sum rot_dim / 2
+                                   ({rot_dim / 2, 0, 0}: ordinary one-axis positions) */
+    int32_t rot_interleaved;    /* 0: the sections one after another. 1: the axes take turns: pair i
+                                   turns by height if i % 3 == 1 and i < 3 * rot_section[1], by
+                                   width if i % 3 == 2 and i < 3 * rot_section[2], else by time */
+    float rope_base;            /* pair i turns by position * base^(-2 i / rot_dim) */
+} msd_pages_config;
+
+/* Caller-owned state, borrowed for the pool's life (kv 16-byte aligned). A page holds
+ * page_size tokens of one sequence, of all layers. Token t of sequence s is at place
+ * t % page_size of page table[s][t / page_size]; entries past the last page are -1. Only
+ * full pages are shared between sequences: refs[p] sequences hold page p, 0: free. */
+typedef struct {
+    void *kv;                   /* [n_layers][n_pages][2][n_kv_heads][page_size][head_dim], K then V */
+    int32_t *table;             /* [max_seqs][max_pages] */
+    int32_t *len;               /* [max_seqs] tokens of each sequence, 0: unused */
+    int32_t *refs;              /* [n_pages] */
+} msd_pages_buffers;
+
+/* The rows of a call: sequence seqs[i] (all different) has rows row_start[i] ..
+ * row_start[i + 1] - 1 of the call's row arrays, and they are its LAST tokens (after
+ * msd_pages_reserve). n <= max_seqs, and <= 1024 for msd_pages_attention. */
+typedef struct {
+    int32_t n;
+    const int32_t *seqs;        /* [n] device */
+    const int32_t *row_start;   /* [n + 1] device, row_start[0] = 0, not decreasing */
+    int32_t rows;               /* = row_start[n] */
+} msd_batch;
+
+/* Creates a pool on the current device; it allocates its workspace once and touches none of
+ * the caller's arrays. Before other calls: msd_pages_restore.
+ * Errors: MSD_ERR_INVALID, MSD_ERR_OOM, MSD_ERR_CUDA. */
+msd_status msd_pages_create(const msd_pages_config *cfg, const msd_pages_buffers *buf, msd_pages **out);
+msd_status msd_pages_destroy(msd_pages *p);
+const char *msd_pages_last_error(const msd_pages *p);
+
+/* Takes len and table as they are (all lengths 0: an empty pool; or a saved state), sets
+ * refs and the free pages from them, and the table's unused entries to -1. A length or a
+ * page id out of range sets the status word. */
+msd_status msd_pages_restore(msd_pages *p, void *stream);
+
+/* Room for each sequence's rows at its end: len grows by them, new pages are the lowest free
+ * ids in the order of the list. */
+msd_status msd_pages_reserve(msd_pages *p, const msd_batch *batch, void *stream);
+
+/* Sequence dst[i] (unused, len 0) becomes a copy of src[i], which keeps its own. Full pages
+ * are shared, the tokens of a last partial page are copied; with deep != 0 every page is. */
+msd_status msd_pages_fork(msd_pages *p, int32_t n, const int32_t *src_dev, const int32_t *dst_dev, int32_t deep,
+                          void *stream);
+
+/* Of the last rows of each sequence (batch: how many), row keep[i * stride + j] becomes row j
+ * (j < n_keep[i]; ascending, keep null: the first n_keep rows) and the others are dropped:
+ * len shrinks, pages past the end are freed. This keeps the accepted path of a tree, takes
+ * tokens back, or cuts a long sequence (rows = its whole length). Pages that change and are
+ * shared are replaced by new ones, so other sequences keep theirs. */
+msd_status msd_pages_compact(msd_pages *p, const msd_batch *batch, const int32_t *keep_dev, int32_t keep_stride,
+                             const int32_t *n_keep_dev, void *stream);
+
+/* Frees n sequences (len 0 afterwards; one that is unused, or listed twice, is no error). */
+msd_status msd_pages_free(msd_pages *p, int32_t n, const int32_t *seqs_dev, void *stream);
+
+/* Rotary positions of interleaved text, images and video: sequence i of the batch has spans
+ * span_start[i] .. span_start[i + 1] - 1 (null: text alone) of spans[][5] = {first row
+ * within the sequence, t, h, w, time step}, ascending, t * h * w rows each. Positions start
+ * at first[i] (null: 0). A text row takes p, p, p and p grows by 1; a span's row (a, b, c)
+ * takes p + a * step, p + b, p + c and p grows by max((t - 1) * step + 1, h, w) after it.
+ * pos[axis * pos_stride + row]; next[i] (nullable) = p after the last row: the position of
+ * the next token. A span out of place sets the status word. */
+msd_status msd_rope_positions(msd_pages *p, const msd_batch *batch, const int32_t *span_start_dev,
+                              const int32_t *spans_dev, const int32_t *first_dev, int32_t *pos_dev,
+                              int64_t pos_stride, int32_t *next_dev, void *stream);
+
+/* Rotates q and k of the batch's rows by their positions (pos[axis * pos_stride + row], any
+ * int32; pos_stride 0: one position for the three axes), writes q to q_out (cache dtype) and
+ * k, v to the rows' slots of `layer`. q, k, v: row r at r * ld elements, heads one after
+ * another, fp32 (src_dtype MSD_F32, as msd_linear writes them) or the cache dtype. Angles
+ * are reduced exactly, products and sums are fp32, rounded once. Pointers and rows are
+ * 16-byte aligned. A row without a slot sets the status word and is skipped. */
+msd_status msd_rope_append(msd_pages *p, int32_t layer, const msd_batch *batch, const void *q_dev, int64_t ldq,
+                           const void *k_dev, int64_t ldk, const void *v_dev, int64_t ldv, int32_t src_dtype,
+                           const int32_t *pos_dev, int64_t pos_stride, void *q_out_dev, int64_t ldo, void *stream);
+
+/* Attention of the batch's rows over their sequences' pages of `layer`:
+ * out = softmax(q k / sqrt(head_dim)) v per head, lse (nullable, [rows][n_heads] fp32) its
+ * natural log-sum-exp. With L = len - rows of a sequence, row r sees the L tokens before the
+ * rows, and of the rows: those up to itself (tree null: decoding, or a chunk of a prompt),
+ * or those whose bit is set in its mask (tree: arrays of stride tree_nodes >= rows per
+ * listed sequence, as msd_verify; mask and depth are read, and n_nodes if given: rows at or
+ * past it see nothing). window > 0: a token at place P is seen from place Q only if
+ * Q - P < window or P < sinks; a row's place is L + r, with a tree L + its depth. A row that
+ * sees nothing gives zeros and -inf. Values that are not finite reach only the rows that
+ * see them; what a page holds past a sequence's end is never read into a result.
+ * q, out: row r at r * ld elements, heads one after another, 16-byte aligned rows. */
+msd_status msd_pages_attention(msd_pages *p, int32_t layer, const msd_batch *batch, const msd_tree *tree,
+                               int32_t tree_nodes, int32_t window, int32_t sinks, const void *q_dev, int64_t ldq,
+                               void *out_dev, int64_t ldo, float *lse_dev, void *stream);
+
 /* Profiling counters (tracing subsystem). kernel_launches counts every kernel
  * the library has run in this process (kernels executed by step graphs
  * included, kernels merely recorded into graphs excluded).

@@ -1,0 +1,104 @@
+// The paged cache: what its operators share on the host and on the device.
+#pragma once
+
+#include <algorithm>
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include "common.cuh"
+#include "msd.h"
+
+namespace msd {
+
+// Device status codes of the paged cache (after common.cuh's).
+enum : int {
+    ST_NO_PAGES = 5,      // fewer free pages than a call needed: the call changed nothing
+    ST_BAD_BATCH = 6,     // sequence ids, row counts or lists that the call cannot take
+};
+
+constexpr int MAX_ROT_PAIRS = 64;
+
+// Turns per position of each rotated pair as a 64-bit fraction (base^(-2i/rot) / 2 pi,
+// scaled by 2^64), and the axis (0 time, 1 height, 2 width) that the pair turns by.
+struct RopeTable {
+    unsigned long long turn[MAX_ROT_PAIRS];
+    unsigned char axis[MAX_ROT_PAIRS];
+};
+
+struct PagesView {
+    void *kv;                 // [layers][n_pages][2][kv_heads][page][head_dim]
+    int *table;               // [max_seqs][max_pages]
+    int *len, *refs;
+    unsigned *bits;           // bit p % 32 of word p / 32: page p is free
+    int *status;
+    int layers, heads, kv_heads, head_dim, page, page_shift;
+    int n_pages, max_seqs, max_pages;
+    __host__ __device__ long page_elems() const { return 2l * kv_heads * page * head_dim; }
+};
+
+// the rows of a call (msd_batch)
+struct BatchView {
+    int n, rows;
+    const int *seqs, *row_start;
+};
+
+__device__ __forceinline__ int pages_of(int tokens, int shift, int page) { return (tokens + page - 1) >> shift; }
+
+// The sequence of a row: the last i with row_start[i] <= row, found by the whole warp, 32
+// boundaries a step (one step up to 32 sequences, two up to 1024).
+__device__ __forceinline__ int row_owner(const int *row_start, int n, int row) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = n;                       // row_start[lo] <= row; row_start[hi] > row or hi == n
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) >> 5;
+        const int at = lo + lane * step;
+        const bool below = at < hi && row_start[at] <= row;
+        const int c = __popc(__ballot_sync(0xffffffffu, below));
+        const int nlo = lo + (c > 0 ? c - 1 : 0) * step;
+        hi = min(hi, nlo + step);
+        lo = nlo;
+    }
+    return lo;
+}
+
+// Attention over the pages (pages_attn_*.cu).
+struct PagesAttn {
+    PagesView pv;
+    BatchView b;
+    int layer;
+    const void *q;            // [rows][ldq]: head j of a row at j * head_dim
+    void *out;
+    float *lse;               // [rows][heads] or null
+    long ldq, ldo;
+    const uint64_t *mask;     // [n][nodes][words], null: each row sees the rows before it and itself
+    const int *depth;         // [n][nodes]
+    const int *n_nodes;       // [n] or null
+    int nodes, words;
+    int window, sinks;        // window 0: none
+    float scale_log2;         // log2(e) / sqrt(head_dim)
+    // partial results of row tiles that several CTAs share
+    float *part_o, *part_ml;
+    int4 *part_item;
+};
+
+constexpr int ATTN_MAX_SEQS = 1024;        // sequences of one launch
+size_t pages_attn_part_rows(int sms);      // rows of partial results that a launch may leave
+
+bool pages_attn_simt_setup();
+cudaError_t launch_pages_attn_join(const PagesAttn &a, int dtype, int ctas, int tile_rows, cudaStream_t s);
+cudaError_t launch_pages_attn_simt(const PagesAttn &a, int dtype, int sms, cudaStream_t s);
+
+}  // namespace msd
+
+struct msd_pages {
+    msd::PagesView v;
+    msd_pages_config cfg;
+    msd::RopeTable rope;
+    int dev, sms;
+    volatile int *status_host;         // page-locked, written by the kernels
+    char *ws;                          // one allocation: what follows
+    int *mark, *flags, *off, *fresh, *plan, *old_table, *rank;
+    float *part_o, *part_ml;
+    int4 *part_item;
+    char err[200];
+};

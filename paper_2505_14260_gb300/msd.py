@@ -76,6 +76,21 @@ class msd_gemm_shape(ctypes.Structure):
                 ("chain", c_int32), ("chunks", c_int32), ("cut_tiles", c_int32)]
 
 
+class msd_pages_config(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("n_layers", c_int32), ("n_heads", c_int32), ("n_kv_heads", c_int32),
+                ("head_dim", c_int32), ("page_size", c_int32), ("n_pages", c_int32), ("max_seqs", c_int32),
+                ("max_pages", c_int32), ("rot_dim", c_int32), ("rot_section", c_int32 * 3),
+                ("rot_interleaved", c_int32), ("rope_base", c_float)]
+
+
+class msd_pages_buffers(ctypes.Structure):
+    _fields_ = [("kv", c_void_p), ("table", c_void_p), ("len", c_void_p), ("refs", c_void_p)]
+
+
+class msd_batch(ctypes.Structure):
+    _fields_ = [("n", c_int32), ("seqs", c_void_p), ("row_start", c_void_p), ("rows", c_int32)]
+
+
 _SIGNATURES = {
     "msd_create": (c_int32, [POINTER(msd_config), POINTER(msd_weights), POINTER(c_void_p)]),
     "msd_destroy": (c_int32, [c_void_p]),
@@ -104,6 +119,20 @@ _SIGNATURES = {
     "msd_profile_slots": (c_int32, [c_void_p, POINTER(msd_kernel_slot), c_int32, POINTER(c_int32)]),
     "msd_state": (c_int32, [c_void_p, POINTER(msd_state_view)]),
     "msd_last_error": (c_char_p, [c_void_p]),
+    "msd_pages_create": (c_int32, [POINTER(msd_pages_config), POINTER(msd_pages_buffers), POINTER(c_void_p)]),
+    "msd_pages_destroy": (c_int32, [c_void_p]),
+    "msd_pages_last_error": (c_char_p, [c_void_p]),
+    "msd_pages_restore": (c_int32, [c_void_p, c_void_p]),
+    "msd_pages_reserve": (c_int32, [c_void_p, POINTER(msd_batch), c_void_p]),
+    "msd_pages_fork": (c_int32, [c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_void_p]),
+    "msd_pages_compact": (c_int32, [c_void_p, POINTER(msd_batch), c_void_p, c_int32, c_void_p, c_void_p]),
+    "msd_pages_free": (c_int32, [c_void_p, c_int32, c_void_p, c_void_p]),
+    "msd_rope_positions": (c_int32, [c_void_p, POINTER(msd_batch), c_void_p, c_void_p, c_void_p, c_void_p,
+                                     c_int64, c_void_p, c_void_p]),
+    "msd_rope_append": (c_int32, [c_void_p, c_int32, POINTER(msd_batch), c_void_p, c_int64, c_void_p, c_int64,
+                                  c_void_p, c_int64, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p]),
+    "msd_pages_attention": (c_int32, [c_void_p, c_int32, POINTER(msd_batch), POINTER(msd_tree), c_int32, c_int32,
+                                      c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p]),
 }
 
 _lib = None
@@ -371,6 +400,164 @@ class Engine:
             eb = int(v.elem_bytes)
             out["target_kv_lo"] = device_view(v.target_kv + v.lo_offset * eb, (c.n_layers, 2, B, nh, S, hd), dt)
             out["draft_kv_lo"] = device_view(v.draft_kv + v.lo_offset * eb, (2, B, nh, S, hd), dt)
+        return out
+
+
+class Batch:
+    """The rows of a call on a Pages pool (msd_batch): int32 device tensors seqs [n] and
+    row_start [n + 1], and the total row count."""
+
+    def __init__(self, seqs: torch.Tensor, row_start: torch.Tensor, rows: int):
+        if row_start.numel() != seqs.numel() + 1:
+            raise ValueError("row_start has one entry more than seqs")
+        self.seqs, self.row_start, self.rows = _ints(seqs), _ints(row_start), int(rows)
+        self._c = msd_batch(seqs.numel(), _ptr(seqs), _ptr(row_start), self.rows)
+
+    def c(self):
+        return ctypes.byref(self._c)
+
+
+def _ints(t: torch.Tensor | None):
+    if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
+        raise ValueError("index arrays are contiguous int32 tensors")
+    return t
+
+
+class Pages:
+    """A pool of K/V pages (msd_pages): many sequences of one model's cache, which share full
+    pages. State lives in the tensors kv [layers, n_pages, 2, kv_heads, page_size, head_dim],
+    table [max_seqs, max_pages], lens [max_seqs] and refs [n_pages], allocated here unless
+    given. A pool made on fresh tensors is empty; on given ones call restore() first."""
+
+    def __init__(self, *, dtype: str, layers: int, heads: int, kv_heads: int, head_dim: int, page_size: int,
+                 n_pages: int, max_seqs: int, max_pages: int, rot_dim: int | None = None, rot_sections=None,
+                 rot_interleaved: bool = False, rope_base: float = 10000.0, kv=None, table=None, lens=None,
+                 refs=None, device="cuda"):
+        rot_dim = head_dim if rot_dim is None else rot_dim
+        sections = (rot_dim // 2, 0, 0) if rot_sections is None else rot_sections
+        self.cfg = msd_pages_config(MSD_BF16 if dtype == "bf16" else MSD_F32, layers, heads, kv_heads, head_dim,
+                                    page_size, n_pages, max_seqs, max_pages, rot_dim, (c_int32 * 3)(*sections),
+                                    int(rot_interleaved), rope_base)
+        self.dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        fresh = lens is None
+        shape = (layers, n_pages, 2, kv_heads, page_size, head_dim)
+        i32 = dict(dtype=torch.int32, device=device)
+        self.kv = torch.empty(shape, dtype=self.dtype, device=device) if kv is None else kv
+        self.table = torch.full((max_seqs, max_pages), -1, **i32) if table is None else table
+        self.lens = torch.zeros(max_seqs, **i32) if lens is None else lens
+        self.refs = torch.zeros(n_pages, **i32) if refs is None else refs
+        if self.kv.dtype != self.dtype or tuple(self.kv.shape) != shape or not self.kv.is_contiguous():
+            raise ValueError(f"kv is a contiguous tensor of shape {shape} in the pool's type")
+        for t, n in ((self.table, max_seqs * max_pages), (self.lens, max_seqs), (self.refs, n_pages)):
+            if _ints(t).numel() != n:
+                raise ValueError("table, lens and refs have an entry per cell, sequence and page")
+        buf = msd_pages_buffers(_ptr(self.kv), _ptr(self.table), _ptr(self.lens), _ptr(self.refs))
+        self.ptr = c_void_p()
+        st = lib().msd_pages_create(ctypes.byref(self.cfg), ctypes.byref(buf), ctypes.byref(self.ptr))
+        if st != MSD_OK:
+            raise MsdError(st, "msd_pages_create", "invalid configuration or allocation failure")
+        if fresh:
+            self.restore()
+
+    def close(self):
+        if getattr(self, "ptr", None) is not None and self.ptr.value:
+            lib().msd_pages_destroy(self.ptr)
+            self.ptr = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check(self, st: int, call: str):
+        if st != MSD_OK:
+            raise MsdError(st, call, lib().msd_pages_last_error(self.ptr).decode())
+
+    def _rows(self, t: torch.Tensor, heads: int, rows: int) -> int:
+        """The row stride of q, k, v or out: [rows, heads, head_dim] or [rows, heads * head_dim]."""
+        width = heads * self.cfg.head_dim
+        if t.shape[0] != rows or t[:1].numel() != width * min(rows, 1) or \
+                (t.dim() == 3 and t.stride(1) != self.cfg.head_dim) or t.stride(-1) != 1 or t.dim() not in (2, 3):
+            raise ValueError(f"expected {rows} rows of {heads} heads of {self.cfg.head_dim} elements, one after another")
+        return t.stride(0) if rows > 1 else width
+
+    def restore(self, stream=None):
+        """Takes lens and table as they are; refs and free pages follow from them."""
+        self._check(lib().msd_pages_restore(self.ptr, _stream(stream)), "msd_pages_restore")
+
+    def reserve(self, batch: Batch, stream=None):
+        """Room for the batch's rows at the end of their sequences."""
+        self._check(lib().msd_pages_reserve(self.ptr, batch.c(), _stream(stream)), "msd_pages_reserve")
+
+    def fork(self, src: torch.Tensor, dst: torch.Tensor, deep: bool = False, stream=None):
+        """Unused sequences dst[i] become copies of src[i]; full pages are shared unless deep."""
+        if src.numel() != dst.numel():
+            raise ValueError("src and dst have one entry per copy")
+        self._check(lib().msd_pages_fork(self.ptr, dst.numel(), _ptr(_ints(src)), _ptr(_ints(dst)), int(deep),
+                                         _stream(stream)), "msd_pages_fork")
+
+    def compact(self, batch: Batch, keep: torch.Tensor | None, n_keep: torch.Tensor, stream=None):
+        """Of the batch's rows keep keep[i, :n_keep[i]] (None: the first n_keep[i])."""
+        n = batch.seqs.numel()
+        if n_keep.numel() != n or (keep is not None and keep.shape[0] != n):
+            raise ValueError("keep and n_keep have an entry per sequence")
+        self._check(lib().msd_pages_compact(self.ptr, batch.c(), _ptr(_ints(keep)),
+                                            0 if keep is None else keep.shape[1], _ptr(_ints(n_keep)),
+                                            _stream(stream)), "msd_pages_compact")
+
+    def free(self, seqs: torch.Tensor, stream=None):
+        self._check(lib().msd_pages_free(self.ptr, seqs.numel(), _ptr(_ints(seqs)), _stream(stream)),
+                    "msd_pages_free")
+
+    def positions(self, batch: Batch, span_start, spans, pos: torch.Tensor, next_pos: torch.Tensor | None = None,
+                  first: torch.Tensor | None = None, stream=None):
+        """pos [3, rows] of interleaved text, images and video (msd_rope_positions)."""
+        if pos.shape[0] != 3 or pos.shape[1] < batch.rows:
+            raise ValueError("pos is [3, rows]")
+        if span_start is not None and (span_start.numel() != batch.seqs.numel() + 1 or spans.shape[-1] != 5):
+            raise ValueError("span_start has an entry per sequence and one more, spans five per span")
+        for t in (next_pos, first):
+            if t is not None and t.numel() != batch.seqs.numel():
+                raise ValueError("next and first have an entry per sequence")
+        self._check(lib().msd_rope_positions(self.ptr, batch.c(), _ptr(_ints(span_start)), _ptr(_ints(spans)),
+                                             _ptr(_ints(first)), _ptr(_ints(pos)), pos.stride(0),
+                                             _ptr(_ints(next_pos)), _stream(stream)), "msd_rope_positions")
+        return pos
+
+    def rope_append(self, layer: int, batch: Batch, q, k, v, pos: torch.Tensor, q_out, stream=None):
+        """Rotated q into q_out, rotated k and v into the rows' slots (msd_rope_append).
+        pos: [3, rows], or [1, rows] where the three axes agree."""
+        c, n = self.cfg, batch.rows
+        if q.dtype != k.dtype or q.dtype != v.dtype or q.dtype not in (torch.float32, torch.bfloat16) or \
+                q_out.dtype != self.dtype:
+            raise ValueError("q, k and v have one type, fp32 or the cache's; q_out the cache's")
+        if pos.dim() != 2 or pos.shape[0] not in (1, 3) or pos.shape[1] < n:
+            raise ValueError("pos is [3, rows] or [1, rows]")
+        st = lib().msd_rope_append(
+            self.ptr, layer, batch.c(), _ptr(q), self._rows(q, c.n_heads, n), _ptr(k),
+            self._rows(k, c.n_kv_heads, n), _ptr(v), self._rows(v, c.n_kv_heads, n),
+            MSD_F32 if q.dtype == torch.float32 else MSD_BF16, _ptr(_ints(pos)),
+            pos.stride(0) if pos.shape[0] == 3 else 0, _ptr(q_out), self._rows(q_out, c.n_heads, n), _stream(stream))
+        self._check(st, "msd_rope_append")
+        return q_out
+
+    def attention(self, layer: int, batch: Batch, q, out, lse: torch.Tensor | None = None, tree: Tree | None = None,
+                  window: int = 0, sinks: int = 0, stream=None):
+        """The batch's rows over their sequences' pages (msd_pages_attention). lse: fp32
+        [rows, heads]; tree: one per listed sequence, its rows the tree's nodes."""
+        c, n = self.cfg, batch.rows
+        if q.dtype != self.dtype or out.dtype != self.dtype:
+            raise ValueError("q and out have the cache's type")
+        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() != n * c.n_heads):
+            raise ValueError("lse is a contiguous fp32 tensor [rows, heads]")
+        if tree is not None and tree.B != batch.seqs.numel():
+            raise ValueError("a tree per listed sequence")
+        t = None if tree is None else ctypes.byref(tree.c())
+        st = lib().msd_pages_attention(self.ptr, layer, batch.c(), t, 0 if tree is None else tree.N, window, sinks,
+                                       _ptr(q), self._rows(q, c.n_heads, n), _ptr(out),
+                                       self._rows(out, c.n_heads, n), _ptr(lse), _stream(stream))
+        self._check(st, "msd_pages_attention")
         return out
 
 
