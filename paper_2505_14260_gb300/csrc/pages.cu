@@ -807,7 +807,7 @@ msd_status msd_pages_create(const msd_pages_config *cfg, const msd_pages_buffers
     ok = ok && cudaHostAlloc(&host, 64, cudaHostAllocMapped) == cudaSuccess;
     p->status_host = static_cast<volatile int *>(host);
     ok = ok && cudaHostGetDevicePointer(&mapped, host, 0) == cudaSuccess;
-    ok = ok && pages_attn_simt_setup();
+    ok = ok && pages_attn_simt_setup() && pages_attn_tc_setup();
     if (!ok) {
         cudaGetLastError();
         msd_pages_destroy(p);
@@ -827,6 +827,10 @@ msd_status msd_pages_create(const msd_pages_config *cfg, const msd_pages_buffers
     p->part_o = reinterpret_cast<float *>(p->ws + o_po);
     p->part_ml = reinterpret_cast<float *>(p->ws + o_pml);
     p->part_item = reinterpret_cast<int4 *>(p->ws + o_item);
+    if (cfg->dtype == MSD_BF16 && !pages_attn_map(p->v, &p->map)) {
+        msd_pages_destroy(p);
+        return MSD_ERR_CUDA;
+    }
     *out = p;
     return MSD_OK;
 }
@@ -1005,7 +1009,9 @@ msd_status msd_pages_attention(msd_pages *p, int32_t layer, const msd_batch *bat
     a.part_o = p->part_o;
     a.part_ml = p->part_ml;
     a.part_item = p->part_item;
-    return leave(p, launch_pages_attn_simt(a, c.dtype, p->sms, static_cast<cudaStream_t>(stream)));
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return leave(p, c.dtype == MSD_BF16 ? launch_pages_attn_tc(p->map, a, p->sms, s)
+                                        : launch_pages_attn_simt(a, p->sms, s));
 }
 
 }  // extern "C"

@@ -85,14 +85,18 @@ constexpr int ATTN_MAX_SEQS = 1024;        // sequences of one launch
 size_t pages_attn_part_rows(int sms);      // rows of partial results that a launch may leave
 
 bool pages_attn_simt_setup();
+bool pages_attn_tc_setup();
+bool pages_attn_map(const PagesView &v, CUtensorMap *map);
+cudaError_t launch_pages_attn_tc(const CUtensorMap &map, const PagesAttn &a, int sms, cudaStream_t s);
 cudaError_t launch_pages_attn_join(const PagesAttn &a, int dtype, int ctas, int tile_rows, cudaStream_t s);
-cudaError_t launch_pages_attn_simt(const PagesAttn &a, int dtype, int sms, cudaStream_t s);
+cudaError_t launch_pages_attn_simt(const PagesAttn &a, int sms, cudaStream_t s);
 
 }  // namespace msd
 
 struct msd_pages {
     msd::PagesView v;
     msd_pages_config cfg;
+    CUtensorMap map;                   // bf16 pools
     msd::RopeTable rope;
     int dev, sms;
     volatile int *status_host;         // page-locked, written by the kernels

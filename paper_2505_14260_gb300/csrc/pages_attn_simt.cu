@@ -1,4 +1,4 @@
-// Attention over pages on CUDA cores, and the launch that joins partial results.
+// Attention over pages on CUDA cores (fp32 pools), and the launch that joins partial results.
 //
 // A CTA takes 64 packed rows (pages_attn.cuh) against key tiles of 64: scores as register
 // tiles of 4 x 4, an online softmax in base 2 over the 16 threads that share a row, O in
@@ -27,13 +27,7 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 
-template <typename T>
-__device__ __forceinline__ void store4(T *g, float4 v) {
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(g) = v;
-    else Split<bf16>::store4(g, 0, v);
-}
-
-template <typename T, int HD>
+template <int HD>
 __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAttn a) {
     using L = Lay<HD>;
     extern __shared__ __align__(16) float sm[];
@@ -45,7 +39,7 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
     const PagesView &v = a.pv;
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, G = v.heads / v.kv_heads;
     if (tid == 0) name_parts<ROWS, KT>(a, sched, blockIdx.x);
-    const T *kv = static_cast<const T *>(v.kv) + (long)a.layer * v.n_pages * v.page_elems();
+    const float *kv = static_cast<const float *>(v.kv) + (long)a.layer * v.n_pages * v.page_elems();
     AttnWalk<ROWS, KT> walk(a, sched);
     Segment g;
     while (walk.next(g)) {
@@ -58,7 +52,8 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
             const int m = e / (HD / 4), c = (e - m * (HD / 4)) * 4, r = (m0 + m) / G;
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
             if (m < nm)
-                x = Vec4<T>::load(static_cast<const T *>(a.q) + (start + r) * a.ldq + (long)(g.h * G + (m0 + m) % G) * HD + c);
+                x = *reinterpret_cast<const float4 *>(static_cast<const float *>(a.q) + (start + r) * a.ldq +
+                                                     (long)(g.h * G + (m0 + m) % G) * HD + c);
             *reinterpret_cast<float4 *>(sQ + m * L::LD + c) = x;
         }
         // this thread's four rows
@@ -92,9 +87,9 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
                 if (slot < len) {
                     const int id = table[slot >> v.page_shift];
                     if ((unsigned)id < (unsigned)v.n_pages) {
-                        const T *src = kv + id * v.page_elems() + ((long)g.h * v.page + (slot & (v.page - 1))) * HD + c;
-                        x = Vec4<T>::load(src);
-                        y = Vec4<T>::load(src + (long)v.kv_heads * v.page * HD);
+                        const float *src = kv + id * v.page_elems() + ((long)g.h * v.page + (slot & (v.page - 1))) * HD + c;
+                        x = *reinterpret_cast<const float4 *>(src);
+                        y = *reinterpret_cast<const float4 *>(src + (long)v.kv_heads * v.page * HD);
                     }
                 }
                 odd |= !(isfinite(y.x) && isfinite(y.y) && isfinite(y.z) && isfinite(y.w));
@@ -194,11 +189,11 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
             if (whole) {
                 // (a sum that is not a number is kept; only an empty row divides by nothing)
                 const float inv = sum[x] == 0.f ? 0.f : 1.f / sum[x];
-                T *out = static_cast<T *>(a.out) + r * a.ldo + (long)head * HD;
+                float *out = static_cast<float *>(a.out) + r * a.ldo + (long)head * HD;
 #pragma unroll
                 for (int c = 0; c < HD / 64; ++c)
-                    store4(out + 64 * c + 4 * tx, make_float4(acc[x][4 * c] * inv, acc[x][4 * c + 1] * inv,
-                                                              acc[x][4 * c + 2] * inv, acc[x][4 * c + 3] * inv));
+                    *reinterpret_cast<float4 *>(out + 64 * c + 4 * tx) =
+                        make_float4(acc[x][4 * c] * inv, acc[x][4 * c + 1] * inv, acc[x][4 * c + 2] * inv, acc[x][4 * c + 3] * inv);
                 if (a.lse && tx == 0)
                     a.lse[(long)r * v.heads + head] = sum[x] == 0.f ? -INFINITY : (mx[x] + log2f(sum[x])) * 0.6931471805599453f;
             } else {
@@ -258,12 +253,12 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) pages_attn_join_kernel(const 
         a.lse[(long)r * v.heads + head] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.6931471805599453f;
 }
 
-template <typename T, int HD>
+template <int HD>
 cudaError_t launch(const PagesAttn &a, int sms, cudaStream_t s) {
     const int ctas = sms * (HD == 64 ? 2 : 1);
-    cudaError_t e = launch_chain(pages_attn_simt_kernel<T, HD>, dim3(ctas), dim3(THREADS), Lay<HD>::SMEM, s, a);
+    cudaError_t e = launch_chain(pages_attn_simt_kernel<HD>, dim3(ctas), dim3(THREADS), Lay<HD>::SMEM, s, a);
     note_launch();
-    return e != cudaSuccess ? e : launch_pages_attn_join(a, sizeof(T) == 4 ? MSD_F32 : MSD_BF16, ctas, ROWS, s);
+    return e != cudaSuccess ? e : launch_pages_attn_join(a, MSD_F32, ctas, ROWS, s);
 }
 
 }  // namespace
@@ -287,15 +282,12 @@ bool pages_attn_simt_setup() {
     auto set = [](const void *f, int bytes) {
         return cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
     };
-    return set((const void *)pages_attn_simt_kernel<float, 64>, Lay<64>::SMEM) &&
-           set((const void *)pages_attn_simt_kernel<float, 128>, Lay<128>::SMEM) &&
-           set((const void *)pages_attn_simt_kernel<bf16, 64>, Lay<64>::SMEM) &&
-           set((const void *)pages_attn_simt_kernel<bf16, 128>, Lay<128>::SMEM);
+    return set((const void *)pages_attn_simt_kernel<64>, Lay<64>::SMEM) &&
+           set((const void *)pages_attn_simt_kernel<128>, Lay<128>::SMEM);
 }
 
-cudaError_t launch_pages_attn_simt(const PagesAttn &a, int dtype, int sms, cudaStream_t s) {
-    if (dtype == MSD_F32) return a.pv.head_dim == 64 ? launch<float, 64>(a, sms, s) : launch<float, 128>(a, sms, s);
-    return a.pv.head_dim == 64 ? launch<bf16, 64>(a, sms, s) : launch<bf16, 128>(a, sms, s);
+cudaError_t launch_pages_attn_simt(const PagesAttn &a, int sms, cudaStream_t s) {
+    return a.pv.head_dim == 64 ? launch<64>(a, sms, s) : launch<128>(a, sms, s);
 }
 
 }  // namespace msd

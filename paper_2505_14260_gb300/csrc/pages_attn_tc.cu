@@ -1,0 +1,793 @@
+// Attention over pages on the 5th-generation tensor cores (bf16 pools).
+//
+// O = softmax(Q K^T) V over tiles of 128 packed rows and 128 keys (pages_attn.cuh: what an item
+// is and how its steps are cut into CTAs). S = Q K^T reads both operands from shared memory;
+// P goes back over S in tensor memory as the A operand of O += P V. A CTA keeps two softmax
+// groups of four warps at work, so that one's S and P V run while the other takes exponentials:
+//   two tiles of rows over the same keys (PAIR), where sequences have many packed rows
+//   (each key tile is read once for 256 rows: the tensor cores bound it), or
+//   one tile of rows over alternate key tiles, each group with a maximum, sum and O of its own,
+//   joined at the end (bytes bound it: what counts is that the copies never pause).
+// Roles (320 threads):
+//   warps 0-7   softmax groups 0 and 1, a row a thread: load the query rows into shared memory
+//               (swizzled as the MMA reads them), then per key tile read S, hide what the row
+//               does not see, online softmax in base 2, P as bf16 over S; at an item's end O
+//   warp 8      TMA: a key tile is one box a page and 64 columns, K and V in slots of their own
+//   warp 9      tensor memory and the MMAs
+// P is rounded to bf16 (the V operand's type; the row's sum takes the weights unrounded): with
+// the result's own rounding that is 2^-9 a value twice, not once. Maxima, sums, S and O are
+// fp32. A row's reference maximum moves (and O is rescaled) only when a tile's exceeds it by
+// more than 2^8, so P <= 256.
+//
+// Hidden keys: S is replaced before it is used, so what K holds there does not matter. V does,
+// because 0 * NaN is a NaN: in a tile that some row does not see in full, the group looks
+// through V in shared memory before P V, zeroes slots past the sequence's end, and zeroes values
+// that are not finite after noting so; the item's end then adds those that a row does see.
+#include <cstring>
+
+#include "pages_attn.cuh"
+
+namespace msd {
+namespace {
+
+constexpr int KT = 128, THREADS = 320, TILE = 128;
+constexpr unsigned long long TIMEOUT_NS = 2000000000ull;
+constexpr float RESCALE_LOG2 = 8.f;
+
+template <int HD>
+struct Lay {
+    static constexpr int NB = HD / 64;                          // 64-column boxes of a row
+    static constexpr uint32_t BOX = TILE * 128;                 // [128 rows][64 bf16]
+    static constexpr uint32_t MAT = NB * BOX;                   // a Q, K or V tile
+    static constexpr int SLOTS = HD == 128 ? 4 : 9;
+    static constexpr uint32_t Q = 0, RING = 2 * MAT, SCHED = RING + SLOTS * MAT;
+    static constexpr uint32_t ML = SCHED + (sizeof(AttnSched) + 15) / 16 * 16;      // [2][128] float2
+    static constexpr uint32_t BYTES = ML + 2 * TILE * 8;
+    static constexpr uint32_t SMEM = BYTES + 1024;
+    // tensor memory: two S (P over its first half), two O
+    static constexpr uint32_t T_S = 0, T_O = 2 * KT, T_COLS = 512;
+    static_assert(SMEM >= tmem_smem_floor((int)T_COLS) && SMEM <= 227 * 1024, "one CTA an SM, by its tensor memory");
+};
+
+__device__ __forceinline__ uint32_t su32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ unsigned long long gtime() {
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "selp.b32 %0, 1, 0, p;\n}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+// Bounded wait: gives up when *abort is set, or after the limit (then sets it, and the status).
+__device__ __noinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, volatile int *abort, int *status) {
+    const unsigned long long t0 = gtime();
+    while (!bar_try(bar, parity)) {
+        if (*abort) return false;
+        if (gtime() - t0 > TIMEOUT_NS) {
+            *abort = 1;
+            set_status(status, ST_TIMEOUT);
+            return false;
+        }
+    }
+    return true;
+}
+// The whole warp waits; the answer is uniform.
+__device__ __forceinline__ bool w_wait(uint32_t bar, uint32_t parity, volatile int *abort, int *status) {
+    if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
+    return __all_sync(0xffffffffu, bar_wait_slow(bar, parity, abort, status));
+}
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// Shared-memory matrix descriptor (128-byte swizzle): start address, leading byte offset (MN-major: between
+// 64-element atoms along N) and stride byte offset (between 8-row groups).
+__device__ __forceinline__ uint64_t sdesc(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)((lbo >> 4) & 0x3FFFu) << 16) |
+           ((uint64_t)((sbo >> 4) & 0x3FFFu) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+// Instruction descriptor, kind::f16: fp32 accumulate, bf16 A (K-major) and B (K-major, or MN-major: b_mn).
+__device__ __forceinline__ uint32_t idesc(int M, int N, int b_mn) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)b_mn << 16) | ((uint32_t)(N >> 3) << 17) |
+           ((uint32_t)(M >> 4) << 24);
+}
+// Issue loops run in whole warps; the lane that elect_one() names issues.
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t on;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.b32 %0, 1, 0, p;\n}" : "=r"(on));
+    return on;
+}
+__device__ __forceinline__ void w_expect_tx(uint32_t on, uint32_t bar, uint32_t bytes) {
+    asm volatile(
+        "{\n.reg .pred q;\nsetp.ne.b32 q, %2, 0;\n"
+        "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n}" ::"r"(bar),
+        "r"(bytes), "r"(on)
+        : "memory");
+}
+__device__ __forceinline__ void w_tma2d(uint32_t on, uint32_t dst, const CUtensorMap *m, int x, int y, uint32_t bar) {
+    asm volatile(
+        "{\n.reg .pred q;\nsetp.ne.b32 q, %5, 0;\n"
+        "@q cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3}], [%4];\n}" ::"r"(dst),
+        "l"(m), "r"(x), "r"(y), "r"(bar), "r"(on)
+        : "memory");
+}
+// D (+)= A B^T, both from shared memory / A from tensor memory
+__device__ __forceinline__ void w_mma_ss(uint32_t on, uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t acc) {
+    asm volatile(
+        "{\n.reg .pred p, q;\nsetp.ne.b32 q, %5, 0;\nsetp.ne.b32 p, %4, 0;\n"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+        "l"(a), "l"(b), "r"(id), "r"(acc), "r"(on));
+}
+__device__ __forceinline__ void w_mma_ts(uint32_t on, uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t acc) {
+    asm volatile(
+        "{\n.reg .pred p, q;\nsetp.ne.b32 q, %5, 0;\nsetp.ne.b32 p, %4, 0;\n"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
+        "r"(a), "l"(b), "r"(id), "r"(acc), "r"(on));
+}
+__device__ __forceinline__ void w_commit(uint32_t on, uint32_t bar) {
+    asm volatile(
+        "{\n.reg .pred q;\nsetp.ne.b32 q, %1, 0;\n"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar), "r"(on)
+        : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ float ex2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Both softmax groups (256 threads).
+__device__ __forceinline__ void groups_sync() {
+    __syncwarp();
+    fence_before();
+    asm volatile("barrier.sync.aligned 1, 256;" ::: "memory");
+    fence_after();
+}
+
+// 128 (or 32) columns of this warp's 32 lanes, waited for in the same statement: the registers
+// are defined once the data has landed.
+__device__ __forceinline__ void tmem_ld128(uint32_t taddr, uint32_t *r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x128.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%"
+        "27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%"
+        "52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63,%64,%65,%66,%67,%68,%69,%70,%71,%72,%73,%74,%75,%76,%"
+        "77,%78,%79,%80,%81,%82,%83,%84,%85,%86,%87,%88,%89,%90,%91,%92,%93,%94,%95,%96,%97,%98,%99,%100,%101"
+        ",%102,%103,%104,%105,%106,%107,%108,%109,%110,%111,%112,%113,%114,%115,%116,%117,%118,%119,%120,%121"
+        ",%122,%123,%124,%125,%126,%127}, [%128];"
+        "\ntcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]),
+          "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]),
+          "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]),
+          "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]),
+          "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63]), "=r"(r[64]),
+          "=r"(r[65]), "=r"(r[66]), "=r"(r[67]), "=r"(r[68]), "=r"(r[69]), "=r"(r[70]), "=r"(r[71]), "=r"(r[72]),
+          "=r"(r[73]), "=r"(r[74]), "=r"(r[75]), "=r"(r[76]), "=r"(r[77]), "=r"(r[78]), "=r"(r[79]), "=r"(r[80]),
+          "=r"(r[81]), "=r"(r[82]), "=r"(r[83]), "=r"(r[84]), "=r"(r[85]), "=r"(r[86]), "=r"(r[87]), "=r"(r[88]),
+          "=r"(r[89]), "=r"(r[90]), "=r"(r[91]), "=r"(r[92]), "=r"(r[93]), "=r"(r[94]), "=r"(r[95]), "=r"(r[96]),
+          "=r"(r[97]), "=r"(r[98]), "=r"(r[99]), "=r"(r[100]), "=r"(r[101]), "=r"(r[102]), "=r"(r[103]), "=r"(r[104]),
+          "=r"(r[105]), "=r"(r[106]), "=r"(r[107]), "=r"(r[108]), "=r"(r[109]), "=r"(r[110]), "=r"(r[111]),
+          "=r"(r[112]), "=r"(r[113]), "=r"(r[114]), "=r"(r[115]), "=r"(r[116]), "=r"(r[117]), "=r"(r[118]),
+          "=r"(r[119]), "=r"(r[120]), "=r"(r[121]), "=r"(r[122]), "=r"(r[123]), "=r"(r[124]), "=r"(r[125]),
+          "=r"(r[126]), "=r"(r[127])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t *r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%"
+        "27,%28,%29,%30,%31}, [%32];"
+        "\ntcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t *r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,"
+        "%28,%29,%30,%31,%32};"
+        "\ntcgen05.wait::st.sync.aligned;" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+
+// bits [a, b) of the 32 keys from `key` on
+__device__ __forceinline__ uint32_t range_bits(int a, int b, int key) {
+    const int lo = min(max(a - key, 0), 32), hi = min(max(b - key, 0), 32);
+    const uint32_t below_hi = hi == 32 ? 0xffffffffu : (1u << hi) - 1u, below_lo = lo == 32 ? 0xffffffffu : (1u << lo) - 1u;
+    return below_hi & ~below_lo;
+}
+// 32 mask bits from bit `at` on (at > -32)
+__device__ __forceinline__ uint32_t mask_bits(const uint64_t *m, int words, int at) {
+    if (at < 0) return words > 0 ? (uint32_t)m[0] << -at : 0u;
+    const int w = at >> 6, o = at & 63;
+    uint64_t x = w < words ? m[w] >> o : 0ull;
+    if (o > 32 && w + 1 < words) x |= m[w + 1] << (64 - o);
+    return (uint32_t)x;
+}
+
+// What a group knows of the segment's rows, and a thread of its own.
+struct Rows {
+    int len, base, rows, live;        // sequence length, tokens before the rows, rows, rows that exist in its tree
+    int r_first, r_last;              // the group's rows
+    int r, place, seq_i;              // the thread's row (-1: none) and its place
+    const uint64_t *mrow;
+};
+
+// Whether every row of [r_first, r_last] that sees anything sees every key of the tile.
+__device__ __forceinline__ bool tile_full(const PagesAttn &a, const Rows &x, int key0) {
+    const int end = key0 + KT;
+    if (end > x.base + (a.mask ? 0 : x.r_first + 1)) return false;
+    if (!a.window || end <= a.sinks) return true;
+    return x.base + (a.mask ? a.nodes : x.r_last) - key0 < a.window;
+}
+
+// The keys of a tile that the thread's row sees.
+__device__ __forceinline__ void seen_bits(const PagesAttn &a, const Rows &x, int key0, uint32_t *w) {
+    if (x.r < 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = 0;
+        return;
+    }
+    const int hi = a.mask ? x.base : x.base + x.r + 1, lo = a.window ? x.place - a.window + 1 : 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int key = key0 + 32 * i;
+        w[i] = range_bits(lo, hi, key) | range_bits(0, min(a.sinks, hi), key);
+        if (a.mask && key + 32 > x.base && key < x.len) {
+            uint32_t m = mask_bits(x.mrow, a.words, key - x.base) & range_bits(x.base, x.len, key);
+            if (a.window && x.place - x.base >= a.window) {       // (else all depths up to its own are inside)
+                for (uint32_t left = m; left; left &= left - 1) {
+                    const int bit = __ffs(left) - 1;
+                    const int at = x.base + a.depth[(long)x.seq_i * a.nodes + key + bit - x.base];
+                    if (x.place - at >= a.window && at >= a.sinks) m &= ~(1u << bit);
+                }
+            }
+            w[i] |= m;
+        }
+    }
+}
+
+// Where the ring holds a segment's tiles: K tiles run `lead` ahead of V tiles.
+struct Ring {
+    int base, n, lead;
+    __device__ int k(int t) const { return t < lead ? base + t : base + lead + 2 * (t - lead) + 1; }
+    __device__ int v(int t) const { return base + lead + t + min(t, n - lead); }
+};
+
+template <int HD, bool PAIR>
+__global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_constant__ CUtensorMap map, const PagesAttn a) {
+    using L = Lay<HD>;
+    constexpr int ROWS = PAIR ? 2 * TILE : TILE, LEAD = PAIR ? 1 : 2, SLOTS = L::SLOTS;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * SLOTS + 9];
+    __shared__ uint32_t s_tmem;
+    __shared__ unsigned s_odd;            // bit i % 32: segment i had values of V that are not finite zeroed
+    __shared__ volatile int s_abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t raw = su32(smem_raw), base = (raw + 1023u) & ~1023u;
+    uint8_t *sm = smem_raw + (base - raw);
+    AttnSched &sched = *reinterpret_cast<AttnSched *>(sm + L::SCHED);
+    float2 *s_ml = reinterpret_cast<float2 *>(sm + L::ML);
+    const uint32_t full0 = su32(bars), empty0 = full0 + 8 * SLOTS, s_full0 = empty0 + 8 * SLOTS, p_full0 = s_full0 + 16,
+                   o_full0 = p_full0 + 16, q_full0 = o_full0 + 16, drain = q_full0 + 16;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < SLOTS; ++i) {
+            bar_init(full0 + 8 * i, 1);
+            bar_init(empty0 + 8 * i, 1);
+        }
+        for (int x = 0; x < 2; ++x) {
+            bar_init(s_full0 + 8 * x, 1);
+            bar_init(p_full0 + 8 * x, 128);
+            bar_init(o_full0 + 8 * x, 1);
+            bar_init(q_full0 + 8 * x, PAIR ? 128 : 256);
+        }
+        bar_init(drain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        s_odd = 0;
+        s_abort = 0;
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(su32(&s_tmem)),
+                     "r"(L::T_COLS)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    wait_prior();
+    allow_dependents();
+    attn_schedule<ROWS, KT, THREADS>(a, sched, blockIdx.x, gridDim.x);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = s_tmem;
+    const PagesView &v = a.pv;
+    const int G = v.heads / v.kv_heads;
+    int *status = v.status;
+    if (threadIdx.x == 0) name_parts<ROWS, KT>(a, sched, blockIdx.x);
+    AttnWalk<ROWS, KT> walk(a, sched);
+    Segment g;
+    // steps of a segment for group x: in a pair the first tile's rows may end before the last key tiles
+    auto steps = [&](const Segment &s, int x) {
+        const int n = s.j1 - s.j0;
+        if (!PAIR) return (n + 1 - x) / 2;
+        const int left = sched.rows[s.i] * G - s.tile * ROWS;
+        if (left <= TILE) return x ? 0 : n;
+        if (x || a.mask) return n;
+        const int hi = sched.len[s.i] - sched.rows[s.i] + (s.tile * ROWS + TILE - 1) / G + 1;
+        return min(n, max(0, s.range.sink_tiles + (hi + KT - 1) / KT - s.range.lo - s.j0));
+    };
+    auto key_of = [](const Segment &s, int t) {
+        const int j = s.j0 + t;
+        return (j < s.range.sink_tiles ? j : s.range.lo + j - s.range.sink_tiles) * KT;
+    };
+
+    if (warp == 8) {
+        // ---- TMA -----------------------------------------------------------
+        const uint32_t on = elect_one();
+        int pos = 0;
+        bool ok = true;
+        const int per = KT >> v.page_shift;
+        auto load = [&](int key0, int what, const int *table, int len, int h) {
+            const int slot = pos % SLOTS;
+            if (!w_wait(empty0 + 8 * slot, (uint32_t)(pos / SLOTS + 1) & 1u, &s_abort, status)) return false;
+            ++pos;
+            const int first = key0 >> v.page_shift, n = min(per, ((len - 1) >> v.page_shift) - first + 1);
+            int id = lane < n ? table[first + lane] : 0;
+            if ((unsigned)id >= (unsigned)v.n_pages) {
+                id = 0;
+                set_status(status, ST_RANGE);
+            }
+            const uint32_t bar = full0 + 8 * slot, dst = base + L::RING + slot * L::MAT;
+            w_expect_tx(on, bar, (uint32_t)n * v.page * HD * 2);
+            for (int i = 0; i < n; ++i) {
+                const int y = (((a.layer * v.n_pages + __shfl_sync(0xffffffffu, id, i)) * 2 + what) * v.kv_heads + h) * v.page;
+#pragma unroll
+                for (int b = 0; b < L::NB; ++b)
+                    w_tma2d(on, dst + b * L::BOX + i * v.page * 128, &map, 64 * b, y, bar);
+            }
+            return true;
+        };
+        while (ok && walk.next(g)) {
+            const int n = g.j1 - g.j0, len = sched.len[g.i];
+            const int *table = v.table + (long)sched.seq[g.i] * v.max_pages;
+            const int lead = min(LEAD, n);
+            for (int t = 0; ok && t < lead; ++t) ok = load(key_of(g, t), 0, table, len, g.h);
+            for (int t = 0; ok && t < n; ++t) {
+                ok = load(key_of(g, t), 1, table, len, g.h);
+                if (ok && t + lead < n) ok = load(key_of(g, t + lead), 0, table, len, g.h);
+            }
+        }
+        if (s_abort) {            // the copies still in flight land before the CTA exits
+            volatile int never = 0;
+            for (int p = max(0, pos - SLOTS); p < pos; ++p)
+                bar_wait_slow(full0 + 8 * (p % SLOTS), (uint32_t)(p / SLOTS) & 1u, &never, status);
+        }
+        __syncwarp();
+    } else if (warp == 9) {
+        // ---- MMA -----------------------------------------------------------
+        const uint32_t on = elect_one();
+        const uint32_t id_s = idesc(TILE, KT, 0), id_o = idesc(TILE, HD, 1);
+        int ring = 0, seg = 0;
+        uint32_t p_ph[2] = {0, 0}, q_ph[2] = {0, 0};
+        bool ok = true;
+        auto wait_slot = [&](int pos) {
+            const bool r = w_wait(full0 + 8 * (pos % SLOTS), (uint32_t)(pos / SLOTS) & 1u, &s_abort, status);
+            fence_after();
+            return r;
+        };
+        auto s_mma = [&](int x, int pos, int qbuf) {
+            const uint32_t k = base + L::RING + (pos % SLOTS) * L::MAT, q = base + L::Q + qbuf * L::MAT;
+#pragma unroll
+            for (int kk = 0; kk < HD / 16; ++kk) {
+                const uint32_t o = (kk >> 2) * L::BOX + (kk & 3) * 32;
+                w_mma_ss(on, tmem + L::T_S + x * KT, sdesc(q + o, 16, 1024), sdesc(k + o, 16, 1024), id_s, kk > 0);
+            }
+            w_commit(on, s_full0 + 8 * x);
+        };
+        auto o_mma = [&](int x, int pos, bool acc) {
+            const uint32_t w = base + L::RING + (pos % SLOTS) * L::MAT;
+#pragma unroll
+            for (int kk = 0; kk < KT / 16; ++kk)
+                w_mma_ts(on, tmem + L::T_O + x * HD, tmem + L::T_S + x * KT + kk * 8, sdesc(w + kk * 2048, L::BOX, 1024), id_o,
+                         kk > 0 || acc);
+        };
+        auto free_slot = [&](int pos) { w_commit(on, empty0 + 8 * (pos % SLOTS)); };
+        auto wait_p = [&](int x) {
+            const bool r = w_wait(p_full0 + 8 * x, p_ph[x], &s_abort, status);
+            p_ph[x] ^= 1u;
+            fence_after();
+            return r;
+        };
+        auto wait_q = [&](int x) {
+            const bool r = w_wait(q_full0 + 8 * x, q_ph[x], &s_abort, status);
+            q_ph[x] ^= 1u;
+            fence_after();
+            return r;
+        };
+        while (ok && walk.next(g)) {
+            const int n = g.j1 - g.j0;
+            const Ring at{ring, n, min(LEAD, n)};
+            if constexpr (PAIR) {
+                const int nx[2] = {steps(g, 0), steps(g, 1)};
+                const int last = nx[1] > 0;
+                for (int t = -1; ok && t < n; ++t) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if (!ok) break;
+                        if (t >= 0 && t < nx[x]) {
+                            ok = wait_p(x) && wait_slot(at.v(t));
+                            if (!ok) break;
+                            o_mma(x, at.v(t), t > 0);
+                            if (x == last) free_slot(at.v(t));
+                            if (t == nx[x] - 1) w_commit(on, o_full0 + 8 * x);
+                        }
+                        if (t + 1 < nx[x]) {
+                            if (t < 0) ok = wait_q(x);
+                            ok = ok && wait_slot(at.k(t + 1));
+                            if (!ok) break;
+                            s_mma(x, at.k(t + 1), x);
+                            if (x == last) free_slot(at.k(t + 1));
+                        }
+                    }
+                }
+            } else {
+                ok = wait_q(0);
+                for (int t = -2; ok && t < n; ++t) {
+                    const int x = t & 1;
+                    if (t >= 0) {
+                        ok = wait_p(x) && wait_slot(at.v(t));
+                        if (!ok) break;
+                        o_mma(x, at.v(t), t > 1);
+                        free_slot(at.v(t));
+                        if (t + 2 >= n) w_commit(on, o_full0 + 8 * x);
+                    }
+                    if (t + 2 < n) {
+                        ok = wait_slot(at.k(t + 2));
+                        if (!ok) break;
+                        s_mma(x, at.k(t + 2), seg & 1);
+                        free_slot(at.k(t + 2));
+                    }
+                }
+            }
+            ring += 2 * n;
+            ++seg;
+        }
+        if (seg > 0 || !ok) {     // no MMA outlives the CTA's tensor memory
+            w_commit(on, drain);
+            volatile int never = 0;
+            bar_wait_slow(drain, 0, &never, status);
+        }
+        __syncwarp();
+    } else {
+        // ---- softmax -------------------------------------------------------
+        const int x = warp >> 2, m = threadIdx.x & 127;
+        const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
+        const uint32_t t_s = lanes + L::T_S + x * KT, t_o = lanes + L::T_O;
+        uint32_t s_ph = 0, o_ph[2] = {0, 0};
+        int ring = 0, seg = 0;
+        bool dead = false;
+        // the query rows of a segment into its buffer: a pair's groups load their own tile, else each half the columns
+        auto load_q = [&](const Segment &s, int index) {
+            const int pm = s.tile * ROWS + (PAIR ? x * TILE : 0) + m;
+            constexpr int N = PAIR ? HD / 8 : HD / 16;                // 16-byte pieces
+            const int c0 = PAIR ? 0 : x * N;
+            uint4 q[N];
+            if (pm < sched.rows[s.i] * G) {
+                const int r = pm / G;
+                const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const bf16 *>(a.q) + (sched.start[s.i] + r) * a.ldq +
+                                                                   (long)(s.h * G + pm - r * G) * HD) + c0;
+#pragma unroll
+                for (int i = 0; i < N; ++i) q[i] = src[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) q[i] = make_uint4(0, 0, 0, 0);
+            }
+            uint8_t *dst = sm + L::Q + (PAIR ? x : index & 1) * L::MAT + m * 128;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int c = c0 + i;
+                *reinterpret_cast<uint4 *>(dst + (c >> 3) * L::BOX + (((c & 7) ^ (m & 7)) << 4)) = q[i];
+            }
+            fence_proxy();
+            bar_arrive(q_full0 + (PAIR ? 8 * x : 0));
+        };
+        bool have = walk.next(g);
+        if (have && steps(g, PAIR ? x : 0) > 0) load_q(g, 0);
+        while (have) {
+            const int n = g.j1 - g.j0, nx = steps(g, x), n_other = steps(g, x ^ 1);
+            const Ring at{ring, n, min(LEAD, n)};
+            const int pm0 = g.tile * ROWS + (PAIR ? x * TILE : 0), pm = pm0 + m;
+            Rows rw;
+            rw.len = sched.len[g.i];
+            rw.rows = sched.rows[g.i];
+            rw.base = rw.len - rw.rows;
+            rw.live = a.mask && a.n_nodes ? min(rw.rows, a.n_nodes[g.i]) : rw.rows;
+            rw.r_first = pm0 / G;
+            rw.r_last = (min(pm0 + TILE, rw.rows * G) - 1) / G;
+            const bool valid = pm < rw.rows * G;
+            const int r = pm / G;
+            rw.r = valid && r < rw.live ? r : -1;
+            rw.seq_i = g.i;
+            rw.place = rw.base + r;
+            rw.mrow = nullptr;
+            if (a.mask && rw.r >= 0) {
+                rw.mrow = a.mask + ((long)g.i * a.nodes + r) * a.words;
+                rw.place = rw.base + (a.window ? a.depth[(long)g.i * a.nodes + r] : 0);
+            }
+            const bool any = __any_sync(0xffffffffu, rw.r >= 0), blind = __any_sync(0xffffffffu, valid && rw.r < 0);
+            float m_ref = -INFINITY, sum = 0.f;
+            for (int t = 0; t < nx; ++t) {
+                const int tt = PAIR ? t : 2 * t + x, key0 = key_of(g, tt);
+                if (!dead && !w_wait(s_full0 + 8 * x, s_ph, &s_abort, status)) dead = true;
+                s_ph ^= 1u;
+                fence_after();
+                const bool full = tile_full(a, rw, key0);
+                if (any) {
+                    uint32_t s[128];
+                    tmem_ld128(t_s, s);
+                    if (!full || blind) {
+                        uint32_t w[4];
+                        seen_bits(a, rw, key0, w);
+#pragma unroll
+                        for (int c = 0; c < 128; ++c)
+                            if (!(w[c >> 5] >> (c & 31) & 1u)) s[c] = 0xff800000u;
+                    }
+                    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int c = 0; c < 128; c += 8) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            top[k] = fmaxf(top[k], fmaxf(__uint_as_float(s[c + k]), __uint_as_float(s[c + 4 + k])));
+                    }
+                    const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
+                    const bool move = m_ref != -INFINITY && now > m_ref + RESCALE_LOG2;
+                    if (__any_sync(0xffffffffu, move)) {
+                        // (S of this tile has landed, so has the P V issued before it)
+                        const float f = move ? ex2_fast(m_ref - now) : 1.f;
+                        sum *= f;
+                        if (move) m_ref = now;
+#pragma unroll
+                        for (int c = 0; c < HD; c += 32) {
+                            uint32_t o[32];
+                            tmem_ld32(t_o + x * HD + c, o);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                            tmem_st32(t_o + x * HD + c, o);
+                        }
+                    }
+                    if (m_ref == -INFINITY) m_ref = now;
+                    const float use = m_ref == -INFINITY ? 0.f : m_ref;
+                    float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t p[32];
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) {
+                            const float e0 = ex2_fast(fmaf(__uint_as_float(s[64 * h + 2 * c]), a.scale_log2, -use));
+                            const float e1 = ex2_fast(fmaf(__uint_as_float(s[64 * h + 2 * c + 1]), a.scale_log2, -use));
+                            part[c & 3] += e0 + e1;
+                            const __nv_bfloat162 b = __floats2bfloat162_rn(e0, e1);
+                            p[c] = *reinterpret_cast<const uint32_t *>(&b);
+                        }
+                        tmem_st32(t_s + 32 * h, p);
+                    }
+                    sum += (part[0] + part[1]) + (part[2] + part[3]);
+                }
+                if (!full) {
+                    // V as the MMA will read it: nothing past the sequence's end, nothing that is not finite
+                    const int pos = at.v(tt);
+                    if (!dead && !w_wait(full0 + 8 * (pos % SLOTS), (uint32_t)(pos / SLOTS) & 1u, &s_abort, status)) dead = true;
+                    uint8_t *row = sm + L::RING + (pos % SLOTS) * L::MAT + m * 128;
+                    const bool held = key0 + m < rw.len;
+#pragma unroll
+                    for (int b = 0; b < L::NB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            uint4 *q = reinterpret_cast<uint4 *>(row + b * L::BOX + (((i + lane) & 7) << 4));
+                            if (!held) {
+                                *q = make_uint4(0, 0, 0, 0);
+                                continue;
+                            }
+                            const uint4 u = *q;
+                            uint32_t w[4] = {u.x, u.y, u.z, u.w}, bad = 0;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                if ((w[k] & 0x7f80u) == 0x7f80u) { w[k] &= 0xffff0000u; bad = 1; }
+                                if ((w[k] & 0x7f800000u) == 0x7f800000u) { w[k] &= 0x0000ffffu; bad = 1; }
+                            }
+                            if (bad) {
+                                atomicOr(&s_odd, 1u << (seg & 31));
+                                __threadfence_block();
+                                *q = make_uint4(w[0], w[1], w[2], w[3]);
+                            }
+                        }
+                    fence_proxy();
+                }
+                fence_before();
+                bar_arrive(p_full0 + 8 * x);
+            }
+            // the next segment's queries, while the last P V runs
+            const Segment cur = g;
+            have = walk.next(g);
+            if (have && steps(g, PAIR ? x : 0) > 0) load_q(g, seg + 1);
+            ring += 2 * n;
+
+            // the item's end: this group's O, or half the columns of both groups' O joined
+            const bool whole = segment_whole(cur);
+            const int head = cur.h * G + pm - r * G;
+            const long row = sched.start[cur.i] + r;
+            const long part = part_slot(cur, blockIdx.x) * ROWS + (PAIR ? x * TILE : 0) + m;
+            float f0 = 1.f, f1 = 0.f;
+            if (nx > 0) {
+                if (!dead && !w_wait(o_full0 + 8 * x, o_ph[x], &s_abort, status)) dead = true;
+                o_ph[x] ^= 1u;
+            }
+            if constexpr (!PAIR) {
+                if (n_other > 0) {
+                    if (!dead && !w_wait(o_full0 + 8 * (x ^ 1), o_ph[x ^ 1], &s_abort, status)) dead = true;
+                    o_ph[x ^ 1] ^= 1u;
+                }
+                s_ml[x * TILE + m] = make_float2(m_ref, sum);
+                groups_sync();
+                const float2 a0 = s_ml[m], a1 = s_ml[TILE + m];
+                const float top = fmaxf(a0.x, a1.x), use = top == -INFINITY ? 0.f : top;
+                f0 = a0.x == top ? 1.f : ex2_fast(a0.x - use);
+                f1 = a1.x == top ? 1.f : ex2_fast(a1.x - use);
+                if (a0.y == 0.f) f0 = 0.f;                        // (nothing seen: 0 times nothing)
+                if (a1.y == 0.f) f1 = 0.f;
+                m_ref = top;
+                sum = (a0.y == 0.f ? 0.f : a0.y * f0) + (a1.y == 0.f ? 0.f : a1.y * f1);
+            }
+            fence_after();
+            constexpr int COLS = PAIR ? HD : HD / 2;
+            const int col0 = PAIR ? 0 : x * COLS;
+            const bool two = !PAIR && cur.j1 - cur.j0 > 1, odd = s_odd >> (seg & 31) & 1u;
+            const bool none = sum == 0.f;                         // the row sees nothing: zeros, whatever O holds
+            const float inv = none ? 0.f : 1.f / sum;
+            if (PAIR && nx == 0) {
+                if (valid && !dead && !whole) *reinterpret_cast<float2 *>(a.part_ml + 2 * part) = make_float2(-INFINITY, 0.f);
+            } else {
+#pragma unroll 1
+                for (int c = 0; c < COLS; c += 32) {
+                    uint32_t o[32];
+                    float acc[32];
+                    tmem_ld32(t_o + (PAIR ? x * HD : 0) + col0 + c, o);
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        acc[k] = none || (!PAIR && f0 == 0.f) ? 0.f : PAIR ? __uint_as_float(o[k]) : __uint_as_float(o[k]) * f0;
+                    if (two) {
+                        tmem_ld32(t_o + HD + col0 + c, o);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (f1 != 0.f) acc[k] = fmaf(__uint_as_float(o[k]), f1, acc[k]);
+                    }
+                    if (odd && rw.r >= 0) {
+                        // values of V that were taken out and that this row sees
+                        for (int t = 0; t < n; ++t) {
+                            const int key0 = key_of(cur, t);
+                            if (key0 + KT <= rw.base + (a.mask ? 0 : 1) && !a.window) continue;      // seen in full by all rows
+                            uint32_t w[4];
+                            seen_bits(a, rw, key0, w);
+                            for (int k = 0; k < KT; ++k) {
+                                const int slot = key0 + k;
+                                if (slot >= rw.len || !(w[k >> 5] >> (k & 31) & 1u)) continue;
+                                const int id = v.table[(long)sched.seq[cur.i] * v.max_pages + (slot >> v.page_shift)];
+                                if ((unsigned)id >= (unsigned)v.n_pages) continue;
+                                const bf16 *src = static_cast<const bf16 *>(v.kv) + ((long)a.layer * v.n_pages + id) * v.page_elems() +
+                                                  ((long)(v.kv_heads + cur.h) * v.page + (slot & (v.page - 1))) * HD + col0 + c;
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) {
+                                    const float y = __bfloat162float(src[e]);
+                                    if (!isfinite(y)) acc[e] += y;
+                                }
+                            }
+                        }
+                    }
+                    if (!valid || dead) continue;
+                    if (whole) {
+                        bf16 *dst = static_cast<bf16 *>(a.out) + row * a.ldo + (long)head * HD + col0 + c;
+#pragma unroll
+                        for (int k = 0; k < 32; k += 8) {
+                            uint32_t u[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const __nv_bfloat162 b = __floats2bfloat162_rn(acc[k + 2 * e] * inv, acc[k + 2 * e + 1] * inv);
+                                u[e] = *reinterpret_cast<const uint32_t *>(&b);
+                            }
+                            *reinterpret_cast<uint4 *>(dst + k) = make_uint4(u[0], u[1], u[2], u[3]);
+                        }
+                    } else {
+                        float *dst = a.part_o + part * HD + col0 + c;
+#pragma unroll
+                        for (int k = 0; k < 32; k += 4)
+                            *reinterpret_cast<float4 *>(dst + k) = make_float4(acc[k], acc[k + 1], acc[k + 2], acc[k + 3]);
+                    }
+                }
+                if (valid && !dead && (PAIR || x == 0)) {
+                    if (!whole) *reinterpret_cast<float2 *>(a.part_ml + 2 * part) = make_float2(m_ref, sum);
+                    else if (a.lse)
+                        a.lse[row * v.heads + head] = sum == 0.f ? -INFINITY : (m_ref + log2f(sum)) * 0.6931471805599453f;
+                }
+            }
+            // the other group's O is not overwritten before this one has read it
+            if constexpr (!PAIR) groups_sync();
+            ++seg;
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::T_COLS) : "memory");
+    }
+}
+
+template <int HD, bool PAIR>
+cudaError_t launch(const CUtensorMap &map, const PagesAttn &a, int sms, cudaStream_t s) {
+    cudaError_t e = launch_chain(pages_attn_tc_kernel<HD, PAIR>, dim3(sms), dim3(THREADS), Lay<HD>::SMEM, s, map, a);
+    note_launch();
+    return e != cudaSuccess ? e : launch_pages_attn_join(a, MSD_BF16, sms, PAIR ? 2 * TILE : TILE, s);
+}
+
+}  // namespace
+
+bool pages_attn_tc_setup() {
+    auto set = [](const void *f, int bytes) {
+        return cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
+    };
+    return set((const void *)pages_attn_tc_kernel<64, false>, Lay<64>::SMEM) &&
+           set((const void *)pages_attn_tc_kernel<64, true>, Lay<64>::SMEM) &&
+           set((const void *)pages_attn_tc_kernel<128, false>, Lay<128>::SMEM) &&
+           set((const void *)pages_attn_tc_kernel<128, true>, Lay<128>::SMEM);
+}
+
+// The pool as rows of head_dim elements, in boxes of a page's tokens and 64 columns.
+bool pages_attn_map(const PagesView &v, CUtensorMap *map) {
+    cudaDriverEntryPointQueryResult q;
+    void *fn = nullptr;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess || !fn)
+        return false;
+    memset(map, 0, sizeof *map);
+    cuuint64_t dims[2] = {(cuuint64_t)v.head_dim, (cuuint64_t)v.layers * v.n_pages * 2 * v.kv_heads * v.page};
+    cuuint64_t strides[1] = {(cuuint64_t)v.head_dim * 2};
+    cuuint32_t box[2] = {64, (cuuint32_t)v.page};
+    cuuint32_t estr[2] = {1, 1};
+    return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn)(
+               map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, v.kv, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+cudaError_t launch_pages_attn_tc(const CUtensorMap &map, const PagesAttn &a, int sms, cudaStream_t s) {
+    // more than one tile of packed rows to a sequence: two tiles share each key tile
+    const bool pair = (long)a.b.rows * (a.pv.heads / a.pv.kv_heads) > (long)TILE * a.b.n;
+    if (a.pv.head_dim == 64) return pair ? launch<64, true>(map, a, sms, s) : launch<64, false>(map, a, sms, s);
+    return pair ? launch<128, true>(map, a, sms, s) : launch<128, false>(map, a, sms, s);
+}
+
+}  // namespace msd

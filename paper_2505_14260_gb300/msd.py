@@ -410,11 +410,12 @@ class Batch:
     def __init__(self, seqs: torch.Tensor, row_start: torch.Tensor, rows: int):
         if row_start.numel() != seqs.numel() + 1:
             raise ValueError("row_start has one entry more than seqs")
-        self.seqs, self.row_start, self.rows = _ints(seqs), _ints(row_start), int(rows)
-        self._c = msd_batch(seqs.numel(), _ptr(seqs), _ptr(row_start), self.rows)
+        self.seqs, self.row_start, self.n, self.rows = _ints(seqs), _ints(row_start), seqs.numel(), int(rows)
+        self._c = msd_batch(self.n, _ptr(seqs), _ptr(row_start), self.rows)
+        self._ref = ctypes.byref(self._c)
 
     def c(self):
-        return ctypes.byref(self._c)
+        return self._ref
 
 
 def _ints(t: torch.Tensor | None):
@@ -439,6 +440,7 @@ class Pages:
                                     page_size, n_pages, max_seqs, max_pages, rot_dim, (c_int32 * 3)(*sections),
                                     int(rot_interleaved), rope_base)
         self.dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self._H, self._K, self._hd = heads, kv_heads, head_dim
         fresh = lens is None
         shape = (layers, n_pages, 2, kv_heads, page_size, head_dim)
         i32 = dict(dtype=torch.int32, device=device)
@@ -476,11 +478,11 @@ class Pages:
 
     def _rows(self, t: torch.Tensor, heads: int, rows: int) -> int:
         """The row stride of q, k, v or out: [rows, heads, head_dim] or [rows, heads * head_dim]."""
-        width = heads * self.cfg.head_dim
-        if t.shape[0] != rows or t[:1].numel() != width * min(rows, 1) or \
-                (t.dim() == 3 and t.stride(1) != self.cfg.head_dim) or t.stride(-1) != 1 or t.dim() not in (2, 3):
-            raise ValueError(f"expected {rows} rows of {heads} heads of {self.cfg.head_dim} elements, one after another")
-        return t.stride(0) if rows > 1 else width
+        hd, shape, stride = self._hd, t.shape, t.stride()
+        if not (shape == (rows, heads * hd) and stride[1] == 1 or
+                shape == (rows, heads, hd) and stride[2] == 1 and (stride[1] == hd or heads == 1)):
+            raise ValueError(f"expected {rows} rows of {heads} heads of {hd} elements, one after another")
+        return stride[0] if rows > 1 else heads * hd
 
     def restore(self, stream=None):
         """Takes lens and table as they are; refs and free pages follow from them."""
@@ -499,7 +501,7 @@ class Pages:
 
     def compact(self, batch: Batch, keep: torch.Tensor | None, n_keep: torch.Tensor, stream=None):
         """Of the batch's rows keep keep[i, :n_keep[i]] (None: the first n_keep[i])."""
-        n = batch.seqs.numel()
+        n = batch.n
         if n_keep.numel() != n or (keep is not None and keep.shape[0] != n):
             raise ValueError("keep and n_keep have an entry per sequence")
         self._check(lib().msd_pages_compact(self.ptr, batch.c(), _ptr(_ints(keep)),
@@ -528,36 +530,37 @@ class Pages:
     def rope_append(self, layer: int, batch: Batch, q, k, v, pos: torch.Tensor, q_out, stream=None):
         """Rotated q into q_out, rotated k and v into the rows' slots (msd_rope_append).
         pos: [3, rows], or [1, rows] where the three axes agree."""
-        c, n = self.cfg, batch.rows
-        if q.dtype != k.dtype or q.dtype != v.dtype or q.dtype not in (torch.float32, torch.bfloat16) or \
-                q_out.dtype != self.dtype:
+        n, dt, H, K = batch.rows, q.dtype, self._H, self._K
+        if k.dtype != dt or v.dtype != dt or dt not in (torch.float32, torch.bfloat16) or q_out.dtype != self.dtype:
             raise ValueError("q, k and v have one type, fp32 or the cache's; q_out the cache's")
-        if pos.dim() != 2 or pos.shape[0] not in (1, 3) or pos.shape[1] < n:
+        axes, width = pos.shape
+        if axes not in (1, 3) or width < n:
             raise ValueError("pos is [3, rows] or [1, rows]")
         st = lib().msd_rope_append(
-            self.ptr, layer, batch.c(), _ptr(q), self._rows(q, c.n_heads, n), _ptr(k),
-            self._rows(k, c.n_kv_heads, n), _ptr(v), self._rows(v, c.n_kv_heads, n),
-            MSD_F32 if q.dtype == torch.float32 else MSD_BF16, _ptr(_ints(pos)),
-            pos.stride(0) if pos.shape[0] == 3 else 0, _ptr(q_out), self._rows(q_out, c.n_heads, n), _stream(stream))
-        self._check(st, "msd_rope_append")
+            self.ptr, layer, batch.c(), q.data_ptr(), self._rows(q, H, n), k.data_ptr(), self._rows(k, K, n),
+            v.data_ptr(), self._rows(v, K, n), MSD_F32 if dt == torch.float32 else MSD_BF16, _ints(pos).data_ptr(),
+            width if axes == 3 else 0, q_out.data_ptr(), self._rows(q_out, H, n), _stream(stream))
+        if st:
+            self._check(st, "msd_rope_append")
         return q_out
 
     def attention(self, layer: int, batch: Batch, q, out, lse: torch.Tensor | None = None, tree: Tree | None = None,
                   window: int = 0, sinks: int = 0, stream=None):
         """The batch's rows over their sequences' pages (msd_pages_attention). lse: fp32
         [rows, heads]; tree: one per listed sequence, its rows the tree's nodes."""
-        c, n = self.cfg, batch.rows
+        n, H = batch.rows, self._H
         if q.dtype != self.dtype or out.dtype != self.dtype:
             raise ValueError("q and out have the cache's type")
-        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() != n * c.n_heads):
+        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() != n * H):
             raise ValueError("lse is a contiguous fp32 tensor [rows, heads]")
-        if tree is not None and tree.B != batch.seqs.numel():
+        if tree is not None and tree.B != batch.n:
             raise ValueError("a tree per listed sequence")
-        t = None if tree is None else ctypes.byref(tree.c())
-        st = lib().msd_pages_attention(self.ptr, layer, batch.c(), t, 0 if tree is None else tree.N, window, sinks,
-                                       _ptr(q), self._rows(q, c.n_heads, n), _ptr(out),
-                                       self._rows(out, c.n_heads, n), _ptr(lse), _stream(stream))
-        self._check(st, "msd_pages_attention")
+        st = lib().msd_pages_attention(
+            self.ptr, layer, batch.c(), None if tree is None else ctypes.byref(tree.c()), 0 if tree is None else tree.N,
+            window, sinks, q.data_ptr(), self._rows(q, H, n), out.data_ptr(), self._rows(out, H, n), _ptr(lse),
+            _stream(stream))
+        if st:
+            self._check(st, "msd_pages_attention")
         return out
 
 
