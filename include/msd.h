@@ -411,7 +411,7 @@ typedef struct {
 
 /* The rows of a call: sequence seqs[i] (all different) has rows row_start[i] ..
  * row_start[i + 1] - 1 of the call's row arrays, and they are its LAST tokens (after
- * msd_pages_reserve). n <= max_seqs, and <= 1024 for msd_pages_attention. */
+ * msd_pages_reserve). n <= max_seqs. */
 typedef struct {
     int32_t n;
     const int32_t *seqs;        /* [n] device */

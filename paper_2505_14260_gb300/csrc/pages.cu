@@ -976,7 +976,6 @@ msd_status msd_pages_attention(msd_pages *p, int32_t layer, const msd_batch *bat
     const msd_pages_config &c = p->cfg;
     if (!batch_view(p, batch, &b) || layer < 0 || layer >= c.n_layers || !q || !out)
         return pfail(p, MSD_ERR_INVALID, "bad batch, layer or null array");
-    if (b.n > ATTN_MAX_SEQS) return pfail(p, MSD_ERR_INVALID, "more than 1024 sequences");
     if (window < 0 || sinks < 0) return pfail(p, MSD_ERR_INVALID, "negative window or sinks");
     if (tree && (!tree->mask || !tree->depth || tree_nodes < 1 || tree_nodes > 1024))
         return pfail(p, MSD_ERR_INVALID, "a tree needs its mask and depths, and 1 to 1024 nodes");
@@ -1010,8 +1009,17 @@ msd_status msd_pages_attention(msd_pages *p, int32_t layer, const msd_batch *bat
     a.part_ml = p->part_ml;
     a.part_item = p->part_item;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return leave(p, c.dtype == MSD_BF16 ? launch_pages_attn_tc(p->map, a, p->sms, s)
-                                        : launch_pages_attn_simt(a, p->sms, s));
+    cudaError_t e = cudaSuccess;
+    for (int i = 0; i < b.n && e == cudaSuccess; i += ATTN_MAX_SEQS) {
+        a.b = BatchView{std::min(b.n - i, ATTN_MAX_SEQS), b.rows, b.seqs + i, b.row_start + i};
+        if (tree) {
+            a.mask = tree->mask + (long)i * tree_nodes * a.words;
+            a.depth = tree->depth + (long)i * tree_nodes;
+            a.n_nodes = tree->n_nodes ? tree->n_nodes + i : nullptr;
+        }
+        e = c.dtype == MSD_BF16 ? launch_pages_attn_tc(p->map, a, p->sms, s) : launch_pages_attn_simt(a, p->sms, s);
+    }
+    return leave(p, e);
 }
 
 }  // extern "C"

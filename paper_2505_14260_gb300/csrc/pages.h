@@ -81,7 +81,7 @@ struct PagesAttn {
     int4 *part_item;
 };
 
-constexpr int ATTN_MAX_SEQS = 1024;        // sequences of one launch
+constexpr int ATTN_MAX_SEQS = 512;         // sequences of one launch
 size_t pages_attn_part_rows(int sms);      // rows of partial results that a launch may leave
 
 bool pages_attn_simt_setup();

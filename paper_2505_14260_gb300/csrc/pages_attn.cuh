@@ -7,17 +7,21 @@
 // sequence, head by head, tile by tile, form one line that the CTAs cut into equal runs: a
 // ragged batch, a causal triangle and one long sequence all load the SMs alike. Where a run
 // ends inside an item, its CTAs leave partial results (O, max, sum) that a second launch
-// joins in order. Lengths are read on the device; the cut depends on them alone.
+// joins in order. Lengths are read on the device; the cut depends on them alone. An item also
+// costs what it takes to begin and end (queries, output): ITEM_STEPS steps of the line before
+// its own, so that many short sequences spread over the SMs like a few long ones.
 #pragma once
 
 #include "pages.h"
 
 namespace msd {
 
+constexpr int ITEM_STEPS = 2;
+
 struct AttnSched {
     long long pre[ATTN_MAX_SEQS + 1];     // steps before each sequence
-    int len[ATTN_MAX_SEQS], rows[ATTN_MAX_SEQS], start[ATTN_MAX_SEQS], seq[ATTN_MAX_SEQS];
-    int4 first;                           // this CTA's first item: sequence, head, tile, step
+    int len[ATTN_MAX_SEQS], rows[ATTN_MAX_SEQS];
+    int4 first;                           // this CTA's first item: sequence, head, tile, place in it
     long long per;                        // steps of a CTA
 };
 
@@ -69,10 +73,8 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
             set_status(v.status, ST_BAD_BATCH);
             rows = 0;
         }
-        s.seq[i] = seq;
         s.len[i] = len;
         s.rows[i] = rows;
-        s.start[i] = r0;
     }
     __syncthreads();
     // steps of each sequence: a thread's own loop over few tiles, a warp's over many
@@ -80,7 +82,7 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
         const int tiles = (s.rows[i] * G + ROWS - 1) / ROWS;
         long long w = 0;
         if (tiles <= 4)
-            for (int t = 0; t < tiles; ++t) w += tile_range<ROWS, KT>(a, G, s.len[i], s.rows[i], t).steps;
+            for (int t = 0; t < tiles; ++t) w += ITEM_STEPS + tile_range<ROWS, KT>(a, G, s.len[i], s.rows[i], t).steps;
         s.pre[i + 1] = w * v.kv_heads;
     }
     __syncthreads();
@@ -88,7 +90,7 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
         const int tiles = (s.rows[i] * G + ROWS - 1) / ROWS;
         if (tiles <= 4) continue;
         long long w = 0;
-        for (int t = lane; t < tiles; t += 32) w += tile_range<ROWS, KT>(a, G, s.len[i], s.rows[i], t).steps;
+        for (int t = lane; t < tiles; t += 32) w += ITEM_STEPS + tile_range<ROWS, KT>(a, G, s.len[i], s.rows[i], t).steps;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
         if (lane == 0) s.pre[i + 1] = w * v.kv_heads;
@@ -134,7 +136,7 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
             int t0 = 0;
             for (; t0 < tiles; t0 += 32) {        // 32 tiles at a time
                 const int t = t0 + lane;
-                int inc = t < tiles ? tile_range<ROWS, KT>(a, G, s.len[lo], s.rows[lo], t).steps : 0;
+                int inc = t < tiles ? ITEM_STEPS + tile_range<ROWS, KT>(a, G, s.len[lo], s.rows[lo], t).steps : 0;
                 const int own = inc;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
@@ -163,35 +165,38 @@ template <int ROWS, int KT>
 struct AttnWalk {
     const PagesAttn &a;
     const AttnSched &s;
-    int G, i, h, tile, step;
+    int G, i, h, tile, place;             // place: of the line, within the item
     long long left;
     __device__ AttnWalk(const PagesAttn &a_, const AttnSched &s_) : a(a_), s(s_) {
         G = a.pv.heads / a.pv.kv_heads;
         i = s.first.x;
         h = s.first.y;
         tile = s.first.z;
-        step = s.first.w;
+        place = s.first.w;
         left = i < 0 ? 0 : s.per;
     }
     __device__ bool next(Segment &g) {
-        if (left <= 0 || i >= a.b.n) return false;
-        g.i = i;
-        g.h = h;
-        g.tile = tile;
-        g.range = tile_range<ROWS, KT>(a, G, s.len[i], s.rows[i], tile);
-        g.j0 = step;
-        g.j1 = (int)min((long long)g.range.steps, step + left);
-        left -= g.j1 - g.j0;
-        step = 0;
-        if (g.j1 == g.range.steps && ++tile * ROWS >= s.rows[i] * G) {
-            tile = 0;
-            if (++h == a.pv.kv_heads) {
-                h = 0;
-                do ++i;
-                while (i < a.b.n && s.rows[i] == 0);
+        while (left > 0 && i < a.b.n) {
+            g.i = i;
+            g.h = h;
+            g.tile = tile;
+            g.range = tile_range<ROWS, KT>(a, G, s.len[i], s.rows[i], tile);
+            const int end = ITEM_STEPS + g.range.steps, stop = (int)min((long long)end, place + left);
+            g.j0 = max(place - ITEM_STEPS, 0);
+            g.j1 = max(stop - ITEM_STEPS, 0);
+            left -= stop - place;
+            place = 0;
+            if (stop == end && ++tile * ROWS >= s.rows[i] * G) {
+                tile = 0;
+                if (++h == a.pv.kv_heads) {
+                    h = 0;
+                    do ++i;
+                    while (i < a.b.n && s.rows[i] == 0);
+                }
             }
+            if (g.j1 > g.j0) return true;         // (else the run ends before the item's first step)
         }
-        return true;
+        return false;
     }
 };
 
@@ -201,7 +206,7 @@ __device__ __forceinline__ bool segment_whole(const Segment &g) { return g.j0 ==
 __device__ __forceinline__ long part_slot(const Segment &g, int cta) { return 2l * cta + (g.j0 > 0 ? 0 : 1); }
 
 // The CTA that ends an item begun elsewhere names it for the joining launch: sequence, head,
-// tile, and the CTA that began it.
+// tile, and the CTA that took its first step.
 template <int ROWS, int KT>
 __device__ void name_parts(const PagesAttn &a, const AttnSched &s, int cta) {
     AttnWalk<ROWS, KT> walk(a, s);

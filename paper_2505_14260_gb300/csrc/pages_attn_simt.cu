@@ -43,10 +43,10 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
     AttnWalk<ROWS, KT> walk(a, sched);
     Segment g;
     while (walk.next(g)) {
-        const int len = sched.len[g.i], rows = sched.rows[g.i], start = sched.start[g.i], base = len - rows;
+        const int len = sched.len[g.i], rows = sched.rows[g.i], start = a.b.row_start[g.i], base = len - rows;
         const int m0 = g.tile * ROWS, nm = min(rows * G - m0, ROWS);
         const int live_rows = a.mask && a.n_nodes ? min(rows, a.n_nodes[g.i]) : rows;
-        const int *table = v.table + (long)sched.seq[g.i] * v.max_pages;
+        const int *table = v.table + (long)a.b.seqs[g.i] * v.max_pages;
         __syncthreads();
         for (int e = tid; e < ROWS * (HD / 4); e += THREADS) {
             const int m = e / (HD / 4), c = (e - m * (HD / 4)) * 4, r = (m0 + m) / G;

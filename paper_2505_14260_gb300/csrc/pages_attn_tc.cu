@@ -34,19 +34,26 @@ constexpr int KT = 128, THREADS = 320, TILE = 128;
 constexpr unsigned long long TIMEOUT_NS = 2000000000ull;
 constexpr float RESCALE_LOG2 = 8.f;
 
-template <int HD>
+// ROWS: packed rows of an item. 256: a pair of tiles. Fewer than 128: the MMA still takes 128 rows; what
+// it reads past the ones there are gives rows of S that nobody looks at, and the shared memory that
+// they would take holds key tiles instead.
+template <int HD, int ROWS>
 struct Lay {
     static constexpr int NB = HD / 64;                          // 64-column boxes of a row
-    static constexpr uint32_t BOX = TILE * 128;                 // [128 rows][64 bf16]
-    static constexpr uint32_t MAT = NB * BOX;                   // a Q, K or V tile
-    static constexpr int SLOTS = HD == 128 ? 4 : 9;
-    static constexpr uint32_t Q = 0, RING = 2 * MAT, SCHED = RING + SLOTS * MAT;
+    static constexpr int QROWS = ROWS < TILE ? ROWS : TILE;
+    static constexpr uint32_t BOX = TILE * 128;                 // [128 keys][64 bf16]
+    static constexpr uint32_t MAT = NB * BOX;                   // a K or V tile
+    static constexpr uint32_t QBOX = QROWS * 128, QMAT = NB * QBOX;
+    static constexpr uint32_t FIXED = 2 * QMAT + (sizeof(AttnSched) + 15) / 16 * 16 + 2 * TILE * 8;
+    static constexpr uint32_t LIMIT = 227 * 1024 - 1024 - 1024; // less alignment and static shared memory
+    static constexpr int SLOTS = (LIMIT - FIXED) / MAT < 12 ? (LIMIT - FIXED) / MAT : 12;
+    static constexpr uint32_t Q = 0, RING = 2 * QMAT, SCHED = RING + SLOTS * MAT;
     static constexpr uint32_t ML = SCHED + (sizeof(AttnSched) + 15) / 16 * 16;      // [2][128] float2
-    static constexpr uint32_t BYTES = ML + 2 * TILE * 8;
-    static constexpr uint32_t SMEM = BYTES + 1024;
+    static constexpr uint32_t SMEM = ML + 2 * TILE * 8 + 1024;
     // tensor memory: two S (P over its first half), two O
     static constexpr uint32_t T_S = 0, T_O = 2 * KT, T_COLS = 512;
-    static_assert(SMEM >= tmem_smem_floor((int)T_COLS) && SMEM <= 227 * 1024, "one CTA an SM, by its tensor memory");
+    static_assert(SMEM >= tmem_smem_floor((int)T_COLS) && SMEM <= 226 * 1024 && SLOTS >= 4, "one CTA an SM, by its tensor memory");
+    static_assert(SLOTS * MAT >= BOX + QBOX, "what the MMA reads past the query rows is shared memory");
 };
 
 __device__ __forceinline__ uint32_t su32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -67,7 +74,7 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 // Bounded wait: gives up when *abort is set, or after the limit (then sets it, and the status).
-__device__ __noinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, volatile int *abort, int *status) {
+__device__ __forceinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, volatile int *abort, int *status) {
     const unsigned long long t0 = gtime();
     while (!bar_try(bar, parity)) {
         if (*abort) return false;
@@ -144,6 +151,28 @@ __device__ __forceinline__ void w_commit(uint32_t on, uint32_t bar) {
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// 16 bytes into shared memory, zeros where `live` is false
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool live) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+}
+// packed pairs of fp32
+__device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(hi));
+    return d;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float lo2(uint64_t v) { return __uint_as_float((uint32_t)v); }
+__device__ __forceinline__ float hi2(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
 __device__ __forceinline__ float ex2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -157,17 +186,14 @@ __device__ __forceinline__ void groups_sync() {
     fence_after();
 }
 
-// 128 (or 32) columns of this warp's 32 lanes, waited for in the same statement: the registers
+// 64 (or 32) columns of this warp's 32 lanes, waited for in the same statement: the registers
 // are defined once the data has landed.
-__device__ __forceinline__ void tmem_ld128(uint32_t taddr, uint32_t *r) {
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t *r) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x128.b32 "
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
         "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%"
         "27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%"
-        "52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63,%64,%65,%66,%67,%68,%69,%70,%71,%72,%73,%74,%75,%76,%"
-        "77,%78,%79,%80,%81,%82,%83,%84,%85,%86,%87,%88,%89,%90,%91,%92,%93,%94,%95,%96,%97,%98,%99,%100,%101"
-        ",%102,%103,%104,%105,%106,%107,%108,%109,%110,%111,%112,%113,%114,%115,%116,%117,%118,%119,%120,%121"
-        ",%122,%123,%124,%125,%126,%127}, [%128];"
+        "52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];"
         "\ntcgen05.wait::ld.sync.aligned;"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
           "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
@@ -176,16 +202,7 @@ __device__ __forceinline__ void tmem_ld128(uint32_t taddr, uint32_t *r) {
           "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]),
           "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]),
           "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]),
-          "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63]), "=r"(r[64]),
-          "=r"(r[65]), "=r"(r[66]), "=r"(r[67]), "=r"(r[68]), "=r"(r[69]), "=r"(r[70]), "=r"(r[71]), "=r"(r[72]),
-          "=r"(r[73]), "=r"(r[74]), "=r"(r[75]), "=r"(r[76]), "=r"(r[77]), "=r"(r[78]), "=r"(r[79]), "=r"(r[80]),
-          "=r"(r[81]), "=r"(r[82]), "=r"(r[83]), "=r"(r[84]), "=r"(r[85]), "=r"(r[86]), "=r"(r[87]), "=r"(r[88]),
-          "=r"(r[89]), "=r"(r[90]), "=r"(r[91]), "=r"(r[92]), "=r"(r[93]), "=r"(r[94]), "=r"(r[95]), "=r"(r[96]),
-          "=r"(r[97]), "=r"(r[98]), "=r"(r[99]), "=r"(r[100]), "=r"(r[101]), "=r"(r[102]), "=r"(r[103]), "=r"(r[104]),
-          "=r"(r[105]), "=r"(r[106]), "=r"(r[107]), "=r"(r[108]), "=r"(r[109]), "=r"(r[110]), "=r"(r[111]),
-          "=r"(r[112]), "=r"(r[113]), "=r"(r[114]), "=r"(r[115]), "=r"(r[116]), "=r"(r[117]), "=r"(r[118]),
-          "=r"(r[119]), "=r"(r[120]), "=r"(r[121]), "=r"(r[122]), "=r"(r[123]), "=r"(r[124]), "=r"(r[125]),
-          "=r"(r[126]), "=r"(r[127])
+          "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
         : "r"(taddr)
         : "memory");
 }
@@ -279,10 +296,11 @@ struct Ring {
     __device__ int v(int t) const { return base + lead + t + min(t, n - lead); }
 };
 
-template <int HD, bool PAIR>
+template <int HD, int ROWS>
 __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_constant__ CUtensorMap map, const PagesAttn a) {
-    using L = Lay<HD>;
-    constexpr int ROWS = PAIR ? 2 * TILE : TILE, LEAD = PAIR ? 1 : 2, SLOTS = L::SLOTS;
+    using L = Lay<HD, ROWS>;
+    constexpr bool PAIR = ROWS == 2 * TILE;
+    constexpr int LEAD = PAIR ? 1 : 2, SLOTS = L::SLOTS;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * SLOTS + 9];
     __shared__ uint32_t s_tmem;
@@ -374,7 +392,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
         };
         while (ok && walk.next(g)) {
             const int n = g.j1 - g.j0, len = sched.len[g.i];
-            const int *table = v.table + (long)sched.seq[g.i] * v.max_pages;
+            const int *table = v.table + (long)a.b.seqs[g.i] * v.max_pages;
             const int lead = min(LEAD, n);
             for (int t = 0; ok && t < lead; ++t) ok = load(key_of(g, t), 0, table, len, g.h);
             for (int t = 0; ok && t < n; ++t) {
@@ -401,12 +419,11 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             return r;
         };
         auto s_mma = [&](int x, int pos, int qbuf) {
-            const uint32_t k = base + L::RING + (pos % SLOTS) * L::MAT, q = base + L::Q + qbuf * L::MAT;
+            const uint32_t k = base + L::RING + (pos % SLOTS) * L::MAT, q = base + L::Q + qbuf * L::QMAT;
 #pragma unroll
-            for (int kk = 0; kk < HD / 16; ++kk) {
-                const uint32_t o = (kk >> 2) * L::BOX + (kk & 3) * 32;
-                w_mma_ss(on, tmem + L::T_S + x * KT, sdesc(q + o, 16, 1024), sdesc(k + o, 16, 1024), id_s, kk > 0);
-            }
+            for (int kk = 0; kk < HD / 16; ++kk)
+                w_mma_ss(on, tmem + L::T_S + x * KT, sdesc(q + (kk >> 2) * L::QBOX + (kk & 3) * 32, 16, 1024),
+                         sdesc(k + (kk >> 2) * L::BOX + (kk & 3) * 32, 16, 1024), id_s, kk > 0);
             w_commit(on, s_full0 + 8 * x);
         };
         auto o_mma = [&](int x, int pos, bool acc) {
@@ -483,7 +500,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             bar_wait_slow(drain, 0, &never, status);
         }
         __syncwarp();
-    } else {
+    } else if (warp < 8) {
         // ---- softmax -------------------------------------------------------
         const int x = warp >> 2, m = threadIdx.x & 127;
         const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
@@ -491,34 +508,36 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
         uint32_t s_ph = 0, o_ph[2] = {0, 0};
         int ring = 0, seg = 0;
         bool dead = false;
-        // the query rows of a segment into its buffer: a pair's groups load their own tile, else each half the columns
+        // the query rows of a segment into its buffer (swizzled as the MMA reads them): a pair's groups load their
+        // own tiles, else both load the one there is. Asked for while there is other work, handed over by give_q.
         auto load_q = [&](const Segment &s, int index) {
-            const int pm = s.tile * ROWS + (PAIR ? x * TILE : 0) + m;
-            constexpr int N = PAIR ? HD / 8 : HD / 16;                // 16-byte pieces
-            const int c0 = PAIR ? 0 : x * N;
-            uint4 q[N];
-            if (pm < sched.rows[s.i] * G) {
-                const int r = pm / G;
-                const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const bf16 *>(a.q) + (sched.start[s.i] + r) * a.ldq +
-                                                                   (long)(s.h * G + pm - r * G) * HD) + c0;
+            constexpr int PIECES = L::QROWS * HD / 8, N = PAIR ? 128 : 256;               // of 16 bytes
+            const int pm0 = s.tile * ROWS + (PAIR ? x * TILE : 0), left = sched.rows[s.i] * G - pm0;
+            const bf16 *src = static_cast<const bf16 *>(a.q) + a.b.row_start[s.i] * a.ldq + (long)s.h * G * HD;
+            const uint32_t dst = base + L::Q + (PAIR ? x : index & 1) * L::QMAT;
 #pragma unroll
-                for (int i = 0; i < N; ++i) q[i] = src[i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) q[i] = make_uint4(0, 0, 0, 0);
+            for (int p0 = 0; p0 < PIECES; p0 += N) {
+                const int p = p0 + (PAIR ? m : (int)threadIdx.x), row = p / (HD / 8), c = p % (HD / 8);
+                const int pm = pm0 + row, r = pm / G;
+                if (PIECES % N == 0 || p < PIECES)
+                    copy16(dst + (c >> 3) * L::QBOX + row * 128 + (((c & 7) ^ (row & 7)) << 4),
+                           row < left ? src + r * a.ldq + (pm - r * G) * HD + 8 * c : src, row < left);
             }
-            uint8_t *dst = sm + L::Q + (PAIR ? x : index & 1) * L::MAT + m * 128;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int c = c0 + i;
-                *reinterpret_cast<uint4 *>(dst + (c >> 3) * L::BOX + (((c & 7) ^ (m & 7)) << 4)) = q[i];
-            }
+        };
+        auto give_q = [&]() {
+            asm volatile("cp.async.wait_all;" ::: "memory");
             fence_proxy();
             bar_arrive(q_full0 + (PAIR ? 8 * x : 0));
         };
-        bool have = walk.next(g);
-        if (have && steps(g, PAIR ? x : 0) > 0) load_q(g, 0);
+        Segment g_next;
+        bool have = walk.next(g), have_next = false, q_next = false;
+        if (have && steps(g, PAIR ? x : 0) > 0) {
+            load_q(g, 0);
+            give_q();
+        }
         while (have) {
+            have_next = walk.next(g_next);
+            q_next = have_next && steps(g_next, PAIR ? x : 0) > 0;
             const int n = g.j1 - g.j0, nx = steps(g, x), n_other = steps(g, x ^ 1);
             const Ring at{ring, n, min(LEAD, n)};
             const int pm0 = g.tile * ROWS + (PAIR ? x * TILE : 0), pm = pm0 + m;
@@ -528,8 +547,8 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             rw.base = rw.len - rw.rows;
             rw.live = a.mask && a.n_nodes ? min(rw.rows, a.n_nodes[g.i]) : rw.rows;
             rw.r_first = pm0 / G;
-            rw.r_last = (min(pm0 + TILE, rw.rows * G) - 1) / G;
-            const bool valid = pm < rw.rows * G;
+            rw.r_last = (min(pm0 + L::QROWS, rw.rows * G) - 1) / G;
+            const bool valid = m < L::QROWS && pm < rw.rows * G;
             const int r = pm / G;
             rw.r = valid && r < rw.live ? r : -1;
             rw.seq_i = g.i;
@@ -546,10 +565,12 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                 if (!dead && !w_wait(s_full0 + 8 * x, s_ph, &s_abort, status)) dead = true;
                 s_ph ^= 1u;
                 fence_after();
+                if (t == nx - 1 && q_next) load_q(g_next, seg + 1);       // (all of this segment's S that read the buffer are done)
                 const bool full = tile_full(a, rw, key0);
                 if (any) {
                     uint32_t s[128];
-                    tmem_ld128(t_s, s);
+                    tmem_ld64(t_s, s);
+                    tmem_ld64(t_s + 64, s + 64);
                     if (!full || blind) {
                         uint32_t w[4];
                         seen_bits(a, rw, key0, w);
@@ -582,21 +603,24 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                     }
                     if (m_ref == -INFINITY) m_ref = now;
                     const float use = m_ref == -INFINITY ? 0.f : m_ref;
-                    float part[4] = {0.f, 0.f, 0.f, 0.f};
+                    uint64_t part[4] = {0, 0, 0, 0};
+                    const uint64_t scale2 = pack2(__float_as_uint(a.scale_log2), __float_as_uint(a.scale_log2));
+                    const uint64_t use2 = pack2(__float_as_uint(-use), __float_as_uint(-use));
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         uint32_t p[32];
 #pragma unroll
                         for (int c = 0; c < 32; ++c) {
-                            const float e0 = ex2_fast(fmaf(__uint_as_float(s[64 * h + 2 * c]), a.scale_log2, -use));
-                            const float e1 = ex2_fast(fmaf(__uint_as_float(s[64 * h + 2 * c + 1]), a.scale_log2, -use));
-                            part[c & 3] += e0 + e1;
+                            const uint64_t z = fma2(pack2(s[64 * h + 2 * c], s[64 * h + 2 * c + 1]), scale2, use2);
+                            const float e0 = ex2_fast(lo2(z)), e1 = ex2_fast(hi2(z));
+                            part[c & 3] = add2(part[c & 3], pack2(__float_as_uint(e0), __float_as_uint(e1)));
                             const __nv_bfloat162 b = __floats2bfloat162_rn(e0, e1);
                             p[c] = *reinterpret_cast<const uint32_t *>(&b);
                         }
                         tmem_st32(t_s + 32 * h, p);
                     }
-                    sum += (part[0] + part[1]) + (part[2] + part[3]);
+                    const uint64_t all = add2(add2(part[0], part[1]), add2(part[2], part[3]));
+                    sum += lo2(all) + hi2(all);
                 }
                 if (!full) {
                     // V as the MMA will read it: nothing past the sequence's end, nothing that is not finite
@@ -631,17 +655,17 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                 fence_before();
                 bar_arrive(p_full0 + 8 * x);
             }
-            // the next segment's queries, while the last P V runs
-            const Segment cur = g;
-            have = walk.next(g);
-            if (have && steps(g, PAIR ? x : 0) > 0) load_q(g, seg + 1);
+            if (q_next) {
+                if (nx == 0) load_q(g_next, seg + 1);
+                give_q();
+            }
             ring += 2 * n;
 
             // the item's end: this group's O, or half the columns of both groups' O joined
-            const bool whole = segment_whole(cur);
-            const int head = cur.h * G + pm - r * G;
-            const long row = sched.start[cur.i] + r;
-            const long part = part_slot(cur, blockIdx.x) * ROWS + (PAIR ? x * TILE : 0) + m;
+            const bool whole = segment_whole(g);
+            const int head = g.h * G + pm - r * G;
+            const long row = a.b.row_start[g.i] + r;
+            const long part = part_slot(g, blockIdx.x) * ROWS + (PAIR ? x * TILE : 0) + m;     // (of a valid row)
             float f0 = 1.f, f1 = 0.f;
             if (nx > 0) {
                 if (!dead && !w_wait(o_full0 + 8 * x, o_ph[x], &s_abort, status)) dead = true;
@@ -666,7 +690,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             fence_after();
             constexpr int COLS = PAIR ? HD : HD / 2;
             const int col0 = PAIR ? 0 : x * COLS;
-            const bool two = !PAIR && cur.j1 - cur.j0 > 1, odd = s_odd >> (seg & 31) & 1u;
+            const bool two = !PAIR && n > 1, odd = s_odd >> (seg & 31) & 1u;
             const bool none = sum == 0.f;                         // the row sees nothing: zeros, whatever O holds
             const float inv = none ? 0.f : 1.f / sum;
             if (PAIR && nx == 0) {
@@ -689,17 +713,17 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                     if (odd && rw.r >= 0) {
                         // values of V that were taken out and that this row sees
                         for (int t = 0; t < n; ++t) {
-                            const int key0 = key_of(cur, t);
+                            const int key0 = key_of(g, t);
                             if (key0 + KT <= rw.base + (a.mask ? 0 : 1) && !a.window) continue;      // seen in full by all rows
                             uint32_t w[4];
                             seen_bits(a, rw, key0, w);
                             for (int k = 0; k < KT; ++k) {
                                 const int slot = key0 + k;
                                 if (slot >= rw.len || !(w[k >> 5] >> (k & 31) & 1u)) continue;
-                                const int id = v.table[(long)sched.seq[cur.i] * v.max_pages + (slot >> v.page_shift)];
+                                const int id = v.table[(long)a.b.seqs[g.i] * v.max_pages + (slot >> v.page_shift)];
                                 if ((unsigned)id >= (unsigned)v.n_pages) continue;
                                 const bf16 *src = static_cast<const bf16 *>(v.kv) + ((long)a.layer * v.n_pages + id) * v.page_elems() +
-                                                  ((long)(v.kv_heads + cur.h) * v.page + (slot & (v.page - 1))) * HD + col0 + c;
+                                                  ((long)(v.kv_heads + g.h) * v.page + (slot & (v.page - 1))) * HD + col0 + c;
 #pragma unroll
                                 for (int e = 0; e < 32; ++e) {
                                     const float y = __bfloat162float(src[e]);
@@ -737,6 +761,8 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             // the other group's O is not overwritten before this one has read it
             if constexpr (!PAIR) groups_sync();
             ++seg;
+            g = g_next;
+            have = have_next;
         }
     }
     fence_before();
@@ -747,23 +773,34 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
     }
 }
 
-template <int HD, bool PAIR>
+template <int HD, int ROWS>
 cudaError_t launch(const CUtensorMap &map, const PagesAttn &a, int sms, cudaStream_t s) {
-    cudaError_t e = launch_chain(pages_attn_tc_kernel<HD, PAIR>, dim3(sms), dim3(THREADS), Lay<HD>::SMEM, s, map, a);
+    cudaError_t e = launch_chain(pages_attn_tc_kernel<HD, ROWS>, dim3(sms), dim3(THREADS), Lay<HD, ROWS>::SMEM, s, map, a);
     note_launch();
-    return e != cudaSuccess ? e : launch_pages_attn_join(a, MSD_BF16, sms, PAIR ? 2 * TILE : TILE, s);
+    return e != cudaSuccess ? e : launch_pages_attn_join(a, MSD_BF16, sms, ROWS, s);
+}
+
+template <int HD, int ROWS>
+bool setup() {
+    return cudaFuncSetAttribute(pages_attn_tc_kernel<HD, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                (int)Lay<HD, ROWS>::SMEM) == cudaSuccess;
+}
+
+// A tile as large as the sequences' packed rows: a small one leaves room for more key tiles in flight.
+template <int HD>
+cudaError_t launch_rows(const CUtensorMap &map, const PagesAttn &a, int sms, cudaStream_t s) {
+    const long packed = ((long)a.b.rows * (a.pv.heads / a.pv.kv_heads) + a.b.n - 1) / a.b.n;
+    return packed <= 32    ? launch<HD, 32>(map, a, sms, s)
+           : packed <= 64  ? launch<HD, 64>(map, a, sms, s)
+           : packed <= 128 ? launch<HD, 128>(map, a, sms, s)
+                           : launch<HD, 256>(map, a, sms, s);
 }
 
 }  // namespace
 
 bool pages_attn_tc_setup() {
-    auto set = [](const void *f, int bytes) {
-        return cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
-    };
-    return set((const void *)pages_attn_tc_kernel<64, false>, Lay<64>::SMEM) &&
-           set((const void *)pages_attn_tc_kernel<64, true>, Lay<64>::SMEM) &&
-           set((const void *)pages_attn_tc_kernel<128, false>, Lay<128>::SMEM) &&
-           set((const void *)pages_attn_tc_kernel<128, true>, Lay<128>::SMEM);
+    return setup<64, 32>() && setup<64, 64>() && setup<64, 128>() && setup<64, 256>() && setup<128, 32>() &&
+           setup<128, 64>() && setup<128, 128>() && setup<128, 256>();
 }
 
 // The pool as rows of head_dim elements, in boxes of a page's tokens and 64 columns.
@@ -784,10 +821,7 @@ bool pages_attn_map(const PagesView &v, CUtensorMap *map) {
 }
 
 cudaError_t launch_pages_attn_tc(const CUtensorMap &map, const PagesAttn &a, int sms, cudaStream_t s) {
-    // more than one tile of packed rows to a sequence: two tiles share each key tile
-    const bool pair = (long)a.b.rows * (a.pv.heads / a.pv.kv_heads) > (long)TILE * a.b.n;
-    if (a.pv.head_dim == 64) return pair ? launch<64, true>(map, a, sms, s) : launch<64, false>(map, a, sms, s);
-    return pair ? launch<128, true>(map, a, sms, s) : launch<128, false>(map, a, sms, s);
+    return a.pv.head_dim == 64 ? launch_rows<64>(map, a, sms, s) : launch_rows<128>(map, a, sms, s);
 }
 
 }  // namespace msd

@@ -453,6 +453,7 @@ class Pages:
         for t, n in ((self.table, max_seqs * max_pages), (self.lens, max_seqs), (self.refs, n_pages)):
             if _ints(t).numel() != n:
                 raise ValueError("table, lens and refs have an entry per cell, sequence and page")
+        self._dev = self.kv.device.index
         buf = msd_pages_buffers(_ptr(self.kv), _ptr(self.table), _ptr(self.lens), _ptr(self.refs))
         self.ptr = c_void_p()
         st = lib().msd_pages_create(ctypes.byref(self.cfg), ctypes.byref(buf), ctypes.byref(self.ptr))
@@ -484,20 +485,25 @@ class Pages:
             raise ValueError(f"expected {rows} rows of {heads} heads of {hd} elements, one after another")
         return stride[0] if rows > 1 else heads * hd
 
+    def _on(self, stream) -> int:
+        """The stream of a call as a number; the current one without making a Stream object
+        (which takes longer than a small launch)."""
+        return torch._C._cuda_getCurrentRawStream(self._dev) if stream is None else stream.cuda_stream
+
     def restore(self, stream=None):
         """Takes lens and table as they are; refs and free pages follow from them."""
-        self._check(lib().msd_pages_restore(self.ptr, _stream(stream)), "msd_pages_restore")
+        self._check(lib().msd_pages_restore(self.ptr, self._on(stream)), "msd_pages_restore")
 
     def reserve(self, batch: Batch, stream=None):
         """Room for the batch's rows at the end of their sequences."""
-        self._check(lib().msd_pages_reserve(self.ptr, batch.c(), _stream(stream)), "msd_pages_reserve")
+        self._check(lib().msd_pages_reserve(self.ptr, batch.c(), self._on(stream)), "msd_pages_reserve")
 
     def fork(self, src: torch.Tensor, dst: torch.Tensor, deep: bool = False, stream=None):
         """Unused sequences dst[i] become copies of src[i]; full pages are shared unless deep."""
         if src.numel() != dst.numel():
             raise ValueError("src and dst have one entry per copy")
         self._check(lib().msd_pages_fork(self.ptr, dst.numel(), _ptr(_ints(src)), _ptr(_ints(dst)), int(deep),
-                                         _stream(stream)), "msd_pages_fork")
+                                         self._on(stream)), "msd_pages_fork")
 
     def compact(self, batch: Batch, keep: torch.Tensor | None, n_keep: torch.Tensor, stream=None):
         """Of the batch's rows keep keep[i, :n_keep[i]] (None: the first n_keep[i])."""
@@ -506,10 +512,10 @@ class Pages:
             raise ValueError("keep and n_keep have an entry per sequence")
         self._check(lib().msd_pages_compact(self.ptr, batch.c(), _ptr(_ints(keep)),
                                             0 if keep is None else keep.shape[1], _ptr(_ints(n_keep)),
-                                            _stream(stream)), "msd_pages_compact")
+                                            self._on(stream)), "msd_pages_compact")
 
     def free(self, seqs: torch.Tensor, stream=None):
-        self._check(lib().msd_pages_free(self.ptr, seqs.numel(), _ptr(_ints(seqs)), _stream(stream)),
+        self._check(lib().msd_pages_free(self.ptr, seqs.numel(), _ptr(_ints(seqs)), self._on(stream)),
                     "msd_pages_free")
 
     def positions(self, batch: Batch, span_start, spans, pos: torch.Tensor, next_pos: torch.Tensor | None = None,
@@ -524,7 +530,7 @@ class Pages:
                 raise ValueError("next and first have an entry per sequence")
         self._check(lib().msd_rope_positions(self.ptr, batch.c(), _ptr(_ints(span_start)), _ptr(_ints(spans)),
                                              _ptr(_ints(first)), _ptr(_ints(pos)), pos.stride(0),
-                                             _ptr(_ints(next_pos)), _stream(stream)), "msd_rope_positions")
+                                             _ptr(_ints(next_pos)), self._on(stream)), "msd_rope_positions")
         return pos
 
     def rope_append(self, layer: int, batch: Batch, q, k, v, pos: torch.Tensor, q_out, stream=None):
@@ -539,7 +545,7 @@ class Pages:
         st = lib().msd_rope_append(
             self.ptr, layer, batch.c(), q.data_ptr(), self._rows(q, H, n), k.data_ptr(), self._rows(k, K, n),
             v.data_ptr(), self._rows(v, K, n), MSD_F32 if dt == torch.float32 else MSD_BF16, _ints(pos).data_ptr(),
-            width if axes == 3 else 0, q_out.data_ptr(), self._rows(q_out, H, n), _stream(stream))
+            width if axes == 3 else 0, q_out.data_ptr(), self._rows(q_out, H, n), self._on(stream))
         if st:
             self._check(st, "msd_rope_append")
         return q_out
@@ -558,7 +564,7 @@ class Pages:
         st = lib().msd_pages_attention(
             self.ptr, layer, batch.c(), None if tree is None else ctypes.byref(tree.c()), 0 if tree is None else tree.N,
             window, sinks, q.data_ptr(), self._rows(q, H, n), out.data_ptr(), self._rows(out, H, n), _ptr(lse),
-            _stream(stream))
+            self._on(stream))
         if st:
             self._check(st, "msd_pages_attention")
         return out
