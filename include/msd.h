@@ -482,7 +482,8 @@ msd_status msd_rope_append(msd_pages *p, int32_t layer, const msd_batch *batch, 
  * Q - P < window or P < sinks; a row's place is L + r, with a tree L + its depth. A row that
  * sees nothing gives zeros and -inf. Values that are not finite reach only the rows that
  * see them; what a page holds past a sequence's end is never read into a result.
- * q, out: row r at r * ld elements, heads one after another, 16-byte aligned rows. */
+ * q, out: row r at r * ld elements, heads one after another, 16-byte aligned rows.
+ * rows * (n_heads / n_kv_heads) < 2^26. */
 msd_status msd_pages_attention(msd_pages *p, int32_t layer, const msd_batch *batch, const msd_tree *tree,
                                int32_t tree_nodes, int32_t window, int32_t sinks, const void *q_dev, int64_t ldq,
                                void *out_dev, int64_t ldo, float *lse_dev, void *stream);

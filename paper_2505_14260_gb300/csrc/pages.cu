@@ -979,6 +979,8 @@ msd_status msd_pages_attention(msd_pages *p, int32_t layer, const msd_batch *bat
     if (window < 0 || sinks < 0) return pfail(p, MSD_ERR_INVALID, "negative window or sinks");
     if (tree && (!tree->mask || !tree->depth || tree_nodes < 1 || tree_nodes > 1024))
         return pfail(p, MSD_ERR_INVALID, "a tree needs its mask and depths, and 1 to 1024 nodes");
+    if ((long)b.rows * (c.n_heads / c.n_kv_heads) >= 1l << 26)
+        return pfail(p, MSD_ERR_INVALID, "rows times query heads of a K/V head reach 2^26");
     if (tree && (long)b.rows > (long)b.n * tree_nodes) return pfail(p, MSD_ERR_INVALID, "more rows than tree nodes");
     const long hd = c.head_dim;
     const size_t de = c.dtype == MSD_F32 ? 4 : 2;
@@ -1004,6 +1006,8 @@ msd_status msd_pages_attention(msd_pages *p, int32_t layer, const msd_batch *bat
     }
     a.window = window;
     a.sinks = window ? sinks : 0;
+    a.group = c.n_heads / c.n_kv_heads;
+    a.group_magic = ((1ull << 32) + a.group - 1) / a.group;
     a.scale_log2 = 1.4426950408889634f / std::sqrt((float)hd);
     a.part_o = p->part_o;
     a.part_ml = p->part_ml;

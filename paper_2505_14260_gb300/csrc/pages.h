@@ -76,10 +76,17 @@ struct PagesAttn {
     int nodes, words;
     int window, sinks;        // window 0: none
     float scale_log2;         // log2(e) / sqrt(head_dim)
+    int group;                // query heads of a K/V head
+    unsigned long long group_magic;        // ceil(2^32 / group): see group_div
     // partial results of row tiles that several CTAs share
     float *part_o, *part_ml;
     int4 *part_item;
 };
+
+// x / group for x < 2^26 (the product is off by x * group at most, below 2^32)
+__device__ __forceinline__ int group_div(const PagesAttn &a, int x) {
+    return (int)((unsigned)x * a.group_magic >> 32);
+}
 
 constexpr int ATTN_MAX_SEQS = 512;         // sequences of one launch
 size_t pages_attn_part_rows(int sms);      // rows of partial results that a launch may leave

@@ -31,13 +31,13 @@ struct TileRange {
 };
 
 template <int ROWS, int KT>
-__device__ __forceinline__ TileRange tile_range(const PagesAttn &a, int G, int len, int rows, int tile) {
-    const int L = len - rows, m0 = tile * ROWS, m1 = min(rows * G, m0 + ROWS);
-    const int hi = a.mask ? len : L + (m1 - 1) / G + 1;
+__device__ __forceinline__ TileRange tile_range(const PagesAttn &a, int len, int rows, int tile) {
+    const int L = len - rows, m0 = tile * ROWS, m1 = min(rows * a.group, m0 + ROWS);
+    const int hi = a.mask ? len : L + group_div(a, m1 - 1) + 1;
     TileRange t;
     int lo = 0, sink = 0;
     if (a.window) {
-        lo = max(0, (a.mask ? L : L + m0 / G) - a.window + 1);
+        lo = max(0, (a.mask ? L : L + group_div(a, m0)) - a.window + 1);
         sink = min(a.sinks, lo);
     }
     t.lo = lo / KT;
@@ -59,7 +59,7 @@ template <int ROWS, int KT, int THREADS>
 __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int ctas) {
     __shared__ long long s_sum[THREADS / 32];
     const PagesView &v = a.pv;
-    const int G = v.heads / v.kv_heads, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int G = a.group, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int NW = THREADS / 32;
     for (int i = threadIdx.x; i < a.b.n; i += THREADS) {
         const int seq = a.b.seqs[i], r0 = a.b.row_start[i], r1 = a.b.row_start[i + 1];
@@ -82,7 +82,7 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
         const int tiles = (s.rows[i] * G + ROWS - 1) / ROWS;
         long long w = 0;
         if (tiles <= 4)
-            for (int t = 0; t < tiles; ++t) w += ITEM_STEPS + tile_range<ROWS, KT>(a, G, s.len[i], s.rows[i], t).steps;
+            for (int t = 0; t < tiles; ++t) w += ITEM_STEPS + tile_range<ROWS, KT>(a, s.len[i], s.rows[i], t).steps;
         s.pre[i + 1] = w * v.kv_heads;
     }
     __syncthreads();
@@ -90,7 +90,7 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
         const int tiles = (s.rows[i] * G + ROWS - 1) / ROWS;
         if (tiles <= 4) continue;
         long long w = 0;
-        for (int t = lane; t < tiles; t += 32) w += ITEM_STEPS + tile_range<ROWS, KT>(a, G, s.len[i], s.rows[i], t).steps;
+        for (int t = lane; t < tiles; t += 32) w += ITEM_STEPS + tile_range<ROWS, KT>(a, s.len[i], s.rows[i], t).steps;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
         if (lane == 0) s.pre[i + 1] = w * v.kv_heads;
@@ -136,7 +136,7 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
             int t0 = 0;
             for (; t0 < tiles; t0 += 32) {        // 32 tiles at a time
                 const int t = t0 + lane;
-                int inc = t < tiles ? ITEM_STEPS + tile_range<ROWS, KT>(a, G, s.len[lo], s.rows[lo], t).steps : 0;
+                int inc = t < tiles ? ITEM_STEPS + tile_range<ROWS, KT>(a, s.len[lo], s.rows[lo], t).steps : 0;
                 const int own = inc;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
@@ -168,7 +168,7 @@ struct AttnWalk {
     int G, i, h, tile, place;             // place: of the line, within the item
     long long left;
     __device__ AttnWalk(const PagesAttn &a_, const AttnSched &s_) : a(a_), s(s_) {
-        G = a.pv.heads / a.pv.kv_heads;
+        G = a.group;
         i = s.first.x;
         h = s.first.y;
         tile = s.first.z;
@@ -180,7 +180,7 @@ struct AttnWalk {
             g.i = i;
             g.h = h;
             g.tile = tile;
-            g.range = tile_range<ROWS, KT>(a, G, s.len[i], s.rows[i], tile);
+            g.range = tile_range<ROWS, KT>(a, s.len[i], s.rows[i], tile);
             const int end = ITEM_STEPS + g.range.steps, stop = (int)min((long long)end, place + left);
             g.j0 = max(place - ITEM_STEPS, 0);
             g.j1 = max(stop - ITEM_STEPS, 0);

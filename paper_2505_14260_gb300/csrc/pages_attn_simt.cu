@@ -37,7 +37,7 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
     allow_dependents();
     attn_schedule<ROWS, KT, THREADS>(a, sched, blockIdx.x, gridDim.x);
     const PagesView &v = a.pv;
-    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, G = v.heads / v.kv_heads;
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, G = a.group;
     if (tid == 0) name_parts<ROWS, KT>(a, sched, blockIdx.x);
     const float *kv = static_cast<const float *>(v.kv) + (long)a.layer * v.n_pages * v.page_elems();
     AttnWalk<ROWS, KT> walk(a, sched);
@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) pages_attn_join_kernel(const 
     const int4 item = a.part_item[blockIdx.x];
     if (item.x < 0) return;
     const PagesView &v = a.pv;
-    const int G = v.heads / v.kv_heads, lane = threadIdx.x & 31;
+    const int G = a.group, lane = threadIdx.x & 31;
     const int m = blockIdx.y * JOIN_WARPS + (threadIdx.x >> 5);
     const int start = a.b.row_start[item.x], rows = a.b.row_start[item.x + 1] - start;
     const int pm = item.z * tile_rows + m;

@@ -14,6 +14,7 @@
 //               does not see, online softmax in base 2, P as bf16 over S; at an item's end O
 //   warp 8      TMA: a key tile is one box a page and 64 columns, K and V in slots of their own
 //   warp 9      tensor memory and the MMAs
+//   warp 10     what each segment of the CTA's run is, for the others, ahead of them
 // P is rounded to bf16 (the V operand's type; the row's sum takes the weights unrounded): with
 // the result's own rounding that is 2^-9 a value twice, not once. Maxima, sums, S and O are
 // fp32. A row's reference maximum moves (and O is rescaled) only when a tile's exceeds it by
@@ -24,15 +25,17 @@
 // through V in shared memory before P V, zeroes slots past the sequence's end, and zeroes values
 // that are not finite after noting so; the item's end then adds those that a row does see.
 #include <cstring>
+#include <type_traits>
 
 #include "pages_attn.cuh"
 
 namespace msd {
 namespace {
 
-constexpr int KT = 128, THREADS = 320, TILE = 128;
+constexpr int KT = 128, THREADS = 384, TILE = 128, SEGS = 8;
 constexpr unsigned long long TIMEOUT_NS = 2000000000ull;
 constexpr float RESCALE_LOG2 = 8.f;
+constexpr int POLY = 2;               // pairs of 8 whose exponentials the FMA pipes take
 
 // ROWS: packed rows of an item. 256: a pair of tiles. Fewer than 128: the MMA still takes 128 rows; what
 // it reads past the ones there are gives rows of S that nobody looks at, and the shared memory that
@@ -45,14 +48,14 @@ struct Lay {
     static constexpr uint32_t MAT = NB * BOX;                   // a K or V tile
     static constexpr uint32_t QBOX = QROWS * 128, QMAT = NB * QBOX;
     static constexpr uint32_t FIXED = 2 * QMAT + (sizeof(AttnSched) + 15) / 16 * 16 + 2 * TILE * 8;
-    static constexpr uint32_t LIMIT = 227 * 1024 - 1024 - 1024; // less alignment and static shared memory
+    static constexpr uint32_t LIMIT = 227 * 1024 - 1024 - 1536; // less alignment and static shared memory
     static constexpr int SLOTS = (LIMIT - FIXED) / MAT < 12 ? (LIMIT - FIXED) / MAT : 12;
     static constexpr uint32_t Q = 0, RING = 2 * QMAT, SCHED = RING + SLOTS * MAT;
     static constexpr uint32_t ML = SCHED + (sizeof(AttnSched) + 15) / 16 * 16;      // [2][128] float2
     static constexpr uint32_t SMEM = ML + 2 * TILE * 8 + 1024;
-    // tensor memory: two S (P over its first half), two O
+    // tensor memory: two S (P over the first half), two O
     static constexpr uint32_t T_S = 0, T_O = 2 * KT, T_COLS = 512;
-    static_assert(SMEM >= tmem_smem_floor((int)T_COLS) && SMEM <= 226 * 1024 && SLOTS >= 4, "one CTA an SM, by its tensor memory");
+    static_assert(SMEM >= tmem_smem_floor((int)T_COLS) && SMEM <= 227 * 1024 - 1536 && SLOTS >= 4, "one CTA an SM, by its tensor memory");
     static_assert(SLOTS * MAT >= BOX + QBOX, "what the MMA reads past the query rows is shared memory");
 };
 
@@ -171,29 +174,32 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
+__device__ __forceinline__ uint64_t pack2f(float lo, float hi) { return pack2(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ uint64_t neg2(uint64_t v) { return v ^ 0x8000000080000000ull; }
 __device__ __forceinline__ float lo2(uint64_t v) { return __uint_as_float((uint32_t)v); }
 __device__ __forceinline__ float hi2(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
+// the largest of three, or NaN if one is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 __device__ __forceinline__ float ex2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// Both softmax groups (256 threads).
-__device__ __forceinline__ void groups_sync() {
-    __syncwarp();
-    fence_before();
-    asm volatile("barrier.sync.aligned 1, 256;" ::: "memory");
-    fence_after();
-}
-
-// 64 (or 32) columns of this warp's 32 lanes, waited for in the same statement: the registers
+// 128 (or 32) columns of this warp's 32 lanes, waited for in the same statement: the registers
 // are defined once the data has landed.
-__device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t *r) {
+__device__ __forceinline__ void tmem_ld128(uint32_t taddr, uint32_t *r) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+        "tcgen05.ld.sync.aligned.32x32b.x128.b32 "
         "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%"
         "27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%"
-        "52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];"
+        "52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63,%64,%65,%66,%67,%68,%69,%70,%71,%72,%73,%74,%75,%76,%"
+        "77,%78,%79,%80,%81,%82,%83,%84,%85,%86,%87,%88,%89,%90,%91,%92,%93,%94,%95,%96,%97,%98,%99,%100,%101"
+        ",%102,%103,%104,%105,%106,%107,%108,%109,%110,%111,%112,%113,%114,%115,%116,%117,%118,%119,%120,%121"
+        ",%122,%123,%124,%125,%126,%127}, [%128];"
         "\ntcgen05.wait::ld.sync.aligned;"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
           "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
@@ -202,7 +208,16 @@ __device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t *r) {
           "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]),
           "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]),
           "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]),
-          "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+          "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63]), "=r"(r[64]),
+          "=r"(r[65]), "=r"(r[66]), "=r"(r[67]), "=r"(r[68]), "=r"(r[69]), "=r"(r[70]), "=r"(r[71]), "=r"(r[72]),
+          "=r"(r[73]), "=r"(r[74]), "=r"(r[75]), "=r"(r[76]), "=r"(r[77]), "=r"(r[78]), "=r"(r[79]), "=r"(r[80]),
+          "=r"(r[81]), "=r"(r[82]), "=r"(r[83]), "=r"(r[84]), "=r"(r[85]), "=r"(r[86]), "=r"(r[87]), "=r"(r[88]),
+          "=r"(r[89]), "=r"(r[90]), "=r"(r[91]), "=r"(r[92]), "=r"(r[93]), "=r"(r[94]), "=r"(r[95]), "=r"(r[96]),
+          "=r"(r[97]), "=r"(r[98]), "=r"(r[99]), "=r"(r[100]), "=r"(r[101]), "=r"(r[102]), "=r"(r[103]), "=r"(r[104]),
+          "=r"(r[105]), "=r"(r[106]), "=r"(r[107]), "=r"(r[108]), "=r"(r[109]), "=r"(r[110]), "=r"(r[111]),
+          "=r"(r[112]), "=r"(r[113]), "=r"(r[114]), "=r"(r[115]), "=r"(r[116]), "=r"(r[117]), "=r"(r[118]),
+          "=r"(r[119]), "=r"(r[120]), "=r"(r[121]), "=r"(r[122]), "=r"(r[123]), "=r"(r[124]), "=r"(r[125]),
+          "=r"(r[126]), "=r"(r[127])
         : "r"(taddr)
         : "memory");
 }
@@ -247,46 +262,127 @@ __device__ __forceinline__ uint32_t mask_bits(const uint64_t *m, int words, int 
     return (uint32_t)x;
 }
 
-// What a group knows of the segment's rows, and a thread of its own.
-struct Rows {
-    int len, base, rows, live;        // sequence length, tokens before the rows, rows, rows that exist in its tree
-    int r_first, r_last;              // the group's rows
-    int r, place, seq_i;              // the thread's row (-1: none) and its place
-    const uint64_t *mrow;
+// A segment as the roles need it: made by one warp ahead of them, in a ring in shared memory.
+struct Seg {
+    int i, h, seq, start;             // listed sequence, K/V head, table row, first row
+    int len, base, rows, live;        // tokens, tokens before the rows, rows, rows that exist in its tree
+    int m0, n, nx[2];                 // first packed row, steps (0: no more segments), steps of each group
+    int j0, sink_tiles, lo, whole;    // first step; which key tiles the steps are; the item's only segment
+    long part;                        // its partial results' first row
+    __device__ int key(int t) const {
+        const int j = j0 + t;
+        return (j < sink_tiles ? j : lo + j - sink_tiles) * KT;
+    }
 };
 
-// Whether every row of [r_first, r_last] that sees anything sees every key of the tile.
-__device__ __forceinline__ bool tile_full(const PagesAttn &a, const Rows &x, int key0) {
-    const int end = key0 + KT;
-    if (end > x.base + (a.mask ? 0 : x.r_first + 1)) return false;
-    if (!a.window || end <= a.sinks) return true;
-    return x.base + (a.mask ? a.nodes : x.r_last) - key0 < a.window;
-}
+// A thread's row.
+struct Row {
+    int r, place;                     // -1: none that sees anything; its place
+    const uint64_t *mask;
+};
 
-// The keys of a tile that the thread's row sees.
-__device__ __forceinline__ void seen_bits(const PagesAttn &a, const Rows &x, int key0, uint32_t *w) {
+// The keys of a tile that a row sees.
+__device__ __forceinline__ void seen_bits(const PagesAttn &a, const Seg &d, const Row &x, int key0, uint32_t *w) {
     if (x.r < 0) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = 0;
         return;
     }
-    const int hi = a.mask ? x.base : x.base + x.r + 1, lo = a.window ? x.place - a.window + 1 : 0;
+    const int hi = a.mask ? d.base : d.base + x.r + 1, lo = a.window ? x.place - a.window + 1 : 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int key = key0 + 32 * i;
-        w[i] = range_bits(lo, hi, key) | range_bits(0, min(a.sinks, hi), key);
-        if (a.mask && key + 32 > x.base && key < x.len) {
-            uint32_t m = mask_bits(x.mrow, a.words, key - x.base) & range_bits(x.base, x.len, key);
-            if (a.window && x.place - x.base >= a.window) {       // (else all depths up to its own are inside)
+        w[i] = range_bits(lo, hi, key);
+        if (a.sinks) w[i] |= range_bits(0, min(a.sinks, hi), key);
+        if (a.mask && key + 32 > d.base && key < d.len) {
+            uint32_t m = mask_bits(x.mask, a.words, key - d.base) & range_bits(d.base, d.len, key);
+            if (a.window && x.place - d.base >= a.window) {       // (else all depths up to its own are inside)
                 for (uint32_t left = m; left; left &= left - 1) {
                     const int bit = __ffs(left) - 1;
-                    const int at = x.base + a.depth[(long)x.seq_i * a.nodes + key + bit - x.base];
+                    const int at = d.base + a.depth[(long)d.i * a.nodes + key + bit - d.base];
                     if (x.place - at >= a.window && at >= a.sinks) m &= ~(1u << bit);
                 }
             }
             w[i] |= m;
         }
     }
+}
+
+// Values of V that a tile's look-through took out, and that the row sees: added to eight of its columns.
+__device__ __noinline__ void add_odd(const PagesAttn &a, const Seg &d, Row x, int hd, int col, float *acc) {
+    const PagesView &v = a.pv;
+    for (int t = 0; t < d.n; ++t) {
+        const int key0 = d.key(t);
+        if (key0 + KT <= d.base + (a.mask ? 0 : 1) && !a.window) continue;      // seen in full by all rows: left as it was
+        uint32_t w[4];
+        seen_bits(a, d, x, key0, w);
+        for (int k = 0; k < KT; ++k) {
+            const int slot = key0 + k;
+            if (slot >= d.len || !((k < 64 ? k < 32 ? w[0] : w[1] : k < 96 ? w[2] : w[3]) >> (k & 31) & 1u)) continue;
+            const int id = v.table[(long)d.seq * v.max_pages + (slot >> v.page_shift)];
+            if ((unsigned)id >= (unsigned)v.n_pages) continue;
+            const bf16 *src = static_cast<const bf16 *>(v.kv) + ((long)a.layer * v.n_pages + id) * v.page_elems() +
+                              ((long)(v.kv_heads + d.h) * v.page + (slot & (v.page - 1))) * hd + col;
+            for (int e = 0; e < 8; ++e) {
+                const float y = __bfloat162float(src[e]);
+                if (!isfinite(y)) acc[e] += y;
+            }
+        }
+    }
+}
+
+// V as the MMA will read it: a thread's key row of a tile, zeros if no token is there (`held` false), and zeros for
+// values that are not finite, which *odd's bit then tells. x * 0 is a NaN for those alone, so the look costs one
+// multiply-add for two values.
+template <int NB>
+__device__ __forceinline__ void clean_row(uint8_t *row, uint32_t box, int lane, bool held, unsigned *odd, unsigned bit) {
+    auto at = [&](int i) { return reinterpret_cast<uint4 *>(row + (i >> 3) * box + (((i + lane) & 7) << 4)); };
+    if (!held) {
+#pragma unroll
+        for (int i = 0; i < 8 * NB; ++i) *at(i) = make_uint4(0, 0, 0, 0);
+        return;
+    }
+    const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+    __nv_bfloat162 acc[4] = {zero, zero, zero, zero};
+#pragma unroll
+    for (int i = 0; i < 8 * NB; ++i) {
+        const uint4 u = *at(i);
+        acc[0] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&u.x), zero, acc[0]);
+        acc[1] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&u.y), zero, acc[1]);
+        acc[2] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&u.z), zero, acc[2]);
+        acc[3] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&u.w), zero, acc[3]);
+    }
+    const __nv_bfloat162 all = __hadd2(__hadd2(acc[0], acc[1]), __hadd2(acc[2], acc[3]));
+    if (__low2float(all) == 0.f && __high2float(all) == 0.f) return;
+    atomicOr(odd, bit);
+    __threadfence_block();
+#pragma unroll 1
+    for (int i = 0; i < 8 * NB; ++i) {
+        uint32_t *q = reinterpret_cast<uint32_t *>(at(i));
+#pragma unroll 1
+        for (int k = 0; k < 4; ++k) {
+            uint32_t u = q[k];
+            if ((u & 0x7f80u) == 0x7f80u) u &= 0xffff0000u;
+            if ((u & 0x7f800000u) == 0x7f800000u) u &= 0x0000ffffu;
+            q[k] = u;
+        }
+    }
+}
+
+// 2^z of two values on the FMA pipes, -126 <= z <= 127: z = n + f with n whole and |f| <= 1/2, a polynomial of degree 4
+// in f (least largest relative error, 2.6e-6; fitted by exchange), n added to the exponent. The exponential unit takes a
+// warp's values at a quarter of the rate of the FMA pipes' pairs, and is what a tile's softmax waits for.
+__device__ __forceinline__ void ex2_pair(uint64_t z, float &e0, float &e1) {
+    const uint64_t floor2 = pack2f(-126.f, -126.f), magic = pack2f(12582912.f, 12582912.f);
+    const uint64_t zc = pack2f(fmaxf(lo2(z), lo2(floor2)), fmaxf(hi2(z), hi2(floor2)));
+    const uint64_t t = add2(zc, magic);                             // 1.5 2^23 + n
+    const uint64_t f = add2(zc, neg2(add2(t, neg2(magic))));
+    uint64_t p = fma2(f, pack2f(0.009570102207362652f, 0.009570102207362652f), pack2f(0.05591785907745361f, 0.05591785907745361f));
+    p = fma2(p, f, pack2f(0.240247443318367f, 0.240247443318367f));
+    p = fma2(p, f, pack2f(0.6931217908859253f, 0.6931217908859253f));
+    p = fma2(p, f, pack2f(0.9999992847442627f, 0.9999992847442627f));
+    e0 = __uint_as_float((uint32_t)p + ((uint32_t)t << 23));
+    e1 = __uint_as_float((uint32_t)(p >> 32) + ((uint32_t)(t >> 32) << 23));
 }
 
 // Where the ring holds a segment's tiles: K tiles run `lead` ahead of V tiles.
@@ -302,17 +398,19 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
     constexpr bool PAIR = ROWS == 2 * TILE;
     constexpr int LEAD = PAIR ? 1 : 2, SLOTS = L::SLOTS;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * SLOTS + 9];
+    __shared__ __align__(8) uint64_t bars[2 * SLOTS + 10 + 2 * SEGS];
     __shared__ uint32_t s_tmem;
     __shared__ unsigned s_odd;            // bit i % 32: segment i had values of V that are not finite zeroed
     __shared__ volatile int s_abort;
+    __shared__ Seg s_seg[SEGS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t raw = su32(smem_raw), base = (raw + 1023u) & ~1023u;
     uint8_t *sm = smem_raw + (base - raw);
     AttnSched &sched = *reinterpret_cast<AttnSched *>(sm + L::SCHED);
     float2 *s_ml = reinterpret_cast<float2 *>(sm + L::ML);
     const uint32_t full0 = su32(bars), empty0 = full0 + 8 * SLOTS, s_full0 = empty0 + 8 * SLOTS, p_full0 = s_full0 + 16,
-                   o_full0 = p_full0 + 16, q_full0 = o_full0 + 16, drain = q_full0 + 16;
+                   o_full0 = p_full0 + 16, q_full0 = o_full0 + 16, drain = q_full0 + 16, g_full0 = drain + 8,
+                   g_empty0 = g_full0 + 8 * SEGS, both = g_empty0 + 8 * SEGS;
     if (threadIdx.x == 0) {
         for (int i = 0; i < SLOTS; ++i) {
             bar_init(full0 + 8 * i, 1);
@@ -325,6 +423,11 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             bar_init(q_full0 + 8 * x, PAIR ? 128 : 256);
         }
         bar_init(drain, 1);
+        bar_init(both, 256);
+        for (int i = 0; i < SEGS; ++i) {
+            bar_init(g_full0 + 8 * i, 1);
+            bar_init(g_empty0 + 8 * i, 2 + 256);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_odd = 0;
         s_abort = 0;
@@ -344,27 +447,56 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
     fence_after();
     const uint32_t tmem = s_tmem;
     const PagesView &v = a.pv;
-    const int G = v.heads / v.kv_heads;
+    const int G = a.group;
     int *status = v.status;
-    if (threadIdx.x == 0) name_parts<ROWS, KT>(a, sched, blockIdx.x);
-    AttnWalk<ROWS, KT> walk(a, sched);
-    Segment g;
-    // steps of a segment for group x: in a pair the first tile's rows may end before the last key tiles
-    auto steps = [&](const Segment &s, int x) {
-        const int n = s.j1 - s.j0;
-        if (!PAIR) return (n + 1 - x) / 2;
-        const int left = sched.rows[s.i] * G - s.tile * ROWS;
-        if (left <= TILE) return x ? 0 : n;
-        if (x || a.mask) return n;
-        const int hi = sched.len[s.i] - sched.rows[s.i] + (s.tile * ROWS + TILE - 1) / G + 1;
-        return min(n, max(0, s.range.sink_tiles + (hi + KT - 1) / KT - s.range.lo - s.j0));
-    };
-    auto key_of = [](const Segment &s, int t) {
-        const int j = s.j0 + t;
-        return (j < s.range.sink_tiles ? j : s.range.lo + j - s.range.sink_tiles) * KT;
-    };
-
-    if (warp == 8) {
+    auto seg_wait = [&](int i) { return w_wait(g_full0 + 8 * (i % SEGS), (uint32_t)(i / SEGS) & 1u, &s_abort, status); };
+    // registers to where they are used: 216 a softmax thread, 72 the others (2 * 216 + 72 = 3 * 168)
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == 10) {
+        // ---- segments ------------------------------------------------------
+        AttnWalk<ROWS, KT> walk(a, sched);
+        Segment g;
+        for (int i = 0;; ++i) {
+            if (!w_wait(g_empty0 + 8 * (i % SEGS), (uint32_t)(i / SEGS + 1) & 1u, &s_abort, status)) break;
+            const bool have = walk.next(g);
+            if (lane == 0) {
+                Seg &d = s_seg[i % SEGS];
+                d.n = 0;
+                if (have) {
+                    d.i = g.i;
+                    d.h = g.h;
+                    d.seq = a.b.seqs[g.i];
+                    d.start = a.b.row_start[g.i];
+                    d.len = sched.len[g.i];
+                    d.rows = sched.rows[g.i];
+                    d.base = d.len - d.rows;
+                    d.live = a.mask && a.n_nodes ? min(d.rows, a.n_nodes[g.i]) : d.rows;
+                    d.m0 = g.tile * ROWS;
+                    d.n = g.j1 - g.j0;
+                    d.j0 = g.j0;
+                    d.sink_tiles = g.range.sink_tiles;
+                    d.lo = g.range.lo;
+                    d.whole = segment_whole(g);
+                    d.part = part_slot(g, blockIdx.x) * ROWS;
+                    if (PAIR) {           // the first tile's rows may end before the last key tiles
+                        const bool two = d.rows * G - d.m0 > TILE;
+                        const int hi = d.base + group_div(a, d.m0 + TILE - 1) + 1;
+                        d.nx[0] = two && !a.mask ? min(d.n, max(0, d.sink_tiles + (hi + KT - 1) / KT - d.lo - d.j0)) : d.n;
+                        d.nx[1] = two ? d.n : 0;
+                    } else {
+                        d.nx[0] = (d.n + 1) / 2;
+                        d.nx[1] = d.n / 2;
+                    }
+                }
+                bar_arrive(g_full0 + 8 * (i % SEGS));
+            }
+            __syncwarp();
+            if (!have) break;
+        }
+        if (lane == 0) name_parts<ROWS, KT>(a, sched, blockIdx.x);
+        __syncwarp();
+    } else if (warp == 8) {
         // ---- TMA -----------------------------------------------------------
         const uint32_t on = elect_one();
         int pos = 0;
@@ -390,15 +522,19 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             }
             return true;
         };
-        while (ok && walk.next(g)) {
-            const int n = g.j1 - g.j0, len = sched.len[g.i];
-            const int *table = v.table + (long)a.b.seqs[g.i] * v.max_pages;
-            const int lead = min(LEAD, n);
-            for (int t = 0; ok && t < lead; ++t) ok = load(key_of(g, t), 0, table, len, g.h);
+        for (int i = 0; ok; ++i) {
+            ok = seg_wait(i);
+            const Seg &d = s_seg[i % SEGS];
+            const int n = d.n, len = d.len, h = d.h, lead = min(LEAD, n);
+            if (!ok || n == 0) break;
+            const int *table = v.table + (long)d.seq * v.max_pages;
+            for (int t = 0; ok && t < lead; ++t) ok = load(d.key(t), 0, table, len, h);
             for (int t = 0; ok && t < n; ++t) {
-                ok = load(key_of(g, t), 1, table, len, g.h);
-                if (ok && t + lead < n) ok = load(key_of(g, t + lead), 0, table, len, g.h);
+                ok = load(d.key(t), 1, table, len, h);
+                if (ok && t + lead < n) ok = load(d.key(t + lead), 0, table, len, h);
             }
+            __syncwarp();
+            if (lane == 0) bar_arrive(g_empty0 + 8 * (i % SEGS));
         }
         if (s_abort) {            // the copies still in flight land before the CTA exits
             volatile int never = 0;
@@ -410,7 +546,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
         // ---- MMA -----------------------------------------------------------
         const uint32_t on = elect_one();
         const uint32_t id_s = idesc(TILE, KT, 0), id_o = idesc(TILE, HD, 1);
-        int ring = 0, seg = 0;
+        int ring = 0;
         uint32_t p_ph[2] = {0, 0}, q_ph[2] = {0, 0};
         bool ok = true;
         auto wait_slot = [&](int pos) {
@@ -430,8 +566,8 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             const uint32_t w = base + L::RING + (pos % SLOTS) * L::MAT;
 #pragma unroll
             for (int kk = 0; kk < KT / 16; ++kk)
-                w_mma_ts(on, tmem + L::T_O + x * HD, tmem + L::T_S + x * KT + kk * 8, sdesc(w + kk * 2048, L::BOX, 1024), id_o,
-                         kk > 0 || acc);
+                w_mma_ts(on, tmem + L::T_O + x * HD, tmem + L::T_S + x * KT + kk * 8, sdesc(w + kk * 2048, L::BOX, 1024),
+                         id_o, kk > 0 || acc);
         };
         auto free_slot = [&](int pos) { w_commit(on, empty0 + 8 * (pos % SLOTS)); };
         auto wait_p = [&](int x) {
@@ -446,11 +582,17 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             fence_after();
             return r;
         };
-        while (ok && walk.next(g)) {
-            const int n = g.j1 - g.j0;
+        int seg = 0;
+        for (;; ++seg) {
+            ok = seg_wait(seg);
+            if (!ok) break;
+            const Seg &d = s_seg[seg % SEGS];
+            const int n = d.n, nx[2] = {d.nx[0], d.nx[1]};
+            if (n == 0) break;
+            __syncwarp();
+            if (lane == 0) bar_arrive(g_empty0 + 8 * (seg % SEGS));
             const Ring at{ring, n, min(LEAD, n)};
             if constexpr (PAIR) {
-                const int nx[2] = {steps(g, 0), steps(g, 1)};
                 const int last = nx[1] > 0;
                 for (int t = -1; ok && t < n; ++t) {
 #pragma unroll
@@ -491,8 +633,8 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                     }
                 }
             }
+            if (!ok) break;
             ring += 2 * n;
-            ++seg;
         }
         if (seg > 0 || !ok) {     // no MMA outlives the CTA's tensor memory
             w_commit(on, drain);
@@ -500,25 +642,37 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             bar_wait_slow(drain, 0, &never, status);
         }
         __syncwarp();
-    } else if (warp < 8) {
+    }
+    } else {
         // ---- softmax -------------------------------------------------------
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         const int x = warp >> 2, m = threadIdx.x & 127;
         const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
         const uint32_t t_s = lanes + L::T_S + x * KT, t_o = lanes + L::T_O;
         uint32_t s_ph = 0, o_ph[2] = {0, 0};
-        int ring = 0, seg = 0;
-        bool dead = false;
+        int ring = 0;
+        bool dead = false;            // a wait ran out, here or in another role
+        auto wait = [&](uint32_t bar, uint32_t parity) {
+            if (!dead && !w_wait(bar, parity, &s_abort, status)) dead = true;
+        };
+        // both groups are here (twice a segment)
+        auto groups_sync = [&](uint32_t parity) {
+            fence_before();
+            bar_arrive(both);
+            wait(both, parity);
+            fence_after();
+        };
         // the query rows of a segment into its buffer (swizzled as the MMA reads them): a pair's groups load their
         // own tiles, else both load the one there is. Asked for while there is other work, handed over by give_q.
-        auto load_q = [&](const Segment &s, int index) {
+        auto load_q = [&](const Seg &d, int index) {
             constexpr int PIECES = L::QROWS * HD / 8, N = PAIR ? 128 : 256;               // of 16 bytes
-            const int pm0 = s.tile * ROWS + (PAIR ? x * TILE : 0), left = sched.rows[s.i] * G - pm0;
-            const bf16 *src = static_cast<const bf16 *>(a.q) + a.b.row_start[s.i] * a.ldq + (long)s.h * G * HD;
+            const int pm0 = d.m0 + (PAIR ? x * TILE : 0), left = d.rows * G - pm0;
+            const bf16 *src = static_cast<const bf16 *>(a.q) + d.start * a.ldq + (long)d.h * G * HD;
             const uint32_t dst = base + L::Q + (PAIR ? x : index & 1) * L::QMAT;
-#pragma unroll
+#pragma unroll 4
             for (int p0 = 0; p0 < PIECES; p0 += N) {
                 const int p = p0 + (PAIR ? m : (int)threadIdx.x), row = p / (HD / 8), c = p % (HD / 8);
-                const int pm = pm0 + row, r = pm / G;
+                const int pm = pm0 + row, r = group_div(a, pm);
                 if (PIECES % N == 0 || p < PIECES)
                     copy16(dst + (c >> 3) * L::QBOX + row * 128 + (((c & 7) ^ (row & 7)) << 4),
                            row < left ? src + r * a.ldq + (pm - r * G) * HD + 8 * c : src, row < left);
@@ -529,51 +683,53 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             fence_proxy();
             bar_arrive(q_full0 + (PAIR ? 8 * x : 0));
         };
-        Segment g_next;
-        bool have = walk.next(g), have_next = false, q_next = false;
-        if (have && steps(g, PAIR ? x : 0) > 0) {
-            load_q(g, 0);
+        if (!seg_wait(0)) dead = true;
+        if (!dead && s_seg[0].nx[PAIR ? x : 0] > 0 && s_seg[0].n > 0) {
+            load_q(s_seg[0], 0);
             give_q();
         }
-        while (have) {
-            have_next = walk.next(g_next);
-            q_next = have_next && steps(g_next, PAIR ? x : 0) > 0;
-            const int n = g.j1 - g.j0, nx = steps(g, x), n_other = steps(g, x ^ 1);
+        for (int seg = 0; !dead; ++seg) {
+            const Seg &d = s_seg[seg % SEGS];
+            const int n = d.n, nx = d.nx[x];
+            if (n == 0) break;
             const Ring at{ring, n, min(LEAD, n)};
-            const int pm0 = g.tile * ROWS + (PAIR ? x * TILE : 0), pm = pm0 + m;
-            Rows rw;
-            rw.len = sched.len[g.i];
-            rw.rows = sched.rows[g.i];
-            rw.base = rw.len - rw.rows;
-            rw.live = a.mask && a.n_nodes ? min(rw.rows, a.n_nodes[g.i]) : rw.rows;
-            rw.r_first = pm0 / G;
-            rw.r_last = (min(pm0 + L::QROWS, rw.rows * G) - 1) / G;
-            const bool valid = m < L::QROWS && pm < rw.rows * G;
-            const int r = pm / G;
-            rw.r = valid && r < rw.live ? r : -1;
-            rw.seq_i = g.i;
-            rw.place = rw.base + r;
-            rw.mrow = nullptr;
+            ring += 2 * n;
+            const int pm0 = d.m0 + (PAIR ? x * TILE : 0), pm = pm0 + m, r = group_div(a, pm);
+            const bool valid = m < L::QROWS && pm < d.rows * G;
+            Row rw;
+            rw.r = valid && r < d.live ? r : -1;
+            rw.place = d.base + r;
+            rw.mask = nullptr;
             if (a.mask && rw.r >= 0) {
-                rw.mrow = a.mask + ((long)g.i * a.nodes + r) * a.words;
-                rw.place = rw.base + (a.window ? a.depth[(long)g.i * a.nodes + r] : 0);
+                rw.mask = a.mask + ((long)d.i * a.nodes + r) * a.words;
+                if (a.window) rw.place = d.base + a.depth[(long)d.i * a.nodes + r];
             }
+            // every row that sees anything sees a whole tile that ends here at the latest, and starts here at the earliest
+            const int full_end = d.base + (a.mask ? 0 : group_div(a, pm0) + 1);
+            const int full_start = !a.window ? 0
+                                   : d.base + (a.mask ? a.nodes : group_div(a, min(pm0 + L::QROWS, d.rows * G) - 1)) - a.window + 1;
             const bool any = __any_sync(0xffffffffu, rw.r >= 0), blind = __any_sync(0xffffffffu, valid && rw.r < 0);
+            bool q_next = false;
             float m_ref = -INFINITY, sum = 0.f;
+            auto next_q = [&]() {
+                wait(g_full0 + 8 * ((seg + 1) % SEGS), (uint32_t)((seg + 1) / SEGS) & 1u);
+                const Seg &e = s_seg[(seg + 1) % SEGS];
+                q_next = !dead && e.n > 0 && e.nx[PAIR ? x : 0] > 0;
+                if (q_next) load_q(e, seg + 1);
+            };
             for (int t = 0; t < nx; ++t) {
-                const int tt = PAIR ? t : 2 * t + x, key0 = key_of(g, tt);
-                if (!dead && !w_wait(s_full0 + 8 * x, s_ph, &s_abort, status)) dead = true;
+                const int tt = PAIR ? t : 2 * t + x, key0 = d.key(tt);
+                wait(s_full0 + 8 * x, s_ph);
                 s_ph ^= 1u;
                 fence_after();
-                if (t == nx - 1 && q_next) load_q(g_next, seg + 1);       // (all of this segment's S that read the buffer are done)
-                const bool full = tile_full(a, rw, key0);
+                const bool full = key0 + KT <= full_end && (key0 >= full_start || key0 + KT <= a.sinks);
                 if (any) {
                     uint32_t s[128];
-                    tmem_ld64(t_s, s);
-                    tmem_ld64(t_s + 64, s + 64);
-                    if (!full || blind) {
+                    tmem_ld128(t_s, s);
+                    const bool hide = !full || blind;
+                    if (hide) {
                         uint32_t w[4];
-                        seen_bits(a, rw, key0, w);
+                        seen_bits(a, d, rw, key0, w);
 #pragma unroll
                         for (int c = 0; c < 128; ++c)
                             if (!(w[c >> 5] >> (c & 31) & 1u)) s[c] = 0xff800000u;
@@ -583,16 +739,16 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                     for (int c = 0; c < 128; c += 8) {
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            top[k] = fmaxf(top[k], fmaxf(__uint_as_float(s[c + k]), __uint_as_float(s[c + 4 + k])));
+                            top[k] = max3_nan(top[k], __uint_as_float(s[c + k]), __uint_as_float(s[c + 4 + k]));
                     }
-                    const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
+                    const float now = max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]) * a.scale_log2;
                     const bool move = m_ref != -INFINITY && now > m_ref + RESCALE_LOG2;
                     if (__any_sync(0xffffffffu, move)) {
                         // (S of this tile has landed, so has the P V issued before it)
                         const float f = move ? ex2_fast(m_ref - now) : 1.f;
                         sum *= f;
                         if (move) m_ref = now;
-#pragma unroll
+#pragma unroll 1
                         for (int c = 0; c < HD; c += 32) {
                             uint32_t o[32];
                             tmem_ld32(t_o + x * HD + c, o);
@@ -601,168 +757,134 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                             tmem_st32(t_o + x * HD + c, o);
                         }
                     }
-                    if (m_ref == -INFINITY) m_ref = now;
+                    if (m_ref == -INFINITY || now != now) m_ref = now;       // (not a number: so are the row's weights)
                     const float use = m_ref == -INFINITY ? 0.f : m_ref;
                     uint64_t part[4] = {0, 0, 0, 0};
-                    const uint64_t scale2 = pack2(__float_as_uint(a.scale_log2), __float_as_uint(a.scale_log2));
-                    const uint64_t use2 = pack2(__float_as_uint(-use), __float_as_uint(-use));
+                    const uint64_t scale2 = pack2f(a.scale_log2, a.scale_log2), use2 = pack2f(-use, -use);
+                    // POLY of 8 pairs on the FMA pipes; in a tile with hidden keys none (-inf has to give 0)
+                    auto weights = [&](auto poly) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t p[32];
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t p[32];
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) {
-                            const uint64_t z = fma2(pack2(s[64 * h + 2 * c], s[64 * h + 2 * c + 1]), scale2, use2);
-                            const float e0 = ex2_fast(lo2(z)), e1 = ex2_fast(hi2(z));
-                            part[c & 3] = add2(part[c & 3], pack2(__float_as_uint(e0), __float_as_uint(e1)));
-                            const __nv_bfloat162 b = __floats2bfloat162_rn(e0, e1);
-                            p[c] = *reinterpret_cast<const uint32_t *>(&b);
+                            for (int c = 0; c < 32; ++c) {
+                                const uint64_t z = fma2(pack2(s[64 * h + 2 * c], s[64 * h + 2 * c + 1]), scale2, use2);
+                                float e0, e1;
+                                if ((c & 7) < decltype(poly)::value) {
+                                    ex2_pair(z, e0, e1);
+                                } else {
+                                    e0 = ex2_fast(lo2(z));
+                                    e1 = ex2_fast(hi2(z));
+                                }
+                                part[c & 3] = add2(part[c & 3], pack2f(e0, e1));
+                                const __nv_bfloat162 b = __floats2bfloat162_rn(e0, e1);
+                                p[c] = *reinterpret_cast<const uint32_t *>(&b);
+                            }
+                            tmem_st32(t_s + 32 * h, p);
                         }
-                        tmem_st32(t_s + 32 * h, p);
-                    }
+                    };
+                    if (PAIR && !hide) weights(std::integral_constant<int, POLY>());
+                    else weights(std::integral_constant<int, 0>());
                     const uint64_t all = add2(add2(part[0], part[1]), add2(part[2], part[3]));
                     sum += lo2(all) + hi2(all);
                 }
                 if (!full) {
-                    // V as the MMA will read it: nothing past the sequence's end, nothing that is not finite
                     const int pos = at.v(tt);
-                    if (!dead && !w_wait(full0 + 8 * (pos % SLOTS), (uint32_t)(pos / SLOTS) & 1u, &s_abort, status)) dead = true;
-                    uint8_t *row = sm + L::RING + (pos % SLOTS) * L::MAT + m * 128;
-                    const bool held = key0 + m < rw.len;
-#pragma unroll
-                    for (int b = 0; b < L::NB; ++b)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            uint4 *q = reinterpret_cast<uint4 *>(row + b * L::BOX + (((i + lane) & 7) << 4));
-                            if (!held) {
-                                *q = make_uint4(0, 0, 0, 0);
-                                continue;
-                            }
-                            const uint4 u = *q;
-                            uint32_t w[4] = {u.x, u.y, u.z, u.w}, bad = 0;
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                if ((w[k] & 0x7f80u) == 0x7f80u) { w[k] &= 0xffff0000u; bad = 1; }
-                                if ((w[k] & 0x7f800000u) == 0x7f800000u) { w[k] &= 0x0000ffffu; bad = 1; }
-                            }
-                            if (bad) {
-                                atomicOr(&s_odd, 1u << (seg & 31));
-                                __threadfence_block();
-                                *q = make_uint4(w[0], w[1], w[2], w[3]);
-                            }
-                        }
+                    wait(full0 + 8 * (pos % SLOTS), (uint32_t)(pos / SLOTS) & 1u);
+                    clean_row<L::NB>(sm + L::RING + (pos % SLOTS) * L::MAT + m * 128, L::BOX, lane, key0 + m < d.len, &s_odd,
+                                     1u << (seg & 31));
                     fence_proxy();
                 }
                 fence_before();
                 bar_arrive(p_full0 + 8 * x);
+                if (t == nx - 1) next_q();           // (all of this segment's S that read the buffer are done)
             }
-            if (q_next) {
-                if (nx == 0) load_q(g_next, seg + 1);
-                give_q();
-            }
-            ring += 2 * n;
+            if (nx == 0) next_q();
+            if (q_next) give_q();
 
             // the item's end: this group's O, or half the columns of both groups' O joined
-            const bool whole = segment_whole(g);
-            const int head = g.h * G + pm - r * G;
-            const long row = a.b.row_start[g.i] + r;
-            const long part = part_slot(g, blockIdx.x) * ROWS + (PAIR ? x * TILE : 0) + m;     // (of a valid row)
             float f0 = 1.f, f1 = 0.f;
             if (nx > 0) {
-                if (!dead && !w_wait(o_full0 + 8 * x, o_ph[x], &s_abort, status)) dead = true;
+                wait(o_full0 + 8 * x, o_ph[x]);
                 o_ph[x] ^= 1u;
             }
             if constexpr (!PAIR) {
-                if (n_other > 0) {
-                    if (!dead && !w_wait(o_full0 + 8 * (x ^ 1), o_ph[x ^ 1], &s_abort, status)) dead = true;
+                if (d.nx[x ^ 1] > 0) {
+                    wait(o_full0 + 8 * (x ^ 1), o_ph[x ^ 1]);
                     o_ph[x ^ 1] ^= 1u;
                 }
                 s_ml[x * TILE + m] = make_float2(m_ref, sum);
-                groups_sync();
+                groups_sync(0);
                 const float2 a0 = s_ml[m], a1 = s_ml[TILE + m];
                 const float top = fmaxf(a0.x, a1.x), use = top == -INFINITY ? 0.f : top;
-                f0 = a0.x == top ? 1.f : ex2_fast(a0.x - use);
-                f1 = a1.x == top ? 1.f : ex2_fast(a1.x - use);
-                if (a0.y == 0.f) f0 = 0.f;                        // (nothing seen: 0 times nothing)
-                if (a1.y == 0.f) f1 = 0.f;
+                f0 = a0.y == 0.f ? 0.f : a0.x == top ? 1.f : ex2_fast(a0.x - use);       // (nothing seen: 0 times nothing)
+                f1 = a1.y == 0.f ? 0.f : a1.x == top ? 1.f : ex2_fast(a1.x - use);
                 m_ref = top;
                 sum = (a0.y == 0.f ? 0.f : a0.y * f0) + (a1.y == 0.f ? 0.f : a1.y * f1);
             }
             fence_after();
             constexpr int COLS = PAIR ? HD : HD / 2;
             const int col0 = PAIR ? 0 : x * COLS;
-            const bool two = !PAIR && n > 1, odd = s_odd >> (seg & 31) & 1u;
-            const bool none = sum == 0.f;                         // the row sees nothing: zeros, whatever O holds
-            const float inv = none ? 0.f : 1.f / sum;
-            if (PAIR && nx == 0) {
-                if (valid && !dead && !whole) *reinterpret_cast<float2 *>(a.part_ml + 2 * part) = make_float2(-INFINITY, 0.f);
-            } else {
+            const bool none = sum == 0.f;            // the row sees nothing: zeros, whatever O holds
+            const bool whole = d.whole, odd = s_odd >> (seg & 31) & 1u;
+            const int head = d.h * G + pm - r * G;
+            const long row = d.start + r, part = d.part + (PAIR ? x * TILE : 0) + m;
+            if (nx > 0 || !PAIR) {
+                const float inv = whole ? none ? 0.f : 1.f / sum : 1.f;
+                const uint64_t g0 = pack2f(f0 * inv, f0 * inv), g1 = pack2f(f1 * inv, f1 * inv);
+                bf16 *dst = static_cast<bf16 *>(a.out) + row * a.ldo + (long)head * HD + col0;
+                float *pdst = a.part_o + part * HD + col0;
+                const bool store = valid && !dead;
 #pragma unroll 1
                 for (int c = 0; c < COLS; c += 32) {
                     uint32_t o[32];
-                    float acc[32];
+                    uint64_t acc[16];
                     tmem_ld32(t_o + (PAIR ? x * HD : 0) + col0 + c, o);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k)
-                        acc[k] = none || (!PAIR && f0 == 0.f) ? 0.f : PAIR ? __uint_as_float(o[k]) : __uint_as_float(o[k]) * f0;
-                    if (two) {
+                    for (int k = 0; k < 16; ++k) acc[k] = f0 == 0.f || none ? 0ull : fma2(pack2(o[2 * k], o[2 * k + 1]), g0, 0ull);
+                    if (!PAIR && n > 1) {
                         tmem_ld32(t_o + HD + col0 + c, o);
 #pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            if (f1 != 0.f) acc[k] = fmaf(__uint_as_float(o[k]), f1, acc[k]);
+                        for (int k = 0; k < 16; ++k)
+                            if (f1 != 0.f) acc[k] = fma2(pack2(o[2 * k], o[2 * k + 1]), g1, acc[k]);
                     }
                     if (odd && rw.r >= 0) {
-                        // values of V that were taken out and that this row sees
-                        for (int t = 0; t < n; ++t) {
-                            const int key0 = key_of(g, t);
-                            if (key0 + KT <= rw.base + (a.mask ? 0 : 1) && !a.window) continue;      // seen in full by all rows
-                            uint32_t w[4];
-                            seen_bits(a, rw, key0, w);
-                            for (int k = 0; k < KT; ++k) {
-                                const int slot = key0 + k;
-                                if (slot >= rw.len || !(w[k >> 5] >> (k & 31) & 1u)) continue;
-                                const int id = v.table[(long)a.b.seqs[g.i] * v.max_pages + (slot >> v.page_shift)];
-                                if ((unsigned)id >= (unsigned)v.n_pages) continue;
-                                const bf16 *src = static_cast<const bf16 *>(v.kv) + ((long)a.layer * v.n_pages + id) * v.page_elems() +
-                                                  ((long)(v.kv_heads + g.h) * v.page + (slot & (v.page - 1))) * HD + col0 + c;
+#pragma unroll 1
+                        for (int e = 0; e < 32; e += 8) {
+                            float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                            add_odd(a, d, rw, HD, col0 + c + e, y);
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) {
-                                    const float y = __bfloat162float(src[e]);
-                                    if (!isfinite(y)) acc[e] += y;
-                                }
-                            }
+                            for (int k = 0; k < 16; ++k)
+                                if (k / 4 == e / 8) acc[k] = add2(acc[k], pack2f(y[2 * (k & 3)], y[2 * (k & 3) + 1]));
                         }
                     }
-                    if (!valid || dead) continue;
+                    if (!store) continue;
                     if (whole) {
-                        bf16 *dst = static_cast<bf16 *>(a.out) + row * a.ldo + (long)head * HD + col0 + c;
 #pragma unroll
-                        for (int k = 0; k < 32; k += 8) {
+                        for (int k = 0; k < 16; k += 4) {
                             uint32_t u[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                const __nv_bfloat162 b = __floats2bfloat162_rn(acc[k + 2 * e] * inv, acc[k + 2 * e + 1] * inv);
+                                const __nv_bfloat162 b = __floats2bfloat162_rn(lo2(acc[k + e]), hi2(acc[k + e]));
                                 u[e] = *reinterpret_cast<const uint32_t *>(&b);
                             }
-                            *reinterpret_cast<uint4 *>(dst + k) = make_uint4(u[0], u[1], u[2], u[3]);
+                            *reinterpret_cast<uint4 *>(dst + c + 2 * k) = make_uint4(u[0], u[1], u[2], u[3]);
                         }
                     } else {
-                        float *dst = a.part_o + part * HD + col0 + c;
 #pragma unroll
-                        for (int k = 0; k < 32; k += 4)
-                            *reinterpret_cast<float4 *>(dst + k) = make_float4(acc[k], acc[k + 1], acc[k + 2], acc[k + 3]);
+                        for (int k = 0; k < 16; k += 2)
+                            *reinterpret_cast<float4 *>(pdst + c + 2 * k) =
+                                make_float4(lo2(acc[k]), hi2(acc[k]), lo2(acc[k + 1]), hi2(acc[k + 1]));
                     }
                 }
-                if (valid && !dead && (PAIR || x == 0)) {
-                    if (!whole) *reinterpret_cast<float2 *>(a.part_ml + 2 * part) = make_float2(m_ref, sum);
-                    else if (a.lse)
-                        a.lse[row * v.heads + head] = sum == 0.f ? -INFINITY : (m_ref + log2f(sum)) * 0.6931471805599453f;
-                }
             }
+            if (valid && !dead && (PAIR || x == 0)) {
+                if (!whole) *reinterpret_cast<float2 *>(a.part_ml + 2 * part) = make_float2(m_ref, sum);
+                else if (a.lse) a.lse[row * v.heads + head] = none ? -INFINITY : (m_ref + log2f(sum)) * 0.6931471805599453f;
+            }
+            bar_arrive(g_empty0 + 8 * (seg % SEGS));
             // the other group's O is not overwritten before this one has read it
-            if constexpr (!PAIR) groups_sync();
-            ++seg;
-            g = g_next;
-            have = have_next;
+            if constexpr (!PAIR) groups_sync(1);
         }
     }
     fence_before();
