@@ -413,12 +413,13 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(const PagesV
     }
 }
 
-// The tables and counts, a CTA per sequence, and the moves: a group of lanes holds one
-// (layer, K or V, head) of a sequence, a lane 16 bytes of every token, and takes the kept
-// tokens in order, U requested before any is stored. keep[j] >= j, so a token's old place is
-// never overwritten before the batch that holds it has been read, by the same lane.
+// The tables and counts, a CTA per sequence, and the moves. `lanes` threads hold one token's head of one (layer, K or
+// V, head), 16 bytes each; `side` tokens go side by side and U follow one another, all requested before any is stored
+// (side > 1: and the CTA's barrier between). keep[j] >= j, so a token's old place is not overwritten before the batch
+// that holds it has been read, and later batches lie behind it. Wide lists (side 16: 128 tokens a batch) are bound by
+// bytes; for an accepted path (side 1) a CTA takes 16 heads, and the round trips of the lookups bound it.
 template <int ESZ, int U>
-__global__ void __launch_bounds__(256) compact_apply_kernel(const PagesView v, const CompactArgs c, int groups) {
+__global__ void __launch_bounds__(256) compact_apply_kernel(const PagesView v, const CompactArgs c, int groups, int side) {
     wait_prior();
     allow_dependents();
     if (!c.flags[2]) return;
@@ -442,22 +443,21 @@ __global__ void __launch_bounds__(256) compact_apply_kernel(const PagesView v, c
         }
         if (threadIdx.x == 0) v.len[s] = after;
     }
-    const int lanes = v.head_dim * ESZ / 16;
-    const int group = blockIdx.y * (256 / lanes) + threadIdx.x / lanes, lane = threadIdx.x % lanes;
-    if (group >= groups) return;
+    const int lanes = v.head_dim * ESZ / 16, unit = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+    const int group = blockIdx.y * (256 / lanes / side) + unit / side, tok = unit % side;
     const int layer = group / (2 * v.kv_heads), kvh = group - layer * 2 * v.kv_heads;
     uint4 *kv = static_cast<uint4 *>(v.kv);
     const long pe16 = v.page_elems() * ESZ / 16;
     const long at0 = (long)layer * v.n_pages * pe16 + (long)kvh * v.page * lanes + lane;
     const int *keep = c.keep ? c.keep + (long)i * c.stride : nullptr;
-    for (int t0 = k0 << v.page_shift; t0 < after; t0 += U) {
+    for (int t0 = k0 << v.page_shift; t0 < after; t0 += U * side) {
         uint4 r[U];
         long to[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int t = t0 + u;
+            const int t = t0 + u * side + tok;
             to[u] = -1;
-            if (t < after) {
+            if (t < after && group < groups) {
                 const int k = t >> v.page_shift, rk = rank[k];
                 const int from = t < base || !keep ? t : base + keep[t - base];
                 const int of = old[from >> v.page_shift], in = rk >= 0 ? ids[rk] : old[k];
@@ -467,6 +467,7 @@ __global__ void __launch_bounds__(256) compact_apply_kernel(const PagesView v, c
                 }
             }
         }
+        if (side > 1) __syncthreads();
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (to[u] >= 0) kv[to[u]] = r[u];
@@ -577,18 +578,36 @@ struct RopeArgs {
     int layer, half;         // half: rotated pairs of a head
 };
 
+// G elements as they are in memory
 template <typename T, int G>
-__device__ __forceinline__ void load_run(const T *g, float *x) {
-    if constexpr (G == 1) {
-        x[0] = (float)*g;
-    } else {
+struct Run {
+    uint4 w[G * sizeof(T) / 16];
+    __device__ __forceinline__ void load(const T *g) {
 #pragma unroll
-        for (int e = 0; e < G; e += 4) {
-            const float4 f = Vec4<T>::load(g + e);
-            x[e] = f.x; x[e + 1] = f.y; x[e + 2] = f.z; x[e + 3] = f.w;
+        for (int i = 0; i < (int)(G * sizeof(T) / 16); ++i) w[i] = reinterpret_cast<const uint4 *>(g)[i];
+    }
+    __device__ __forceinline__ void to(float *x) const {
+#pragma unroll
+        for (int i = 0; i < (int)(G * sizeof(T) / 16); ++i) {
+            const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (sizeof(T) == 4) {
+                    x[4 * i + k] = __uint_as_float(u[k]);
+                } else {
+                    x[8 * i + 2 * k] = __uint_as_float(u[k] << 16);
+                    x[8 * i + 2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
+                }
+            }
         }
     }
-}
+};
+template <typename T>
+struct Run<T, 1> {
+    T w;
+    __device__ __forceinline__ void load(const T *g) { w = *g; }
+    __device__ __forceinline__ void to(float *x) const { x[0] = (float)w; }
+};
 
 template <typename T, int G>
 __device__ __forceinline__ void store_run(T *g, const float *x) {
@@ -610,18 +629,19 @@ __device__ __forceinline__ void store_run(T *g, const float *x) {
     }
 }
 
-// CTA (row, chunk of heads): a thread takes 2 G elements of a head, G of them and the G
-// that they pair with (past the rotated part: 2 G in a row). The angle in turns is the
-// product of the position and a 64-bit fraction mod 1, which whole-number arithmetic gives
-// exactly at any position; its upper 32 bits go to sincospi. Bytes bound it: the rows are
-// read and written once.
-template <typename TS, typename TD, int G>
+// CTA (RB rows, chunk of heads): a thread takes 2 G elements of a head of every row, G of them and the G that they pair
+// with (past the rotated part: 2 G in a row), all requested first; meanwhile a warp a row finds its slot (four dependent
+// loads) and the CTA the rows' sines. The angle in turns is the product of the position and a 64-bit fraction mod 1,
+// which whole-number arithmetic gives exactly at any position; its upper 32 bits go to sincospi. Bytes bound it: the
+// rows are read and written once.
+template <typename TS, typename TD, int G, int RB>
 __global__ void __launch_bounds__(256) rope_append_kernel(const PagesView v, const BatchView b,
                                                           const __grid_constant__ RopeTable rt, const RopeArgs a) {
-    __shared__ float2 s_cs[MAX_ROT_PAIRS];
+    __shared__ float2 s_cs[RB][MAX_ROT_PAIRS];
+    __shared__ long s_slot[RB];                               // elements from the layer's first to the row's K of head 0
     wait_prior();
     allow_dependents();
-    const int row = blockIdx.x, hd = v.head_dim;
+    const int row0 = blockIdx.x * RB, hd = v.head_dim, warp = threadIdx.x >> 5;
     const int units = hd / (2 * G), per = 256 / units;        // threads of a head, heads of a CTA
     const int heads = v.heads + 2 * v.kv_heads;
     const int head = blockIdx.y * per + threadIdx.x / units, unit = threadIdx.x % units;
@@ -629,54 +649,90 @@ __global__ void __launch_bounds__(256) rope_append_kernel(const PagesView v, con
     // first elements of the two runs
     const bool turns = unit * G < a.half;
     const int e0 = turns ? unit * G : 2 * a.half + 2 * (unit * G - a.half), e1 = turns ? e0 + a.half : e0 + G;
-    float x[G], y[G];
+    Run<TS, G> in0[RB], in1[RB];
     if (live) {
-        const TS *src = head < v.heads ? static_cast<const TS *>(a.q) + row * a.ldq + (long)head * hd
-                        : head < v.heads + v.kv_heads
-                            ? static_cast<const TS *>(a.k) + row * a.ldk + (long)(head - v.heads) * hd
-                            : static_cast<const TS *>(a.v) + row * a.ldv + (long)(head - v.heads - v.kv_heads) * hd;
-        load_run<TS, G>(src + e0, x);
-        load_run<TS, G>(src + e1, y);
+        const bool is_q = head < v.heads, is_k = !is_q && head < v.heads + v.kv_heads;
+        const TS *src = static_cast<const TS *>(is_q ? a.q : is_k ? a.k : a.v) +
+                        (long)(is_q ? head : is_k ? head - v.heads : head - v.heads - v.kv_heads) * hd;
+        const long ld = is_q ? a.ldq : is_k ? a.ldk : a.ldv;
+#pragma unroll
+        for (int u = 0; u < RB; ++u)
+            if (row0 + u < b.rows) {
+                in0[u].load(src + (row0 + u) * ld + e0);
+                in1[u].load(src + (row0 + u) * ld + e1);
+            }
     }
-    if (threadIdx.x < a.half) {
-        const int pair = threadIdx.x;
-        const long p = a.pos[rt.axis[pair] * a.pos_stride + row];
-        const int angle = (int)(((unsigned long long)p * rt.turn[pair]) >> 32);
-        float s, c;
-        sincospif((float)angle * 0x1p-31f, &s, &c);
-        s_cs[pair] = make_float2(c, s);
+    for (int e = threadIdx.x; e < RB * a.half; e += 256) {
+        const int u = e / a.half, pair = e - u * a.half;
+        if (row0 + u < b.rows) {
+            const long p = a.pos[rt.axis[pair] * a.pos_stride + row0 + u];
+            const int angle = (int)(((unsigned long long)p * rt.turn[pair]) >> 32);
+            float s, c;
+            sincospif((float)angle * 0x1p-31f, &s, &c);
+            s_cs[u][pair] = make_float2(c, s);
+        }
     }
-    // the row's sequence and slot
-    const int i = row_owner(b.row_start, b.n, row);
-    const int r = row - b.row_start[i], n = b.row_start[i + 1] - b.row_start[i], s = b.seqs[i];
-    TD *dst = nullptr;
-    if (live) {
-        if (head < v.heads) {
-            dst = static_cast<TD *>(a.out) + row * a.ldo + (long)head * hd;
-        } else if ((unsigned)s < (unsigned)v.max_seqs) {
+    if (warp < RB && row0 + warp < b.rows) {
+        const int row = row0 + warp, i = row_owner(b.row_start, b.n, row);
+        const int r = row - b.row_start[i], n = b.row_start[i + 1] - b.row_start[i], s = b.seqs[i];
+        long at = -1;
+        if ((unsigned)s < (unsigned)v.max_seqs) {
             const int len = v.len[s], slot = len - n + r;
-            if (r >= 0 && r < n && slot >= 0) {
+            if (r >= 0 && r < n && slot >= 0 && slot < (long)v.max_pages * v.page) {
                 const int id = v.table[(long)s * v.max_pages + (slot >> v.page_shift)];
-                if ((unsigned)id < (unsigned)v.n_pages)
-                    dst = static_cast<TD *>(v.kv) + ((long)a.layer * v.n_pages + id) * v.page_elems() +
-                          ((long)(head - v.heads) * v.page + (slot & (v.page - 1))) * hd;
+                if ((unsigned)id < (unsigned)v.n_pages) at = id * v.page_elems() + (slot & (v.page - 1)) * hd;
             }
         }
-        if (!dst) set_status(v.status, ST_RANGE);
-    }
-    __syncthreads();
-    if (!dst) return;
-    if (turns && head < v.heads + v.kv_heads) {
-#pragma unroll
-        for (int e = 0; e < G; ++e) {
-            const float2 cs = s_cs[unit * G + e];
-            const float u = x[e], w = y[e];
-            x[e] = u * cs.x - w * cs.y;
-            y[e] = w * cs.x + u * cs.y;
+        if ((threadIdx.x & 31) == 0) {
+            s_slot[warp] = at;
+            if (at < 0) set_status(v.status, ST_RANGE);
         }
     }
-    store_run<TD, G>(dst + e0, x);
-    store_run<TD, G>(dst + e1, y);
+    __syncthreads();
+    if (!live) return;
+    TD *kv = static_cast<TD *>(v.kv) + (long)a.layer * v.n_pages * v.page_elems() + (long)(head - v.heads) * v.page * hd;
+#pragma unroll
+    for (int u = 0; u < RB; ++u) {
+        if (row0 + u >= b.rows) break;
+        TD *dst;
+        if (head < v.heads) {
+            dst = static_cast<TD *>(a.out) + (row0 + u) * a.ldo + (long)head * hd;
+        } else {
+            if (s_slot[u] < 0) continue;
+            dst = kv + s_slot[u];
+        }
+        float x[G], y[G];
+        in0[u].to(x);
+        in1[u].to(y);
+        if (turns && head < v.heads + v.kv_heads) {
+#pragma unroll
+            for (int e = 0; e < G; ++e) {
+                const float2 cs = s_cs[u][unit * G + e];
+                const float f = x[e], w = y[e];
+                x[e] = f * cs.x - w * cs.y;
+                y[e] = w * cs.x + f * cs.y;
+            }
+        }
+        store_run<TD, G>(dst + e0, x);
+        store_run<TD, G>(dst + e1, y);
+    }
+}
+
+template <typename TS, typename TD>
+cudaError_t launch_rope(const msd_pages *p, const BatchView &b, const RopeArgs &a, cudaStream_t s) {
+    // runs of 8 elements where the rotated part allows it, else pair by pair
+    const int run = a.half % 8 == 0 ? 8 : 1;
+    const int per = 256 / (p->cfg.head_dim / (2 * run)), chunks = (p->cfg.n_heads + 2 * p->cfg.n_kv_heads + per - 1) / per;
+    auto go = [&](auto kernel, int rb) {
+        const cudaError_t e = launch_chain(kernel, dim3((b.rows + rb - 1) / rb, chunks), dim3(256), 0, s, p->v, b, p->rope, a);
+        note_launch();
+        return e;
+    };
+    // several rows to a CTA once they fill the SMs: more bytes in flight behind the same lookups
+    if (run == 1) return go(rope_append_kernel<TS, TD, 1, 1>, 1);
+    constexpr int RB = sizeof(TS) == 4 ? 4 : 8;
+    return (long)b.rows * chunks >= 4l * RB * p->sms ? go(rope_append_kernel<TS, TD, 8, RB>, RB)
+                                                     : go(rope_append_kernel<TS, TD, 8, 1>, 1);
 }
 
 }  // namespace
@@ -897,11 +953,13 @@ msd_status msd_pages_compact(msd_pages *p, const msd_batch *batch, const int32_t
     cudaError_t e = chain(compact_plan_kernel, dim3(b.n), PLAN_THREADS, s, p->v, b, c);
     if (e == cudaSuccess) {
         const int groups = p->cfg.n_layers * 2 * p->cfg.n_kv_heads;
-        const int per = 256 / (p->cfg.head_dim * (p->cfg.dtype == MSD_F32 ? 4 : 2) / 16);
-        const dim3 grid(b.n, (groups + per - 1) / per);
+        const int units = 256 / (p->cfg.head_dim * (p->cfg.dtype == MSD_F32 ? 4 : 2) / 16);
+        // lists of 64 and more side by side (16 lists of 1027, 8 layers of 8 heads: 287 us one by one)
+        const int side = keep && keep_stride < 64 ? 1 : std::min(units, 16);
+        const dim3 grid(b.n, (groups + units / side - 1) / (units / side));
         if (grid.y > 65535) return pfail(p, MSD_ERR_INVALID, "more layers and heads than a launch takes");
-        e = p->cfg.dtype == MSD_F32 ? chain(compact_apply_kernel<4, 8>, grid, 256, s, p->v, c, groups)
-                                    : chain(compact_apply_kernel<2, 8>, grid, 256, s, p->v, c, groups);
+        e = p->cfg.dtype == MSD_F32 ? chain(compact_apply_kernel<4, 8>, grid, 256, s, p->v, c, groups, side)
+                                    : chain(compact_apply_kernel<2, 8>, grid, 256, s, p->v, c, groups, side);
     }
     return leave(p, e);
 }
@@ -949,21 +1007,9 @@ msd_status msd_rope_append(msd_pages *p, int32_t layer, const msd_batch *batch, 
     if (b.rows == 0) return MSD_OK;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const RopeArgs a{q, k, v, (long)ldq, (long)ldk, (long)ldv, pos, (long)pos_stride, out, (long)ldo, layer, c.rot_dim / 2};
-    // runs of 8 elements where the rotated part allows it, else pair by pair
-    const int run = a.half % 8 == 0 ? 8 : 1;
-    const int per = 256 / (c.head_dim / (2 * run));
-    const dim3 grid(b.rows, (c.n_heads + 2 * c.n_kv_heads + per - 1) / per);
-    cudaError_t e;
-    if (c.dtype == MSD_F32)
-        e = run == 8 ? chain(rope_append_kernel<float, float, 8>, grid, 256, s, p->v, b, p->rope, a)
-                     : chain(rope_append_kernel<float, float, 1>, grid, 256, s, p->v, b, p->rope, a);
-    else if (src_dtype == MSD_F32)
-        e = run == 8 ? chain(rope_append_kernel<float, bf16, 8>, grid, 256, s, p->v, b, p->rope, a)
-                     : chain(rope_append_kernel<float, bf16, 1>, grid, 256, s, p->v, b, p->rope, a);
-    else
-        e = run == 8 ? chain(rope_append_kernel<bf16, bf16, 8>, grid, 256, s, p->v, b, p->rope, a)
-                     : chain(rope_append_kernel<bf16, bf16, 1>, grid, 256, s, p->v, b, p->rope, a);
-    return leave(p, e);
+    return leave(p, c.dtype == MSD_F32       ? launch_rope<float, float>(p, b, a, s)
+                    : src_dtype == MSD_F32 ? launch_rope<float, bf16>(p, b, a, s)
+                                           : launch_rope<bf16, bf16>(p, b, a, s));
 }
 
 msd_status msd_pages_attention(msd_pages *p, int32_t layer, const msd_batch *batch, const msd_tree *tree,

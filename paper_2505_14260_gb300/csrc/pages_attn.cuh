@@ -53,15 +53,23 @@ struct Segment {
     TileRange range;
 };
 
-// Fills s (whole CTA, THREADS threads; ends with a barrier). Sequences that cannot be read
+// Up to so many sequences one warp lays out a CTA's run, without the CTA's barriers.
+constexpr int ATTN_WARP_SEQS = 64;
+
+// Fills s (by THREADS threads: the whole CTA or its one warp; ends with a barrier among them). Sequences that cannot be read
 // (ids, lengths or row counts out of range) get no steps and set the status word.
 template <int ROWS, int KT, int THREADS>
 __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int ctas) {
     __shared__ long long s_sum[THREADS / 32];
+    auto sync = [] {
+        if constexpr (THREADS == 32) __syncwarp();
+        else __syncthreads();
+    };
+    const int tid = THREADS == 32 ? threadIdx.x & 31 : threadIdx.x;
     const PagesView &v = a.pv;
-    const int G = a.group, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int G = a.group, lane = tid & 31, warp = tid >> 5;
     constexpr int NW = THREADS / 32;
-    for (int i = threadIdx.x; i < a.b.n; i += THREADS) {
+    for (int i = tid; i < a.b.n; i += THREADS) {
         const int seq = a.b.seqs[i], r0 = a.b.row_start[i], r1 = a.b.row_start[i + 1];
         int len = 0, rows = r1 - r0;
         bool ok = (unsigned)seq < (unsigned)v.max_seqs && r0 >= 0 && rows >= 0 && r1 <= a.b.rows;
@@ -76,16 +84,16 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
         s.len[i] = len;
         s.rows[i] = rows;
     }
-    __syncthreads();
+    sync();
     // steps of each sequence: a thread's own loop over few tiles, a warp's over many
-    for (int i = threadIdx.x; i < a.b.n; i += THREADS) {
+    for (int i = tid; i < a.b.n; i += THREADS) {
         const int tiles = (s.rows[i] * G + ROWS - 1) / ROWS;
         long long w = 0;
         if (tiles <= 4)
             for (int t = 0; t < tiles; ++t) w += ITEM_STEPS + tile_range<ROWS, KT>(a, s.len[i], s.rows[i], t).steps;
         s.pre[i + 1] = w * v.kv_heads;
     }
-    __syncthreads();
+    sync();
     for (int i = warp; i < a.b.n; i += NW) {
         const int tiles = (s.rows[i] * G + ROWS - 1) / ROWS;
         if (tiles <= 4) continue;
@@ -95,11 +103,11 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
         for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
         if (lane == 0) s.pre[i + 1] = w * v.kv_heads;
     }
-    __syncthreads();
+    sync();
     // inclusive sums
     long long carry = 0;
     for (int i0 = 0; i0 < a.b.n; i0 += THREADS) {
-        const int i = i0 + threadIdx.x;
+        const int i = i0 + tid;
         long long x = i < a.b.n ? s.pre[i + 1] : 0;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -107,18 +115,18 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
             if (lane >= o) x += y;
         }
         if (lane == 31) s_sum[warp] = x;
-        __syncthreads();
+        sync();
         long long before = carry;
         for (int w = 0; w < NW; ++w) {
             if (w < warp) before += s_sum[w];
             carry += s_sum[w];
         }
         if (i < a.b.n) s.pre[i + 1] = before + x;
-        __syncthreads();
+        sync();
     }
-    if (threadIdx.x == 0) s.pre[0] = 0;
+    if (tid == 0) s.pre[0] = 0;
     const long long per = max(1ll, (carry + ctas - 1) / ctas), x0 = per * cta;
-    __syncthreads();
+    sync();
     if (warp == 0) {
         int4 f = make_int4(-1, 0, 0, 0);
         if (x0 < carry) {
@@ -157,7 +165,7 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
             s.per = per;
         }
     }
-    __syncthreads();
+    sync();
 }
 
 // The segments of a CTA's run, in order: every role of the CTA walks them by itself.

@@ -35,7 +35,9 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
     AttnSched &sched = *reinterpret_cast<AttnSched *>(sm + L::SCHED);
     wait_prior();
     allow_dependents();
-    attn_schedule<ROWS, KT, THREADS>(a, sched, blockIdx.x, gridDim.x);
+    if (a.b.n > ATTN_WARP_SEQS) attn_schedule<ROWS, KT, THREADS>(a, sched, blockIdx.x, gridDim.x);
+    else if (threadIdx.x < 32) attn_schedule<ROWS, KT, 32>(a, sched, blockIdx.x, gridDim.x);
+    __syncthreads();
     const PagesView &v = a.pv;
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, G = a.group;
     if (tid == 0) name_parts<ROWS, KT>(a, sched, blockIdx.x);
@@ -208,37 +210,66 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
     }
 }
 
-// Joins the partial results of items that several CTAs worked on, in the order of the keys:
-// block (CTA that ended an item, rows), a warp a row.
+// Joins the partial results of items that several CTAs worked on: block (CTA that ended an item, rows), a warp
+// a row. A lane holds the weight of a part (32 at a time), then the parts' O are added in the order of the keys,
+// eight requested at once.
 template <typename T, int HD>
 __global__ void __launch_bounds__(32 * JOIN_WARPS) pages_attn_join_kernel(const PagesAttn a, int tile_rows) {
     wait_prior();
     allow_dependents();
     const int4 item = a.part_item[blockIdx.x];
     if (item.x < 0) return;
-    const PagesView &v = a.pv;
     const int G = a.group, lane = threadIdx.x & 31;
     const int m = blockIdx.y * JOIN_WARPS + (threadIdx.x >> 5);
     const int start = a.b.row_start[item.x], rows = a.b.row_start[item.x + 1] - start;
     const int pm = item.z * tile_rows + m;
-    if (m >= tile_rows || pm >= rows * G) return;
+    if (pm >= rows * G) return;
     constexpr int E = HD / 32;
-    float acc[E] = {}, mx = -INFINITY, sum = 0.f;
-    for (int c = item.w; c <= (int)blockIdx.x; ++c) {
-        const long at = (2l * c + (c == item.w ? 1 : 0)) * tile_rows + m;
-        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * at);
-        float x[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = a.part_o[at * HD + lane * E + e];
-        if (ml.y == 0.f) continue;                    // nothing seen there
-        const float now = fmaxf(mx, ml.x);
-        const float f = mx == now ? 1.f : exp2f(mx - now), w = ml.x == now ? 1.f : exp2f(ml.x - now);
-        mx = now;
-        sum = sum * f + ml.y * w;
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = acc[e] * f + (w == 0.f ? 0.f : x[e] * w);
+    const int c0 = item.w, parts = (int)blockIdx.x - c0 + 1;
+    auto at = [&](int k) { return (2l * (c0 + k) + (k == 0 ? 1 : 0)) * tile_rows + m; };
+    float top = -INFINITY;
+    for (int k = lane; k < parts; k += 32) {
+        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * at(k));
+        if (ml.y != 0.f) top = fmaxf(top, ml.x);
     }
-    const int r = start + pm / G, head = item.y * G + pm % G;
+    top = warp_max(top);
+    float acc[E] = {}, sum = 0.f;
+    for (int k0 = 0; k0 < parts; k0 += 32) {
+        float w = 0.f;
+        if (k0 + lane < parts) {
+            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * at(k0 + lane));
+            if (ml.y != 0.f) {                        // (else nothing was seen there)
+                w = ml.x == top ? 1.f : exp2f(ml.x - top);
+                sum += ml.y * w;
+            }
+        }
+        const int n = min(32, parts - k0);
+        for (int k = 0; k < n; k += 8) {
+            float x[8][E];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (k + u < n) {
+                    const float *src = a.part_o + at(k0 + k + u) * HD + lane * E;
+                    if constexpr (E == 4) {
+                        const float4 y = *reinterpret_cast<const float4 *>(src);
+                        x[u][0] = y.x; x[u][1] = y.y; x[u][2] = y.z; x[u][3] = y.w;
+                    } else {
+                        const float2 y = *reinterpret_cast<const float2 *>(src);
+                        x[u][0] = y.x; x[u][1] = y.y;
+                    }
+                }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float wu = __shfl_sync(0xffffffffu, w, (k + u) & 31);
+                if (k + u < n && wu != 0.f) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) acc[e] = fmaf(x[u][e], wu, acc[e]);
+                }
+            }
+        }
+    }
+    sum = warp_sum(sum);
+    const int r = start + group_div(a, pm), head = item.y * G + pm - group_div(a, pm) * G;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     T *out = static_cast<T *>(a.out) + r * a.ldo + (long)head * HD + lane * E;
     if constexpr (sizeof(T) == 4) {
@@ -250,7 +281,7 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) pages_attn_join_kernel(const 
             *reinterpret_cast<__nv_bfloat162 *>(out + e) = __floats2bfloat162_rn(acc[e] * inv, acc[e + 1] * inv);
     }
     if (a.lse && lane == 0)
-        a.lse[(long)r * v.heads + head] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.6931471805599453f;
+        a.lse[(long)r * a.pv.heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
 template <int HD>

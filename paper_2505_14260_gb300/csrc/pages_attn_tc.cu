@@ -35,7 +35,6 @@ namespace {
 constexpr int KT = 128, THREADS = 384, TILE = 128, SEGS = 8;
 constexpr unsigned long long TIMEOUT_NS = 2000000000ull;
 constexpr float RESCALE_LOG2 = 8.f;
-constexpr int POLY = 2;               // pairs of 8 whose exponentials the FMA pipes take
 
 // ROWS: packed rows of an item. 256: a pair of tiles. Fewer than 128: the MMA still takes 128 rows; what
 // it reads past the ones there are gives rows of S that nobody looks at, and the shared memory that
@@ -175,7 +174,6 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     return d;
 }
 __device__ __forceinline__ uint64_t pack2f(float lo, float hi) { return pack2(__float_as_uint(lo), __float_as_uint(hi)); }
-__device__ __forceinline__ uint64_t neg2(uint64_t v) { return v ^ 0x8000000080000000ull; }
 __device__ __forceinline__ float lo2(uint64_t v) { return __uint_as_float((uint32_t)v); }
 __device__ __forceinline__ float hi2(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
 // the largest of three, or NaN if one is
@@ -369,22 +367,6 @@ __device__ __forceinline__ void clean_row(uint8_t *row, uint32_t box, int lane, 
     }
 }
 
-// 2^z of two values on the FMA pipes, -126 <= z <= 127: z = n + f with n whole and |f| <= 1/2, a polynomial of degree 4
-// in f (least largest relative error, 2.6e-6; fitted by exchange), n added to the exponent. The exponential unit takes a
-// warp's values at a quarter of the rate of the FMA pipes' pairs, and is what a tile's softmax waits for.
-__device__ __forceinline__ void ex2_pair(uint64_t z, float &e0, float &e1) {
-    const uint64_t floor2 = pack2f(-126.f, -126.f), magic = pack2f(12582912.f, 12582912.f);
-    const uint64_t zc = pack2f(fmaxf(lo2(z), lo2(floor2)), fmaxf(hi2(z), hi2(floor2)));
-    const uint64_t t = add2(zc, magic);                             // 1.5 2^23 + n
-    const uint64_t f = add2(zc, neg2(add2(t, neg2(magic))));
-    uint64_t p = fma2(f, pack2f(0.009570102207362652f, 0.009570102207362652f), pack2f(0.05591785907745361f, 0.05591785907745361f));
-    p = fma2(p, f, pack2f(0.240247443318367f, 0.240247443318367f));
-    p = fma2(p, f, pack2f(0.6931217908859253f, 0.6931217908859253f));
-    p = fma2(p, f, pack2f(0.9999992847442627f, 0.9999992847442627f));
-    e0 = __uint_as_float((uint32_t)p + ((uint32_t)t << 23));
-    e1 = __uint_as_float((uint32_t)(p >> 32) + ((uint32_t)(t >> 32) << 23));
-}
-
 // Where the ring holds a segment's tiles: K tiles run `lead` ahead of V tiles.
 struct Ring {
     int base, n, lead;
@@ -441,7 +423,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
     }
     wait_prior();
     allow_dependents();
-    attn_schedule<ROWS, KT, THREADS>(a, sched, blockIdx.x, gridDim.x);
+    if (a.b.n > ATTN_WARP_SEQS) attn_schedule<ROWS, KT, THREADS>(a, sched, blockIdx.x, gridDim.x);
     fence_before();
     __syncthreads();
     fence_after();
@@ -455,6 +437,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 10) {
         // ---- segments ------------------------------------------------------
+        if (a.b.n <= ATTN_WARP_SEQS) attn_schedule<ROWS, KT, 32>(a, sched, blockIdx.x, gridDim.x);
         AttnWalk<ROWS, KT> walk(a, sched);
         Segment g;
         for (int i = 0;; ++i) {
@@ -761,30 +744,19 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                     const float use = m_ref == -INFINITY ? 0.f : m_ref;
                     uint64_t part[4] = {0, 0, 0, 0};
                     const uint64_t scale2 = pack2f(a.scale_log2, a.scale_log2), use2 = pack2f(-use, -use);
-                    // POLY of 8 pairs on the FMA pipes; in a tile with hidden keys none (-inf has to give 0)
-                    auto weights = [&](auto poly) {
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            uint32_t p[32];
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t p[32];
 #pragma unroll
-                            for (int c = 0; c < 32; ++c) {
-                                const uint64_t z = fma2(pack2(s[64 * h + 2 * c], s[64 * h + 2 * c + 1]), scale2, use2);
-                                float e0, e1;
-                                if ((c & 7) < decltype(poly)::value) {
-                                    ex2_pair(z, e0, e1);
-                                } else {
-                                    e0 = ex2_fast(lo2(z));
-                                    e1 = ex2_fast(hi2(z));
-                                }
-                                part[c & 3] = add2(part[c & 3], pack2f(e0, e1));
-                                const __nv_bfloat162 b = __floats2bfloat162_rn(e0, e1);
-                                p[c] = *reinterpret_cast<const uint32_t *>(&b);
-                            }
-                            tmem_st32(t_s + 32 * h, p);
+                        for (int c = 0; c < 32; ++c) {
+                            const uint64_t z = fma2(pack2(s[64 * h + 2 * c], s[64 * h + 2 * c + 1]), scale2, use2);
+                            const float e0 = ex2_fast(lo2(z)), e1 = ex2_fast(hi2(z));
+                            part[c & 3] = add2(part[c & 3], pack2f(e0, e1));
+                            const __nv_bfloat162 b = __floats2bfloat162_rn(e0, e1);
+                            p[c] = *reinterpret_cast<const uint32_t *>(&b);
                         }
-                    };
-                    if (PAIR && !hide) weights(std::integral_constant<int, POLY>());
-                    else weights(std::integral_constant<int, 0>());
+                        tmem_st32(t_s + 32 * h, p);
+                    }
                     const uint64_t all = add2(add2(part[0], part[1]), add2(part[2], part[3]));
                     sum += lo2(all) + hi2(all);
                 }
