@@ -568,6 +568,9 @@ __global__ void __launch_bounds__(SPAN_TILE) positions_kernel(const PagesView v,
 
 // ---- rotation and append ---------------------------------------------------
 
+constexpr int ROPE_P = 4;               // rows of a thread in a call of at least ROPE_LARGE elements an SM
+constexpr long ROPE_LARGE = 16 * 1536 * ROPE_P;
+
 struct RopeArgs {
     const void *q, *k, *v;
     long ldq, ldk, ldv;
@@ -629,110 +632,114 @@ __device__ __forceinline__ void store_run(T *g, const float *x) {
     }
 }
 
-// CTA (RB rows, chunk of heads): a thread takes 2 G elements of a head of every row, G of them and the G that they pair
-// with (past the rotated part: 2 G in a row), all requested first; meanwhile a warp a row finds its slot (four dependent
-// loads) and the CTA the rows' sines. The angle in turns is the product of the position and a 64-bit fraction mod 1,
+// The slot of a row of listed sequence i: elements from the layer's first to its K of head 0, or -1.
+__device__ __forceinline__ long slot_of(const PagesView &v, const BatchView &b, int i, int row) {
+    const int r = row - b.row_start[i], n = b.row_start[i + 1] - b.row_start[i], s = b.seqs[i];
+    if ((unsigned)s >= (unsigned)v.max_seqs) return -1;
+    const int slot = v.len[s] - n + r;
+    if (r < 0 || r >= n || slot < 0 || slot >= (long)v.max_pages * v.page) return -1;
+    const int id = v.table[(long)s * v.max_pages + (slot >> v.page_shift)];
+    return (unsigned)id < (unsigned)v.n_pages ? id * v.page_elems() + (slot & (v.page - 1)) * v.head_dim : -1;
+}
+
+constexpr int ROPE_ROWS = 32, ROPE_THREADS = 512;      // of a CTA, at most
+
+// CTA (P * side rows, a chunk of heads): a thread takes 2 G elements of one head, G of them and the G that they pair
+// with (past the rotated part: 2 G in a row), of P rows, all requested first; where a row's heads do not fill the CTA,
+// `side` rows lie side by side. Meanwhile a warp a row finds its slot (four dependent loads; only where the chunk has K or
+// V heads) and the CTA the rows' sines. The angle in turns is the product of the position and a 64-bit fraction mod 1,
 // which whole-number arithmetic gives exactly at any position; its upper 32 bits go to sincospi. Bytes bound it: the
 // rows are read and written once.
-template <typename TS, typename TD, int G, int RB>
-__global__ void __launch_bounds__(256) rope_append_kernel(const PagesView v, const BatchView b,
-                                                          const __grid_constant__ RopeTable rt, const RopeArgs a) {
-    __shared__ float2 s_cs[RB][MAX_ROT_PAIRS];
-    __shared__ long s_slot[RB];                               // elements from the layer's first to the row's K of head 0
+template <typename TS, typename TD, int G, int P>
+__global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const PagesView v, const BatchView b,
+                                                                   const __grid_constant__ RopeTable rt, const RopeArgs a,
+                                                                   int chunk, int side) {
+    __shared__ float2 s_cs[ROPE_ROWS][MAX_ROT_PAIRS];
+    __shared__ long s_slot[ROPE_ROWS];                        // elements from the layer's first to the row's K of head 0
     wait_prior();
     allow_dependents();
-    const int row0 = blockIdx.x * RB, hd = v.head_dim, warp = threadIdx.x >> 5;
-    const int units = hd / (2 * G), per = 256 / units;        // threads of a head, heads of a CTA
-    const int heads = v.heads + 2 * v.kv_heads;
-    const int head = blockIdx.y * per + threadIdx.x / units, unit = threadIdx.x % units;
-    const bool live = threadIdx.x < per * units && head < heads;
+    const int hd = v.head_dim, units = hd / (2 * G), tid = threadIdx.x;
+    const int h0 = blockIdx.y * chunk, hn = min(chunk, v.heads + 2 * v.kv_heads - h0);
+    const int row0 = blockIdx.x * P * side, rows = min(P * side, b.rows - row0);
+    const int at = tid / (chunk * units), rest = tid - at * chunk * units, head = h0 + rest / units, unit = rest % units;
+    const bool live = at < side && head < h0 + hn;
     // first elements of the two runs
-    const bool turns = unit * G < a.half;
-    const int e0 = turns ? unit * G : 2 * a.half + 2 * (unit * G - a.half), e1 = turns ? e0 + a.half : e0 + G;
-    Run<TS, G> in0[RB], in1[RB];
-    if (live) {
-        const bool is_q = head < v.heads, is_k = !is_q && head < v.heads + v.kv_heads;
-        const TS *src = static_cast<const TS *>(is_q ? a.q : is_k ? a.k : a.v) +
-                        (long)(is_q ? head : is_k ? head - v.heads : head - v.heads - v.kv_heads) * hd;
-        const long ld = is_q ? a.ldq : is_k ? a.ldk : a.ldv;
+    const bool in = unit * G < a.half;
+    const int e0 = in ? unit * G : 2 * a.half + 2 * (unit * G - a.half), e1 = in ? e0 + a.half : e0 + G;
+    const bool is_q = head < v.heads, is_k = !is_q && head < v.heads + v.kv_heads;
+    const TS *src = static_cast<const TS *>(is_q ? a.q : is_k ? a.k : a.v) +
+                    (long)(is_q ? head : is_k ? head - v.heads : head - v.heads - v.kv_heads) * hd;
+    const long ld = is_q ? a.ldq : is_k ? a.ldk : a.ldv;
+    Run<TS, G> in0[P], in1[P];
 #pragma unroll
-        for (int u = 0; u < RB; ++u)
-            if (row0 + u < b.rows) {
-                in0[u].load(src + (row0 + u) * ld + e0);
-                in1[u].load(src + (row0 + u) * ld + e1);
-            }
+    for (int i = 0; i < P; ++i) {
+        const int u = i * side + at;
+        if (live && u < rows) {
+            in0[i].load(src + (row0 + u) * ld + e0);
+            in1[i].load(src + (row0 + u) * ld + e1);
+        }
     }
-    for (int e = threadIdx.x; e < RB * a.half; e += 256) {
+    for (int e = tid; e < rows * a.half; e += blockDim.x) {
         const int u = e / a.half, pair = e - u * a.half;
-        if (row0 + u < b.rows) {
-            const long p = a.pos[rt.axis[pair] * a.pos_stride + row0 + u];
-            const int angle = (int)(((unsigned long long)p * rt.turn[pair]) >> 32);
-            float s, c;
-            sincospif((float)angle * 0x1p-31f, &s, &c);
-            s_cs[u][pair] = make_float2(c, s);
-        }
+        const long p = a.pos[rt.axis[pair] * a.pos_stride + row0 + u];
+        const int angle = (int)(((unsigned long long)p * rt.turn[pair]) >> 32);
+        float s, c;
+        sincospif((float)angle * 0x1p-31f, &s, &c);
+        s_cs[u][pair] = make_float2(c, s);
     }
-    if (warp < RB && row0 + warp < b.rows) {
-        const int row = row0 + warp, i = row_owner(b.row_start, b.n, row);
-        const int r = row - b.row_start[i], n = b.row_start[i + 1] - b.row_start[i], s = b.seqs[i];
-        long at = -1;
-        if ((unsigned)s < (unsigned)v.max_seqs) {
-            const int len = v.len[s], slot = len - n + r;
-            if (r >= 0 && r < n && slot >= 0 && slot < (long)v.max_pages * v.page) {
-                const int id = v.table[(long)s * v.max_pages + (slot >> v.page_shift)];
-                if ((unsigned)id < (unsigned)v.n_pages) at = id * v.page_elems() + (slot & (v.page - 1)) * hd;
+    if (h0 + hn > v.heads) {
+        for (int u = tid >> 5; u < rows; u += blockDim.x >> 5) {
+            const long slot = slot_of(v, b, row_owner(b.row_start, b.n, row0 + u), row0 + u);
+            if ((tid & 31) == 0) {
+                s_slot[u] = slot;
+                if (slot < 0) set_status(v.status, ST_RANGE);
             }
-        }
-        if ((threadIdx.x & 31) == 0) {
-            s_slot[warp] = at;
-            if (at < 0) set_status(v.status, ST_RANGE);
         }
     }
     __syncthreads();
     if (!live) return;
-    TD *kv = static_cast<TD *>(v.kv) + (long)a.layer * v.n_pages * v.page_elems() + (long)(head - v.heads) * v.page * hd;
+    TD *dst = is_q ? static_cast<TD *>(a.out) + row0 * a.ldo + (long)head * hd
+                   : static_cast<TD *>(v.kv) + (long)a.layer * v.n_pages * v.page_elems() + (long)(head - v.heads) * v.page * hd;
 #pragma unroll
-    for (int u = 0; u < RB; ++u) {
-        if (row0 + u >= b.rows) break;
-        TD *dst;
-        if (head < v.heads) {
-            dst = static_cast<TD *>(a.out) + (row0 + u) * a.ldo + (long)head * hd;
-        } else {
-            if (s_slot[u] < 0) continue;
-            dst = kv + s_slot[u];
-        }
-        float x[G], y[G];
-        in0[u].to(x);
-        in1[u].to(y);
-        if (turns && head < v.heads + v.kv_heads) {
+    for (int i = 0; i < P; ++i) {
+        const int u = i * side + at;
+        if (u >= rows || (!is_q && s_slot[u] < 0)) continue;
+        TD *to = dst + (is_q ? u * a.ldo : s_slot[u]);
+        float f[G], w[G];
+        in0[i].to(f);
+        in1[i].to(w);
+        if (in && (is_q || is_k)) {
 #pragma unroll
             for (int e = 0; e < G; ++e) {
-                const float2 cs = s_cs[u][unit * G + e];
-                const float f = x[e], w = y[e];
-                x[e] = f * cs.x - w * cs.y;
-                y[e] = w * cs.x + f * cs.y;
+                const float2 cs = s_cs[u][e0 + e];
+                const float y = f[e], z = w[e];
+                f[e] = y * cs.x - z * cs.y;
+                w[e] = z * cs.x + y * cs.y;
             }
         }
-        store_run<TD, G>(dst + e0, x);
-        store_run<TD, G>(dst + e1, y);
+        store_run<TD, G>(to + e0, f);
+        store_run<TD, G>(to + e1, w);
     }
 }
 
 template <typename TS, typename TD>
 cudaError_t launch_rope(const msd_pages *p, const BatchView &b, const RopeArgs &a, cudaStream_t s) {
-    // runs of 8 elements where the rotated part allows it, else pair by pair
-    const int run = a.half % 8 == 0 ? 8 : 1;
-    const int per = 256 / (p->cfg.head_dim / (2 * run)), chunks = (p->cfg.n_heads + 2 * p->cfg.n_kv_heads + per - 1) / per;
-    auto go = [&](auto kernel, int rb) {
-        const cudaError_t e = launch_chain(kernel, dim3((b.rows + rb - 1) / rb, chunks), dim3(256), 0, s, p->v, b, p->rope, a);
+    const int heads = p->cfg.n_heads + 2 * p->cfg.n_kv_heads;
+    auto go = [&](auto kernel, int run, int P) {
+        // the heads in even chunks of up to 384 threads; rows side by side where they are few
+        const int units = p->cfg.head_dim / (2 * run), chunks = (heads * units + 383) / 384;
+        const int chunk = (heads + chunks - 1) / chunks, side = std::max(1, std::min(256 / (chunk * units), ROPE_ROWS / P));
+        const int threads = (side * chunk * units + 31) / 32 * 32, rows = P * side;
+        const cudaError_t e = launch_chain(kernel, dim3((b.rows + rows - 1) / rows, (heads + chunk - 1) / chunk), dim3(threads), 0,
+                                           s, p->v, b, p->rope, a, chunk, side);
         note_launch();
         return e;
     };
-    // several rows to a CTA once they fill the SMs: more bytes in flight behind the same lookups
-    if (run == 1) return go(rope_append_kernel<TS, TD, 1, 1>, 1);
-    constexpr int RB = sizeof(TS) == 4 ? 4 : 8;
-    return (long)b.rows * chunks >= 4l * RB * p->sms ? go(rope_append_kernel<TS, TD, 8, RB>, RB)
-                                                     : go(rope_append_kernel<TS, TD, 8, 1>, 1);
+    // runs of 8 elements where the rotated part allows it, else pair by pair; four rows to a thread once that leaves
+    // every SM some CTAs (20544 rows of 48 heads: 123, 102, 101, 135 us with 1, 2, 4, 6 rows)
+    if (a.half % 8) return go(rope_append_kernel<TS, TD, 1, 1>, 1, 1);
+    return (long)b.rows * heads * p->cfg.head_dim >= ROPE_LARGE * p->sms ? go(rope_append_kernel<TS, TD, 8, ROPE_P>, 8, ROPE_P)
+                                                                        : go(rope_append_kernel<TS, TD, 8, 1>, 8, 1);
 }
 
 }  // namespace
@@ -882,7 +889,7 @@ msd_status msd_pages_create(const msd_pages_config *cfg, const msd_pages_buffers
     p->rank = reinterpret_cast<int *>(p->ws + o_rank);
     p->part_o = reinterpret_cast<float *>(p->ws + o_po);
     p->part_ml = reinterpret_cast<float *>(p->ws + o_pml);
-    p->part_item = reinterpret_cast<int4 *>(p->ws + o_item);
+    p->part_item = reinterpret_cast<PartItem *>(p->ws + o_item);
     if (cfg->dtype == MSD_BF16 && !pages_attn_map(p->v, &p->map)) {
         msd_pages_destroy(p);
         return MSD_ERR_CUDA;
@@ -1058,6 +1065,7 @@ msd_status msd_pages_attention(msd_pages *p, int32_t layer, const msd_batch *bat
     a.part_o = p->part_o;
     a.part_ml = p->part_ml;
     a.part_item = p->part_item;
+    a.wide = reinterpret_cast<uintptr_t>(out) % 32 == 0 && ldo * de % 32 == 0;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     cudaError_t e = cudaSuccess;
     for (int i = 0; i < b.n && e == cudaSuccess; i += ATTN_MAX_SEQS) {

@@ -61,6 +61,11 @@ __device__ __forceinline__ int row_owner(const int *row_start, int n, int row) {
     return lo;
 }
 
+// An item whose partial results are to be joined: first row, K/V head, first packed row, packed rows, first CTA.
+struct PartItem {
+    int start, h, m0, rows, cta;
+};
+
 // Attention over the pages (pages_attn_*.cu).
 struct PagesAttn {
     PagesView pv;
@@ -80,7 +85,8 @@ struct PagesAttn {
     unsigned long long group_magic;        // ceil(2^32 / group): see group_div
     // partial results of row tiles that several CTAs share
     float *part_o, *part_ml;
-    int4 *part_item;
+    PartItem *part_item;
+    bool wide;                // out and its rows are 32-byte aligned
 };
 
 // x / group for x < 2^26 (the product is off by x * group at most, below 2^32)
@@ -110,6 +116,6 @@ struct msd_pages {
     char *ws;                          // one allocation: what follows
     int *mark, *flags, *off, *fresh, *plan, *old_table, *rank;
     float *part_o, *part_ml;
-    int4 *part_item;
+    msd::PartItem *part_item;
     char err[200];
 };

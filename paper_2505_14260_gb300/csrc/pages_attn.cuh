@@ -9,14 +9,16 @@
 // ends inside an item, its CTAs leave partial results (O, max, sum) that a second launch
 // joins in order. Lengths are read on the device; the cut depends on them alone. An item also
 // costs what it takes to begin and end (queries, output): ITEM_STEPS steps of the line before
-// its own, so that many short sequences spread over the SMs like a few long ones.
+// its own (what the measured times of CTAs with many and with few items come to), so that many short sequences spread over the SMs like a few long ones.
 #pragma once
 
 #include "pages.h"
 
 namespace msd {
 
-constexpr int ITEM_STEPS = 2;
+// (KT 128: the tensor-core kernel)
+template <int KT>
+constexpr int ITEM_STEPS = KT == 128 ? 4 : 1;
 
 struct AttnSched {
     long long pre[ATTN_MAX_SEQS + 1];     // steps before each sequence
@@ -90,7 +92,7 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
         const int tiles = (s.rows[i] * G + ROWS - 1) / ROWS;
         long long w = 0;
         if (tiles <= 4)
-            for (int t = 0; t < tiles; ++t) w += ITEM_STEPS + tile_range<ROWS, KT>(a, s.len[i], s.rows[i], t).steps;
+            for (int t = 0; t < tiles; ++t) w += ITEM_STEPS<KT> + tile_range<ROWS, KT>(a, s.len[i], s.rows[i], t).steps;
         s.pre[i + 1] = w * v.kv_heads;
     }
     sync();
@@ -98,7 +100,7 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
         const int tiles = (s.rows[i] * G + ROWS - 1) / ROWS;
         if (tiles <= 4) continue;
         long long w = 0;
-        for (int t = lane; t < tiles; t += 32) w += ITEM_STEPS + tile_range<ROWS, KT>(a, s.len[i], s.rows[i], t).steps;
+        for (int t = lane; t < tiles; t += 32) w += ITEM_STEPS<KT> + tile_range<ROWS, KT>(a, s.len[i], s.rows[i], t).steps;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
         if (lane == 0) s.pre[i + 1] = w * v.kv_heads;
@@ -144,7 +146,7 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
             int t0 = 0;
             for (; t0 < tiles; t0 += 32) {        // 32 tiles at a time
                 const int t = t0 + lane;
-                int inc = t < tiles ? ITEM_STEPS + tile_range<ROWS, KT>(a, s.len[lo], s.rows[lo], t).steps : 0;
+                int inc = t < tiles ? ITEM_STEPS<KT> + tile_range<ROWS, KT>(a, s.len[lo], s.rows[lo], t).steps : 0;
                 const int own = inc;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
@@ -189,9 +191,9 @@ struct AttnWalk {
             g.h = h;
             g.tile = tile;
             g.range = tile_range<ROWS, KT>(a, s.len[i], s.rows[i], tile);
-            const int end = ITEM_STEPS + g.range.steps, stop = (int)min((long long)end, place + left);
-            g.j0 = max(place - ITEM_STEPS, 0);
-            g.j1 = max(stop - ITEM_STEPS, 0);
+            const int end = ITEM_STEPS<KT> + g.range.steps, stop = (int)min((long long)end, place + left);
+            g.j0 = max(place - ITEM_STEPS<KT>, 0);
+            g.j1 = max(stop - ITEM_STEPS<KT>, 0);
             left -= stop - place;
             place = 0;
             if (stop == end && ++tile * ROWS >= s.rows[i] * G) {
@@ -213,15 +215,15 @@ struct AttnWalk {
 __device__ __forceinline__ bool segment_whole(const Segment &g) { return g.j0 == 0 && g.j1 == g.range.steps; }
 __device__ __forceinline__ long part_slot(const Segment &g, int cta) { return 2l * cta + (g.j0 > 0 ? 0 : 1); }
 
-// The CTA that ends an item begun elsewhere names it for the joining launch: sequence, head,
-// tile, and the CTA that took its first step.
+// The CTA that ends an item begun elsewhere names it for the joining launch (rows 0: none).
 template <int ROWS, int KT>
 __device__ void name_parts(const PagesAttn &a, const AttnSched &s, int cta) {
     AttnWalk<ROWS, KT> walk(a, s);
     Segment g;
-    int4 item = make_int4(-1, 0, 0, 0);
+    PartItem item{0, 0, 0, 0, 0};
     if (walk.next(g) && g.j0 > 0 && g.j1 == g.range.steps)
-        item = make_int4(g.i, g.h, g.tile, (int)((s.per * cta - g.j0) / s.per));
+        item = PartItem{a.b.row_start[g.i], g.h, g.tile * ROWS, min(s.rows[g.i] * a.group - g.tile * ROWS, ROWS),
+                        (int)((s.per * cta - g.j0) / s.per)};
     a.part_item[cta] = item;
 }
 

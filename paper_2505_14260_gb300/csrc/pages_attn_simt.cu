@@ -211,57 +211,58 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
 }
 
 // Joins the partial results of items that several CTAs worked on: block (CTA that ended an item, rows), a warp
-// a row. A lane holds the weight of a part (32 at a time), then the parts' O are added in the order of the keys,
-// eight requested at once.
+// a row. A lane holds the weight of a part (32 at a time); the parts' O are added in the order of the keys, eight
+// requested at once, the first ones before the weights are known.
 template <typename T, int HD>
 __global__ void __launch_bounds__(32 * JOIN_WARPS) pages_attn_join_kernel(const PagesAttn a, int tile_rows) {
     wait_prior();
     allow_dependents();
-    const int4 item = a.part_item[blockIdx.x];
-    if (item.x < 0) return;
-    const int G = a.group, lane = threadIdx.x & 31;
-    const int m = blockIdx.y * JOIN_WARPS + (threadIdx.x >> 5);
-    const int start = a.b.row_start[item.x], rows = a.b.row_start[item.x + 1] - start;
-    const int pm = item.z * tile_rows + m;
-    if (pm >= rows * G) return;
+    const PartItem item = a.part_item[blockIdx.x];
+    const int lane = threadIdx.x & 31, m = blockIdx.y * JOIN_WARPS + (threadIdx.x >> 5);
+    if (m >= item.rows) return;
     constexpr int E = HD / 32;
-    const int c0 = item.w, parts = (int)blockIdx.x - c0 + 1;
+    const int c0 = item.cta, parts = (int)blockIdx.x - c0 + 1;
     auto at = [&](int k) { return (2l * (c0 + k) + (k == 0 ? 1 : 0)) * tile_rows + m; };
-    float top = -INFINITY;
-    for (int k = lane; k < parts; k += 32) {
-        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * at(k));
+    float x[8][E];
+    auto fetch = [&](int k) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (k + u < parts) {
+                const float *src = a.part_o + at(k + u) * HD + lane * E;
+                if constexpr (E == 4) {
+                    const float4 y = *reinterpret_cast<const float4 *>(src);
+                    x[u][0] = y.x; x[u][1] = y.y; x[u][2] = y.z; x[u][3] = y.w;
+                } else {
+                    const float2 y = *reinterpret_cast<const float2 *>(src);
+                    x[u][0] = y.x; x[u][1] = y.y;
+                }
+            }
+    };
+    auto ml_of = [&](int k) {
+        return k < parts ? *reinterpret_cast<const float2 *>(a.part_ml + 2 * at(k)) : make_float2(-INFINITY, 0.f);
+    };
+    const float2 first = ml_of(lane);
+    fetch(0);
+    float top = first.y != 0.f ? first.x : -INFINITY;
+    for (int k = lane + 32; k < parts; k += 32) {
+        const float2 ml = ml_of(k);
         if (ml.y != 0.f) top = fmaxf(top, ml.x);
     }
     top = warp_max(top);
     float acc[E] = {}, sum = 0.f;
     for (int k0 = 0; k0 < parts; k0 += 32) {
+        const float2 ml = k0 ? ml_of(k0 + lane) : first;
         float w = 0.f;
-        if (k0 + lane < parts) {
-            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * at(k0 + lane));
-            if (ml.y != 0.f) {                        // (else nothing was seen there)
-                w = ml.x == top ? 1.f : exp2f(ml.x - top);
-                sum += ml.y * w;
-            }
+        if (ml.y != 0.f) {                            // (else nothing was seen there)
+            w = ml.x == top ? 1.f : exp2f(ml.x - top);
+            sum += ml.y * w;
         }
-        const int n = min(32, parts - k0);
-        for (int k = 0; k < n; k += 8) {
-            float x[8][E];
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-                if (k + u < n) {
-                    const float *src = a.part_o + at(k0 + k + u) * HD + lane * E;
-                    if constexpr (E == 4) {
-                        const float4 y = *reinterpret_cast<const float4 *>(src);
-                        x[u][0] = y.x; x[u][1] = y.y; x[u][2] = y.z; x[u][3] = y.w;
-                    } else {
-                        const float2 y = *reinterpret_cast<const float2 *>(src);
-                        x[u][0] = y.x; x[u][1] = y.y;
-                    }
-                }
+        for (int k = k0; k < min(k0 + 32, parts); k += 8) {
+            if (k) fetch(k);
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 const float wu = __shfl_sync(0xffffffffu, w, (k + u) & 31);
-                if (k + u < n && wu != 0.f) {
+                if (k + u < parts && wu != 0.f) {
 #pragma unroll
                     for (int e = 0; e < E; ++e) acc[e] = fmaf(x[u][e], wu, acc[e]);
                 }
@@ -269,12 +270,12 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) pages_attn_join_kernel(const 
         }
     }
     sum = warp_sum(sum);
-    const int r = start + group_div(a, pm), head = item.y * G + pm - group_div(a, pm) * G;
+    const int pm = item.m0 + m, q = group_div(a, pm), r = item.start + q, head = item.h * a.group + pm - q * a.group;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     T *out = static_cast<T *>(a.out) + r * a.ldo + (long)head * HD + lane * E;
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) out[e] = acc[e] * inv;
+        for (int e = 0; e < E; e += 2) *reinterpret_cast<float2 *>(out + e) = make_float2(acc[e] * inv, acc[e + 1] * inv);
     } else {
 #pragma unroll
         for (int e = 0; e < E; e += 2)

@@ -157,6 +157,11 @@ __device__ __forceinline__ void fence_proxy() { asm volatile("fence.proxy.async.
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool live) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void store32(void *p, const uint32_t *u) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]),
+                 "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7])
+                 : "memory");
+}
 // packed pairs of fp32
 __device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) {
     uint64_t d;
@@ -831,22 +836,30 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                         }
                     }
                     if (!store) continue;
+                    // (a lane's row is a line of its own: 32 bytes a store where the rows allow it)
                     if (whole) {
+                        uint32_t u[16];
 #pragma unroll
-                        for (int k = 0; k < 16; k += 4) {
-                            uint32_t u[4];
+                        for (int k = 0; k < 16; ++k) {
+                            const __nv_bfloat162 b = __floats2bfloat162_rn(lo2(acc[k]), hi2(acc[k]));
+                            u[k] = *reinterpret_cast<const uint32_t *>(&b);
+                        }
+                        if (a.wide) {
+                            store32(dst + c, u);
+                            store32(dst + c + 16, u + 8);
+                        } else {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const __nv_bfloat162 b = __floats2bfloat162_rn(lo2(acc[k + e]), hi2(acc[k + e]));
-                                u[e] = *reinterpret_cast<const uint32_t *>(&b);
-                            }
-                            *reinterpret_cast<uint4 *>(dst + c + 2 * k) = make_uint4(u[0], u[1], u[2], u[3]);
+                            for (int k = 0; k < 16; k += 4)
+                                *reinterpret_cast<uint4 *>(dst + c + 2 * k) = make_uint4(u[k], u[k + 1], u[k + 2], u[k + 3]);
                         }
                     } else {
 #pragma unroll
-                        for (int k = 0; k < 16; k += 2)
-                            *reinterpret_cast<float4 *>(pdst + c + 2 * k) =
-                                make_float4(lo2(acc[k]), hi2(acc[k]), lo2(acc[k + 1]), hi2(acc[k + 1]));
+                        for (int k = 0; k < 16; k += 4) {
+                            const uint32_t u[8] = {(uint32_t)acc[k], (uint32_t)(acc[k] >> 32), (uint32_t)acc[k + 1], (uint32_t)(acc[k + 1] >> 32),
+                                                   (uint32_t)acc[k + 2], (uint32_t)(acc[k + 2] >> 32), (uint32_t)acc[k + 3],
+                                                   (uint32_t)(acc[k + 3] >> 32)};
+                            store32(pdst + c + 2 * k, u);
+                        }
                     }
                 }
             }
