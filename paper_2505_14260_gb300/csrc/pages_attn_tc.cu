@@ -7,7 +7,8 @@
 //   two tiles of rows over the same keys (PAIR), where sequences have many packed rows
 //   (each key tile is read once for 256 rows: the tensor cores bound it), or
 //   one tile of rows over alternate key tiles, each group with a maximum, sum and O of its own,
-//   joined at the end (bytes bound it: what counts is that the copies never pause).
+//   joined at the end (bytes bound it: what counts is that the copies never pause). The groups
+//   take the CTA's steps in turns across items too, so short items overlap.
 // Roles (320 threads):
 //   warps 0-7   softmax groups 0 and 1, a row a thread: load the query rows into shared memory
 //               (swizzled as the MMA reads them), then per key tile read S, hide what the row
@@ -270,6 +271,7 @@ struct Seg {
     int i, h, seq, start;             // listed sequence, K/V head, table row, first row
     int len, base, rows, live;        // tokens, tokens before the rows, rows, rows that exist in its tree
     int m0, n, nx[2];                 // first packed row, steps (0: no more segments), steps of each group
+    int u0;                           // the CTA's steps before it
     int j0, sink_tiles, lo, whole;    // first step; which key tiles the steps are; the item's only segment
     long part;                        // its partial results' first row
     __device__ int key(int t) const {
@@ -372,12 +374,23 @@ __device__ __forceinline__ void clean_row(uint8_t *row, uint32_t box, int lane, 
     }
 }
 
-// Where the ring holds a segment's tiles: K tiles run `lead` ahead of V tiles.
-struct Ring {
-    int base, n, lead;
-    __device__ int k(int t) const { return t < lead ? base + t : base + lead + 2 * (t - lead) + 1; }
-    __device__ int v(int t) const { return base + lead + t + min(t, n - lead); }
+// A place of the ring and the parity of its phase, counted.
+template <int SLOTS>
+struct Ticket {
+    int slot = 0;
+    uint32_t phase = 0;
+    __device__ void next() {
+        if (++slot == SLOTS) {
+            slot = 0;
+            phase ^= 1u;
+        }
+    }
 };
+
+// Where the ring holds the V tile of the CTA's step u: K tiles run LEAD steps ahead of V tiles (K0 K1 V0 K2 V1 ... for two; at
+// the end of the run the places of K tiles that there are none of stay empty).
+template <int LEAD>
+__device__ __forceinline__ int ring_v(int u) { return 2 * u + LEAD; }
 
 template <int HD, int ROWS>
 __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_constant__ CUtensorMap map, const PagesAttn a) {
@@ -407,7 +420,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             bar_init(s_full0 + 8 * x, 1);
             bar_init(p_full0 + 8 * x, 128);
             bar_init(o_full0 + 8 * x, 1);
-            bar_init(q_full0 + 8 * x, PAIR ? 128 : 256);
+            bar_init(q_full0 + 8 * x, 128);
         }
         bar_init(drain, 1);
         bar_init(both, 256);
@@ -445,6 +458,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
         if (a.b.n <= ATTN_WARP_SEQS) attn_schedule<ROWS, KT, 32>(a, sched, blockIdx.x, gridDim.x);
         AttnWalk<ROWS, KT> walk(a, sched);
         Segment g;
+        int u0 = 0;
         for (int i = 0;; ++i) {
             if (!w_wait(g_empty0 + 8 * (i % SEGS), (uint32_t)(i / SEGS + 1) & 1u, &s_abort, status)) break;
             const bool have = walk.next(g);
@@ -472,10 +486,12 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                         const int hi = d.base + group_div(a, d.m0 + TILE - 1) + 1;
                         d.nx[0] = two && !a.mask ? min(d.n, max(0, d.sink_tiles + (hi + KT - 1) / KT - d.lo - d.j0)) : d.n;
                         d.nx[1] = two ? d.n : 0;
-                    } else {
-                        d.nx[0] = (d.n + 1) / 2;
-                        d.nx[1] = d.n / 2;
+                    } else {              // steps in turns
+                        d.nx[u0 & 1] = (d.n + 1) / 2;
+                        d.nx[(u0 & 1) ^ 1] = d.n / 2;
                     }
+                    d.u0 = u0;
+                    u0 += d.n;
                 }
                 bar_arrive(g_full0 + 8 * (i % SEGS));
             }
@@ -486,143 +502,219 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
         __syncwarp();
     } else if (warp == 8) {
         // ---- TMA -----------------------------------------------------------
+        // A key tile costs this warp as little as can be: its page ids are asked for one tile ahead and kept for V, and
+        // places of the ring are counted, not divided (with the ids loaded and the places computed where they are
+        // needed, this warp held up the others: ragged chunks 400 us).
         const uint32_t on = elect_one();
-        int pos = 0;
+        const int per = KT >> v.page_shift, page_rows = v.kv_heads * v.page;          // rows of K, or V, of a page
+        const uint32_t page_bytes = v.page * 128;                                     // of a box
+        Ticket<SLOTS> at;
+        int filled = 0;
         bool ok = true;
-        const int per = KT >> v.page_shift;
-        auto load = [&](int key0, int what, const int *table, int len, int h) {
-            const int slot = pos % SLOTS;
-            if (!w_wait(empty0 + 8 * slot, (uint32_t)(pos / SLOTS + 1) & 1u, &s_abort, status)) return false;
-            ++pos;
-            const int first = key0 >> v.page_shift, n = min(per, ((len - 1) >> v.page_shift) - first + 1);
-            int id = lane < n ? table[first + lane] : 0;
-            if ((unsigned)id >= (unsigned)v.n_pages) {
-                id = 0;
-                set_status(status, ST_RANGE);
-            }
-            const uint32_t bar = full0 + 8 * slot, dst = base + L::RING + slot * L::MAT;
-            w_expect_tx(on, bar, (uint32_t)n * v.page * HD * 2);
-            for (int i = 0; i < n; ++i) {
-                const int y = (((a.layer * v.n_pages + __shfl_sync(0xffffffffu, id, i)) * 2 + what) * v.kv_heads + h) * v.page;
+        struct Tile {
+            int id, n, y0;                // the lane's page, pages, the row of page 0's K head
+        };
+        auto load = [&](const Tile &x, int what) {
+            if (!w_wait(empty0 + 8 * at.slot, at.phase ^ 1u, &s_abort, status)) return false;
+            const uint32_t bar = full0 + 8 * at.slot;
+            uint32_t dst = base + L::RING + at.slot * L::MAT;
+            w_expect_tx(on, bar, (uint32_t)x.n * page_bytes * L::NB);
+            const int y0 = x.y0 + what * page_rows;
+            for (int i = 0; i < x.n; ++i, dst += page_bytes) {
+                const int y = y0 + __shfl_sync(0xffffffffu, x.id, i) * 2 * page_rows;
 #pragma unroll
-                for (int b = 0; b < L::NB; ++b)
-                    w_tma2d(on, dst + b * L::BOX + i * v.page * 128, &map, 64 * b, y, bar);
+                for (int b = 0; b < L::NB; ++b) w_tma2d(on, dst + b * L::BOX, &map, 64 * b, y, bar);
             }
+            at.next();
+            ++filled;
             return true;
         };
-        for (int i = 0; ok; ++i) {
-            ok = seg_wait(i);
-            const Seg &d = s_seg[i % SEGS];
-            const int n = d.n, len = d.len, h = d.h, lead = min(LEAD, n);
-            if (!ok || n == 0) break;
-            const int *table = v.table + (long)d.seq * v.max_pages;
-            for (int t = 0; ok && t < lead; ++t) ok = load(d.key(t), 0, table, len, h);
-            for (int t = 0; ok && t < n; ++t) {
-                ok = load(d.key(t), 1, table, len, h);
-                if (ok && t + lead < n) ok = load(d.key(t + lead), 0, table, len, h);
+        // the walk over K tiles, LEAD ahead of V's; V tiles' segments are only counted (for the ring of segments)
+        int ks = 0, kt = 0, kn = 0, k_len = 0, k_y0 = 0, k_j0 = 0, k_sinks = 0, k_lo = 0, vs = 0, v_left = 0;
+        const int *table = nullptr;
+        Tile ahead{0, 0, 0}, wait_v[LEAD + 1] = {};               // the next K tile; V tiles of the K tiles loaded
+        auto fetch = [&]() {              // `ahead`: n 0 at the end
+            ahead.n = 0;
+            if (kt == kn) {
+                if (!seg_wait(ks)) return false;
+                const Seg &d = s_seg[ks % SEGS];
+                kn = d.n;
+                kt = 0;
+                if (kn == 0) return true;
+                ++ks;
+                k_len = d.len;
+                k_y0 = a.layer * v.n_pages * 2 * page_rows + d.h * v.page;
+                k_j0 = d.j0;
+                k_sinks = d.sink_tiles;
+                k_lo = d.lo;
+                table = v.table + (long)d.seq * v.max_pages;
             }
-            __syncwarp();
-            if (lane == 0) bar_arrive(g_empty0 + 8 * (i % SEGS));
+            const int j = k_j0 + kt++, key0 = (j < k_sinks ? j : k_lo + j - k_sinks) * KT, first = key0 >> v.page_shift;
+            ahead.n = min(per, ((k_len - 1) >> v.page_shift) - first + 1);
+            ahead.y0 = k_y0;
+            ahead.id = lane < ahead.n ? table[first + lane] : 0;
+            return true;
+        };
+        auto next_k = [&](Tile &x) {      // loads `ahead` and asks for the one after it; x: its V
+            x = ahead;
+            if (x.n == 0) {               // no K tile: its place stays empty
+                at.next();
+                return true;
+            }
+            if ((unsigned)x.id >= (unsigned)v.n_pages) {
+                x.id = 0;
+                set_status(status, ST_RANGE);
+            }
+            return load(x, 0) && fetch();
+        };
+        ok = fetch();
+        for (int u = -LEAD; ok; ++u) {
+            if (u >= 0) {
+                if (wait_v[0].n == 0) break;
+                if (v_left == 0) v_left = s_seg[vs % SEGS].n;     // (K's walk has been there)
+                ok = load(wait_v[0], 1);
+                if (--v_left == 0) {
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(g_empty0 + 8 * (vs % SEGS));
+                    ++vs;
+                }
+            }
+            ok = ok && next_k(wait_v[LEAD]);
+#pragma unroll
+            for (int i = 0; i < LEAD; ++i) wait_v[i] = wait_v[i + 1];
         }
         if (s_abort) {            // the copies still in flight land before the CTA exits
             volatile int never = 0;
-            for (int p = max(0, pos - SLOTS); p < pos; ++p)
-                bar_wait_slow(full0 + 8 * (p % SLOTS), (uint32_t)(p / SLOTS) & 1u, &never, status);
+            Ticket<SLOTS> p;
+            for (int i = 0; i < filled; ++i, p.next())
+                if (i >= filled - SLOTS) bar_wait_slow(full0 + 8 * p.slot, p.phase, &never, status);
         }
         __syncwarp();
     } else if (warp == 9) {
         // ---- MMA -----------------------------------------------------------
+        // (code that is short: every call of these is inlined once a loop. Unrolled over the groups, the loop below made 64
+        // ragged requests take 112 us, not 97: its instructions did not stay beside the softmax's)
         const uint32_t on = elect_one();
         const uint32_t id_s = idesc(TILE, KT, 0), id_o = idesc(TILE, HD, 1);
-        int ring = 0;
-        uint32_t p_ph[2] = {0, 0}, q_ph[2] = {0, 0};
+        uint32_t p_ph = 0, q_ph = 0;      // a bit a group, a buffer
         bool ok = true;
-        auto wait_slot = [&](int pos) {
-            const bool r = w_wait(full0 + 8 * (pos % SLOTS), (uint32_t)(pos / SLOTS) & 1u, &s_abort, status);
+        auto wait_slot = [&](const Ticket<SLOTS> &p) {
+            const bool r = w_wait(full0 + 8 * p.slot, p.phase, &s_abort, status);
             fence_after();
             return r;
         };
-        auto s_mma = [&](int x, int pos, int qbuf) {
-            const uint32_t k = base + L::RING + (pos % SLOTS) * L::MAT, q = base + L::Q + qbuf * L::QMAT;
+        const uint64_t d_q = sdesc(base + L::Q, 16, 1024), d_k = sdesc(base + L::RING, 16, 1024),
+                       d_v = sdesc(base + L::RING, L::BOX, 1024);
+        auto s_mma = [&](int x, int slot, int qbuf) {
+            const uint64_t k = d_k + (uint32_t)slot * (L::MAT >> 4), q = d_q + (uint32_t)qbuf * (L::QMAT >> 4);
 #pragma unroll
             for (int kk = 0; kk < HD / 16; ++kk)
-                w_mma_ss(on, tmem + L::T_S + x * KT, sdesc(q + (kk >> 2) * L::QBOX + (kk & 3) * 32, 16, 1024),
-                         sdesc(k + (kk >> 2) * L::BOX + (kk & 3) * 32, 16, 1024), id_s, kk > 0);
+                w_mma_ss(on, tmem + L::T_S + x * KT, q + (((kk >> 2) * L::QBOX + (kk & 3) * 32) >> 4),
+                         k + (((kk >> 2) * L::BOX + (kk & 3) * 32) >> 4), id_s, kk > 0);
             w_commit(on, s_full0 + 8 * x);
         };
-        auto o_mma = [&](int x, int pos, bool acc) {
-            const uint32_t w = base + L::RING + (pos % SLOTS) * L::MAT;
+        auto o_mma = [&](int x, int slot, bool acc) {
+            const uint64_t w = d_v + (uint32_t)slot * (L::MAT >> 4);
 #pragma unroll
             for (int kk = 0; kk < KT / 16; ++kk)
-                w_mma_ts(on, tmem + L::T_O + x * HD, tmem + L::T_S + x * KT + kk * 8, sdesc(w + kk * 2048, L::BOX, 1024),
-                         id_o, kk > 0 || acc);
+                w_mma_ts(on, tmem + L::T_O + x * HD, tmem + L::T_S + x * KT + kk * 8, w + (kk * 2048 >> 4), id_o, kk > 0 || acc);
         };
-        auto free_slot = [&](int pos) { w_commit(on, empty0 + 8 * (pos % SLOTS)); };
+        auto free_slot = [&](int slot) { w_commit(on, empty0 + 8 * slot); };
         auto wait_p = [&](int x) {
-            const bool r = w_wait(p_full0 + 8 * x, p_ph[x], &s_abort, status);
-            p_ph[x] ^= 1u;
+            const bool r = w_wait(p_full0 + 8 * x, p_ph >> x & 1u, &s_abort, status);
+            p_ph ^= 1u << x;
             fence_after();
             return r;
         };
         auto wait_q = [&](int x) {
-            const bool r = w_wait(q_full0 + 8 * x, q_ph[x], &s_abort, status);
-            q_ph[x] ^= 1u;
+            const bool r = w_wait(q_full0 + 8 * x, q_ph >> x & 1u, &s_abort, status);
+            q_ph ^= 1u << x;
             fence_after();
             return r;
         };
         int seg = 0;
-        for (;; ++seg) {
-            ok = seg_wait(seg);
-            if (!ok) break;
-            const Seg &d = s_seg[seg % SEGS];
-            const int n = d.n, nx[2] = {d.nx[0], d.nx[1]};
-            if (n == 0) break;
-            __syncwarp();
-            if (lane == 0) bar_arrive(g_empty0 + 8 * (seg % SEGS));
-            const Ring at{ring, n, min(LEAD, n)};
-            if constexpr (PAIR) {
-                const int last = nx[1] > 0;
+        Ticket<SLOTS> at;                 // the ring's tiles in the order of their use
+        if constexpr (PAIR) {
+            for (;; ++seg) {
+                ok = seg_wait(seg);
+                if (!ok) break;
+                const Seg &d = s_seg[seg % SEGS];
+                const int n = d.n, nx0 = d.nx[0], nx1 = d.nx[1], last = nx1 > 0;
+                if (n == 0) break;
+                __syncwarp();
+                if (lane == 0) bar_arrive(g_empty0 + 8 * (seg % SEGS));
                 for (int t = -1; ok && t < n; ++t) {
-#pragma unroll
+                    Ticket<SLOTS> tv = at, tk = at;
+                    if (t >= 0) tk.next();
+#pragma unroll 1
                     for (int x = 0; x < 2; ++x) {
+                        const int nx = x ? nx1 : nx0;
                         if (!ok) break;
-                        if (t >= 0 && t < nx[x]) {
-                            ok = wait_p(x) && wait_slot(at.v(t));
+                        if (t >= 0 && t < nx) {
+                            ok = wait_p(x) && wait_slot(tv);
                             if (!ok) break;
-                            o_mma(x, at.v(t), t > 0);
-                            if (x == last) free_slot(at.v(t));
-                            if (t == nx[x] - 1) w_commit(on, o_full0 + 8 * x);
+                            o_mma(x, tv.slot, t > 0);
+                            if (x == last) free_slot(tv.slot);
+                            if (t == nx - 1) w_commit(on, o_full0 + 8 * x);
                         }
-                        if (t + 1 < nx[x]) {
+                        if (t + 1 < nx) {
                             if (t < 0) ok = wait_q(x);
-                            ok = ok && wait_slot(at.k(t + 1));
+                            ok = ok && wait_slot(tk);
                             if (!ok) break;
-                            s_mma(x, at.k(t + 1), x);
-                            if (x == last) free_slot(at.k(t + 1));
+                            s_mma(x, tk.slot, x);
+                            if (x == last) free_slot(tk.slot);
                         }
                     }
+                    if (t >= 0) at.next();
+                    if (t + 1 < n) at.next();
                 }
-            } else {
-                ok = wait_q(0);
-                for (int t = -2; ok && t < n; ++t) {
-                    const int x = t & 1;
-                    if (t >= 0) {
-                        ok = wait_p(x) && wait_slot(at.v(t));
-                        if (!ok) break;
-                        o_mma(x, at.v(t), t > 1);
-                        free_slot(at.v(t));
-                        if (t + 2 >= n) w_commit(on, o_full0 + 8 * x);
-                    }
-                    if (t + 2 < n) {
-                        ok = wait_slot(at.k(t + 2));
-                        if (!ok) break;
-                        s_mma(x, at.k(t + 2), seg & 1);
-                        free_slot(at.k(t + 2));
-                    }
-                }
+                if (!ok) break;
             }
-            if (!ok) break;
-            ring += 2 * n;
+        } else {
+            // S two steps ahead of P V, across segments: what P V of a step needs to know of its segment waits in three bits
+            // a step (1: not its group's first there, 2: its group's last there, 4: there is such a step)
+            int left = 0, t = 0, qbuf = 1;                        // steps left, and done, of the segment that S is in
+            uint32_t flags = 0;                                   // of the step that P V is at, and the next ones
+            bool more = true;
+            auto next_s = [&](int x, int shift) {
+                if (!more) return true;
+                if (left == 0) {
+                    if (!seg_wait(seg)) return false;
+                    left = s_seg[seg % SEGS].n;
+                    if (left == 0) {
+                        more = false;
+                        return true;
+                    }
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(g_empty0 + 8 * (seg % SEGS));
+                    t = 0;
+                    qbuf ^= 1;
+                    if (!wait_q(qbuf)) return false;
+                    ++seg;
+                }
+                if (!wait_slot(at)) return false;
+                s_mma(x, at.slot, qbuf);
+                free_slot(at.slot);
+                flags |= ((t > 1 ? 1u : 0u) | (left <= 2 ? 2u : 0u) | 4u) << shift;
+                ++t;
+                --left;
+                return true;
+            };
+            for (int u = -2; ok; ++u) {
+                const int x = u & 1;
+                if (u >= 0) {
+                    if (!(flags & 4u)) break;
+                    ok = wait_p(x) && wait_slot(at);
+                    if (!ok) break;
+                    o_mma(x, at.slot, flags & 1u);
+                    free_slot(at.slot);
+                    if (flags & 2u) w_commit(on, o_full0 + 8 * x);
+                    at.next();
+                    flags >>= 3;
+                }
+                ok = next_s(x, u == -2 ? 0 : 3);
+                at.next();
+            }
         }
         if (seg > 0 || !ok) {     // no MMA outlives the CTA's tensor memory
             w_commit(on, drain);
@@ -638,7 +730,6 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
         const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
         const uint32_t t_s = lanes + L::T_S + x * KT, t_o = lanes + L::T_O;
         uint32_t s_ph = 0, o_ph[2] = {0, 0};
-        int ring = 0;
         bool dead = false;            // a wait ran out, here or in another role
         auto wait = [&](uint32_t bar, uint32_t parity) {
             if (!dead && !w_wait(bar, parity, &s_abort, status)) dead = true;
@@ -650,38 +741,41 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             wait(both, parity);
             fence_after();
         };
-        // the query rows of a segment into its buffer (swizzled as the MMA reads them): a pair's groups load their
-        // own tiles, else both load the one there is. Asked for while there is other work, handed over by give_q.
-        auto load_q = [&](const Seg &d, int index) {
-            constexpr int PIECES = L::QROWS * HD / 8, N = PAIR ? 128 : 256;               // of 16 bytes
+        // the query rows of a segment into a buffer (swizzled as the MMA reads them) by one group: a pair's groups load
+        // their own tiles, else see below. Asked for while there is other work, handed over by give_q.
+        auto load_q = [&](const Seg &d, int buf) {
+            constexpr int PIECES = L::QROWS * HD / 8;             // of 16 bytes
             const int pm0 = d.m0 + (PAIR ? x * TILE : 0), left = d.rows * G - pm0;
             const bf16 *src = static_cast<const bf16 *>(a.q) + d.start * a.ldq + (long)d.h * G * HD;
-            const uint32_t dst = base + L::Q + (PAIR ? x : index & 1) * L::QMAT;
+            const uint32_t dst = base + L::Q + buf * L::QMAT;
 #pragma unroll 4
-            for (int p0 = 0; p0 < PIECES; p0 += N) {
-                const int p = p0 + (PAIR ? m : (int)threadIdx.x), row = p / (HD / 8), c = p % (HD / 8);
+            for (int p0 = 0; p0 < PIECES; p0 += 128) {
+                const int p = p0 + m, row = p / (HD / 8), c = p % (HD / 8);
                 const int pm = pm0 + row, r = group_div(a, pm);
-                if (PIECES % N == 0 || p < PIECES)
-                    copy16(dst + (c >> 3) * L::QBOX + row * 128 + (((c & 7) ^ (row & 7)) << 4),
-                           row < left ? src + r * a.ldq + (pm - r * G) * HD + 8 * c : src, row < left);
+                copy16(dst + (c >> 3) * L::QBOX + row * 128 + (((c & 7) ^ (row & 7)) << 4),
+                       row < left ? src + r * a.ldq + (pm - r * G) * HD + 8 * c : src, row < left);
             }
         };
-        auto give_q = [&]() {
+        auto give_q = [&](int buf) {
             asm volatile("cp.async.wait_all;" ::: "memory");
             fence_proxy();
-            bar_arrive(q_full0 + (PAIR ? 8 * x : 0));
+            bar_arrive(q_full0 + 8 * buf);
         };
-        if (!seg_wait(0)) dead = true;
-        if (!dead && s_seg[0].nx[PAIR ? x : 0] > 0 && s_seg[0].n > 0) {
-            load_q(s_seg[0], 0);
-            give_q();
+        // segment i, if there is one (each segment but the first follows one that is there)
+        auto has = [&](int i) {
+            wait(g_full0 + 8 * (i % SEGS), (uint32_t)(i / SEGS) & 1u);
+            return !dead && s_seg[i % SEGS].n > 0;
+        };
+        // the first segments' queries: a pair's groups their own tile of the first, else group x that of segment x
+        if (has(0) && (PAIR ? s_seg[0].nx[x] > 0 : x == 0 || has(1))) {
+            load_q(s_seg[PAIR ? 0 : x], x);
+            give_q(x);
         }
         for (int seg = 0; !dead; ++seg) {
             const Seg &d = s_seg[seg % SEGS];
             const int n = d.n, nx = d.nx[x];
             if (n == 0) break;
-            const Ring at{ring, n, min(LEAD, n)};
-            ring += 2 * n;
+            const int first = PAIR ? 0 : (d.u0 ^ x) & 1;          // the group's first step of the segment
             const int pm0 = d.m0 + (PAIR ? x * TILE : 0), pm = pm0 + m, r = group_div(a, pm);
             const bool valid = m < L::QROWS && pm < d.rows * G;
             Row rw;
@@ -697,16 +791,21 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             const int full_start = !a.window ? 0
                                    : d.base + (a.mask ? a.nodes : group_div(a, min(pm0 + L::QROWS, d.rows * G) - 1)) - a.window + 1;
             const bool any = __any_sync(0xffffffffu, rw.r >= 0), blind = __any_sync(0xffffffffu, valid && rw.r < 0);
-            bool q_next = false;
             float m_ref = -INFINITY, sum = 0.f;
+            // The queries to load once this segment's S are done, seen by the group that gets the last of them: the next
+            // segment's (a pair: each group its own tile), or those of the one after it, into this one's buffer.
+            bool q_next = false;
             auto next_q = [&]() {
-                wait(g_full0 + 8 * ((seg + 1) % SEGS), (uint32_t)((seg + 1) / SEGS) & 1u);
-                const Seg &e = s_seg[(seg + 1) % SEGS];
-                q_next = !dead && e.n > 0 && e.nx[PAIR ? x : 0] > 0;
-                if (q_next) load_q(e, seg + 1);
+                if constexpr (PAIR) {
+                    q_next = has(seg + 1) && s_seg[(seg + 1) % SEGS].nx[x] > 0;
+                    if (q_next) load_q(s_seg[(seg + 1) % SEGS], x);
+                } else {
+                    q_next = has(seg + 1) && has(seg + 2);
+                    if (q_next) load_q(s_seg[(seg + 2) % SEGS], seg & 1);
+                }
             };
             for (int t = 0; t < nx; ++t) {
-                const int tt = PAIR ? t : 2 * t + x, key0 = d.key(tt);
+                const int tt = PAIR ? t : 2 * t + first, key0 = d.key(tt);
                 wait(s_full0 + 8 * x, s_ph);
                 s_ph ^= 1u;
                 fence_after();
@@ -766,7 +865,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                     sum += lo2(all) + hi2(all);
                 }
                 if (!full) {
-                    const int pos = at.v(tt);
+                    const int pos = ring_v<LEAD>(d.u0 + tt);
                     wait(full0 + 8 * (pos % SLOTS), (uint32_t)(pos / SLOTS) & 1u);
                     clean_row<L::NB>(sm + L::RING + (pos % SLOTS) * L::MAT + m * 128, L::BOX, lane, key0 + m < d.len, &s_odd,
                                      1u << (seg & 31));
@@ -774,10 +873,15 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                 }
                 fence_before();
                 bar_arrive(p_full0 + 8 * x);
-                if (t == nx - 1) next_q();           // (all of this segment's S that read the buffer are done)
+                if (PAIR ? t == nx - 1 : tt == n - 1) next_q();
             }
-            if (nx == 0) next_q();
-            if (q_next) give_q();
+            if (PAIR && nx == 0) next_q();
+            if (!PAIR && nx == 0) {                  // the other group's alone
+                o_ph[x ^ 1] ^= 1u;
+                bar_arrive(g_empty0 + 8 * (seg % SEGS));
+                if (!dead) wait(g_full0 + 8 * ((seg + 1) % SEGS), (uint32_t)((seg + 1) / SEGS) & 1u);
+                continue;
+            }
 
             // the item's end: this group's O, or half the columns of both groups' O joined
             float f0 = 1.f, f1 = 0.f;
@@ -785,14 +889,17 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                 wait(o_full0 + 8 * x, o_ph[x]);
                 o_ph[x] ^= 1u;
             }
+            if (q_next) give_q(PAIR ? x : seg & 1);
             if constexpr (!PAIR) {
-                if (d.nx[x ^ 1] > 0) {
+                float2 a0 = make_float2(m_ref, sum), a1 = make_float2(-INFINITY, 0.f);
+                if (n > 1) {
                     wait(o_full0 + 8 * (x ^ 1), o_ph[x ^ 1]);
                     o_ph[x ^ 1] ^= 1u;
+                    s_ml[x * TILE + m] = a0;
+                    groups_sync(0);
+                    a0 = s_ml[m];
+                    a1 = s_ml[TILE + m];
                 }
-                s_ml[x * TILE + m] = make_float2(m_ref, sum);
-                groups_sync(0);
-                const float2 a0 = s_ml[m], a1 = s_ml[TILE + m];
                 const float top = fmaxf(a0.x, a1.x), use = top == -INFINITY ? 0.f : top;
                 f0 = a0.y == 0.f ? 0.f : a0.x == top ? 1.f : ex2_fast(a0.x - use);       // (nothing seen: 0 times nothing)
                 f1 = a1.y == 0.f ? 0.f : a1.x == top ? 1.f : ex2_fast(a1.x - use);
@@ -800,26 +907,27 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                 sum = (a0.y == 0.f ? 0.f : a0.y * f0) + (a1.y == 0.f ? 0.f : a1.y * f1);
             }
             fence_after();
-            constexpr int COLS = PAIR ? HD : HD / 2;
-            const int col0 = PAIR ? 0 : x * COLS;
+            // two groups' results: each half of the columns; one's: all of them
+            const bool two = !PAIR && n > 1;
+            const int cols = two ? HD / 2 : HD, col0 = two ? x * (HD / 2) : 0;
             const bool none = sum == 0.f;            // the row sees nothing: zeros, whatever O holds
             const bool whole = d.whole, odd = s_odd >> (seg & 31) & 1u;
             const int head = d.h * G + pm - r * G;
             const long row = d.start + r, part = d.part + (PAIR ? x * TILE : 0) + m;
-            if (nx > 0 || !PAIR) {
+            if (nx > 0) {
                 const float inv = whole ? none ? 0.f : 1.f / sum : 1.f;
                 const uint64_t g0 = pack2f(f0 * inv, f0 * inv), g1 = pack2f(f1 * inv, f1 * inv);
                 bf16 *dst = static_cast<bf16 *>(a.out) + row * a.ldo + (long)head * HD + col0;
                 float *pdst = a.part_o + part * HD + col0;
                 const bool store = valid && !dead;
 #pragma unroll 1
-                for (int c = 0; c < COLS; c += 32) {
+                for (int c = 0; c < cols; c += 32) {
                     uint32_t o[32];
                     uint64_t acc[16];
-                    tmem_ld32(t_o + (PAIR ? x * HD : 0) + col0 + c, o);
+                    tmem_ld32(t_o + (two ? 0 : x * HD) + col0 + c, o);
 #pragma unroll
                     for (int k = 0; k < 16; ++k) acc[k] = f0 == 0.f || none ? 0ull : fma2(pack2(o[2 * k], o[2 * k + 1]), g0, 0ull);
-                    if (!PAIR && n > 1) {
+                    if (two) {
                         tmem_ld32(t_o + HD + col0 + c, o);
 #pragma unroll
                         for (int k = 0; k < 16; ++k)
@@ -863,13 +971,15 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                     }
                 }
             }
-            if (valid && !dead && (PAIR || x == 0)) {
+            if (valid && !dead && (!two || x == 0)) {
                 if (!whole) *reinterpret_cast<float2 *>(a.part_ml + 2 * part) = make_float2(m_ref, sum);
                 else if (a.lse) a.lse[row * v.heads + head] = none ? -INFINITY : (m_ref + log2f(sum)) * 0.6931471805599453f;
             }
-            bar_arrive(g_empty0 + 8 * (seg % SEGS));
+            // the next segment is known before this one's place may go to a later one
+            if (!dead) wait(g_full0 + 8 * ((seg + 1) % SEGS), (uint32_t)((seg + 1) / SEGS) & 1u);
             // the other group's O is not overwritten before this one has read it
-            if constexpr (!PAIR) groups_sync(1);
+            if (two) groups_sync(1);
+            bar_arrive(g_empty0 + 8 * (seg % SEGS));
         }
     }
     fence_before();
