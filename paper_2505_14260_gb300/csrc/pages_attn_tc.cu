@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
     }
     wait_prior();
     allow_dependents();
-    if (a.b.n > ATTN_WARP_SEQS) attn_schedule<ROWS, KT, THREADS>(a, sched, blockIdx.x, gridDim.x);
+    attn_schedule<ROWS, KT, THREADS>(a, sched, blockIdx.x, gridDim.x);
     fence_before();
     __syncthreads();
     fence_after();
@@ -455,7 +455,6 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 10) {
         // ---- segments ------------------------------------------------------
-        if (a.b.n <= ATTN_WARP_SEQS) attn_schedule<ROWS, KT, 32>(a, sched, blockIdx.x, gridDim.x);
         AttnWalk<ROWS, KT> walk(a, sched);
         Segment g;
         int u0 = 0;
@@ -812,15 +811,22 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                 const bool full = key0 + KT <= full_end && (key0 >= full_start || key0 + KT <= a.sinks);
                 if (any) {
                     uint32_t s[128];
-                    tmem_ld128(t_s, s);
-                    const bool hide = !full || blind;
-                    if (hide) {
+                    if (!full || blind) {            // (a loop over tensor memory: short beside what every tile runs)
                         uint32_t w[4];
                         seen_bits(a, d, rw, key0, w);
+#pragma unroll 1
+                        for (int c = 0; c < 128; c += 32) {
+                            tmem_ld32(t_s + c, s);
 #pragma unroll
-                        for (int c = 0; c < 128; ++c)
-                            if (!(w[c >> 5] >> (c & 31) & 1u)) s[c] = 0xff800000u;
+                            for (int k = 0; k < 32; ++k)
+                                if (!(w[0] >> k & 1u)) s[k] = 0xff800000u;
+                            tmem_st32(t_s + c, s);
+                            w[0] = w[1];
+                            w[1] = w[2];
+                            w[2] = w[3];
+                        }
                     }
+                    tmem_ld128(t_s, s);
                     float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                     for (int c = 0; c < 128; c += 8) {
