@@ -17,7 +17,7 @@
 namespace msd {
 namespace {
 
-constexpr int PLAN_THREADS = 1024;     // the planning CTA
+constexpr int PLAN_THREADS = 1024;     // of a planning CTA, at most
 constexpr int PLAN_INTS = 6;           // per listed sequence: id, base, new length, first page that changes,
                                        // pages before, pages after
 
@@ -257,8 +257,9 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(const PagesView
     }
 }
 
-// CTA (i, layer, z of gridDim.z): the copies' tables and counts (layer 0, z 0), and the
-// tokens of the pages that are copied, 16 bytes a thread and four requests in flight.
+// CTA (i, layer, z of gridDim.z): the copies' tables and counts (layer 0, z 0), and the tokens of the pages that are
+// copied: the pieces of K and V of all heads, 16 bytes a thread and four requests in flight, the (page, head)s spread
+// over z.
 template <int ESZ>
 __global__ void __launch_bounds__(256) fork_apply_kernel(const PagesView v, const int *src, const int *dst, int deep,
                                                          const int *off, const int *fresh, const int *ok) {
@@ -284,17 +285,18 @@ __global__ void __launch_bounds__(256) fork_apply_kernel(const PagesView v, cons
         }
         if (threadIdx.x == 0) v.len[d] = len;
     }
-    const long pe = v.page_elems();
-    const int run16 = v.head_dim * ESZ / 16;          // 16-byte pieces of a token's head
-    const int stride16 = v.page * run16;              // pieces of a head's page
-    for (int k = first + blockIdx.z; k < n; k += gridDim.z) {
+    const int heads = 2 * v.kv_heads, run16 = v.head_dim * ESZ / 16;     // of a page; 16-byte pieces of a token's head
+    const int stride16 = v.page * run16;                                 // pieces of a head's page
+    const long pe16 = v.page_elems() * ESZ / 16;
+    uint4 *kv = static_cast<uint4 *>(v.kv) + (long)layer * v.n_pages * pe16;
+    const int per = (heads + (int)gridDim.z - 1) / (int)gridDim.z;       // heads of a CTA, or more than one page's
+    const int splits = (heads + per - 1) / per;
+    for (int w = blockIdx.z; w < (n - first) * splits; w += gridDim.z) {
+        const int k = first + w / splits, h0 = w % splits * per, hn = min(per, heads - h0);
         if ((unsigned)from[k] >= (unsigned)v.n_pages) continue;
-        const int tokens = min(v.page, len - (k << v.page_shift));
-        const uint4 *s = reinterpret_cast<const uint4 *>(static_cast<const char *>(v.kv) +
-                                                         ((long)layer * v.n_pages + from[k]) * pe * ESZ);
-        uint4 *t = reinterpret_cast<uint4 *>(static_cast<char *>(v.kv) +
-                                             ((long)layer * v.n_pages + ids[k - first]) * pe * ESZ);
-        const int live = tokens * run16, all = 2 * v.kv_heads * live;
+        const int live = min(v.page, len - (k << v.page_shift)) * run16, all = hn * live;
+        const uint4 *s = kv + from[k] * pe16 + h0 * stride16;
+        uint4 *t = kv + ids[k - first] * pe16 + h0 * stride16;
         for (int x0 = threadIdx.x; x0 < all; x0 += 4 * blockDim.x) {
             uint4 r[4];
             int at[4];
@@ -413,13 +415,17 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(const PagesV
     }
 }
 
-// The tables and counts, a CTA per sequence, and the moves. `lanes` threads hold one token's head of one (layer, K or
-// V, head), 16 bytes each; `side` tokens go side by side and U follow one another, all requested before any is stored
+constexpr int MOVE_TOKENS = 1024;      // whose places a CTA lays out at once
+
+// The tables and counts, a CTA per sequence, and the moves. A CTA first lays out where the next MOVE_TOKENS kept tokens
+// come from and go to (four dependent loads), then moves them: `lanes` threads hold one token's head of one (layer, K
+// or V, head), 16 bytes each; `side` tokens go side by side and U follow one another, all requested before any is stored
 // (side > 1: and the CTA's barrier between). keep[j] >= j, so a token's old place is not overwritten before the batch
 // that holds it has been read, and later batches lie behind it. Wide lists (side 16: 128 tokens a batch) are bound by
 // bytes; for an accepted path (side 1) a CTA takes 16 heads, and the round trips of the lookups bound it.
 template <int ESZ, int U>
 __global__ void __launch_bounds__(256) compact_apply_kernel(const PagesView v, const CompactArgs c, int groups, int side) {
+    __shared__ long s_from[MOVE_TOKENS], s_to[MOVE_TOKENS];   // 16-byte pieces from the layer's first; s_from -1: stays
     wait_prior();
     allow_dependents();
     if (!c.flags[2]) return;
@@ -446,31 +452,34 @@ __global__ void __launch_bounds__(256) compact_apply_kernel(const PagesView v, c
     const int lanes = v.head_dim * ESZ / 16, unit = threadIdx.x / lanes, lane = threadIdx.x % lanes;
     const int group = blockIdx.y * (256 / lanes / side) + unit / side, tok = unit % side;
     const int layer = group / (2 * v.kv_heads), kvh = group - layer * 2 * v.kv_heads;
-    uint4 *kv = static_cast<uint4 *>(v.kv);
     const long pe16 = v.page_elems() * ESZ / 16;
-    const long at0 = (long)layer * v.n_pages * pe16 + (long)kvh * v.page * lanes + lane;
+    uint4 *kv = static_cast<uint4 *>(v.kv) + (long)layer * v.n_pages * pe16 + (long)kvh * v.page * lanes + lane;
     const int *keep = c.keep ? c.keep + (long)i * c.stride : nullptr;
-    for (int t0 = k0 << v.page_shift; t0 < after; t0 += U * side) {
-        uint4 r[U];
-        long to[U];
+    for (int c0 = k0 << v.page_shift; c0 < after; c0 += MOVE_TOKENS) {
+        const int n = min(MOVE_TOKENS, after - c0);
+        __syncthreads();
+        for (int x = threadIdx.x; x < n; x += 256) {
+            const int t = c0 + x, k = t >> v.page_shift, rk = rank[k];
+            const int from = t < base || !keep ? t : base + keep[t - base];
+            const int of = old[from >> v.page_shift], in = rk >= 0 ? ids[rk] : old[k];
+            s_from[x] = of != in || from != t ? of * pe16 + (long)(from & (v.page - 1)) * lanes : -1;
+            s_to[x] = in * pe16 + (long)(t & (v.page - 1)) * lanes;
+        }
+        __syncthreads();
+        for (int t0 = 0; t0 < n; t0 += U * side) {
+            uint4 r[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int t = t0 + u * side + tok;
-            to[u] = -1;
-            if (t < after && group < groups) {
-                const int k = t >> v.page_shift, rk = rank[k];
-                const int from = t < base || !keep ? t : base + keep[t - base];
-                const int of = old[from >> v.page_shift], in = rk >= 0 ? ids[rk] : old[k];
-                if (of != in || from != t) {
-                    r[u] = kv[at0 + of * pe16 + (long)(from & (v.page - 1)) * lanes];
-                    to[u] = at0 + in * pe16 + (long)(t & (v.page - 1)) * lanes;
-                }
+            for (int u = 0; u < U; ++u) {
+                const int t = t0 + u * side + tok;
+                if (t < n && group < groups && s_from[t] >= 0) r[u] = kv[s_from[t]];
+            }
+            if (side > 1) __syncthreads();
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int t = t0 + u * side + tok;
+                if (t < n && group < groups && s_from[t] >= 0) kv[s_to[t]] = r[u];
             }
         }
-        if (side > 1) __syncthreads();
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (to[u] >= 0) kv[to[u]] = r[u];
     }
 }
 
@@ -793,6 +802,12 @@ bool batch_view(const msd_pages *p, const msd_batch *b, BatchView *out) {
     return true;
 }
 
+// Threads of a planning CTA: a thread for each of n entries and each 128 pages of the free bitmap. (Its barriers cost
+// more the more threads there are.)
+int plan_threads(const msd_pages *p, int n) {
+    return std::min(PLAN_THREADS, std::max(128, (std::max(n, p->cfg.n_pages / 128 + 1) + 31) / 32 * 32));
+}
+
 template <typename... KArgs, typename... Args>
 cudaError_t chain(void (*kernel)(KArgs...), dim3 grid, int threads, cudaStream_t s, Args &&...args) {
     const cudaError_t e = launch_chain(kernel, grid, dim3(threads), 0, s, std::forward<Args>(args)...);
@@ -926,7 +941,7 @@ msd_status msd_pages_reserve(msd_pages *p, const msd_batch *batch, void *stream)
     if (st != MSD_OK) return st;
     BatchView b;
     if (!batch_view(p, batch, &b)) return pfail(p, MSD_ERR_INVALID, "bad batch");
-    return leave(p, chain(reserve_kernel, dim3(1), PLAN_THREADS, static_cast<cudaStream_t>(stream), p->v, b, p->mark,
+    return leave(p, chain(reserve_kernel, dim3(1), plan_threads(p, b.n), static_cast<cudaStream_t>(stream), p->v, b, p->mark,
                           p->off, p->fresh));
 }
 
@@ -936,10 +951,12 @@ msd_status msd_pages_fork(msd_pages *p, int32_t n, const int32_t *src, const int
     if (st != MSD_OK) return st;
     if (n < 1 || n > p->cfg.max_seqs || !src || !dst) return pfail(p, MSD_ERR_INVALID, "bad count or null list");
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    cudaError_t e = chain(fork_plan_kernel, dim3(1), PLAN_THREADS, s, p->v, n, src, dst, deep != 0, p->mark, p->off,
+    cudaError_t e = chain(fork_plan_kernel, dim3(1), plan_threads(p, n), s, p->v, n, src, dst, deep != 0, p->mark, p->off,
                           p->fresh, p->flags + 2);
     if (e == cudaSuccess) {
-        const dim3 grid(n, p->cfg.n_layers, deep ? 32 : 1);
+        // enough CTAs for every SM's eight, by the heads (and pages) of a copy
+        const long base = (long)n * p->cfg.n_layers, want = (8l * p->sms + base - 1) / base;
+        const dim3 grid(n, p->cfg.n_layers, (unsigned)std::max(1l, std::min(want, deep ? 64l : 2l * p->cfg.n_kv_heads)));
         e = p->cfg.dtype == MSD_F32
                 ? chain(fork_apply_kernel<4>, grid, 256, s, p->v, src, dst, deep != 0, p->off, p->fresh, p->flags + 2)
                 : chain(fork_apply_kernel<2>, grid, 256, s, p->v, src, dst, deep != 0, p->off, p->fresh, p->flags + 2);
@@ -957,7 +974,7 @@ msd_status msd_pages_compact(msd_pages *p, const msd_batch *batch, const int32_t
         return pfail(p, MSD_ERR_INVALID, "bad batch, stride or null count");
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const CompactArgs c{keep, keep_stride, n_keep, p->mark, p->off, p->fresh, p->plan, p->old_table, p->rank, p->flags};
-    cudaError_t e = chain(compact_plan_kernel, dim3(b.n), PLAN_THREADS, s, p->v, b, c);
+    cudaError_t e = chain(compact_plan_kernel, dim3(b.n), plan_threads(p, std::max(b.n, keep ? keep_stride : 0)), s, p->v, b, c);
     if (e == cudaSuccess) {
         const int groups = p->cfg.n_layers * 2 * p->cfg.n_kv_heads;
         const int units = 256 / (p->cfg.head_dim * (p->cfg.dtype == MSD_F32 ? 4 : 2) / 16);

@@ -16,9 +16,9 @@
 
 namespace msd {
 
-// (KT 128: the tensor-core kernel)
+// (of key tiles of 128, the tensor cores' kernel; the other's items begin and end quickly)
 template <int KT>
-constexpr int ITEM_STEPS = KT == 128 ? 4 : 1;
+constexpr int ITEM_STEPS = KT == 128 ? 4 : 0;
 
 struct AttnSched {
     long long pre[ATTN_MAX_SEQS + 1];     // steps before each sequence
@@ -55,22 +55,16 @@ struct Segment {
     TileRange range;
 };
 
-// Up to so many sequences one warp lays out a CTA's run, without the CTA's barriers.
-constexpr int ATTN_WARP_SEQS = 64;
-
-// Fills s (by THREADS threads: the whole CTA or its one warp; ends with a barrier among them). Sequences that cannot be read
+// Fills s (whole CTA, THREADS threads; ends with a barrier). Sequences that cannot be read
 // (ids, lengths or row counts out of range) get no steps and set the status word.
 template <int ROWS, int KT, int THREADS>
 __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int ctas) {
     __shared__ long long s_sum[THREADS / 32];
-    auto sync = [] {
-        if constexpr (THREADS == 32) __syncwarp();
-        else __syncthreads();
-    };
-    const int tid = THREADS == 32 ? threadIdx.x & 31 : threadIdx.x;
     const PagesView &v = a.pv;
-    const int G = a.group, lane = tid & 31, warp = tid >> 5;
+    const int G = a.group, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     constexpr int NW = THREADS / 32;
+    // steps of each sequence: a thread's own loop over few tiles, a warp's over many
+    bool many = false;
     for (int i = tid; i < a.b.n; i += THREADS) {
         const int seq = a.b.seqs[i], r0 = a.b.row_start[i], r1 = a.b.row_start[i + 1];
         int len = 0, rows = r1 - r0;
@@ -85,27 +79,25 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
         }
         s.len[i] = len;
         s.rows[i] = rows;
-    }
-    sync();
-    // steps of each sequence: a thread's own loop over few tiles, a warp's over many
-    for (int i = tid; i < a.b.n; i += THREADS) {
-        const int tiles = (s.rows[i] * G + ROWS - 1) / ROWS;
+        const int tiles = (rows * G + ROWS - 1) / ROWS;
         long long w = 0;
-        if (tiles <= 4)
-            for (int t = 0; t < tiles; ++t) w += ITEM_STEPS<KT> + tile_range<ROWS, KT>(a, s.len[i], s.rows[i], t).steps;
+        if (tiles > 4) many = true;
+        else
+            for (int t = 0; t < tiles; ++t) w += ITEM_STEPS<KT> + tile_range<ROWS, KT>(a, len, rows, t).steps;
         s.pre[i + 1] = w * v.kv_heads;
     }
-    sync();
-    for (int i = warp; i < a.b.n; i += NW) {
-        const int tiles = (s.rows[i] * G + ROWS - 1) / ROWS;
-        if (tiles <= 4) continue;
-        long long w = 0;
-        for (int t = lane; t < tiles; t += 32) w += ITEM_STEPS<KT> + tile_range<ROWS, KT>(a, s.len[i], s.rows[i], t).steps;
+    if (__syncthreads_or(many)) {
+        for (int i = warp; i < a.b.n; i += NW) {
+            const int tiles = (s.rows[i] * G + ROWS - 1) / ROWS;
+            if (tiles <= 4) continue;
+            long long w = 0;
+            for (int t = lane; t < tiles; t += 32) w += ITEM_STEPS<KT> + tile_range<ROWS, KT>(a, s.len[i], s.rows[i], t).steps;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
-        if (lane == 0) s.pre[i + 1] = w * v.kv_heads;
+            for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
+            if (lane == 0) s.pre[i + 1] = w * v.kv_heads;
+        }
+        __syncthreads();
     }
-    sync();
     // inclusive sums
     long long carry = 0;
     for (int i0 = 0; i0 < a.b.n; i0 += THREADS) {
@@ -116,19 +108,19 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
             const long long y = __shfl_up_sync(0xffffffffu, x, o);
             if (lane >= o) x += y;
         }
+        if (i0) __syncthreads();
         if (lane == 31) s_sum[warp] = x;
-        sync();
+        __syncthreads();
         long long before = carry;
         for (int w = 0; w < NW; ++w) {
             if (w < warp) before += s_sum[w];
             carry += s_sum[w];
         }
         if (i < a.b.n) s.pre[i + 1] = before + x;
-        sync();
     }
     if (tid == 0) s.pre[0] = 0;
     const long long per = max(1ll, (carry + ctas - 1) / ctas), x0 = per * cta;
-    sync();
+    __syncthreads();
     if (warp == 0) {
         int4 f = make_int4(-1, 0, 0, 0);
         if (x0 < carry) {
@@ -167,7 +159,7 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
             s.per = per;
         }
     }
-    sync();
+    __syncthreads();
 }
 
 // The segments of a CTA's run, in order: every role of the CTA walks them by itself.

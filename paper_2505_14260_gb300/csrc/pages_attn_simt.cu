@@ -66,9 +66,7 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
     AttnSched &sched = *reinterpret_cast<AttnSched *>(sm + L::SCHED);
     wait_prior();
     allow_dependents();
-    if (a.b.n > ATTN_WARP_SEQS) attn_schedule<ROWS, KT, THREADS>(a, sched, blockIdx.x, gridDim.x);
-    else if (threadIdx.x < 32) attn_schedule<ROWS, KT, 32>(a, sched, blockIdx.x, gridDim.x);
-    __syncthreads();
+    attn_schedule<ROWS, KT, THREADS>(a, sched, blockIdx.x, gridDim.x);
     const PagesView &v = a.pv;
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, G = a.group;
     if (tid == 0) name_parts<ROWS, KT>(a, sched, blockIdx.x);
