@@ -428,7 +428,8 @@ const char *msd_pages_last_error(const msd_pages *p);
 
 /* Takes len and table as they are (all lengths 0: an empty pool; or a saved state), sets
  * refs and the free pages from them, and the table's unused entries to -1. A length or a
- * page id out of range sets the status word. */
+ * page id out of range, or a page that is not full in several sequences, sets the status
+ * word. */
 msd_status msd_pages_restore(msd_pages *p, void *stream);
 
 /* Room for each sequence's rows at its end: len grows by them, new pages are the lowest free
@@ -457,9 +458,10 @@ msd_status msd_pages_free(msd_pages *p, int32_t n, const int32_t *seqs_dev, void
  * at first[i] (null: 0). A text row takes p, p, p and p grows by 1; a span's row (a, b, c)
  * takes p + a * step, p + b, p + c and p grows by max((t - 1) * step + 1, h, w) after it.
  * pos[axis * pos_stride + row]; next[i] (nullable) = p after the last row: the position of
- * the next token. A span out of place sets the status word. */
+ * the next token. n_spans: entries of spans. A span out of place sets the status word (that
+ * sequence's positions are then not to be used). */
 msd_status msd_rope_positions(msd_pages *p, const msd_batch *batch, const int32_t *span_start_dev,
-                              const int32_t *spans_dev, const int32_t *first_dev, int32_t *pos_dev,
+                              const int32_t *spans_dev, int32_t n_spans, const int32_t *first_dev, int32_t *pos_dev,
                               int64_t pos_stride, int32_t *next_dev, void *stream);
 
 /* Rotates q and k of the batch's rows by their positions (pos[axis * pos_stride + row], any

@@ -23,6 +23,9 @@ constexpr int PLAN_INTS = 6;           // per listed sequence: id, base, new len
 
 __device__ __forceinline__ bool seq_ok(const PagesView &v, int s) { return (unsigned)s < (unsigned)v.max_seqs; }
 
+// a length that the table can hold (the caller's array, read before it bounds anything)
+__device__ __forceinline__ bool len_ok(const PagesView &v, int len) { return len >= 0 && len <= (long)v.max_pages * v.page; }
+
 __device__ __forceinline__ int *row_of(const PagesView &v, int s) { return v.table + (long)s * v.max_pages; }
 
 // A reference to page `id` less; the last one frees it. (Adds and ors of whole numbers: the
@@ -101,7 +104,7 @@ __global__ void restore_count_kernel(const PagesView v) {
     allow_dependents();
     const int s = blockIdx.x;
     const int len = v.len[s];
-    const bool ok = len >= 0 && len <= (long)v.max_pages * v.page;
+    const bool ok = len_ok(v, len);
     const int n = ok ? pages_of(len, v.page_shift, v.page) : 0;
     __syncthreads();
     if (!ok && threadIdx.x == 0) {
@@ -119,9 +122,14 @@ __global__ void restore_count_kernel(const PagesView v) {
     if (bad) set_status(v.status, ST_RANGE);
 }
 
+// The free pages; a page that is not full and held by several sequences is reported.
 __global__ void restore_bits_kernel(const PagesView v) {
     wait_prior();
     allow_dependents();
+    for (int s = blockIdx.x * blockDim.x + threadIdx.x; s < v.max_seqs; s += gridDim.x * blockDim.x) {
+        const int len = v.len[s], id = len & (v.page - 1) ? row_of(v, s)[len >> v.page_shift] : -1;
+        if ((unsigned)id < (unsigned)v.n_pages && v.refs[id] > 1) set_status(v.status, ST_RANGE);
+    }
     const int words = (v.n_pages + 31) / 32;
     for (int w = (blockIdx.x * blockDim.x + threadIdx.x) >> 5; w < words; w += (gridDim.x * blockDim.x) >> 5) {
         const int p = 32 * w + (threadIdx.x & 31);
@@ -142,7 +150,13 @@ __global__ void free_kernel(const PagesView v, const int *seqs) {
         if (threadIdx.x == 0) set_status(v.status, ST_BAD_BATCH);
         return;
     }
-    if (threadIdx.x == 0) s_len = atomicExch(v.len + s, 0);
+    if (threadIdx.x == 0) {
+        s_len = atomicExch(v.len + s, 0);
+        if (!len_ok(v, s_len)) {
+            s_len = 0;
+            set_status(v.status, ST_RANGE);
+        }
+    }
     __syncthreads();
     const int n = pages_of(s_len, v.page_shift, v.page);
     int *row = row_of(v, s);
@@ -176,7 +190,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) reserve_kernel(const PagesView v
             if (ok) {
                 const int len = v.len[s];
                 const long after = (long)len + add;
-                ok = after <= (long)v.max_pages * v.page;
+                ok = len_ok(v, len) && after <= (long)v.max_pages * v.page;
                 if (ok) need = pages_of((int)after, v.page_shift, v.page) - pages_of(len, v.page_shift, v.page);
             }
             if (!ok) s_bad = 1;
@@ -231,7 +245,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(const PagesView
             const int a = src[i], d = dst[i];
             bool ok = seq_ok(v, a) && seq_ok(v, d);
             if (ok && atomicExch(mark + d, 1) != 0) ok = false;
-            if (ok && v.len[d] != 0) ok = false;
+            if (ok && (v.len[d] != 0 || !len_ok(v, v.len[a]))) ok = false;
             if (ok) {
                 const int len = v.len[a];
                 need = deep ? pages_of(len, v.page_shift, v.page) : (len & (v.page - 1)) != 0;
@@ -336,7 +350,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(const PagesV
     const int nk = c.n_keep[i];
     if (threadIdx.x == 0) {
         s_bad = !seq_ok(v, s) || rows < 0 || nk < 0 || nk > rows || (c.keep && nk > c.stride);
-        if (!s_bad) s_bad = v.len[s] < rows || atomicExch(c.mark + s, 1) != 0;
+        if (!s_bad) s_bad = v.len[s] < rows || !len_ok(v, v.len[s]) || atomicExch(c.mark + s, 1) != 0;
         s_first = nk;
     }
     __syncthreads();
@@ -492,7 +506,7 @@ constexpr int SPAN_TILE = 256;
 // position is its number less the sum of what the spans before it fall short. The spans
 // come in tiles of 256, with a prefix sum of those shortfalls and a binary search.
 __global__ void __launch_bounds__(SPAN_TILE) positions_kernel(const PagesView v, const BatchView b, const int *span_start,
-                                                              const int *spans, const int *first, int *pos,
+                                                              const int *spans, int n_spans, const int *first, int *pos,
                                                               long pos_stride, int *next) {
     __shared__ int s_scan[33];
     __shared__ int s_row[SPAN_TILE], s_size[SPAN_TILE], s_less[SPAN_TILE], s_before[SPAN_TILE];
@@ -502,7 +516,7 @@ __global__ void __launch_bounds__(SPAN_TILE) positions_kernel(const PagesView v,
     const int r0 = b.row_start[i], rows = b.row_start[i + 1] - r0;
     const int a = span_start ? span_start[i] : 0, z = span_start ? span_start[i + 1] : 0;
     const int start = first ? first[i] : 0;
-    if (rows < 0 || r0 < 0 || (long)r0 + rows > b.rows || a < 0 || z < a) {
+    if (rows < 0 || r0 < 0 || (long)r0 + rows > b.rows || a < 0 || z < a || z > n_spans) {
         if (threadIdx.x == 0) set_status(v.status, ST_BAD_BATCH);
         return;
     }
@@ -997,16 +1011,17 @@ msd_status msd_pages_free(msd_pages *p, int32_t n, const int32_t *seqs, void *st
 }
 
 msd_status msd_rope_positions(msd_pages *p, const msd_batch *batch, const int32_t *span_start, const int32_t *spans,
-                              const int32_t *first, int32_t *pos, int64_t pos_stride, int32_t *next, void *stream) {
+                              int32_t n_spans, const int32_t *first, int32_t *pos, int64_t pos_stride, int32_t *next,
+                              void *stream) {
     if (!p) return MSD_ERR_INVALID;
     msd_status st = enter(p, "msd_rope_positions");
     if (st != MSD_OK) return st;
     BatchView b;
-    if (!batch_view(p, batch, &b) || !pos || (span_start && !spans) || pos_stride < b.rows)
+    if (!batch_view(p, batch, &b) || !pos || (span_start && (!spans || n_spans < 0)) || pos_stride < b.rows)
         return pfail(p, MSD_ERR_INVALID, "bad batch, stride or null array");
     const int chunks = std::max(1, std::min((b.rows + SPAN_TILE - 1) / SPAN_TILE, 64));
     return leave(p, chain(positions_kernel, dim3(b.n, chunks), SPAN_TILE, static_cast<cudaStream_t>(stream), p->v, b,
-                          span_start, spans, first, pos, (long)pos_stride, next));
+                          span_start, spans, span_start ? n_spans : 0, first, pos, (long)pos_stride, next));
 }
 
 msd_status msd_rope_append(msd_pages *p, int32_t layer, const msd_batch *batch, const void *q, int64_t ldq,

@@ -127,7 +127,7 @@ _SIGNATURES = {
     "msd_pages_fork": (c_int32, [c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_void_p]),
     "msd_pages_compact": (c_int32, [c_void_p, POINTER(msd_batch), c_void_p, c_int32, c_void_p, c_void_p]),
     "msd_pages_free": (c_int32, [c_void_p, c_int32, c_void_p, c_void_p]),
-    "msd_rope_positions": (c_int32, [c_void_p, POINTER(msd_batch), c_void_p, c_void_p, c_void_p, c_void_p,
+    "msd_rope_positions": (c_int32, [c_void_p, POINTER(msd_batch), c_void_p, c_void_p, c_int32, c_void_p, c_void_p,
                                      c_int64, c_void_p, c_void_p]),
     "msd_rope_append": (c_int32, [c_void_p, c_int32, POINTER(msd_batch), c_void_p, c_int64, c_void_p, c_int64,
                                   c_void_p, c_int64, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p]),
@@ -529,7 +529,8 @@ class Pages:
             if t is not None and t.numel() != batch.seqs.numel():
                 raise ValueError("next and first have an entry per sequence")
         self._check(lib().msd_rope_positions(self.ptr, batch.c(), _ptr(_ints(span_start)), _ptr(_ints(spans)),
-                                             _ptr(_ints(first)), _ptr(_ints(pos)), pos.stride(0),
+                                             0 if spans is None else spans.shape[0], _ptr(_ints(first)),
+                                             _ptr(_ints(pos)), pos.stride(0),
                                              _ptr(_ints(next_pos)), self._on(stream)), "msd_rope_positions")
         return pos
 

@@ -110,6 +110,9 @@ def test_many_rows_of_many_heads():
 def test_many_sequences_and_long_ones():
     lens = [1 + (i * 37) % 200 for i in range(300)]
     run(lens, [1] * 300, heads=2, kv_heads=1, page=16)
+    run([1 + (i * 37) % 90 for i in range(700)], [1] * 700, heads=2, kv_heads=2, page=16)       # past one launch's
+    run([9 + (i * 5) % 40 for i in range(600)], [7] * 600, tree=7, heads=2, kv_heads=1, valid=[1 + i % 7 for i in range(600)])
+    run([1 + (i * 37) % 90 for i in range(600)], [1] * 600, dtype="f32", heads=2, kv_heads=2)
     run([30000, 5, 9000], [1, 1, 2], heads=8, kv_heads=2, head_dim=128, page=64)
     run([20000], [3], dtype="f32", heads=4, kv_heads=4, page=128)
 

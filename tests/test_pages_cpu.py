@@ -54,7 +54,7 @@ def test_null_pools_are_refused(lib):
     assert lib.msd_pages_fork(None, 1, 16, 16, 0, None) == msd.MSD_ERR_INVALID
     assert lib.msd_pages_compact(None, b, None, 0, 16, None) == msd.MSD_ERR_INVALID
     assert lib.msd_pages_free(None, 1, 16, None) == msd.MSD_ERR_INVALID
-    assert lib.msd_rope_positions(None, b, None, None, None, 16, 1, None, None) == msd.MSD_ERR_INVALID
+    assert lib.msd_rope_positions(None, b, None, None, 0, None, 16, 1, None, None) == msd.MSD_ERR_INVALID
     assert lib.msd_pages_destroy(None) == msd.MSD_OK
     assert lib.msd_pages_last_error(None) == b"null pool"
 

@@ -229,6 +229,11 @@ def test_restore_counts_shared_pages_and_reports_bad_tables():
     with pytest.raises(msd.MsdError):
         p.restore()
     p.table[2, 1] = p.table[0, 1]
+    p.lens[2] = 30                                                # its second page is half full, and sequence 0's
+    p.restore()
+    torch.cuda.synchronize()
+    with pytest.raises(msd.MsdError):
+        p.restore()
     p.lens[2] = -4
     p.restore()
     torch.cuda.synchronize()
@@ -277,12 +282,27 @@ def test_positions(many):
     assert pos[:, :T].T.tolist() == [[x] * 3 for n in rows for x in range(n)]
 
 
+def test_lengths_past_the_table_are_reported_and_bound_nothing():
+    p = pool([20, 40], extra_seqs=1)
+    for call in (lambda: p.free(i32([0])), lambda: p.reserve(batch([0], [1])), lambda: p.fork(i32([0]), i32([2])),
+                 lambda: p.compact(batch([0], [1]), None, i32([1]))):
+        for bad in (-7, p.cfg.max_pages * 16 + 1, 2 ** 31 - 1):
+            p.lens[0] = bad
+            table, refs = p.table.clone(), p.refs.clone()
+            call()
+            torch.cuda.synchronize()
+            with pytest.raises(msd.MsdError) as e:
+                p.free(i32([2]))
+            assert e.value.status == msd.MSD_ERR_DEVICE
+            assert torch.equal(p.table, table) and torch.equal(p.refs, refs)
+
+
 def test_spans_out_of_place_are_reported():
     p = pool([1])
     pos, b = torch.zeros(3, 30, dtype=torch.int32, device="cuda"), batch([0], [30])
     for spans in [[[25, 1, 2, 3, 1]], [[-1, 1, 2, 2, 1]], [[0, 0, 2, 2, 1]], [[0, 1, 2, 2, 0]], [[0, 1, 2, 3, 1], [5, 1, 1, 1, 1]],
-                  [[0, 1 << 30, 1 << 30, 4, 1]], [[9, 1, 1, 1, 1], [3, 1, 1, 1, 1]]]:
-        p.positions(b, starts([len(spans)]), i32(spans), pos)
+                  [[0, 1 << 30, 1 << 30, 4, 1]], [[9, 1, 1, 1, 1], [3, 1, 1, 1, 1]], None]:
+        p.positions(b, i32([0, 2]) if spans is None else starts([len(spans)]), i32(spans or [[0, 1, 1, 1, 1]]), pos)
         torch.cuda.synchronize()
         with pytest.raises(msd.MsdError) as e:
             p.restore()
@@ -411,5 +431,5 @@ def test_refusals():
     assert L.msd_pages_free(p.ptr, 9, p.lens.data_ptr(), S) == msd.MSD_ERR_INVALID
     assert L.msd_pages_free(p.ptr, 1, None, S) == msd.MSD_ERR_INVALID
     assert L.msd_pages_compact(p.ptr, b.c(), None, 0, None, S) == msd.MSD_ERR_INVALID
-    assert L.msd_rope_positions(p.ptr, b.c(), None, None, None, pos.data_ptr(), 1, None, S) == msd.MSD_ERR_INVALID
+    assert L.msd_rope_positions(p.ptr, b.c(), None, None, 0, None, pos.data_ptr(), 1, None, S) == msd.MSD_ERR_INVALID
     assert L.msd_pages_destroy(None) == msd.MSD_OK and L.msd_pages_last_error(None) == b"null pool"
