@@ -591,9 +591,6 @@ __global__ void __launch_bounds__(SPAN_TILE) positions_kernel(const PagesView v,
 
 // ---- rotation and append ---------------------------------------------------
 
-constexpr int ROPE_P = 4;               // rows of a thread in a call of at least ROPE_LARGE elements an SM
-constexpr long ROPE_LARGE = 16 * 1536 * ROPE_P;
-
 struct RopeArgs {
     const void *q, *k, *v;
     long ldq, ldk, ldv;
@@ -655,22 +652,37 @@ __device__ __forceinline__ void store_run(T *g, const float *x) {
     }
 }
 
-// The slot of a row of listed sequence i: elements from the layer's first to its K of head 0, or -1.
-__device__ __forceinline__ long slot_of(const PagesView &v, const BatchView &b, int i, int row) {
-    const int r = row - b.row_start[i], n = b.row_start[i + 1] - b.row_start[i], s = b.seqs[i];
-    if ((unsigned)s >= (unsigned)v.max_seqs) return -1;
-    const int slot = v.len[s] - n + r;
-    if (r < 0 || r >= n || slot < 0 || slot >= (long)v.max_pages * v.page) return -1;
+// The slot of a row: elements from the layer's first to its K of head 0, or -1. Whole warp. Up to 32 sequences the lanes
+// hold all of the list after one round trip (then the length, then the page); more are searched.
+__device__ __forceinline__ long row_slot(const PagesView &v, const BatchView &b, int row) {
+    const int lane = threadIdx.x & 31;
+    int first, next, s;
+    if (b.n <= 32) {
+        const int start = lane < b.n ? b.row_start[lane] : 0x7fffffff, seq = lane < b.n ? b.seqs[lane] : -1;
+        const int end = b.row_start[b.n];
+        const int i = max(__popc(__ballot_sync(0xffffffffu, start <= row)) - 1, 0);
+        first = __shfl_sync(0xffffffffu, start, i);
+        next = i + 1 < b.n ? __shfl_sync(0xffffffffu, start, i + 1) : end;
+        s = __shfl_sync(0xffffffffu, seq, i);
+    } else {
+        const int i = row_owner(b.row_start, b.n, row);
+        first = b.row_start[i];
+        next = b.row_start[i + 1];
+        s = b.seqs[i];
+    }
+    if ((unsigned)s >= (unsigned)v.max_seqs || row < first || row >= next) return -1;
+    const int slot = v.len[s] - next + row;
+    if (slot < 0 || slot >= (long)v.max_pages * v.page) return -1;
     const int id = v.table[(long)s * v.max_pages + (slot >> v.page_shift)];
     return (unsigned)id < (unsigned)v.n_pages ? id * v.page_elems() + (slot & (v.page - 1)) * v.head_dim : -1;
 }
 
-constexpr int ROPE_ROWS = 32, ROPE_THREADS = 512;      // of a CTA, at most
+constexpr int ROPE_ROWS = 32, ROPE_THREADS = 256;      // of a CTA, at most
 
 // CTA (P * side rows, a chunk of heads): a thread takes 2 G elements of one head, G of them and the G that they pair
 // with (past the rotated part: 2 G in a row), of P rows, all requested first; where a row's heads do not fill the CTA,
-// `side` rows lie side by side. Meanwhile a warp a row finds its slot (four dependent loads; only where the chunk has K or
-// V heads) and the CTA the rows' sines. The angle in turns is the product of the position and a 64-bit fraction mod 1,
+// `side` rows lie side by side. Meanwhile a warp a row finds its slot (three round trips; only where the chunk has K or V
+// heads) and the CTA the rows' sines. The angle in turns is the product of the position and a 64-bit fraction mod 1,
 // which whole-number arithmetic gives exactly at any position; its upper 32 bits go to sincospi. Bytes bound it: the
 // rows are read and written once.
 template <typename TS, typename TD, int G, int P>
@@ -712,7 +724,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const PagesVi
     }
     if (h0 + hn > v.heads) {
         for (int u = tid >> 5; u < rows; u += blockDim.x >> 5) {
-            const long slot = slot_of(v, b, row_owner(b.row_start, b.n, row0 + u), row0 + u);
+            const long slot = row_slot(v, b, row0 + u);
             if ((tid & 31) == 0) {
                 s_slot[u] = slot;
                 if (slot < 0) set_status(v.status, ST_RANGE);
@@ -749,20 +761,24 @@ template <typename TS, typename TD>
 cudaError_t launch_rope(const msd_pages *p, const BatchView &b, const RopeArgs &a, cudaStream_t s) {
     const int heads = p->cfg.n_heads + 2 * p->cfg.n_kv_heads;
     auto go = [&](auto kernel, int run, int P) {
-        // the heads in even chunks of up to 384 threads; rows side by side where they are few
-        const int units = p->cfg.head_dim / (2 * run), chunks = (heads * units + 383) / 384;
-        const int chunk = (heads + chunks - 1) / chunks, side = std::max(1, std::min(256 / (chunk * units), ROPE_ROWS / P));
+        // the heads in even chunks of up to 192 threads (large CTAs leave an SM's registers half used); rows side by
+        // side where they are few
+        const int units = p->cfg.head_dim / (2 * run), chunks = (heads * units + 191) / 192;
+        const int chunk = (heads + chunks - 1) / chunks, side = std::max(1, std::min(192 / (chunk * units), ROPE_ROWS / P));
         const int threads = (side * chunk * units + 31) / 32 * 32, rows = P * side;
         const cudaError_t e = launch_chain(kernel, dim3((b.rows + rows - 1) / rows, (heads + chunk - 1) / chunk), dim3(threads), 0,
                                            s, p->v, b, p->rope, a, chunk, side);
         note_launch();
         return e;
     };
-    // runs of 8 elements where the rotated part allows it, else pair by pair; four rows to a thread once that leaves
-    // every SM some CTAs (20544 rows of 48 heads: 123, 102, 101, 135 us with 1, 2, 4, 6 rows)
+    // runs of 8 elements where the rotated part allows it, else pair by pair; several rows to a thread once that leaves
+    // every SM some CTAs (rows of 48 heads of 128: 20544 rows take 119, 91, 82, 116 us with 1, 2, 4, 8 rows a thread,
+    // 960 rows 9.6, 7.6, 9.1, 8.9 us)
     if (a.half % 8) return go(rope_append_kernel<TS, TD, 1, 1>, 1, 1);
-    return (long)b.rows * heads * p->cfg.head_dim >= ROPE_LARGE * p->sms ? go(rope_append_kernel<TS, TD, 8, ROPE_P>, 8, ROPE_P)
-                                                                        : go(rope_append_kernel<TS, TD, 8, 1>, 8, 1);
+    const long each = (long)b.rows * heads * p->cfg.head_dim / p->sms;        // elements of an SM
+    return each >= 150000  ? go(rope_append_kernel<TS, TD, 8, 4>, 8, 4)
+           : each >= 15000 ? go(rope_append_kernel<TS, TD, 8, 2>, 8, 2)
+                           : go(rope_append_kernel<TS, TD, 8, 1>, 8, 1);
 }
 
 }  // namespace
@@ -988,7 +1004,7 @@ msd_status msd_pages_compact(msd_pages *p, const msd_batch *batch, const int32_t
         return pfail(p, MSD_ERR_INVALID, "bad batch, stride or null count");
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const CompactArgs c{keep, keep_stride, n_keep, p->mark, p->off, p->fresh, p->plan, p->old_table, p->rank, p->flags};
-    cudaError_t e = chain(compact_plan_kernel, dim3(b.n), plan_threads(p, std::max(b.n, keep ? keep_stride : 0)), s, p->v, b, c);
+    cudaError_t e = chain(compact_plan_kernel, dim3(b.n), plan_threads(p, std::max(b.n, keep ? keep_stride / 4 : 0)), s, p->v, b, c);
     if (e == cudaSuccess) {
         const int groups = p->cfg.n_layers * 2 * p->cfg.n_kv_heads;
         const int units = 256 / (p->cfg.head_dim * (p->cfg.dtype == MSD_F32 ? 4 : 2) / 16);
@@ -1019,7 +1035,7 @@ msd_status msd_rope_positions(msd_pages *p, const msd_batch *batch, const int32_
     BatchView b;
     if (!batch_view(p, batch, &b) || !pos || (span_start && (!spans || n_spans < 0)) || pos_stride < b.rows)
         return pfail(p, MSD_ERR_INVALID, "bad batch, stride or null array");
-    const int chunks = std::max(1, std::min((b.rows + SPAN_TILE - 1) / SPAN_TILE, 64));
+    const int chunks = std::max(1, std::min((b.rows / b.n + SPAN_TILE - 1) / SPAN_TILE, 64));        // (of an even batch)
     return leave(p, chain(positions_kernel, dim3(b.n, chunks), SPAN_TILE, static_cast<cudaStream_t>(stream), p->v, b,
                           span_start, spans, span_start ? n_spans : 0, first, pos, (long)pos_stride, next));
 }

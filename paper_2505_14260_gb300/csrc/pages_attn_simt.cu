@@ -256,78 +256,98 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
 }
 
 // Joins the partial results of items that several CTAs worked on: block (CTA that ended an item, rows), a warp
-// a row. A lane holds the weight of a part (32 at a time); the parts' O are added in the order of the keys, eight
-// requested at once, the first ones before the weights are known.
-template <typename T, int HD>
+// RW rows. A lane holds the weight of a part (32 at a time); the parts' O are added in the order of the keys, PRE
+// requested at once, the first ones before the weights are known. Long contexts have few rows and many parts (RW 1,
+// PRE 8), prompts many rows and mostly two parts (RW 4, PRE 2: 152 x 256 rows in 20 us one by one).
+template <typename T, int HD, int RW, int PRE>
 __global__ void __launch_bounds__(32 * JOIN_WARPS) pages_attn_join_kernel(const PagesAttn a, int tile_rows) {
     wait_prior();
     allow_dependents();
     const PartItem item = a.part_item[blockIdx.x];
-    const int lane = threadIdx.x & 31, m = blockIdx.y * JOIN_WARPS + (threadIdx.x >> 5);
-    if (m >= item.rows) return;
+    const int lane = threadIdx.x & 31, m0 = (blockIdx.y * JOIN_WARPS + (threadIdx.x >> 5)) * RW;
+    if (m0 >= item.rows) return;
     constexpr int E = HD / 32;
     const int c0 = item.cta, parts = (int)blockIdx.x - c0 + 1;
-    auto at = [&](int k) { return (2l * (c0 + k) + (k == 0 ? 1 : 0)) * tile_rows + m; };
-    float x[8][E];
-    auto fetch = [&](int k) {
+    auto at = [&](int k, int m) { return (2l * (c0 + k) + (k == 0 ? 1 : 0)) * tile_rows + m; };
+    float x[RW][PRE][E];
+    auto fetch = [&](int w, int k) {
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
-            if (k + u < parts) {
-                const float *src = a.part_o + at(k + u) * HD + lane * E;
+        for (int u = 0; u < PRE; ++u)
+            if (k + u < parts && m0 + w < item.rows) {
+                const float *src = a.part_o + at(k + u, m0 + w) * HD + lane * E;
                 if constexpr (E == 4) {
                     const float4 y = *reinterpret_cast<const float4 *>(src);
-                    x[u][0] = y.x; x[u][1] = y.y; x[u][2] = y.z; x[u][3] = y.w;
+                    x[w][u][0] = y.x; x[w][u][1] = y.y; x[w][u][2] = y.z; x[w][u][3] = y.w;
                 } else {
                     const float2 y = *reinterpret_cast<const float2 *>(src);
-                    x[u][0] = y.x; x[u][1] = y.y;
+                    x[w][u][0] = y.x; x[w][u][1] = y.y;
                 }
             }
     };
-    auto ml_of = [&](int k) {
-        return k < parts ? *reinterpret_cast<const float2 *>(a.part_ml + 2 * at(k)) : make_float2(-INFINITY, 0.f);
+    auto ml_of = [&](int w, int k) {
+        return k < parts && m0 + w < item.rows ? *reinterpret_cast<const float2 *>(a.part_ml + 2 * at(k, m0 + w))
+                                               : make_float2(-INFINITY, 0.f);
     };
-    const float2 first = ml_of(lane);
-    fetch(0);
-    float top = first.y != 0.f ? first.x : -INFINITY;
-    for (int k = lane + 32; k < parts; k += 32) {
-        const float2 ml = ml_of(k);
-        if (ml.y != 0.f) top = fmaxf(top, ml.x);
+    float2 first[RW];
+#pragma unroll
+    for (int w = 0; w < RW; ++w) {
+        first[w] = ml_of(w, lane);
+        fetch(w, 0);
     }
-    top = warp_max(top);
-    float acc[E] = {}, sum = 0.f;
-    for (int k0 = 0; k0 < parts; k0 += 32) {
-        const float2 ml = k0 ? ml_of(k0 + lane) : first;
-        float w = 0.f;
-        if (ml.y != 0.f) {                            // (else nothing was seen there)
-            w = ml.x == top ? 1.f : exp2f(ml.x - top);
-            sum += ml.y * w;
+#pragma unroll
+    for (int w = 0; w < RW; ++w) {
+        if (m0 + w >= item.rows) break;
+        float top = first[w].y != 0.f ? first[w].x : -INFINITY;
+        for (int k = lane + 32; k < parts; k += 32) {
+            const float2 ml = ml_of(w, k);
+            if (ml.y != 0.f) top = fmaxf(top, ml.x);
         }
-        for (int k = k0; k < min(k0 + 32, parts); k += 8) {
-            if (k) fetch(k);
+        top = warp_max(top);
+        float acc[E] = {}, sum = 0.f;
+        for (int k0 = 0; k0 < parts; k0 += 32) {
+            const float2 ml = k0 ? ml_of(w, k0 + lane) : first[w];
+            float f = 0.f;
+            if (ml.y != 0.f) {                        // (else nothing was seen there)
+                f = ml.x == top ? 1.f : exp2f(ml.x - top);
+                sum += ml.y * f;
+            }
+            for (int k = k0; k < min(k0 + 32, parts); k += PRE) {
+                if (k) fetch(w, k);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const float wu = __shfl_sync(0xffffffffu, w, (k + u) & 31);
-                if (k + u < parts && wu != 0.f) {
+                for (int u = 0; u < PRE; ++u) {
+                    const float fu = __shfl_sync(0xffffffffu, f, (k + u) & 31);
+                    if (k + u < parts && fu != 0.f) {
 #pragma unroll
-                    for (int e = 0; e < E; ++e) acc[e] = fmaf(x[u][e], wu, acc[e]);
+                        for (int e = 0; e < E; ++e) acc[e] = fmaf(x[w][u][e], fu, acc[e]);
+                    }
                 }
             }
         }
-    }
-    sum = warp_sum(sum);
-    const int pm = item.m0 + m, q = group_div(a, pm), r = item.start + q, head = item.h * a.group + pm - q * a.group;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    T *out = static_cast<T *>(a.out) + r * a.ldo + (long)head * HD + lane * E;
-    if constexpr (sizeof(T) == 4) {
+        sum = warp_sum(sum);
+        const int pm = item.m0 + m0 + w, q = group_div(a, pm), r = item.start + q, head = item.h * a.group + pm - q * a.group;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        T *out = static_cast<T *>(a.out) + r * a.ldo + (long)head * HD + lane * E;
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int e = 0; e < E; e += 2) *reinterpret_cast<float2 *>(out + e) = make_float2(acc[e] * inv, acc[e + 1] * inv);
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; e += 2)
-            *reinterpret_cast<__nv_bfloat162 *>(out + e) = __floats2bfloat162_rn(acc[e] * inv, acc[e + 1] * inv);
+            for (int e = 0; e < E; e += 2) *reinterpret_cast<float2 *>(out + e) = make_float2(acc[e] * inv, acc[e + 1] * inv);
+        } else if constexpr (E == 4) {
+            const __nv_bfloat162 b0 = __floats2bfloat162_rn(acc[0] * inv, acc[1] * inv),
+                                 b1 = __floats2bfloat162_rn(acc[2] * inv, acc[3] * inv);
+            *reinterpret_cast<uint2 *>(out) = make_uint2(*reinterpret_cast<const uint32_t *>(&b0), *reinterpret_cast<const uint32_t *>(&b1));
+        } else {
+            *reinterpret_cast<__nv_bfloat162 *>(out) = __floats2bfloat162_rn(acc[0] * inv, acc[1] * inv);
+        }
+        if (a.lse && lane == 0)
+            a.lse[(long)r * a.pv.heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
     }
-    if (a.lse && lane == 0)
-        a.lse[(long)r * a.pv.heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+}
+
+template <typename T, int HD>
+cudaError_t launch_join(const PagesAttn &a, int ctas, int tile_rows, cudaStream_t s) {
+    const int rows = JOIN_WARPS * (tile_rows > 128 ? 4 : 1);
+    const dim3 grid(ctas, (tile_rows + rows - 1) / rows), block(32 * JOIN_WARPS);
+    return tile_rows > 128 ? launch_chain(pages_attn_join_kernel<T, HD, 4, 2>, grid, block, 0, s, a, tile_rows)
+                           : launch_chain(pages_attn_join_kernel<T, HD, 1, 8>, grid, block, 0, s, a, tile_rows);
 }
 
 template <int HD, int ROWS>
@@ -349,14 +369,10 @@ bool setup() {
 size_t pages_attn_part_rows(int sms) { return 2 * 256 * (size_t)sms; }
 
 cudaError_t launch_pages_attn_join(const PagesAttn &a, int dtype, int ctas, int tile_rows, cudaStream_t s) {
-    const dim3 grid(ctas, (tile_rows + JOIN_WARPS - 1) / JOIN_WARPS), block(32 * JOIN_WARPS);
-    cudaError_t e;
-    if (dtype == MSD_F32)
-        e = a.pv.head_dim == 64 ? launch_chain(pages_attn_join_kernel<float, 64>, grid, block, 0, s, a, tile_rows)
-                                : launch_chain(pages_attn_join_kernel<float, 128>, grid, block, 0, s, a, tile_rows);
-    else
-        e = a.pv.head_dim == 64 ? launch_chain(pages_attn_join_kernel<bf16, 64>, grid, block, 0, s, a, tile_rows)
-                                : launch_chain(pages_attn_join_kernel<bf16, 128>, grid, block, 0, s, a, tile_rows);
+    const bool wide = a.pv.head_dim == 128;
+    const cudaError_t e = dtype == MSD_F32 ? wide ? launch_join<float, 128>(a, ctas, tile_rows, s) : launch_join<float, 64>(a, ctas, tile_rows, s)
+                          : wide           ? launch_join<bf16, 128>(a, ctas, tile_rows, s)
+                                           : launch_join<bf16, 64>(a, ctas, tile_rows, s);
     note_launch();
     return e;
 }
