@@ -16,9 +16,9 @@
 
 namespace msd {
 
-// (of key tiles of 128, the tensor cores' kernel; the other's items begin and end quickly)
-template <int KT>
-constexpr int ITEM_STEPS = KT == 128 ? 4 : 0;
+// (the tensor cores' kernel, key tiles of 128: a pair of row tiles, or one; the other kernel's items begin and end quickly)
+template <int KT, int ROWS>
+constexpr int ITEM_STEPS = KT != 128 ? 0 : ROWS == 256 ? 4 : 3;
 
 struct AttnSched {
     long long pre[ATTN_MAX_SEQS + 1];     // steps before each sequence
@@ -83,7 +83,7 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
         long long w = 0;
         if (tiles > 4) many = true;
         else
-            for (int t = 0; t < tiles; ++t) w += ITEM_STEPS<KT> + tile_range<ROWS, KT>(a, len, rows, t).steps;
+            for (int t = 0; t < tiles; ++t) w += ITEM_STEPS<KT, ROWS> + tile_range<ROWS, KT>(a, len, rows, t).steps;
         s.pre[i + 1] = w * v.kv_heads;
     }
     if (__syncthreads_or(many)) {
@@ -91,7 +91,7 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
             const int tiles = (s.rows[i] * G + ROWS - 1) / ROWS;
             if (tiles <= 4) continue;
             long long w = 0;
-            for (int t = lane; t < tiles; t += 32) w += ITEM_STEPS<KT> + tile_range<ROWS, KT>(a, s.len[i], s.rows[i], t).steps;
+            for (int t = lane; t < tiles; t += 32) w += ITEM_STEPS<KT, ROWS> + tile_range<ROWS, KT>(a, s.len[i], s.rows[i], t).steps;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
             if (lane == 0) s.pre[i + 1] = w * v.kv_heads;
@@ -138,7 +138,7 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
             int t0 = 0;
             for (; t0 < tiles; t0 += 32) {        // 32 tiles at a time
                 const int t = t0 + lane;
-                int inc = t < tiles ? ITEM_STEPS<KT> + tile_range<ROWS, KT>(a, s.len[lo], s.rows[lo], t).steps : 0;
+                int inc = t < tiles ? ITEM_STEPS<KT, ROWS> + tile_range<ROWS, KT>(a, s.len[lo], s.rows[lo], t).steps : 0;
                 const int own = inc;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
@@ -183,9 +183,9 @@ struct AttnWalk {
             g.h = h;
             g.tile = tile;
             g.range = tile_range<ROWS, KT>(a, s.len[i], s.rows[i], tile);
-            const int end = ITEM_STEPS<KT> + g.range.steps, stop = (int)min((long long)end, place + left);
-            g.j0 = max(place - ITEM_STEPS<KT>, 0);
-            g.j1 = max(stop - ITEM_STEPS<KT>, 0);
+            const int end = ITEM_STEPS<KT, ROWS> + g.range.steps, stop = (int)min((long long)end, place + left);
+            g.j0 = max(place - ITEM_STEPS<KT, ROWS>, 0);
+            g.j1 = max(stop - ITEM_STEPS<KT, ROWS>, 0);
             left -= stop - place;
             place = 0;
             if (stop == end && ++tile * ROWS >= s.rows[i] * G) {

@@ -258,7 +258,8 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
 // Joins the partial results of items that several CTAs worked on: block (CTA that ended an item, rows), a warp
 // RW rows. A lane holds the weight of a part (32 at a time); the parts' O are added in the order of the keys, PRE
 // requested at once, the first ones before the weights are known. Long contexts have few rows and many parts (RW 1,
-// PRE 8), prompts many rows and mostly two parts (RW 4, PRE 2: 152 x 256 rows in 20 us one by one).
+// PRE 8), prompts many rows and mostly two parts (RW 2, PRE 2; joined by the last CTA to be done instead, inside
+// the main kernel, ragged chunks took 340 us, not 300, and a tree 47, not 23).
 template <typename T, int HD, int RW, int PRE>
 __global__ void __launch_bounds__(32 * JOIN_WARPS) pages_attn_join_kernel(const PagesAttn a, int tile_rows) {
     wait_prior();
@@ -344,9 +345,9 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) pages_attn_join_kernel(const 
 
 template <typename T, int HD>
 cudaError_t launch_join(const PagesAttn &a, int ctas, int tile_rows, cudaStream_t s) {
-    const int rows = JOIN_WARPS * (tile_rows > 128 ? 4 : 1);
+    const int rows = JOIN_WARPS * (tile_rows > 128 ? 2 : 1);
     const dim3 grid(ctas, (tile_rows + rows - 1) / rows), block(32 * JOIN_WARPS);
-    return tile_rows > 128 ? launch_chain(pages_attn_join_kernel<T, HD, 4, 2>, grid, block, 0, s, a, tile_rows)
+    return tile_rows > 128 ? launch_chain(pages_attn_join_kernel<T, HD, 2, 2>, grid, block, 0, s, a, tile_rows)
                            : launch_chain(pages_attn_join_kernel<T, HD, 1, 8>, grid, block, 0, s, a, tile_rows);
 }
 
