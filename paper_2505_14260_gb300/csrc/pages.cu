@@ -432,7 +432,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(const PagesV
 constexpr int MOVE_TOKENS = 1024;      // whose places a CTA lays out at once
 
 // The tables and counts, a CTA per sequence, and the moves. A CTA first lays out where the next MOVE_TOKENS kept tokens
-// come from and go to (four dependent loads), then moves them: `lanes` threads hold one token's head of one (layer, K
+// come from and go to (three round trips), then moves them: `lanes` threads hold one token's head of one (layer, K
 // or V, head), 16 bytes each; `side` tokens go side by side and U follow one another, all requested before any is stored
 // (side > 1: and the CTA's barrier between). keep[j] >= j, so a token's old place is not overwritten before the batch
 // that holds it has been read, and later batches lie behind it. Wide lists (side 16: 128 tokens a batch) are bound by
@@ -771,14 +771,12 @@ cudaError_t launch_rope(const msd_pages *p, const BatchView &b, const RopeArgs &
         note_launch();
         return e;
     };
-    // runs of 8 elements where the rotated part allows it, else pair by pair; several rows to a thread once that leaves
-    // every SM some CTAs (rows of 48 heads of 128: 20544 rows take 119, 91, 82, 116 us with 1, 2, 4, 8 rows a thread,
-    // 960 rows 9.6, 7.6, 9.1, 8.9 us)
+    // runs of 8 elements where the rotated part allows it, else pair by pair; two rows to a thread once that leaves every
+    // SM some CTAs (1, 2 and 4 rows a thread: 60 rows of 96 heads of 128 take 3.5, 3.7, 4.1 us, 240 rows 5.6, 4.8, 5.1,
+    // 20544 rows of 48 heads 121, 90, 91: 5.6 TB/s)
     if (a.half % 8) return go(rope_append_kernel<TS, TD, 1, 1>, 1, 1);
     const long each = (long)b.rows * heads * p->cfg.head_dim / p->sms;        // elements of an SM
-    return each >= 150000  ? go(rope_append_kernel<TS, TD, 8, 4>, 8, 4)
-           : each >= 15000 ? go(rope_append_kernel<TS, TD, 8, 2>, 8, 2)
-                           : go(rope_append_kernel<TS, TD, 8, 1>, 8, 1);
+    return each >= 15000 ? go(rope_append_kernel<TS, TD, 8, 2>, 8, 2) : go(rope_append_kernel<TS, TD, 8, 1>, 8, 1);
 }
 
 }  // namespace
@@ -1008,7 +1006,7 @@ msd_status msd_pages_compact(msd_pages *p, const msd_batch *batch, const int32_t
     if (e == cudaSuccess) {
         const int groups = p->cfg.n_layers * 2 * p->cfg.n_kv_heads;
         const int units = 256 / (p->cfg.head_dim * (p->cfg.dtype == MSD_F32 ? 4 : 2) / 16);
-        // lists of 64 and more side by side (16 lists of 1027, 8 layers of 8 heads: 287 us one by one)
+        // lists of 64 and more side by side (16 lists of 1027, 8 layers of 8 heads, with the fork before them: 99 us, and 227 one by one)
         const int side = keep && keep_stride < 64 ? 1 : std::min(units, 16);
         const dim3 grid(b.n, (groups + units / side - 1) / (units / side));
         if (grid.y > 65535) return pfail(p, MSD_ERR_INVALID, "more layers and heads than a launch takes");

@@ -9,7 +9,8 @@
 // ends inside an item, its CTAs leave partial results (O, max, sum) that a second launch
 // joins in order. Lengths are read on the device; the cut depends on them alone. An item also
 // costs what it takes to begin and end (queries, output): ITEM_STEPS steps of the line before
-// its own (what the measured times of CTAs with many and with few items come to), so that many short sequences spread over the SMs like a few long ones.
+// its own (what the times of CTAs with many and with few items come to), so that many short
+// sequences spread over the SMs like a few long ones.
 #pragma once
 
 #include "pages.h"

@@ -9,7 +9,7 @@
 //   one tile of rows over alternate key tiles, each group with a maximum, sum and O of its own,
 //   joined at the end (bytes bound it: what counts is that the copies never pause). The groups
 //   take the CTA's steps in turns across items too, so short items overlap.
-// Roles (320 threads):
+// Roles (384 threads, one warp without work; 216 registers for the softmax, 72 for the others):
 //   warps 0-7   softmax groups 0 and 1, a row a thread: load the query rows into shared memory
 //               (swizzled as the MMA reads them), then per key tile read S, hide what the row
 //               does not see, online softmax in base 2, P as bf16 over S; at an item's end O
