@@ -9,6 +9,9 @@
 //   one tile of rows over alternate key tiles, each group with a maximum, sum and O of its own,
 //   joined at the end (bytes bound it: what counts is that the copies never pause). The groups
 //   take the CTA's steps in turns across items too, so short items overlap.
+// Measured, with the join (32 heads of 128, 8 K/V heads): one token each of 64 requests of up to 8192
+// tokens 78 us, 5.0 TB/s; one token behind 131071 90 us, 6.0 TB/s; two chunks of up to 4096 rows behind
+// 4096 in a loop 297 us, 1.44 PFLOP/s (the tensor pipe at work in 64% of the cycles).
 // Roles (384 threads, one warp without work; 216 registers for the softmax, 72 for the others):
 //   warps 0-7   softmax groups 0 and 1, a row a thread: load the query rows into shared memory
 //               (swizzled as the MMA reads them), then per key tile read S, hide what the row
@@ -503,7 +506,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
         // ---- TMA -----------------------------------------------------------
         // A key tile costs this warp as little as can be: its page ids are asked for one tile ahead and kept for V, and
         // places of the ring are counted, not divided (with the ids loaded and the places computed where they are
-        // needed, this warp held up the others: ragged chunks 400 us).
+        // needed, ragged chunks took 355 us; with shorter issue loops as well, 314).
         const uint32_t on = elect_one();
         const int per = KT >> v.page_shift, page_rows = v.kv_heads * v.page;          // rows of K, or V, of a page
         const uint32_t page_bytes = v.page * 128;                                     // of a box
