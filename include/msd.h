@@ -449,7 +449,8 @@ msd_status msd_pages_fork(msd_pages *p, int32_t n, const int32_t *src_dev, const
 msd_status msd_pages_compact(msd_pages *p, const msd_batch *batch, const int32_t *keep_dev, int32_t keep_stride,
                              const int32_t *n_keep_dev, void *stream);
 
-/* Frees n sequences (len 0 afterwards; one that is unused, or listed twice, is no error). */
+/* Frees n sequences (len 0 afterwards; one that is unused, or listed twice, is no error). An
+ * id or a length out of range: none of them is freed. */
 msd_status msd_pages_free(msd_pages *p, int32_t n, const int32_t *seqs_dev, void *stream);
 
 /* Rotary positions of interleaved text, images and video: sequence i of the batch has spans

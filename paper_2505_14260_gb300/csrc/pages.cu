@@ -143,30 +143,34 @@ __global__ void restore_bits_kernel(const PagesView v) {
 
 // ---- free ------------------------------------------------------------------
 
-// One CTA a listed sequence. A sequence listed twice is freed once (the exchange).
-__global__ void free_kernel(const PagesView v, const int *seqs) {
+// Every CTA looks through the whole list first, so that it is freed whole or not at all (a length that another CTA has
+// set to 0 by then is as good as the one it was), then frees its share of it. A sequence listed twice is freed once
+// (the exchange).
+__global__ void __launch_bounds__(128) free_kernel(const PagesView v, int n, const int *seqs) {
     __shared__ int s_len;
     wait_prior();
     allow_dependents();
-    const int s = seqs[blockIdx.x];
-    if (!seq_ok(v, s)) {
-        if (threadIdx.x == 0) set_status(v.status, ST_BAD_BATCH);
-        return;
+    bool bad = false;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const int s = seqs[i];
+        const bool known = seq_ok(v, s);
+        if (known && len_ok(v, v.len[s])) continue;
+        bad = true;
+        if (blockIdx.x == 0) set_status(v.status, known ? ST_RANGE : ST_BAD_BATCH);
     }
-    if (threadIdx.x == 0) {
-        s_len = atomicExch(v.len + s, 0);
-        if (!len_ok(v, s_len)) {
-            s_len = 0;
-            set_status(v.status, ST_RANGE);
+    if (__syncthreads_or(bad)) return;
+    for (int i = blockIdx.x; i < n; i += gridDim.x) {
+        const int s = seqs[i];
+        if (threadIdx.x == 0) s_len = atomicExch(v.len + s, 0);
+        __syncthreads();
+        const int pages = pages_of(s_len, v.page_shift, v.page);
+        int *row = row_of(v, s);
+        for (int k = threadIdx.x; k < pages; k += blockDim.x) {
+            const int id = row[k];
+            row[k] = -1;
+            drop_ref(v, id);
         }
-    }
-    __syncthreads();
-    const int n = pages_of(s_len, v.page_shift, v.page);
-    int *row = row_of(v, s);
-    for (int k = threadIdx.x; k < n; k += blockDim.x) {
-        const int id = row[k];
-        row[k] = -1;
-        drop_ref(v, id);
+        __syncthreads();
     }
 }
 
@@ -1024,7 +1028,7 @@ msd_status msd_pages_free(msd_pages *p, int32_t n, const int32_t *seqs, void *st
     msd_status st = enter(p, "msd_pages_free");
     if (st != MSD_OK) return st;
     if (n < 1 || n > p->cfg.max_seqs || !seqs) return pfail(p, MSD_ERR_INVALID, "bad count or null list");
-    return leave(p, chain(free_kernel, dim3(n), 128, static_cast<cudaStream_t>(stream), p->v, seqs));
+    return leave(p, chain(free_kernel, dim3(std::min(n, 8 * p->sms)), 128, static_cast<cudaStream_t>(stream), p->v, n, seqs));
 }
 
 msd_status msd_rope_positions(msd_pages *p, const msd_batch *batch, const int32_t *span_start, const int32_t *spans,
