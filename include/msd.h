@@ -370,8 +370,12 @@ msd_status msd_test_gemm_shape(int32_t m, int32_t k, int32_t o, int32_t planes, 
  * read lengths and tables on the device and never synchronise. Argument errors
  * are returned at once. What only the device can see sets the pool's status word;
  * the first later call that observes it returns MSD_ERR_CAPACITY (too few free
- * pages) or MSD_ERR_DEVICE (anything else), launches nothing, and clears it. A
- * page operation that cannot be carried out changes nothing. A pool is used from
+ * pages) or MSD_ERR_DEVICE (anything else), does nothing else, and clears it (a
+ * call that is being recorded returns it too, and leaves it for one that is not).
+ * A page operation (reserve, fork, compact, free) that cannot be carried out
+ * changes nothing, and until a call has reported it the operations, appends and
+ * attention queued behind it, replays of recorded ones included, change and write
+ * nothing either: they were made for what it should have done. A pool is used from
  * one host thread and one stream at a time (or streams that are ordered by
  * events), on the device that was current when it was created. Calls can be
  * captured into a CUDA graph.

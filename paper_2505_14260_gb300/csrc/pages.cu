@@ -6,7 +6,8 @@
 // pool. A page that is not full belongs to one sequence, so appending never copies; forks
 // share full pages only. Allocation takes the lowest free page ids in the order of the
 // call's list, so a sequence of calls always gives the same tables. A call that cannot be
-// carried out (too few pages, bad lists) changes nothing and sets the status word.
+// carried out (too few pages, bad lists) changes nothing, sets the status word, and keeps the
+// calls behind it from running until the host has seen that (refuse, in pages.h).
 // Round trips bound the lists: freeing takes 3 to 4 us, planning 64 forks 7, reserving for 16
 // sequences 6, planning 16 compactions of 1027 tokens 13, positions of 20544 rows 4; bytes
 // bound the moves (66 us there).
@@ -141,6 +142,16 @@ __global__ void restore_bits_kernel(const PagesView v) {
     }
 }
 
+// ---- after an error --------------------------------------------------------
+
+// Behind the calls that were held back: they may run again, unless one of them has met an error of its own since the
+// host took the status word (that is yet to be seen).
+__global__ void resume_kernel(const PagesView v) {
+    wait_prior();
+    allow_dependents();
+    if (atomicAdd(v.status, 0) == 0) *v.refused = 0;
+}
+
 // ---- free ------------------------------------------------------------------
 
 // Every CTA looks through the whole list first, so that it is freed whole or not at all (a length that another CTA has
@@ -150,13 +161,13 @@ __global__ void __launch_bounds__(128) free_kernel(const PagesView v, int n, con
     __shared__ int s_len;
     wait_prior();
     allow_dependents();
-    bool bad = false;
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    bool bad = *v.refused;                // (also by CTA 0 of this launch, then the others come to it too)
+    for (int i = threadIdx.x; !bad && i < n; i += blockDim.x) {
         const int s = seqs[i];
         const bool known = seq_ok(v, s);
         if (known && len_ok(v, v.len[s])) continue;
         bad = true;
-        if (blockIdx.x == 0) set_status(v.status, known ? ST_RANGE : ST_BAD_BATCH);
+        if (blockIdx.x == 0) refuse(v, known ? ST_RANGE : ST_BAD_BATCH);
     }
     if (__syncthreads_or(bad)) return;
     for (int i = blockIdx.x; i < n; i += gridDim.x) {
@@ -183,6 +194,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) reserve_kernel(const PagesView v
     __shared__ int s_scan[33], s_bad;
     wait_prior();
     allow_dependents();
+    if (*v.refused) return;
     if (threadIdx.x == 0) s_bad = 0;
     __syncthreads();
     int total = 0;
@@ -211,11 +223,11 @@ __global__ void __launch_bounds__(PLAN_THREADS) reserve_kernel(const PagesView v
     for (int i = threadIdx.x; i < b.n; i += blockDim.x)
         if (seq_ok(v, b.seqs[i])) mark[b.seqs[i]] = 0;
     if (s_bad) {
-        if (threadIdx.x == 0) set_status(v.status, ST_BAD_BATCH);
+        if (threadIdx.x == 0) refuse(v, ST_BAD_BATCH);
         return;
     }
     if (total > v.n_pages || !take_pages(v, total, fresh, s_scan)) {
-        if (threadIdx.x == 0) set_status(v.status, ST_NO_PAGES);
+        if (threadIdx.x == 0) refuse(v, ST_NO_PAGES);
         return;
     }
     for (int x = threadIdx.x; x < total; x += blockDim.x) {
@@ -242,6 +254,10 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(const PagesView
     __shared__ int s_scan[33], s_bad;
     wait_prior();
     allow_dependents();
+    if (*v.refused) {
+        if (threadIdx.x == 0) *ok_out = 0;
+        return;
+    }
     if (threadIdx.x == 0) s_bad = 0;
     __syncthreads();
     int total = 0;
@@ -274,7 +290,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(const PagesView
     const bool ok = !bad && total <= v.n_pages && take_pages(v, total, fresh, s_scan);
     if (threadIdx.x == 0) {
         *ok_out = ok;
-        if (!ok) set_status(v.status, bad ? ST_BAD_BATCH : ST_NO_PAGES);
+        if (!ok) refuse(v, bad ? ST_BAD_BATCH : ST_NO_PAGES);
     }
 }
 
@@ -351,6 +367,10 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(const PagesV
     __shared__ int s_scan[33], s_first, s_bad, s_last;
     wait_prior();
     allow_dependents();
+    if (*v.refused) {                                 // (set by the launch's last CTA at the earliest, so the same for all)
+        if (blockIdx.x == 0 && threadIdx.x == 0) c.flags[2] = 0;
+        return;
+    }
     const int i = blockIdx.x;
     const int s = b.seqs[i];
     const int rows = b.row_start[i + 1] - b.row_start[i];
@@ -432,7 +452,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(const PagesV
         c.flags[0] = 0;
         c.flags[1] = 0;
         c.flags[2] = ok;
-        if (!ok) set_status(v.status, bad ? ST_BAD_BATCH : ST_NO_PAGES);
+        if (!ok) refuse(v, bad ? ST_BAD_BATCH : ST_NO_PAGES);
     }
 }
 
@@ -704,6 +724,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const PagesVi
     const int h0 = blockIdx.y * chunk, hn = min(chunk, v.heads + 2 * v.kv_heads - h0);
     const int row0 = blockIdx.x * P * side, rows = min(P * side, b.rows - row0);
     const int at = tid / (chunk * units), rest = tid - at * chunk * units, head = h0 + rest / units, unit = rest % units;
+    const int refused = *v.refused;                           // (asked for first, looked at before anything is written)
     const bool live = at < side && head < h0 + hn;
     // first elements of the two runs
     const bool in = unit * G < a.half;
@@ -734,12 +755,12 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const PagesVi
             const long slot = row_slot(v, b, row0 + u);
             if ((tid & 31) == 0) {
                 s_slot[u] = slot;
-                if (slot < 0) set_status(v.status, ST_RANGE);
+                if (slot < 0 && !refused) set_status(v.status, ST_RANGE);
             }
         }
     }
     __syncthreads();
-    if (!live) return;
+    if (!live || refused) return;
     TD *dst = is_q ? static_cast<TD *>(a.out) + row0 * a.ldo + (long)head * hd
                    : static_cast<TD *>(v.kv) + (long)a.layer * v.n_pages * v.page_elems() + (long)(head - v.heads) * v.page * hd;
 #pragma unroll
@@ -798,9 +819,18 @@ msd_status pfail(msd_pages *p, msd_status st, const char *msg) {
     return st;
 }
 
+template <typename... KArgs, typename... Args>
+cudaError_t chain(void (*kernel)(KArgs...), dim3 grid, int threads, cudaStream_t s, Args &&...args) {
+    const cudaError_t e = launch_chain(kernel, grid, dim3(threads), 0, s, std::forward<Args>(args)...);
+    note_launch();
+    return e;
+}
+
 // What every call begins with: an error that was pending before it, the pool's device, and
-// the status word of earlier calls.
-msd_status enter(msd_pages *p, const char *call) {
+// the status word of earlier calls. Reporting that lets later calls run again: the mark that holds them
+// back is cleared on the stream, behind the calls that it is for. A call that is being recorded
+// cannot do that (it would be recorded too), so the word stays for the next one that is not.
+msd_status enter(msd_pages *p, const char *call, cudaStream_t s) {
     p->err[0] = 0;
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) {
@@ -812,7 +842,13 @@ msd_status enter(msd_pages *p, const char *call) {
         return pfail(p, MSD_ERR_INVALID, "the pool belongs to another device than the current one");
     const int code = *p->status_host;
     if (code != 0) {
-        *p->status_host = 0;
+        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusActive;
+        if (cudaStreamIsCapturing(s, &capture) != cudaSuccess) cudaGetLastError();       // (the default stream, while another records)
+        if (capture == cudaStreamCaptureStatusNone) {
+            *p->status_host = 0;
+            const cudaError_t failed = chain(resume_kernel, dim3(1), 1, s, p->v);
+            if (failed != cudaSuccess) return pfail(p, MSD_ERR_CUDA, cudaGetErrorString(failed));
+        }
         if (code == ST_NO_PAGES)
             return pfail(p, MSD_ERR_CAPACITY, "an earlier call needed more free pages than there were; it changed nothing");
         snprintf(p->err, sizeof p->err, "an earlier call set the device status word (code %d: %s)", code,
@@ -841,13 +877,6 @@ bool batch_view(const msd_pages *p, const msd_batch *b, BatchView *out) {
 // more the more threads there are.)
 int plan_threads(const msd_pages *p, int n) {
     return std::min(PLAN_THREADS, std::max(128, (std::max(n, p->cfg.n_pages / 128 + 1) + 31) / 32 * 32));
-}
-
-template <typename... KArgs, typename... Args>
-cudaError_t chain(void (*kernel)(KArgs...), dim3 grid, int threads, cudaStream_t s, Args &&...args) {
-    const cudaError_t e = launch_chain(kernel, grid, dim3(threads), 0, s, std::forward<Args>(args)...);
-    note_launch();
-    return e;
 }
 
 bool valid(const msd_pages_config *c) {
@@ -928,7 +957,7 @@ msd_status msd_pages_create(const msd_pages_config *cfg, const msd_pages_buffers
     }
     *p->status_host = 0;
     p->v = PagesView{buf->kv, buf->table, buf->len, buf->refs, reinterpret_cast<unsigned *>(p->ws + o_bits),
-                     static_cast<int *>(mapped), cfg->n_layers, cfg->n_heads, cfg->n_kv_heads, cfg->head_dim,
+                     static_cast<int *>(mapped), reinterpret_cast<int *>(p->ws + o_flags) + 3, cfg->n_layers, cfg->n_heads, cfg->n_kv_heads, cfg->head_dim,
                      cfg->page_size, shift, cfg->n_pages, cfg->max_seqs, cfg->max_pages};
     p->mark = reinterpret_cast<int *>(p->ws + o_mark);
     p->flags = reinterpret_cast<int *>(p->ws + o_flags);
@@ -960,7 +989,7 @@ const char *msd_pages_last_error(const msd_pages *p) { return p ? p->err : "null
 
 msd_status msd_pages_restore(msd_pages *p, void *stream) {
     if (!p) return MSD_ERR_INVALID;
-    msd_status st = enter(p, "msd_pages_restore");
+    msd_status st = enter(p, "msd_pages_restore", static_cast<cudaStream_t>(stream));
     if (st != MSD_OK) return st;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int blocks = std::min((p->cfg.n_pages + 255) / 256, 4 * p->sms);
@@ -972,7 +1001,7 @@ msd_status msd_pages_restore(msd_pages *p, void *stream) {
 
 msd_status msd_pages_reserve(msd_pages *p, const msd_batch *batch, void *stream) {
     if (!p) return MSD_ERR_INVALID;
-    msd_status st = enter(p, "msd_pages_reserve");
+    msd_status st = enter(p, "msd_pages_reserve", static_cast<cudaStream_t>(stream));
     if (st != MSD_OK) return st;
     BatchView b;
     if (!batch_view(p, batch, &b)) return pfail(p, MSD_ERR_INVALID, "bad batch");
@@ -982,7 +1011,7 @@ msd_status msd_pages_reserve(msd_pages *p, const msd_batch *batch, void *stream)
 
 msd_status msd_pages_fork(msd_pages *p, int32_t n, const int32_t *src, const int32_t *dst, int32_t deep, void *stream) {
     if (!p) return MSD_ERR_INVALID;
-    msd_status st = enter(p, "msd_pages_fork");
+    msd_status st = enter(p, "msd_pages_fork", static_cast<cudaStream_t>(stream));
     if (st != MSD_OK) return st;
     if (n < 1 || n > p->cfg.max_seqs || !src || !dst) return pfail(p, MSD_ERR_INVALID, "bad count or null list");
     cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -1002,7 +1031,7 @@ msd_status msd_pages_fork(msd_pages *p, int32_t n, const int32_t *src, const int
 msd_status msd_pages_compact(msd_pages *p, const msd_batch *batch, const int32_t *keep, int32_t keep_stride,
                              const int32_t *n_keep, void *stream) {
     if (!p) return MSD_ERR_INVALID;
-    msd_status st = enter(p, "msd_pages_compact");
+    msd_status st = enter(p, "msd_pages_compact", static_cast<cudaStream_t>(stream));
     if (st != MSD_OK) return st;
     BatchView b;
     if (!batch_view(p, batch, &b) || !n_keep || (keep && keep_stride < 1))
@@ -1025,7 +1054,7 @@ msd_status msd_pages_compact(msd_pages *p, const msd_batch *batch, const int32_t
 
 msd_status msd_pages_free(msd_pages *p, int32_t n, const int32_t *seqs, void *stream) {
     if (!p) return MSD_ERR_INVALID;
-    msd_status st = enter(p, "msd_pages_free");
+    msd_status st = enter(p, "msd_pages_free", static_cast<cudaStream_t>(stream));
     if (st != MSD_OK) return st;
     if (n < 1 || n > p->cfg.max_seqs || !seqs) return pfail(p, MSD_ERR_INVALID, "bad count or null list");
     return leave(p, chain(free_kernel, dim3(std::min(n, 8 * p->sms)), 128, static_cast<cudaStream_t>(stream), p->v, n, seqs));
@@ -1035,7 +1064,7 @@ msd_status msd_rope_positions(msd_pages *p, const msd_batch *batch, const int32_
                               int32_t n_spans, const int32_t *first, int32_t *pos, int64_t pos_stride, int32_t *next,
                               void *stream) {
     if (!p) return MSD_ERR_INVALID;
-    msd_status st = enter(p, "msd_rope_positions");
+    msd_status st = enter(p, "msd_rope_positions", static_cast<cudaStream_t>(stream));
     if (st != MSD_OK) return st;
     BatchView b;
     if (!batch_view(p, batch, &b) || !pos || (span_start && (!spans || n_spans < 0)) || pos_stride < b.rows)
@@ -1049,7 +1078,7 @@ msd_status msd_rope_append(msd_pages *p, int32_t layer, const msd_batch *batch, 
                            const void *k, int64_t ldk, const void *v, int64_t ldv, int32_t src_dtype,
                            const int32_t *pos, int64_t pos_stride, void *out, int64_t ldo, void *stream) {
     if (!p) return MSD_ERR_INVALID;
-    msd_status st = enter(p, "msd_rope_append");
+    msd_status st = enter(p, "msd_rope_append", static_cast<cudaStream_t>(stream));
     if (st != MSD_OK) return st;
     BatchView b;
     const msd_pages_config &c = p->cfg;
@@ -1076,7 +1105,7 @@ msd_status msd_pages_attention(msd_pages *p, int32_t layer, const msd_batch *bat
                                int32_t tree_nodes, int32_t window, int32_t sinks, const void *q, int64_t ldq, void *out,
                                int64_t ldo, float *lse, void *stream) {
     if (!p) return MSD_ERR_INVALID;
-    msd_status st = enter(p, "msd_pages_attention");
+    msd_status st = enter(p, "msd_pages_attention", static_cast<cudaStream_t>(stream));
     if (st != MSD_OK) return st;
     BatchView b;
     const msd_pages_config &c = p->cfg;

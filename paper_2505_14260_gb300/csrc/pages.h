@@ -31,10 +31,19 @@ struct PagesView {
     int *len, *refs;
     unsigned *bits;           // bit p % 32 of word p / 32: page p is free
     int *status;
+    int *refused;             // not 0: a page operation was not carried out and the host has not seen it
     int layers, heads, kv_heads, head_dim, page, page_shift;
     int n_pages, max_seqs, max_pages;
     __host__ __device__ long page_elems() const { return 2l * kv_heads * page * head_dim; }
 };
+
+// A page operation that cannot be carried out (one thread calls it, before anything has changed). The calls queued
+// behind it, recorded ones too, were made for what it should have done, so they do nothing: the host takes the mark
+// away, in the stream's order, with the call that reports the status word.
+__device__ __forceinline__ void refuse(const PagesView &v, int code) {
+    set_status(v.status, code);
+    *v.refused = 1;
+}
 
 // the rows of a call (msd_batch)
 struct BatchView {

@@ -57,7 +57,8 @@ struct Segment {
 };
 
 // Fills s (whole CTA, THREADS threads; ends with a barrier). Sequences that cannot be read
-// (ids, lengths or row counts out of range) get no steps and set the status word.
+// (ids, lengths or row counts out of range) get no steps and set the status word; behind a page
+// operation that was not carried out no sequence gets any.
 template <int ROWS, int KT, int THREADS>
 __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int ctas) {
     __shared__ long long s_sum[THREADS / 32];
@@ -66,6 +67,7 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
     constexpr int NW = THREADS / 32;
     // steps of each sequence: a thread's own loop over few tiles, a warp's over many
     bool many = false;
+    const int refused = *v.refused;
     for (int i = tid; i < a.b.n; i += THREADS) {
         const int seq = a.b.seqs[i], r0 = a.b.row_start[i], r1 = a.b.row_start[i + 1];
         int len = 0, rows = r1 - r0;
@@ -74,10 +76,8 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
             len = v.len[seq];
             ok = len >= rows && len <= (long)v.max_pages * v.page && (!a.mask || rows <= a.nodes);
         }
-        if (!ok) {
-            set_status(v.status, ST_BAD_BATCH);
-            rows = 0;
-        }
+        if (!ok && !refused) set_status(v.status, ST_BAD_BATCH);
+        if (!ok || refused) rows = 0;
         s.len[i] = len;
         s.rows[i] = rows;
         const int tiles = (rows * G + ROWS - 1) / ROWS;

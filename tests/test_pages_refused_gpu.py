@@ -31,6 +31,132 @@ def reported(p, status):
 
 
 # ---------------------------------------------------------------------------
+# Calls queued behind one that could not be carried out
+# ---------------------------------------------------------------------------
+def step(p, seqs, rows, *, reserve=True):
+    """A pass of a model over new rows, as it is queued: room, rotation and K/V, attention, then the first two
+    rows of each stay. Returns what it writes beside the pool."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    n = len(seqs) * rows
+    x = torch.randn(n, 8 * 64, generator=g, device="cuda").to(p.dtype)
+    q, out = (torch.full((n, 4, 64), 7.0, device="cuda", dtype=p.dtype) for _ in range(2))
+    lse, pos = torch.full((n, 4), 7.0, device="cuda"), i32([list(range(n))])
+    b, n_keep = batch(seqs, [rows] * len(seqs)), i32([2] * len(seqs))
+
+    def run():
+        if reserve:
+            p.reserve(b)
+        p.rope_append(0, b, x[:, :256], x[:, 256:384], x[:, 384:], pos, q)
+        p.attention(0, b, q, out, lse=lse)
+        p.compact(b, None, n_keep)
+    return run, (q, out, lse)
+
+
+def shared_pool(dtype="bf16"):
+    """Sequences 0 and 1 share four full pages, 2 holds six of its own; one page is free."""
+    p = pool([64, 96], dtype=dtype, extra_seqs=3, spare=1, extra_pages=8)
+    p.fork(i32([0]), i32([2]))
+    torch.cuda.synchronize()
+    return p
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("graph", [False, True])
+def test_calls_behind_a_failed_reserve_change_nothing(dtype, graph):
+    """Too few pages, then the rest of the pass before the host can know of it: nothing changes, not even the
+    outputs; after the error has been reported and pages are free, the same calls run."""
+    p = shared_pool(dtype)
+    run, outs = step(p, [0, 2], 20)                  # four pages; one is free
+    one, src, dst = i32([1]), i32([0]), i32([3])
+    before = state(p)
+    if graph:
+        recorded = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(recorded):
+            run()
+        for _ in range(3):
+            recorded.replay()
+    else:
+        torch.cuda._sleep(40_000_000)                # what follows is queued before any of it runs
+        run()
+        p.free(one)
+        p.fork(src, dst)
+    torch.cuda.synchronize()
+    assert same(p, before)
+    assert all((t == 7).all() for t in outs)
+    reported(p, msd.MSD_ERR_CAPACITY)
+    p.free(one)
+    recorded.replay() if graph else run()
+    torch.cuda.synchronize()
+    assert p.lens.tolist() == [66, 0, 66, 0, 0] and not any((t == 7).all() for t in outs)
+    assert torch.equal(p.table[0, :4], p.table[2, :4]) and p.table[0, 4] != p.table[2, 4]
+    p.restore()                                      # nothing is pending
+
+
+@pytest.mark.parametrize("fail", ["fork", "compact", "free"])
+def test_calls_behind_other_failed_operations_change_nothing(fail):
+    p = shared_pool()
+    p.free(i32([1]))
+    run, outs = step(p, [0, 2], 20)
+    zero, two, pair, five = i32([0]), i32([2]), i32([0, 77]), batch([0], [5])
+    keep = i32([[1, 0]])
+    before = state(p)
+    torch.cuda._sleep(40_000_000)                    # what follows is queued before any of it runs
+    if fail == "fork":
+        p.fork(zero, two)                            # in use
+    elif fail == "compact":
+        p.compact(five, keep, two)
+    else:
+        p.free(pair)
+    run()
+    torch.cuda.synchronize()
+    assert same(p, before) and all((t == 7).all() for t in outs)
+    reported(p, msd.MSD_ERR_DEVICE)
+    run()
+    torch.cuda.synchronize()
+    assert p.lens.tolist() == [66, 0, 66, 0, 0]
+
+
+def test_an_error_that_the_host_has_not_seen_is_not_cleared_with_an_earlier_one():
+    """The host is told of an attention's error while a reserve that will fail is still queued: what it queues
+    then waits for the reserve's own error to be reported."""
+    p = shared_pool()
+    x, one, told = torch.zeros(1, 4, 64, device="cuda", dtype=p.dtype), batch([4], [1]), torch.cuda.Event()
+    b, n_keep = batch([0, 2], [20, 20]), i32([2, 2])
+    before = state(p)
+    torch.cuda._sleep(40_000_000)
+    p.attention(0, one, x, x)                        # a row of a sequence without tokens
+    told.record()
+    torch.cuda._sleep(100_000_000)
+    p.reserve(b)
+    told.synchronize()
+    with pytest.raises(msd.MsdError) as e:
+        p.restore()
+    assert e.value.status == msd.MSD_ERR_DEVICE
+    p.compact(b, None, n_keep)
+    torch.cuda.synchronize()
+    assert same(p, before)
+    reported(p, msd.MSD_ERR_CAPACITY)
+    p.free(one.seqs)
+
+
+def test_an_error_met_while_recording_is_reported_again():
+    """A call that is being recorded reports the error but cannot take note of it: nothing runs then."""
+    p = shared_pool()
+    p.reserve(batch([0], [40]))
+    torch.cuda.synchronize()
+    x = torch.ones(1, device="cuda")
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        x.add_(1)
+        for _ in range(2):
+            with pytest.raises(msd.MsdError):
+                p.restore()
+    reported(p, msd.MSD_ERR_CAPACITY)
+    p.reserve(batch([0], [16]))
+    torch.cuda.synchronize()
+    assert int(p.lens[0]) == 80
+
+
+# ---------------------------------------------------------------------------
 # Lists that are refused whole
 # ---------------------------------------------------------------------------
 def test_free_takes_a_list_whole_or_not_at_all():
