@@ -474,7 +474,8 @@ msd_status msd_rope_positions(msd_pages *p, const msd_batch *batch, const int32_
  * k, v to the rows' slots of `layer`. q, k, v: row r at r * ld elements, heads one after
  * another, fp32 (src_dtype MSD_F32, as msd_linear writes them) or the cache dtype. Angles
  * are reduced exactly, products and sums are fp32, rounded once. Pointers and rows are
- * 16-byte aligned. A row without a slot sets the status word and is skipped. */
+ * 16-byte aligned. A row without a slot, or with one on a page that several sequences hold
+ * (none has after msd_pages_reserve), sets the status word; its k and v are skipped. */
 msd_status msd_rope_append(msd_pages *p, int32_t layer, const msd_batch *batch, const void *q_dev, int64_t ldq,
                            const void *k_dev, int64_t ldk, const void *v_dev, int64_t ldv, int32_t src_dtype,
                            const int32_t *pos_dev, int64_t pos_stride, void *q_out_dev, int64_t ldo, void *stream);

@@ -679,8 +679,9 @@ __device__ __forceinline__ void store_run(T *g, const float *x) {
     }
 }
 
-// The slot of a row: elements from the layer's first to its K of head 0, or -1. Whole warp. Up to 32 sequences the lanes
-// hold all of the list after one round trip (then the length, then the page); more are searched.
+// The slot of a row: elements from the layer's first to its K of head 0, or -1 (none, or on a page that other sequences
+// hold as well). Whole warp. Up to 32 sequences the lanes hold all of the list after one round trip (then the length, the
+// page, its count); more are searched.
 __device__ __forceinline__ long row_slot(const PagesView &v, const BatchView &b, int row) {
     const int lane = threadIdx.x & 31;
     int first, next, s;
@@ -701,14 +702,14 @@ __device__ __forceinline__ long row_slot(const PagesView &v, const BatchView &b,
     const int slot = v.len[s] - next + row;
     if (slot < 0 || slot >= (long)v.max_pages * v.page) return -1;
     const int id = v.table[(long)s * v.max_pages + (slot >> v.page_shift)];
-    return (unsigned)id < (unsigned)v.n_pages ? id * v.page_elems() + (slot & (v.page - 1)) * v.head_dim : -1;
+    return (unsigned)id < (unsigned)v.n_pages && v.refs[id] <= 1 ? id * v.page_elems() + (slot & (v.page - 1)) * v.head_dim : -1;
 }
 
 constexpr int ROPE_ROWS = 32, ROPE_THREADS = 256;      // of a CTA, at most
 
 // CTA (P * side rows, a chunk of heads): a thread takes 2 G elements of one head, G of them and the G that they pair
 // with (past the rotated part: 2 G in a row), of P rows, all requested first; where a row's heads do not fill the CTA,
-// `side` rows lie side by side. Meanwhile a warp a row finds its slot (three round trips; only where the chunk has K or V
+// `side` rows lie side by side. Meanwhile a warp a row finds its slot (four round trips; only where the chunk has K or V
 // heads) and the CTA the rows' sines. The angle in turns is the product of the position and a 64-bit fraction mod 1,
 // which whole-number arithmetic gives exactly at any position; its upper 32 bits go to sincospi. Bytes bound it: the
 // rows are read and written once.

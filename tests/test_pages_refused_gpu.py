@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2505_14260_gb300 import build, msd
-from tests.pages_support import batch, i32, pool
+from tests.pages_support import batch, i32, pool, tokens
 
 pytestmark = pytest.mark.gpu
 
@@ -33,7 +33,7 @@ def reported(p, status):
 # ---------------------------------------------------------------------------
 # Calls queued behind one that could not be carried out
 # ---------------------------------------------------------------------------
-def step(p, seqs, rows, *, reserve=True):
+def step(p, seqs, rows):
     """A pass of a model over new rows, as it is queued: room, rotation and K/V, attention, then the first two
     rows of each stay. Returns what it writes beside the pool."""
     g = torch.Generator(device="cuda").manual_seed(5)
@@ -44,8 +44,7 @@ def step(p, seqs, rows, *, reserve=True):
     b, n_keep = batch(seqs, [rows] * len(seqs)), i32([2] * len(seqs))
 
     def run():
-        if reserve:
-            p.reserve(b)
+        p.reserve(b)
         p.rope_append(0, b, x[:, :256], x[:, 256:384], x[:, 384:], pos, q)
         p.attention(0, b, q, out, lse=lse)
         p.compact(b, None, n_keep)
@@ -154,6 +153,29 @@ def test_an_error_met_while_recording_is_reported_again():
     p.reserve(batch([0], [16]))
     torch.cuda.synchronize()
     assert int(p.lens[0]) == 80
+
+
+# ---------------------------------------------------------------------------
+# Pages that several sequences hold
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_on_shared_pages_are_not_written(dtype):
+    """Rows appended without room of their own lie on the fork's pages too: skipped and reported."""
+    p = shared_pool(dtype)
+    before = state(p)
+    q = torch.full((20, 4, 64), 7.0, device="cuda", dtype=p.dtype)
+    g = torch.randn(20, 512, device="cuda").to(p.dtype)
+    p.rope_append(0, batch([0], [20]), g[:, :256], g[:, 256:384], g[:, 384:], i32([list(range(20))]), q)
+    torch.cuda.synchronize()
+    assert same(p, before) and not (q == 7).any()
+    reported(p, msd.MSD_ERR_DEVICE)
+    p.free(i32([2]))                                 # now they are its own
+    p.rope_append(0, batch([0], [20]), g[:, :256], g[:, 256:384], g[:, 384:], i32([list(range(20))]), q)
+    p.restore()
+    torch.cuda.synchronize()
+    p.restore()
+    _, v = tokens(p, 0, 0)
+    assert torch.equal(v[44:], g[:, 384:].double().view(20, 2, 64))
 
 
 # ---------------------------------------------------------------------------
