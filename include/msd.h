@@ -489,7 +489,9 @@ msd_status msd_rope_append(msd_pages *p, int32_t layer, const msd_batch *batch, 
  * past it see nothing). window > 0: a token at place P is seen from place Q only if
  * Q - P < window or P < sinks; a row's place is L + r, with a tree L + its depth. A row that
  * sees nothing gives zeros and -inf. Values that are not finite reach only the rows that
- * see them; what a page holds past a sequence's end is never read into a result.
+ * see them; what a page holds past a sequence's end is never read into a result. An entry of
+ * the table below a sequence's length that is no page sets the status word; K and V of its
+ * tokens count as zeros.
  * q, out: row r at r * ld elements, heads one after another, 16-byte aligned rows.
  * rows * (n_heads / n_kv_heads) < 2^26. */
 msd_status msd_pages_attention(msd_pages *p, int32_t layer, const msd_batch *batch, const msd_tree *tree,

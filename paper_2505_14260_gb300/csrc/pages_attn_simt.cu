@@ -86,7 +86,8 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
             for (int e = tid; e < KT * (HD / 4); e += THREADS) {
                 const int k = e / (HD / 4), c = (e - k * (HD / 4)) * 4, slot = key0 + k;
                 int id = slot < len ? table[slot >> v.page_shift] : -1;
-                const bool live = (unsigned)id < (unsigned)v.n_pages;
+                const bool live = (unsigned)id < (unsigned)v.n_pages;         // (else zeros)
+                if (!live && slot < len) set_status(v.status, ST_RANGE);
                 copy16(dst + k * L::LD + c,
                        live ? kv + id * v.page_elems() + ((long)(what * v.kv_heads + g.h) * v.page + (slot & (v.page - 1))) * HD + c : kv,
                        live);

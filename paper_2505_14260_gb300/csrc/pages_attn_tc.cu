@@ -514,7 +514,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
         int filled = 0;
         bool ok = true;
         struct Tile {
-            int id, n, y0;                // the lane's page, pages, the row of page 0's K head
+            int id, n, y0;                // the lane's page (-1: none, read as zeros), pages, the row of page 0's K head
         };
         auto load = [&](const Tile &x, int what) {
             if (!w_wait(empty0 + 8 * at.slot, at.phase ^ 1u, &s_abort, status)) return false;
@@ -523,7 +523,8 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             w_expect_tx(on, bar, (uint32_t)x.n * page_bytes * L::NB);
             const int y0 = x.y0 + what * page_rows;
             for (int i = 0; i < x.n; ++i, dst += page_bytes) {
-                const int y = y0 + __shfl_sync(0xffffffffu, x.id, i) * 2 * page_rows;
+                const int id = __shfl_sync(0xffffffffu, x.id, i);
+                const int y = id < 0 ? -v.page : y0 + id * 2 * page_rows;         // (before the pool's first row: zeros)
 #pragma unroll
                 for (int b = 0; b < L::NB; ++b) w_tma2d(on, dst + b * L::BOX, &map, 64 * b, y, bar);
             }
@@ -564,7 +565,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                 return true;
             }
             if ((unsigned)x.id >= (unsigned)v.n_pages) {
-                x.id = 0;
+                x.id = -1;
                 set_status(status, ST_RANGE);
             }
             return load(x, 0) && fetch();

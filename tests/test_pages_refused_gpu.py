@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2505_14260_gb300 import build, msd
-from tests.pages_support import batch, i32, pool, tokens
+from tests.pages_support import attend, batch, bounds, i32, pool, tokens
 
 pytestmark = pytest.mark.gpu
 
@@ -156,7 +156,7 @@ def test_an_error_met_while_recording_is_reported_again():
 
 
 # ---------------------------------------------------------------------------
-# Pages that several sequences hold
+# Pages that several sequences hold, pages that are none
 # ---------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_on_shared_pages_are_not_written(dtype):
@@ -176,6 +176,37 @@ def test_rows_on_shared_pages_are_not_written(dtype):
     p.restore()
     _, v = tokens(p, 0, 0)
     assert torch.equal(v[44:], g[:, 384:].double().view(20, 2, 64))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("entry", [-1, 1 << 20])
+def test_an_entry_that_is_no_page_is_read_as_zeros_and_reported(dtype, page, entry):
+    """In the middle of a sequence, and its last page: K and V there count as zeros, in both types; other
+    sequences are as they were."""
+    p = pool([5 * page + 3, 3 * page, 2 * page], dtype=dtype, page=page, heads=4, kv_heads=2)
+    counts = [40, 9, 1]
+    kv = [tokens(p, 0, s) for s in range(3)]
+    for s, k in ((0, 1), (0, 5), (1, 2)):
+        p.table[s, k] = entry
+        for x in kv[s]:
+            x[k * page:(k + 1) * page] = 0
+    for window, sinks in ((0, 0), (4 * page, 3)):
+        q = torch.randn(sum(counts), 4, 64, device="cuda").to(p.dtype)
+        out, lse = torch.full_like(q, 7.0), torch.zeros(sum(counts), 4, device="cuda")
+        p.attention(0, batch([0, 1, 2], counts), q, out, lse=lse, window=window, sinks=sinks)
+        reported(p, msd.MSD_ERR_DEVICE)
+        at = 0
+        for (k, v), n in zip(kv, counts):
+            place = torch.arange(k.shape[0], device="cuda")
+            ok = place[None] <= place[-n:, None]
+            if window:
+                ok &= (place[-n:, None] - place[None] < window) | (place < sinks)[None]
+            ref, rl = attend(q[at:at + n], k, v, ok)
+            bo, bl = bounds(q[at:at + n], k, v, ref, rl, dtype)
+            assert bool(((out[at:at + n].double() - ref).abs() <= bo).all())
+            assert bool(((lse[at:at + n].double() - rl).abs() <= bl).all())
+            at += n
 
 
 # ---------------------------------------------------------------------------
