@@ -27,7 +27,9 @@
 // Hidden keys: S is replaced before it is used, so what K holds there does not matter. V does,
 // because 0 * NaN is a NaN: in a tile that some row does not see in full, the group looks
 // through V in shared memory before P V, zeroes slots past the sequence's end, and zeroes values
-// that are not finite after noting so; the item's end then adds those that a row does see.
+// that are not finite after noting the step; the item's end then goes over the noted steps' keys and adds
+// those that a row does see. Such tiles lie at the diagonal, at a window's edges and in a tree, so they are
+// few however long the prompt is.
 #include <cstring>
 #include <type_traits>
 
@@ -275,11 +277,16 @@ struct Seg {
     int len, base, rows, live;        // tokens, tokens before the rows, rows, rows that exist in its tree
     int m0, n, nx[2];                 // first packed row, steps (0: no more segments), steps of each group
     int u0;                           // the CTA's steps before it
+    int full_start, full_end;         // a tile within these is seen in full by all rows that see anything
+    unsigned odd;                     // bit t % 32: V of step t had values that are not finite, taken out
     int j0, sink_tiles, lo, whole;    // first step; which key tiles the steps are; the item's only segment
     long part;                        // its partial results' first row
     __device__ int key(int t) const {
         const int j = j0 + t;
         return (j < sink_tiles ? j : lo + j - sink_tiles) * KT;
+    }
+    __device__ bool full(const PagesAttn &a, int key0) const {
+        return key0 + KT <= full_end && (key0 >= full_start || key0 + KT <= a.sinks);
     }
 };
 
@@ -317,11 +324,12 @@ __device__ __forceinline__ void seen_bits(const PagesAttn &a, const Seg &d, cons
 }
 
 // Values of V that a tile's look-through took out, and that the row sees: added to eight of its columns.
-__device__ __noinline__ void add_odd(const PagesAttn &a, const Seg &d, Row x, int hd, int col, float *acc) {
+// (A tile that one group of a pair sees in full may have been looked through by the other.)
+__device__ __noinline__ void add_odd(const PagesAttn &a, const Seg &d, unsigned odd, Row x, int hd, int col, float *acc) {
     const PagesView &v = a.pv;
     for (int t = 0; t < d.n; ++t) {
         const int key0 = d.key(t);
-        if (key0 + KT <= d.base + (a.mask ? 0 : 1) && !a.window) continue;      // seen in full by all rows: left as it was
+        if (!(odd >> (t & 31) & 1u) || d.full(a, key0)) continue;
         uint32_t w[4];
         seen_bits(a, d, x, key0, w);
         for (int k = 0; k < KT; ++k) {
@@ -403,7 +411,6 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * SLOTS + 10 + 2 * SEGS];
     __shared__ uint32_t s_tmem;
-    __shared__ unsigned s_odd;            // bit i % 32: segment i had values of V that are not finite zeroed
     __shared__ volatile int s_abort;
     __shared__ Seg s_seg[SEGS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -432,7 +439,6 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             bar_init(g_empty0 + 8 * i, 2 + 256);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        s_odd = 0;
         s_abort = 0;
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
     }
@@ -492,6 +498,10 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                         d.nx[u0 & 1] = (d.n + 1) / 2;
                         d.nx[(u0 & 1) ^ 1] = d.n / 2;
                     }
+                    d.full_end = d.base + (a.mask ? 0 : group_div(a, d.m0) + 1);
+                    d.full_start = !a.window ? 0
+                                   : d.base + (a.mask ? a.nodes : group_div(a, min(d.m0 + ROWS, d.rows * G) - 1)) - a.window + 1;
+                    d.odd = 0;
                     d.u0 = u0;
                     u0 += d.n;
                 }
@@ -877,8 +887,8 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                 if (!full) {
                     const int pos = ring_v<LEAD>(d.u0 + tt);
                     wait(full0 + 8 * (pos % SLOTS), (uint32_t)(pos / SLOTS) & 1u);
-                    clean_row<L::NB>(sm + L::RING + (pos % SLOTS) * L::MAT + m * 128, L::BOX, lane, key0 + m < d.len, &s_odd,
-                                     1u << (seg & 31));
+                    clean_row<L::NB>(sm + L::RING + (pos % SLOTS) * L::MAT + m * 128, L::BOX, lane, key0 + m < d.len,
+                                     &s_seg[seg % SEGS].odd, 1u << (tt & 31));
                     fence_proxy();
                 }
                 fence_before();
@@ -921,7 +931,8 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             const bool two = !PAIR && n > 1;
             const int cols = two ? HD / 2 : HD, col0 = two ? x * (HD / 2) : 0;
             const bool none = sum == 0.f;            // the row sees nothing: zeros, whatever O holds
-            const bool whole = d.whole, odd = s_odd >> (seg & 31) & 1u;
+            const bool whole = d.whole;
+            const unsigned odd = d.odd;
             const int head = d.h * G + pm - r * G;
             const long row = d.start + r, part = d.part + (PAIR ? x * TILE : 0) + m;
             if (nx > 0) {
@@ -947,7 +958,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
 #pragma unroll 1
                         for (int e = 0; e < 32; e += 8) {
                             float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                            add_odd(a, d, rw, HD, col0 + c + e, y);
+                            add_odd(a, d, odd, rw, HD, col0 + c + e, y);
 #pragma unroll
                             for (int k = 0; k < 16; ++k)
                                 if (k / 4 == e / 8) acc[k] = add2(acc[k], pack2f(y[2 * (k & 3)], y[2 * (k & 3) + 1]));

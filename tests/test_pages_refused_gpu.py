@@ -247,3 +247,24 @@ def test_free_of_a_long_list():
     p.free(b.seqs)
     torch.cuda.synchronize()
     assert not p.refs.any() and not p.lens.any() and (p.table == -1).all()
+
+
+# ---------------------------------------------------------------------------
+# Values that are not finite in a long prompt
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("window,sinks", [(0, 0), (4096, 2)])
+def test_a_long_prompt_with_values_that_are_not_finite(window, sinks):
+    """Some entries of V: the rows that see them have them in their columns, everything else is what it is
+    without them, to the bit, and the launch ends by itself (no wait runs out)."""
+    n = 131072
+    p = pool([n], heads=8, kv_heads=1, head_dim=128, page=128, stale=0.0)
+    q = torch.randn(n, 8, 128, device="cuda").to(p.dtype)
+    b, want, got = batch([0], [n]), torch.empty_like(q), torch.empty_like(q)
+    p.attention(0, b, q, want, window=window, sinks=sinks)
+    for slot, col, value in ((5, 3, float("nan")), (70000, 40, float("inf")), (n - 9, 100, -float("inf"))):
+        p.kv[0, p.table[0, slot // 128].long(), 1, 0, slot % 128, col] = value
+        want[slot:slot + window if window else n, :, col] = value
+    p.attention(0, b, q, got, window=window, sinks=sinks)
+    torch.cuda.synchronize()
+    p.restore()                                      # nothing to report
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(), want.nan_to_num())
