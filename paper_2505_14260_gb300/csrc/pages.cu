@@ -470,12 +470,12 @@ __global__ void __launch_bounds__(256) compact_apply_kernel(const PagesView v, c
     wait_prior();
     allow_dependents();
     if (!c.flags[2]) return;
-    const int i = blockIdx.x;
+    const int i = blockIdx.y;
     const int *p = c.plan + PLAN_INTS * i;
     const int s = p[0], base = p[1], after = p[2], k0 = p[3], was = p[4], now = p[5];
     const int *old = c.old_table + (long)i * v.max_pages, *rank = c.rank + (long)i * v.max_pages;
     const int *ids = c.fresh + c.off[i];
-    if (blockIdx.y == 0) {
+    if (blockIdx.x == 0) {
         int *row = row_of(v, s);
         for (int k = k0 + threadIdx.x; k < was; k += blockDim.x) {
             const int r = rank[k];
@@ -491,7 +491,7 @@ __global__ void __launch_bounds__(256) compact_apply_kernel(const PagesView v, c
         if (threadIdx.x == 0) v.len[s] = after;
     }
     const int lanes = v.head_dim * ESZ / 16, unit = threadIdx.x / lanes, lane = threadIdx.x % lanes;
-    const int group = blockIdx.y * (256 / lanes / side) + unit / side, tok = unit % side;
+    const int group = blockIdx.x * (256 / lanes / side) + unit / side, tok = unit % side;
     const int layer = group / (2 * v.kv_heads), kvh = group - layer * 2 * v.kv_heads;
     const long pe16 = v.page_elems() * ESZ / 16;
     uint4 *kv = static_cast<uint4 *>(v.kv) + (long)layer * v.n_pages * pe16 + (long)kvh * v.page * lanes + lane;
@@ -1045,8 +1045,7 @@ msd_status msd_pages_compact(msd_pages *p, const msd_batch *batch, const int32_t
         const int units = 256 / (p->cfg.head_dim * (p->cfg.dtype == MSD_F32 ? 4 : 2) / 16);
         // lists of 64 and more side by side (16 lists of 1027, 8 layers of 8 heads, with the fork before them: 99 us, and 227 one by one)
         const int side = keep && keep_stride < 64 ? 1 : std::min(units, 16);
-        const dim3 grid(b.n, (groups + units / side - 1) / (units / side));
-        if (grid.y > 65535) return pfail(p, MSD_ERR_INVALID, "more layers and heads than a launch takes");
+        const dim3 grid((groups + units / side - 1) / (units / side), b.n);        // (sequences are few enough for y, groups need not be)
         e = p->cfg.dtype == MSD_F32 ? chain(compact_apply_kernel<4, 8>, grid, 256, s, p->v, c, groups, side)
                                     : chain(compact_apply_kernel<2, 8>, grid, 256, s, p->v, c, groups, side);
     }

@@ -268,3 +268,26 @@ def test_a_long_prompt_with_values_that_are_not_finite(window, sinks):
     torch.cuda.synchronize()
     p.restore()                                      # nothing to report
     assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(), want.nan_to_num())
+
+
+# ---------------------------------------------------------------------------
+# Limits
+# ---------------------------------------------------------------------------
+def test_compaction_of_a_pool_of_many_layers():
+    """More (layer, K or V) pairs than a launch's y extent; shared pages are replaced in every layer."""
+    layers = 65535
+    p = msd.Pages(dtype="bf16", layers=layers, heads=1, kv_heads=1, head_dim=128, page_size=16, n_pages=4, max_seqs=2,
+                  max_pages=3)
+    p.reserve(batch([0], [32]))
+    p.kv.view(layers, -1).copy_(torch.arange(layers, device="cuda")[:, None].remainder(251))
+    p.kv[:, :, :, :, 16 - 3:] += 1000
+    p.fork(i32([0]), i32([1]))
+    p.compact(batch([0], [3]), None, i32([1]))
+    p.compact(batch([1], [20]), i32([[0, 18]]), i32([2]))
+    torch.cuda.synchronize()
+    assert p.lens.tolist() == [30, 14] and int(p.refs.sum()) == 3
+    for seq, slot, value in ((0, 12, 0), (0, 13, 1000), (0, 28, 0), (0, 29, 1000), (1, 11, 0), (1, 12, 0), (1, 13, 1000)):
+        page = p.kv[:, p.table[seq, slot // 16].long(), :, 0, slot % 16].float()
+        assert torch.equal(page, (torch.arange(layers, device="cuda") % 251 + value)[:, None, None].to(p.dtype).float().expand_as(page))
+    del p
+    torch.cuda.empty_cache()
