@@ -144,6 +144,9 @@ __global__ void restore_bits_kernel(const PagesView v) {
 
 // ---- after an error --------------------------------------------------------
 
+// (The operations read the mark beside their lists and look at it once those are there, so that it costs no round trip
+// of its own.)
+
 // Behind the calls that were held back: they may run again, unless one of them has met an error of its own since the
 // host took the status word (that is yet to be seen).
 __global__ void resume_kernel(const PagesView v) {
@@ -161,15 +164,15 @@ __global__ void __launch_bounds__(128) free_kernel(const PagesView v, int n, con
     __shared__ int s_len;
     wait_prior();
     allow_dependents();
-    bool bad = *v.refused;                // (also by CTA 0 of this launch, then the others come to it too)
-    for (int i = threadIdx.x; !bad && i < n; i += blockDim.x) {
+    const int held = *v.refused;          // (or by CTA 0 of this launch: then the others find the same)
+    int code = 0;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
         const int s = seqs[i];
-        const bool known = seq_ok(v, s);
-        if (known && len_ok(v, v.len[s])) continue;
-        bad = true;
-        if (blockIdx.x == 0) refuse(v, known ? ST_RANGE : ST_BAD_BATCH);
+        if (!seq_ok(v, s)) code = ST_BAD_BATCH;
+        else if (!len_ok(v, v.len[s])) code = ST_RANGE;
     }
-    if (__syncthreads_or(bad)) return;
+    if (code && !held && blockIdx.x == 0) refuse(v, code);
+    if (__syncthreads_or(code | held)) return;
     for (int i = blockIdx.x; i < n; i += gridDim.x) {
         const int s = seqs[i];
         if (threadIdx.x == 0) s_len = atomicExch(v.len + s, 0);
@@ -194,7 +197,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) reserve_kernel(const PagesView v
     __shared__ int s_scan[33], s_bad;
     wait_prior();
     allow_dependents();
-    if (*v.refused) return;
+    const int held = *v.refused;
     if (threadIdx.x == 0) s_bad = 0;
     __syncthreads();
     int total = 0;
@@ -222,6 +225,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) reserve_kernel(const PagesView v
     __syncthreads();
     for (int i = threadIdx.x; i < b.n; i += blockDim.x)
         if (seq_ok(v, b.seqs[i])) mark[b.seqs[i]] = 0;
+    if (held) return;
     if (s_bad) {
         if (threadIdx.x == 0) refuse(v, ST_BAD_BATCH);
         return;
@@ -254,10 +258,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(const PagesView
     __shared__ int s_scan[33], s_bad;
     wait_prior();
     allow_dependents();
-    if (*v.refused) {
-        if (threadIdx.x == 0) *ok_out = 0;
-        return;
-    }
+    const int held = *v.refused;
     if (threadIdx.x == 0) s_bad = 0;
     __syncthreads();
     int total = 0;
@@ -287,10 +288,10 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(const PagesView
     for (int i = threadIdx.x; i < n; i += blockDim.x)
         if (seq_ok(v, dst[i])) mark[dst[i]] = 0;
     const bool bad = s_bad != 0;
-    const bool ok = !bad && total <= v.n_pages && take_pages(v, total, fresh, s_scan);
+    const bool ok = !bad && !held && total <= v.n_pages && take_pages(v, total, fresh, s_scan);
     if (threadIdx.x == 0) {
         *ok_out = ok;
-        if (!ok) refuse(v, bad ? ST_BAD_BATCH : ST_NO_PAGES);
+        if (!ok && !held) refuse(v, bad ? ST_BAD_BATCH : ST_NO_PAGES);
     }
 }
 
@@ -367,10 +368,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(const PagesV
     __shared__ int s_scan[33], s_first, s_bad, s_last;
     wait_prior();
     allow_dependents();
-    if (*v.refused) {                                 // (set by the launch's last CTA at the earliest, so the same for all)
-        if (blockIdx.x == 0 && threadIdx.x == 0) c.flags[2] = 0;
-        return;
-    }
+    const int held = *v.refused;                      // (set by the launch's last CTA at the earliest, so the same for all)
     const int i = blockIdx.x;
     const int s = b.seqs[i];
     const int rows = b.row_start[i + 1] - b.row_start[i];
@@ -446,13 +444,13 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(const PagesV
         total = min(total + sum, v.n_pages + 1);
     }
     const bool bad = __ldcg(c.flags + 1) != 0;
-    const bool ok = !bad && total <= v.n_pages && take_pages(v, total, c.fresh, s_scan);
+    const bool ok = !bad && !held && total <= v.n_pages && take_pages(v, total, c.fresh, s_scan);
     __syncthreads();
     if (threadIdx.x == 0) {
         c.flags[0] = 0;
         c.flags[1] = 0;
         c.flags[2] = ok;
-        if (!ok) refuse(v, bad ? ST_BAD_BATCH : ST_NO_PAGES);
+        if (!ok && !held) refuse(v, bad ? ST_BAD_BATCH : ST_NO_PAGES);
     }
 }
 
@@ -725,7 +723,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const PagesVi
     const int h0 = blockIdx.y * chunk, hn = min(chunk, v.heads + 2 * v.kv_heads - h0);
     const int row0 = blockIdx.x * P * side, rows = min(P * side, b.rows - row0);
     const int at = tid / (chunk * units), rest = tid - at * chunk * units, head = h0 + rest / units, unit = rest % units;
-    const int refused = *v.refused;                           // (asked for first, looked at before anything is written)
+    const int held = *v.refused;                              // (asked for first, looked at before anything is written)
     const bool live = at < side && head < h0 + hn;
     // first elements of the two runs
     const bool in = unit * G < a.half;
@@ -756,12 +754,12 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const PagesVi
             const long slot = row_slot(v, b, row0 + u);
             if ((tid & 31) == 0) {
                 s_slot[u] = slot;
-                if (slot < 0 && !refused) set_status(v.status, ST_RANGE);
+                if (slot < 0 && !held) set_status(v.status, ST_RANGE);
             }
         }
     }
     __syncthreads();
-    if (!live || refused) return;
+    if (!live || held) return;
     TD *dst = is_q ? static_cast<TD *>(a.out) + row0 * a.ldo + (long)head * hd
                    : static_cast<TD *>(v.kv) + (long)a.layer * v.n_pages * v.page_elems() + (long)(head - v.heads) * v.page * hd;
 #pragma unroll

@@ -67,17 +67,17 @@ __device__ void attn_schedule(const PagesAttn &a, AttnSched &s, int cta, int cta
     constexpr int NW = THREADS / 32;
     // steps of each sequence: a thread's own loop over few tiles, a warp's over many
     bool many = false;
-    const int refused = *v.refused;
     for (int i = tid; i < a.b.n; i += THREADS) {
         const int seq = a.b.seqs[i], r0 = a.b.row_start[i], r1 = a.b.row_start[i + 1];
+        const int held = *static_cast<volatile const int *>(v.refused);      // (asked for with the others, not before them)
         int len = 0, rows = r1 - r0;
         bool ok = (unsigned)seq < (unsigned)v.max_seqs && r0 >= 0 && rows >= 0 && r1 <= a.b.rows;
         if (ok) {
             len = v.len[seq];
             ok = len >= rows && len <= (long)v.max_pages * v.page && (!a.mask || rows <= a.nodes);
         }
-        if (!ok && !refused) set_status(v.status, ST_BAD_BATCH);
-        if (!ok || refused) rows = 0;
+        if (!ok && !held) set_status(v.status, ST_BAD_BATCH);
+        if (!ok || held) rows = 0;
         s.len[i] = len;
         s.rows[i] = rows;
         const int tiles = (rows * G + ROWS - 1) / ROWS;
