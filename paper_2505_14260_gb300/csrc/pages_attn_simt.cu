@@ -80,6 +80,7 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
         const int live_rows = a.mask && a.n_nodes ? min(rows, a.n_nodes[g.i]) : rows;
         const int *table = v.table + (long)a.b.seqs[g.i] * v.max_pages;
         auto key_of = [&](int j) { return (j < g.range.sink_tiles ? j : g.range.lo + j - g.range.sink_tiles) * KT; };
+        bool lost = false;                               // an entry is no page
         // K (what 0) or V (1) of a tile
         auto load = [&](float *dst, int what, int key0) {
 #pragma unroll
@@ -87,7 +88,7 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
                 const int k = e / (HD / 4), c = (e - k * (HD / 4)) * 4, slot = key0 + k;
                 int id = slot < len ? table[slot >> v.page_shift] : -1;
                 const bool live = (unsigned)id < (unsigned)v.n_pages;         // (else zeros)
-                if (!live && slot < len) set_status(v.status, ST_RANGE);
+                lost |= !live && slot < len;
                 copy16(dst + k * L::LD + c,
                        live ? kv + id * v.page_elems() + ((long)(what * v.kv_heads + g.h) * v.page + (slot & (v.page - 1))) * HD + c : kv,
                        live);
@@ -232,6 +233,7 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
                 load(sV, 1, key_of(j + 1));
             }
         }
+        if (lost) set_status(v.status, ST_RANGE);
         const bool whole = segment_whole(g);
         const long slot = part_slot(g, blockIdx.x) * ROWS;
 #pragma unroll

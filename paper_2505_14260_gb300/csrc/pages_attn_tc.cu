@@ -524,17 +524,15 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
         int filled = 0;
         bool ok = true;
         struct Tile {
-            int id, n, y0;                // the lane's page (-1: none, read as zeros), pages, the row of page 0's K head
+            int y, n;                     // the row of the lane's page where its K head begins; pages
         };
         auto load = [&](const Tile &x, int what) {
             if (!w_wait(empty0 + 8 * at.slot, at.phase ^ 1u, &s_abort, status)) return false;
             const uint32_t bar = full0 + 8 * at.slot;
             uint32_t dst = base + L::RING + at.slot * L::MAT;
             w_expect_tx(on, bar, (uint32_t)x.n * page_bytes * L::NB);
-            const int y0 = x.y0 + what * page_rows;
             for (int i = 0; i < x.n; ++i, dst += page_bytes) {
-                const int id = __shfl_sync(0xffffffffu, x.id, i);
-                const int y = id < 0 ? -v.page : y0 + id * 2 * page_rows;         // (before the pool's first row: zeros)
+                const int y = __shfl_sync(0xffffffffu, x.y, i) + what * page_rows;
 #pragma unroll
                 for (int b = 0; b < L::NB; ++b) w_tma2d(on, dst + b * L::BOX, &map, 64 * b, y, bar);
             }
@@ -545,7 +543,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
         // the walk over K tiles, LEAD ahead of V's; V tiles' segments are only counted (for the ring of segments)
         int ks = 0, kt = 0, kn = 0, k_len = 0, k_y0 = 0, k_j0 = 0, k_sinks = 0, k_lo = 0, vs = 0, v_left = 0;
         const int *table = nullptr;
-        Tile ahead{0, 0, 0}, wait_v[LEAD + 1] = {};               // the next K tile; V tiles of the K tiles loaded
+        Tile ahead{0, 0}, wait_v[LEAD + 1] = {};               // the next K tile; V tiles of the K tiles loaded
         auto fetch = [&]() {              // `ahead`: n 0 at the end
             ahead.n = 0;
             if (kt == kn) {
@@ -564,8 +562,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             }
             const int j = k_j0 + kt++, key0 = (j < k_sinks ? j : k_lo + j - k_sinks) * KT, first = key0 >> v.page_shift;
             ahead.n = min(per, ((k_len - 1) >> v.page_shift) - first + 1);
-            ahead.y0 = k_y0;
-            ahead.id = lane < ahead.n ? table[first + lane] : 0;
+            ahead.y = lane < ahead.n ? table[first + lane] : 0;       // (a page id as yet)
             return true;
         };
         auto next_k = [&](Tile &x) {      // loads `ahead` and asks for the one after it; x: its V
@@ -574,8 +571,10 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
                 at.next();
                 return true;
             }
-            if ((unsigned)x.id >= (unsigned)v.n_pages) {
-                x.id = -1;
+            if ((unsigned)x.y < (unsigned)v.n_pages) {
+                x.y = k_y0 + x.y * 2 * page_rows;       // (K's walk is still in its segment)
+            } else {                      // no page: K and V from before the pool's first row, which are zeros
+                x.y = -v.page - page_rows;
                 set_status(status, ST_RANGE);
             }
             return load(x, 0) && fetch();
