@@ -40,13 +40,15 @@ __device__ __forceinline__ void drop_ref(const PagesView &v, int id) {
 }
 
 // Exclusive prefix sum over the CTA; *total gets the sum. s: 33 ints of shared memory.
-__device__ __forceinline__ int block_scan(int x, int *s, int *total) {
+// cap > 0: no sum passes it (for x in 0 .. cap; where the total reaches it the prefixes are of no use).
+__device__ __forceinline__ int block_scan(int x, int *s, int *total, int cap = 0) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
+    auto add = [&](int a, int b) { return cap ? min(a + b, cap) : a + b; };
     int inc = x;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += y;
+        if (lane >= o) inc = add(inc, y);
     }
     __syncthreads();                    // (the previous scan's readers are done)
     if (lane == 31) s[warp] = inc;
@@ -56,13 +58,19 @@ __device__ __forceinline__ int block_scan(int x, int *s, int *total) {
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, t, o);
-            if (lane >= o) t += y;
+            if (lane >= o) t = add(t, y);
         }
         s[lane] = t;
     }
     __syncthreads();
     *total = s[nw - 1];
     return inc - x + (warp ? s[warp - 1] : 0);
+}
+
+// The same of pages that each of a list's sequences needs: sums stop at one more than there are (32 sequences may need
+// 2^31 pages), which the callers refuse.
+__device__ __forceinline__ int pages_scan(const PagesView &v, int need, int *s, int *total) {
+    return block_scan(min(need, v.n_pages + 1), s, total, v.n_pages + 1);
 }
 
 // The `total` lowest free pages, ascending, into fresh[]; their bits cleared. Returns
@@ -218,7 +226,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) reserve_kernel(const PagesView v
             if (!ok) s_bad = 1;
         }
         int sum;
-        const int at = block_scan(need, s_scan, &sum);
+        const int at = pages_scan(v, need, s_scan, &sum);
         if (i < b.n) off[i] = total + at;
         total = min(total + sum, v.n_pages + 1);         // (more than there are: refused below)
     }
@@ -277,7 +285,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(const PagesView
             if (!ok) s_bad = 1;
         }
         int sum;
-        const int at = block_scan(need, s_scan, &sum);
+        const int at = pages_scan(v, need, s_scan, &sum);
         if (i < n) off[i] = total + at;
         total = min(total + sum, v.n_pages + 1);
     }
@@ -436,7 +444,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(const PagesV
     for (int i0 = 0; i0 < b.n; i0 += blockDim.x) {
         const int x = i0 + threadIdx.x;
         int sum;
-        const int at = block_scan(x < b.n ? __ldcg(c.off + x) : 0, s_scan, &sum);
+        const int at = pages_scan(v, x < b.n ? __ldcg(c.off + x) : 0, s_scan, &sum);
         if (x < b.n) {
             c.off[x] = total + at;
             if (seq_ok(v, b.seqs[x])) c.mark[b.seqs[x]] = 0;

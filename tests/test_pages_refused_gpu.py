@@ -249,6 +249,25 @@ def test_free_of_a_long_list():
     assert not p.refs.any() and not p.lens.any() and (p.table == -1).all()
 
 
+def test_page_counts_past_32_bits_are_refused():
+    """Rows that would need 32 x 2^26 pages, more than 32 bits count: refused, nothing grows. (20 GB of tables.)"""
+    p = msd.Pages(dtype="bf16", layers=1, heads=1, kv_heads=1, head_dim=64, page_size=16, n_pages=40, max_seqs=33,
+                  max_pages=1 << 26)
+    p.reserve(batch([32], [5]))
+    for n in (32, 31):
+        b = msd.Batch(i32(list(range(n))), torch.zeros(n + 1, dtype=torch.int32, device="cuda"), 0)
+        # every sequence asks for 2^30 rows: the boundaries wrap, their differences do not
+        b.row_start.copy_(((torch.arange(n + 1) << 30) & 0xffffffff).to(torch.int64).to(torch.int32))
+        p.reserve(b)
+        reported(p, msd.MSD_ERR_CAPACITY)
+        assert p.lens.tolist() == [0] * 32 + [5] and int(p.refs.sum()) == 1
+    p.reserve(batch([0, 1], [30, 17]))
+    torch.cuda.synchronize()
+    assert p.lens[:2].tolist() == [30, 17] and int(p.refs.sum()) == 5
+    del p
+    torch.cuda.empty_cache()
+
+
 # ---------------------------------------------------------------------------
 # Values that are not finite in a long prompt
 # ---------------------------------------------------------------------------
