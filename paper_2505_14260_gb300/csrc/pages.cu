@@ -1148,6 +1148,7 @@ msd_status msd_pages_attention(msd_pages *p, int32_t layer, const msd_batch *bat
     a.window = window;
     a.sinks = window ? sinks : 0;
     a.group = c.n_heads / c.n_kv_heads;
+    a.packed = (int)(((long)b.rows * a.group + b.n - 1) / b.n);
     a.group_magic = ((1ull << 32) + a.group - 1) / a.group;
     a.scale_log2 = 1.4426950408889634f / std::sqrt((float)hd);
     a.part_o = p->part_o;

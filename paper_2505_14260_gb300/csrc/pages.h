@@ -91,6 +91,7 @@ struct PagesAttn {
     int window, sinks;        // window 0: none
     float scale_log2;         // log2(e) / sqrt(head_dim)
     int group;                // query heads of a K/V head
+    int packed;               // packed rows of a sequence, the mean of the whole call (which may take several launches)
     unsigned long long group_magic;        // ceil(2^32 / group): see group_div
     // partial results of row tiles that several CTAs share
     float *part_o, *part_ml;

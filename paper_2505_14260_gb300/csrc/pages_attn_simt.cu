@@ -387,7 +387,7 @@ bool pages_attn_simt_setup() { return setup<64, 16>() && setup<64, 64>() && setu
 
 cudaError_t launch_pages_attn_simt(const PagesAttn &a, int sms, cudaStream_t s) {
     // few packed rows to a sequence: tiles of 16, whose steps are short
-    const bool few = (long)a.b.rows * a.group <= 16l * a.b.n;
+    const bool few = a.packed <= 16;
     if (a.pv.head_dim == 64) return few ? launch<64, 16>(a, sms, s) : launch<64, 64>(a, sms, s);
     return few ? launch<128, 16>(a, sms, s) : launch<128, 64>(a, sms, s);
 }

@@ -1026,11 +1026,10 @@ bool setup() {
 // A tile as large as the sequences' packed rows: a small one leaves room for more key tiles in flight.
 template <int HD>
 cudaError_t launch_rows(const CUtensorMap &map, const PagesAttn &a, int sms, cudaStream_t s) {
-    const long packed = ((long)a.b.rows * (a.pv.heads / a.pv.kv_heads) + a.b.n - 1) / a.b.n;
-    return packed <= 32    ? launch<HD, 32>(map, a, sms, s)
-           : packed <= 64  ? launch<HD, 64>(map, a, sms, s)
-           : packed <= 128 ? launch<HD, 128>(map, a, sms, s)
-                           : launch<HD, 256>(map, a, sms, s);
+    return a.packed <= 32    ? launch<HD, 32>(map, a, sms, s)
+           : a.packed <= 64  ? launch<HD, 64>(map, a, sms, s)
+           : a.packed <= 128 ? launch<HD, 128>(map, a, sms, s)
+                             : launch<HD, 256>(map, a, sms, s);
 }
 
 }  // namespace

@@ -310,3 +310,17 @@ def test_compaction_of_a_pool_of_many_layers():
         assert torch.equal(page, (torch.arange(layers, device="cuda") % 251 + value)[:, None, None].to(p.dtype).float().expand_as(page))
     del p
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sequences_past_one_launch_take_the_tiles_of_the_whole_call(dtype):
+    """The 513th of 513 single tokens is computed as it is by itself, to the bit."""
+    lens = [1 + i % 30 for i in range(512)] + [60000]
+    p = pool(lens, dtype=dtype, heads=8, kv_heads=2, head_dim=128)
+    q = torch.randn(513, 8, 128, device="cuda").to(p.dtype)
+    out, lse = torch.empty_like(q), torch.empty(513, 8, device="cuda")
+    p.attention(0, batch(list(range(513)), [1] * 513), q, out, lse=lse)
+    one, l1 = torch.empty_like(q[:1]), torch.empty(1, 8, device="cuda")
+    p.attention(0, batch([512], [1]), q[512:], one, lse=l1)
+    torch.cuda.synchronize()
+    assert torch.equal(out[512:], one) and torch.equal(lse[512:], l1)
