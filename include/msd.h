@@ -486,7 +486,8 @@ msd_status msd_rope_append(msd_pages *p, int32_t layer, const msd_batch *batch, 
  * rows, and of the rows: those up to itself (tree null: decoding, or a chunk of a prompt),
  * or those whose bit is set in its mask (tree: arrays of stride tree_nodes >= rows per
  * listed sequence, as msd_verify; mask and depth are read, and n_nodes if given: rows at or
- * past it see nothing). window > 0: a token at place P is seen from place Q only if
+ * past it see nothing; depths are 0 .. tree_nodes - 1, and with a window one that is not sets
+ * the status word and counts as the nearest). window > 0: a token at place P is seen from place Q only if
  * Q - P < window or P < sinks; a row's place is L + r, with a tree L + its depth. A row that
  * sees nothing gives zeros and -inf. Values that are not finite reach only the rows that
  * see them; what a page holds past a sequence's end is never read into a result. An entry of

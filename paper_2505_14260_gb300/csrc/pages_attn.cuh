@@ -28,6 +28,12 @@ struct AttnSched {
     long long per;                        // steps of a CTA
 };
 
+// The depth of node j of listed sequence i. Which tiles a window shows in full follows from depths being 0 .. nodes - 1;
+// one that is not counts as the nearest (and is reported: check_depths).
+__device__ __forceinline__ int node_depth(const PagesAttn &a, int i, int j) {
+    return min(max(a.depth[(long)i * a.nodes + j], 0), a.nodes - 1);
+}
+
 // the steps of a tile of rows
 struct TileRange {
     int sink_tiles, lo, steps;            // key tile of step j: j < sink_tiles ? j : lo + j - sink_tiles
@@ -218,6 +224,20 @@ __device__ void name_parts(const PagesAttn &a, const AttnSched &s, int cta) {
         item = PartItem{a.b.row_start[g.i], g.h, g.tile * ROWS, min(s.rows[g.i] * a.group - g.tile * ROWS, ROWS),
                         (int)((s.per * cta - g.j0) / s.per)};
     a.part_item[cta] = item;
+}
+
+// Reports depths out of range of the rows in the CTA's run, a thread every `step`-th of a segment's. (A call of its own,
+// away from the loops: with the report where depths are used, in the bf16 kernel a tree took 24.1 us for 23.4 and 64 ragged
+// tokens 77.3 for 76.2, without any depth to read.)
+template <int ROWS, int KT>
+__device__ __noinline__ void check_depths(const PagesAttn &a, const AttnSched &s, int first, int step) {
+    AttnWalk<ROWS, KT> walk(a, s);
+    Segment g;
+    while (walk.next(g)) {
+        const int live = a.n_nodes ? min(s.rows[g.i], a.n_nodes[g.i]) : s.rows[g.i];
+        for (int r = group_div(a, g.tile * ROWS) + first; r < live && r * a.group < (g.tile + 1) * ROWS; r += step)
+            if ((unsigned)a.depth[(long)g.i * a.nodes + r] >= (unsigned)a.nodes) set_status(a.pv.status, ST_BAD_BATCH);
+    }
 }
 
 }  // namespace msd

@@ -71,6 +71,7 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
     const PagesView &v = a.pv;
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, G = a.group;
     if (tid == 0) name_parts<ROWS, KT>(a, sched, blockIdx.x);
+    if (a.mask && a.window) check_depths<ROWS, KT>(a, sched, tid, THREADS);
     const float *kv = static_cast<const float *>(v.kv) + (long)a.layer * v.n_pages * v.page_elems();
     AttnWalk<ROWS, KT> walk(a, sched);
     Segment g;
@@ -114,7 +115,7 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
             qrow[x] = in ? r : -1;
             const long at = (long)g.i * a.nodes + r;
             mrow[x] = in && a.mask ? a.mask + at * a.words : nullptr;
-            place[x] = base + (a.mask ? (in && a.window ? a.depth[at] : 0) : r);
+            place[x] = base + (a.mask ? (in && a.window ? node_depth(a, g.i, r) : 0) : r);
         }
         // all rows that are there see a whole tile that ends and starts within these
         const bool blind = group_div(a, m0 + nm - 1) >= live_rows;
@@ -165,7 +166,7 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
                         if (ok && node >= 0) {
                             if (a.mask) {
                                 ok = mrow[x][node >> 6] >> (node & 63) & 1;
-                                if (a.window) at = base + a.depth[(long)g.i * a.nodes + node];
+                                if (a.window) at = base + node_depth(a, g.i, node);
                             } else {
                                 ok = node <= qrow[x];
                             }

@@ -314,7 +314,7 @@ __device__ __forceinline__ void seen_bits(const PagesAttn &a, const Seg &d, cons
             if (a.window && x.place - d.base >= a.window) {       // (else all depths up to its own are inside)
                 for (uint32_t left = m; left; left &= left - 1) {
                     const int bit = __ffs(left) - 1;
-                    const int at = d.base + a.depth[(long)d.i * a.nodes + key + bit - d.base];
+                    const int at = d.base + node_depth(a, d.i, key + bit - d.base);
                     if (x.place - at >= a.window && at >= a.sinks) m &= ~(1u << bit);
                 }
             }
@@ -511,6 +511,8 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             if (!have) break;
         }
         if (lane == 0) name_parts<ROWS, KT>(a, sched, blockIdx.x);
+        __syncwarp();
+        if (a.mask && a.window) check_depths<ROWS, KT>(a, sched, lane, 32);
         __syncwarp();
     } else if (warp == 8) {
         // ---- TMA -----------------------------------------------------------
@@ -796,7 +798,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_attn_tc_kernel(const __grid_
             rw.mask = nullptr;
             if (a.mask && rw.r >= 0) {
                 rw.mask = a.mask + ((long)d.i * a.nodes + r) * a.words;
-                if (a.window) rw.place = d.base + a.depth[(long)d.i * a.nodes + r];
+                if (a.window) rw.place = d.base + node_depth(a, d.i, r);
             }
             // every row that sees anything sees a whole tile that ends here at the latest, and starts here at the earliest
             const int full_end = d.base + (a.mask ? 0 : group_div(a, pm0) + 1);

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2505_14260_gb300 import build, msd
-from tests.pages_support import attend, batch, bounds, i32, pool, tokens
+from tests.pages_support import attend, batch, bounds, i32, pool, random_tree, tokens
 
 pytestmark = pytest.mark.gpu
 
@@ -310,6 +310,32 @@ def test_compaction_of_a_pool_of_many_layers():
         assert torch.equal(page, (torch.arange(layers, device="cuda") % 251 + value)[:, None, None].to(p.dtype).float().expand_as(page))
     del p
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_depths_that_no_tree_has_are_reported(dtype):
+    """A window goes by depths: one outside 0 .. tree_nodes - 1 is told, and taken as the nearest that is inside."""
+    p = pool([300, 40], dtype=dtype)
+    t, _, _ = random_tree(2, 20, 3)
+    q = torch.randn(40, 4, 64, device="cuda").to(p.dtype)
+    b, got = batch([0, 1], [20, 20]), []
+    for bad, inside in ((10 ** 6, 19), (-3, 0)):
+        for value in (bad, inside):
+            t.depth.view(2, 20)[0, 7] = value
+            out, lse = torch.empty_like(q), torch.empty(40, 4, device="cuda")
+            p.attention(0, b, q, out, lse=lse, tree=t, window=30, sinks=2)
+            if value == bad:
+                reported(p, msd.MSD_ERR_DEVICE)
+            got.append((out, lse))
+        torch.cuda.synchronize()
+        p.restore()
+        for x, y in zip(got[-2], got[-1]):
+            assert torch.equal(x, y)
+    t.n_nodes[1] = 12
+    t.depth.view(2, 20)[1, 12:] = -9                 # past the tree's nodes: of no account
+    p.attention(0, b, q, out, lse=lse, tree=t, window=30, sinks=2)
+    torch.cuda.synchronize()
+    p.restore()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
