@@ -434,6 +434,8 @@ class Pages:
                  n_pages: int, max_seqs: int, max_pages: int, rot_dim: int | None = None, rot_sections=None,
                  rot_interleaved: bool = False, rope_base: float = 10000.0, kv=None, table=None, lens=None,
                  refs=None, device="cuda"):
+        if dtype not in ("bf16", "f32"):
+            raise ValueError('dtype is "bf16" or "f32"')
         rot_dim = head_dim if rot_dim is None else rot_dim
         sections = (rot_dim // 2, 0, 0) if rot_sections is None else rot_sections
         self.cfg = msd_pages_config(MSD_BF16 if dtype == "bf16" else MSD_F32, layers, heads, kv_heads, head_dim,
