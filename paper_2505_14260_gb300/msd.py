@@ -419,8 +419,8 @@ class Batch:
 
 
 def _ints(t: torch.Tensor | None):
-    if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
-        raise ValueError("index arrays are contiguous int32 tensors")
+    if t is not None and not (t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()):
+        raise ValueError("index arrays are contiguous int32 tensors on the GPU")
     return t
 
 
@@ -450,8 +450,8 @@ class Pages:
         self.table = torch.full((max_seqs, max_pages), -1, **i32) if table is None else table
         self.lens = torch.zeros(max_seqs, **i32) if lens is None else lens
         self.refs = torch.zeros(n_pages, **i32) if refs is None else refs
-        if self.kv.dtype != self.dtype or tuple(self.kv.shape) != shape or not self.kv.is_contiguous():
-            raise ValueError(f"kv is a contiguous tensor of shape {shape} in the pool's type")
+        if self.kv.dtype != self.dtype or tuple(self.kv.shape) != shape or not self.kv.is_contiguous() or not self.kv.is_cuda:
+            raise ValueError(f"kv is a contiguous tensor of shape {shape} in the pool's type, on the GPU")
         for t, n in ((self.table, max_seqs * max_pages), (self.lens, max_seqs), (self.refs, n_pages)):
             if _ints(t).numel() != n:
                 raise ValueError("table, lens and refs have an entry per cell, sequence and page")
@@ -482,9 +482,9 @@ class Pages:
     def _rows(self, t: torch.Tensor, heads: int, rows: int) -> int:
         """The row stride of q, k, v or out: [rows, heads, head_dim] or [rows, heads * head_dim]."""
         hd, shape, stride = self._hd, t.shape, t.stride()
-        if not (shape == (rows, heads * hd) and stride[1] == 1 or
-                shape == (rows, heads, hd) and stride[2] == 1 and (stride[1] == hd or heads == 1)):
-            raise ValueError(f"expected {rows} rows of {heads} heads of {hd} elements, one after another")
+        if not t.is_cuda or not (shape == (rows, heads * hd) and stride[1] == 1 or
+                                 shape == (rows, heads, hd) and stride[2] == 1 and (stride[1] == hd or heads == 1)):
+            raise ValueError(f"expected {rows} rows of {heads} heads of {hd} elements, one after another, on the GPU")
         return stride[0] if rows > 1 else heads * hd
 
     def _on(self, stream) -> int:
@@ -560,10 +560,10 @@ class Pages:
         n, H = batch.rows, self._H
         if q.dtype != self.dtype or out.dtype != self.dtype:
             raise ValueError("q and out have the cache's type")
-        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() != n * H):
-            raise ValueError("lse is a contiguous fp32 tensor [rows, heads]")
-        if tree is not None and tree.B != batch.n:
-            raise ValueError("a tree per listed sequence")
+        if lse is not None and not (lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == n * H):
+            raise ValueError("lse is a contiguous fp32 tensor [rows, heads] on the GPU")
+        if tree is not None and (tree.B != batch.n or not tree.mask.is_cuda):
+            raise ValueError("a tree per listed sequence, on the GPU")
         st = lib().msd_pages_attention(
             self.ptr, layer, batch.c(), None if tree is None else ctypes.byref(tree.c()), 0 if tree is None else tree.N,
             window, sinks, q.data_ptr(), self._rows(q, H, n), out.data_ptr(), self._rows(out, H, n), _ptr(lse),
