@@ -62,6 +62,8 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
     using L = Lay<HD, ROWS>;
     constexpr int R = ROWS / 16, C = HD / 64;            // rows of a thread; groups of 4 columns of O
     extern __shared__ __align__(16) float sm[];
+    __shared__ int s_lost;                               // an entry of the table is no page
+    if (threadIdx.x == 0) s_lost = 0;
     float *sQ = sm + L::Q, *sK = sm + L::K, *sV = sm + L::V;
     unsigned long long *sP = reinterpret_cast<unsigned long long *>(sm + L::P);
     AttnSched &sched = *reinterpret_cast<AttnSched *>(sm + L::SCHED);
@@ -81,7 +83,6 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
         const int live_rows = a.mask && a.n_nodes ? min(rows, a.n_nodes[g.i]) : rows;
         const int *table = v.table + (long)a.b.seqs[g.i] * v.max_pages;
         auto key_of = [&](int j) { return (j < g.range.sink_tiles ? j : g.range.lo + j - g.range.sink_tiles) * KT; };
-        bool lost = false;                               // an entry is no page
         // K (what 0) or V (1) of a tile
         auto load = [&](float *dst, int what, int key0) {
 #pragma unroll
@@ -89,7 +90,7 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
                 const int k = e / (HD / 4), c = (e - k * (HD / 4)) * 4, slot = key0 + k;
                 int id = slot < len ? table[slot >> v.page_shift] : -1;
                 const bool live = (unsigned)id < (unsigned)v.n_pages;         // (else zeros)
-                lost |= !live && slot < len;
+                if (!live && slot < len) s_lost = 1;
                 copy16(dst + k * L::LD + c,
                        live ? kv + id * v.page_elems() + ((long)(what * v.kv_heads + g.h) * v.page + (slot & (v.page - 1))) * HD + c : kv,
                        live);
@@ -234,7 +235,6 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
                 load(sV, 1, key_of(j + 1));
             }
         }
-        if (lost) set_status(v.status, ST_RANGE);
         const bool whole = segment_whole(g);
         const long slot = part_slot(g, blockIdx.x) * ROWS;
 #pragma unroll
@@ -258,6 +258,8 @@ __global__ void __launch_bounds__(THREADS) pages_attn_simt_kernel(const PagesAtt
             }
         }
     }
+    __syncthreads();
+    if (tid == 0 && s_lost) set_status(v.status, ST_RANGE);
 }
 
 // Joins the partial results of items that several CTAs worked on: block (CTA that ended an item, rows), a warp
