@@ -8,9 +8,9 @@
 // call's list, so a sequence of calls always gives the same tables. A call that cannot be
 // carried out (too few pages, bad lists) changes nothing, sets the status word, and keeps the
 // calls behind it from running until the host has seen that (refuse, in pages.h).
-// Round trips bound the lists: freeing takes 3 to 4 us, planning 64 forks 7, reserving for 16
-// sequences 6, planning 16 compactions of 1027 tokens 13, positions of 20544 rows 4; bytes
-// bound the moves (66 us there).
+// Round trips bound the lists (launches by themselves, cold): freeing takes 4.5 to 6 us, planning
+// 64 forks 8.7, reserving for 16 sequences 7.6, planning 16 compactions of 1027 tokens 14.6,
+// positions of 20544 rows 6.0; bytes bound the moves (68 us there).
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -807,8 +807,9 @@ cudaError_t launch_rope(const msd_pages *p, const BatchView &b, const RopeArgs &
         return e;
     };
     // runs of 8 elements where the rotated part allows it, else pair by pair; two rows to a thread once that leaves every
-    // SM some CTAs (1, 2 and 4 rows a thread: 60 rows of 96 heads of 128 take 3.5, 3.7, 4.1 us, 240 rows 5.6, 4.8, 5.1,
-    // 20544 rows of 48 heads 121, 90, 91: 5.6 TB/s)
+    // SM some CTAs. One and two rows a thread from fp32 (from bf16) rows of 96 heads of 128, in a loop: 60 rows 3.7, 3.7 us
+    // (3.5, 3.7), 124 rows 4.5, 4.3 (4.1, 4.1), 186 rows, where the rule turns, 4.7, 4.6 (4.5, 4.5), 240 rows 5.8, 5.0
+    // (5.2, 4.9). 20544 bf16 rows of 48 heads take 93 us by themselves, 5.4 TB/s (one row a thread 121 where two took 90).
     if (a.half % 8) return go(rope_append_kernel<TS, TD, 1, 1>, 1, 1);
     const long each = (long)b.rows * heads * p->cfg.head_dim / p->sms;        // elements of an SM
     return each >= 15000 ? go(rope_append_kernel<TS, TD, 8, 2>, 8, 2) : go(rope_append_kernel<TS, TD, 8, 1>, 8, 1);
@@ -1049,7 +1050,10 @@ msd_status msd_pages_compact(msd_pages *p, const msd_batch *batch, const int32_t
     if (e == cudaSuccess) {
         const int groups = p->cfg.n_layers * 2 * p->cfg.n_kv_heads;
         const int units = 256 / (p->cfg.head_dim * (p->cfg.dtype == MSD_F32 ? 4 : 2) / 16);
-        // lists of 64 and more side by side (16 lists of 1027, 8 layers of 8 heads, with the fork before them: 99 us, and 227 one by one)
+        // Lists of 64 and more side by side: 16 lists of 1027 tokens, 8 layers of 8 heads, with the fork before them, take 100 us,
+        // and 227 one by one. Near 64 the two cross, later the more layers there are (room, lists of every other row, cut
+        // again; side by side and one by one): 32 layers of 8 heads 80, 63 us at 32 tokens, 100, 96 at 64, 116, 120 at 96;
+        // 8 layers of 8 heads 37, 39 at 32, 39, 43 at 64, 51, 64 at 128; 4 layers of 4 heads 25, 31 at 32.
         const int side = keep && keep_stride < 64 ? 1 : std::min(units, 16);
         const dim3 grid((groups + units / side - 1) / (units / side), b.n);        // (sequences are few enough for y, groups need not be)
         e = p->cfg.dtype == MSD_F32 ? chain(compact_apply_kernel<4, 8>, grid, 256, s, p->v, c, groups, side)
@@ -1075,7 +1079,9 @@ msd_status msd_rope_positions(msd_pages *p, const msd_batch *batch, const int32_
     BatchView b;
     if (!batch_view(p, batch, &b) || !pos || (span_start && (!spans || n_spans < 0)) || pos_stride < b.rows)
         return pfail(p, MSD_ERR_INVALID, "bad batch, stride or null array");
-    const int chunks = std::max(1, std::min((b.rows / b.n + SPAN_TILE - 1) / SPAN_TILE, 64));        // (of an even batch)
+    // CTAs of a sequence, by an even batch's (16 sequences of 1260 rows 1.5 us warm, one of 20000 among 15 short ones 3.1,
+    // among 255 of one row 9.2)
+    const int chunks = std::max(1, std::min((b.rows / b.n + SPAN_TILE - 1) / SPAN_TILE, 64));
     return leave(p, chain(positions_kernel, dim3(b.n, chunks), SPAN_TILE, static_cast<cudaStream_t>(stream), p->v, b,
                           span_start, spans, span_start ? n_spans : 0, first, pos, (long)pos_stride, next));
 }

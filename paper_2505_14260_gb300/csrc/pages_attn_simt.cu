@@ -5,9 +5,10 @@
 // the weights as pairs (p, p) in shared memory, O in registers as packed columns. K and V have one buffer each: the next
 // tile's K is copied (cp.async) while the weights meet V, and its V while the next scores are made. What bounds it: the
 // shared-memory loads that feed the FMAs, and at few tiles the chain of round trips (schedule, table, K). Measured with
-// the join: 16 heads of 64, two chunks of up to 333 rows 33 us; a tree of 16 rows behind 96 tokens 11 us.
+// the join: 16 heads of 64, two chunks of up to 333 rows 34 us; a tree of 16 rows behind 96 tokens 11 us.
 // A key that a row does not see has the weight -0, and in a tile whose V holds a NaN or an infinity such keys are
-// skipped (looked for only where a row does not see the whole tile); slots past the sequence's end are not read.
+// skipped (looked for only where a row does not see the whole tile); slots past the sequence's end are not read, and
+// those of a table entry that is no page count as zeros.
 #include <type_traits>
 
 #include "pages_attn.cuh"

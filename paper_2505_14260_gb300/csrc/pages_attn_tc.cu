@@ -10,8 +10,8 @@
 //   joined at the end (bytes bound it: what counts is that the copies never pause). The groups
 //   take the CTA's steps in turns across items too, so short items overlap.
 // Measured, with the join (32 heads of 128, 8 K/V heads): one token each of 64 requests of up to 8192
-// tokens 78 us, 5.0 TB/s; one token behind 131071 90 us, 6.0 TB/s; two chunks of up to 4096 rows behind
-// 4096 in a loop 297 us, 1.44 PFLOP/s (the tensor pipe at work in 64% of the cycles).
+// tokens 76 us, 5.1 TB/s; one token behind 131071 90 to 91 us, 5.9 TB/s; two chunks of up to 4096 rows behind
+// 4096 299 us in a loop of their own, 1.43 PFLOP/s (the tensor pipe at work in 64% of the cycles), 315 us among other calls.
 // Roles (384 threads, one warp without work; 216 registers for the softmax, 72 for the others):
 //   warps 0-7   softmax groups 0 and 1, a row a thread: load the query rows into shared memory
 //               (swizzled as the MMA reads them), then per key tile read S, hide what the row
@@ -1025,7 +1025,9 @@ bool setup() {
                                 (int)Lay<HD, ROWS>::SMEM) == cudaSuccess;
 }
 
-// A tile as large as the sequences' packed rows: a small one leaves room for more key tiles in flight.
+// A tile as large as the sequences' packed rows: a small one leaves room for more key tiles in flight. One shape serves
+// the whole call, by the mean: a chunk among many single tokens then runs in small tiles (of 32 rows for one of 512 rows and
+// 127 tokens, four heads to a K/V head: 64 tiles where 8 would do), and tokens beside a long chunk in large ones.
 template <int HD>
 cudaError_t launch_rows(const CUtensorMap &map, const PagesAttn &a, int sms, cudaStream_t s) {
     return a.packed <= 32    ? launch<HD, 32>(map, a, sms, s)

@@ -428,7 +428,9 @@ class Pages:
     """A pool of K/V pages (msd_pages): many sequences of one model's cache, which share full
     pages. State lives in the tensors kv [layers, n_pages, 2, kv_heads, page_size, head_dim],
     table [max_seqs, max_pages], lens [max_seqs] and refs [n_pages], allocated here unless
-    given. A pool made on fresh tensors is empty; on given ones call restore() first."""
+    given. A pool made on fresh tensors is empty; on given ones call restore() first. Calls
+    are queued: an error that only the device can see (too few pages, bad lists) is raised by a
+    later call, and what was queued behind a page operation that failed has done nothing."""
 
     def __init__(self, *, dtype: str, layers: int, heads: int, kv_heads: int, head_dim: int, page_size: int,
                  n_pages: int, max_seqs: int, max_pages: int, rot_dim: int | None = None, rot_sections=None,
