@@ -155,12 +155,14 @@ __global__ void restore_bits_kernel(const PagesView v) {
 // (The operations read the mark beside their lists and look at it once those are there, so that it costs no round trip
 // of its own.)
 
-// Behind the calls that were held back: they may run again, unless one of them has met an error of its own since the
-// host took the status word (that is yet to be seen).
-__global__ void resume_kernel(const PagesView v) {
+// Behind what the host had queued when it took `code` from the status word. The calls that were held back may run again
+// if that was the refused operation's error. If it was another one's, the refusal is put where the host sees it next.
+__global__ void resume_kernel(const PagesView v, int code) {
     wait_prior();
     allow_dependents();
-    if (atomicAdd(v.status, 0) == 0) *v.refused = 0;
+    const int held = *v.refused;
+    if (held && code == held) *v.refused = 0;
+    else if (held) set_status(v.status, held);
 }
 
 // ---- free ------------------------------------------------------------------
@@ -835,8 +837,8 @@ cudaError_t chain(void (*kernel)(KArgs...), dim3 grid, int threads, cudaStream_t
 }
 
 // What every call begins with: an error that was pending before it, the pool's device, and
-// the status word of earlier calls. Reporting that lets later calls run again: the mark that holds them
-// back is cleared on the stream, behind the calls that it is for. A call that is being recorded
+// the status word of earlier calls. Reporting a refusal lets later calls run again: the mark that holds
+// them back is cleared on the stream, behind the calls that it is for. A call that is being recorded
 // cannot do that (it would be recorded too), so the word stays for the next one that is not.
 msd_status enter(msd_pages *p, const char *call, cudaStream_t s) {
     p->err[0] = 0;
@@ -848,15 +850,19 @@ msd_status enter(msd_pages *p, const char *call, cudaStream_t s) {
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || dev != p->dev)
         return pfail(p, MSD_ERR_INVALID, "the pool belongs to another device than the current one");
-    const int code = *p->status_host;
+    int code = *p->status_host;
     if (code != 0) {
         cudaStreamCaptureStatus capture = cudaStreamCaptureStatusActive;
         if (cudaStreamIsCapturing(s, &capture) != cudaSuccess) cudaGetLastError();       // (the default stream, while another records)
         if (capture == cudaStreamCaptureStatusNone) {
             *p->status_host = 0;
-            const cudaError_t failed = chain(resume_kernel, dim3(1), 1, s, p->v);
-            if (failed != cudaSuccess) return pfail(p, MSD_ERR_CUDA, cudaGetErrorString(failed));
+            const cudaError_t failed = chain(resume_kernel, dim3(1), 1, s, p->v, code);
+            if (failed != cudaSuccess) {                // (still to be reported)
+                *p->status_host = code;
+                return pfail(p, MSD_ERR_CUDA, cudaGetErrorString(failed));
+            }
         }
+        code &= ~ST_REFUSED;
         if (code == ST_NO_PAGES)
             return pfail(p, MSD_ERR_CAPACITY, "an earlier call needed more free pages than there were; it changed nothing");
         snprintf(p->err, sizeof p->err, "an earlier call set the device status word (code %d: %s)", code,

@@ -14,6 +14,7 @@ namespace msd {
 enum : int {
     ST_NO_PAGES = 5,      // fewer free pages than a call needed: the call changed nothing
     ST_BAD_BATCH = 6,     // sequence ids, row counts or lists that the call cannot take
+    ST_REFUSED = 0x100,   // with one of the others: a page operation was not carried out
 };
 
 constexpr int MAX_ROT_PAIRS = 64;
@@ -31,18 +32,18 @@ struct PagesView {
     int *len, *refs;
     unsigned *bits;           // bit p % 32 of word p / 32: page p is free
     int *status;
-    int *refused;             // not 0: a page operation was not carried out and the host has not seen it
+    int *refused;             // not 0: the code of a page operation that was not carried out, which the host has not reported
     int layers, heads, kv_heads, head_dim, page, page_shift;
     int n_pages, max_seqs, max_pages;
     __host__ __device__ long page_elems() const { return 2l * kv_heads * page * head_dim; }
 };
 
 // A page operation that cannot be carried out (one thread calls it, before anything has changed). The calls queued
-// behind it, recorded ones too, were made for what it should have done, so they do nothing: the host takes the mark
-// away, in the stream's order, with the call that reports the status word.
+// behind it, recorded ones too, were made for what it should have done, so they do nothing: the mark goes, in the
+// stream's order, with the call that reports this very error (the status word may hold another that came before it).
 __device__ __forceinline__ void refuse(const PagesView &v, int code) {
-    set_status(v.status, code);
-    *v.refused = 1;
+    set_status(v.status, code | ST_REFUSED);
+    *v.refused = code | ST_REFUSED;
 }
 
 // the rows of a call (msd_batch)

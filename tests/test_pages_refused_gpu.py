@@ -138,6 +138,31 @@ def test_an_error_that_the_host_has_not_seen_is_not_cleared_with_an_earlier_one(
     p.free(one.seqs)
 
 
+@pytest.mark.parametrize("bad", [False, True])
+def test_a_refusal_that_another_error_hides_is_reported_too(bad):
+    """An attention's error and a reserve's (too few pages, or a bad list: the attention's own kind) before the host
+    looks: the first report is the attention's, and nothing runs until the second."""
+    p = shared_pool()
+    x, one = torch.zeros(1, 4, 64, device="cuda", dtype=p.dtype), batch([4], [1])
+    b, twice, last, n_keep = batch([0, 2], [20, 20]), batch([0, 0], [1, 1]), batch([0], [20]), i32([2])
+    before = state(p)
+    torch.cuda._sleep(40_000_000)
+    p.attention(0, one, x, x)                        # a row of a sequence without tokens
+    p.reserve(twice if bad else b)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(40_000_000)
+    with pytest.raises(msd.MsdError) as e:
+        p.compact(last, None, n_keep)
+    assert e.value.status == msd.MSD_ERR_DEVICE
+    p.compact(last, None, n_keep)                    # queued before the reserve's error has come up
+    torch.cuda.synchronize()
+    assert same(p, before)
+    reported(p, msd.MSD_ERR_DEVICE if bad else msd.MSD_ERR_CAPACITY)
+    p.compact(last, None, n_keep)                    # runs
+    torch.cuda.synchronize()
+    assert p.lens.tolist() == [46, 96, 64, 0, 0]
+
+
 def test_an_error_met_while_recording_is_reported_again():
     """A call that is being recorded reports the error but cannot take note of it: nothing runs then."""
     p = shared_pool()
