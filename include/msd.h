@@ -499,6 +499,90 @@ msd_status msd_pages_attention(msd_pages *p, int32_t layer, const msd_batch *bat
                                int32_t tree_nodes, int32_t window, int32_t sinks, const void *q_dev, int64_t ldq,
                                void *out_dev, int64_t ldo, float *lse_dev, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Products with 4-bit weights, and tokens from logits: operators that need no
+ * context and no pool, for the programs of the paged cache above and for the
+ * head of any other. They allocate nothing, keep nothing between calls, read
+ * every size but the arguments' on the device and never synchronise, so calls on
+ * several streams or threads do not meet and all of them can be captured into a
+ * CUDA graph. Arrays are caller-owned memory of the current device. Argument
+ * errors are returned at once (MSD_ERR_INVALID); MSD_ERR_CUDA: a launch failed.
+ * ------------------------------------------------------------------------- */
+
+/* A weight matrix [o][k] in 4 bits: code c stands for scale * (c - zero) with the scale
+ * and zero of its group, `group` consecutive elements of a row (the last group of a row
+ * may be shorter). k is a multiple of 8; group is 32, 64 or 128. */
+typedef struct {
+    uint8_t *codes;             /* [o][k / 2], 4-byte aligned: element 2 i in the low half of byte i,
+                                   2 i + 1 in the high half */
+    void *scales;               /* [o][ceil(k / group)] bf16 */
+    uint8_t *zeros;             /* [o][ceil(k / group)], 0 .. 15; null: 8 everywhere */
+    int32_t o, k, group;
+} msd_weight4;
+
+/* y[i][j] (= or, if accumulate != 0, +=) sum_t x[i][t] * w[j][t] for i < m, j < o, as msd_linear
+ * but with a weight in 4 bits. x [m][ldx] is bf16 (x_dtype MSD_BF16) or fp32 (MSD_F32), its rows
+ * 16-byte aligned; y [m][ldy] is fp32. Differences c - zero are exact, sums are fp32, and a
+ * group's sum is multiplied by its scale: no weight is rounded on the way. fp32 x enters as three
+ * bf16 values that add up to it exactly. A value of x that is not finite makes its row of y so. */
+msd_status msd_linear4(const void *x_dev, int64_t ldx, int32_t x_dtype, int32_t m, const msd_weight4 *w,
+                       float *y_dev, int64_t ldy, int32_t accumulate, void *stream);
+
+/* Writes the codes, scales and (unless null) zeros of *out from w [o][ldw], bf16 or fp32 with
+ * 16-byte aligned rows. Per group, without zeros: scale = max|w| / 7 rounded to bf16; with zeros:
+ * scale = (max(w, 0) - min(w, 0)) / 15 rounded to bf16, zero = -min(w, 0) / scale to the nearest
+ * integer within 0 .. 15. code = w / scale to the nearest integer, plus the zero, within 0 .. 15.
+ * Quotients are rounded exactly, ties to even; a scale below 2^-126 becomes 0, and the codes of such
+ * a group its zero (0 with zeros). NaN counts as 0; |w| < 2^125. values (nullable) [o][ldv]: scale * (code - zero), in w's type. */
+msd_status msd_quantize4(const void *w_dev, int64_t ldw, int32_t w_dtype, const msd_weight4 *out,
+                         void *values_dev, int64_t ldv, void *stream);
+
+/* What is left of a row of logits, per row (msd_sample) or per sequence (msd_accept_batch): device
+ * arrays, each nullable (that setting is off). A token's weight is exp((logit - max) / temperature);
+ * tokens are ordered by logit, the lower id first among equals. Left are the top_k first ones; of
+ * them the shortest run from the first whose weights reach top_p of theirs; of these the ones whose
+ * weight is min_p of the largest or more; and always the first one.
+ * Off: temperature 1, top_k <= 0, top_p >= 1 or NaN, min_p <= 0 or NaN. A temperature that is NaN or
+ * below 2^-100 leaves the first token alone (greedy); one above 2^100 counts as 2^100. */
+typedef struct {
+    const float *temperature;
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+} msd_filter;
+
+/* tokens[r] for r < rows: the smallest id whose cumulative weight, in id order over what the row's
+ * settings leave, exceeds u[r] of the whole (u in [0, 1); NaN and less count as 0, 1 and more as
+ * the largest float below 1). logits [rows][ld] fp32 or bf16 (dtype); ids are 0 .. vocab - 1. A
+ * token whose logit is -inf or NaN has no weight; where one is +inf, those that are have equal ones
+ * and the others none. A row without any weight gives -1. logp (nullable): the natural logarithm of
+ * the token's share of the weight, -inf for a token of -1. probs (nullable) [rows][ldp] fp32: every
+ * id's share. Weights are taken to 2^-44 of the largest and summed exactly, so tokens do not depend on the
+ * grid and agree with an exact evaluation unless u or top_p lies within vocab * 2^-44 of a border.
+ * f: null, or the rows' settings. vocab <= 393216. */
+msd_status msd_sample(const void *logits_dev, int64_t ld, int32_t dtype, int32_t rows, int32_t vocab,
+                      const msd_filter *f, const float *u_dev, int32_t *tokens_dev, float *logp_dev,
+                      float *probs_dev, int64_t ldp, void *stream);
+
+/* Speculative sampling over the drafted trees of a batch (msd_accept_sample's rule, without a
+ * context, on what the settings leave). Row row_start[i] + j of logits belongs to node j of tree i
+ * of the batch (tokens and parent of stride tree_nodes, as msd_pages_attention takes them, and
+ * n_nodes if given; a sequence has as many nodes as rows, n_nodes and tree_nodes allow; mask and
+ * depth are not read). From node 0, the children of the current node are tried in index order, the
+ * first `children` of them, with u[(i * (depth + 1) + d) * (children + 1) + c] for the c-th at d
+ * drafts accepted: a child is accepted if u of the weight that is left is less than its token's
+ * weight, and becomes the current node; a rejected one's token loses its weight. At depth drafts,
+ * or with no child accepted, bonus[i] is drawn from what is left with the u of c = children. A node
+ * whose parent does not precede it is never reached, nor a token outside the vocabulary accepted.
+ * path[i * (depth + 1) + d]: the nodes accepted, node 0 first, then -1; accept_len[i]: their
+ * number less one. path and accept_len + 1 are what msd_pages_compact takes. A sequence without
+ * rows gives -1, 0 and a bonus of -1; a row without any weight a bonus of -1.
+ * scratch: [2 * rows] int32, any contents, not used by another call at the same time. depth >= 0,
+ * children 1 .. 256, tree_nodes <= 1024. */
+msd_status msd_accept_batch(const void *logits_dev, int64_t ld, int32_t dtype, int32_t vocab, const msd_batch *batch,
+                            const msd_tree *tree, int32_t tree_nodes, const msd_filter *f, const float *u_dev,
+                            int32_t depth, int32_t children, int32_t *scratch_dev, int32_t *path_dev,
+                            int32_t *accept_len_dev, int32_t *bonus_dev, void *stream);
+
 /* Profiling counters (tracing subsystem). kernel_launches counts every kernel
  * the library has run in this process (kernels executed by step graphs
  * included, kernels merely recorded into graphs excluded).

@@ -91,6 +91,15 @@ class msd_batch(ctypes.Structure):
     _fields_ = [("n", c_int32), ("seqs", c_void_p), ("row_start", c_void_p), ("rows", c_int32)]
 
 
+class msd_weight4(ctypes.Structure):
+    _fields_ = [("codes", c_void_p), ("scales", c_void_p), ("zeros", c_void_p), ("o", c_int32), ("k", c_int32),
+                ("group", c_int32)]
+
+
+class msd_filter(ctypes.Structure):
+    _fields_ = [("temperature", c_void_p), ("top_k", c_void_p), ("top_p", c_void_p), ("min_p", c_void_p)]
+
+
 _SIGNATURES = {
     "msd_create": (c_int32, [POINTER(msd_config), POINTER(msd_weights), POINTER(c_void_p)]),
     "msd_destroy": (c_int32, [c_void_p]),
@@ -133,6 +142,14 @@ _SIGNATURES = {
                                   c_void_p, c_int64, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p]),
     "msd_pages_attention": (c_int32, [c_void_p, c_int32, POINTER(msd_batch), POINTER(msd_tree), c_int32, c_int32,
                                       c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p]),
+    "msd_linear4": (c_int32, [c_void_p, c_int64, c_int32, c_int32, POINTER(msd_weight4), c_void_p, c_int64, c_int32,
+                              c_void_p]),
+    "msd_quantize4": (c_int32, [c_void_p, c_int64, c_int32, POINTER(msd_weight4), c_void_p, c_int64, c_void_p]),
+    "msd_sample": (c_int32, [c_void_p, c_int64, c_int32, c_int32, c_int32, POINTER(msd_filter), c_void_p, c_void_p,
+                             c_void_p, c_void_p, c_int64, c_void_p]),
+    "msd_accept_batch": (c_int32, [c_void_p, c_int64, c_int32, c_int32, POINTER(msd_batch), POINTER(msd_tree), c_int32,
+                                   POINTER(msd_filter), c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p,
+                                   c_void_p, c_void_p]),
 }
 
 _lib = None
@@ -573,6 +590,166 @@ class Pages:
         if st:
             self._check(st, "msd_pages_attention")
         return out
+
+
+_TYPES = {torch.float32: MSD_F32, torch.bfloat16: MSD_BF16}
+
+
+def _matrix(t: torch.Tensor, what: str, types=_TYPES) -> int:
+    """The row stride of a 2-D tensor on the current GPU whose rows are contiguous."""
+    if t.dim() != 2 or t.dtype not in types or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: a matrix with contiguous rows on the GPU, {' or '.join(str(d) for d in types)}")
+    if t.device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"{what} is not on the current GPU")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _vector(t: torch.Tensor | None, what: str, dtype: torch.dtype, n: int, device) -> int | None:
+    """The address of n contiguous values (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != device or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what}: {n} contiguous values of {dtype} on {device}")
+    return t.data_ptr()
+
+
+def _raw_stream(stream, device) -> int:
+    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+
+
+def _call(st: int, call: str):
+    if st != MSD_OK:
+        raise MsdError(st, call, "bad sizes, strides or alignment" if st == MSD_ERR_INVALID else "launch failed")
+
+
+class Weight4:
+    """A weight matrix [out, in] in 4 bits (msd_weight4): codes uint8 [out, in / 2], scales bf16
+    [out, groups] and zeros uint8 [out, groups] or None, held by the caller. Weight4.of(w) makes
+    one from a bf16 or fp32 matrix."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor | None = None, group: int = 128):
+        if codes.dim() != 2 or codes.dtype != torch.uint8 or not codes.is_cuda or not codes.is_contiguous():
+            raise ValueError("codes are a contiguous uint8 matrix on the GPU")
+        if group not in (32, 64, 128):
+            raise ValueError("group is 32, 64 or 128")
+        self.o, self.k, self.group = codes.shape[0], 2 * codes.shape[1], group
+        self.codes, self.scales, self.zeros = codes, scales, zeros
+        n = self.o * -(-self.k // group)
+        self._c = msd_weight4(codes.data_ptr(), _vector(scales, "scales", torch.bfloat16, n, codes.device),
+                              _vector(zeros, "zeros", torch.uint8, n, codes.device), self.o, self.k, group)
+        self._ref = ctypes.byref(self._c)
+
+    @classmethod
+    def of(cls, w: torch.Tensor, group: int = 128, zeros: bool = False, stream=None) -> "Weight4":
+        """w [out, in] in 4 bits (msd_quantize4)."""
+        _matrix(w, "w")
+        if group not in (32, 64, 128):
+            raise ValueError("group is 32, 64 or 128")
+        o, k = w.shape
+        n = -(-k // group)
+        self = cls(torch.empty(o, k // 2, dtype=torch.uint8, device=w.device),
+                   torch.empty(o, n, dtype=torch.bfloat16, device=w.device),
+                   torch.empty(o, n, dtype=torch.uint8, device=w.device) if zeros else None, group)
+        return self.quantize(w, stream=stream)
+
+    def quantize(self, w: torch.Tensor, values: torch.Tensor | None = None, stream=None) -> "Weight4":
+        """Codes, scales and zeros from w; values (optional, w's type): what they stand for."""
+        ld, ldv = _matrix(w, "w"), 0
+        if w.shape != (self.o, self.k):
+            raise ValueError(f"w is [{self.o}, {self.k}]")
+        if values is not None:
+            ldv = _matrix(values, "values")
+            if values.shape != w.shape or values.dtype != w.dtype:
+                raise ValueError("values has w's shape and type")
+        self._on(w)
+        _call(lib().msd_quantize4(w.data_ptr(), ld, _TYPES[w.dtype], self._ref, _ptr(values), ldv,
+                                  _raw_stream(stream, w.device)), "msd_quantize4")
+        return self
+
+    def linear(self, x: torch.Tensor, y: torch.Tensor, accumulate: bool = False, stream=None) -> torch.Tensor:
+        """y (=|+=) x w^T (msd_linear4): x [m, in] bf16 or fp32, y [m, out] fp32."""
+        ldx, ldy = _matrix(x, "x"), _matrix(y, "y", (torch.float32,))
+        if x.shape[1] != self.k or y.shape != (x.shape[0], self.o):
+            raise ValueError(f"x is [m, {self.k}] and y [m, {self.o}]")
+        self._on(x)
+        st = lib().msd_linear4(x.data_ptr(), ldx, _TYPES[x.dtype], x.shape[0], self._ref, y.data_ptr(), ldy,
+                               int(accumulate), _raw_stream(stream, x.device))
+        if st:
+            _call(st, "msd_linear4")
+        return y
+
+    def _on(self, t: torch.Tensor):
+        if t.device != self.codes.device:
+            raise ValueError("the weight is on another GPU")
+
+
+class Filter:
+    """Settings of rows of logits (msd_filter), a value per row (sample) or per sequence
+    (accept): fp32 temperature, top_p and min_p, int32 top_k, each None where it is off."""
+
+    def __init__(self, temperature: torch.Tensor | None = None, top_k: torch.Tensor | None = None,
+                 top_p: torch.Tensor | None = None, min_p: torch.Tensor | None = None):
+        given = [t for t in (temperature, top_k, top_p, min_p) if t is not None]
+        self.n = given[0].numel() if given else None
+        self.device = given[0].device if given else None
+        if given and not given[0].is_cuda:
+            raise ValueError("settings are tensors on the GPU")
+        f32 = lambda t, what: _vector(t, what, torch.float32, self.n, self.device)  # noqa: E731
+        self._c = msd_filter(f32(temperature, "temperature"), _vector(top_k, "top_k", torch.int32, self.n, self.device),
+                             f32(top_p, "top_p"), f32(min_p, "min_p"))
+        self._held = given
+        self._ref = ctypes.byref(self._c)
+
+    def _for(self, n: int, device):
+        if self.n is not None and (self.n != n or self.device != device):
+            raise ValueError(f"settings have {n} values each, on the logits' GPU")
+        return self._ref
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, settings: Filter | None, tokens: torch.Tensor,
+           logp: torch.Tensor | None = None, probs: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """A token for each row of logits [rows, vocab] (fp32 or bf16) from the uniforms u [rows]
+    (msd_sample). tokens: int32 [rows]; logp: fp32 [rows]; probs: fp32 [rows, vocab]."""
+    ld, dev, (rows, vocab) = _matrix(logits, "logits"), logits.device, logits.shape
+    ldp = 0
+    if probs is not None:
+        ldp = _matrix(probs, "probs", (torch.float32,))
+        if probs.shape != logits.shape:
+            raise ValueError("probs has the logits' shape")
+    st = lib().msd_sample(logits.data_ptr(), ld, _TYPES[logits.dtype], rows, vocab,
+                          None if settings is None else settings._for(rows, dev),
+                          _vector(u, "u", torch.float32, rows, dev), _vector(tokens, "tokens", torch.int32, rows, dev),
+                          _vector(logp, "logp", torch.float32, rows, dev), _ptr(probs), ldp, _raw_stream(stream, dev))
+    if st:
+        _call(st, "msd_sample")
+    return tokens
+
+
+def accept(logits: torch.Tensor, batch: Batch, tree: Tree, u: torch.Tensor, settings: Filter | None, path: torch.Tensor,
+           accept_len: torch.Tensor, bonus: torch.Tensor, stream=None):
+    """Speculative sampling over a batch's drafted trees (msd_accept_batch). logits [rows, vocab]:
+    the batch's rows are the trees' nodes; u [n, depth + 1, children + 1]; path [n, depth + 1],
+    accept_len [n] and bonus [n] int32. path and accept_len + 1 go to Pages.compact."""
+    ld, dev, n, rows = _matrix(logits, "logits"), logits.device, batch.n, batch.rows
+    if logits.shape[0] != rows or tree.B != n:
+        raise ValueError("a row of logits per row of the batch, a tree per sequence")
+    if u.dim() != 3 or u.shape[0] != n or path.shape != (n, u.shape[1]):
+        raise ValueError("u is [n, depth + 1, children + 1], path [n, depth + 1]")
+    for t in (batch.seqs, tree.tokens):
+        if t.device != dev:
+            raise ValueError("batch, tree and logits are on one GPU")
+    scratch = torch.empty(2 * rows, dtype=torch.int32, device=dev)
+    if stream is not None:
+        scratch.record_stream(stream)
+    st = lib().msd_accept_batch(
+        logits.data_ptr(), ld, _TYPES[logits.dtype], logits.shape[1], batch.c(), ctypes.byref(tree.c()), tree.N,
+        None if settings is None else settings._for(n, dev), _vector(u, "u", torch.float32, u.numel(), dev),
+        u.shape[1] - 1, u.shape[2] - 1, scratch.data_ptr(), _vector(path, "path", torch.int32, path.numel(), dev),
+        _vector(accept_len, "accept_len", torch.int32, n, dev), _vector(bonus, "bonus", torch.int32, n, dev),
+        _raw_stream(stream, dev))
+    if st:
+        _call(st, "msd_accept_batch")
+    return path, accept_len, bonus
 
 
 def make_config(wl, max_seq: int, batch: int | None = None) -> msd_config:

@@ -1,0 +1,83 @@
+"""Filtered sampling, tree acceptance and 4-bit products: arguments that are refused before
+anything touches a GPU, and the sums behind the fixed-point weights."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2505_14260_gb300 import build, msd
+
+P = ctypes.c_void_p
+A = 1 << 20                      # an address that nothing reads: every call here is refused
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return msd.lib()
+
+
+def linear(lib, x=A, ldx=64, xt=msd.MSD_BF16, m=1, codes=A, scales=A, o=8, k=64, group=32, y=A, ldy=8):
+    w = msd.msd_weight4(codes, scales, None, o, k, group)
+    return lib.msd_linear4(x, ldx, xt, m, ctypes.byref(w), y, ldy, 0, None)
+
+
+@pytest.mark.parametrize("bad", [dict(x=None), dict(ldx=63), dict(ldx=68), dict(xt=2), dict(m=-1), dict(codes=None), dict(scales=None),
+                                 dict(o=0), dict(k=0), dict(k=60), dict(k=12, ldx=16), dict(group=16), dict(group=48), dict(y=None),
+                                 dict(ldy=7), dict(x=A + 2), dict(x=A + 8), dict(y=A + 2), dict(codes=A + 2), dict(scales=A + 1)], ids=str)
+def test_linear4_refuses(lib, bad):
+    assert linear(lib, **bad) == msd.MSD_ERR_INVALID
+
+
+def test_linear4_without_rows_or_weight(lib):
+    assert linear(lib, m=0) == msd.MSD_OK
+    assert lib.msd_linear4(A, 64, 1, 1, None, A, 8, 0, None) == msd.MSD_ERR_INVALID
+
+
+@pytest.mark.parametrize("bad", [dict(x=None), dict(ld=63), dict(ld=66), dict(t=3), dict(x=A + 4), dict(v=A + 8), dict(ldv=60), dict(k=20)], ids=str)
+def test_quantize4_refuses(lib, bad):
+    a = dict(x=A, ld=64, t=msd.MSD_F32, k=64, v=A, ldv=64)
+    a.update(bad)
+    w = msd.msd_weight4(A, A, None, 8, a["k"], 32)
+    assert lib.msd_quantize4(a["x"], a["ld"], a["t"], ctypes.byref(w), a["v"], a["ldv"], None) == msd.MSD_ERR_INVALID
+
+
+@pytest.mark.parametrize("bad", [dict(x=None), dict(ld=99), dict(t=2), dict(rows=-1), dict(vocab=0), dict(vocab=393217, ld=400000), dict(u=None),
+                                 dict(tokens=None), dict(probs=A, ldp=99), dict(x=A + 2), dict(probs=A + 1, ldp=100)], ids=str)
+def test_sample_refuses(lib, bad):
+    a = dict(x=A, ld=100, t=msd.MSD_F32, rows=2, vocab=100, u=A, tokens=A, probs=None, ldp=0)
+    a.update(bad)
+    assert lib.msd_sample(a["x"], a["ld"], a["t"], a["rows"], a["vocab"], None, a["u"], a["tokens"], None, a["probs"], a["ldp"],
+                          None) == msd.MSD_ERR_INVALID
+
+
+@pytest.mark.parametrize("bad", [dict(x=None), dict(ld=99), dict(t=5), dict(vocab=0), dict(nodes=0), dict(nodes=1025), dict(u=None), dict(depth=-1),
+                                 dict(children=0), dict(children=257), dict(scratch=None), dict(path=None), dict(len_=None), dict(bonus=None),
+                                 dict(tokens=None), dict(parent=None), dict(start=None), dict(n=-1), dict(rows=-1)], ids=str)
+def test_accept_refuses(lib, bad):
+    a = dict(x=A, ld=100, t=msd.MSD_F32, vocab=100, nodes=4, u=A, depth=2, children=3, scratch=A, path=A, len_=A, bonus=A, tokens=A, parent=A,
+             start=A, n=2, rows=4)
+    a.update(bad)
+    b = msd.msd_batch(a["n"], A, a["start"], a["rows"])
+    t = msd.msd_tree(a["tokens"], a["parent"], None, None, None)
+    assert lib.msd_accept_batch(a["x"], a["ld"], a["t"], a["vocab"], ctypes.byref(b), ctypes.byref(t), a["nodes"], None, a["u"], a["depth"],
+                                a["children"], a["scratch"], a["path"], a["len_"], a["bonus"], None) == msd.MSD_ERR_INVALID
+
+
+def test_nothing_to_do_needs_no_gpu(lib):
+    assert lib.msd_sample(None, 0, 0, 0, 100, None, None, None, None, None, 0, None) == msd.MSD_OK
+    b, t = msd.msd_batch(0, None, None, 0), msd.msd_tree()
+    assert lib.msd_accept_batch(None, 0, 0, 100, ctypes.byref(b), ctypes.byref(t), 4, None, None, 2, 3, None, None, None, None, None) == msd.MSD_OK
+
+
+def test_the_binding_refuses_host_tensors(lib):
+    c, s = torch.zeros(4, 32, dtype=torch.uint8), torch.ones(4, 2, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        msd.Weight4(c, s, None, 32)
+    with pytest.raises(ValueError):
+        msd.Weight4.of(torch.zeros(4, 64))
+    with pytest.raises(ValueError):
+        msd.sample(torch.zeros(2, 10), torch.zeros(2), None, torch.zeros(2, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        msd.Filter(temperature=torch.ones(2))
+    assert msd.Filter().n is None
