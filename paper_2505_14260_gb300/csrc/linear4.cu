@@ -14,41 +14,267 @@ struct Weight {
     int o, k, group, groups;
 };
 
-// y[i][j] = sum over groups of scale * sum x (code - zero): a warp per output and 8 rows of x.
-template <typename T>
-__global__ void __launch_bounds__(256)
-linear4_kernel(const T *__restrict__ x, long ldx, int m, Weight w, float *__restrict__ y, long ldy, int accumulate) {
+// ---------------------------------------------------------------------------
+// A few rows of x (m <= 16): mma.sync m16n8k16, weights as A (16 outputs), rows of x as B.
+//
+// The codes are what has to be read, and at the rate of memory 50 of them arrive per SM and
+// cycle, so what counts is instructions per code. A word of 8 codes becomes 4 bf16 pairs with
+// three shifts, four selections (code | 0x4300 is the bf16 128 + code) and four subtractions of
+// 128 + zero (exact), 11 for 8 codes of a lane; the products' order within a word is free, so
+// pairs are (0, 4), (1, 5), (2, 6), (3, 7) of it and x is permuted alike. Each mma takes codes of
+// one group, and a group's sum is scaled on the way into the total, so no weight is rounded.
+//
+// A warp has 32 outputs and every 8th run of groups; the 8 warps' totals meet in shared memory in
+// a fixed order. Weights go from memory to registers, DEPTH chunks of 128 elements ahead; x is
+// read from the caches (16 bytes a lane and word).
+// ---------------------------------------------------------------------------
+constexpr int FEW_WARPS = 8, FEW_OUT = 32, FEW_DEPTH = 3;
+
+__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                          uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Codes i and i + 4 of a word (i < 4, the word shifted by 4 i) less the zero, as a bf16 pair. off: 128 + zero, twice.
+__device__ __forceinline__ uint32_t pair_of(uint32_t shifted, __nv_bfloat162 off) {
+    uint32_t v;
+    asm("lop3.b32 %0, %1, 0x000F000F, 0x43004300, 0xEA;" : "=r"(v) : "r"(shifted));      // (a & b) | c
+    const __nv_bfloat162 d = __hsub2(*reinterpret_cast<__nv_bfloat162 *>(&v), off);
+    return *reinterpret_cast<const uint32_t *>(&d);
+}
+
+// 8 values of x as the pairs (0, 4), (1, 5), (2, 6), (3, 7); fp32 as three bf16 planes that add up to them.
+template <typename T> struct Octet;
+template <> struct Octet<bf16> {
+    static constexpr int PLANES = 1;
+    uint4 v;
+    __device__ __forceinline__ void load(const bf16 *p) { v = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void clear() { v = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void pairs(uint32_t (&b)[1][4]) const {
+        b[0][0] = __byte_perm(v.x, v.z, 0x5410);
+        b[0][1] = __byte_perm(v.x, v.z, 0x7632);
+        b[0][2] = __byte_perm(v.y, v.w, 0x5410);
+        b[0][3] = __byte_perm(v.y, v.w, 0x7632);
+    }
+};
+template <> struct Octet<float> {
+    static constexpr int PLANES = 3;
+    float4 lo, hi;
+    __device__ __forceinline__ void load(const float *p) {
+        lo = *reinterpret_cast<const float4 *>(p);
+        hi = *reinterpret_cast<const float4 *>(p + 4);
+    }
+    __device__ __forceinline__ void clear() { lo = hi = make_float4(0.f, 0.f, 0.f, 0.f); }
+    // A value's upper 16 bits, those of what is left, and the 8 bits left then: truncations, so the three parts add
+    // up to it and none overflows. What is not finite goes into the first part alone.
+    static __device__ __forceinline__ void part(float a, float c, uint32_t (&b)[3][4], int i) {
+        const uint32_t ua = __float_as_uint(a), uc = __float_as_uint(c);
+        b[0][i] = __byte_perm(ua, uc, 0x7632);
+        float ra = a - __uint_as_float(ua & 0xFFFF0000u), rc = c - __uint_as_float(uc & 0xFFFF0000u);
+        if (!(fabsf(a) < INFINITY)) { ra = 0.f; if (a != a) b[0][i] |= 0x7FC0u; }
+        if (!(fabsf(c) < INFINITY)) { rc = 0.f; if (c != c) b[0][i] |= 0x7FC00000u; }
+        const uint32_t va = __float_as_uint(ra), vc = __float_as_uint(rc);
+        b[1][i] = __byte_perm(va, vc, 0x7632);
+        b[2][i] = __byte_perm(__float_as_uint(ra - __uint_as_float(va & 0xFFFF0000u)),
+                              __float_as_uint(rc - __uint_as_float(vc & 0xFFFF0000u)), 0x7632);
+    }
+    __device__ __forceinline__ void pairs(uint32_t (&b)[3][4]) const {
+        part(lo.x, hi.x, b, 0);
+        part(lo.y, hi.y, b, 1);
+        part(lo.z, hi.z, b, 2);
+        part(lo.w, hi.w, b, 3);
+    }
+};
+
+// GROUP elements share a scale; lane t % 4 has GROUP / 4 consecutive ones of each group of its rows. NT: tiles of 8
+// rows of x. WIDE: the codes of a lane and group are aligned to their size.
+template <typename T, int GROUP, int NT, bool WIDE>
+__global__ void __launch_bounds__(FEW_WARPS * 32)
+linear4_few_kernel(const T *__restrict__ x, long ldx, int m, Weight w, float *__restrict__ y, long ldy, int accumulate,
+                   int staged) {
+    constexpr int WORDS = GROUP / 32;           // words of a lane, row and group
+    constexpr int PER = 128 / GROUP;            // groups of a chunk
+    constexpr int P = Octet<T>::PLANES;
     wait_prior();
     allow_dependents();
-    const int lane = threadIdx.x & 31, j = blockIdx.x * 8 + (threadIdx.x >> 5), i0 = blockIdx.y * 8;
-    if (j >= w.o) return;
-    const uint32_t *codes = reinterpret_cast<const uint32_t *>(w.codes + (long)j * (w.k / 2));
-    float acc[8] = {};
-    for (int c = lane; c < w.k / 8; c += 32) {
-        const uint32_t q = codes[c];
-        const long g = (long)j * w.groups + c * 8 / w.group;
-        const float s = __bfloat162float(w.scales[g]);
-        const int z = w.zeros ? w.zeros[g] : 8;
+    extern __shared__ __align__(16) uint8_t smem[];
+    float *part = reinterpret_cast<float *>(smem);                                  // [warps][FEW_OUT][NT * 8]
+    bf16 *scales = reinterpret_cast<bf16 *>(smem + FEW_WARPS * FEW_OUT * NT * 8 * 4);   // [FEW_OUT][groups]
+    uint8_t *zeros = reinterpret_cast<uint8_t *>(scales + FEW_OUT * w.groups);          // [FEW_OUT][groups]
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const int j0 = blockIdx.x * FEW_OUT, outs = min(FEW_OUT, w.o - j0);
+    const int chunks = (w.groups + PER - 1) / PER, c0 = chunks * warp / FEW_WARPS, c1 = chunks * (warp + 1) / FEW_WARPS;
+    const int words_row = w.k / 8;
+    const uint32_t *codes = reinterpret_cast<const uint32_t *>(w.codes);
+    const uint32_t *row[4];                     // outputs g, g + 8, g + 16, g + 24; the last one's codes stand in for those past it
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (i0 + i >= m) break;
-            const float4 a = Vec4<T>::load(x + (long)(i0 + i) * ldx + c * 8), b = Vec4<T>::load(x + (long)(i0 + i) * ldx + c * 8 + 4);
-            const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-            float t = 0.f;
+    for (int r = 0; r < 4; ++r) row[r] = codes + (long)(j0 + min(g + 8 * r, outs - 1)) * words_row;
+
+    uint32_t q[FEW_DEPTH][4][4];                // [chunk][row][word]
+    auto fetch = [&](int c, uint32_t (&to)[4][4]) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) t = fmaf(v[e], (float)((int)(q >> (4 * e) & 15) - z), t);
-            acc[i] = fmaf(s, t, acc[i]);
+        for (int e = 0; e < PER; ++e) {
+            const int at = (c * PER + e) * (GROUP / 8) + t * WORDS;       // first word
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                uint32_t *d = to[r] + e * WORDS;
+                if (WIDE && at + WORDS <= words_row) {
+                    if constexpr (WORDS == 4) {
+                        const uint4 v = __ldcs(reinterpret_cast<const uint4 *>(row[r] + at));
+                        d[0] = v.x; d[1] = v.y; d[2] = v.z; d[3] = v.w;
+                    } else if constexpr (WORDS == 2) {
+                        const uint2 v = __ldcs(reinterpret_cast<const uint2 *>(row[r] + at));
+                        d[0] = v.x; d[1] = v.y;
+                    } else {
+                        d[0] = __ldcs(row[r] + at);
+                    }
+                } else {
+#pragma unroll
+                    for (int v = 0; v < WORDS; ++v) d[v] = at + v < words_row ? __ldcs(row[r] + at + v) : 0;
+                }
+            }
+        }
+    };
+#pragma unroll
+    for (int d = 0; d < FEW_DEPTH; ++d)
+        if (c0 + d < c1) fetch(c0 + d, q[d]);
+
+    const bf16 *sc_at = w.scales + (long)j0 * w.groups;
+    const uint8_t *z_at = w.zeros + (long)j0 * w.groups;
+    if (staged) {   // scales and zeros of the tile: one run of each
+        const int n = outs * w.groups;
+        const bf16 *from = w.scales + (long)j0 * w.groups;
+        if (reinterpret_cast<uintptr_t>(from) % 16 == 0) {
+            for (int i = tid; i < n / 8; i += FEW_WARPS * 32) reinterpret_cast<uint4 *>(scales)[i] = reinterpret_cast<const uint4 *>(from)[i];
+            for (int i = n / 8 * 8 + tid; i < n; i += FEW_WARPS * 32) scales[i] = from[i];
+        } else {
+            for (int i = tid; i < n; i += FEW_WARPS * 32) scales[i] = from[i];
+        }
+        if (w.zeros) {
+            const uint8_t *z = w.zeros + (long)j0 * w.groups;
+            for (int i = tid; i < n; i += FEW_WARPS * 32) zeros[i] = z[i];
+        }
+        sc_at = scales;
+        z_at = zeros;
+    }
+    __syncthreads();
+
+    float total[2][NT][4] = {};
+    const T *xr[NT];
+    bool on[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        on[n] = 8 * n + g < m;
+        xr[n] = x + (long)(on[n] ? 8 * n + g : 0) * ldx;
+    }
+    auto chunk = [&](int c, const uint32_t (&from)[4][4]) {
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            const int group = c * PER + e;
+            if (PER > 1 && group >= w.groups) break;
+            float acc[2][NT][4] = {};
+            __nv_bfloat162 off[4];
+            float sc[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int at = min(g + 8 * r, outs - 1) * w.groups + group;
+                const unsigned o = 0x4300u + (w.zeros ? z_at[at] : 8u);             // 128 + zero
+                const uint32_t both = o | o << 16;
+                off[r] = *reinterpret_cast<const __nv_bfloat162 *>(&both);
+                sc[r] = __bfloat162float(sc_at[at]);
+            }
+#pragma unroll
+            for (int v = 0; v < WORDS; ++v) {
+                const int at = (group * (GROUP / 8) + t * WORDS + v) * 8;           // first element of the word
+                Octet<T> o[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    if (on[n] && at < w.k) o[n].load(xr[n] + at); else o[n].clear();
+                }
+                uint32_t a[4][4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) a[r][i] = pair_of(from[r][e * WORDS + v] >> (4 * i), off[r]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    uint32_t b[P][4];
+                    o[n].pairs(b);
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            mma_16816(acc[h][n], a[2 * h][0], a[2 * h + 1][0], a[2 * h][1], a[2 * h + 1][1], b[p][0], b[p][1]);
+                            mma_16816(acc[h][n], a[2 * h][2], a[2 * h + 1][2], a[2 * h][3], a[2 * h + 1][3], b[p][2], b[p][3]);
+                        }
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) total[h][n][i] = fmaf(sc[2 * h + (i >> 1)], acc[h][n][i], total[h][n][i]);
+        }
+    };
+    for (int c = c0; c < c1; c += FEW_DEPTH) {
+#pragma unroll
+        for (int d = 0; d < FEW_DEPTH; ++d) {
+            if (c + d < c1) {
+                chunk(c + d, q[d]);
+                if (c + d + FEW_DEPTH < c1) fetch(c + d + FEW_DEPTH, q[d]);
+            }
         }
     }
+
+    // totals of the warps, added in their order
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (i0 + i >= m) break;
-        const float t = warp_sum(acc[i]);
-        if (lane == 0) {
-            float *at = y + (long)(i0 + i) * ldy + j;
-            *at = accumulate ? *at + t : t;
-        }
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                part[(warp * NT * 8 + n * 8 + 2 * t + (i & 1)) * FEW_OUT + 16 * h + 8 * (i >> 1) + g] = total[h][n][i];
+    __syncthreads();
+    for (int i = tid; i < NT * 8 * FEW_OUT; i += FEW_WARPS * 32) {
+        const int j = i % FEW_OUT, r = i / FEW_OUT;
+        if (j >= outs || r >= m) continue;
+        float v = 0.f;
+#pragma unroll
+        for (int k = 0; k < FEW_WARPS; ++k) v += part[(k * NT * 8 + r) * FEW_OUT + j];
+        float *to = y + (long)r * ldy + j0 + j;
+        *to = accumulate ? *to + v : v;
     }
+}
+
+template <typename T>
+using FewKernel = void (*)(const T *, long, int, Weight, float *, long, int, int);
+
+template <typename T, int GROUP>
+static FewKernel<T> few_kernel(bool two, bool wide) {
+    return two ? wide ? linear4_few_kernel<T, GROUP, 2, true> : linear4_few_kernel<T, GROUP, 2, false>
+               : wide ? linear4_few_kernel<T, GROUP, 1, true> : linear4_few_kernel<T, GROUP, 1, false>;
+}
+
+template <typename T>
+static cudaError_t launch_few(const T *x, long ldx, int m, const Weight &w, float *y, long ldy, int accumulate, cudaStream_t s) {
+    const int align = w.group / 8;              // bytes of a lane's codes of a group
+    const bool wide = reinterpret_cast<uintptr_t>(w.codes) % align == 0 && w.k / 2 % align == 0;
+    const int step = m > 8 ? 16 : 8;
+    const FewKernel<T> f = w.group == 128 ? few_kernel<T, 128>(m > 8, wide) : w.group == 64 ? few_kernel<T, 64>(m > 8, wide) : few_kernel<T, 32>(m > 8, wide);
+    const size_t sums = (size_t)FEW_WARPS * FEW_OUT * step * 4, beside = (size_t)FEW_OUT * w.groups * 3;
+    const bool staged = beside <= 64 * 1024;    // longer rows read them where they are
+    const size_t smem = sums + (staged ? beside : 0);
+    cudaError_t e = cudaSuccess;
+    if (smem > 48 * 1024) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    for (int i = 0; i < m && e == cudaSuccess; i += step) {
+        e = launch_chain(f, (w.o + FEW_OUT - 1) / FEW_OUT, FEW_WARPS * 32, smem, s, x + (long)i * ldx, ldx, std::min(m - i, step), w,
+                         y + (long)i * ldy, ldy, accumulate, (int)staged);
+        note_launch();
+    }
+    return e;
 }
 
 // The bf16 nearest to span / n (ties to even), span = hi + lo exactly, n = 7 or 15, span >= 0. The
@@ -141,16 +367,10 @@ msd_status msd_linear4(const void *x, int64_t ldx, int32_t x_dtype, int32_t m, c
     if (m < 0 || !take_weight(weight, &w) || (x_dtype != MSD_F32 && x_dtype != MSD_BF16)) return MSD_ERR_INVALID;
     if (m == 0) return MSD_OK;
     if (bad_rows(x, ldx, x_dtype, w.k) || !y || ldy < w.o || reinterpret_cast<uintptr_t>(y) % 4) return MSD_ERR_INVALID;
-    if (m > 65535 * 8) return MSD_ERR_INVALID;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const dim3 grid((w.o + 7) / 8, (m + 7) / 8);
-    const cudaError_t e =
-        x_dtype == MSD_F32
-            ? launch_chain(linear4_kernel<float>, grid, 256, 0, s, static_cast<const float *>(x), (long)ldx, m, w, y, (long)ldy, accumulate)
-            : launch_chain(linear4_kernel<bf16>, grid, 256, 0, s, static_cast<const bf16 *>(x), (long)ldx, m, w, y, (long)ldy, accumulate);
-    if (e != cudaSuccess) return MSD_ERR_CUDA;
-    note_launch();
-    return MSD_OK;
+    const cudaError_t e = x_dtype == MSD_F32 ? launch_few(static_cast<const float *>(x), (long)ldx, m, w, y, (long)ldy, accumulate, s)
+                                             : launch_few(static_cast<const bf16 *>(x), (long)ldx, m, w, y, (long)ldy, accumulate, s);
+    return e == cudaSuccess ? MSD_OK : MSD_ERR_CUDA;
 }
 
 msd_status msd_quantize4(const void *x, int64_t ldw, int32_t dtype, const msd_weight4 *out, void *values, int64_t ldv,
