@@ -2,17 +2,9 @@
 // (msd_quantize4). Formats in include/msd.h.
 #include <algorithm>
 
-#include "common.cuh"
-#include "msd.h"
+#include "linear4.cuh"
 
 namespace msd {
-
-struct Weight {
-    uint8_t *codes;
-    bf16 *scales;
-    uint8_t *zeros;
-    int o, k, group, groups;
-};
 
 // ---------------------------------------------------------------------------
 // A few rows of x (m <= 16): mma.sync m16n8k16, weights as A (16 outputs), rows of x as B.
@@ -36,57 +28,6 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-
-// Codes i and i + 4 of a word (i < 4, the word shifted by 4 i) less the zero, as a bf16 pair. off: 128 + zero, twice.
-__device__ __forceinline__ uint32_t pair_of(uint32_t shifted, __nv_bfloat162 off) {
-    uint32_t v;
-    asm("lop3.b32 %0, %1, 0x000F000F, 0x43004300, 0xEA;" : "=r"(v) : "r"(shifted));      // (a & b) | c
-    const __nv_bfloat162 d = __hsub2(*reinterpret_cast<__nv_bfloat162 *>(&v), off);
-    return *reinterpret_cast<const uint32_t *>(&d);
-}
-
-// 8 values of x as the pairs (0, 4), (1, 5), (2, 6), (3, 7); fp32 as three bf16 planes that add up to them.
-template <typename T> struct Octet;
-template <> struct Octet<bf16> {
-    static constexpr int PLANES = 1;
-    uint4 v;
-    __device__ __forceinline__ void load(const bf16 *p) { v = *reinterpret_cast<const uint4 *>(p); }
-    __device__ __forceinline__ void clear() { v = make_uint4(0, 0, 0, 0); }
-    __device__ __forceinline__ void pairs(uint32_t (&b)[1][4]) const {
-        b[0][0] = __byte_perm(v.x, v.z, 0x5410);
-        b[0][1] = __byte_perm(v.x, v.z, 0x7632);
-        b[0][2] = __byte_perm(v.y, v.w, 0x5410);
-        b[0][3] = __byte_perm(v.y, v.w, 0x7632);
-    }
-};
-template <> struct Octet<float> {
-    static constexpr int PLANES = 3;
-    float4 lo, hi;
-    __device__ __forceinline__ void load(const float *p) {
-        lo = *reinterpret_cast<const float4 *>(p);
-        hi = *reinterpret_cast<const float4 *>(p + 4);
-    }
-    __device__ __forceinline__ void clear() { lo = hi = make_float4(0.f, 0.f, 0.f, 0.f); }
-    // A value's upper 16 bits, those of what is left, and the 8 bits left then: truncations, so the three parts add
-    // up to it and none overflows. What is not finite goes into the first part alone.
-    static __device__ __forceinline__ void part(float a, float c, uint32_t (&b)[3][4], int i) {
-        const uint32_t ua = __float_as_uint(a), uc = __float_as_uint(c);
-        b[0][i] = __byte_perm(ua, uc, 0x7632);
-        float ra = a - __uint_as_float(ua & 0xFFFF0000u), rc = c - __uint_as_float(uc & 0xFFFF0000u);
-        if (!(fabsf(a) < INFINITY)) { ra = 0.f; if (a != a) b[0][i] |= 0x7FC0u; }
-        if (!(fabsf(c) < INFINITY)) { rc = 0.f; if (c != c) b[0][i] |= 0x7FC00000u; }
-        const uint32_t va = __float_as_uint(ra), vc = __float_as_uint(rc);
-        b[1][i] = __byte_perm(va, vc, 0x7632);
-        b[2][i] = __byte_perm(__float_as_uint(ra - __uint_as_float(va & 0xFFFF0000u)),
-                              __float_as_uint(rc - __uint_as_float(vc & 0xFFFF0000u)), 0x7632);
-    }
-    __device__ __forceinline__ void pairs(uint32_t (&b)[3][4]) const {
-        part(lo.x, hi.x, b, 0);
-        part(lo.y, hi.y, b, 1);
-        part(lo.z, hi.z, b, 2);
-        part(lo.w, hi.w, b, 3);
-    }
-};
 
 // GROUP elements share a scale; lane t % 4 has GROUP / 4 consecutive ones of each group of its rows. NT: tiles of 8
 // rows of x. WIDE: the codes of a lane and group are aligned to their size.
@@ -368,8 +309,12 @@ msd_status msd_linear4(const void *x, int64_t ldx, int32_t x_dtype, int32_t m, c
     if (m == 0) return MSD_OK;
     if (bad_rows(x, ldx, x_dtype, w.k) || !y || ldy < w.o || reinterpret_cast<uintptr_t>(y) % 4) return MSD_ERR_INVALID;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = x_dtype == MSD_F32 ? launch_few(static_cast<const float *>(x), (long)ldx, m, w, y, (long)ldy, accumulate, s)
-                                             : launch_few(static_cast<const bf16 *>(x), (long)ldx, m, w, y, (long)ldy, accumulate, s);
+    // tensor copies take rows of codes that start on 16 bytes
+    const bool tc = reinterpret_cast<uintptr_t>(w.codes) % 16 == 0 && w.k % 32 == 0 && m > (x_dtype == MSD_F32 ? 3 : 16);
+    const auto run = [&](auto *p) {
+        return tc ? launch_linear4_tc(p, (long)ldx, m, w, y, (long)ldy, accumulate, s) : launch_few(p, (long)ldx, m, w, y, (long)ldy, accumulate, s);
+    };
+    const cudaError_t e = x_dtype == MSD_F32 ? run(static_cast<const float *>(x)) : run(static_cast<const bf16 *>(x));
     return e == cudaSuccess ? MSD_OK : MSD_ERR_CUDA;
 }
 
