@@ -3,10 +3,17 @@
 // (msd_accept_batch).
 //
 // Every setting leaves a run from the front of the order (larger logit first, then lower id), so
-// what is left is described by the last logit in it, by how many of the tokens that have just
-// this logit are in it (the ones with the lowest ids), and by the exponent that min-p allows.
-// Weights are integers (weight_exp.cuh), so sums over any part of a row are exact, and every
-// search below is one for the place where an exact, monotone sum passes a bound.
+// what is left is described by the last logit in it, by the last of the ids that have just this
+// logit, and by the exponent that min-p allows. Weights are integers (weight_exp.cuh), so sums over
+// any part of a row are exact, and every search below is one for the place where an exact,
+// monotone sum passes a bound.
+//
+// A row belongs to a cluster of 1 to 8 CTAs, each with a slice of it in shared memory: it is read
+// from memory once. The end of the run is found by a histogram of the order (1024 buckets, linear
+// in the exponent; counts for top-k, exact masses in three 32-bit pieces for top-p), a look at the
+// one bucket that the bound falls into, and the comparison of its few tokens with one another. A
+// bucket with too many tokens is split again by the logits' bits, down to equal logits, where ids
+// decide; so nothing depends on how logits are spread. Sums of blocks of 128 or 256 ids then lead to the token.
 #include <algorithm>
 
 #include "msd.h"
@@ -18,7 +25,9 @@ typedef unsigned long long u64;
 
 static __device__ const ExpTable g_exp_table = ExpTable();
 
-constexpr int ROW_THREADS = 512;
+constexpr int ROW_THREADS = 512, WARPS = ROW_THREADS / 32;
+constexpr int BUCKETS = 1024, LIST = 512;
+constexpr float Y_MOST = 46.f;                  // exponents from here on have weight 0
 constexpr int MAX_VOCAB = 393216;
 constexpr int MAX_CHILDREN = 256;
 constexpr int MAX_TREE_NODES = 1024;
@@ -64,170 +73,538 @@ __device__ __forceinline__ u64 weight_left(const Left &l, float x, int id, const
     return weight_of(y, table);
 }
 
-struct Shared {
-    float2 table[EXP_STEPS];
-    u64 red[33];
+// ---------------------------------------------------------------------------
+// A row over the CTAs of a cluster
+// ---------------------------------------------------------------------------
+struct Found {                // the end of a run, or a bucket
+    unsigned bucket;
+    u64 above;                // weight or count of what comes before the bucket
 };
 
-__device__ __forceinline__ u64 block_total(u64 v, u64 *red) {
+struct Shared {
+    float2 table[EXP_STEPS];
+    unsigned hist[3][BUCKETS];
+    u64 red[WARPS + 1];
+    u64 seg[8];               // of each CTA of the cluster
+    u64 total[8];
+    unsigned top[8], low[8], valid[8];
+    Found found;
+    unsigned list_key[LIST];  // rank 0: tokens of a bucket
+    int list_id[LIST];
+    unsigned list_n, range_lo, range_hi;        // rank 0's list_n; own smallest and largest key
+    unsigned end_key;
+    int end_id;
+    int token;
+    int next, gones, gone[MAX_CHILDREN];
+    u64 kid_w[MAX_CHILDREN];
+    u64 left;
+};
+
+__device__ __forceinline__ uint32_t peer_address(const void *p, int rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void put(u64 *p, int rank, u64 v) {
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(peer_address(p, rank)), "l"(v) : "memory");
+}
+__device__ __forceinline__ void put(unsigned *p, int rank, unsigned v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_address(p, rank)), "r"(v) : "memory");
+}
+__device__ __forceinline__ void put(int *p, int rank, int v) { put(reinterpret_cast<unsigned *>(p), rank, (unsigned)v); }
+__device__ __forceinline__ unsigned get(const unsigned *p, int rank) {
+    unsigned v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(peer_address(p, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ unsigned take_slot(unsigned *p, int rank) {
+    unsigned v;
+    asm volatile("atom.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(v) : "r"(peer_address(p, rank)) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ u64 warp_total(u64 v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-    __syncthreads();
-    if (threadIdx.x < 32) {
-        u64 t = threadIdx.x < blockDim.x >> 5 ? red[threadIdx.x] : 0;
+    return v;
+}
+
+// 16 bytes of a row.
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+    static constexpr int E = 4;
+    static __device__ __forceinline__ void get(const uint4 &v, float (&x)[4]) {
+        x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+    }
+};
+template <> struct Vec<bf16> {
+    static constexpr int E = 8;
+    static __device__ __forceinline__ void get(const uint4 &v, float (&x)[8]) {
+        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-        if (threadIdx.x == 0) red[32] = t;
-    }
-    __syncthreads();
-    return red[32];
-}
-
-// Sum of f(id, logit) over the row.
-template <typename T, typename F>
-__device__ __forceinline__ u64 row_total(const T *row, int V, Shared &sh, F f) {
-    u64 v = 0;
-    for (int i = threadIdx.x; i < V; i += blockDim.x) v += f(i, logit_at(row, i));
-    return block_total(v, sh.red);
-}
-
-__device__ __forceinline__ void load_table(Shared &sh) {
-    for (int i = threadIdx.x; i < EXP_STEPS; i += blockDim.x)
-        sh.table[i] = make_float2(g_exp_table.hi[i], g_exp_table.lo[i]);
-    __syncthreads();
-}
-
-// What the settings of entry `at` leave of a row.
-template <typename T>
-__device__ Left filter_row(const T *row, int V, const Settings &f, int at, Shared &sh) {
-    Left l;
-    unsigned best = 0;
-    for (int i = threadIdx.x; i < V; i += blockDim.x) best = max(best, key_of(logit_at(row, i)));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) sh.red[threadIdx.x >> 5] = best;
-    __syncthreads();
-    for (int i = 0; i < (int)(blockDim.x >> 5); ++i) best = max(best, (unsigned)sh.red[i]);
-    l.total = 0;
-    l.key = 1;
-    l.tie = V;
-    l.limit = make_float2(INFINITY, 0.f);
-    l.scale = RowScale{logit_of(best), 0.f, 0.f};
-    if (best == 0) return l;
-
-    float temp = f.temperature ? f.temperature[at] : 1.f;
-    int k = f.top_k ? f.top_k[at] : 0;
-    const float p = f.top_p ? f.top_p[at] : 1.f, m = f.min_p ? f.min_p[at] : 0.f;
-    if (!(temp >= 0x1p-100f) || m > 1.f || p <= 0.f) k = 1;
-    temp = fminf(fmaxf(temp, 0x1p-100f), 0x1p100f);
-    if (!(temp > 0.f)) temp = 1.f;
-    const double c = 1.4426950408889634074 / (double)temp;
-    l.scale.c_hi = (float)c;
-    l.scale.c_lo = (float)(c - (double)l.scale.c_hi);
-
-    u64 need = ~0ull;                                   // ids with the last key that are left
-    const auto weigh = [&](float x) {
-        Left all = l;
-        all.key = 1;
-        return weight_left(all, x, 0, sh.table);
-    };
-    if (k > 0 && k < V) {
-        unsigned t = 0;
-        for (int bit = 31; bit >= 0; --bit) {
-            const unsigned c2 = t | 1u << bit;
-            if (row_total(row, V, sh, [&](int, float x) { return (u64)(key_of(x) >= c2); }) >= (u64)k) t = c2;
-        }
-        if (t > 0) {
-            l.key = t;
-            need = k - row_total(row, V, sh, [&](int, float x) { return (u64)(key_of(x) > t); });
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(u[i] << 16);
+            x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
         }
     }
-    if (p < 1.f && k != 1) {
-        const u64 above = row_total(row, V, sh, [&](int, float x) { return key_of(x) > l.key ? weigh(x) : 0; });
-        const u64 ties = row_total(row, V, sh, [&](int, float x) { return (u64)(key_of(x) == l.key); });
-        const u64 goal = max(share_floor(p, above + (ties ? min(need, ties) * weigh(logit_of(l.key)) : 0), true), 1ull);
-        unsigned t = 0;
-        for (int bit = 31; bit >= 0; --bit) {
-            const unsigned c2 = t | 1u << bit;
-            if (c2 <= l.key || row_total(row, V, sh, [&](int, float x) { return key_of(x) >= c2 ? weigh(x) : 0; }) >= goal)
-                t = c2;
-        }
-        const u64 over = row_total(row, V, sh, [&](int, float x) { return key_of(x) > t ? weigh(x) : 0; });
-        const u64 each = max(weigh(logit_of(t)), 1ull);
-        const u64 some = (goal - over + each - 1) / each;
-        need = t == l.key ? min(need, some) : some;
-        l.key = t;
-    }
-    if (m > 0.f) {
-        const double y = -log2((double)fminf(m, 1.f));
-        l.limit.x = (float)y;
-        l.limit.y = (float)(y - (double)l.limit.x);
-    }
-    if (need < (u64)V) {
-        // the need-th id with the last key
-        unsigned t = 0;
-        for (int bit = 18; bit >= 0; --bit) {
-            const unsigned c2 = t | 1u << bit;          // ids below c2
-            if (row_total(row, V, sh, [&](int i, float x) { return (u64)((unsigned)i < c2 && key_of(x) == l.key); }) < need)
-                t = c2;
-        }
-        l.tie = (int)t;
-    }
-    l.total = row_total(row, V, sh, [&](int i, float x) { return weight_left(l, x, i, sh.table); });
-    return l;
-}
-
-// The smallest id whose cumulative weight exceeds u of all; w(id, logit) are the weights, total their sum.
-template <typename T, typename F>
-__device__ int draw_row(const T *row, int V, float u, u64 total, Shared &sh, F w) {
-    if (total == 0) return -1;
-    u = fminf(u > 0.f ? u : 0.f, 0x1.fffffep-1f);
-    const u64 goal = share_floor(u, total, false);
-    unsigned t = 0;
-    for (int bit = 18; bit >= 0; --bit) {
-        const unsigned c2 = t | 1u << bit;
-        if (row_total(row, V, sh, [&](int i, float x) { return (unsigned)i < c2 ? w(i, x) : 0; }) <= goal) t = c2;
-    }
-    return (int)t;
-}
+};
 
 template <typename T>
-__global__ void __launch_bounds__(ROW_THREADS)
-sample_kernel(const T *__restrict__ logits, long ld, int V, Settings f, const float *__restrict__ u,
+struct Row {
+    static constexpr int E = Vec<T>::E, BLOCK = 32 * E;
+    const T *row;             // in memory
+    int V, ctas, rank;
+    Shared *sh;
+    u64 *sums;                // of the slice's blocks
+    uint4 *data;              // the slice, -inf around it, in whole blocks
+    int first, count, mis, blocks;              // ids of the slice; element `first` is data's element `mis`
+    unsigned top, valid;      // largest key; tokens that have weight
+    float x_low;              // smallest logit of these
+    float bucket_scale;
+
+    __device__ __forceinline__ void sync() const {
+        if (ctas > 1) asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        else __syncthreads();
+    }
+    template <typename U> __device__ __forceinline__ void tell(U *p, U v) const {          // one thread: to every CTA
+        for (int r = 0; r < ctas; ++r) put(p, r, v);
+    }
+    __device__ __forceinline__ u64 block_sum(u64 v) const {
+        v = warp_total(v);
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) sh->red[threadIdx.x >> 5] = v;
+        __syncthreads();
+        if (threadIdx.x < 32) {
+            const u64 t = warp_total(threadIdx.x < WARPS ? sh->red[threadIdx.x] : 0);
+            if (threadIdx.x == 0) sh->red[WARPS] = t;
+        }
+        __syncthreads();
+        return sh->red[WARPS];
+    }
+
+    // f(logits, first id) for the blocks of this warp, whole warps at a time. Ids around the slice have -inf.
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+        for (int b = threadIdx.x >> 5; b < blocks; b += WARPS) {
+            float x[E];
+            Vec<T>::get(data[b * 32 + (threadIdx.x & 31)], x);
+            f(x, first - mis + b * BLOCK + (int)(threadIdx.x & 31) * E, b);
+        }
+    }
+
+    // The slice into shared memory; largest and smallest logit of the row, tokens that have weight.
+    __device__ void load() {
+        const int tid = threadIdx.x;
+        if (ctas > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+        for (int i = tid; i < EXP_STEPS; i += ROW_THREADS) sh->table[i] = make_float2(g_exp_table.hi[i], g_exp_table.lo[i]);
+        const T *from = row + first - mis;                                  // 16-byte aligned
+        const uint4 *from16 = reinterpret_cast<const uint4 *>(from);
+        const int vecs = blocks * 32;
+        unsigned hi = 0, lo = ~0u, n = 0;
+        constexpr int U = 8;
+        for (int v0 = tid; v0 < vecs; v0 += U * ROW_THREADS) {
+            uint4 q[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int v = v0 + u * ROW_THREADS, i = v * E;              // first element of the vector
+                if (i >= mis && i + E <= mis + count) {
+                    q[u] = __ldcs(from16 + v);
+                } else {
+                    constexpr unsigned NONE = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
+                    q[u] = make_uint4(NONE, NONE, NONE, NONE);
+                    if (v < vecs)
+                        for (int e = 0; e < E; ++e)
+                            if (i + e >= mis && i + e < mis + count) {
+                                if constexpr (sizeof(T) == 4) {
+                                    (&q[u].x)[e] = __float_as_uint(from[i + e]);
+                                } else {
+                                    const unsigned b = __bfloat16_as_ushort(from[i + e]);
+                                    unsigned &w = (&q[u].x)[e >> 1];
+                                    w = e & 1 ? (w & 0xFFFFu) | b << 16 : (w & 0xFFFF0000u) | b;
+                                }
+                            }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int v = v0 + u * ROW_THREADS;
+                if (v >= vecs) break;
+                data[v] = q[u];
+                float x[E];
+                Vec<T>::get(q[u], x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const unsigned k = key_of(x[e]);
+                    hi = max(hi, k);
+                    lo = min(lo, k - 1);                                    // a key of 0 does not count
+                    n += k != 0;
+                }
+            }
+        }
+        hi = __reduce_max_sync(0xffffffffu, hi);
+        lo = __reduce_min_sync(0xffffffffu, lo);
+        n = __reduce_add_sync(0xffffffffu, n);
+        unsigned *part = sh->hist[0];
+        const int warp = tid >> 5;
+        if ((tid & 31) == 0) { part[warp] = hi; part[32 + warp] = lo; part[64 + warp] = n; }
+        if (ctas > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");     // all CTAs run: their shared memory is there
+        __syncthreads();
+        if (tid < 32) {
+            hi = __reduce_max_sync(0xffffffffu, tid < WARPS ? part[tid] : 0u);
+            lo = __reduce_min_sync(0xffffffffu, tid < WARPS ? part[32 + tid] : ~0u);
+            n = __reduce_add_sync(0xffffffffu, tid < WARPS ? part[64 + tid] : 0u);
+            if (tid < ctas) {
+                put(&sh->top[rank], tid, hi);
+                put(&sh->low[rank], tid, lo);
+                put(&sh->valid[rank], tid, n);
+            }
+        }
+        sync();
+        top = 0;
+        lo = ~0u;
+        valid = 0;
+        for (int r = 0; r < ctas; ++r) {
+            top = max(top, sh->top[r]);
+            lo = min(lo, sh->low[r]);
+            valid += sh->valid[r];
+        }
+        x_low = logit_of(lo + 1);
+    }
+
+    // Buckets of equal width in the exponent between the largest logit and x_end.
+    __device__ __forceinline__ void spread(const Left &l, float x_end) {
+        const float y = fminf((l.scale.top - x_end) * l.scale.c_hi, Y_MOST);
+        bucket_scale = y > 0.f ? (float)(BUCKETS - 1) / y * l.scale.c_hi : 0.f;
+    }
+    __device__ __forceinline__ unsigned bucket_of(float x, const Left &l) const {
+        return x == l.scale.top ? 0u : (unsigned)__float2int_rz(fminf((l.scale.top - x) * bucket_scale, (float)(BUCKETS - 1)));
+    }
+
+    // Where the run of tokens of `l` ends whose count (mass false) reaches `goal`, or whose weight reaches the share
+    // `p` of theirs (mass true): narrows l.key and l.tie. The bound lies within the run.
+    __device__ void cut(Left &l, bool mass, u64 goal, float p) {
+        const int tid = threadIdx.x;
+        Left whole = l;                                                     // weights of single tokens
+        whole.key = 1;
+        whole.tie = V;
+        const auto in_run = [&](unsigned k, int id) { return k > l.key || (k == l.key && id <= l.tie && k != 0); };
+        u64 above = 0;
+        unsigned k_lo = l.key, k_hi = top;                                  // keys that the bound lies among
+        int shift = -1;                                                     // -1: buckets of the exponent; else of the key's bits
+        const auto place = [&](float x, unsigned k) { return shift < 0 ? bucket_of(x, l) : (k_hi - k) >> shift; };
+        for (int round = 0;; ++round) {
+            for (int i = tid; i < BUCKETS; i += ROW_THREADS) sh->hist[0][i] = sh->hist[1][i] = sh->hist[2][i] = 0;
+            if (tid == 0) { sh->list_n = 0; sh->range_lo = ~0u; sh->range_hi = 0; }
+            __syncthreads();
+            each([&](const float (&x)[E], int id, int) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const unsigned k = key_of(x[e]);
+                    if (k < k_lo || k > k_hi || !in_run(k, id + e)) continue;
+                    const unsigned b = place(x[e], k);
+                    if (mass) {
+                        const u64 w = weight_left(whole, x[e], id + e, sh->table);
+                        atomicAdd(&sh->hist[0][b], (unsigned)w & 0x7FFFu);
+                        atomicAdd(&sh->hist[1][b], (unsigned)(w >> 15) & 0x7FFFu);
+                        atomicAdd(&sh->hist[2][b], (unsigned)(w >> 30));
+                    } else {
+                        atomicAdd(&sh->hist[0][b], 1u);
+                    }
+                }
+            });
+            sync();
+            // this CTA's part of the buckets: BUCKETS / ctas of them, PER a thread
+            const int mine = BUCKETS / ctas, per = (mine + ROW_THREADS - 1) / ROW_THREADS;
+            u64 v[2] = {0, 0};
+            for (int i = 0; i < per; ++i) {
+                const int at = tid * per + i, b = rank * mine + at;
+                if (at < mine)
+                    for (int r = 0; r < ctas; ++r) {
+                        v[i] += get(&sh->hist[0][b], r);
+                        if (mass) v[i] += ((u64)get(&sh->hist[1][b], r) << 15) + ((u64)get(&sh->hist[2][b], r) << 30);
+                    }
+            }
+            u64 run = v[0] + v[1];                                          // inclusive over the threads
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const u64 t = __shfl_up_sync(0xffffffffu, run, o);
+                if ((tid & 31) >= o) run += t;
+            }
+            if ((tid & 31) == 31) sh->red[tid >> 5] = run;
+            __syncthreads();
+            for (int i = 0; i < (tid >> 5); ++i) run += sh->red[i];
+            if (tid == ROW_THREADS - 1) tell(&sh->seg[rank], run);
+            sync();
+            u64 before = above, all = 0;
+            for (int r = 0; r < ctas; ++r) {
+                if (r < rank) before += sh->seg[r];
+                all += sh->seg[r];
+            }
+            if (round == 0 && mass) goal = max(share_floor(p, all, true), 1ull);
+            u64 at = before + run - v[0] - v[1];
+            for (int i = 0; i < per; ++i) {
+                if (v[i] && at < goal && goal <= at + v[i])
+                    for (int r = 0; r < ctas; ++r) {
+                        put(&sh->found.bucket, r, (unsigned)(rank * mine + tid * per + i));
+                        put(&sh->found.above, r, at);
+                    }
+                at += v[i];
+            }
+            sync();
+            const unsigned bucket = sh->found.bucket;
+            above = sh->found.above;
+            // the bucket's tokens, and the range of their keys
+            unsigned lo = ~0u, hi = 0;
+            each([&](const float (&x)[E], int id, int) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const unsigned k = key_of(x[e]);
+                    if (k < k_lo || k > k_hi || !in_run(k, id + e) || place(x[e], k) != bucket) continue;
+                    lo = min(lo, k);
+                    hi = max(hi, k);
+                    const unsigned slot = take_slot(&sh->list_n, 0);
+                    if (slot < LIST) {
+                        put(&sh->list_key[slot], 0, k);
+                        put(&sh->list_id[slot], 0, id + e);
+                    }
+                }
+            });
+            lo = __reduce_min_sync(0xffffffffu, lo);
+            hi = __reduce_max_sync(0xffffffffu, hi);
+            if ((tid & 31) == 0 && hi) {
+                for (int r = 0; r < ctas; ++r) {
+                    asm volatile("red.shared::cluster.min.u32 [%0], %1;" ::"r"(peer_address(&sh->range_lo, r)), "r"(lo) : "memory");
+                    asm volatile("red.shared::cluster.max.u32 [%0], %1;" ::"r"(peer_address(&sh->range_hi, r)), "r"(hi) : "memory");
+                }
+            }
+            sync();
+            const unsigned n = get(&sh->list_n, 0);
+            k_lo = sh->range_lo;
+            k_hi = sh->range_hi;
+            if (n <= LIST) {
+                if (rank == 0) {
+                    u64 *w = reinterpret_cast<u64 *>(sh->hist);             // the tokens' weights
+                    for (unsigned i = tid; i < n; i += ROW_THREADS)
+                        w[i] = mass ? weight_left(whole, logit_of(sh->list_key[i]), sh->list_id[i], sh->table) : 1;
+                    __syncthreads();
+                    for (unsigned i = tid; i < n; i += ROW_THREADS) {
+                        const unsigned k = sh->list_key[i];
+                        const int id = sh->list_id[i];
+                        u64 s = above;
+                        for (unsigned j = 0; j < n; ++j) {
+                            const unsigned kj = sh->list_key[j];
+                            if (kj > k || (kj == k && sh->list_id[j] < id)) s += w[j];
+                        }
+                        if (s < goal && goal <= s + w[i]) {
+                            tell(&sh->end_key, k);
+                            tell(&sh->end_id, id);
+                        }
+                    }
+                }
+                sync();
+                l.key = sh->end_key;
+                l.tie = sh->end_id;
+                return;
+            }
+            if (k_lo == k_hi) {                                             // equal logits: ids decide
+                const u64 each_w = mass ? max(weight_left(whole, logit_of(k_lo), 0, sh->table), 1ull) : 1;
+                const u64 need = (goal - above + each_w - 1) / each_w;
+                add_up([&](float x, int id) { return (u64)(key_of(x) == k_lo && in_run(k_lo, id)); });
+                const int id = locate(need - 1, [&](float x, int id) { return (u64)(key_of(x) == k_lo && in_run(k_lo, id)); });
+                l.key = k_lo;
+                l.tie = id;
+                return;
+            }
+            shift = max(0, 22 - __clz(k_hi - k_lo));                        // (k_hi - k_lo) >> shift < BUCKETS
+            sync();                                                         // all have read the list's length and the range
+        }
+    }
+
+    // Sums of w(logit, id) over each block, this CTA's, and all.
+    template <typename W>
+    __device__ u64 add_up(W w) {
+        u64 sum = 0;
+        each([&](const float (&x)[E], int id, int b) {
+            u64 v = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) v += w(x[e], id + e);
+            if (__any_sync(0xffffffffu, v != 0)) v = warp_total(v);
+            if ((threadIdx.x & 31) == 0) { sums[b] = v; sum += v; }
+        });
+        sum = block_sum(sum);
+        if (threadIdx.x == 0) tell(&sh->total[rank], sum);
+        sync();
+        u64 all = 0;
+        for (int r = 0; r < ctas; ++r) all += sh->total[r];
+        return all;
+    }
+
+    // After add_up: the smallest id whose cumulative w exceeds `goal`, which is less than the whole.
+    template <typename W>
+    __device__ int locate(u64 goal, W w) {
+        u64 before = 0;
+        for (int r = 0; r < rank; ++r) before += sh->total[r];
+        if (before <= goal && goal < before + sh->total[rank] && threadIdx.x < 32) {
+            const int lane = threadIdx.x;
+            u64 rest = goal - before;
+            int b0 = 0;
+            u64 in = 0;
+            for (;; b0 += 32) {                                             // the 32 blocks, then the one
+                in = b0 + lane < blocks ? sums[b0 + lane] : 0;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const u64 t = __shfl_up_sync(0xffffffffu, in, o);
+                    if (lane >= o) in += t;
+                }
+                const u64 all = __shfl_sync(0xffffffffu, in, 31);
+                if (rest < all || b0 + 32 >= blocks) break;
+                rest -= all;
+            }
+            const unsigned over = __ballot_sync(0xffffffffu, in > rest);
+            const int at = over ? __ffs(over) - 1 : 31;
+            const u64 less = __shfl_sync(0xffffffffu, in, max(at - 1, 0));
+            if (at > 0) rest -= less;
+            const int b = b0 + at;
+            float x[E];
+            Vec<T>::get(data[b * 32 + lane], x);
+            const int id = first - mis + b * BLOCK + lane * E;
+            u64 v[E], sum = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) { v[e] = w(x[e], id + e); sum += v[e]; }
+            u64 run = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const u64 t = __shfl_up_sync(0xffffffffu, run, o);
+                if (lane >= o) run += t;
+            }
+            u64 c = run - sum;
+            if (c <= rest && rest < run)
+                for (int e = 0; e < E; ++e) {
+                    if (rest < c + v[e]) { tell(&sh->token, id + e); break; }
+                    c += v[e];
+                }
+        }
+        sync();
+        return sh->token;
+    }
+
+    // What the settings of entry `at` leave.
+    __device__ Left filter(const Settings &f, int at) {
+        Left l;
+        l.total = 0;
+        l.key = 1;
+        l.tie = V;
+        l.limit = make_float2(INFINITY, 0.f);
+        l.scale = RowScale{logit_of(top), 0.f, 0.f};
+        if (top == 0) return l;
+        float temp = f.temperature ? f.temperature[at] : 1.f;
+        int k = f.top_k ? f.top_k[at] : 0;
+        const float p = f.top_p ? f.top_p[at] : 1.f, m = f.min_p ? f.min_p[at] : 0.f;
+        if (!(temp >= 0x1p-100f) || m > 1.f || p <= 0.f) k = 1;
+        temp = temp > 0.f ? fminf(fmaxf(temp, 0x1p-100f), 0x1p100f) : 1.f;
+        const double c = 1.4426950408889634074 / (double)temp;
+        l.scale.c_hi = (float)c;
+        l.scale.c_lo = (float)(c - (double)l.scale.c_hi);
+        if (k == 1) {                                                       // the first token alone
+            unsigned id = ~0u;
+            const float best = l.scale.top;
+            each([&](const float (&x)[E], int first_id, int) {
+#pragma unroll
+                for (int e = E - 1; e >= 0; --e)
+                    if (x[e] == best) id = min(id, (unsigned)(first_id + e));
+            });
+            id = __reduce_min_sync(0xffffffffu, id);
+            if (threadIdx.x == 0) sh->range_lo = ~0u;
+            sync();
+            if ((threadIdx.x & 31) == 0 && id != ~0u)
+                for (int r = 0; r < ctas; ++r)
+                    asm volatile("red.shared::cluster.min.u32 [%0], %1;" ::"r"(peer_address(&sh->range_lo, r)), "r"(id) : "memory");
+            sync();
+            l.key = top;
+            l.tie = (int)sh->range_lo;
+            l.total = 1ull << WEIGHT_BITS;
+            return l;
+        }
+        float x_end = x_low;
+        if (k > 0 && (unsigned)k < valid) {
+            spread(l, x_end);
+            cut(l, false, (u64)k, 1.f);
+            x_end = logit_of(l.key);
+        }
+        if (p < 1.f) {
+            spread(l, x_end);
+            cut(l, true, 0, p);
+        }
+        if (m > 0.f) {
+            const double y = -log2((double)fminf(m, 1.f));
+            l.limit.x = (float)y;
+            l.limit.y = (float)(y - (double)l.limit.x);
+        }
+        l.total = add_up([&](float x, int id) { return weight_left(l, x, id, sh->table); });
+        return l;
+    }
+};
+
+__device__ __forceinline__ float uniform(float u) { return fminf(u > 0.f ? u : 0.f, 0x1.fffffep-1f); }
+
+template <typename T>
+__device__ __forceinline__ Row<T> open_row(const T *row, int V, int ctas, int rank, int slice, Shared *sh, uint8_t *behind) {
+    Row<T> r;
+    r.row = row;
+    r.V = V;
+    r.ctas = ctas;
+    r.rank = rank;
+    r.sh = sh;
+    r.first = min(rank * slice, V);
+    r.count = min(slice, V - r.first);
+    r.mis = (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T));       // slices are multiples of 16 bytes
+    r.blocks = (r.mis + r.count + Row<T>::BLOCK - 1) / Row<T>::BLOCK;
+    const int most = (slice + 16 / (int)sizeof(T) + Row<T>::BLOCK - 1) / Row<T>::BLOCK;
+    r.sums = reinterpret_cast<u64 *>(behind);
+    r.data = reinterpret_cast<uint4 *>(behind + (most * 8 + 15) / 16 * 16);
+    r.load();
+    return r;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(ROW_THREADS, 2)
+sample_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int slice, Settings f, const float *__restrict__ u,
               int *__restrict__ tokens, float *__restrict__ logp, float *__restrict__ probs, long ldp) {
     wait_prior();
     allow_dependents();
-    __shared__ Shared sh;
-    load_table(sh);
-    const T *row = logits + (long)blockIdx.x * ld;
-    const Left l = filter_row(row, V, f, blockIdx.x, sh);
-    const int t = draw_row(row, V, u[blockIdx.x], l.total, sh,
-                           [&](int i, float x) { return weight_left(l, x, i, sh.table); });
-    if (threadIdx.x == 0) {
-        tokens[blockIdx.x] = t;
+    extern __shared__ __align__(16) uint8_t smem[];
+    Shared &sh = *reinterpret_cast<Shared *>(smem);
+    const int r = blockIdx.x / ctas, rank = blockIdx.x % ctas;
+    Row<T> row = open_row(logits + (long)r * ld, V, ctas, rank, slice, &sh, smem + sizeof(Shared));
+    const Left l = row.filter(f, r);
+    int t = -1;
+    if (l.key == row.top && row.top) t = l.total == 1ull << WEIGHT_BITS ? l.tie : -1;
+    if (t < 0 && l.total)
+        t = row.locate(share_floor(uniform(u[r]), l.total, false), [&](float x, int id) { return weight_left(l, x, id, sh.table); });
+    if (rank == 0 && threadIdx.x == 0) {
+        tokens[r] = t;
         if (logp) {
-            const float x = t < 0 ? 0.f : logit_at(row, t);
+            const float x = t < 0 ? 0.f : logit_at(row.row, t);
             const float2 y = t < 0 || x == l.scale.top ? make_float2(0.f, 0.f) : exponent_of(x, l.scale);
-            logp[blockIdx.x] = t < 0 ? -INFINITY : (float)(-0.69314718055994530942 * ((double)y.x + (double)y.y + log2((double)l.total) - WEIGHT_BITS));
+            logp[r] = t < 0 ? -INFINITY : (float)(-0.69314718055994530942 * ((double)y.x + (double)y.y + log2((double)l.total) - WEIGHT_BITS));
         }
     }
     if (probs) {
-        const double inv = l.total ? 1.0 / (double)l.total : 0.0;
-        const float scale = (float)(inv * 0x1p44);
-        for (int i = threadIdx.x; i < V; i += blockDim.x) {
-            const float x = logit_at(row, i);
+        const float scale = l.total ? (float)(0x1p44 / (double)l.total) : 0.f;
+        const T *data = reinterpret_cast<const T *>(row.data) + row.mis;
+        float *to = probs + (long)r * ldp + row.first;
+        for (int i = threadIdx.x; i < row.count; i += ROW_THREADS) {
+            const float x = logit_at(data, i);
             float w = 0.f;
             const unsigned k = key_of(x);
-            if (k > l.key || (k == l.key && i <= l.tie && k)) {
+            if (k > l.key || (k == l.key && row.first + i <= l.tie && k)) {
                 const float2 y = x == l.scale.top ? make_float2(0.f, 0.f) : exponent_of(x, l.scale);
                 if ((y.x - l.limit.x) + (y.y - l.limit.y) <= 0.f) w = exp2f(-y.x) * (1.f - 0.69314718f * y.y) * scale;
             }
-            probs[(long)blockIdx.x * ldp + i] = w;
+            to[i] = w;
         }
     }
+    if (ctas > 1) row.sync();           // no CTA leaves while another may write to it
 }
 
 // Per node of the trees: the child that is accepted there, or -1 and the token drawn there.
@@ -245,14 +622,13 @@ __device__ __forceinline__ int nodes_of(const TreeArgs &a, int b) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(ROW_THREADS)
-accept_rows_kernel(const T *__restrict__ logits, long ld, int V, Settings f, TreeArgs a) {
+__global__ void __launch_bounds__(ROW_THREADS, 2)
+accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int slice, Settings f, TreeArgs a) {
     wait_prior();
     allow_dependents();
-    __shared__ Shared sh;
-    __shared__ int s_next, s_gone[MAX_CHILDREN], s_gones;
-    __shared__ u64 s_left;
-    const int r = blockIdx.x;
+    extern __shared__ __align__(16) uint8_t smem[];
+    Shared &sh = *reinterpret_cast<Shared *>(smem);
+    const int r = blockIdx.x / ctas, rank = blockIdx.x % ctas;
     int b = 0;
     for (int hi = a.n; hi - b > 1;) {                   // the last sequence that starts at or before the row
         const int mid = (b + hi) >> 1;
@@ -260,50 +636,98 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, Settings f, Tre
     }
     const int node = r - a.row_start[b], n = nodes_of(a, b);
     const int *parent = a.parent + (long)b * a.nodes, *tokens = a.tokens + (long)b * a.nodes;
-    if (node >= n) return;
+    if (node < 0 || node >= n) return;
     int d = 0;
     for (int i = node; i > 0; ++d) {
         const int up = parent[i];
         if (up < 0 || up >= i) { d = a.depth + 1; break; }
         i = up;
     }
-    if (d > a.depth) return;                            // never reached
-    load_table(sh);
-    const T *row = logits + (long)r * ld;
-    const Left l = filter_row(row, V, f, b, sh);
+    if (d > a.depth) return;                            // never reached (the whole cluster leaves)
+    Row<T> row = open_row(logits + (long)r * ld, V, ctas, rank, slice, &sh, smem + sizeof(Shared));
+    const Left l = row.filter(f, b);
     const float *u = a.u + ((long)b * (a.depth + 1) + d) * (a.children + 1);
-    if (threadIdx.x == 0) {
+    if (rank == 0 && threadIdx.x < 32) {
+        // the first `children` children, in index order; their weights; then the decisions one after another
+        const int lane = threadIdx.x;
+        int kids = 0;
+        if (d < a.depth)
+            for (int j0 = node + 1; j0 < n && kids < a.children; j0 += 32) {
+                const int j = j0 + lane;
+                const bool is = j < n && parent[j] == node;
+                const unsigned all = __ballot_sync(0xffffffffu, is);
+                const int slot = kids + __popc(all & ((1u << lane) - 1u));
+                if (is && slot < a.children) {
+                    const int t = tokens[j];
+                    sh.list_key[slot] = (unsigned)j;
+                    sh.list_id[slot] = t;
+                    sh.kid_w[slot] = t >= 0 && t < V && l.total ? weight_left(l, logit_at(row.row, t), t, sh.table) : 0;
+                }
+                kids = min(kids + __popc(all), a.children);
+            }
+        __syncwarp();
         u64 left = l.total;
         int gone = 0, next = -1;
-        for (int j = node + 1, c = 0; j < n && c < a.children && d < a.depth && next < 0; ++j) {
-            if (parent[j] != node) continue;
-            const int t = tokens[j];
-            u64 w = t >= 0 && t < V && l.total ? weight_left(l, logit_at(row, t), t, sh.table) : 0;
-            for (int i = 0; i < gone; ++i)
-                if (s_gone[i] == t) w = 0;
-            const float v = fminf(u[c] > 0.f ? u[c] : 0.f, 0x1.fffffep-1f);
-            if (share_floor(v, left, false) < w) next = j;
-            else if (w) { left -= w; s_gone[gone++] = t; }
-            ++c;
+        for (int c = 0; c < kids; ++c) {
+            const int t = sh.list_id[c];
+            u64 w = sh.kid_w[c];
+            bool again = false;
+            for (int i = lane; i < gone; i += 32) again |= sh.gone[i] == t;
+            if (__any_sync(0xffffffffu, again)) w = 0;
+            if (share_floor(uniform(u[c]), left, false) < w) {
+                next = (int)sh.list_key[c];
+                break;
+            }
+            if (w) {
+                left -= w;
+                if (lane == 0) sh.gone[gone] = t;
+                ++gone;
+                __syncwarp();
+            }
         }
-        s_next = next;
-        s_gones = gone;
-        s_left = left;
+        if (lane == 0) {
+            row.tell(&sh.next, next);
+            row.tell(&sh.gones, gone);
+            row.tell(&sh.left, left);
+        }
+        for (int p = 1; p < ctas; ++p)
+            for (int i = lane; i < gone; i += 32) put(&sh.gone[i], p, sh.gone[i]);
     }
-    __syncthreads();
+    row.sync();
     int t = -1;
-    if (s_next < 0)
-        t = draw_row(row, V, u[a.children], s_left, sh, [&](int i, float x) {
-            const u64 w = weight_left(l, x, i, sh.table);
-            if (w)
-                for (int g = 0; g < s_gones; ++g)
-                    if (s_gone[g] == i) return 0ull;
-            return w;
-        });
-    if (threadIdx.x == 0) {
-        a.next[r] = s_next;
+    const int gones = sh.gones;
+    if (sh.next < 0 && sh.left) {
+        if (l.key == row.top && l.total == 1ull << WEIGHT_BITS) {
+            t = l.tie;
+        } else {
+            // the sums without the rejected tokens
+            const auto w = [&](float x, int id) {
+                u64 v = weight_left(l, x, id, sh.table);
+                if (v)
+                    for (int g = 0; g < gones; ++g)
+                        if (sh.gone[g] == id) return 0ull;
+                return v;
+            };
+            if (threadIdx.x == 0 && gones) {
+                u64 less = 0;
+                for (int g = 0; g < gones; ++g) {
+                    const int i = sh.gone[g] - row.first;
+                    if (i < 0 || i >= row.count) continue;
+                    const u64 v = weight_left(l, logit_at(reinterpret_cast<const T *>(row.data), row.mis + i), sh.gone[g], sh.table);
+                    row.sums[(row.mis + i) / Row<T>::BLOCK] -= v;
+                    less += v;
+                }
+                if (less) row.tell(&sh.total[rank], sh.total[rank] - less);
+            }
+            row.sync();
+            t = row.locate(share_floor(uniform(u[a.children]), sh.left, false), w);
+        }
+    }
+    if (rank == 0 && threadIdx.x == 0) {
+        a.next[r] = sh.next;
         a.drawn[r] = t;
     }
+    if (ctas > 1) row.sync();
 }
 
 __global__ void accept_walk_kernel(TreeArgs a) {
@@ -323,6 +747,46 @@ __global__ void accept_walk_kernel(TreeArgs a) {
     a.accept_len[b] = max(d - 1, 0);
     a.bonus[b] = bonus;
     for (; d <= a.depth; ++d) path[d] = -1;
+}
+
+// How many CTAs share a row, and the ids of each: as few as leave room for two CTAs on an SM, more where there are few
+// rows (and 2048 ids for each).
+struct Cut {
+    int ctas, slice;
+    size_t smem;
+};
+static Cut cut_rows(int rows, int V, int size) {
+    const auto smem = [&](int slice) {
+        const int block = 512 / size, most = (slice + 16 / size + block - 1) / block;
+        return sizeof(Shared) + (most * 8 + 15) / 16 * 16 + (size_t)most * 512;
+    };
+    const auto slice_of = [&](int ctas) { return ((V + ctas - 1) / ctas + 7) / 8 * 8; };
+    int c = 1;
+    while (c < 8 && smem(slice_of(c)) > 112 * 1024) c *= 2;
+    while (c < 8 && (long)rows * c * 2 <= 304 && slice_of(c * 2) >= 2048) c *= 2;
+    return Cut{c, slice_of(c), smem(slice_of(c))};
+}
+
+template <typename... K, typename... A>
+static cudaError_t launch_rows(void (*kernel)(K...), int rows, const Cut &c, cudaStream_t s, A... args) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)rows * c.ctas);
+    lc.blockDim = ROW_THREADS;
+    lc.dynamicSmemBytes = c.smem;
+    lc.stream = s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = c.ctas;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = at;
+    lc.numAttrs = programmatic(s) ? 2 : 1;
+    e = cudaLaunchKernelEx(&lc, kernel, K(args)...);
+    note_launch();
+    return e;
 }
 
 static bool take_filter(const msd_filter *f, Settings *s) {
@@ -351,15 +815,15 @@ msd_status msd_sample(const void *logits, int64_t ld, int32_t dtype, int32_t row
     Settings s;
     take_filter(f, &s);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const Cut c = cut_rows(rows, vocab, dtype == MSD_F32 ? 4 : 2);
+    if ((long)rows * c.ctas > 0x7FFFFFFF) return MSD_ERR_INVALID;
     const cudaError_t e =
         dtype == MSD_F32
-            ? launch_chain(sample_kernel<float>, rows, ROW_THREADS, 0, st, static_cast<const float *>(logits), (long)ld,
-                           vocab, s, u, tokens, logp, probs, (long)ldp)
-            : launch_chain(sample_kernel<bf16>, rows, ROW_THREADS, 0, st, static_cast<const bf16 *>(logits), (long)ld,
-                           vocab, s, u, tokens, logp, probs, (long)ldp);
-    if (e != cudaSuccess) return MSD_ERR_CUDA;
-    note_launch();
-    return MSD_OK;
+            ? launch_rows(sample_kernel<float>, rows, c, st, static_cast<const float *>(logits), (long)ld, vocab, c.ctas, c.slice, s, u,
+                          tokens, logp, probs, (long)ldp)
+            : launch_rows(sample_kernel<bf16>, rows, c, st, static_cast<const bf16 *>(logits), (long)ld, vocab, c.ctas, c.slice, s, u,
+                          tokens, logp, probs, (long)ldp);
+    return e == cudaSuccess ? MSD_OK : MSD_ERR_CUDA;
 }
 
 msd_status msd_accept_batch(const void *logits, int64_t ld, int32_t dtype, int32_t vocab, const msd_batch *batch,
@@ -378,14 +842,15 @@ msd_status msd_accept_batch(const void *logits, int64_t ld, int32_t dtype, int32
                      scratch, scratch + batch->rows, path, accept_len, bonus};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (batch->rows > 0) {
+        const Cut c = cut_rows(batch->rows, vocab, dtype == MSD_F32 ? 4 : 2);
+        if ((long)batch->rows * c.ctas > 0x7FFFFFFF) return MSD_ERR_INVALID;
         const cudaError_t e =
             dtype == MSD_F32
-                ? launch_chain(accept_rows_kernel<float>, batch->rows, ROW_THREADS, 0, st,
-                               static_cast<const float *>(logits), (long)ld, vocab, s, a)
-                : launch_chain(accept_rows_kernel<bf16>, batch->rows, ROW_THREADS, 0, st,
-                               static_cast<const bf16 *>(logits), (long)ld, vocab, s, a);
+                ? launch_rows(accept_rows_kernel<float>, batch->rows, c, st, static_cast<const float *>(logits), (long)ld, vocab, c.ctas,
+                              c.slice, s, a)
+                : launch_rows(accept_rows_kernel<bf16>, batch->rows, c, st, static_cast<const bf16 *>(logits), (long)ld, vocab, c.ctas,
+                              c.slice, s, a);
         if (e != cudaSuccess) return MSD_ERR_CUDA;
-        note_launch();
     }
     if (launch_chain(accept_walk_kernel, (batch->n + 31) / 32, 32, 0, st, a) != cudaSuccess) return MSD_ERR_CUDA;
     note_launch();
