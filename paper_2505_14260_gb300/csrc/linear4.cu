@@ -1,6 +1,7 @@
 // Products with weights in 4 bits (msd_linear4) and the codes, scales and zeros of such a weight
 // (msd_quantize4). Formats in include/msd.h.
 #include <algorithm>
+#include <type_traits>
 
 #include "linear4.cuh"
 
@@ -230,57 +231,127 @@ __device__ __forceinline__ float scale_of(float hi, float lo, float n) {
     return s >= 0x1p-126f ? s : 0.f;                    // 1 / s is finite
 }
 
-// w / s to the nearest integer, ties to even, |w / s| < 2^8. The residual w - q s is exact.
+// w / s to the nearest integer, ties to even, |w / s| <= 16. The residual w - q s is exact, so it shows where the
+// rounded product w (1 / s) fell on the wrong side of a border.
 __device__ __forceinline__ float nearest(float w, float s, float inv) {
     float q = rintf(w * inv);
-    const float r = fmaf(-q, s, w);
-    const float twice = r + r;
-    const bool odd = (int)q & 1;
-    if (twice > s || (twice == s && odd)) q += 1.f;
-    else if (twice < -s || (twice == -s && odd)) q -= 1.f;
+    const float r = fmaf(-q, s, w), twice = r + r;
+    if (fabsf(twice) >= s) {
+        const bool odd = (int)q & 1;
+        if (twice > s || (twice == s && odd)) q += 1.f;
+        else if (twice < -s || (twice == -s && odd)) q -= 1.f;
+    }
     return q;
 }
 
-__device__ __forceinline__ float clean(float w) { return w == w ? w : 0.f; }
+__device__ __forceinline__ void load8(const float *p, float (&v)[8]) {
+    const float4 a = __ldcs(reinterpret_cast<const float4 *>(p)), b = __ldcs(reinterpret_cast<const float4 *>(p + 4));
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void load8(const bf16 *p, float (&v)[8]) {
+    const uint4 a = __ldcs(reinterpret_cast<const uint4 *>(p));
+    const uint32_t u[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(u[i] << 16);
+        v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void store8(float *p, const float (&v)[8]) {
+    __stcs(reinterpret_cast<float4 *>(p), make_float4(v[0], v[1], v[2], v[3]));
+    __stcs(reinterpret_cast<float4 *>(p + 4), make_float4(v[4], v[5], v[6], v[7]));
+}
+__device__ __forceinline__ void store8(bf16 *p, const float (&v)[8]) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        u[i] = *reinterpret_cast<const uint32_t *>(&b);
+    }
+    __stcs(reinterpret_cast<uint4 *>(p), make_uint4(u[0], u[1], u[2], u[3]));
+}
 
-// One thread per group (simple form).
-template <typename T>
-__global__ void __launch_bounds__(128)
-quantize4_kernel(const T *__restrict__ x, long ldw, Weight w, T *__restrict__ values, long ldv) {
+// Codes of a matrix: 8 consecutive elements a lane, 4, 8 or 16 lanes a group, so a warp has a run of 256 elements of a
+// row and reads, and writes codes and values, in whole lines. Each value is read once; what bounds it is memory.
+constexpr int Q_THREADS = 256, Q_RUN = 256;
+template <typename T, int GROUP, bool ZEROS>
+__global__ void __launch_bounds__(Q_THREADS)
+quantize4_kernel(const T *__restrict__ x, long ldw, Weight w, T *__restrict__ values, long ldv, int runs, long tasks) {
+    constexpr int LANES = GROUP / 8, U = 2;                 // U runs in flight a warp
     wait_prior();
     allow_dependents();
-    const long at = (long)blockIdx.x * 128 + threadIdx.x;
-    if (at >= (long)w.o * w.groups) return;
-    const int j = (int)(at / w.groups), g = (int)(at % w.groups);
-    const int k0 = g * w.group, k1 = min(k0 + w.group, w.k);
-    const T *row = x + (long)j * ldw;
-    float lo = 0.f, hi = 0.f;
-    for (int k = k0; k < k1; ++k) {
-        const float v = clean((float)row[k]);
-        lo = fminf(lo, v);
-        hi = fmaxf(hi, v);
-    }
-    float s, z = 8.f;
-    if (w.zeros) {
-        const float d = hi - lo, b = d - hi;
-        s = scale_of(d, (hi - (d - b)) + (-lo - b), 15.f);
-        z = s > 0.f ? fminf(fmaxf(nearest(-lo, s, 1.f / s), 0.f), 15.f) : 0.f;
-        w.zeros[at] = (uint8_t)z;
-    } else {
-        s = scale_of(fmaxf(hi, -lo), 0.f, 7.f);
-    }
-    w.scales[at] = __float2bfloat16(s);
-    const float inv = s > 0.f ? 1.f / s : 0.f;
-    for (int k = k0; k < k1; k += 2) {
-        unsigned byte = 0;
-        for (int e = 0; e < 2; ++e) {
-            const float v = fminf(fmaxf(clean((float)row[k + e]), -16.f * s), 16.f * s);
-            const float q = s > 0.f ? fminf(fmaxf(nearest(v, s, inv) + z, 0.f), 15.f) : z;
-            byte |= (unsigned)q << (4 * e);
-            if (values) values[(long)j * ldv + k + e] = (T)(s * (q - z));
+    const int lane = threadIdx.x & 31;
+    const long t0 = ((long)blockIdx.x * (Q_THREADS / 32) + (threadIdx.x >> 5)) * U;
+    float v[U][8];
+    int j[U], k[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const unsigned long t = t0 + u;
+        j[u] = (int)(tasks <= 0x7FFFFFFF ? (unsigned)t / (unsigned)runs : t / (unsigned)runs);
+        k[u] = (int)(t - (unsigned long)j[u] * runs) * Q_RUN + lane * 8;
+        if ((long)t < tasks && k[u] < w.k) {
+            load8(x + (long)j[u] * ldw + k[u], v[u]);
+        } else {
+            k[u] = w.k;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
         }
-        w.codes[(long)j * (w.k / 2) + k / 2] = (uint8_t)byte;
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float lo = 0.f, hi = 0.f;                           // (fminf and fmaxf leave NaN out)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (ZEROS) {
+                lo = fminf(lo, v[u][i]);
+                hi = fmaxf(hi, v[u][i]);
+            } else {
+                hi = fmaxf(hi, fabsf(v[u][i]));
+            }
+        }
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1) {
+            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+            if (ZEROS) lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+        }
+        float s, z = 8.f;
+        if (ZEROS) {
+            const float d = hi - lo, b = d - hi;            // d + its rounding error = hi - lo
+            s = scale_of(d, (hi - (d - b)) + (-lo - b), 15.f);
+            z = s > 0.f ? fminf(fmaxf(nearest(-lo, s, 1.f / s), 0.f), 15.f) : 0.f;
+        } else {
+            s = scale_of(hi, 0.f, 7.f);
+        }
+        if (k[u] >= w.k) continue;
+        const long g = (long)j[u] * w.groups + k[u] / GROUP;
+        if ((lane & (LANES - 1)) == 0) {
+            w.scales[g] = __float2bfloat16(s);
+            if (ZEROS) w.zeros[g] = (uint8_t)z;
+        }
+        const float inv = s > 0.f ? 1.f / s : 0.f, most = 16.f * s;
+        uint32_t word = 0;
+        float back[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float c = v[u][i] == v[u][i] ? fminf(fmaxf(v[u][i], -most), most) : 0.f;
+            const float q = s > 0.f ? fminf(fmaxf(nearest(c, s, inv) + z, 0.f), 15.f) : z;
+            word |= (uint32_t)q << (4 * i);
+            back[i] = s * (q - z);
+        }
+        reinterpret_cast<uint32_t *>(w.codes)[(long)j[u] * (w.k / 8) + k[u] / 8] = word;
+        if (values) store8(values + (long)j[u] * ldv + k[u], back);
+    }
+}
+
+template <typename T, int GROUP>
+static cudaError_t launch_quantize(const T *x, long ldw, const Weight &w, T *values, long ldv, cudaStream_t s) {
+    const int runs = (w.k + Q_RUN - 1) / Q_RUN;
+    const long tasks = (long)w.o * runs, ctas = (tasks + Q_THREADS / 32 * 2 - 1) / (Q_THREADS / 32 * 2);
+    if (ctas > 0x7FFFFFFF) return cudaErrorInvalidValue;
+    const cudaError_t e = w.zeros ? launch_chain(quantize4_kernel<T, GROUP, true>, (unsigned)ctas, Q_THREADS, 0, s, x, ldw, w, values, ldv, runs, tasks)
+                                  : launch_chain(quantize4_kernel<T, GROUP, false>, (unsigned)ctas, Q_THREADS, 0, s, x, ldw, w, values, ldv, runs, tasks);
+    note_launch();
+    return e;
 }
 
 static bool take_weight(const msd_weight4 *w, Weight *out) {
@@ -324,15 +395,15 @@ msd_status msd_quantize4(const void *x, int64_t ldw, int32_t dtype, const msd_we
     if (!take_weight(out, &w) || (dtype != MSD_F32 && dtype != MSD_BF16) || bad_rows(x, ldw, dtype, w.k) ||
         (values && bad_rows(values, ldv, dtype, w.k)))
         return MSD_ERR_INVALID;
-    const long ctas = ((long)w.o * w.groups + 127) / 128;
-    if (ctas > 0x7FFFFFFF) return MSD_ERR_INVALID;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e =
-        dtype == MSD_F32 ? launch_chain(quantize4_kernel<float>, (unsigned)ctas, 128, 0, s, static_cast<const float *>(x), (long)ldw, w, static_cast<float *>(values), (long)ldv)
-                         : launch_chain(quantize4_kernel<bf16>, (unsigned)ctas, 128, 0, s, static_cast<const bf16 *>(x), (long)ldw, w, static_cast<bf16 *>(values), (long)ldv);
-    if (e != cudaSuccess) return MSD_ERR_CUDA;
-    note_launch();
-    return MSD_OK;
+    const auto run = [&](auto *from, auto *to) {
+        return w.group == 128  ? launch_quantize<std::remove_pointer_t<decltype(to)>, 128>(from, (long)ldw, w, to, (long)ldv, s)
+               : w.group == 64 ? launch_quantize<std::remove_pointer_t<decltype(to)>, 64>(from, (long)ldw, w, to, (long)ldv, s)
+                               : launch_quantize<std::remove_pointer_t<decltype(to)>, 32>(from, (long)ldw, w, to, (long)ldv, s);
+    };
+    const cudaError_t e = dtype == MSD_F32 ? run(static_cast<const float *>(x), static_cast<float *>(values))
+                                           : run(static_cast<const bf16 *>(x), static_cast<bf16 *>(values));
+    return e == cudaSuccess ? MSD_OK : MSD_ERR_CUDA;
 }
 
 }  // extern "C"

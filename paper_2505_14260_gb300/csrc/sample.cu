@@ -55,19 +55,26 @@ struct Settings {
     const float *top_p, *min_p;
 };
 
-// What is left of a row.
+// What is left of a row: logits above `end`, and of the ids with just this logit the ones up to `tie`.
 struct Left {
     RowScale scale;
-    unsigned key;             // smallest key in it
-    int tie;                  // of the ids with this key, the ones up to here
+    float end;
+    int tie;
     float2 limit;             // largest exponent (min-p)
     u64 total;                // its weight; 0: nothing is left
+
+    // (NaN and -inf are in no run: it starts at -inf with no id)
+    __device__ __forceinline__ bool has(float x, int id) const { return x > end || (x == end && id <= tie); }
 };
 
+// Weight of a token of a run, without min-p.
+__device__ __forceinline__ u64 weight_in(const RowScale &r, float x, const float2 *table) {
+    return x == r.top ? 1ull << WEIGHT_BITS : weight_of(exponent_of(x, r), table);      // (top may be +inf)
+}
+
 __device__ __forceinline__ u64 weight_left(const Left &l, float x, int id, const float2 *table) {
-    const unsigned k = key_of(x);
-    if (k < l.key || (k == l.key && id > l.tie) || k == 0) return 0;
-    if (x == l.scale.top) return 1ull << WEIGHT_BITS;   // also where it is +inf
+    if (!l.has(x, id)) return 0;
+    if (x == l.scale.top) return 1ull << WEIGHT_BITS;
     const float2 y = exponent_of(x, l.scale);
     if (!((y.x - l.limit.x) + (y.y - l.limit.y) <= 0.f)) return 0;
     return weight_of(y, table);
@@ -76,29 +83,30 @@ __device__ __forceinline__ u64 weight_left(const Left &l, float x, int id, const
 // ---------------------------------------------------------------------------
 // A row over the CTAs of a cluster
 // ---------------------------------------------------------------------------
-struct Found {                // the end of a run, or a bucket
-    unsigned bucket;
-    u64 above;                // weight or count of what comes before the bucket
-};
-
 struct Shared {
     float2 table[EXP_STEPS];
-    unsigned hist[3][BUCKETS];
+    unsigned hist[3][BUCKETS];                  // own: counts, or masses in pieces of 15, 15 and 14 bits
+    u64 all[BUCKETS];                           // of the whole row
     u64 red[WARPS + 1];
-    u64 seg[8];               // of each CTA of the cluster
-    u64 total[8];
-    unsigned top[8], low[8], valid[8];
-    Found found;
-    unsigned list_key[LIST];  // rank 0: tokens of a bucket
-    int list_id[LIST];
-    unsigned list_n, range_lo, range_hi;        // rank 0's list_n; own smallest and largest key
-    unsigned end_key;
-    int end_id;
-    int token;
+    u64 total[8];                               // of each CTA of the cluster
+    float top[8], low[8];
+    unsigned valid[8];
+    u64 above;
+    unsigned bucket;
+    unsigned own_n, list_n, base[8];
+    unsigned range_lo, range_hi;                // keys of the bucket's tokens
+    float end;
+    int tie, token;
     int next, gones, gone[MAX_CHILDREN];
-    u64 kid_w[MAX_CHILDREN];
     u64 left;
+    // where the histogram was, once it is added up: weights of a bucket's tokens, and these, of the slice and of the row
+    __device__ __forceinline__ u64 *list_w() { return reinterpret_cast<u64 *>(hist[0]); }
+    __device__ __forceinline__ float *own_x() { return reinterpret_cast<float *>(hist[1]); }
+    __device__ __forceinline__ int *own_id() { return reinterpret_cast<int *>(hist[1]) + LIST; }
+    __device__ __forceinline__ float *list_x() { return reinterpret_cast<float *>(hist[2]); }
+    __device__ __forceinline__ int *list_id() { return reinterpret_cast<int *>(hist[2]) + LIST; }
 };
+static_assert(2 * LIST <= BUCKETS && sizeof(Shared) + 771 * 512 / 2 + 771 / 2 * 8 + 32 <= 227 * 1024, "the largest slice of 8 fits");
 
 __device__ __forceinline__ uint32_t peer_address(const void *p, int rank) {
     uint32_t a;
@@ -112,14 +120,19 @@ __device__ __forceinline__ void put(unsigned *p, int rank, unsigned v) {
     asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_address(p, rank)), "r"(v) : "memory");
 }
 __device__ __forceinline__ void put(int *p, int rank, int v) { put(reinterpret_cast<unsigned *>(p), rank, (unsigned)v); }
-__device__ __forceinline__ unsigned get(const unsigned *p, int rank) {
-    unsigned v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(peer_address(p, rank)) : "memory");
-    return v;
+__device__ __forceinline__ void put(float *p, int rank, float v) { put(reinterpret_cast<unsigned *>(p), rank, __float_as_uint(v)); }
+__device__ __forceinline__ void add(u64 *p, int rank, u64 v) {
+    asm volatile("red.shared::cluster.add.u64 [%0], %1;" ::"r"(peer_address(p, rank)), "l"(v) : "memory");
 }
-__device__ __forceinline__ unsigned take_slot(unsigned *p, int rank) {
+__device__ __forceinline__ void least(unsigned *p, int rank, unsigned v) {
+    asm volatile("red.shared::cluster.min.u32 [%0], %1;" ::"r"(peer_address(p, rank)), "r"(v) : "memory");
+}
+__device__ __forceinline__ void most(unsigned *p, int rank, unsigned v) {
+    asm volatile("red.shared::cluster.max.u32 [%0], %1;" ::"r"(peer_address(p, rank)), "r"(v) : "memory");
+}
+__device__ __forceinline__ unsigned take(unsigned *p, int rank, unsigned n) {
     unsigned v;
-    asm volatile("atom.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(v) : "r"(peer_address(p, rank)) : "memory");
+    asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(v) : "r"(peer_address(p, rank)), "r"(n) : "memory");
     return v;
 }
 
@@ -158,8 +171,8 @@ struct Row {
     u64 *sums;                // of the slice's blocks
     uint4 *data;              // the slice, -inf around it, in whole blocks
     int first, count, mis, blocks;              // ids of the slice; element `first` is data's element `mis`
-    unsigned top, valid;      // largest key; tokens that have weight
-    float x_low;              // smallest logit of these
+    float top, low;           // largest and smallest logit above -inf
+    unsigned valid;           // how many there are
     float bucket_scale;
 
     __device__ __forceinline__ void sync() const {
@@ -182,13 +195,24 @@ struct Row {
         return sh->red[WARPS];
     }
 
-    // f(logits, first id) for the blocks of this warp, whole warps at a time. Ids around the slice have -inf.
+    // f(logits, first id, block) for the blocks of this warp, whole warps at a time, two blocks in flight. Around the
+    // slice there is -inf.
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
-        for (int b = threadIdx.x >> 5; b < blocks; b += WARPS) {
+        const int lane = threadIdx.x & 31, at = first - mis + lane * E;
+        int b = threadIdx.x >> 5;
+        for (; b + WARPS < blocks; b += 2 * WARPS) {
+            const uint4 v0 = data[b * 32 + lane], v1 = data[(b + WARPS) * 32 + lane];
             float x[E];
-            Vec<T>::get(data[b * 32 + (threadIdx.x & 31)], x);
-            f(x, first - mis + b * BLOCK + (int)(threadIdx.x & 31) * E, b);
+            Vec<T>::get(v0, x);
+            f(x, at + b * BLOCK, b);
+            Vec<T>::get(v1, x);
+            f(x, at + (b + WARPS) * BLOCK, b + WARPS);
+        }
+        if (b < blocks) {
+            float x[E];
+            Vec<T>::get(data[b * 32 + lane], x);
+            f(x, at + b * BLOCK, b);
         }
     }
 
@@ -196,11 +220,15 @@ struct Row {
     __device__ void load() {
         const int tid = threadIdx.x;
         if (ctas > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-        for (int i = tid; i < EXP_STEPS; i += ROW_THREADS) sh->table[i] = make_float2(g_exp_table.hi[i], g_exp_table.lo[i]);
+        for (int i = tid; i < EXP_STEPS; i += ROW_THREADS) {
+            sh->table[i] = make_float2(g_exp_table.hi[i], g_exp_table.lo[i]);
+            sh->all[i] = 0;                                                 // (as many buckets)
+        }
         const T *from = row + first - mis;                                  // 16-byte aligned
         const uint4 *from16 = reinterpret_cast<const uint4 *>(from);
         const int vecs = blocks * 32;
-        unsigned hi = 0, lo = ~0u, n = 0;
+        float hi = -INFINITY, lo = INFINITY;
+        unsigned n = 0;
         constexpr int U = 8;
         for (int v0 = tid; v0 < vecs; v0 += U * ROW_THREADS) {
             uint4 q[U];
@@ -234,25 +262,25 @@ struct Row {
                 Vec<T>::get(q[u], x);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const unsigned k = key_of(x[e]);
-                    hi = max(hi, k);
-                    lo = min(lo, k - 1);                                    // a key of 0 does not count
-                    n += k != 0;
+                    const bool is = x[e] > -INFINITY;
+                    hi = fmaxf(hi, x[e]);                                   // (leaves NaN out)
+                    lo = is ? fminf(lo, x[e]) : lo;
+                    n += is;
                 }
             }
         }
-        hi = __reduce_max_sync(0xffffffffu, hi);
-        lo = __reduce_min_sync(0xffffffffu, lo);
+        hi = warp_max(hi);
+        lo = -warp_max(-lo);
         n = __reduce_add_sync(0xffffffffu, n);
-        unsigned *part = sh->hist[0];
+        float *part = reinterpret_cast<float *>(sh->hist[0]);
         const int warp = tid >> 5;
-        if ((tid & 31) == 0) { part[warp] = hi; part[32 + warp] = lo; part[64 + warp] = n; }
+        if ((tid & 31) == 0) { part[warp] = hi; part[32 + warp] = lo; sh->hist[1][warp] = n; }
         if (ctas > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");     // all CTAs run: their shared memory is there
         __syncthreads();
         if (tid < 32) {
-            hi = __reduce_max_sync(0xffffffffu, tid < WARPS ? part[tid] : 0u);
-            lo = __reduce_min_sync(0xffffffffu, tid < WARPS ? part[32 + tid] : ~0u);
-            n = __reduce_add_sync(0xffffffffu, tid < WARPS ? part[64 + tid] : 0u);
+            hi = warp_max(tid < WARPS ? part[tid] : -INFINITY);
+            lo = -warp_max(tid < WARPS ? -part[32 + tid] : -INFINITY);
+            n = __reduce_add_sync(0xffffffffu, tid < WARPS ? sh->hist[1][tid] : 0u);
             if (tid < ctas) {
                 put(&sh->top[rank], tid, hi);
                 put(&sh->low[rank], tid, lo);
@@ -260,15 +288,14 @@ struct Row {
             }
         }
         sync();
-        top = 0;
-        lo = ~0u;
+        top = -INFINITY;
+        low = INFINITY;
         valid = 0;
         for (int r = 0; r < ctas; ++r) {
-            top = max(top, sh->top[r]);
-            lo = min(lo, sh->low[r]);
+            top = fmaxf(top, sh->top[r]);
+            low = fminf(low, sh->low[r]);
             valid += sh->valid[r];
         }
-        x_low = logit_of(lo + 1);
     }
 
     // Buckets of equal width in the exponent between the largest logit and x_end.
@@ -281,29 +308,31 @@ struct Row {
     }
 
     // Where the run of tokens of `l` ends whose count (mass false) reaches `goal`, or whose weight reaches the share
-    // `p` of theirs (mass true): narrows l.key and l.tie. The bound lies within the run.
+    // `p` of theirs (mass true): narrows l.end and l.tie. The bound lies within the run. Every CTA finds it by itself
+    // from the whole row's histogram and the bucket's tokens, which all are sent.
     __device__ void cut(Left &l, bool mass, u64 goal, float p) {
-        const int tid = threadIdx.x;
-        Left whole = l;                                                     // weights of single tokens
-        whole.key = 1;
-        whole.tie = V;
-        const auto in_run = [&](unsigned k, int id) { return k > l.key || (k == l.key && id <= l.tie && k != 0); };
+        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
         u64 above = 0;
-        unsigned k_lo = l.key, k_hi = top;                                  // keys that the bound lies among
-        int shift = -1;                                                     // -1: buckets of the exponent; else of the key's bits
-        const auto place = [&](float x, unsigned k) { return shift < 0 ? bucket_of(x, l) : (k_hi - k) >> shift; };
+        unsigned k_lo = 0, k_hi = 0;                                        // from the second round on: keys that the bound lies among
+        int shift = -1;                                                     // -1: buckets of the exponent; else of the keys' bits
+        const auto is_in = [&](float x, int id) {
+            if (!l.has(x, id)) return false;
+            if (shift < 0) return true;
+            const unsigned k = key_of(x);
+            return k >= k_lo && k <= k_hi;
+        };
+        const auto place = [&](float x) { return shift < 0 ? bucket_of(x, l) : (k_hi - key_of(x)) >> shift; };
         for (int round = 0;; ++round) {
             for (int i = tid; i < BUCKETS; i += ROW_THREADS) sh->hist[0][i] = sh->hist[1][i] = sh->hist[2][i] = 0;
-            if (tid == 0) { sh->list_n = 0; sh->range_lo = ~0u; sh->range_hi = 0; }
+            if (tid == 0) { sh->own_n = sh->list_n = 0; sh->range_lo = ~0u; sh->range_hi = 0; }
             __syncthreads();
             each([&](const float (&x)[E], int id, int) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const unsigned k = key_of(x[e]);
-                    if (k < k_lo || k > k_hi || !in_run(k, id + e)) continue;
-                    const unsigned b = place(x[e], k);
+                    if (!is_in(x[e], id + e)) continue;
+                    const unsigned b = place(x[e]);
                     if (mass) {
-                        const u64 w = weight_left(whole, x[e], id + e, sh->table);
+                        const u64 w = weight_in(l.scale, x[e], sh->table);
                         atomicAdd(&sh->hist[0][b], (unsigned)w & 0x7FFFu);
                         atomicAdd(&sh->hist[1][b], (unsigned)(w >> 15) & 0x7FFFu);
                         atomicAdd(&sh->hist[2][b], (unsigned)(w >> 30));
@@ -312,111 +341,114 @@ struct Row {
                     }
                 }
             });
-            sync();
-            // this CTA's part of the buckets: BUCKETS / ctas of them, PER a thread
-            const int mine = BUCKETS / ctas, per = (mine + ROW_THREADS - 1) / ROW_THREADS;
-            u64 v[2] = {0, 0};
-            for (int i = 0; i < per; ++i) {
-                const int at = tid * per + i, b = rank * mine + at;
-                if (at < mine)
-                    for (int r = 0; r < ctas; ++r) {
-                        v[i] += get(&sh->hist[0][b], r);
-                        if (mass) v[i] += ((u64)get(&sh->hist[1][b], r) << 15) + ((u64)get(&sh->hist[2][b], r) << 30);
-                    }
+            __syncthreads();
+            for (int i = tid; i < BUCKETS; i += ROW_THREADS) {
+                const u64 v = mass ? sh->hist[0][i] + ((u64)sh->hist[1][i] << 15) + ((u64)sh->hist[2][i] << 30) : sh->hist[0][i];
+                if (v)
+                    for (int r = 0; r < ctas; ++r) add(&sh->all[i], r, v);
             }
-            u64 run = v[0] + v[1];                                          // inclusive over the threads
+            sync();
+            // the bucket that the bound falls into
+            constexpr int PER = BUCKETS / ROW_THREADS;
+            u64 v[PER], run = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                v[i] = sh->all[tid * PER + i];
+                sh->all[tid * PER + i] = 0;                                 // (the next time that it is added to lies behind a sync)
+                run += v[i];
+            }
+            const u64 own = run;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const u64 t = __shfl_up_sync(0xffffffffu, run, o);
-                if ((tid & 31) >= o) run += t;
+                if (lane >= o) run += t;
             }
-            if ((tid & 31) == 31) sh->red[tid >> 5] = run;
+            if (lane == 31) sh->red[warp] = run;
             __syncthreads();
-            for (int i = 0; i < (tid >> 5); ++i) run += sh->red[i];
-            if (tid == ROW_THREADS - 1) tell(&sh->seg[rank], run);
-            sync();
             u64 before = above, all = 0;
-            for (int r = 0; r < ctas; ++r) {
-                if (r < rank) before += sh->seg[r];
-                all += sh->seg[r];
+            for (int i = 0; i < WARPS; ++i) {
+                if (i < warp) before += sh->red[i];
+                all += sh->red[i];
             }
             if (round == 0 && mass) goal = max(share_floor(p, all, true), 1ull);
-            u64 at = before + run - v[0] - v[1];
-            for (int i = 0; i < per; ++i) {
-                if (v[i] && at < goal && goal <= at + v[i])
-                    for (int r = 0; r < ctas; ++r) {
-                        put(&sh->found.bucket, r, (unsigned)(rank * mine + tid * per + i));
-                        put(&sh->found.above, r, at);
-                    }
+            u64 at = before + run - own;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                if (at < goal && goal <= at + v[i]) { sh->bucket = tid * PER + i; sh->above = at; }
                 at += v[i];
             }
-            sync();
-            const unsigned bucket = sh->found.bucket;
-            above = sh->found.above;
-            // the bucket's tokens, and the range of their keys
+            __syncthreads();
+            const unsigned bucket = sh->bucket;
+            above = sh->above;
+            // its tokens, and the range of their keys
             unsigned lo = ~0u, hi = 0;
             each([&](const float (&x)[E], int id, int) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const unsigned k = key_of(x[e]);
-                    if (k < k_lo || k > k_hi || !in_run(k, id + e) || place(x[e], k) != bucket) continue;
+                    if (!is_in(x[e], id + e) || place(x[e]) != bucket) continue;
+                    const unsigned k = key_of(x[e]), slot = atomicAdd(&sh->own_n, 1u);
                     lo = min(lo, k);
                     hi = max(hi, k);
-                    const unsigned slot = take_slot(&sh->list_n, 0);
-                    if (slot < LIST) {
-                        put(&sh->list_key[slot], 0, k);
-                        put(&sh->list_id[slot], 0, id + e);
-                    }
+                    if (slot < LIST) { sh->own_x()[slot] = x[e]; sh->own_id()[slot] = id + e; }
                 }
             });
             lo = __reduce_min_sync(0xffffffffu, lo);
             hi = __reduce_max_sync(0xffffffffu, hi);
-            if ((tid & 31) == 0 && hi) {
+            if (lane == 0 && hi)
+                for (int r = 0; r < ctas; ++r) { least(&sh->range_lo, r, lo); most(&sh->range_hi, r, hi); }
+            __syncthreads();
+            const unsigned own_n = sh->own_n;
+            if (own_n && tid < ctas) sh->base[tid] = take(&sh->list_n, tid, own_n);
+            __syncthreads();
+            for (unsigned i = tid; i < min(own_n, (unsigned)LIST); i += ROW_THREADS)
                 for (int r = 0; r < ctas; ++r) {
-                    asm volatile("red.shared::cluster.min.u32 [%0], %1;" ::"r"(peer_address(&sh->range_lo, r)), "r"(lo) : "memory");
-                    asm volatile("red.shared::cluster.max.u32 [%0], %1;" ::"r"(peer_address(&sh->range_hi, r)), "r"(hi) : "memory");
+                    const unsigned slot = sh->base[r] + i;
+                    if (slot < LIST) {
+                        put(&sh->list_x()[slot], r, sh->own_x()[i]);
+                        put(&sh->list_id()[slot], r, sh->own_id()[i]);
+                    }
                 }
-            }
             sync();
-            const unsigned n = get(&sh->list_n, 0);
+            const unsigned n = sh->list_n;
             k_lo = sh->range_lo;
             k_hi = sh->range_hi;
             if (n <= LIST) {
-                if (rank == 0) {
-                    u64 *w = reinterpret_cast<u64 *>(sh->hist);             // the tokens' weights
-                    for (unsigned i = tid; i < n; i += ROW_THREADS)
-                        w[i] = mass ? weight_left(whole, logit_of(sh->list_key[i]), sh->list_id[i], sh->table) : 1;
-                    __syncthreads();
-                    for (unsigned i = tid; i < n; i += ROW_THREADS) {
-                        const unsigned k = sh->list_key[i];
-                        const int id = sh->list_id[i];
-                        u64 s = above;
-                        for (unsigned j = 0; j < n; ++j) {
-                            const unsigned kj = sh->list_key[j];
-                            if (kj > k || (kj == k && sh->list_id[j] < id)) s += w[j];
-                        }
-                        if (s < goal && goal <= s + w[i]) {
-                            tell(&sh->end_key, k);
-                            tell(&sh->end_id, id);
-                        }
+                // each token's place among them
+                u64 *w = sh->list_w();
+                for (unsigned i = tid; i < n; i += ROW_THREADS) w[i] = mass ? weight_in(l.scale, sh->list_x()[i], sh->table) : 1;
+                __syncthreads();
+                for (unsigned i = tid; i < n; i += ROW_THREADS) {
+                    const float x = sh->list_x()[i];
+                    const int id = sh->list_id()[i];
+                    u64 s = above;
+                    for (unsigned j = 0; j < n; ++j) {
+                        const float xj = sh->list_x()[j];
+                        if (xj > x || (xj == x && sh->list_id()[j] < id)) s += w[j];
                     }
+                    if (s < goal && goal <= s + w[i]) { sh->end = x; sh->tie = id; }
                 }
-                sync();
-                l.key = sh->end_key;
-                l.tie = sh->end_id;
+                __syncthreads();
+                l.end = sh->end;
+                l.tie = sh->tie;
                 return;
             }
             if (k_lo == k_hi) {                                             // equal logits: ids decide
-                const u64 each_w = mass ? max(weight_left(whole, logit_of(k_lo), 0, sh->table), 1ull) : 1;
+                const u64 each_w = mass ? max(weight_in(l.scale, sh->list_x()[0], sh->table), 1ull) : 1;
                 const u64 need = (goal - above + each_w - 1) / each_w;
-                add_up([&](float x, int id) { return (u64)(key_of(x) == k_lo && in_run(k_lo, id)); });
-                const int id = locate(need - 1, [&](float x, int id) { return (u64)(key_of(x) == k_lo && in_run(k_lo, id)); });
-                l.key = k_lo;
-                l.tie = id;
+                const float x_end = sh->list_x()[0];
+                const auto one = [&](float x, int id) { return (u64)(x == x_end && l.has(x, id)); };
+                add_up(one);
+                const int id = locate(need - 1, one);
+                if (id >= 0)
+                    for (int r = 0; r < ctas; ++r) put(&sh->token, r, id);
+                sync();
+                const int found = sh->token;
+                l.end = x_end;
+                l.tie = found;
                 return;
             }
             shift = max(0, 22 - __clz(k_hi - k_lo));                        // (k_hi - k_lo) >> shift < BUCKETS
-            sync();                                                         // all have read the list's length and the range
+            __syncthreads();                                                // all have read the list's length and the range
         }
     }
 
@@ -439,9 +471,11 @@ struct Row {
         return all;
     }
 
-    // After add_up: the smallest id whose cumulative w exceeds `goal`, which is less than the whole.
+    // After add_up: the smallest id whose cumulative w exceeds `goal`, which is less than the whole. One thread of one
+    // CTA gets it, the others -1.
     template <typename W>
     __device__ int locate(u64 goal, W w) {
+        int found = -1;
         u64 before = 0;
         for (int r = 0; r < rank; ++r) before += sh->total[r];
         if (before <= goal && goal < before + sh->total[rank] && threadIdx.x < 32) {
@@ -480,23 +514,23 @@ struct Row {
             u64 c = run - sum;
             if (c <= rest && rest < run)
                 for (int e = 0; e < E; ++e) {
-                    if (rest < c + v[e]) { tell(&sh->token, id + e); break; }
+                    if (rest < c + v[e]) { found = id + e; break; }
                     c += v[e];
                 }
         }
-        sync();
-        return sh->token;
+        return found;
     }
 
-    // What the settings of entry `at` leave.
-    __device__ Left filter(const Settings &f, int at) {
+    // What the settings of entry `at` leave. `single`: a run of one token, which is then l.tie (no sums are made).
+    __device__ Left filter(const Settings &f, int at, bool *single) {
         Left l;
         l.total = 0;
-        l.key = 1;
-        l.tie = V;
+        l.end = -INFINITY;
+        l.tie = -1;
         l.limit = make_float2(INFINITY, 0.f);
-        l.scale = RowScale{logit_of(top), 0.f, 0.f};
-        if (top == 0) return l;
+        l.scale = RowScale{top, 0.f, 0.f};
+        *single = true;
+        if (valid == 0) return l;
         float temp = f.temperature ? f.temperature[at] : 1.f;
         int k = f.top_k ? f.top_k[at] : 0;
         const float p = f.top_p ? f.top_p[at] : 1.f, m = f.min_p ? f.min_p[at] : 0.f;
@@ -507,7 +541,7 @@ struct Row {
         l.scale.c_lo = (float)(c - (double)l.scale.c_hi);
         if (k == 1) {                                                       // the first token alone
             unsigned id = ~0u;
-            const float best = l.scale.top;
+            const float best = top;
             each([&](const float (&x)[E], int first_id, int) {
 #pragma unroll
                 for (int e = E - 1; e >= 0; --e)
@@ -517,19 +551,19 @@ struct Row {
             if (threadIdx.x == 0) sh->range_lo = ~0u;
             sync();
             if ((threadIdx.x & 31) == 0 && id != ~0u)
-                for (int r = 0; r < ctas; ++r)
-                    asm volatile("red.shared::cluster.min.u32 [%0], %1;" ::"r"(peer_address(&sh->range_lo, r)), "r"(id) : "memory");
+                for (int r = 0; r < ctas; ++r) least(&sh->range_lo, r, id);
             sync();
-            l.key = top;
+            l.end = top;
             l.tie = (int)sh->range_lo;
             l.total = 1ull << WEIGHT_BITS;
             return l;
         }
-        float x_end = x_low;
+        *single = false;
+        float x_end = low;
         if (k > 0 && (unsigned)k < valid) {
             spread(l, x_end);
             cut(l, false, (u64)k, 1.f);
-            x_end = logit_of(l.key);
+            x_end = l.end;
         }
         if (p < 1.f) {
             spread(l, x_end);
@@ -576,12 +610,14 @@ sample_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int slice,
     Shared &sh = *reinterpret_cast<Shared *>(smem);
     const int r = blockIdx.x / ctas, rank = blockIdx.x % ctas;
     Row<T> row = open_row(logits + (long)r * ld, V, ctas, rank, slice, &sh, smem + sizeof(Shared));
-    const Left l = row.filter(f, r);
+    bool single;
+    const Left l = row.filter(f, r, &single);
+    // the thread that knows the token writes it
     int t = -1;
-    if (l.key == row.top && row.top) t = l.total == 1ull << WEIGHT_BITS ? l.tie : -1;
-    if (t < 0 && l.total)
-        t = row.locate(share_floor(uniform(u[r]), l.total, false), [&](float x, int id) { return weight_left(l, x, id, sh.table); });
-    if (rank == 0 && threadIdx.x == 0) {
+    const bool speaks = rank == 0 && threadIdx.x == 0;
+    if (single) t = l.tie;
+    else t = row.locate(share_floor(uniform(u[r]), l.total, false), [&](float x, int id) { return weight_left(l, x, id, sh.table); });
+    if (single ? speaks : t >= 0) {
         tokens[r] = t;
         if (logp) {
             const float x = t < 0 ? 0.f : logit_at(row.row, t);
@@ -596,15 +632,13 @@ sample_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int slice,
         for (int i = threadIdx.x; i < row.count; i += ROW_THREADS) {
             const float x = logit_at(data, i);
             float w = 0.f;
-            const unsigned k = key_of(x);
-            if (k > l.key || (k == l.key && row.first + i <= l.tie && k)) {
+            if (l.has(x, row.first + i)) {
                 const float2 y = x == l.scale.top ? make_float2(0.f, 0.f) : exponent_of(x, l.scale);
                 if ((y.x - l.limit.x) + (y.y - l.limit.y) <= 0.f) w = exp2f(-y.x) * (1.f - 0.69314718f * y.y) * scale;
             }
             to[i] = w;
         }
     }
-    if (ctas > 1) row.sync();           // no CTA leaves while another may write to it
 }
 
 // Per node of the trees: the child that is accepted there, or -1 and the token drawn there.
@@ -645,11 +679,13 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
     }
     if (d > a.depth) return;                            // never reached (the whole cluster leaves)
     Row<T> row = open_row(logits + (long)r * ld, V, ctas, rank, slice, &sh, smem + sizeof(Shared));
-    const Left l = row.filter(f, b);
+    bool single;
+    const Left l = row.filter(f, b, &single);
     const float *u = a.u + ((long)b * (a.depth + 1) + d) * (a.children + 1);
     if (rank == 0 && threadIdx.x < 32) {
         // the first `children` children, in index order; their weights; then the decisions one after another
         const int lane = threadIdx.x;
+        u64 *kid_w = sh.all;
         int kids = 0;
         if (d < a.depth)
             for (int j0 = node + 1; j0 < n && kids < a.children; j0 += 32) {
@@ -659,9 +695,9 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
                 const int slot = kids + __popc(all & ((1u << lane) - 1u));
                 if (is && slot < a.children) {
                     const int t = tokens[j];
-                    sh.list_key[slot] = (unsigned)j;
-                    sh.list_id[slot] = t;
-                    sh.kid_w[slot] = t >= 0 && t < V && l.total ? weight_left(l, logit_at(row.row, t), t, sh.table) : 0;
+                    sh.own_id()[slot] = j;
+                    sh.list_id()[slot] = t;
+                    kid_w[slot] = t >= 0 && t < V && l.total ? weight_left(l, logit_at(row.row, t), t, sh.table) : 0;
                 }
                 kids = min(kids + __popc(all), a.children);
             }
@@ -669,13 +705,13 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
         u64 left = l.total;
         int gone = 0, next = -1;
         for (int c = 0; c < kids; ++c) {
-            const int t = sh.list_id[c];
-            u64 w = sh.kid_w[c];
+            const int t = sh.list_id()[c];
+            u64 w = kid_w[c];
             bool again = false;
             for (int i = lane; i < gone; i += 32) again |= sh.gone[i] == t;
             if (__any_sync(0xffffffffu, again)) w = 0;
             if (share_floor(uniform(u[c]), left, false) < w) {
-                next = (int)sh.list_key[c];
+                next = sh.own_id()[c];
                 break;
             }
             if (w) {
@@ -694,40 +730,37 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
             for (int i = lane; i < gone; i += 32) put(&sh.gone[i], p, sh.gone[i]);
     }
     row.sync();
-    int t = -1;
+    if (rank == 0 && threadIdx.x == 0) a.next[r] = sh.next;
+    if (sh.next >= 0) return;
     const int gones = sh.gones;
-    if (sh.next < 0 && sh.left) {
-        if (l.key == row.top && l.total == 1ull << WEIGHT_BITS) {
-            t = l.tie;
-        } else {
-            // the sums without the rejected tokens
-            const auto w = [&](float x, int id) {
-                u64 v = weight_left(l, x, id, sh.table);
-                if (v)
-                    for (int g = 0; g < gones; ++g)
-                        if (sh.gone[g] == id) return 0ull;
-                return v;
-            };
-            if (threadIdx.x == 0 && gones) {
-                u64 less = 0;
-                for (int g = 0; g < gones; ++g) {
-                    const int i = sh.gone[g] - row.first;
-                    if (i < 0 || i >= row.count) continue;
-                    const u64 v = weight_left(l, logit_at(reinterpret_cast<const T *>(row.data), row.mis + i), sh.gone[g], sh.table);
-                    row.sums[(row.mis + i) / Row<T>::BLOCK] -= v;
-                    less += v;
-                }
-                if (less) row.tell(&sh.total[rank], sh.total[rank] - less);
+    const u64 left = sh.left;
+    if (single || left == 0) {
+        if (rank == 0 && threadIdx.x == 0) a.drawn[r] = left ? l.tie : -1;
+        return;
+    }
+    // the sums without the rejected tokens
+    if (gones) {
+        if (threadIdx.x == 0) {
+            u64 less = 0;
+            for (int g = 0; g < gones; ++g) {
+                const int i = sh.gone[g] - row.first;
+                if (i < 0 || i >= row.count) continue;
+                const u64 v = weight_left(l, logit_at(reinterpret_cast<const T *>(row.data), row.mis + i), sh.gone[g], sh.table);
+                row.sums[(row.mis + i) / Row<T>::BLOCK] -= v;
+                less += v;
             }
-            row.sync();
-            t = row.locate(share_floor(uniform(u[a.children]), sh.left, false), w);
+            if (less) row.tell(&sh.total[rank], sh.total[rank] - less);
         }
+        row.sync();
     }
-    if (rank == 0 && threadIdx.x == 0) {
-        a.next[r] = sh.next;
-        a.drawn[r] = t;
-    }
-    if (ctas > 1) row.sync();
+    const int t = row.locate(share_floor(uniform(u[a.children]), left, false), [&](float x, int id) {
+        u64 v = weight_left(l, x, id, sh.table);
+        if (v)
+            for (int g = 0; g < gones; ++g)
+                if (sh.gone[g] == id) v = 0;
+        return v;
+    });
+    if (t >= 0) a.drawn[r] = t;
 }
 
 __global__ void accept_walk_kernel(TreeArgs a) {

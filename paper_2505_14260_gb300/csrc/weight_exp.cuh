@@ -78,14 +78,10 @@ __device__ __forceinline__ unsigned long long weight_of(float2 y, const float2 *
     return ((unsigned long long)top << 22) + (long long)low;
 }
 
-// Orders logits as unsigned numbers; what has no weight is 0, and -0 equals 0.
+// Orders finite and infinite logits as unsigned numbers (-0 as 0).
 __device__ __forceinline__ unsigned key_of(float x) {
     const unsigned b = __float_as_uint(x + 0.f);
-    if (!(x > -INFINITY)) return 0;
     return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ float logit_of(unsigned key) {
-    return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
 }
 
 }  // namespace msd
