@@ -32,9 +32,8 @@ constexpr int MAX_VOCAB = 393216;
 constexpr int MAX_CHILDREN = 256;
 constexpr int MAX_TREE_NODES = 1024;
 
-template <typename T> __device__ __forceinline__ float logit_at(const T *row, int i);
-template <> __device__ __forceinline__ float logit_at<float>(const float *row, int i) { return row[i]; }
-template <> __device__ __forceinline__ float logit_at<bf16>(const bf16 *row, int i) { return __bfloat162float(row[i]); }
+__device__ __forceinline__ float logit_at(const float *row, int i) { return row[i]; }
+__device__ __forceinline__ float logit_at(const bf16 *row, int i) { return __bfloat162float(row[i]); }
 
 // floor(f * z) and ceil(f * z) for f in [0, 1): f is an integer of 24 bits times a power of two.
 __device__ __forceinline__ u64 share_floor(float f, u64 z, bool up) {
@@ -60,7 +59,7 @@ struct Left {
     RowScale scale;
     float end;
     int tie;
-    float2 limit;             // largest exponent (min-p)
+    u64 least;                // smallest weight (min-p)
     u64 total;                // its weight; 0: nothing is left
 
     // (NaN and -inf are in no run: it starts at -inf with no id)
@@ -74,16 +73,17 @@ __device__ __forceinline__ u64 weight_in(const RowScale &r, float x, const float
 
 __device__ __forceinline__ u64 weight_left(const Left &l, float x, int id, const float2 *table) {
     if (!l.has(x, id)) return 0;
-    if (x == l.scale.top) return 1ull << WEIGHT_BITS;
-    const float2 y = exponent_of(x, l.scale);
-    if (!((y.x - l.limit.x) + (y.y - l.limit.y) <= 0.f)) return 0;
-    return weight_of(y, table);
+    const u64 w = weight_in(l.scale, x, table);
+    return w >= l.least ? w : 0;
 }
 
 // ---------------------------------------------------------------------------
 // A row over the CTAs of a cluster
+//
+// The code is kept short (functions that are called, state of the row in shared memory, loops over
+// single elements): with everything inlined and unrolled, warps waited for instructions half of the time.
 // ---------------------------------------------------------------------------
-struct Shared {
+struct __align__(16) Shared {                   // (the sums and the slice lie behind it)
     float2 table[EXP_STEPS];
     unsigned hist[3][BUCKETS];                  // own: counts, or masses in pieces of 15, 15 and 14 bits
     u64 all[BUCKETS];                           // of the whole row
@@ -91,14 +91,15 @@ struct Shared {
     u64 total[8];                               // of each CTA of the cluster
     float top[8], low[8];
     unsigned valid[8];
-    u64 above;
-    unsigned bucket;
-    unsigned own_n, list_n, base[8];
+    u64 above, left;
+    double log_total;
+    unsigned bucket, own_n, list_n, base[8];
     unsigned range_lo, range_hi;                // keys of the bucket's tokens
     float end;
     int tie, token;
     int next, gones, gone[MAX_CHILDREN];
-    u64 left;
+    // the slice: ids [first, first + count), element i of it at data[mis + i], -inf around it, in whole blocks
+    int ctas, rank, first, count, mis, blocks, data_at;
     // where the histogram was, once it is added up: weights of a bucket's tokens, and these, of the slice and of the row
     __device__ __forceinline__ u64 *list_w() { return reinterpret_cast<u64 *>(hist[0]); }
     __device__ __forceinline__ float *own_x() { return reinterpret_cast<float *>(hist[1]); }
@@ -106,7 +107,14 @@ struct Shared {
     __device__ __forceinline__ float *list_x() { return reinterpret_cast<float *>(hist[2]); }
     __device__ __forceinline__ int *list_id() { return reinterpret_cast<int *>(hist[2]) + LIST; }
 };
-static_assert(2 * LIST <= BUCKETS && sizeof(Shared) + 771 * 512 / 2 + 771 / 2 * 8 + 32 <= 227 * 1024, "the largest slice of 8 fits");
+constexpr int BLOCK = 128;                      // ids that have a sum of their own
+
+extern __shared__ __align__(16) uint8_t g_smem[];
+__device__ __forceinline__ Shared &shared() { return *reinterpret_cast<Shared *>(g_smem); }
+__device__ __forceinline__ u64 *block_sums() { return reinterpret_cast<u64 *>(g_smem + sizeof(Shared)); }
+template <typename T> __device__ __forceinline__ T *slice_data() { return reinterpret_cast<T *>(g_smem + shared().data_at); }
+constexpr size_t data_offset(int blocks) { return sizeof(Shared) + (size_t)(blocks * 8 + 15) / 16 * 16; }
+constexpr int most_blocks(int slice, int size) { return (slice + 16 / size + BLOCK - 1) / BLOCK; }
 
 __device__ __forceinline__ uint32_t peer_address(const void *p, int rank) {
     uint32_t a;
@@ -142,463 +150,393 @@ __device__ __forceinline__ u64 warp_total(u64 v) {
     return v;
 }
 
-// 16 bytes of a row.
-template <typename T> struct Vec;
-template <> struct Vec<float> {
-    static constexpr int E = 4;
-    static __device__ __forceinline__ void get(const uint4 &v, float (&x)[4]) {
-        x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
-    }
-};
-template <> struct Vec<bf16> {
-    static constexpr int E = 8;
-    static __device__ __forceinline__ void get(const uint4 &v, float (&x)[8]) {
-        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(u[i] << 16);
-            x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-        }
-    }
+__device__ __forceinline__ void meet() {        // of all threads of the row
+    if (shared().ctas > 1) asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    else __syncthreads();
+}
+template <typename U> __device__ __forceinline__ void tell(U *p, U v) {                    // one thread: to every CTA
+    for (int r = 0; r < shared().ctas; ++r) put(p, r, v);
+}
+
+struct Extent {               // of the row's logits above -inf
+    float top, low;
+    unsigned valid;
 };
 
+// This CTA's slice into shared memory, and the row's extent.
 template <typename T>
-struct Row {
-    static constexpr int E = Vec<T>::E, BLOCK = 32 * E;
-    const T *row;             // in memory
-    int V, ctas, rank;
-    Shared *sh;
-    u64 *sums;                // of the slice's blocks
-    uint4 *data;              // the slice, -inf around it, in whole blocks
-    int first, count, mis, blocks;              // ids of the slice; element `first` is data's element `mis`
-    float top, low;           // largest and smallest logit above -inf
-    unsigned valid;           // how many there are
-    float bucket_scale;
-
-    __device__ __forceinline__ void sync() const {
-        if (ctas > 1) asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-        else __syncthreads();
-    }
-    template <typename U> __device__ __forceinline__ void tell(U *p, U v) const {          // one thread: to every CTA
-        for (int r = 0; r < ctas; ++r) put(p, r, v);
-    }
-    __device__ __forceinline__ u64 block_sum(u64 v) const {
-        v = warp_total(v);
-        __syncthreads();
-        if ((threadIdx.x & 31) == 0) sh->red[threadIdx.x >> 5] = v;
-        __syncthreads();
-        if (threadIdx.x < 32) {
-            const u64 t = warp_total(threadIdx.x < WARPS ? sh->red[threadIdx.x] : 0);
-            if (threadIdx.x == 0) sh->red[WARPS] = t;
-        }
-        __syncthreads();
-        return sh->red[WARPS];
-    }
-
-    // f(logits, first id, block) for the blocks of this warp, whole warps at a time, two blocks in flight. Around the
-    // slice there is -inf.
-    template <typename F>
-    __device__ __forceinline__ void each(F f) const {
-        const int lane = threadIdx.x & 31, at = first - mis + lane * E;
-        int b = threadIdx.x >> 5;
-        for (; b + WARPS < blocks; b += 2 * WARPS) {
-            const uint4 v0 = data[b * 32 + lane], v1 = data[(b + WARPS) * 32 + lane];
-            float x[E];
-            Vec<T>::get(v0, x);
-            f(x, at + b * BLOCK, b);
-            Vec<T>::get(v1, x);
-            f(x, at + (b + WARPS) * BLOCK, b + WARPS);
-        }
-        if (b < blocks) {
-            float x[E];
-            Vec<T>::get(data[b * 32 + lane], x);
-            f(x, at + b * BLOCK, b);
-        }
-    }
-
-    // The slice into shared memory; largest and smallest logit of the row, tokens that have weight.
-    __device__ void load() {
-        const int tid = threadIdx.x;
-        if (ctas > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-        for (int i = tid; i < EXP_STEPS; i += ROW_THREADS) {
-            sh->table[i] = make_float2(g_exp_table.hi[i], g_exp_table.lo[i]);
-            sh->all[i] = 0;                                                 // (as many buckets)
-        }
-        const T *from = row + first - mis;                                  // 16-byte aligned
-        const uint4 *from16 = reinterpret_cast<const uint4 *>(from);
-        const int vecs = blocks * 32;
-        float hi = -INFINITY, lo = INFINITY;
-        unsigned n = 0;
-        constexpr int U = 8;
-        for (int v0 = tid; v0 < vecs; v0 += U * ROW_THREADS) {
-            uint4 q[U];
+__device__ Extent load_row(const T *row, int V, int ctas, int rank, int slice) {
+    constexpr int E = 16 / sizeof(T), U = 4;
+    Shared &sh = shared();
+    const int tid = threadIdx.x, warp = tid >> 5;
+    if (ctas > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    const int first = min(rank * slice, V), count = min(slice, V - first);
+    const int mis = (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T));               // slices are multiples of 16 bytes
+    const int blocks = (mis + count + BLOCK - 1) / BLOCK;
+    const int data_at = (int)data_offset(most_blocks(slice, sizeof(T)));
+    T *const data = reinterpret_cast<T *>(g_smem + data_at);
+    const T *const from = row + first - mis;                                                // 16-byte aligned
+    const int v0 = mis ? 1 : 0, v1 = max((mis + count) / E, v0);                            // whole vectors
+    float hi = -INFINITY, lo = INFINITY;
+    unsigned n = 0;
+    const auto note = [&](float x) {
+        const bool is = x > -INFINITY;
+        hi = fmaxf(hi, x);                                                                  // (leaves NaN out)
+        lo = is ? fminf(lo, x) : lo;
+        n += is;
+    };
+    for (int v = v0 + tid; v < v1; v += U * ROW_THREADS) {
+        uint4 q[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int v = v0 + u * ROW_THREADS, i = v * E;              // first element of the vector
-                if (i >= mis && i + E <= mis + count) {
-                    q[u] = __ldcs(from16 + v);
+        for (int u = 0; u < U; ++u)
+            if (v + u * ROW_THREADS < v1) q[u] = __ldcs(reinterpret_cast<const uint4 *>(from) + v + u * ROW_THREADS);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (v + u * ROW_THREADS >= v1) break;
+            reinterpret_cast<uint4 *>(data)[v + u * ROW_THREADS] = q[u];
+            const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (E == 4) {
+                    note(__uint_as_float(w[e]));
                 } else {
-                    constexpr unsigned NONE = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
-                    q[u] = make_uint4(NONE, NONE, NONE, NONE);
-                    if (v < vecs)
-                        for (int e = 0; e < E; ++e)
-                            if (i + e >= mis && i + e < mis + count) {
-                                if constexpr (sizeof(T) == 4) {
-                                    (&q[u].x)[e] = __float_as_uint(from[i + e]);
-                                } else {
-                                    const unsigned b = __bfloat16_as_ushort(from[i + e]);
-                                    unsigned &w = (&q[u].x)[e >> 1];
-                                    w = e & 1 ? (w & 0xFFFFu) | b << 16 : (w & 0xFFFF0000u) | b;
-                                }
-                            }
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int v = v0 + u * ROW_THREADS;
-                if (v >= vecs) break;
-                data[v] = q[u];
-                float x[E];
-                Vec<T>::get(q[u], x);
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const bool is = x[e] > -INFINITY;
-                    hi = fmaxf(hi, x[e]);                                   // (leaves NaN out)
-                    lo = is ? fminf(lo, x[e]) : lo;
-                    n += is;
+                    note(__uint_as_float(w[e] << 16));
+                    note(__uint_as_float(w[e] & 0xFFFF0000u));
                 }
             }
         }
-        hi = warp_max(hi);
-        lo = -warp_max(-lo);
-        n = __reduce_add_sync(0xffffffffu, n);
-        float *part = reinterpret_cast<float *>(sh->hist[0]);
-        const int warp = tid >> 5;
-        if ((tid & 31) == 0) { part[warp] = hi; part[32 + warp] = lo; sh->hist[1][warp] = n; }
-        if (ctas > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");     // all CTAs run: their shared memory is there
+    }
+    // the edges: elements before the first whole vector and behind the last one
+    for (int i = tid; i < v0 * E + blocks * BLOCK - v1 * E; i += ROW_THREADS) {
+        const int at = i < v0 * E ? i : i - v0 * E + v1 * E;
+        const bool is = at >= mis && at < mis + count;
+        const float x = is ? logit_at(from, at) : -INFINITY;
+        data[at] = (T)x;
+        note(x);
+    }
+    reinterpret_cast<uint4 *>(sh.table)[tid] = reinterpret_cast<const uint4 *>(g_exp_table.pair)[tid];
+    static_assert(EXP_STEPS * 8 == ROW_THREADS * 16, "");
+    for (int i = tid; i < BUCKETS; i += ROW_THREADS) sh.all[i] = 0;
+    if (tid == 0) {
+        sh.ctas = ctas; sh.rank = rank; sh.first = first; sh.count = count; sh.mis = mis; sh.blocks = blocks; sh.data_at = data_at;
+    }
+    hi = warp_max(hi);
+    lo = -warp_max(-lo);
+    n = __reduce_add_sync(0xffffffffu, n);
+    float *part = reinterpret_cast<float *>(sh.hist[0]);
+    if ((tid & 31) == 0) { part[warp] = hi; part[32 + warp] = lo; sh.hist[1][warp] = n; }
+    if (ctas > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");               // all CTAs run: their shared memory is there
+    __syncthreads();
+    if (tid < 32) {
+        hi = warp_max(tid < WARPS ? part[tid] : -INFINITY);
+        lo = -warp_max(tid < WARPS ? -part[32 + tid] : -INFINITY);
+        n = __reduce_add_sync(0xffffffffu, tid < WARPS ? sh.hist[1][tid] : 0u);
+        if (tid < ctas) {
+            put(&sh.top[rank], tid, hi);
+            put(&sh.low[rank], tid, lo);
+            put(&sh.valid[rank], tid, n);
+        }
+    }
+    meet();
+    Extent e{-INFINITY, INFINITY, 0};
+    for (int r = 0; r < ctas; ++r) {
+        e.top = fmaxf(e.top, sh.top[r]);
+        e.low = fminf(e.low, sh.low[r]);
+        e.valid += sh.valid[r];
+    }
+    return e;
+}
+
+// What a token counts for: its weight, or, to count equal logits, 1 for the ids of `l` that have just l.end.
+__device__ __forceinline__ u64 value_of(const Left &l, bool ties, float x, int id, const float2 *table) {
+    return ties ? (u64)(x == l.end && id <= l.tie) : weight_left(l, x, id, table);
+}
+
+// Sums of value_of over each block, this CTA's, and all (returned).
+template <typename T>
+__device__ __noinline__ u64 add_up(const Left l, bool ties) {
+    Shared &sh = shared();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, id0 = sh.first - sh.mis + lane, blocks = sh.blocks;
+    const T *data = slice_data<T>() + lane;
+    u64 sum = 0;
+    for (int b = warp; b < blocks; b += WARPS) {
+        u64 v = 0;
+#pragma unroll 1
+        for (int i = b * BLOCK; i < (b + 1) * BLOCK; i += 32) {
+            const float x = logit_at(data, i);
+            if (l.has(x, id0 + i)) v += value_of(l, ties, x, id0 + i, sh.table);
+        }
+        if (__any_sync(0xffffffffu, v != 0)) v = warp_total(v);
+        if (lane == 0) block_sums()[b] = v;
+        sum += v;
+    }
+    __syncthreads();
+    if (lane == 0) sh.red[warp] = sum;
+    __syncthreads();
+    if (warp == 0) {
+        sum = warp_total(lane < WARPS ? sh.red[lane] : 0);
+        if (lane < sh.ctas) put(&sh.total[sh.rank], lane, sum);
+    }
+    meet();
+    u64 all = 0;
+    for (int r = 0; r < sh.ctas; ++r) all += sh.total[r];
+    return all;
+}
+
+// After add_up: the smallest id whose cumulative value exceeds `goal`, which is less than the whole; tokens
+// gone[0 .. gones) count for nothing. One thread of one CTA gets it, the others -1.
+template <typename T>
+__device__ __noinline__ int locate(const Left l, bool ties, u64 goal, int gones) {
+    Shared &sh = shared();
+    u64 rest = goal;
+    for (int r = 0; r < sh.rank; ++r) {
+        if (rest < sh.total[r]) return -1;
+        rest -= sh.total[r];
+    }
+    if (rest >= sh.total[sh.rank] || threadIdx.x >= 32) return -1;
+    const int lane = threadIdx.x, blocks = sh.blocks;
+    const auto scan = [&](u64 v) {
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const u64 t = __shfl_up_sync(0xffffffffu, v, o);
+            if (lane >= o) v += t;
+        }
+        return v;
+    };
+    int b = 0;
+    for (int b0 = 0; b0 < blocks; b0 += 32) {                               // the 32 blocks, then the one
+        const u64 own = b0 + lane < blocks ? block_sums()[b0 + lane] : 0, in = scan(own);
+        const unsigned over = __ballot_sync(0xffffffffu, in > rest);
+        if (over) {
+            const int at = __ffs(over) - 1;
+            rest -= __shfl_sync(0xffffffffu, in - own, at);
+            b = b0 + at;
+            break;
+        }
+        rest -= __shfl_sync(0xffffffffu, in, 31);
+    }
+    const int id0 = sh.first - sh.mis + lane;
+#pragma unroll 1
+    for (int i = b * BLOCK; i < (b + 1) * BLOCK; i += 32) {
+        const float x = logit_at(slice_data<T>(), i + lane);
+        u64 own = value_of(l, ties, x, id0 + i, sh.table);
+        if (own)
+            for (int g = 0; g < gones; ++g)
+                if (sh.gone[g] == id0 + i) own = 0;
+        const u64 in = scan(own);
+        const unsigned over = __ballot_sync(0xffffffffu, in > rest);
+        if (over) return __ffs(over) - 1 == lane ? id0 + i : -1;
+        rest -= __shfl_sync(0xffffffffu, in, 31);
+    }
+    return -1;
+}
+
+// Where the run of tokens of `l` ends whose count (mass false) reaches `goal`, or whose weight reaches the share `p` of
+// theirs (mass true): a narrower l. The bound lies within the run; x_end is its smallest logit. Every CTA finds it by itself from
+// the whole row's histogram and the bucket's tokens, which all are sent.
+template <typename T>
+__device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_end) {
+    Shared &sh = shared();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, ctas = sh.ctas;
+    const int id0 = sh.first - sh.mis, n_all = sh.blocks * BLOCK;
+    const T *data = slice_data<T>();
+    // buckets of equal width in the exponent between the largest logit and x_end; from the second round on, of the keys' bits
+    const float y_end = fminf((l.scale.top - x_end) * l.scale.c_hi, Y_MOST);
+    const float scale = y_end > 0.f ? (float)(BUCKETS - 1) / y_end * l.scale.c_hi : 0.f;
+    u64 above = 0;
+    unsigned k_lo = 0, k_hi = ~0u;
+    int shift = -1;
+    const auto place = [&](float x, int id) -> unsigned {                   // BUCKETS: not one of them
+        if (!l.has(x, id)) return BUCKETS;
+        if (shift < 0) return x == l.scale.top ? 0u : (unsigned)__float2int_rz(fminf((l.scale.top - x) * scale, (float)(BUCKETS - 1)));
+        const unsigned k = key_of(x);
+        return k >= k_lo && k <= k_hi ? (k_hi - k) >> shift : BUCKETS;
+    };
+    for (int round = 0;; ++round) {
+        for (int i = tid; i < BUCKETS; i += ROW_THREADS) sh.hist[0][i] = sh.hist[1][i] = sh.hist[2][i] = 0;
+        if (tid == 0) { sh.own_n = sh.list_n = 0; sh.range_lo = ~0u; sh.range_hi = 0; }
         __syncthreads();
-        if (tid < 32) {
-            hi = warp_max(tid < WARPS ? part[tid] : -INFINITY);
-            lo = -warp_max(tid < WARPS ? -part[32 + tid] : -INFINITY);
-            n = __reduce_add_sync(0xffffffffu, tid < WARPS ? sh->hist[1][tid] : 0u);
-            if (tid < ctas) {
-                put(&sh->top[rank], tid, hi);
-                put(&sh->low[rank], tid, lo);
-                put(&sh->valid[rank], tid, n);
+        if (mass) {
+#pragma unroll 1
+            for (int i = tid; i < n_all; i += ROW_THREADS) {
+                const float x = logit_at(data, i);
+                const unsigned b = place(x, id0 + i);
+                if (b == BUCKETS) continue;
+                const u64 w = weight_in(l.scale, x, sh.table);
+                atomicAdd(&sh.hist[0][b], (unsigned)w & 0x7FFFu);
+                atomicAdd(&sh.hist[1][b], (unsigned)(w >> 15) & 0x7FFFu);
+                atomicAdd(&sh.hist[2][b], (unsigned)(w >> 30));
+            }
+        } else {
+#pragma unroll 2
+            for (int i = tid; i < n_all; i += ROW_THREADS) {
+                const unsigned b = place(logit_at(data, i), id0 + i);
+                if (b != BUCKETS) atomicAdd(&sh.hist[0][b], 1u);
             }
         }
-        sync();
-        top = -INFINITY;
-        low = INFINITY;
-        valid = 0;
-        for (int r = 0; r < ctas; ++r) {
-            top = fmaxf(top, sh->top[r]);
-            low = fminf(low, sh->low[r]);
-            valid += sh->valid[r];
+        __syncthreads();
+        for (int i = tid; i < BUCKETS; i += ROW_THREADS) {
+            const u64 v = mass ? sh.hist[0][i] + ((u64)sh.hist[1][i] << 15) + ((u64)sh.hist[2][i] << 30) : sh.hist[0][i];
+            if (ctas == 1) sh.all[i] = v;
+            else if (v)
+                for (int r = 0; r < ctas; ++r) add(&sh.all[i], r, v);
         }
-    }
-
-    // Buckets of equal width in the exponent between the largest logit and x_end.
-    __device__ __forceinline__ void spread(const Left &l, float x_end) {
-        const float y = fminf((l.scale.top - x_end) * l.scale.c_hi, Y_MOST);
-        bucket_scale = y > 0.f ? (float)(BUCKETS - 1) / y * l.scale.c_hi : 0.f;
-    }
-    __device__ __forceinline__ unsigned bucket_of(float x, const Left &l) const {
-        return x == l.scale.top ? 0u : (unsigned)__float2int_rz(fminf((l.scale.top - x) * bucket_scale, (float)(BUCKETS - 1)));
-    }
-
-    // Where the run of tokens of `l` ends whose count (mass false) reaches `goal`, or whose weight reaches the share
-    // `p` of theirs (mass true): narrows l.end and l.tie. The bound lies within the run. Every CTA finds it by itself
-    // from the whole row's histogram and the bucket's tokens, which all are sent.
-    __device__ void cut(Left &l, bool mass, u64 goal, float p) {
-        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-        u64 above = 0;
-        unsigned k_lo = 0, k_hi = 0;                                        // from the second round on: keys that the bound lies among
-        int shift = -1;                                                     // -1: buckets of the exponent; else of the keys' bits
-        const auto is_in = [&](float x, int id) {
-            if (!l.has(x, id)) return false;
-            if (shift < 0) return true;
-            const unsigned k = key_of(x);
-            return k >= k_lo && k <= k_hi;
-        };
-        const auto place = [&](float x) { return shift < 0 ? bucket_of(x, l) : (k_hi - key_of(x)) >> shift; };
-        for (int round = 0;; ++round) {
-            for (int i = tid; i < BUCKETS; i += ROW_THREADS) sh->hist[0][i] = sh->hist[1][i] = sh->hist[2][i] = 0;
-            if (tid == 0) { sh->own_n = sh->list_n = 0; sh->range_lo = ~0u; sh->range_hi = 0; }
-            __syncthreads();
-            each([&](const float (&x)[E], int id, int) {
+        meet();
+        // the bucket that the bound falls into
+        constexpr int PER = BUCKETS / ROW_THREADS;
+        u64 v[PER], run = 0;
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    if (!is_in(x[e], id + e)) continue;
-                    const unsigned b = place(x[e]);
-                    if (mass) {
-                        const u64 w = weight_in(l.scale, x[e], sh->table);
-                        atomicAdd(&sh->hist[0][b], (unsigned)w & 0x7FFFu);
-                        atomicAdd(&sh->hist[1][b], (unsigned)(w >> 15) & 0x7FFFu);
-                        atomicAdd(&sh->hist[2][b], (unsigned)(w >> 30));
-                    } else {
-                        atomicAdd(&sh->hist[0][b], 1u);
-                    }
+        for (int i = 0; i < PER; ++i) {
+            v[i] = sh.all[tid * PER + i];
+            sh.all[tid * PER + i] = 0;                                      // (the next time that it is added to lies behind a meeting)
+            run += v[i];
+        }
+        const u64 own = run;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const u64 t = __shfl_up_sync(0xffffffffu, run, o);
+            if (lane >= o) run += t;
+        }
+        if (lane == 31) sh.red[warp] = run;
+        __syncthreads();
+        u64 before = above, all = 0;
+#pragma unroll 4
+        for (int i = 0; i < WARPS; ++i) {
+            if (i < warp) before += sh.red[i];
+            all += sh.red[i];
+        }
+        if (round == 0 && mass) goal = max(share_floor(p, all, true), 1ull);
+        u64 at = before + run - own;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (at < goal && goal <= at + v[i]) { sh.bucket = tid * PER + i; sh.above = at; }
+            at += v[i];
+        }
+        __syncthreads();
+        const unsigned bucket = sh.bucket;
+        above = sh.above;
+        // its tokens, and the range of their keys
+        unsigned lo = ~0u, hi = 0;
+#pragma unroll 2
+        for (int i = tid; i < n_all; i += ROW_THREADS) {
+            const float x = logit_at(data, i);
+            if (place(x, id0 + i) != bucket) continue;
+            const unsigned k = key_of(x), slot = atomicAdd(&sh.own_n, 1u);
+            lo = min(lo, k);
+            hi = max(hi, k);
+            if (slot < LIST) { sh.own_x()[slot] = x; sh.own_id()[slot] = id0 + i; }
+        }
+        lo = __reduce_min_sync(0xffffffffu, lo);
+        hi = __reduce_max_sync(0xffffffffu, hi);
+        if (hi && lane < ctas) { least(&sh.range_lo, lane, lo); most(&sh.range_hi, lane, hi); }
+        __syncthreads();
+        const unsigned own_n = sh.own_n;
+        if (own_n && tid < ctas) sh.base[tid] = take(&sh.list_n, tid, own_n);
+        __syncthreads();
+        for (unsigned i = tid; i < min(own_n, (unsigned)LIST); i += ROW_THREADS)
+            for (int r = 0; r < ctas; ++r) {
+                const unsigned slot = sh.base[r] + i;
+                if (slot < LIST) {
+                    put(&sh.list_x()[slot], r, sh.own_x()[i]);
+                    put(&sh.list_id()[slot], r, sh.own_id()[i]);
                 }
-            });
-            __syncthreads();
-            for (int i = tid; i < BUCKETS; i += ROW_THREADS) {
-                const u64 v = mass ? sh->hist[0][i] + ((u64)sh->hist[1][i] << 15) + ((u64)sh->hist[2][i] << 30) : sh->hist[0][i];
-                if (v)
-                    for (int r = 0; r < ctas; ++r) add(&sh->all[i], r, v);
             }
-            sync();
-            // the bucket that the bound falls into
-            constexpr int PER = BUCKETS / ROW_THREADS;
-            u64 v[PER], run = 0;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                v[i] = sh->all[tid * PER + i];
-                sh->all[tid * PER + i] = 0;                                 // (the next time that it is added to lies behind a sync)
-                run += v[i];
-            }
-            const u64 own = run;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const u64 t = __shfl_up_sync(0xffffffffu, run, o);
-                if (lane >= o) run += t;
-            }
-            if (lane == 31) sh->red[warp] = run;
-            __syncthreads();
-            u64 before = above, all = 0;
-            for (int i = 0; i < WARPS; ++i) {
-                if (i < warp) before += sh->red[i];
-                all += sh->red[i];
-            }
-            if (round == 0 && mass) goal = max(share_floor(p, all, true), 1ull);
-            u64 at = before + run - own;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                if (at < goal && goal <= at + v[i]) { sh->bucket = tid * PER + i; sh->above = at; }
-                at += v[i];
-            }
-            __syncthreads();
-            const unsigned bucket = sh->bucket;
-            above = sh->above;
-            // its tokens, and the range of their keys
-            unsigned lo = ~0u, hi = 0;
-            each([&](const float (&x)[E], int id, int) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    if (!is_in(x[e], id + e) || place(x[e]) != bucket) continue;
-                    const unsigned k = key_of(x[e]), slot = atomicAdd(&sh->own_n, 1u);
-                    lo = min(lo, k);
-                    hi = max(hi, k);
-                    if (slot < LIST) { sh->own_x()[slot] = x[e]; sh->own_id()[slot] = id + e; }
-                }
-            });
-            lo = __reduce_min_sync(0xffffffffu, lo);
-            hi = __reduce_max_sync(0xffffffffu, hi);
-            if (lane == 0 && hi)
-                for (int r = 0; r < ctas; ++r) { least(&sh->range_lo, r, lo); most(&sh->range_hi, r, hi); }
-            __syncthreads();
-            const unsigned own_n = sh->own_n;
-            if (own_n && tid < ctas) sh->base[tid] = take(&sh->list_n, tid, own_n);
-            __syncthreads();
-            for (unsigned i = tid; i < min(own_n, (unsigned)LIST); i += ROW_THREADS)
-                for (int r = 0; r < ctas; ++r) {
-                    const unsigned slot = sh->base[r] + i;
-                    if (slot < LIST) {
-                        put(&sh->list_x()[slot], r, sh->own_x()[i]);
-                        put(&sh->list_id()[slot], r, sh->own_id()[i]);
-                    }
-                }
-            sync();
-            const unsigned n = sh->list_n;
-            k_lo = sh->range_lo;
-            k_hi = sh->range_hi;
-            if (n <= LIST) {
-                // each token's place among them
-                u64 *w = sh->list_w();
-                for (unsigned i = tid; i < n; i += ROW_THREADS) w[i] = mass ? weight_in(l.scale, sh->list_x()[i], sh->table) : 1;
-                __syncthreads();
-                for (unsigned i = tid; i < n; i += ROW_THREADS) {
-                    const float x = sh->list_x()[i];
-                    const int id = sh->list_id()[i];
-                    u64 s = above;
-                    for (unsigned j = 0; j < n; ++j) {
-                        const float xj = sh->list_x()[j];
-                        if (xj > x || (xj == x && sh->list_id()[j] < id)) s += w[j];
-                    }
-                    if (s < goal && goal <= s + w[i]) { sh->end = x; sh->tie = id; }
-                }
-                __syncthreads();
-                l.end = sh->end;
-                l.tie = sh->tie;
-                return;
-            }
-            if (k_lo == k_hi) {                                             // equal logits: ids decide
-                const u64 each_w = mass ? max(weight_in(l.scale, sh->list_x()[0], sh->table), 1ull) : 1;
-                const u64 need = (goal - above + each_w - 1) / each_w;
-                const float x_end = sh->list_x()[0];
-                const auto one = [&](float x, int id) { return (u64)(x == x_end && l.has(x, id)); };
-                add_up(one);
-                const int id = locate(need - 1, one);
-                if (id >= 0)
-                    for (int r = 0; r < ctas; ++r) put(&sh->token, r, id);
-                sync();
-                const int found = sh->token;
-                l.end = x_end;
-                l.tie = found;
-                return;
-            }
+        meet();
+        const unsigned n = sh.list_n;
+        k_lo = sh.range_lo;
+        k_hi = sh.range_hi;
+        const bool few = n <= LIST;
+        if (!few && k_lo != k_hi) {
             shift = max(0, 22 - __clz(k_hi - k_lo));                        // (k_hi - k_lo) >> shift < BUCKETS
             __syncthreads();                                                // all have read the list's length and the range
+            continue;
         }
-    }
-
-    // Sums of w(logit, id) over each block, this CTA's, and all.
-    template <typename W>
-    __device__ u64 add_up(W w) {
-        u64 sum = 0;
-        each([&](const float (&x)[E], int id, int b) {
-            u64 v = 0;
-#pragma unroll
-            for (int e = 0; e < E; ++e) v += w(x[e], id + e);
-            if (__any_sync(0xffffffffu, v != 0)) v = warp_total(v);
-            if ((threadIdx.x & 31) == 0) { sums[b] = v; sum += v; }
-        });
-        sum = block_sum(sum);
-        if (threadIdx.x == 0) tell(&sh->total[rank], sum);
-        sync();
-        u64 all = 0;
-        for (int r = 0; r < ctas; ++r) all += sh->total[r];
-        return all;
-    }
-
-    // After add_up: the smallest id whose cumulative w exceeds `goal`, which is less than the whole. One thread of one
-    // CTA gets it, the others -1.
-    template <typename W>
-    __device__ int locate(u64 goal, W w) {
-        int found = -1;
-        u64 before = 0;
-        for (int r = 0; r < rank; ++r) before += sh->total[r];
-        if (before <= goal && goal < before + sh->total[rank] && threadIdx.x < 32) {
-            const int lane = threadIdx.x;
-            u64 rest = goal - before;
-            int b0 = 0;
-            u64 in = 0;
-            for (;; b0 += 32) {                                             // the 32 blocks, then the one
-                in = b0 + lane < blocks ? sums[b0 + lane] : 0;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const u64 t = __shfl_up_sync(0xffffffffu, in, o);
-                    if (lane >= o) in += t;
+        u64 *w = sh.list_w();
+        for (unsigned i = tid; i < (few ? n : 1u); i += ROW_THREADS) w[i] = mass ? max(weight_in(l.scale, sh.list_x()[i], sh.table), 1ull) : 1;
+        __syncthreads();
+        if (few) {                                                          // each token's place among them
+            for (unsigned i = tid; i < n; i += ROW_THREADS) {
+                const float x = sh.list_x()[i];
+                const int id = sh.list_id()[i];
+                u64 s = above;
+#pragma unroll 2
+                for (unsigned j = 0; j < n; ++j) {
+                    const float xj = sh.list_x()[j];
+                    if (xj > x || (xj == x && sh.list_id()[j] < id)) s += w[j];
                 }
-                const u64 all = __shfl_sync(0xffffffffu, in, 31);
-                if (rest < all || b0 + 32 >= blocks) break;
-                rest -= all;
+                if (s < goal && goal <= s + w[i]) { sh.end = x; sh.tie = id; }
             }
-            const unsigned over = __ballot_sync(0xffffffffu, in > rest);
-            const int at = over ? __ffs(over) - 1 : 31;
-            const u64 less = __shfl_sync(0xffffffffu, in, max(at - 1, 0));
-            if (at > 0) rest -= less;
-            const int b = b0 + at;
-            float x[E];
-            Vec<T>::get(data[b * 32 + lane], x);
-            const int id = first - mis + b * BLOCK + lane * E;
-            u64 v[E], sum = 0;
-#pragma unroll
-            for (int e = 0; e < E; ++e) { v[e] = w(x[e], id + e); sum += v[e]; }
-            u64 run = sum;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const u64 t = __shfl_up_sync(0xffffffffu, run, o);
-                if (lane >= o) run += t;
+        } else {                                                            // equal logits: ids decide
+            const u64 need = (goal - above + w[0] - 1) / w[0];
+            const float x = sh.list_x()[0];
+            if (l.end < x) l.tie = 0x7FFFFFFF;
+            l.end = x;
+            add_up<T>(l, true);
+            const int id = locate<T>(l, true, need - 1, 0);
+            if (id >= 0) {
+                tell(&sh.end, x);
+                tell(&sh.tie, id);
             }
-            u64 c = run - sum;
-            if (c <= rest && rest < run)
-                for (int e = 0; e < E; ++e) {
-                    if (rest < c + v[e]) { found = id + e; break; }
-                    c += v[e];
-                }
+            meet();
         }
-        return found;
-    }
-
-    // What the settings of entry `at` leave. `single`: a run of one token, which is then l.tie (no sums are made).
-    __device__ Left filter(const Settings &f, int at, bool *single) {
-        Left l;
-        l.total = 0;
-        l.end = -INFINITY;
-        l.tie = -1;
-        l.limit = make_float2(INFINITY, 0.f);
-        l.scale = RowScale{top, 0.f, 0.f};
-        *single = true;
-        if (valid == 0) return l;
-        float temp = f.temperature ? f.temperature[at] : 1.f;
-        int k = f.top_k ? f.top_k[at] : 0;
-        const float p = f.top_p ? f.top_p[at] : 1.f, m = f.min_p ? f.min_p[at] : 0.f;
-        if (!(temp >= 0x1p-100f) || m > 1.f || p <= 0.f) k = 1;
-        temp = temp > 0.f ? fminf(fmaxf(temp, 0x1p-100f), 0x1p100f) : 1.f;
-        const double c = 1.4426950408889634074 / (double)temp;
-        l.scale.c_hi = (float)c;
-        l.scale.c_lo = (float)(c - (double)l.scale.c_hi);
-        if (k == 1) {                                                       // the first token alone
-            unsigned id = ~0u;
-            const float best = top;
-            each([&](const float (&x)[E], int first_id, int) {
-#pragma unroll
-                for (int e = E - 1; e >= 0; --e)
-                    if (x[e] == best) id = min(id, (unsigned)(first_id + e));
-            });
-            id = __reduce_min_sync(0xffffffffu, id);
-            if (threadIdx.x == 0) sh->range_lo = ~0u;
-            sync();
-            if ((threadIdx.x & 31) == 0 && id != ~0u)
-                for (int r = 0; r < ctas; ++r) least(&sh->range_lo, r, id);
-            sync();
-            l.end = top;
-            l.tie = (int)sh->range_lo;
-            l.total = 1ull << WEIGHT_BITS;
-            return l;
-        }
-        *single = false;
-        float x_end = low;
-        if (k > 0 && (unsigned)k < valid) {
-            spread(l, x_end);
-            cut(l, false, (u64)k, 1.f);
-            x_end = l.end;
-        }
-        if (p < 1.f) {
-            spread(l, x_end);
-            cut(l, true, 0, p);
-        }
-        if (m > 0.f) {
-            const double y = -log2((double)fminf(m, 1.f));
-            l.limit.x = (float)y;
-            l.limit.y = (float)(y - (double)l.limit.x);
-        }
-        l.total = add_up([&](float x, int id) { return weight_left(l, x, id, sh->table); });
+        __syncthreads();
+        l.end = sh.end;
+        l.tie = sh.tie;
         return l;
     }
-};
+}
+
+// What the settings of entry `at` leave. `single`: a run of one token, which is then l.tie (no sums are made).
+template <typename T>
+__device__ __forceinline__ Left filter_row(const Extent &e, const Settings &f, int at, bool *single) {
+    Shared &sh = shared();
+    Left l;
+    l.total = 0;
+    l.end = -INFINITY;
+    l.tie = -1;
+    l.least = 0;
+    l.scale = RowScale{e.top, 0.f, 0.f};
+    *single = true;
+    if (e.valid == 0) return l;
+    float temp = f.temperature ? f.temperature[at] : 1.f;
+    int k = f.top_k ? f.top_k[at] : 0;
+    const float p = f.top_p ? f.top_p[at] : 1.f, m = f.min_p ? f.min_p[at] : 0.f;
+    if (!(temp >= 0x1p-100f) || m > 1.f || p <= 0.f) k = 1;
+    temp = temp > 0.f ? fminf(fmaxf(temp, 0x1p-100f), 0x1p100f) : 1.f;
+    // log2(e) / temp as a pair (the remainder of the division is exact): fp64, a few lanes a cycle, took 3 us here
+    constexpr float LOG2E = 1.44269504088896340736f, LOG2E_LO = (float)(1.44269504088896340736 - (double)1.44269504088896340736f);
+    l.scale.c_hi = __fdiv_rn(LOG2E, temp);
+    l.scale.c_lo = __fdiv_rn(fmaf(-l.scale.c_hi, temp, LOG2E) + LOG2E_LO, temp);
+    if (k == 1) {                                                           // the first token alone
+        const T *data = slice_data<T>();
+        unsigned id = ~0u;
+        for (int i = threadIdx.x; i < sh.blocks * BLOCK; i += ROW_THREADS)
+            if (logit_at(data, i) == e.top) id = min(id, (unsigned)(sh.first - sh.mis + i));
+        id = __reduce_min_sync(0xffffffffu, id);
+        if (threadIdx.x == 0) sh.range_lo = ~0u;
+        meet();
+        const int lane = threadIdx.x & 31;
+        if (lane < sh.ctas && id != ~0u) least(&sh.range_lo, lane, id);
+        meet();
+        l.end = e.top;
+        l.tie = (int)sh.range_lo;
+        l.total = 1ull << WEIGHT_BITS;
+        return l;
+    }
+    *single = false;
+    float x_end = e.low;
+#pragma unroll 1
+    for (int by = 0; by < 2; ++by) {                                        // top-k, then top-p
+        if (by == 0 ? k <= 0 || (unsigned)k >= e.valid : !(p < 1.f)) continue;
+        l = cut<T>(l, by == 1, (u64)k, p, x_end);
+        x_end = l.end;
+    }
+    if (m > 0.f) l.least = m < 1.f ? share_floor(m, 1ull << WEIGHT_BITS, true) : 1ull << WEIGHT_BITS;
+    l.total = add_up<T>(l, false);
+    return l;
+}
 
 __device__ __forceinline__ float uniform(float u) { return fminf(u > 0.f ? u : 0.f, 0x1.fffffep-1f); }
-
-template <typename T>
-__device__ __forceinline__ Row<T> open_row(const T *row, int V, int ctas, int rank, int slice, Shared *sh, uint8_t *behind) {
-    Row<T> r;
-    r.row = row;
-    r.V = V;
-    r.ctas = ctas;
-    r.rank = rank;
-    r.sh = sh;
-    r.first = min(rank * slice, V);
-    r.count = min(slice, V - r.first);
-    r.mis = (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T));       // slices are multiples of 16 bytes
-    r.blocks = (r.mis + r.count + Row<T>::BLOCK - 1) / Row<T>::BLOCK;
-    const int most = (slice + 16 / (int)sizeof(T) + Row<T>::BLOCK - 1) / Row<T>::BLOCK;
-    r.sums = reinterpret_cast<u64 *>(behind);
-    r.data = reinterpret_cast<uint4 *>(behind + (most * 8 + 15) / 16 * 16);
-    r.load();
-    return r;
-}
 
 template <typename T>
 __global__ void __launch_bounds__(ROW_THREADS, 2)
@@ -606,35 +544,34 @@ sample_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int slice,
               int *__restrict__ tokens, float *__restrict__ logp, float *__restrict__ probs, long ldp) {
     wait_prior();
     allow_dependents();
-    extern __shared__ __align__(16) uint8_t smem[];
-    Shared &sh = *reinterpret_cast<Shared *>(smem);
+    Shared &sh = shared();
     const int r = blockIdx.x / ctas, rank = blockIdx.x % ctas;
-    Row<T> row = open_row(logits + (long)r * ld, V, ctas, rank, slice, &sh, smem + sizeof(Shared));
+    const T *row = logits + (long)r * ld;
+    const Extent e = load_row(row, V, ctas, rank, slice);
     bool single;
-    const Left l = row.filter(f, r, &single);
+    const Left l = filter_row<T>(e, f, r, &single);
     // the thread that knows the token writes it
-    int t = -1;
-    const bool speaks = rank == 0 && threadIdx.x == 0;
-    if (single) t = l.tie;
-    else t = row.locate(share_floor(uniform(u[r]), l.total, false), [&](float x, int id) { return weight_left(l, x, id, sh.table); });
-    if (single ? speaks : t >= 0) {
+    if (logp && threadIdx.x == 32) sh.log_total = single ? 0.0 : log2((double)l.total) - WEIGHT_BITS;     // (a warp that is free)
+    const int t = single ? l.tie : locate<T>(l, false, share_floor(uniform(u[r]), l.total, false), 0);
+    __syncthreads();
+    if (single ? rank == 0 && threadIdx.x == 0 : t >= 0) {
         tokens[r] = t;
         if (logp) {
-            const float x = t < 0 ? 0.f : logit_at(row.row, t);
+            const float x = t < 0 ? 0.f : logit_at(row, t);
             const float2 y = t < 0 || x == l.scale.top ? make_float2(0.f, 0.f) : exponent_of(x, l.scale);
-            logp[r] = t < 0 ? -INFINITY : (float)(-0.69314718055994530942 * ((double)y.x + (double)y.y + log2((double)l.total) - WEIGHT_BITS));
+            logp[r] = t < 0 ? -INFINITY : (float)(-0.69314718055994530942 * ((double)y.x + (double)y.y + sh.log_total));
         }
     }
     if (probs) {
         const float scale = l.total ? (float)(0x1p44 / (double)l.total) : 0.f;
-        const T *data = reinterpret_cast<const T *>(row.data) + row.mis;
-        float *to = probs + (long)r * ldp + row.first;
-        for (int i = threadIdx.x; i < row.count; i += ROW_THREADS) {
+        const T *data = slice_data<T>() + sh.mis;
+        float *to = probs + (long)r * ldp + sh.first;
+        for (int i = threadIdx.x; i < sh.count; i += ROW_THREADS) {
             const float x = logit_at(data, i);
             float w = 0.f;
-            if (l.has(x, row.first + i)) {
+            if (l.has(x, sh.first + i)) {
                 const float2 y = x == l.scale.top ? make_float2(0.f, 0.f) : exponent_of(x, l.scale);
-                if ((y.x - l.limit.x) + (y.y - l.limit.y) <= 0.f) w = exp2f(-y.x) * (1.f - 0.69314718f * y.y) * scale;
+                if (y.x < 160.f && (l.least == 0 || weight_in(l.scale, x, sh.table) >= l.least)) w = exp2f(-y.x) * (1.f - 0.69314718f * y.y) * scale;
             }
             to[i] = w;
         }
@@ -660,9 +597,8 @@ __global__ void __launch_bounds__(ROW_THREADS, 2)
 accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int slice, Settings f, TreeArgs a) {
     wait_prior();
     allow_dependents();
-    extern __shared__ __align__(16) uint8_t smem[];
-    Shared &sh = *reinterpret_cast<Shared *>(smem);
-    const int r = blockIdx.x / ctas, rank = blockIdx.x % ctas;
+    Shared &sh = shared();
+    const int r = blockIdx.x / ctas, rank = blockIdx.x % ctas, lane = threadIdx.x & 31;
     int b = 0;
     for (int hi = a.n; hi - b > 1;) {                   // the last sequence that starts at or before the row
         const int mid = (b + hi) >> 1;
@@ -678,15 +614,15 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
         i = up;
     }
     if (d > a.depth) return;                            // never reached (the whole cluster leaves)
-    Row<T> row = open_row(logits + (long)r * ld, V, ctas, rank, slice, &sh, smem + sizeof(Shared));
+    const T *row = logits + (long)r * ld;
+    const Extent e = load_row(row, V, ctas, rank, slice);
     bool single;
-    const Left l = row.filter(f, b, &single);
+    const Left l = filter_row<T>(e, f, b, &single);
     const float *u = a.u + ((long)b * (a.depth + 1) + d) * (a.children + 1);
     if (rank == 0 && threadIdx.x < 32) {
-        // the first `children` children, in index order; their weights; then the decisions one after another
-        const int lane = threadIdx.x;
+        // the first `children` children, in index order, and their weights; then the decisions one after another
         u64 *kid_w = sh.all;
-        int kids = 0;
+        int *kid = sh.own_id(), *kid_token = sh.list_id(), kids = 0;
         if (d < a.depth)
             for (int j0 = node + 1; j0 < n && kids < a.children; j0 += 32) {
                 const int j = j0 + lane;
@@ -695,9 +631,9 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
                 const int slot = kids + __popc(all & ((1u << lane) - 1u));
                 if (is && slot < a.children) {
                     const int t = tokens[j];
-                    sh.own_id()[slot] = j;
-                    sh.list_id()[slot] = t;
-                    kid_w[slot] = t >= 0 && t < V && l.total ? weight_left(l, logit_at(row.row, t), t, sh.table) : 0;
+                    kid[slot] = j;
+                    kid_token[slot] = t;
+                    kid_w[slot] = t >= 0 && t < V && l.total ? weight_left(l, logit_at(row, t), t, sh.table) : 0;
                 }
                 kids = min(kids + __popc(all), a.children);
             }
@@ -705,13 +641,13 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
         u64 left = l.total;
         int gone = 0, next = -1;
         for (int c = 0; c < kids; ++c) {
-            const int t = sh.list_id()[c];
+            const int t = kid_token[c];
             u64 w = kid_w[c];
             bool again = false;
             for (int i = lane; i < gone; i += 32) again |= sh.gone[i] == t;
             if (__any_sync(0xffffffffu, again)) w = 0;
             if (share_floor(uniform(u[c]), left, false) < w) {
-                next = sh.own_id()[c];
+                next = kid[c];
                 break;
             }
             if (w) {
@@ -721,15 +657,15 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
                 __syncwarp();
             }
         }
-        if (lane == 0) {
-            row.tell(&sh.next, next);
-            row.tell(&sh.gones, gone);
-            row.tell(&sh.left, left);
+        if (lane < ctas) {
+            put(&sh.next, lane, next);
+            put(&sh.gones, lane, gone);
+            put(&sh.left, lane, left);
         }
         for (int p = 1; p < ctas; ++p)
             for (int i = lane; i < gone; i += 32) put(&sh.gone[i], p, sh.gone[i]);
     }
-    row.sync();
+    meet();
     if (rank == 0 && threadIdx.x == 0) a.next[r] = sh.next;
     if (sh.next >= 0) return;
     const int gones = sh.gones;
@@ -738,28 +674,21 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
         if (rank == 0 && threadIdx.x == 0) a.drawn[r] = left ? l.tie : -1;
         return;
     }
-    // the sums without the rejected tokens
-    if (gones) {
+    if (gones) {                                        // the sums without the rejected tokens
         if (threadIdx.x == 0) {
             u64 less = 0;
             for (int g = 0; g < gones; ++g) {
-                const int i = sh.gone[g] - row.first;
-                if (i < 0 || i >= row.count) continue;
-                const u64 v = weight_left(l, logit_at(reinterpret_cast<const T *>(row.data), row.mis + i), sh.gone[g], sh.table);
-                row.sums[(row.mis + i) / Row<T>::BLOCK] -= v;
+                const int i = sh.gone[g] - sh.first;
+                if (i < 0 || i >= sh.count) continue;
+                const u64 v = weight_left(l, logit_at(slice_data<T>(), sh.mis + i), sh.gone[g], sh.table);
+                block_sums()[(sh.mis + i) / BLOCK] -= v;
                 less += v;
             }
-            if (less) row.tell(&sh.total[rank], sh.total[rank] - less);
+            if (less) tell(&sh.total[rank], sh.total[rank] - less);
         }
-        row.sync();
+        meet();
     }
-    const int t = row.locate(share_floor(uniform(u[a.children]), left, false), [&](float x, int id) {
-        u64 v = weight_left(l, x, id, sh.table);
-        if (v)
-            for (int g = 0; g < gones; ++g)
-                if (sh.gone[g] == id) v = 0;
-        return v;
-    });
+    const int t = locate<T>(l, false, share_floor(uniform(u[a.children]), left, false), gones);
     if (t >= 0) a.drawn[r] = t;
 }
 
@@ -782,6 +711,8 @@ __global__ void accept_walk_kernel(TreeArgs a) {
     for (; d <= a.depth; ++d) path[d] = -1;
 }
 
+static_assert(data_offset(most_blocks(MAX_VOCAB / 8, 4)) + (size_t)most_blocks(MAX_VOCAB / 8, 4) * BLOCK * 4 <= 227 * 1024, "the largest row fits");
+
 // How many CTAs share a row, and the ids of each: as few as leave room for two CTAs on an SM, more where there are few
 // rows (and 2048 ids for each).
 struct Cut {
@@ -789,10 +720,7 @@ struct Cut {
     size_t smem;
 };
 static Cut cut_rows(int rows, int V, int size) {
-    const auto smem = [&](int slice) {
-        const int block = 512 / size, most = (slice + 16 / size + block - 1) / block;
-        return sizeof(Shared) + (most * 8 + 15) / 16 * 16 + (size_t)most * 512;
-    };
+    const auto smem = [&](int slice) { return data_offset(most_blocks(slice, size)) + (size_t)most_blocks(slice, size) * BLOCK * size; };
     const auto slice_of = [&](int ctas) { return ((V + ctas - 1) / ctas + 7) / 8 * 8; };
     int c = 1;
     while (c < 8 && smem(slice_of(c)) > 112 * 1024) c *= 2;

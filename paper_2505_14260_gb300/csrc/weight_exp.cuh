@@ -21,9 +21,9 @@ namespace msd {
 constexpr int EXP_STEPS = 1024;
 constexpr int WEIGHT_BITS = 44;             // 393216 weights of 2^44 stay below 2^63
 
-struct ExpTable {
-    float hi[EXP_STEPS], lo[EXP_STEPS];     // 2^(-j / 1024) as a pair
-    constexpr ExpTable() : hi(), lo() {
+struct alignas(16) ExpTable {
+    float pair[2 * EXP_STEPS];              // 2^(-j / 1024): the fp32 value, and what it leaves
+    constexpr ExpTable() : pair() {
         for (int j = 0; j < EXP_STEPS; ++j) {
             const double a = -0.69314718055994530942 * j / EXP_STEPS;
             double term = 1.0, sum = 0.0;
@@ -31,8 +31,8 @@ struct ExpTable {
                 sum += term;
                 term *= a / n;
             }
-            hi[j] = (float)sum;
-            lo[j] = (float)(sum - (double)(float)sum);
+            pair[2 * j] = (float)sum;
+            pair[2 * j + 1] = (float)(sum - (double)(float)sum);
         }
     }
 };
