@@ -68,8 +68,11 @@ struct Left {
 
 // Weight of a token of a run, without min-p.
 __device__ __forceinline__ u64 weight_in(const RowScale &r, float x, const float2 *table) {
-    return x == r.top ? 1ull << WEIGHT_BITS : weight_of(exponent_of(x, r), table);      // (top may be +inf)
+    return weight_of(exponent_of(x, r), table);
 }
+
+// A row whose largest logit is +inf counts as one of zeros at its infinities and -inf elsewhere.
+__device__ __forceinline__ float tame(float x, bool infinite) { return !infinite ? x : x == INFINITY ? 0.f : -INFINITY; }
 
 __device__ __forceinline__ u64 weight_left(const Left &l, float x, int id, const float2 *table) {
     if (!l.has(x, id)) return 0;
@@ -83,6 +86,15 @@ __device__ __forceinline__ u64 weight_left(const Left &l, float x, int id, const
 // The code is kept short (functions that are called, state of the row in shared memory, loops over
 // single elements): with everything inlined and unrolled, warps waited for instructions half of the time.
 // ---------------------------------------------------------------------------
+// A token of a list: order_of() it, and its weight.
+struct __align__(16) Token {
+    u64 order, w;
+};
+// Larger for a token that comes earlier in the order (larger logit, then lower id).
+__device__ __forceinline__ u64 order_of(float x, int id) { return (u64)key_of(x) << 32 | (unsigned)~id; }
+__device__ __forceinline__ float logit_of_order(u64 o) { return logit_of((unsigned)(o >> 32)); }
+__device__ __forceinline__ int id_of_order(u64 o) { return (int)~(unsigned)o; }
+
 struct __align__(16) Shared {                   // (the sums and the slice lie behind it)
     float2 table[EXP_STEPS];
     unsigned hist[3][BUCKETS];                  // own: counts, or masses in pieces of 15, 15 and 14 bits
@@ -90,22 +102,18 @@ struct __align__(16) Shared {                   // (the sums and the slice lie b
     u64 red[WARPS + 1];
     u64 total[8];                               // of each CTA of the cluster
     float top[8], low[8];
-    unsigned valid[8];
     u64 above, left;
     double log_total;
-    unsigned bucket, own_n, list_n, base[8];
-    unsigned range_lo, range_hi;                // keys of the bucket's tokens
+    unsigned bucket, own_n[2], list_n[2], base[8];            // (a round may gather twice)
+    unsigned range_lo[2], range_hi[2];          // keys of the tokens gathered
     float end;
     int tie, token;
     int next, gones, gone[MAX_CHILDREN];
     // the slice: ids [first, first + count), element i of it at data[mis + i], -inf around it, in whole blocks
     int ctas, rank, first, count, mis, blocks, data_at;
-    // where the histogram was, once it is added up: weights of a bucket's tokens, and these, of the slice and of the row
-    __device__ __forceinline__ u64 *list_w() { return reinterpret_cast<u64 *>(hist[0]); }
-    __device__ __forceinline__ float *own_x() { return reinterpret_cast<float *>(hist[1]); }
-    __device__ __forceinline__ int *own_id() { return reinterpret_cast<int *>(hist[1]) + LIST; }
-    __device__ __forceinline__ float *list_x() { return reinterpret_cast<float *>(hist[2]); }
-    __device__ __forceinline__ int *list_id() { return reinterpret_cast<int *>(hist[2]) + LIST; }
+    // where the histogram was, once it is added up: the tokens gathered, of the row and of the slice
+    __device__ __forceinline__ Token *list() { return reinterpret_cast<Token *>(hist); }
+    __device__ __forceinline__ u64 *own() { return reinterpret_cast<u64 *>(hist[2]); }
 };
 constexpr int BLOCK = 128;                      // ids that have a sum of their own
 
@@ -159,9 +167,33 @@ template <typename U> __device__ __forceinline__ void tell(U *p, U v) {         
 }
 
 struct Extent {               // of the row's logits above -inf
-    float top, low;
-    unsigned valid;
+    float top, low;           // low: about the smallest (of a part of them)
+    bool infinite;            // the largest was +inf; the slice holds what tame() gives
 };
+
+// f(logit, id) for every logit of the slice, whole warps at a time; around it there is -inf.
+template <typename T, typename F>
+__device__ __forceinline__ void each(F f) {
+    constexpr int E = 16 / sizeof(T);
+    Shared &sh = shared();
+    const uint4 *data = slice_data<uint4>();
+    const int n = sh.blocks * (BLOCK / E), id0 = sh.first - sh.mis;
+#pragma unroll 1
+    for (int v = threadIdx.x; v - (int)(threadIdx.x & 31) < n; v += ROW_THREADS) {
+        constexpr unsigned NONE = E == 4 ? 0xFF800000u : 0xFF80FF80u;
+        const uint4 q = v < n ? data[v] : make_uint4(NONE, NONE, NONE, NONE);
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (E == 4) {
+                f(__uint_as_float(w[e]), id0 + v * 4 + e);
+            } else {
+                f(__uint_as_float(w[e] << 16), id0 + v * 8 + 2 * e);
+                f(__uint_as_float(w[e] & 0xFFFF0000u), id0 + v * 8 + 2 * e + 1);
+            }
+        }
+    }
+}
 
 // This CTA's slice into shared memory, and the row's extent.
 template <typename T>
@@ -178,13 +210,7 @@ __device__ Extent load_row(const T *row, int V, int ctas, int rank, int slice) {
     const T *const from = row + first - mis;                                                // 16-byte aligned
     const int v0 = mis ? 1 : 0, v1 = max((mis + count) / E, v0);                            // whole vectors
     float hi = -INFINITY, lo = INFINITY;
-    unsigned n = 0;
-    const auto note = [&](float x) {
-        const bool is = x > -INFINITY;
-        hi = fmaxf(hi, x);                                                                  // (leaves NaN out)
-        lo = is ? fminf(lo, x) : lo;
-        n += is;
-    };
+    const auto low = [&](float x) { lo = x > -INFINITY ? fminf(lo, x) : lo; };
     for (int v = v0 + tid; v < v1; v += U * ROW_THREADS) {
         uint4 q[U];
 #pragma unroll
@@ -196,14 +222,14 @@ __device__ Extent load_row(const T *row, int V, int ctas, int rank, int slice) {
             reinterpret_cast<uint4 *>(data)[v + u * ROW_THREADS] = q[u];
             const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < 4; ++e) {                                                   // (fmaxf leaves NaN out)
                 if constexpr (E == 4) {
-                    note(__uint_as_float(w[e]));
+                    hi = fmaxf(hi, __uint_as_float(w[e]));
                 } else {
-                    note(__uint_as_float(w[e] << 16));
-                    note(__uint_as_float(w[e] & 0xFFFF0000u));
+                    hi = fmaxf(hi, fmaxf(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xFFFF0000u)));
                 }
             }
+            if (u == 0) low(__uint_as_float(E == 4 ? w[0] : w[0] & 0xFFFF0000u));
         }
     }
     // the edges: elements before the first whole vector and behind the last one
@@ -212,7 +238,8 @@ __device__ Extent load_row(const T *row, int V, int ctas, int rank, int slice) {
         const bool is = at >= mis && at < mis + count;
         const float x = is ? logit_at(from, at) : -INFINITY;
         data[at] = (T)x;
-        note(x);
+        hi = fmaxf(hi, x);
+        low(x);
     }
     reinterpret_cast<uint4 *>(sh.table)[tid] = reinterpret_cast<const uint4 *>(g_exp_table.pair)[tid];
     static_assert(EXP_STEPS * 8 == ROW_THREADS * 16, "");
@@ -222,28 +249,30 @@ __device__ Extent load_row(const T *row, int V, int ctas, int rank, int slice) {
     }
     hi = warp_max(hi);
     lo = -warp_max(-lo);
-    n = __reduce_add_sync(0xffffffffu, n);
     float *part = reinterpret_cast<float *>(sh.hist[0]);
-    if ((tid & 31) == 0) { part[warp] = hi; part[32 + warp] = lo; sh.hist[1][warp] = n; }
+    if ((tid & 31) == 0) { part[warp] = hi; part[32 + warp] = lo; }
     if (ctas > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");               // all CTAs run: their shared memory is there
     __syncthreads();
     if (tid < 32) {
         hi = warp_max(tid < WARPS ? part[tid] : -INFINITY);
         lo = -warp_max(tid < WARPS ? -part[32 + tid] : -INFINITY);
-        n = __reduce_add_sync(0xffffffffu, tid < WARPS ? sh.hist[1][tid] : 0u);
         if (tid < ctas) {
             put(&sh.top[rank], tid, hi);
             put(&sh.low[rank], tid, lo);
-            put(&sh.valid[rank], tid, n);
         }
     }
     meet();
-    Extent e{-INFINITY, INFINITY, 0};
+    Extent e{-INFINITY, INFINITY, false};
     for (int r = 0; r < ctas; ++r) {
         e.top = fmaxf(e.top, sh.top[r]);
         e.low = fminf(e.low, sh.low[r]);
-        e.valid += sh.valid[r];
     }
+    if (e.top == INFINITY) {
+        e = Extent{0.f, 0.f, true};
+        for (int i = tid; i < blocks * BLOCK; i += ROW_THREADS) data[i] = (T)tame(logit_at(data, i), true);
+        __syncthreads();
+    }
+    e.low = fminf(e.low, e.top);
     return e;
 }
 
@@ -263,8 +292,7 @@ __device__ __noinline__ u64 add_up(const Left l, bool ties) {
         u64 v = 0;
 #pragma unroll 1
         for (int i = b * BLOCK; i < (b + 1) * BLOCK; i += 32) {
-            const float x = logit_at(data, i);
-            if (l.has(x, id0 + i)) v += value_of(l, ties, x, id0 + i, sh.table);
+            v += value_of(l, ties, logit_at(data, i), id0 + i, sh.table);
         }
         if (__any_sync(0xffffffffu, v != 0)) v = warp_total(v);
         if (lane == 0) block_sums()[b] = v;
@@ -331,15 +359,127 @@ __device__ __noinline__ int locate(const Left l, bool ties, u64 goal, int gones)
     return -1;
 }
 
+// A run of few tokens, gathered in the first CTA: what top-k, top-p and min-p leave of it, by comparing each token with
+// every other. mass: the weight that top-p's share is taken of, where top-k is off. The list's weights become what is left.
+__device__ __noinline__ Left rest_of_list(Left l, int n, int k, float p, u64 mass) {
+    Shared &sh = shared();
+    const int i = threadIdx.x, lane = i & 31, warp = i >> 5;
+    const auto block_sum = [&](u64 v) {
+        v = warp_total(v);
+        __syncthreads();
+        if (lane == 0) sh.red[warp] = v;
+        __syncthreads();
+        u64 t = 0;
+#pragma unroll 4
+        for (int w = 0; w < WARPS; ++w) t += sh.red[w];
+        return t;
+    };
+    int before = 0;
+    u64 order = 0, w = 0, above = 0;
+    if (i < n) {
+        order = sh.list()[i].order;
+        w = weight_in(l.scale, logit_of_order(order), sh.table);
+        sh.list()[i].w = w;
+    }
+    __syncthreads();
+    if (i < n)
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) {
+            const Token t = sh.list()[j];
+            if (t.order > order) {
+                above += t.w;
+                ++before;
+            }
+        }
+    bool in = i < n && (k <= 0 || before < k);
+    if (p < 1.f) {
+        if (k > 0) mass = block_sum(in ? w : 0);
+        in = in && above < max(share_floor(p, mass, true), 1ull);
+    }
+    in = in && (w >= l.least || before == 0);
+    l.total = block_sum(in ? w : 0);
+    const int left = __syncthreads_count(in);
+    if (i < n) sh.list()[i].w = in ? w : 0;
+    if (in && before == left - 1) { sh.end = logit_of_order(order); sh.tie = id_of_order(order); }
+    __syncthreads();
+    l.end = sh.end;
+    l.tie = sh.tie;
+    return l;
+}
+
+// The smallest id of the list whose cumulative weight exceeds `goal`; gone[0 .. gones) have none. One thread gets it, the others -1.
+__device__ __noinline__ int locate_in_list(int n, u64 goal, int gones) {
+    Shared &sh = shared();
+    const int i = threadIdx.x;
+    u64 w = 0, upto = 0;
+    unsigned low = 0;                                                       // (of the order: larger for a lower id)
+    int id = -1;
+    if (i < n) {
+        w = sh.list()[i].w;
+        low = (unsigned)sh.list()[i].order;
+        id = (int)~low;
+        for (int g = 0; g < gones; ++g)
+            if (sh.gone[g] == id) w = 0;
+        sh.list()[i].w = w;
+    }
+    __syncthreads();
+    if (w == 0) return -1;
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) {
+        const Token t = sh.list()[j];
+        if ((unsigned)t.order >= low) upto += t.w;
+    }
+    return upto - w <= goal && goal < upto ? id : -1;
+}
+
+enum : int { ONE_TOKEN = 0, IN_LIST = 1, IN_ROW = 2 };        // what is left: l.tie alone; the first CTA's list; add_up's sums
+
+// Tokens of the places from `first` to `last` into the first CTA's list, or (all_lists) every CTA's; their number, which may
+// be more than the list has. `which`: 0 or 1, the counters (zero before the last meeting). Keys' range in sh.range_*.
+template <typename T, typename P>
+__device__ __forceinline__ unsigned gather(int which, P place, unsigned first, unsigned last, bool all_lists) {
+    Shared &sh = shared();
+    const int tid = threadIdx.x, lane = tid & 31, ctas = sh.ctas;
+    unsigned lo = ~0u, hi = 0;
+    each<T>([&](float x, int id) {
+        const unsigned b = place(x, id);
+        const bool in = b >= first && b <= last;
+        const unsigned all = __ballot_sync(0xffffffffu, in);
+        if (all == 0) return;
+        unsigned slot = 0;
+        if (lane == __ffs(all) - 1) slot = atomicAdd(&sh.own_n[which], __popc(all));
+        slot = __shfl_sync(0xffffffffu, slot, __ffs(all) - 1) + __popc(all & ((1u << lane) - 1u));
+        if (in) {
+            const u64 o = order_of(x, id);
+            lo = min(lo, (unsigned)(o >> 32));
+            hi = max(hi, (unsigned)(o >> 32));
+            if (slot < LIST) sh.own()[slot] = o;
+        }
+    });
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    if (hi && lane < ctas) { least(&sh.range_lo[which], lane, lo); most(&sh.range_hi[which], lane, hi); }
+    __syncthreads();
+    const unsigned own_n = sh.own_n[which];
+    if (own_n && tid < ctas) sh.base[tid] = take(&sh.list_n[which], tid, own_n);
+    __syncthreads();
+    for (unsigned i = tid; i < min(own_n, (unsigned)LIST); i += ROW_THREADS)
+        for (int r = 0; r < (all_lists ? ctas : 1); ++r) {
+            const unsigned slot = sh.base[r] + i;
+            if (slot < LIST) put(&sh.list()[slot].order, r, sh.own()[i]);
+        }
+    meet();
+    return sh.list_n[which];
+}
+
 // Where the run of tokens of `l` ends whose count (mass false) reaches `goal`, or whose weight reaches the share `p` of
-// theirs (mass true): a narrower l. The bound lies within the run; x_end is its smallest logit. Every CTA finds it by itself from
-// the whole row's histogram and the bucket's tokens, which all are sent.
+// theirs (mass true): a narrower l. x_end is about its smallest logit. Every CTA finds it by itself from the whole row's
+// histogram and the bucket's tokens, which all are sent. Where few tokens lie before the bucket's end, they are gathered instead
+// (*mode becomes IN_LIST, *n their number) and l.total is the weight that p is a share of; nothing else of l changes then.
 template <typename T>
-__device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_end) {
+__device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_end, int *mode, unsigned *list_n) {
     Shared &sh = shared();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, ctas = sh.ctas;
-    const int id0 = sh.first - sh.mis, n_all = sh.blocks * BLOCK;
-    const T *data = slice_data<T>();
     // buckets of equal width in the exponent between the largest logit and x_end; from the second round on, of the keys' bits
     const float y_end = fminf((l.scale.top - x_end) * l.scale.c_hi, Y_MOST);
     const float scale = y_end > 0.f ? (float)(BUCKETS - 1) / y_end * l.scale.c_hi : 0.f;
@@ -348,15 +488,17 @@ __device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_e
     int shift = -1;
     const auto place = [&](float x, int id) -> unsigned {                   // BUCKETS: not one of them
         if (!l.has(x, id)) return BUCKETS;
-        if (shift < 0) return x == l.scale.top ? 0u : (unsigned)__float2int_rz(fminf((l.scale.top - x) * scale, (float)(BUCKETS - 1)));
+        if (shift < 0) return __float_as_uint(fminf((l.scale.top - x) * scale, (float)(BUCKETS - 1)) + 12582912.f) & (2 * BUCKETS - 1);
         const unsigned k = key_of(x);
         return k >= k_lo && k <= k_hi ? (k_hi - k) >> shift : BUCKETS;
     };
     for (int round = 0;; ++round) {
         for (int i = tid; i < BUCKETS; i += ROW_THREADS) sh.hist[0][i] = sh.hist[1][i] = sh.hist[2][i] = 0;
-        if (tid == 0) { sh.own_n = sh.list_n = 0; sh.range_lo = ~0u; sh.range_hi = 0; }
+        if (tid < 2) { sh.own_n[tid] = sh.list_n[tid] = 0; sh.range_lo[tid] = ~0u; sh.range_hi[tid] = 0; }
         __syncthreads();
         if (mass) {
+            const T *data = slice_data<T>();
+            const int id0 = sh.first - sh.mis, n_all = sh.blocks * BLOCK;
 #pragma unroll 1
             for (int i = tid; i < n_all; i += ROW_THREADS) {
                 const float x = logit_at(data, i);
@@ -368,11 +510,10 @@ __device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_e
                 atomicAdd(&sh.hist[2][b], (unsigned)(w >> 30));
             }
         } else {
-#pragma unroll 2
-            for (int i = tid; i < n_all; i += ROW_THREADS) {
-                const unsigned b = place(logit_at(data, i), id0 + i);
+            each<T>([&](float x, int id) {
+                const unsigned b = place(x, id);
                 if (b != BUCKETS) atomicAdd(&sh.hist[0][b], 1u);
-            }
+            });
         }
         __syncthreads();
         for (int i = tid; i < BUCKETS; i += ROW_THREADS) {
@@ -405,70 +546,58 @@ __device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_e
             if (i < warp) before += sh.red[i];
             all += sh.red[i];
         }
-        if (round == 0 && mass) goal = max(share_floor(p, all, true), 1ull);
+        if (round == 0) {
+            if (mass) goal = max(share_floor(p, all, true), 1ull);
+            else if (all <= goal) {                                         // it has no more tokens than that
+                meet();
+                return l;
+            }
+        }
         u64 at = before + run - own;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            if (at < goal && goal <= at + v[i]) { sh.bucket = tid * PER + i; sh.above = at; }
+            if (at < goal && goal <= at + v[i]) { sh.bucket = tid * PER + i; sh.above = at; sh.left = at + v[i]; }
             at += v[i];
         }
         __syncthreads();
         const unsigned bucket = sh.bucket;
         above = sh.above;
-        // its tokens, and the range of their keys
-        unsigned lo = ~0u, hi = 0;
-#pragma unroll 2
-        for (int i = tid; i < n_all; i += ROW_THREADS) {
-            const float x = logit_at(data, i);
-            if (place(x, id0 + i) != bucket) continue;
-            const unsigned k = key_of(x), slot = atomicAdd(&sh.own_n, 1u);
-            lo = min(lo, k);
-            hi = max(hi, k);
-            if (slot < LIST) { sh.own_x()[slot] = x; sh.own_id()[slot] = id0 + i; }
-        }
-        lo = __reduce_min_sync(0xffffffffu, lo);
-        hi = __reduce_max_sync(0xffffffffu, hi);
-        if (hi && lane < ctas) { least(&sh.range_lo, lane, lo); most(&sh.range_hi, lane, hi); }
-        __syncthreads();
-        const unsigned own_n = sh.own_n;
-        if (own_n && tid < ctas) sh.base[tid] = take(&sh.list_n, tid, own_n);
-        __syncthreads();
-        for (unsigned i = tid; i < min(own_n, (unsigned)LIST); i += ROW_THREADS)
-            for (int r = 0; r < ctas; ++r) {
-                const unsigned slot = sh.base[r] + i;
-                if (slot < LIST) {
-                    put(&sh.list_x()[slot], r, sh.own_x()[i]);
-                    put(&sh.list_id()[slot], r, sh.own_id()[i]);
-                }
+        if (round == 0 && (mass || sh.left <= LIST)) {                      // few tokens?
+            const unsigned n = gather<T>(0, place, 0, bucket, false);
+            if (n <= LIST) {
+                l.total = mass ? all : 0;
+                *mode = IN_LIST;
+                *list_n = n;
+                return l;
             }
-        meet();
-        const unsigned n = sh.list_n;
-        k_lo = sh.range_lo;
-        k_hi = sh.range_hi;
+        }
+        const unsigned n = gather<T>(1, place, bucket, bucket, true);
+        k_lo = sh.range_lo[1];
+        k_hi = sh.range_hi[1];
         const bool few = n <= LIST;
         if (!few && k_lo != k_hi) {
             shift = max(0, 22 - __clz(k_hi - k_lo));                        // (k_hi - k_lo) >> shift < BUCKETS
             __syncthreads();                                                // all have read the list's length and the range
             continue;
         }
-        u64 *w = sh.list_w();
-        for (unsigned i = tid; i < (few ? n : 1u); i += ROW_THREADS) w[i] = mass ? max(weight_in(l.scale, sh.list_x()[i], sh.table), 1ull) : 1;
+        Token *const list = sh.list();
+        for (unsigned i = tid; i < (few ? n : 1u); i += ROW_THREADS)
+            list[i].w = mass ? max(weight_in(l.scale, logit_of_order(list[i].order), sh.table), 1ull) : 1;
         __syncthreads();
         if (few) {                                                          // each token's place among them
             for (unsigned i = tid; i < n; i += ROW_THREADS) {
-                const float x = sh.list_x()[i];
-                const int id = sh.list_id()[i];
+                const Token own_token = list[i];
                 u64 s = above;
-#pragma unroll 2
+#pragma unroll 4
                 for (unsigned j = 0; j < n; ++j) {
-                    const float xj = sh.list_x()[j];
-                    if (xj > x || (xj == x && sh.list_id()[j] < id)) s += w[j];
+                    const Token t = list[j];
+                    if (t.order > own_token.order) s += t.w;
                 }
-                if (s < goal && goal <= s + w[i]) { sh.end = x; sh.tie = id; }
+                if (s < goal && goal <= s + own_token.w) { sh.end = logit_of_order(own_token.order); sh.tie = id_of_order(own_token.order); }
             }
         } else {                                                            // equal logits: ids decide
-            const u64 need = (goal - above + w[0] - 1) / w[0];
-            const float x = sh.list_x()[0];
+            const u64 need = (goal - above + list[0].w - 1) / list[0].w;
+            const float x = logit_of_order(list[0].order);
             if (l.end < x) l.tie = 0x7FFFFFFF;
             l.end = x;
             add_up<T>(l, true);
@@ -486,9 +615,10 @@ __device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_e
     }
 }
 
-// What the settings of entry `at` leave. `single`: a run of one token, which is then l.tie (no sums are made).
+// What the settings of entry `at` leave: *mode, with IN_LIST in the first CTA alone (the others get a total of 0), *n
+// tokens in its list. whole: every CTA gets to know l in that case too.
 template <typename T>
-__device__ __forceinline__ Left filter_row(const Extent &e, const Settings &f, int at, bool *single) {
+__device__ __forceinline__ Left filter_row(const Extent &e, const Settings &f, int at, bool whole, int *mode, unsigned *n) {
     Shared &sh = shared();
     Left l;
     l.total = 0;
@@ -496,8 +626,8 @@ __device__ __forceinline__ Left filter_row(const Extent &e, const Settings &f, i
     l.tie = -1;
     l.least = 0;
     l.scale = RowScale{e.top, 0.f, 0.f};
-    *single = true;
-    if (e.valid == 0) return l;
+    *mode = ONE_TOKEN;
+    if (e.top == -INFINITY) return l;
     float temp = f.temperature ? f.temperature[at] : 1.f;
     int k = f.top_k ? f.top_k[at] : 0;
     const float p = f.top_p ? f.top_p[at] : 1.f, m = f.min_p ? f.min_p[at] : 0.f;
@@ -508,31 +638,49 @@ __device__ __forceinline__ Left filter_row(const Extent &e, const Settings &f, i
     l.scale.c_hi = __fdiv_rn(LOG2E, temp);
     l.scale.c_lo = __fdiv_rn(fmaf(-l.scale.c_hi, temp, LOG2E) + LOG2E_LO, temp);
     if (k == 1) {                                                           // the first token alone
-        const T *data = slice_data<T>();
         unsigned id = ~0u;
-        for (int i = threadIdx.x; i < sh.blocks * BLOCK; i += ROW_THREADS)
-            if (logit_at(data, i) == e.top) id = min(id, (unsigned)(sh.first - sh.mis + i));
+        each<T>([&](float x, int i) {
+            if (x == e.top) id = min(id, (unsigned)i);
+        });
         id = __reduce_min_sync(0xffffffffu, id);
-        if (threadIdx.x == 0) sh.range_lo = ~0u;
+        if (threadIdx.x == 0) sh.range_lo[0] = ~0u;
         meet();
         const int lane = threadIdx.x & 31;
-        if (lane < sh.ctas && id != ~0u) least(&sh.range_lo, lane, id);
+        if (lane < sh.ctas && id != ~0u) least(&sh.range_lo[0], lane, id);
         meet();
         l.end = e.top;
-        l.tie = (int)sh.range_lo;
+        l.tie = (int)sh.range_lo[0];
         l.total = 1ull << WEIGHT_BITS;
         return l;
     }
-    *single = false;
+    *mode = IN_ROW;
+    if (m > 0.f) l.least = m < 1.f ? share_floor(m, 1ull << WEIGHT_BITS, true) : 1ull << WEIGHT_BITS;
     float x_end = e.low;
 #pragma unroll 1
-    for (int by = 0; by < 2; ++by) {                                        // top-k, then top-p
-        if (by == 0 ? k <= 0 || (unsigned)k >= e.valid : !(p < 1.f)) continue;
-        l = cut<T>(l, by == 1, (u64)k, p, x_end);
-        x_end = l.end;
+    for (int by = 0; by < 2 && *mode == IN_ROW; ++by) {                     // top-k, then top-p
+        if (by == 0 ? k <= 0 : !(p < 1.f)) continue;
+        l = cut<T>(l, by == 1, (u64)k, p, x_end, mode, n);
+        if (*mode == IN_LIST && by == 1) k = 0;                             // (top-k is behind it already)
+        if (l.end > -INFINITY) x_end = l.end;
     }
-    if (m > 0.f) l.least = m < 1.f ? share_floor(m, 1ull << WEIGHT_BITS, true) : 1ull << WEIGHT_BITS;
-    l.total = add_up<T>(l, false);
+    if (*mode == IN_ROW) {
+        l.total = add_up<T>(l, false);
+        return l;
+    }
+    const u64 mass = l.total;
+    l.total = 0;
+    if (sh.rank == 0) l = rest_of_list(l, (int)*n, k, p, mass);
+    if (whole && sh.ctas > 1) {
+        if (sh.rank == 0 && threadIdx.x == 0) {
+            tell(&sh.end, l.end);
+            tell(&sh.tie, l.tie);
+            tell(&sh.left, l.total);
+        }
+        meet();
+        l.end = sh.end;
+        l.tie = sh.tie;
+        l.total = sh.left;
+    }
     return l;
 }
 
@@ -548,17 +696,22 @@ sample_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int slice,
     const int r = blockIdx.x / ctas, rank = blockIdx.x % ctas;
     const T *row = logits + (long)r * ld;
     const Extent e = load_row(row, V, ctas, rank, slice);
-    bool single;
-    const Left l = filter_row<T>(e, f, r, &single);
+    int mode;
+    unsigned n = 0;
+    const Left l = filter_row<T>(e, f, r, probs != nullptr, &mode, &n);
     // the thread that knows the token writes it
-    if (logp && threadIdx.x == 32) sh.log_total = single ? 0.0 : log2((double)l.total) - WEIGHT_BITS;     // (a warp that is free)
-    const int t = single ? l.tie : locate<T>(l, false, share_floor(uniform(u[r]), l.total, false), 0);
+    if (mode == IN_LIST && rank > 0 && !probs) return;
+    if (logp && threadIdx.x == 32) sh.log_total = mode == ONE_TOKEN ? 0.0 : log2((double)l.total) - WEIGHT_BITS;     // (a warp that is free)
+    const u64 goal = share_floor(uniform(u[r]), l.total, false);
+    int t = -1;
+    if (mode == ONE_TOKEN) t = l.tie;
+    else if (mode == IN_ROW) t = locate<T>(l, false, goal, 0);
+    else if (rank == 0) t = locate_in_list((int)n, goal, 0);
     __syncthreads();
-    if (single ? rank == 0 && threadIdx.x == 0 : t >= 0) {
+    if (mode == ONE_TOKEN ? rank == 0 && threadIdx.x == 0 : t >= 0) {
         tokens[r] = t;
         if (logp) {
-            const float x = t < 0 ? 0.f : logit_at(row, t);
-            const float2 y = t < 0 || x == l.scale.top ? make_float2(0.f, 0.f) : exponent_of(x, l.scale);
+            const float2 y = t < 0 ? make_float2(0.f, 0.f) : exponent_of(tame(logit_at(row, t), e.infinite), l.scale);
             logp[r] = t < 0 ? -INFINITY : (float)(-0.69314718055994530942 * ((double)y.x + (double)y.y + sh.log_total));
         }
     }
@@ -570,7 +723,7 @@ sample_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int slice,
             const float x = logit_at(data, i);
             float w = 0.f;
             if (l.has(x, sh.first + i)) {
-                const float2 y = x == l.scale.top ? make_float2(0.f, 0.f) : exponent_of(x, l.scale);
+                const float2 y = exponent_of(x, l.scale);
                 if (y.x < 160.f && (l.least == 0 || weight_in(l.scale, x, sh.table) >= l.least)) w = exp2f(-y.x) * (1.f - 0.69314718f * y.y) * scale;
             }
             to[i] = w;
@@ -616,13 +769,21 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
     if (d > a.depth) return;                            // never reached (the whole cluster leaves)
     const T *row = logits + (long)r * ld;
     const Extent e = load_row(row, V, ctas, rank, slice);
-    bool single;
-    const Left l = filter_row<T>(e, f, b, &single);
+    int mode;
+    unsigned in_list = 0;
+    const Left l = filter_row<T>(e, f, b, false, &mode, &in_list);
+    if (mode == IN_LIST) {                              // the first CTA goes on alone
+        if (rank > 0) return;
+        __syncthreads();
+        if (threadIdx.x == 0) sh.ctas = 1;
+        __syncthreads();
+    }
+    const int ranks = sh.ctas;
     const float *u = a.u + ((long)b * (a.depth + 1) + d) * (a.children + 1);
     if (rank == 0 && threadIdx.x < 32) {
         // the first `children` children, in index order, and their weights; then the decisions one after another
         u64 *kid_w = sh.all;
-        int *kid = sh.own_id(), *kid_token = sh.list_id(), kids = 0;
+        int *kid = reinterpret_cast<int *>(sh.own()), *kid_token = kid + MAX_CHILDREN, kids = 0;
         if (d < a.depth)
             for (int j0 = node + 1; j0 < n && kids < a.children; j0 += 32) {
                 const int j = j0 + lane;
@@ -633,7 +794,7 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
                     const int t = tokens[j];
                     kid[slot] = j;
                     kid_token[slot] = t;
-                    kid_w[slot] = t >= 0 && t < V && l.total ? weight_left(l, logit_at(row, t), t, sh.table) : 0;
+                    kid_w[slot] = t >= 0 && t < V && l.total ? weight_left(l, tame(logit_at(row, t), e.infinite), t, sh.table) : 0;
                 }
                 kids = min(kids + __popc(all), a.children);
             }
@@ -657,12 +818,12 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
                 __syncwarp();
             }
         }
-        if (lane < ctas) {
+        if (lane < ranks) {
             put(&sh.next, lane, next);
             put(&sh.gones, lane, gone);
             put(&sh.left, lane, left);
         }
-        for (int p = 1; p < ctas; ++p)
+        for (int p = 1; p < ranks; ++p)
             for (int i = lane; i < gone; i += 32) put(&sh.gone[i], p, sh.gone[i]);
     }
     meet();
@@ -670,11 +831,12 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
     if (sh.next >= 0) return;
     const int gones = sh.gones;
     const u64 left = sh.left;
-    if (single || left == 0) {
+    if (mode == ONE_TOKEN || left == 0) {
         if (rank == 0 && threadIdx.x == 0) a.drawn[r] = left ? l.tie : -1;
         return;
     }
-    if (gones) {                                        // the sums without the rejected tokens
+    const u64 goal = share_floor(uniform(u[a.children]), left, false);
+    if (mode == IN_ROW && gones) {                      // the sums without the rejected tokens
         if (threadIdx.x == 0) {
             u64 less = 0;
             for (int g = 0; g < gones; ++g) {
@@ -688,7 +850,7 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
         }
         meet();
     }
-    const int t = locate<T>(l, false, share_floor(uniform(u[a.children]), left, false), gones);
+    const int t = mode == IN_ROW ? locate<T>(l, false, goal, gones) : locate_in_list((int)in_list, goal, gones);
     if (t >= 0) a.drawn[r] = t;
 }
 

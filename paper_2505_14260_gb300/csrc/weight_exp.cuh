@@ -37,7 +37,7 @@ struct alignas(16) ExpTable {
     }
 };
 
-// The scale log2(e) / T of a row as a pair, and the row's largest logit.
+// The scale log2(e) / T of a row as a pair, and the row's largest logit (finite).
 struct RowScale {
     float top, c_hi, c_lo;
 };
@@ -48,40 +48,42 @@ __device__ __forceinline__ float2 exponent_of(float x, const RowScale &r) {
     const float b = s - r.top;
     const float e = (r.top - (s - b)) + (-x - b);       // s + e = top - x exactly
     const float p = __fmul_rn(s, r.c_hi);               // _rn: not to be fused with what follows
-    const float q = fmaf(s, r.c_hi, -p) + fmaf(s, r.c_lo, e * r.c_hi);
-    return make_float2(p, q);
+    return make_float2(p, fmaf(s, r.c_lo, fmaf(e, r.c_hi, fmaf(s, r.c_hi, -p))));
 }
 
-// 2^44 * 2^-(y.x + y.y), to a unit or two; 0 where y.x >= 46. hi, lo: the table in shared memory.
+// 2^44 * 2^-(y.x + y.y), to a unit or two; 0 where y.x >= 46. table: in shared memory.
 __device__ __forceinline__ unsigned long long weight_of(float2 y, const float2 *table) {
-    if (!(y.x < 46.f)) return 0;
-    constexpr float MAGIC = 12582912.f;                 // 1.5 * 2^23: adding it rounds to an integer
+    constexpr float MAGIC = 12582912.f;                 // 1.5 * 2^23 = 0x4B400000: adding it rounds to an integer
+    constexpr unsigned BIAS = 0x4B400000u;
     constexpr float L = -0.693147180559945309f, L_LO = (float)(-0.69314718055994530942 - (double)-0.693147180559945309f);
     const float t = fmaf(y.x, (float)EXP_STEPS, MAGIC);
-    const int j = __float_as_int(t) - 0x4B400000;
+    const unsigned j = __float_as_uint(t);              // BIAS + j; BIAS's low 10 bits, and the 9 above bit 13, are 0
     const float g = fmaf(t - MAGIC, -1.f / EXP_STEPS, y.x);        // exact
     const float a = __fmul_rn(g, L);
-    const float a_lo = fmaf(g, L, -a) + fmaf(g, L_LO, y.y * L);
+    const float a_lo = fmaf(y.y, L, fmaf(g, L_LO, fmaf(g, L, -a)));
     const float m = fmaf(a, fmaf(a, fmaf(a, 1.f / 6.f, 0.5f), a_lo), a_lo);      // e^(a + a_lo) = 1 + a + m
     const float2 w = table[j & (EXP_STEPS - 1)];
-    const float b = __fmul_rn(w.x, a);
-    const float h = w.x + b;
-    const float l = (b - (h - w.x)) + (fmaf(w.x, a, -b) + fmaf(w.x, m, fmaf(w.y, a, w.y)));
-    // (h + l) * 2^(44 - n) as an integer: its part above 2^22, and what is left of it (at most 3/4 * 2^22,
+    const float h = fmaf(w.x, a, w.x);                  // h + l = (w.x + w.y) (1 + a + m)
+    const float l = fmaf(w.y, a, fmaf(w.x, m, fmaf(w.x, a, w.x - h))) + w.y;
+    // (h + l) * 2^(44 - n), n = j >> 10, as an integer: its part above 2^22, and what is left of it (at most 3/4 * 2^22,
     // so that MAGIC still rounds it to an integer)
-    const float scale = __int_as_float((127 + WEIGHT_BITS - 22 - (j >> 10)) << 23);
+    const float scale = __uint_as_float((127u + WEIGHT_BITS - 22 - (j >> 10)) << 23);
     const float v = __fmul_rn(h, scale);
     const float tv = v + MAGIC;
-    const float rest = __fmul_rn(fmaf(l, scale, v - (tv - MAGIC)), 4194304.f);
-    const int top = __float_as_int(tv) - 0x4B400000;
-    const int low = __float_as_int(rest + MAGIC) - 0x4B400000;
-    return ((unsigned long long)top << 22) + (long long)low;
+    const float rest = fmaf(fmaf(l, scale, v - (tv - MAGIC)), 4194304.f, MAGIC);
+    const unsigned long long sum = (unsigned long long)__float_as_uint(tv) * 4194304u + __float_as_uint(rest) -
+                                   ((unsigned long long)BIAS * 4194304u + BIAS);
+    return y.x < 46.f ? sum : 0;
 }
 
 // Orders finite and infinite logits as unsigned numbers (-0 as 0).
 __device__ __forceinline__ unsigned key_of(float x) {
     const unsigned b = __float_as_uint(x + 0.f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+__device__ __forceinline__ float logit_of(unsigned key) {
+    return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
 }
 
 }  // namespace msd
