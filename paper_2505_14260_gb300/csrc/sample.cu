@@ -75,9 +75,8 @@ __device__ __forceinline__ u64 weight_in(const RowScale &r, float x, const float
 __device__ __forceinline__ float tame(float x, bool infinite) { return !infinite ? x : x == INFINITY ? 0.f : -INFINITY; }
 
 __device__ __forceinline__ u64 weight_left(const Left &l, float x, int id, const float2 *table) {
-    if (!l.has(x, id)) return 0;
-    const u64 w = weight_in(l.scale, x, table);
-    return w >= l.least ? w : 0;
+    const u64 w = weight_in(l.scale, x, table);         // (no branch: several are under way at once)
+    return l.has(x, id) && w >= l.least ? w : 0;
 }
 
 // ---------------------------------------------------------------------------
@@ -97,8 +96,17 @@ __device__ __forceinline__ int id_of_order(u64 o) { return (int)~(unsigned)o; }
 
 struct __align__(16) Shared {                   // (the sums and the slice lie behind it)
     float2 table[EXP_STEPS];
-    unsigned hist[3][BUCKETS];                  // own: counts, or masses in pieces of 15, 15 and 14 bits
-    u64 all[BUCKETS];                           // of the whole row
+    union {
+        unsigned hist[3][BUCKETS];              // own: counts, or masses in pieces of 15, 15 and 14 bits
+        struct {                                // once they are added up: tokens gathered, of the row and of the slice
+            Token list[LIST];
+            u64 own[LIST];
+        };
+    };
+    union {
+        u64 all[BUCKETS];                       // of the whole row; 0 between uses
+        u64 kid_w[MAX_CHILDREN];
+    };
     u64 red[WARPS + 1];
     u64 total[8];                               // of each CTA of the cluster
     float top[8], low[8];
@@ -111,9 +119,6 @@ struct __align__(16) Shared {                   // (the sums and the slice lie b
     int next, gones, gone[MAX_CHILDREN];
     // the slice: ids [first, first + count), element i of it at data[mis + i], -inf around it, in whole blocks
     int ctas, rank, first, count, mis, blocks, data_at;
-    // where the histogram was, once it is added up: the tokens gathered, of the row and of the slice
-    __device__ __forceinline__ Token *list() { return reinterpret_cast<Token *>(hist); }
-    __device__ __forceinline__ u64 *own() { return reinterpret_cast<u64 *>(hist[2]); }
 };
 constexpr int BLOCK = 128;                      // ids that have a sum of their own
 
@@ -171,27 +176,30 @@ struct Extent {               // of the row's logits above -inf
     bool infinite;            // the largest was +inf; the slice holds what tame() gives
 };
 
+// A lane's 4 of the 128 ids of a block.
+template <typename T> __device__ __forceinline__ void block_logits(int b, float (&x)[4]) {
+    const int at = b * 32 + (threadIdx.x & 31);
+    if constexpr (sizeof(T) == 4) {
+        const float4 q = slice_data<float4>()[at];
+        x[0] = q.x; x[1] = q.y; x[2] = q.z; x[3] = q.w;
+    } else {
+        const uint2 q = slice_data<uint2>()[at];
+        x[0] = __uint_as_float(q.x << 16); x[1] = __uint_as_float(q.x & 0xFFFF0000u);
+        x[2] = __uint_as_float(q.y << 16); x[3] = __uint_as_float(q.y & 0xFFFF0000u);
+    }
+}
+
 // f(logit, id) for every logit of the slice, whole warps at a time; around it there is -inf.
 template <typename T, typename F>
 __device__ __forceinline__ void each(F f) {
-    constexpr int E = 16 / sizeof(T);
     Shared &sh = shared();
-    const uint4 *data = slice_data<uint4>();
-    const int n = sh.blocks * (BLOCK / E), id0 = sh.first - sh.mis;
+    const int blocks = sh.blocks, id0 = sh.first - sh.mis + (int)(threadIdx.x & 31) * 4;
 #pragma unroll 1
-    for (int v = threadIdx.x; v - (int)(threadIdx.x & 31) < n; v += ROW_THREADS) {
-        constexpr unsigned NONE = E == 4 ? 0xFF800000u : 0xFF80FF80u;
-        const uint4 q = v < n ? data[v] : make_uint4(NONE, NONE, NONE, NONE);
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    for (int b = threadIdx.x >> 5; b < blocks; b += WARPS) {
+        float x[4];
+        block_logits<T>(b, x);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if constexpr (E == 4) {
-                f(__uint_as_float(w[e]), id0 + v * 4 + e);
-            } else {
-                f(__uint_as_float(w[e] << 16), id0 + v * 8 + 2 * e);
-                f(__uint_as_float(w[e] & 0xFFFF0000u), id0 + v * 8 + 2 * e + 1);
-            }
-        }
+        for (int e = 0; e < 4; ++e) f(x[e], id0 + b * BLOCK + e);
     }
 }
 
@@ -285,16 +293,23 @@ __device__ __forceinline__ u64 value_of(const Left &l, bool ties, float x, int i
 template <typename T>
 __device__ __noinline__ u64 add_up(const Left l, bool ties) {
     Shared &sh = shared();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, id0 = sh.first - sh.mis + lane, blocks = sh.blocks;
-    const T *data = slice_data<T>() + lane;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, id0 = sh.first - sh.mis + lane * 4, blocks = sh.blocks;
     u64 sum = 0;
-    for (int b = warp; b < blocks; b += WARPS) {
-        u64 v = 0;
 #pragma unroll 1
-        for (int i = b * BLOCK; i < (b + 1) * BLOCK; i += 32) {
-            v += value_of(l, ties, logit_at(data, i), id0 + i, sh.table);
+    for (int b = warp; b < blocks; b += WARPS) {
+        float x[4];
+        block_logits<T>(b, x);
+        const int id = id0 + b * BLOCK;
+        const bool any = l.has(x[0], id) || l.has(x[1], id + 1) || l.has(x[2], id + 2) || l.has(x[3], id + 3);
+        u64 v = 0;
+        if (__any_sync(0xffffffffu, any)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v += value_of(l, ties, x[e], id + e, sh.table);
+            // less than 2^46 a lane: three sums of 16 bits
+            const u64 lo = __reduce_add_sync(0xffffffffu, (unsigned)v & 0xFFFFu), mid = __reduce_add_sync(0xffffffffu, (unsigned)v >> 16),
+                      hi = __reduce_add_sync(0xffffffffu, (unsigned)(v >> 32));
+            v = lo + (mid << 16) + (hi << 32);
         }
-        if (__any_sync(0xffffffffu, v != 0)) v = warp_total(v);
         if (lane == 0) block_sums()[b] = v;
         sum += v;
     }
@@ -343,64 +358,151 @@ __device__ __noinline__ int locate(const Left l, bool ties, u64 goal, int gones)
         }
         rest -= __shfl_sync(0xffffffffu, in, 31);
     }
-    const int id0 = sh.first - sh.mis + lane;
-#pragma unroll 1
-    for (int i = b * BLOCK; i < (b + 1) * BLOCK; i += 32) {
-        const float x = logit_at(slice_data<T>(), i + lane);
-        u64 own = value_of(l, ties, x, id0 + i, sh.table);
-        if (own)
-            for (int g = 0; g < gones; ++g)
-                if (sh.gone[g] == id0 + i) own = 0;
-        const u64 in = scan(own);
-        const unsigned over = __ballot_sync(0xffffffffu, in > rest);
-        if (over) return __ffs(over) - 1 == lane ? id0 + i : -1;
-        rest -= __shfl_sync(0xffffffffu, in, 31);
+    const int id = sh.first - sh.mis + b * BLOCK + lane * 4;
+    float x[4];
+    block_logits<T>(b, x);
+    u64 v[4], own = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        v[e] = value_of(l, ties, x[e], id + e, sh.table);
+        for (int g = 0; g < gones; ++g)
+            if (sh.gone[g] == id + e) v[e] = 0;
+        own += v[e];
     }
-    return -1;
+    u64 upto = scan(own) - own;
+    int found = -1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (upto <= rest && rest < upto + v[e]) found = id + e;
+        upto += v[e];
+    }
+    return found;
 }
 
-// A run of few tokens, gathered in the first CTA: what top-k, top-p and min-p leave of it, by comparing each token with
-// every other. mass: the weight that top-p's share is taken of, where top-k is off. The list's weights become what is left.
-__device__ __noinline__ Left rest_of_list(Left l, int n, int k, float p, u64 mass) {
+// Larger values first: thread i gets the i-th of the block's. n of them are not 0.
+__device__ u64 sorted(u64 v, unsigned n) {
+    u64 *const buf = shared().own;                                          // (sent by now)
+    const unsigned tid = threadIdx.x;
+    unsigned size = 32;
+    while (size < n) size *= 2;
+#pragma unroll 1
+    for (unsigned k = 2; k <= size; k *= 2)
+#pragma unroll 1
+        for (unsigned j = k / 2; j > 0; j /= 2) {
+            u64 o;
+            if (j < 32) {
+                o = __shfl_xor_sync(0xffffffffu, v, j);
+            } else {
+                __syncthreads();
+                buf[tid] = v;
+                __syncthreads();
+                o = buf[tid ^ j];
+            }
+            const bool larger = ((tid & j) == 0) == ((tid & k) == 0 || k == size);
+            v = (o > v) == larger ? o : v;
+        }
+    return v;
+}
+
+// Sum over the threads up to this one, and of all.
+__device__ u64 sum_up_to(u64 v, u64 *all) {
     Shared &sh = shared();
-    const int i = threadIdx.x, lane = i & 31, warp = i >> 5;
-    const auto block_sum = [&](u64 v) {
-        v = warp_total(v);
-        __syncthreads();
-        if (lane == 0) sh.red[warp] = v;
-        __syncthreads();
-        u64 t = 0;
-#pragma unroll 4
-        for (int w = 0; w < WARPS; ++w) t += sh.red[w];
-        return t;
-    };
-    int before = 0;
-    u64 order = 0, w = 0, above = 0;
-    if (i < n) {
-        order = sh.list()[i].order;
-        w = weight_in(l.scale, logit_of_order(order), sh.table);
-        sh.list()[i].w = w;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const u64 t = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += t;
     }
     __syncthreads();
-    if (i < n)
+    if (lane == 31) sh.red[warp] = v;
+    __syncthreads();
+    u64 sum = 0;
 #pragma unroll 4
-        for (int j = 0; j < n; ++j) {
-            const Token t = sh.list()[j];
-            if (t.order > order) {
-                above += t.w;
-                ++before;
+    for (int i = 0; i < WARPS; ++i) {
+        if (i == warp) v += sum;
+        sum += sh.red[i];
+    }
+    *all = sum;
+    return v;
+}
+
+// A token of the list, its rank, and the weight of those before it.
+struct Placed {
+    u64 order, w, ahead;
+    int rank;
+    bool is;                  // this thread has one
+};
+// Places the list's n tokens (weights in it) by order, or by id: up to 256 by comparing all pairs, with all threads, more by
+// sorting (for 64 tokens pairs take 1 us less than sorting, for 512 3 us more).
+// (By order, sorting loses sight of the weights, which are made again: 1 without mass.)
+__device__ __noinline__ Placed place_tokens(int n, bool by_id, bool mass, const RowScale scale) {
+    Shared &sh = shared();
+    const unsigned tid = threadIdx.x;
+    Placed t{0, 0, 0, 0, false};
+    // by id: the order's lower half is larger for a lower id
+    if (n > LIST / 2) {
+        const u64 o = tid < (unsigned)n ? sh.list[tid].order : 0;
+        const u64 in_order = sorted(by_id ? o << 32 | tid : o, n);
+        t.is = tid < (unsigned)n;
+        t.rank = (int)tid;
+        if (by_id) {
+            const Token own = t.is ? sh.list[(unsigned)in_order] : Token{0, 0};
+            t.order = own.order;
+            t.w = own.w;
+        } else {
+            t.order = in_order;
+            t.w = !t.is ? 0 : mass ? weight_in(scale, logit_of_order(in_order), sh.table) : 1;
+        }
+        u64 all;
+        t.ahead = sum_up_to(t.w, &all) - t.w;
+        return t;
+    }
+    const int bits = min(5, __clz(max(n - 1, 1)) - 23), per = 1 << bits;    // 512 / per >= n
+    const int i = (int)tid >> bits, part = (int)tid & (per - 1);
+    if (i < n) {
+        const Token own = sh.list[i];
+        t.order = own.order;
+        t.w = own.w;
+        const u64 key = by_id ? own.order << 32 : own.order;
+#pragma unroll 4
+        for (int j = part; j < n; j += per) {
+            const Token o = sh.list[j];
+            if ((by_id ? o.order << 32 : o.order) > key) {
+                t.ahead += o.w;
+                ++t.rank;
             }
         }
-    bool in = i < n && (k <= 0 || before < k);
-    if (p < 1.f) {
-        if (k > 0) mass = block_sum(in ? w : 0);
-        in = in && above < max(share_floor(p, mass, true), 1ull);
     }
-    in = in && (w >= l.least || before == 0);
-    l.total = block_sum(in ? w : 0);
+    for (int o = 1; o < per; o *= 2) {
+        t.ahead += __shfl_xor_sync(0xffffffffu, t.ahead, o);
+        t.rank += __shfl_xor_sync(0xffffffffu, t.rank, o);
+    }
+    t.is = i < n && part == 0;
+    return t;
+}
+
+// A run of few tokens, gathered in the first CTA: what top-k, top-p and min-p leave of it. mass: the weight that top-p's
+// share is taken of, where top-k is off. The list's weights become what is left of them.
+__device__ __noinline__ Left rest_of_list(Left l, int n, int k, float p, u64 mass) {
+    Shared &sh = shared();
+    const int tid = threadIdx.x;
+    if (tid < n) sh.list[tid].w = weight_in(l.scale, logit_of_order(sh.list[tid].order), sh.table);
+    __syncthreads();
+    Placed t = place_tokens(n, false, true, l.scale);
+    bool in = t.is && (k <= 0 || t.rank < k);
+    if (p < 1.f) {
+        u64 all;
+        if (k > 0) {
+            sum_up_to(in ? t.w : 0, &all);
+            mass = all;
+        }
+        in = in && t.ahead < max(share_floor(p, mass, true), 1ull);
+    }
+    in = in && (t.w >= l.least || t.rank == 0);
+    sum_up_to(in ? t.w : 0, &l.total);
     const int left = __syncthreads_count(in);
-    if (i < n) sh.list()[i].w = in ? w : 0;
-    if (in && before == left - 1) { sh.end = logit_of_order(order); sh.tie = id_of_order(order); }
+    if (t.is && t.rank < n) sh.list[t.rank] = Token{t.order, in ? t.w : 0};
+    if (in && t.rank == left - 1) { sh.end = logit_of_order(t.order); sh.tie = id_of_order(t.order); }
     __syncthreads();
     l.end = sh.end;
     l.tie = sh.tie;
@@ -410,26 +512,15 @@ __device__ __noinline__ Left rest_of_list(Left l, int n, int k, float p, u64 mas
 // The smallest id of the list whose cumulative weight exceeds `goal`; gone[0 .. gones) have none. One thread gets it, the others -1.
 __device__ __noinline__ int locate_in_list(int n, u64 goal, int gones) {
     Shared &sh = shared();
-    const int i = threadIdx.x;
-    u64 w = 0, upto = 0;
-    unsigned low = 0;                                                       // (of the order: larger for a lower id)
-    int id = -1;
-    if (i < n) {
-        w = sh.list()[i].w;
-        low = (unsigned)sh.list()[i].order;
-        id = (int)~low;
-        for (int g = 0; g < gones; ++g)
-            if (sh.gone[g] == id) w = 0;
-        sh.list()[i].w = w;
+    const int tid = threadIdx.x;
+    if (gones) {
+        if (tid < n)
+            for (int g = 0; g < gones; ++g)
+                if (sh.gone[g] == id_of_order(sh.list[tid].order)) sh.list[tid].w = 0;
+        __syncthreads();
     }
-    __syncthreads();
-    if (w == 0) return -1;
-#pragma unroll 4
-    for (int j = 0; j < n; ++j) {
-        const Token t = sh.list()[j];
-        if ((unsigned)t.order >= low) upto += t.w;
-    }
-    return upto - w <= goal && goal < upto ? id : -1;
+    const Placed t = place_tokens(n, true, true, RowScale{});
+    return t.is && t.ahead <= goal && goal < t.ahead + t.w ? id_of_order(t.order) : -1;
 }
 
 enum : int { ONE_TOKEN = 0, IN_LIST = 1, IN_ROW = 2 };        // what is left: l.tie alone; the first CTA's list; add_up's sums
@@ -453,7 +544,7 @@ __device__ __forceinline__ unsigned gather(int which, P place, unsigned first, u
             const u64 o = order_of(x, id);
             lo = min(lo, (unsigned)(o >> 32));
             hi = max(hi, (unsigned)(o >> 32));
-            if (slot < LIST) sh.own()[slot] = o;
+            if (slot < LIST) sh.own[slot] = o;
         }
     });
     lo = __reduce_min_sync(0xffffffffu, lo);
@@ -466,7 +557,7 @@ __device__ __forceinline__ unsigned gather(int which, P place, unsigned first, u
     for (unsigned i = tid; i < min(own_n, (unsigned)LIST); i += ROW_THREADS)
         for (int r = 0; r < (all_lists ? ctas : 1); ++r) {
             const unsigned slot = sh.base[r] + i;
-            if (slot < LIST) put(&sh.list()[slot].order, r, sh.own()[i]);
+            if (slot < LIST) put(&sh.list[slot].order, r, sh.own[i]);
         }
     meet();
     return sh.list_n[which];
@@ -497,18 +588,14 @@ __device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_e
         if (tid < 2) { sh.own_n[tid] = sh.list_n[tid] = 0; sh.range_lo[tid] = ~0u; sh.range_hi[tid] = 0; }
         __syncthreads();
         if (mass) {
-            const T *data = slice_data<T>();
-            const int id0 = sh.first - sh.mis, n_all = sh.blocks * BLOCK;
-#pragma unroll 1
-            for (int i = tid; i < n_all; i += ROW_THREADS) {
-                const float x = logit_at(data, i);
-                const unsigned b = place(x, id0 + i);
-                if (b == BUCKETS) continue;
+            each<T>([&](float x, int id) {
+                const unsigned b = place(x, id);
                 const u64 w = weight_in(l.scale, x, sh.table);
+                if (b == BUCKETS) return;
                 atomicAdd(&sh.hist[0][b], (unsigned)w & 0x7FFFu);
                 atomicAdd(&sh.hist[1][b], (unsigned)(w >> 15) & 0x7FFFu);
                 atomicAdd(&sh.hist[2][b], (unsigned)(w >> 30));
-            }
+            });
         } else {
             each<T>([&](float x, int id) {
                 const unsigned b = place(x, id);
@@ -562,7 +649,23 @@ __device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_e
         __syncthreads();
         const unsigned bucket = sh.bucket;
         above = sh.above;
-        if (round == 0 && (mass || sh.left <= LIST)) {                      // few tokens?
+        // few tokens? (by mass: about as many as the buckets' masses are weights of their ends)
+        bool few_before = round == 0 && sh.left <= LIST;
+        if (round == 0 && mass) {
+            float about = 0.f;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (tid * PER + i <= bucket) about += (float)v[i] * exp2f((float)(tid * PER + i) * (y_end / (BUCKETS - 1)) - WEIGHT_BITS);
+            about = warp_sum(about);
+            if (lane == 0) sh.red[warp] = (u64)about;
+            __syncthreads();
+            u64 sum = 0;
+#pragma unroll 4
+            for (int i = 0; i < WARPS; ++i) sum += sh.red[i];
+            few_before = sum < LIST;
+            __syncthreads();
+        }
+        if (few_before) {
             const unsigned n = gather<T>(0, place, 0, bucket, false);
             if (n <= LIST) {
                 l.total = mass ? all : 0;
@@ -580,24 +683,17 @@ __device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_e
             __syncthreads();                                                // all have read the list's length and the range
             continue;
         }
-        Token *const list = sh.list();
-        for (unsigned i = tid; i < (few ? n : 1u); i += ROW_THREADS)
-            list[i].w = mass ? max(weight_in(l.scale, logit_of_order(list[i].order), sh.table), 1ull) : 1;
-        __syncthreads();
         if (few) {                                                          // each token's place among them
-            for (unsigned i = tid; i < n; i += ROW_THREADS) {
-                const Token own_token = list[i];
-                u64 s = above;
-#pragma unroll 4
-                for (unsigned j = 0; j < n; ++j) {
-                    const Token t = list[j];
-                    if (t.order > own_token.order) s += t.w;
-                }
-                if (s < goal && goal <= s + own_token.w) { sh.end = logit_of_order(own_token.order); sh.tie = id_of_order(own_token.order); }
+            if (tid < (int)n) sh.list[tid].w = mass ? weight_in(l.scale, logit_of_order(sh.list[tid].order), sh.table) : 1;
+            __syncthreads();
+            const Placed t = place_tokens((int)n, false, mass, l.scale);
+            if (t.is && above + t.ahead < goal && goal <= above + t.ahead + t.w) {
+                sh.end = logit_of_order(t.order);
+                sh.tie = id_of_order(t.order);
             }
         } else {                                                            // equal logits: ids decide
-            const u64 need = (goal - above + list[0].w - 1) / list[0].w;
-            const float x = logit_of_order(list[0].order);
+            const float x = logit_of_order(sh.list[0].order);
+            const u64 w = !mass ? 1 : max(weight_in(l.scale, x, sh.table), 1ull), need = (goal - above + w - 1) / w;
             if (l.end < x) l.tie = 0x7FFFFFFF;
             l.end = x;
             add_up<T>(l, true);
@@ -782,8 +878,8 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
     const float *u = a.u + ((long)b * (a.depth + 1) + d) * (a.children + 1);
     if (rank == 0 && threadIdx.x < 32) {
         // the first `children` children, in index order, and their weights; then the decisions one after another
-        u64 *kid_w = sh.all;
-        int *kid = reinterpret_cast<int *>(sh.own()), *kid_token = kid + MAX_CHILDREN, kids = 0;
+        u64 *kid_w = sh.kid_w;
+        int *kid = reinterpret_cast<int *>(sh.own), *kid_token = kid + MAX_CHILDREN, kids = 0;
         if (d < a.depth)
             for (int j0 = node + 1; j0 < n && kids < a.children; j0 += 32) {
                 const int j = j0 + lane;
