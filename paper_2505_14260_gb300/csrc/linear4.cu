@@ -85,19 +85,26 @@ linear4_few_kernel(const T *__restrict__ x, long ldx, int m, Weight w, float *__
 
     const bf16 *sc_at = w.scales + (long)j0 * w.groups;
     const uint8_t *z_at = w.zeros + (long)j0 * w.groups;
-    if (staged) {   // scales and zeros of the tile: one run of each
-        const int n = outs * w.groups;
-        const bf16 *from = w.scales + (long)j0 * w.groups;
-        if (reinterpret_cast<uintptr_t>(from) % 16 == 0) {
-            for (int i = tid; i < n / 8; i += FEW_WARPS * 32) reinterpret_cast<uint4 *>(scales)[i] = reinterpret_cast<const uint4 *>(from)[i];
-            for (int i = n / 8 * 8 + tid; i < n; i += FEW_WARPS * 32) scales[i] = from[i];
-        } else {
-            for (int i = tid; i < n; i += FEW_WARPS * 32) scales[i] = from[i];
-        }
-        if (w.zeros) {
-            const uint8_t *z = w.zeros + (long)j0 * w.groups;
-            for (int i = tid; i < n; i += FEW_WARPS * 32) zeros[i] = z[i];
-        }
+    if (staged) {   // scales and zeros of the tile: one run of each, in 16-byte pieces where they lie so
+        const auto copy = [&](uint8_t *to, const uint8_t *from, int bytes) {
+            constexpr int T = FEW_WARPS * 32, U = 4;
+            int done = 0;
+            if (reinterpret_cast<uintptr_t>(from) % 16 == 0) {
+                const int n = bytes / 16;
+                for (int i0 = tid; i0 < n; i0 += U * T) {
+                    uint4 v[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) v[u] = reinterpret_cast<const uint4 *>(from)[min(i0 + u * T, n - 1)];
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        if (i0 + u * T < n) reinterpret_cast<uint4 *>(to)[i0 + u * T] = v[u];
+                }
+                done = n * 16;
+            }
+            for (int i = done + tid; i < bytes; i += T) to[i] = from[i];
+        };
+        copy(reinterpret_cast<uint8_t *>(scales), reinterpret_cast<const uint8_t *>(sc_at), outs * w.groups * 2);
+        if (w.zeros) copy(zeros, z_at, outs * w.groups);
         sc_at = scales;
         z_at = zeros;
     }

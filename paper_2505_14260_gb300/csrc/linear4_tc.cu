@@ -8,17 +8,19 @@
 // integer and bf16 operations for 8 codes, one fused multiply per row of x for each group, and
 // nothing in the tensor cores that another form would save.
 //
-// A CTA (448 threads, one an SM: it holds all of the tensor memory) has 256 outputs, two groups of
-// four warps with 128 each, and up to N rows of x; K is cut between the CTAs of a cluster where
-// there are fewer tiles than SMs, and their totals meet through distributed shared memory in rank
-// order. Roles:
-//   warps 0-7    a row of W a thread: codes -> tensor memory, and the chunk before: sums -> totals
-//   warps 8-11   x of a chunk of 128 elements, swizzled as the MMA reads it, a chunk a warp
-//   warp 12      MMAs       warp 13      copies of codes
-// The codes of a word go in as the pairs (0, 4), (1, 5), (2, 6), (3, 7), so x's octets are ordered
-// alike. A wait that runs out (2 s) leaves NaN in the CTA's part of y.
+// A CTA (one an SM: it holds all of the tensor memory) has 256 outputs, two halves of 128, and up to N rows of x; K is
+// cut between the CTAs of a cluster where there are fewer tiles than SMs, and their totals meet through distributed
+// shared memory in rank order. Chunks are 128 elements of K. Roles:
+//   warps 0-15   a row of W a thread: codes -> tensor memory; four warps for the even chunks of a half, four for the odd ones
+//   warps 16-23  a row of W a thread: a group's sum from tensor memory, scaled, into fp32 totals
+//   warps 24-27  MMAs of a half each, copies of codes and of bf16 x
+//   warps 28-31  (fp32 x only) x as three bf16 planes that add up to it, swizzled as the MMA reads them
+// What bounds it is the integer pipe: 8 selections for 8 codes, at half a warp a cycle, 512 cycles for a chunk of 256 outputs
+// (an MMA of such a chunk takes 128 to 512, a copy 330 at the rate of memory). One group of warps a half doing everything in turn
+// took 1800 cycles a chunk, waiting for one another. A wait that runs out (2 s) leaves NaN in the CTA's part of y.
 #include <algorithm>
 #include <cstring>
+#include <type_traits>
 
 #include <cudaTypedefs.h>
 
@@ -28,20 +30,26 @@
 namespace msd {
 namespace {
 
-constexpr int THREADS = 448, TILE = 128, CHUNK = 128, OUT = 256, X_WARPS = 4;
+constexpr int TILE = 128, CHUNK = 128, OUT = 256;
 constexpr uint32_t WBOX = TILE * CHUNK / 2, WSTAGE = 2 * WBOX;
 constexpr uint32_t SMEM_MOST = 227 * 1024 - 2048;               // less static shared memory
+constexpr int CODE_WARPS = 16, SUM_WARPS = 8, X_WARPS = 4;
 
 template <typename T, int GROUP, int N>
 struct Lay {
+    static constexpr bool SPLIT = sizeof(T) == 4;               // x in planes
     static constexpr int P = Octet<T>::PLANES, PER = CHUNK / GROUP;
+    static constexpr int THREADS = 32 * (CODE_WARPS + SUM_WARPS + 4 + (SPLIT ? X_WARPS : 0));
+    // registers by role: their sum over the groups of four warps is the launch's (72 * 7, 64 * 8)
+    static constexpr int R_CODE = 56, R_SUM = SPLIT ? 96 : 112, R_ISSUE = SPLIT ? 40 : 56, R_X = 56;
+    static_assert(4 * R_CODE + 2 * R_SUM + R_ISSUE + (SPLIT ? R_X : 0) <= (SPLIT ? 64 * 8 : 72 * 7), "");
     static constexpr uint32_t XBOX = N * 128, XPLANE = 2 * XBOX, XSTAGE = P * XPLANE;
     static constexpr int XS = XSTAGE > 24 * 1024 ? 2 : 4;
     static constexpr int WS = XSTAGE > 24 * 1024 ? 5 : 6;
-    static constexpr int DS = 128 / N;                          // accumulators of a group of warps
+    static constexpr int DS = 128 / N;                          // accumulators of a half
     static constexpr uint32_t X = 0, W = XS * XSTAGE, SCALES = W + WS * WSTAGE;
     static constexpr uint32_t ROOM = SMEM_MOST - 1024 - SCALES; // for scales and zeros
-    static constexpr uint32_t T_A = 0, T_D = 128, T_HALF = 256; // columns of a group of warps
+    static constexpr uint32_t T_A = 0, T_D = 128, T_HALF = 256; // columns of a half
     static_assert(N * OUT * 4 <= SCALES, "totals of a CTA fit where the stages were");
     static_assert(SCALES + 1024 <= SMEM_MOST, "");
 };
@@ -73,9 +81,24 @@ __device__ __forceinline__ void sts16(uint32_t a, const uint32_t *v) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
 
+// Codes 2 i and 2 i + 1 of a word (byte i) less the zero, as a bf16 pair. off: 128 + zero, twice.
+__device__ __forceinline__ uint32_t pair_of_byte(uint32_t word, int i, __nv_bfloat162 off) {
+    uint32_t v;
+    const uint32_t byte = __byte_perm(word, 0, 0x4440 | i);
+    asm("lop3.b32 %0, %1, 0x000F000F, 0x43004300, 0xEA;" : "=r"(v) : "r"(byte * 0x1001u));   // the upper half 12 bits up; (a & b) | c
+    const __nv_bfloat162 d = __hsub2(*reinterpret_cast<__nv_bfloat162 *>(&v), off);
+    return *reinterpret_cast<const uint32_t *>(&d);
+}
+
+// One thread waits.
+__device__ __forceinline__ bool t_wait(uint32_t bar, int use, int lap, volatile int *abort) {
+    const uint32_t parity = (uint32_t)(use / lap) & 1u;
+    return bar_try(bar, parity) || bar_wait_slow(bar, parity, abort, nullptr);
+}
+
 template <typename T, int GROUP, int N>
-__global__ void __launch_bounds__(THREADS, 1)
-linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const Args a) {
+__global__ void __launch_bounds__(Lay<T, GROUP, N>::THREADS, 1)
+linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap x_map, const Args a) {
     using L = Lay<T, GROUP, N>;
     constexpr int PER = L::PER, P = L::P, XS = L::XS, WS = L::WS, DS = L::DS;
     extern __shared__ uint8_t smem_raw[];
@@ -98,21 +121,22 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const Args a) {
         }
         for (int i = 0; i < XS; ++i) {
             bar_init(x_full + 8 * i, 1);
-            bar_init(x_empty + 8 * i, 1);
+            bar_init(x_empty + 8 * i, 2);
         }
         for (int i = 0; i < 4; ++i) {
-            bar_init(a_full + 8 * i, 128);
+            bar_init(a_full + 8 * i, 4);
             bar_init(a_empty + 8 * i, 1);
         }
         for (int i = 0; i < 2 * DS; ++i) {
             bar_init(d_full + 8 * i, 1);
-            bar_init(d_empty + 8 * i, 128);
+            bar_init(d_empty + 8 * i, 4);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_abort = 0;
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
+        if constexpr (!L::SPLIT) asm volatile("prefetch.tensormap [%0];" ::"l"(&x_map) : "memory");
     }
-    if (warp == 12) {
+    if (warp == 24) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(su32(&s_tmem)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -123,105 +147,201 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const Args a) {
     wait_prior();
     allow_dependents();
 
-    float total[N];
-    if (warp < 8) {
-        // ---- codes to tensor memory, sums to totals --------------------------------------------
+    // scales and zeros [group][output], a run of outputs beside one another
+    constexpr int SPITCH = OUT + 2, ZPITCH = OUT + 4;
+    bf16 *const s_scales = reinterpret_cast<bf16 *>(smem + L::SCALES);
+    uint8_t *const s_zeros = smem + L::SCALES + (size_t)a.slice * SPITCH * 2;
+    const int g0 = c0 * PER, gs = min(nc * PER, a.w.groups - g0), outs = min(OUT, a.w.o - j0);
+    const auto stage = [&](auto *to, const auto *from, int pitch, int t, int threads) {
+        const unsigned magic = 0xFFFFFFFFu / (unsigned)gs + 1;          // i / gs for i * gs < 2^32; gs 1: 0
+        constexpr int U = 8;                                            // loads in flight a thread
+        for (int b = t; b < outs * gs; b += U * threads) {
+            std::remove_reference_t<decltype(*to)> v[U];
+            int at[U];
 #pragma unroll
-        for (int i = 0; i < N; ++i) total[i] = 0.f;
-        const int half = warp >> 2, row = (warp & 3) * 32 + lane, out = half * TILE + row;
-        const int spitch = OUT + 2, zpitch = OUT + 4;
-        bf16 *const s_scales = reinterpret_cast<bf16 *>(smem + L::SCALES);
-        uint8_t *const s_zeros = smem + L::SCALES + (size_t)a.slice * spitch * 2;
-        const int g0 = c0 * PER, gs = min(nc * PER, a.w.groups - g0), outs = min(OUT, a.w.o - j0);
-        if (a.staged) {
-            const unsigned magic = 0xFFFFFFFFu / (unsigned)gs + 1;          // i / gs for i * gs < 2^32; gs 1: 0
-            for (int i = tid; i < outs * gs; i += 256) {
+            for (int u = 0; u < U; ++u) {
+                const int i = min(b + u * threads, outs * gs - 1);
                 const int r = gs > 1 ? (int)__umulhi((unsigned)i, magic) : i, g = i - r * gs;
-                const long at = (long)(j0 + r) * a.w.groups + g0 + g;
-                s_scales[g * spitch + r] = a.w.scales[at];
-                if (a.w.zeros) s_zeros[g * zpitch + r] = a.w.zeros[at];
+                v[u] = from[(long)(j0 + r) * a.w.groups + g0 + g];
+                at[u] = g * pitch + r;
             }
-            asm volatile("bar.sync 1, 256;" ::: "memory");
+#pragma unroll
+            for (int u = 0; u < U; ++u) to[at[u]] = v[u];
         }
-        const long wide_at = (long)(j0 + min(out, outs - 1)) * a.w.groups + g0;
-        auto scale_at = [&](int g) {
-            if (g >= gs || out >= outs) return 0.f;
-            return __bfloat162float(a.staged ? s_scales[g * spitch + out] : a.w.scales[wide_at + g]);
-        };
-        auto zero_at = [&](int g) {
-            if (!a.w.zeros || g >= gs || out >= outs) return 8u;
-            return (unsigned)(a.staged ? s_zeros[g * zpitch + out] : a.w.zeros[wide_at + g]);
-        };
-        const uint32_t t_a = tmem + ((uint32_t)(warp & 3) << 21) + half * L::T_HALF + L::T_A;
-        const uint32_t t_d = tmem + ((uint32_t)(warp & 3) << 21) + half * L::T_HALF + L::T_D;
-        const uint32_t code_row = base + L::W + half * WBOX + row * 64;
-        const uint32_t swz = (uint32_t)(row >> 1 & 3) << 4;
+    };
+
+    // every role ends here: stages, accumulators and codes are done with
+    const auto done = [] { fence_before(); asm volatile("bar.sync 3, %0;" ::"n"(L::THREADS) : "memory"); };
+    if (warp < CODE_WARPS) {
+        // ---- codes to tensor memory ---------------------------------------------------------------
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::R_CODE));
+        const int half = warp >> 3, slot = warp >> 2 & 1, row = (warp & 3) * 32 + lane, out = half * TILE + row;
+        if (a.staged && a.w.zeros) {
+            stage(s_zeros, a.w.zeros, ZPITCH, tid, CODE_WARPS * 32);
+            asm volatile("bar.sync 1, 512;" ::: "memory");
+        }
+        const uint32_t t_a = tmem + ((uint32_t)(warp & 3) << 21) + half * L::T_HALF + L::T_A + slot * 64;
+        const uint32_t code_row = base + L::W + half * WBOX + row * 64, swz = (uint32_t)(row >> 1 & 3) << 4;
+        const uint8_t *const z_at = a.staged ? s_zeros + out : a.w.zeros + (long)(j0 + min(out, outs - 1)) * a.w.groups + g0;
+        const int z_step = a.staged ? ZPITCH : 1;
         bool ok = true;
-        auto promote = [&](int ci) {
-#pragma unroll
-            for (int e = 0; e < PER; ++e) {
-                const int gi = ci * PER + e, ds = gi % DS;
-                const float s = scale_at(gi);
-                ok = w_wait(d_full + 8 * (half * DS + ds), (uint32_t)(gi / DS) & 1u, &s_abort, nullptr);
-                if (!ok) return;
-                fence_after();
-                constexpr int STEP = N < 32 ? N : 32;
-                uint32_t d[N];
-#pragma unroll
-                for (int i = 0; i < N; i += STEP) {
-                    if constexpr (STEP == 16) tmem_ld16(t_d + ds * N + i, d + i);
-                    else tmem_ld32(t_d + ds * N + i, d + i);
-                }
-                fence_before();
-                bar_arrive(d_empty + 8 * (half * DS + ds));
-#pragma unroll
-                for (int i = 0; i < N; ++i) total[i] = fmaf(s, __uint_as_float(d[i]), total[i]);
-            }
-        };
-        for (int ci = 0; ci < nc && ok; ++ci) {
-            const int ws = ci % WS, slot = ci & 1;
+        for (int ci = slot; ci < nc && ok; ci += 2) {
+            const int ws = ci % WS;
             ok = w_wait(w_full + 8 * ws, (uint32_t)(ci / WS) & 1u, &s_abort, nullptr);
             if (!ok) break;
             uint4 q[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) q[i] = lds16(code_row + ws * WSTAGE + ((i << 4) ^ swz));
+            unsigned z[PER];
+#pragma unroll
+            for (int e = 0; e < PER; ++e) z[e] = a.w.zeros && ci * PER + e < gs ? z_at[(long)(ci * PER + e) * z_step] : 8u;
             __syncwarp();
             if (lane == 0) bar_arrive(w_empty + 8 * ws);
             ok = w_wait(a_empty + 8 * (half * 2 + slot), ((uint32_t)(ci >> 1) & 1u) ^ 1u, &s_abort, nullptr);
             if (!ok) break;
             fence_after();
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {                       // 64 elements: 32 columns
-                uint32_t p[32];
+            for (int i = 0; i < 4; ++i) {                       // 32 elements: 16 columns
+                const uint32_t both = (0x4300u + z[i * 32 / GROUP]) * 0x10001u;
+                const __nv_bfloat162 off = *reinterpret_cast<const __nv_bfloat162 *>(&both);
+                const uint32_t f[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+                uint32_t p[16];
 #pragma unroll
-                for (int v = 0; v < 8; ++v) {
-                    const int word = 8 * h + v;
-                    const unsigned z = 0x4300u + zero_at(ci * PER + word * 8 / GROUP);
-                    const uint32_t both = z | z << 16;
-                    const uint4 &f = q[word >> 2];
-                    const uint32_t c = (word & 3) == 0 ? f.x : (word & 3) == 1 ? f.y : (word & 3) == 2 ? f.z : f.w;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) p[4 * v + i] = pair_of(c >> (4 * i), *reinterpret_cast<const __nv_bfloat162 *>(&both));
-                }
-                tmem_st32(t_a + slot * 64 + 32 * h, p);
+                for (int c = 0; c < 16; ++c) p[c] = pair_of_byte(f[c >> 2], c & 3, off);
+                tmem_st16(t_a + 16 * i, p);
             }
+            tmem_st_wait();
             fence_before();
-            bar_arrive(a_full + 8 * (half * 2 + slot));
-            if (ci > 0) promote(ci - 1);
+            __syncwarp();
+            if (lane == 0) bar_arrive(a_full + 8 * (half * 2 + slot));
         }
-        if (ok) promote(nc - 1);
+        done();
+    } else if (warp < CODE_WARPS + SUM_WARPS) {
+        // ---- sums to totals -------------------------------------------------------------------------
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::R_SUM));
+        const int half = (warp - CODE_WARPS) >> 2, out = tid - CODE_WARPS * 32;
+        if (a.staged) {
+            stage(s_scales, a.w.scales, SPITCH, out, SUM_WARPS * 32);
+            asm volatile("bar.sync 2, 256;" ::: "memory");
+        }
+        const bf16 *const s_at = a.staged ? s_scales + out : a.w.scales + (long)(j0 + min(out, outs - 1)) * a.w.groups + g0;
+        const int s_step = a.staged ? SPITCH : 1;
+        const uint32_t t_d = tmem + ((uint32_t)(warp & 3) << 21) + half * L::T_HALF + L::T_D;
+        float total[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) total[i] = 0.f;
+        bool ok = true;
+        for (int gi = 0; gi < nc * PER; ++gi) {
+            const int ds = gi % DS;
+            const float s = gi < gs && out < outs ? __bfloat162float(s_at[(long)gi * s_step]) : 0.f;
+            ok = w_wait(d_full + 8 * (half * DS + ds), (uint32_t)(gi / DS) & 1u, &s_abort, nullptr);
+            if (!ok) break;
+            fence_after();
+            constexpr int STEP = 16;
+#pragma unroll
+            for (int i0 = 0; i0 < N; i0 += STEP) {
+                uint32_t d[STEP];
+                tmem_ld16(t_d + ds * N + i0, d);
+                if (i0 + STEP == N) {
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(d_empty + 8 * (half * DS + ds));
+                }
+#pragma unroll
+                for (int i = 0; i < STEP; ++i) total[i0 + i] = fmaf(s, __uint_as_float(d[i]), total[i0 + i]);
+            }
+        }
         if (!ok || s_abort)
 #pragma unroll
             for (int i = 0; i < N; ++i) total[i] = NAN;
-    } else if (warp < 8 + X_WARPS) {
-        // ---- rows of x --------------------------------------------------------------------------
+        done();
+        const int j = j0 + out;
+        if (a.split > 1) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) reinterpret_cast<float *>(smem)[i * OUT + out] = total[i];
+        } else if (j < a.w.o) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (i < rows) {
+                    float *at = a.y + (long)(i0 + i) * a.ldy + j;
+                    *at = a.accumulate ? *at + total[i] : total[i];
+                }
+            }
+        }
+    } else if (warp < CODE_WARPS + SUM_WARPS + 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::R_ISSUE));
+        const int role = warp - CODE_WARPS - SUM_WARPS;
+        if (role < 2 && lane == 0) {
+            // ---- MMAs of a half ---------------------------------------------------------------------
+            const int half = role;
+            const uint32_t id = idesc(TILE, N, 0), t = tmem + half * L::T_HALF;
+            bool ok = true;
+            for (int ci = 0; ci < nc && ok; ++ci) {
+                const int xs = ci % XS, slot = ci & 1;
+                ok = t_wait(x_full + 8 * xs, ci, XS, &s_abort) && t_wait(a_full + 8 * (half * 2 + slot), ci, 2, &s_abort);
+                const uint64_t d_x = sdesc(base + L::X + xs * L::XSTAGE, 16, 1024);
+#pragma unroll
+                for (int e = 0; e < PER; ++e) {
+                    const int gi = ci * PER + e, ds = gi % DS;
+                    ok = ok && t_wait(d_empty + 8 * (half * DS + ds), gi + DS, DS, &s_abort);
+                    if (!ok) break;
+                    fence_after();
+#pragma unroll
+                    for (int kk = 0; kk < GROUP / 16; ++kk) {
+                        const int k16 = e * (GROUP / 16) + kk;
+#pragma unroll
+                        for (int p = 0; p < P; ++p)
+                            w_mma_ts(1, t + L::T_D + ds * N, t + L::T_A + slot * 64 + k16 * 8,
+                                     d_x + ((p * L::XPLANE + (k16 >> 2) * L::XBOX + (k16 & 3) * 32) >> 4), id, kk > 0 || p > 0);
+                    }
+                    w_commit(1, d_full + 8 * (half * DS + ds));
+                }
+                if (ok) {
+                    w_commit(1, a_empty + 8 * (half * 2 + slot));
+                    w_commit(1, x_empty + 8 * xs);
+                }
+            }
+        } else if (role == 2 && lane == 0) {
+            // ---- copies -----------------------------------------------------------------------------
+            int w_done = 0, x_done = 0;
+            while (w_done < nc && !s_abort) {
+                if (!L::SPLIT && x_done < nc && x_done < w_done + 2) {     // x is used a little after the codes
+                    const int xs = x_done % XS;
+                    if (!t_wait(x_empty + 8 * xs, x_done + XS, XS, &s_abort)) break;
+                    const uint32_t to = base + L::X + xs * L::XSTAGE;
+                    w_expect_tx(1, x_full + 8 * xs, L::XSTAGE);
+                    w_tma2d(1, to, &x_map, (c0 + x_done) * CHUNK, i0, x_full + 8 * xs);
+                    w_tma2d(1, to + L::XBOX, &x_map, (c0 + x_done) * CHUNK + 64, i0, x_full + 8 * xs);
+                    ++x_done;
+                    continue;
+                }
+                const int ws = w_done % WS;
+                if (!t_wait(w_empty + 8 * ws, w_done + WS, WS, &s_abort)) break;
+                const uint32_t to = base + L::W + ws * WSTAGE;
+                w_expect_tx(1, w_full + 8 * ws, WSTAGE);
+                w_tma2d(1, to, &map, (c0 + w_done) * (CHUNK / 2), j0, w_full + 8 * ws);
+                w_tma2d(1, to + WBOX, &map, (c0 + w_done) * (CHUNK / 2), j0 + TILE, w_full + 8 * ws);
+                ++w_done;
+            }
+            if (s_abort) {                                      // copies in flight land before the CTA goes on
+                volatile int never = 0;
+                for (int i = max(w_done - WS, 0); i < w_done; ++i) bar_wait_slow(w_full + 8 * (i % WS), (uint32_t)(i / WS) & 1u, &never, nullptr);
+                for (int i = max(x_done - XS, 0); i < x_done; ++i) bar_wait_slow(x_full + 8 * (i % XS), (uint32_t)(i / XS) & 1u, &never, nullptr);
+            }
+        }
+        __syncwarp();
+        done();
+    } else if constexpr (L::SPLIT) {
+        // ---- fp32 rows of x ------------------------------------------------------------------------
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::R_X));
         const T *const x = static_cast<const T *>(a.x) + (long)i0 * a.ldx;
-        for (int ci = warp - 8; ci < nc && warp - 8 < XS; ci += XS) {
+        const int w = warp - (CODE_WARPS + SUM_WARPS + 4);
+        for (int ci = w; ci < nc && w < XS; ci += XS) {
             const int slot = ci % XS;
             if (!w_wait(x_empty + 8 * slot, ((uint32_t)(ci / XS) & 1u) ^ 1u, &s_abort, nullptr)) break;
             const uint32_t to = base + L::X + slot * L::XSTAGE;
             const int k0 = (c0 + ci) * CHUNK;
-            constexpr int BATCH = N / 2 < 8 ? N / 2 : 8;
+            constexpr int BATCH = 4;
             for (int b = 0; b < N / 2; b += BATCH) {
                 Octet<T> o[BATCH];
 #pragma unroll
@@ -233,7 +353,7 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const Args a) {
                 for (int i = 0; i < BATCH; ++i) {
                     const int n = ((b + i) * 32 + lane) >> 4, c = lane & 15;
                     uint32_t v[P][4];
-                    o[i].pairs(v);
+                    o[i].planes(v);
 #pragma unroll
                     for (int p = 0; p < P; ++p)
                         sts16(to + p * L::XPLANE + (c >> 3) * L::XBOX + n * 128 + (((c & 7) ^ (n & 7)) << 4), v[p]);
@@ -243,97 +363,33 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const Args a) {
             __syncwarp();
             if (lane == 0) bar_arrive(x_full + 8 * slot);
         }
-    } else if (warp == 12) {
-        // ---- MMAs ---------------------------------------------------------------------------------
-        const uint32_t on = elect_one(), id = idesc(TILE, N, 0);
-        bool ok = true;
-        for (int ci = 0; ci < nc && ok; ++ci) {
-            const int xs = ci % XS, slot = ci & 1;
-            ok = w_wait(x_full + 8 * xs, (uint32_t)(ci / XS) & 1u, &s_abort, nullptr);
-            const uint64_t d_x = sdesc(base + L::X + xs * L::XSTAGE, 16, 1024);
-            for (int half = 0; half < 2 && ok; ++half) {
-                ok = w_wait(a_full + 8 * (half * 2 + slot), (uint32_t)(ci >> 1) & 1u, &s_abort, nullptr);
-                const uint32_t t = tmem + half * L::T_HALF;
-#pragma unroll
-                for (int e = 0; e < PER; ++e) {
-                    const int gi = ci * PER + e, ds = gi % DS;
-                    if (ok) ok = w_wait(d_empty + 8 * (half * DS + ds), ((uint32_t)(gi / DS) & 1u) ^ 1u, &s_abort, nullptr);
-                    if (!ok) break;
-                    fence_after();
-#pragma unroll
-                    for (int kk = 0; kk < GROUP / 16; ++kk) {
-                        const int k16 = e * (GROUP / 16) + kk;
-#pragma unroll
-                        for (int p = 0; p < P; ++p)
-                            w_mma_ts(on, t + L::T_D + ds * N, t + L::T_A + slot * 64 + k16 * 8,
-                                     d_x + ((p * L::XPLANE + (k16 >> 2) * L::XBOX + (k16 & 3) * 32) >> 4), id, kk > 0 || p > 0);
-                    }
-                    w_commit(on, d_full + 8 * (half * DS + ds));
-                }
-                if (ok) w_commit(on, a_empty + 8 * (half * 2 + slot));
-            }
-            if (ok) w_commit(on, x_empty + 8 * xs);
-        }
-        __syncwarp();
-    } else {
-        // ---- copies of codes ---------------------------------------------------------------------
-        const uint32_t on = elect_one();
-        int filled = 0;
-        for (; filled < nc; ++filled) {
-            const int ws = filled % WS;
-            if (!w_wait(w_empty + 8 * ws, ((uint32_t)(filled / WS) & 1u) ^ 1u, &s_abort, nullptr)) break;
-            const uint32_t to = base + L::W + ws * WSTAGE;
-            w_expect_tx(on, w_full + 8 * ws, WSTAGE);
-            w_tma2d(on, to, &map, (c0 + filled) * (CHUNK / 2), j0, w_full + 8 * ws);
-            w_tma2d(on, to + WBOX, &map, (c0 + filled) * (CHUNK / 2), j0 + TILE, w_full + 8 * ws);
-        }
-        if (s_abort) {                                          // copies in flight land before the CTA goes on
-            volatile int never = 0;
-            for (int i = max(filled - WS, 0); i < filled; ++i) bar_wait_slow(w_full + 8 * (i % WS), (uint32_t)(i / WS) & 1u, &never, nullptr);
-        }
-        __syncwarp();
+        done();
     }
-    fence_before();
-    __syncthreads();
-    if (warp == 12) {
+    if (warp == 24) {
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }
 
+    if (a.split == 1) return;
     float *const y = a.y + (long)i0 * a.ldy;
-    if (a.split == 1) {
-        const int j = j0 + warp * 32 + lane;
-        if (warp < 8 && j < a.w.o) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if (i < rows) {
-                    float *at = y + (long)i * a.ldy + j;
-                    *at = a.accumulate ? *at + total[i] : total[i];
-                }
-            }
-        }
-        return;
-    }
-    float *const buf = reinterpret_cast<float *>(smem);         // [N][OUT]
-    if (warp < 8)
-#pragma unroll
-        for (int i = 0; i < N; ++i) buf[i * OUT + tid] = total[i];
-    cluster_sync();
-    if (warp < 8) {
-        const int j = j0 + tid;
-        for (int i = rank; i < rows; i += a.split) {
-            float v = 0.f;
-            for (int r = 0; r < a.split; ++r) v += peer_value(base + (i * OUT + tid) * 4, r);
-            if (j < a.w.o) {
-                float *at = y + (long)i * a.ldy + j;
-                *at = a.accumulate ? *at + v : v;
-            }
+    cluster_sync();                                             // totals [N][OUT] of every CTA
+    // a part of the rows of x for each CTA, a row for each eight warps
+    for (int i = rank + a.split * (tid / OUT); i < rows; i += a.split * (L::THREADS / OUT)) {
+        const int o = tid % OUT;
+        if (tid >= L::THREADS / OUT * OUT) break;
+        float v = 0.f;
+        for (int r = 0; r < a.split; ++r) v += peer_value(base + (i * OUT + o) * 4, r);
+        if (j0 + o < a.w.o) {
+            float *at = y + (long)i * a.ldy + j0 + o;
+            *at = a.accumulate ? *at + v : v;
         }
     }
     cluster_sync();
 }
 
-bool code_map(const Weight &w, CUtensorMap *map) {
+// A matrix of `rows` rows of `bytes` bytes (a multiple of 16), `pitch` apart, as boxes of inner x height elements.
+bool make_map(CUtensorMap *map, CUtensorMapDataType type, int size, const void *p, long width, long rows, long pitch, int inner, int height,
+              CUtensorMapSwizzle swizzle) {
     static PFN_cuTensorMapEncodeTiled_v12000 encode = [] {
         cudaDriverEntryPointQueryResult q;
         void *fn = nullptr;
@@ -343,18 +399,22 @@ bool code_map(const Weight &w, CUtensorMap *map) {
         return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
     }();
     if (!encode) return false;
-    memset(map, 0, sizeof *map);
-    const cuuint64_t dims[2] = {(cuuint64_t)w.k / 2, (cuuint64_t)w.o};
-    const cuuint64_t strides[1] = {(cuuint64_t)w.k / 2};
-    const cuuint32_t box[2] = {CHUNK / 2, TILE};
+    const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)pitch * size};
+    const cuuint32_t box[2] = {(cuuint32_t)inner, (cuuint32_t)height};
     const cuuint32_t estr[2] = {1, 1};
-    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, w.codes, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return encode(map, type, 2, const_cast<void *>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <typename T, int GROUP, int N>
-cudaError_t launch(const CUtensorMap &map, Args a, cudaStream_t s) {
+cudaError_t launch(Args a, cudaStream_t s) {
     using L = Lay<T, GROUP, N>;
+    CUtensorMap map, x_map;
+    memset(&x_map, 0, sizeof x_map);
+    if (!make_map(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.w.codes, a.w.k / 2, a.w.o, a.w.k / 2, CHUNK / 2, TILE, CU_TENSOR_MAP_SWIZZLE_64B) ||
+        (!L::SPLIT && !make_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.x, a.w.k, a.m, a.ldx, 64, N, CU_TENSOR_MAP_SWIZZLE_128B)))
+        return cudaErrorUnknown;
     const int chunks = (a.w.k + CHUNK - 1) / CHUNK, tiles = (a.w.o + OUT - 1) / OUT, cols = (a.m + N - 1) / N;
     a.split = std::max(1, std::min({8, chunks, 152 / std::max(1, tiles * cols)}));
     const int slice = (chunks + a.split - 1) / a.split * L::PER;
@@ -366,7 +426,7 @@ cudaError_t launch(const CUtensorMap &map, Args a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3(tiles * a.split, cols);
-    lc.blockDim = THREADS;
+    lc.blockDim = L::THREADS;
     lc.dynamicSmemBytes = smem;
     lc.stream = s;
     cudaLaunchAttribute at[2];
@@ -377,24 +437,22 @@ cudaError_t launch(const CUtensorMap &map, Args a, cudaStream_t s) {
     at[1].val.programmaticStreamSerializationAllowed = 1;
     lc.attrs = at;
     lc.numAttrs = programmatic(s) ? 2 : 1;
-    e = cudaLaunchKernelEx(&lc, linear4_tc_kernel<T, GROUP, N>, map, a);
+    e = cudaLaunchKernelEx(&lc, linear4_tc_kernel<T, GROUP, N>, map, x_map, a);
     note_launch();
     return e;
 }
 
 template <typename T, int GROUP>
-cudaError_t launch_n(const CUtensorMap &map, const Args &a, cudaStream_t s) {
-    return a.m <= 16 ? launch<T, GROUP, 16>(map, a, s) : a.m <= 32 ? launch<T, GROUP, 32>(map, a, s) : launch<T, GROUP, 64>(map, a, s);
+cudaError_t launch_n(const Args &a, cudaStream_t s) {
+    return a.m <= 16 ? launch<T, GROUP, 16>(a, s) : a.m <= 32 ? launch<T, GROUP, 32>(a, s) : launch<T, GROUP, 64>(a, s);
 }
 
 }  // namespace
 
 template <typename T>
 cudaError_t launch_linear4_tc(const T *x, long ldx, int m, const Weight &w, float *y, long ldy, int accumulate, cudaStream_t s) {
-    CUtensorMap map;
-    if (!code_map(w, &map)) return cudaErrorUnknown;
     const Args a{w, x, ldx, ldy, y, m, accumulate, 1, 0, 0};
-    return w.group == 128 ? launch_n<T, 128>(map, a, s) : w.group == 64 ? launch_n<T, 64>(map, a, s) : launch_n<T, 32>(map, a, s);
+    return w.group == 128 ? launch_n<T, 128>(a, s) : w.group == 64 ? launch_n<T, 64>(a, s) : launch_n<T, 32>(a, s);
 }
 
 template cudaError_t launch_linear4_tc<float>(const float *, long, int, const Weight &, float *, long, int, cudaStream_t);
