@@ -11,9 +11,10 @@
 // A CTA (one an SM: it holds all of the tensor memory) has 256 outputs, two halves of 128, and up to N rows of x; K is
 // cut between the CTAs of a cluster where there are fewer tiles than SMs, and their totals meet through distributed
 // shared memory in rank order. Chunks are 128 elements of K. Roles:
-//   warps 0-15   a row of W a thread: codes -> tensor memory; four warps for the even chunks of a half, four for the odd ones
-//   warps 16-23  a row of W a thread: a group's sum from tensor memory, scaled, into fp32 totals
-//   warps 24-27  MMAs of a half each, copies of codes and of bf16 x
+//   warps 0-3    MMAs of a half each, copies of codes, copies of bf16 x (first, since a scheduler prefers them: as the
+//                last warps, an MMA's issue took them 100 cycles)
+//   warps 4-11   a row of W a thread: a group's sum from tensor memory, scaled, into fp32 totals
+//   warps 12-27  a row of W a thread: codes -> tensor memory; four warps for the even chunks of a half, four for the odd ones
 //   warps 28-31  (fp32 x only) x as three bf16 planes that add up to it, swizzled as the MMA reads them
 // What bounds it is the integer pipe: 8 selections for 8 codes, at half a warp a cycle, 512 cycles for a chunk of 256 outputs
 // (an MMA of such a chunk takes 128 to 512, a copy 330 at the rate of memory). One group of warps a half doing everything in turn
@@ -34,6 +35,7 @@ constexpr int TILE = 128, CHUNK = 128, OUT = 256;
 constexpr uint32_t WBOX = TILE * CHUNK / 2, WSTAGE = 2 * WBOX;
 constexpr uint32_t SMEM_MOST = 227 * 1024 - 2048;               // less static shared memory
 constexpr int CODE_WARPS = 16, SUM_WARPS = 8, X_WARPS = 4;
+constexpr int SUM_0 = 4, CODE_0 = SUM_0 + SUM_WARPS, X_0 = CODE_0 + CODE_WARPS;        // first warps of the roles
 
 template <typename T, int GROUP, int N>
 struct Lay {
@@ -90,10 +92,9 @@ __device__ __forceinline__ uint32_t pair_of_byte(uint32_t word, int i, __nv_bflo
     return *reinterpret_cast<const uint32_t *>(&d);
 }
 
-// One thread waits.
-__device__ __forceinline__ bool t_wait(uint32_t bar, int use, int lap, volatile int *abort) {
-    const uint32_t parity = (uint32_t)(use / lap) & 1u;
-    return bar_try(bar, parity) || bar_wait_slow(bar, parity, abort, nullptr);
+// A warp waits for the barrier's use-th completion (in laps of `lap` uses).
+__device__ __forceinline__ bool use_wait(uint32_t bar, int use, int lap, volatile int *abort) {
+    return w_wait(bar, (uint32_t)(use / lap) & 1u, abort, nullptr);
 }
 
 template <typename T, int GROUP, int N>
@@ -136,7 +137,7 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
         if constexpr (!L::SPLIT) asm volatile("prefetch.tensormap [%0];" ::"l"(&x_map) : "memory");
     }
-    if (warp == 24) {
+    if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(su32(&s_tmem)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -172,12 +173,12 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
 
     // every role ends here: stages, accumulators and codes are done with
     const auto done = [] { fence_before(); asm volatile("bar.sync 3, %0;" ::"n"(L::THREADS) : "memory"); };
-    if (warp < CODE_WARPS) {
+    if (warp >= CODE_0 && warp < X_0) {
         // ---- codes to tensor memory ---------------------------------------------------------------
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::R_CODE));
-        const int half = warp >> 3, slot = warp >> 2 & 1, row = (warp & 3) * 32 + lane, out = half * TILE + row;
+        const int half = (warp - CODE_0) >> 3, slot = (warp - CODE_0) >> 2 & 1, row = (warp & 3) * 32 + lane, out = half * TILE + row;
         if (a.staged && a.w.zeros) {
-            stage(s_zeros, a.w.zeros, ZPITCH, tid, CODE_WARPS * 32);
+            stage(s_zeros, a.w.zeros, ZPITCH, tid - CODE_0 * 32, CODE_WARPS * 32);
             asm volatile("bar.sync 1, 512;" ::: "memory");
         }
         const uint32_t t_a = tmem + ((uint32_t)(warp & 3) << 21) + half * L::T_HALF + L::T_A + slot * 64;
@@ -216,10 +217,10 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             if (lane == 0) bar_arrive(a_full + 8 * (half * 2 + slot));
         }
         done();
-    } else if (warp < CODE_WARPS + SUM_WARPS) {
+    } else if (warp >= SUM_0 && warp < CODE_0) {
         // ---- sums to totals -------------------------------------------------------------------------
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::R_SUM));
-        const int half = (warp - CODE_WARPS) >> 2, out = tid - CODE_WARPS * 32;
+        const int half = (warp - SUM_0) >> 2, out = tid - SUM_0 * 32;
         if (a.staged) {
             stage(s_scales, a.w.scales, SPITCH, out, SUM_WARPS * 32);
             asm volatile("bar.sync 2, 256;" ::: "memory");
@@ -268,22 +269,22 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
                 }
             }
         }
-    } else if (warp < CODE_WARPS + SUM_WARPS + 4) {
+    } else if (warp < SUM_0) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::R_ISSUE));
-        const int role = warp - CODE_WARPS - SUM_WARPS;
-        if (role < 2 && lane == 0) {
+        const uint32_t on = elect_one();                        // (whole warps: addresses stay in uniform registers)
+        if (warp < 2) {
             // ---- MMAs of a half ---------------------------------------------------------------------
-            const int half = role;
+            const int half = warp;
             const uint32_t id = idesc(TILE, N, 0), t = tmem + half * L::T_HALF;
             bool ok = true;
             for (int ci = 0; ci < nc && ok; ++ci) {
                 const int xs = ci % XS, slot = ci & 1;
-                ok = t_wait(x_full + 8 * xs, ci, XS, &s_abort) && t_wait(a_full + 8 * (half * 2 + slot), ci, 2, &s_abort);
+                ok = use_wait(x_full + 8 * xs, ci, XS, &s_abort) && use_wait(a_full + 8 * (half * 2 + slot), ci, 2, &s_abort);
                 const uint64_t d_x = sdesc(base + L::X + xs * L::XSTAGE, 16, 1024);
 #pragma unroll
                 for (int e = 0; e < PER; ++e) {
                     const int gi = ci * PER + e, ds = gi % DS;
-                    ok = ok && t_wait(d_empty + 8 * (half * DS + ds), gi + DS, DS, &s_abort);
+                    ok = ok && use_wait(d_empty + 8 * (half * DS + ds), gi + DS, DS, &s_abort);
                     if (!ok) break;
                     fence_after();
 #pragma unroll
@@ -291,42 +292,42 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
                         const int k16 = e * (GROUP / 16) + kk;
 #pragma unroll
                         for (int p = 0; p < P; ++p)
-                            w_mma_ts(1, t + L::T_D + ds * N, t + L::T_A + slot * 64 + k16 * 8,
+                            w_mma_ts(on, t + L::T_D + ds * N, t + L::T_A + slot * 64 + k16 * 8,
                                      d_x + ((p * L::XPLANE + (k16 >> 2) * L::XBOX + (k16 & 3) * 32) >> 4), id, kk > 0 || p > 0);
                     }
-                    w_commit(1, d_full + 8 * (half * DS + ds));
+                    w_commit(on, d_full + 8 * (half * DS + ds));
                 }
                 if (ok) {
-                    w_commit(1, a_empty + 8 * (half * 2 + slot));
-                    w_commit(1, x_empty + 8 * xs);
+                    w_commit(on, a_empty + 8 * (half * 2 + slot));
+                    w_commit(on, x_empty + 8 * xs);
                 }
             }
-        } else if (role == 2 && lane == 0) {
-            // ---- copies -----------------------------------------------------------------------------
-            int w_done = 0, x_done = 0;
-            while (w_done < nc && !s_abort) {
-                if (!L::SPLIT && x_done < nc && x_done < w_done + 2) {     // x is used a little after the codes
-                    const int xs = x_done % XS;
-                    if (!t_wait(x_empty + 8 * xs, x_done + XS, XS, &s_abort)) break;
-                    const uint32_t to = base + L::X + xs * L::XSTAGE;
-                    w_expect_tx(1, x_full + 8 * xs, L::XSTAGE);
-                    w_tma2d(1, to, &x_map, (c0 + x_done) * CHUNK, i0, x_full + 8 * xs);
-                    w_tma2d(1, to + L::XBOX, &x_map, (c0 + x_done) * CHUNK + 64, i0, x_full + 8 * xs);
-                    ++x_done;
-                    continue;
+        } else if (warp == 2 || !L::SPLIT) {
+            // ---- copies of codes, of x ----------------------------------------------------------------
+            const bool codes = warp == 2;
+            const uint32_t full = codes ? w_full : x_full, empty = codes ? w_empty : x_empty;
+            const int stages = codes ? WS : XS;
+            int filled = 0;
+            for (; filled < nc; ++filled) {
+                const int st = filled % stages;
+                if (!use_wait(empty + 8 * st, filled + stages, stages, &s_abort)) break;
+                const uint32_t bar = full + 8 * st;
+                if (codes) {
+                    const uint32_t to = base + L::W + st * WSTAGE;
+                    w_expect_tx(on, bar, WSTAGE);
+                    w_tma2d(on, to, &map, (c0 + filled) * (CHUNK / 2), j0, bar);
+                    w_tma2d(on, to + WBOX, &map, (c0 + filled) * (CHUNK / 2), j0 + TILE, bar);
+                } else {
+                    const uint32_t to = base + L::X + st * L::XSTAGE;
+                    w_expect_tx(on, bar, L::XSTAGE);
+                    w_tma2d(on, to, &x_map, (c0 + filled) * CHUNK, i0, bar);
+                    w_tma2d(on, to + L::XBOX, &x_map, (c0 + filled) * CHUNK + 64, i0, bar);
                 }
-                const int ws = w_done % WS;
-                if (!t_wait(w_empty + 8 * ws, w_done + WS, WS, &s_abort)) break;
-                const uint32_t to = base + L::W + ws * WSTAGE;
-                w_expect_tx(1, w_full + 8 * ws, WSTAGE);
-                w_tma2d(1, to, &map, (c0 + w_done) * (CHUNK / 2), j0, w_full + 8 * ws);
-                w_tma2d(1, to + WBOX, &map, (c0 + w_done) * (CHUNK / 2), j0 + TILE, w_full + 8 * ws);
-                ++w_done;
             }
             if (s_abort) {                                      // copies in flight land before the CTA goes on
                 volatile int never = 0;
-                for (int i = max(w_done - WS, 0); i < w_done; ++i) bar_wait_slow(w_full + 8 * (i % WS), (uint32_t)(i / WS) & 1u, &never, nullptr);
-                for (int i = max(x_done - XS, 0); i < x_done; ++i) bar_wait_slow(x_full + 8 * (i % XS), (uint32_t)(i / XS) & 1u, &never, nullptr);
+                for (int i = max(filled - stages, 0); i < filled; ++i)
+                    bar_wait_slow(full + 8 * (i % stages), (uint32_t)(i / stages) & 1u, &never, nullptr);
             }
         }
         __syncwarp();
@@ -335,7 +336,7 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         // ---- fp32 rows of x ------------------------------------------------------------------------
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::R_X));
         const T *const x = static_cast<const T *>(a.x) + (long)i0 * a.ldx;
-        const int w = warp - (CODE_WARPS + SUM_WARPS + 4);
+        const int w = warp - X_0;
         for (int ci = w; ci < nc && w < XS; ci += XS) {
             const int slot = ci % XS;
             if (!w_wait(x_empty + 8 * slot, ((uint32_t)(ci / XS) & 1u) ^ 1u, &s_abort, nullptr)) break;
@@ -365,7 +366,7 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         }
         done();
     }
-    if (warp == 24) {
+    if (warp == 0) {
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }
@@ -407,6 +408,23 @@ bool make_map(CUtensorMap *map, CUtensorMapDataType type, int size, const void *
                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Into how many parts K is cut. A part is a CTA that has an SM to itself, so what counts is how many clusters of that size fit the
+// GPU at once (GPCs have 16 to 20 SMs: 152, 76, 46, 36, 28, 23, 15 and 15 were counted) and what a CTA does beside its chunks:
+// about 6 chunks' time to start and to end, 3 more to join.
+int best_split(long tiles, int chunks) {
+    constexpr int fit[8] = {152, 76, 46, 36, 28, 23, 15, 15};
+    int best = 1;
+    long least = -1;
+    for (int s = 1; s <= 8 && s <= chunks; ++s) {
+        const long cost = (tiles + fit[s - 1] - 1) / fit[s - 1] * ((chunks + s - 1) / s + 6 + (s > 1 ? 3 : 0));
+        if (least < 0 || cost < least) {
+            least = cost;
+            best = s;
+        }
+    }
+    return best;
+}
+
 template <typename T, int GROUP, int N>
 cudaError_t launch(Args a, cudaStream_t s) {
     using L = Lay<T, GROUP, N>;
@@ -416,7 +434,7 @@ cudaError_t launch(Args a, cudaStream_t s) {
         (!L::SPLIT && !make_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.x, a.w.k, a.m, a.ldx, 64, N, CU_TENSOR_MAP_SWIZZLE_128B)))
         return cudaErrorUnknown;
     const int chunks = (a.w.k + CHUNK - 1) / CHUNK, tiles = (a.w.o + OUT - 1) / OUT, cols = (a.m + N - 1) / N;
-    a.split = std::max(1, std::min({8, chunks, 152 / std::max(1, tiles * cols)}));
+    a.split = best_split(tiles * cols, chunks);
     const int slice = (chunks + a.split - 1) / a.split * L::PER;
     const size_t beside = (size_t)slice * ((OUT + 2) * 2 + (a.w.zeros ? OUT + 4 : 0));
     a.staged = beside <= L::ROOM;
