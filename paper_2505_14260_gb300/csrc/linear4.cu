@@ -387,8 +387,13 @@ msd_status msd_linear4(const void *x, int64_t ldx, int32_t x_dtype, int32_t m, c
     if (m == 0) return MSD_OK;
     if (bad_rows(x, ldx, x_dtype, w.k) || !y || ldy < w.o || reinterpret_cast<uintptr_t>(y) % 4) return MSD_ERR_INVALID;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    // tensor copies take rows of codes that start on 16 bytes
-    const bool tc = reinterpret_cast<uintptr_t>(w.codes) % 16 == 0 && w.k % 32 == 0 && m > (x_dtype == MSD_F32 ? 3 : 16);
+    // Which of the two: measured with 1 to 16 rows, k and o of 4096 and 11008. The warps of a few rows win up to 8 rows (fp32: 3, a
+    // tile of B operands) while their CTAs of 32 outputs fit the GPU at once (o 4096, k 11008, groups of 128: 12.0 us, 14.6 on
+    // tcgen05; 16 rows, k 4096: 7.6 and 9.9), and with one scale for 128 codes of bf16 rows (o 11008: 11.7 and 12.5; with 64 codes 19.2 and 14.0).
+    // Tensor copies take rows of codes that start on 16 bytes.
+    const bool f32 = x_dtype == MSD_F32, small = w.o <= 32 * 152;
+    const bool few = m <= (f32 ? 3 : 8) ? small || (!f32 && w.group == 128) : !f32 && m <= 16 && (long)w.o * w.k <= 20l << 20;
+    const bool tc = !few && reinterpret_cast<uintptr_t>(w.codes) % 16 == 0 && w.k % 32 == 0;
     const auto run = [&](auto *p) {
         return tc ? launch_linear4_tc(p, (long)ldx, m, w, y, (long)ldy, accumulate, s) : launch_few(p, (long)ldx, m, w, y, (long)ldy, accumulate, s);
     };

@@ -44,17 +44,13 @@ template <> struct Octet<float> {
     }
     __device__ __forceinline__ void clear() { lo = hi = make_float4(0.f, 0.f, 0.f, 0.f); }
     // A value's upper 16 bits, those of what is left, and the 8 bits left then: truncations, so the three parts add
-    // up to it and none overflows. What is not finite goes into the first part alone.
+    // up to it and none overflows. What is not finite leaves NaN in the later parts.
     static __device__ __forceinline__ void part(float a, float c, uint32_t (&b)[3][4], int i) {
-        const uint32_t ua = __float_as_uint(a), uc = __float_as_uint(c);
-        b[0][i] = __byte_perm(ua, uc, 0x7632);
-        float ra = a - __uint_as_float(ua & 0xFFFF0000u), rc = c - __uint_as_float(uc & 0xFFFF0000u);
-        if (!(fabsf(a) < INFINITY)) { ra = 0.f; if (a != a) b[0][i] |= 0x7FC0u; }
-        if (!(fabsf(c) < INFINITY)) { rc = 0.f; if (c != c) b[0][i] |= 0x7FC00000u; }
-        const uint32_t va = __float_as_uint(ra), vc = __float_as_uint(rc);
-        b[1][i] = __byte_perm(va, vc, 0x7632);
-        b[2][i] = __byte_perm(__float_as_uint(ra - __uint_as_float(va & 0xFFFF0000u)),
-                              __float_as_uint(rc - __uint_as_float(vc & 0xFFFF0000u)), 0x7632);
+        const auto upper = [](float v) { return __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); };
+        const float ra = a - upper(a), rc = c - upper(c), la = ra - upper(ra), lc = rc - upper(rc);
+        b[0][i] = __byte_perm(__float_as_uint(a), __float_as_uint(c), 0x7632);
+        b[1][i] = __byte_perm(__float_as_uint(ra), __float_as_uint(rc), 0x7632);
+        b[2][i] = __byte_perm(__float_as_uint(la), __float_as_uint(lc), 0x7632);
     }
     __device__ __forceinline__ void planes(uint32_t (&b)[3][4]) const {          // in the order that they lie in
         part(lo.x, lo.y, b, 0);

@@ -11,11 +11,12 @@
 // A CTA (one an SM: it holds all of the tensor memory) has 256 outputs, two halves of 128, and up to N rows of x; K is
 // cut between the CTAs of a cluster where there are fewer tiles than SMs, and their totals meet through distributed
 // shared memory in rank order. Chunks are 128 elements of K. Roles:
-//   warps 0-3    MMAs of a half each, copies of codes, copies of bf16 x (first, since a scheduler prefers them: as the
-//                last warps, an MMA's issue took them 100 cycles)
-//   warps 4-11   a row of W a thread: a group's sum from tensor memory, scaled, into fp32 totals
-//   warps 12-27  a row of W a thread: codes -> tensor memory; four warps for the even chunks of a half, four for the odd ones
-//   warps 28-31  (fp32 x only) x as three bf16 planes that add up to it, swizzled as the MMA reads them
+//   warps 0-3    MMAs, of the even or the odd chunks of a half (first, since a scheduler prefers them: as the last warps, an
+//                MMA's issue took them 100 cycles)
+//   warps 4-7    x: copies of bf16, put into order; fp32 as three bf16 planes that add up to it, swizzled as the MMA reads them
+//   warps 8-15   a row of W a thread: a group's sum from tensor memory, scaled, into fp32 totals
+//   warps 16-31  a row of W a thread: codes -> tensor memory; four warps for the even chunks of a half, four for the odd ones;
+//                the first of those also issue the copies of codes, four chunks ahead
 // What bounds it is the integer pipe: 8 selections for 8 codes, at half a warp a cycle, 512 cycles for a chunk of 256 outputs
 // (an MMA of such a chunk takes 128 to 512, a copy 330 at the rate of memory). One group of warps a half doing everything in turn
 // took 1800 cycles a chunk, waiting for one another. A wait that runs out (2 s) leaves NaN in the CTA's part of y.
@@ -34,21 +35,22 @@ namespace {
 constexpr int TILE = 128, CHUNK = 128, OUT = 256;
 constexpr uint32_t WBOX = TILE * CHUNK / 2, WSTAGE = 2 * WBOX;
 constexpr uint32_t SMEM_MOST = 227 * 1024 - 2048;               // less static shared memory
-constexpr int CODE_WARPS = 16, SUM_WARPS = 8, X_WARPS = 4;
-constexpr int SUM_0 = 4, CODE_0 = SUM_0 + SUM_WARPS, X_0 = CODE_0 + CODE_WARPS;        // first warps of the roles
+constexpr int CODE_WARPS = 16, SUM_WARPS = 8, THREADS = 1024;
+constexpr int AHEAD = 4;                                        // chunks (even, and less than a ring has stages)
+constexpr int COPY_0 = 4, SUM_0 = 8, CODE_0 = SUM_0 + SUM_WARPS;                   // first warps of the roles
 
 template <typename T, int GROUP, int N>
 struct Lay {
     static constexpr bool SPLIT = sizeof(T) == 4;               // x in planes
     static constexpr int P = Octet<T>::PLANES, PER = CHUNK / GROUP;
-    static constexpr int THREADS = 32 * (CODE_WARPS + SUM_WARPS + 4 + (SPLIT ? X_WARPS : 0));
-    // registers by role: their sum over the groups of four warps is the launch's (72 * 7, 64 * 8)
-    static constexpr int R_CODE = 56, R_SUM = SPLIT ? 96 : 112, R_ISSUE = SPLIT ? 40 : 56, R_X = 56;
-    static_assert(4 * R_CODE + 2 * R_SUM + R_ISSUE + (SPLIT ? R_X : 0) <= (SPLIT ? 64 * 8 : 72 * 7), "");
+    // registers by role: over the eight groups of four warps they are the launch's 64 a thread
+    static constexpr int R_CODE = 56, R_SUM = SPLIT ? 96 : 104, R_ISSUE = 40, R_COPY = SPLIT ? 56 : 40;
+    static_assert(4 * R_CODE + 2 * R_SUM + R_ISSUE + R_COPY <= 64 * 8, "");
     static constexpr uint32_t XBOX = N * 128, XPLANE = 2 * XBOX, XSTAGE = P * XPLANE;
-    static constexpr int XS = XSTAGE > 24 * 1024 ? 2 : 4;
-    static constexpr int WS = XSTAGE > 24 * 1024 ? 5 : 6;
-    static constexpr int DS = 128 / N;                          // accumulators of a half
+    static constexpr int XS = SPLIT && N > 16 ? 2 : 4;          // even: a stage's chunks are all even or all odd ones
+    static constexpr int X_PARTS = SPLIT ? 4 / XS : 1;          // warps that fill a stage of x
+    static constexpr int WS = 6;
+    static constexpr int DS = 128 / N, HS = DS / 2;             // accumulators of a half, of its even or odd chunks
     static constexpr uint32_t X = 0, W = XS * XSTAGE, SCALES = W + WS * WSTAGE;
     static constexpr uint32_t ROOM = SMEM_MOST - 1024 - SCALES; // for scales and zeros
     static constexpr uint32_t T_A = 0, T_D = 128, T_HALF = 256; // columns of a half
@@ -83,34 +85,44 @@ __device__ __forceinline__ void sts16(uint32_t a, const uint32_t *v) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
 
-// Codes 2 i and 2 i + 1 of a word (byte i) less the zero, as a bf16 pair. off: 128 + zero, twice.
-__device__ __forceinline__ uint32_t pair_of_byte(uint32_t word, int i, __nv_bfloat162 off) {
-    uint32_t v;
-    const uint32_t byte = __byte_perm(word, 0, 0x4440 | i);
-    asm("lop3.b32 %0, %1, 0x000F000F, 0x43004300, 0xEA;" : "=r"(v) : "r"(byte * 0x1001u));   // the upper half 12 bits up; (a & b) | c
-    const __nv_bfloat162 d = __hsub2(*reinterpret_cast<__nv_bfloat162 *>(&v), off);
-    return *reinterpret_cast<const uint32_t *>(&d);
+// A warp waits for the barrier's use-th completion (in laps of `lap` uses). It sleeps in the barrier for up to 20 us at a time: what
+// polls takes issue slots, and they are what the kernel runs out of.
+__device__ __forceinline__ bool use_wait_slow(uint32_t bar, uint32_t parity, volatile int *abort) {
+    const unsigned long long t0 = gtime();
+    for (;;) {
+        uint32_t ok;
+        asm volatile(
+            "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.b32 %0, 1, 0, p;\n}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity), "r"(20000u)
+            : "memory");
+        if (__all_sync(0xffffffffu, ok)) return true;
+        if (__any_sync(0xffffffffu, *abort)) return false;
+        if (__any_sync(0xffffffffu, gtime() - t0 > TIMEOUT_NS)) {
+            *abort = 1;
+            return false;
+        }
+    }
 }
-
-// A warp waits for the barrier's use-th completion (in laps of `lap` uses).
 __device__ __forceinline__ bool use_wait(uint32_t bar, int use, int lap, volatile int *abort) {
-    return w_wait(bar, (uint32_t)(use / lap) & 1u, abort, nullptr);
+    const uint32_t parity = (uint32_t)(use / lap) & 1u;
+    return __all_sync(0xffffffffu, bar_try(bar, parity)) || use_wait_slow(bar, parity, abort);
 }
 
 template <typename T, int GROUP, int N>
-__global__ void __launch_bounds__(Lay<T, GROUP, N>::THREADS, 1)
+__global__ void __launch_bounds__(THREADS, 1)
 linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap x_map, const Args a) {
     using L = Lay<T, GROUP, N>;
-    constexpr int PER = L::PER, P = L::P, XS = L::XS, WS = L::WS, DS = L::DS;
+    constexpr int PER = L::PER, P = L::P, XS = L::XS, WS = L::WS, DS = L::DS, HS = L::HS;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * WS + 2 * XS + 8 + 4 * DS];
+    __shared__ __align__(8) uint64_t bars[2 * WS + 3 * XS + 16 + 4 * DS];
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_abort;
     const uint32_t base = (su32(smem_raw) + 1023u) & ~1023u;
     uint8_t *const smem = smem_raw + (base - su32(smem_raw));
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t w_full = su32(bars), w_empty = w_full + 8 * WS, x_full = w_empty + 8 * WS, x_empty = x_full + 8 * XS,
-                   a_full = x_empty + 8 * XS, a_empty = a_full + 32, d_full = a_empty + 32, d_empty = d_full + 16 * DS;
+                   a_full = x_empty + 8 * XS, a_empty = a_full + 64, d_full = a_empty + 64, d_empty = d_full + 16 * DS, x_raw = d_empty + 16 * DS;
     const int rank = (int)(blockIdx.x % a.split), tile = (int)(blockIdx.x / a.split);
     const int j0 = tile * OUT, i0 = (int)blockIdx.y * N, rows = min(N, a.m - i0);
     const int chunks = (a.w.k + CHUNK - 1) / CHUNK;
@@ -121,10 +133,11 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             bar_init(w_empty + 8 * i, 8);
         }
         for (int i = 0; i < XS; ++i) {
-            bar_init(x_full + 8 * i, 1);
+            bar_init(x_full + 8 * i, L::X_PARTS);
             bar_init(x_empty + 8 * i, 2);
+            bar_init(x_raw + 8 * i, 1);
         }
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 8; ++i) {
             bar_init(a_full + 8 * i, 4);
             bar_init(a_empty + 8 * i, 1);
         }
@@ -172,23 +185,38 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     };
 
     // every role ends here: stages, accumulators and codes are done with
-    const auto done = [] { fence_before(); asm volatile("bar.sync 3, %0;" ::"n"(L::THREADS) : "memory"); };
-    if (warp >= CODE_0 && warp < X_0) {
+    const auto done = [] { fence_before(); asm volatile("bar.sync 3, %0;" ::"n"(THREADS) : "memory"); };
+    if (warp >= CODE_0) {
         // ---- codes to tensor memory ---------------------------------------------------------------
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::R_CODE));
         const int half = (warp - CODE_0) >> 3, slot = (warp - CODE_0) >> 2 & 1, row = (warp & 3) * 32 + lane, out = half * TILE + row;
-        if (a.staged && a.w.zeros) {
-            stage(s_zeros, a.w.zeros, ZPITCH, tid - CODE_0 * 32, CODE_WARPS * 32);
-            asm volatile("bar.sync 1, 512;" ::: "memory");
-        }
         const uint32_t t_a = tmem + ((uint32_t)(warp & 3) << 21) + half * L::T_HALF + L::T_A + slot * 64;
         const uint32_t code_row = base + L::W + half * WBOX + row * 64, swz = (uint32_t)(row >> 1 & 3) << 4;
         const uint8_t *const z_at = a.staged ? s_zeros + out : a.w.zeros + (long)(j0 + min(out, outs - 1)) * a.w.groups + g0;
         const int z_step = a.staged ? ZPITCH : 1;
+        const bool copies = warp == CODE_0 || warp == CODE_0 + 4;         // (a warp for the even chunks, one for the odd ones)
+        const uint32_t on = elect_one();
+        int copied = slot;                                      // chunks copied: slot, slot + 2, ... below this
+        const auto copy = [&](int ci) {
+            const int ws = ci % WS;
+            if (!use_wait(w_empty + 8 * ws, ci + WS, WS, &s_abort)) return;
+            const uint32_t to = base + L::W + ws * WSTAGE, bar = w_full + 8 * ws;
+            w_expect_tx(on, bar, WSTAGE);
+            w_tma2d(on, to, &map, (c0 + ci) * (CHUNK / 2), j0, bar);
+            w_tma2d(on, to + WBOX, &map, (c0 + ci) * (CHUNK / 2), j0 + TILE, bar);
+            copied = ci + 2;
+        };
+        if (copies)
+            for (int ci = slot; ci < min(nc, AHEAD); ci += 2) copy(ci);
+        if (a.staged && a.w.zeros) {
+            stage(s_zeros, a.w.zeros, ZPITCH, tid - CODE_0 * 32, CODE_WARPS * 32);
+            asm volatile("bar.sync 1, 512;" ::: "memory");
+        }
         bool ok = true;
         for (int ci = slot; ci < nc && ok; ci += 2) {
             const int ws = ci % WS;
-            ok = w_wait(w_full + 8 * ws, (uint32_t)(ci / WS) & 1u, &s_abort, nullptr);
+            if (copies && ci + AHEAD < nc) copy(ci + AHEAD);
+            ok = use_wait(w_full + 8 * ws, ci, WS, &s_abort);
             if (!ok) break;
             uint4 q[4];
 #pragma unroll
@@ -198,26 +226,37 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             for (int e = 0; e < PER; ++e) z[e] = a.w.zeros && ci * PER + e < gs ? z_at[(long)(ci * PER + e) * z_step] : 8u;
             __syncwarp();
             if (lane == 0) bar_arrive(w_empty + 8 * ws);
-            ok = w_wait(a_empty + 8 * (half * 2 + slot), ((uint32_t)(ci >> 1) & 1u) ^ 1u, &s_abort, nullptr);
-            if (!ok) break;
-            fence_after();
+            // 64 elements at a time, so that the MMAs of the first are done when the next chunk's come
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {                       // 32 elements: 16 columns
-                const uint32_t both = (0x4300u + z[i * 32 / GROUP]) * 0x10001u;
-                const __nv_bfloat162 off = *reinterpret_cast<const __nv_bfloat162 *>(&both);
-                const uint32_t f[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
-                uint32_t p[16];
+            for (int sub = 0; sub < 2; ++sub) {
+                const uint32_t bar = 8 * ((half * 2 + slot) * 2 + sub);
+                ok = ok && use_wait(a_empty + bar, ci + 2, 2, &s_abort);
+                if (!ok) break;
+                fence_after();
 #pragma unroll
-                for (int c = 0; c < 16; ++c) p[c] = pair_of_byte(f[c >> 2], c & 3, off);
-                tmem_st16(t_a + 16 * i, p);
+                for (int i = 2 * sub; i < 2 * sub + 2; ++i) {   // 32 elements: 16 columns
+                    const uint32_t both = (0x4300u + z[i * 32 / GROUP]) * 0x10001u;
+                    const __nv_bfloat162 off = *reinterpret_cast<const __nv_bfloat162 *>(&both);
+                    const uint32_t f[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+                    uint32_t p[16];
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) p[c] = pair_of(f[c >> 2] >> (4 * (c & 3)), off);
+                    tmem_st16(t_a + 16 * i, p);
+                }
+                tmem_st_wait();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(a_full + bar);
             }
-            tmem_st_wait();
-            fence_before();
+        }
+        if (copies && s_abort) {                                // copies in flight land before the CTA goes on
+            volatile int never = 0;
+            for (int ci = slot; ci < copied; ci += 2)
+                if (ci + WS >= copied) bar_wait_slow(w_full + 8 * (ci % WS), (uint32_t)(ci / WS) & 1u, &never, nullptr);
             __syncwarp();
-            if (lane == 0) bar_arrive(a_full + 8 * (half * 2 + slot));
         }
         done();
-    } else if (warp >= SUM_0 && warp < CODE_0) {
+    } else if (warp >= SUM_0) {
         // ---- sums to totals -------------------------------------------------------------------------
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::R_SUM));
         const int half = (warp - SUM_0) >> 2, out = tid - SUM_0 * 32;
@@ -233,9 +272,9 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         for (int i = 0; i < N; ++i) total[i] = 0.f;
         bool ok = true;
         for (int gi = 0; gi < nc * PER; ++gi) {
-            const int ds = gi % DS;
+            const int ci = gi / PER, li = (ci >> 1) * PER + gi % PER, ds = (ci & 1) * HS + li % HS;
             const float s = gi < gs && out < outs ? __bfloat162float(s_at[(long)gi * s_step]) : 0.f;
-            ok = w_wait(d_full + 8 * (half * DS + ds), (uint32_t)(gi / DS) & 1u, &s_abort, nullptr);
+            ok = use_wait(d_full + 8 * (half * DS + ds), li, HS, &s_abort);
             if (!ok) break;
             fence_after();
             constexpr int STEP = 16;
@@ -269,100 +308,110 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
                 }
             }
         }
-    } else if (warp < SUM_0) {
+    } else if (warp < COPY_0) {
+        // ---- MMAs ---------------------------------------------------------------------------------
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::R_ISSUE));
         const uint32_t on = elect_one();                        // (whole warps: addresses stay in uniform registers)
-        if (warp < 2) {
-            // ---- MMAs of a half ---------------------------------------------------------------------
-            const int half = warp;
-            const uint32_t id = idesc(TILE, N, 0), t = tmem + half * L::T_HALF;
-            bool ok = true;
-            for (int ci = 0; ci < nc && ok; ++ci) {
-                const int xs = ci % XS, slot = ci & 1;
-                ok = use_wait(x_full + 8 * xs, ci, XS, &s_abort) && use_wait(a_full + 8 * (half * 2 + slot), ci, 2, &s_abort);
-                const uint64_t d_x = sdesc(base + L::X + xs * L::XSTAGE, 16, 1024);
+        const int half = warp >> 1, slot = warp & 1;
+        const uint32_t id = idesc(TILE, N, 0), t = tmem + half * L::T_HALF;
+        bool ok = true;
+        for (int ci = slot; ci < nc && ok; ci += 2) {
+            const int xs = ci % XS;
+            ok = use_wait(x_full + 8 * xs, ci, XS, &s_abort);
+            const uint64_t d_x = sdesc(base + L::X + xs * L::XSTAGE, 16, 1024);
 #pragma unroll
-                for (int e = 0; e < PER; ++e) {
-                    const int gi = ci * PER + e, ds = gi % DS;
-                    ok = ok && use_wait(d_empty + 8 * (half * DS + ds), gi + DS, DS, &s_abort);
-                    if (!ok) break;
-                    fence_after();
+            for (int e = 0; e < PER; ++e) {
+                const int li = (ci >> 1) * PER + e, ds = slot * HS + li % HS;      // (no accumulator is shared by two warps' waits)
+                ok = ok && use_wait(d_empty + 8 * (half * DS + ds), li + HS, HS, &s_abort);
+                if (!ok) break;
+                fence_after();
 #pragma unroll
-                    for (int kk = 0; kk < GROUP / 16; ++kk) {
-                        const int k16 = e * (GROUP / 16) + kk;
-#pragma unroll
-                        for (int p = 0; p < P; ++p)
-                            w_mma_ts(on, t + L::T_D + ds * N, t + L::T_A + slot * 64 + k16 * 8,
-                                     d_x + ((p * L::XPLANE + (k16 >> 2) * L::XBOX + (k16 & 3) * 32) >> 4), id, kk > 0 || p > 0);
+                for (int kk = 0; kk < GROUP / 16; ++kk) {
+                    const int k16 = e * (GROUP / 16) + kk;
+                    const uint32_t bar = 8 * ((half * 2 + slot) * 2 + (k16 >> 2));
+                    if (k16 % 4 == 0) {
+                        ok = ok && use_wait(a_full + bar, ci, 2, &s_abort);
+                        if (!ok) break;
+                        fence_after();
                     }
-                    w_commit(on, d_full + 8 * (half * DS + ds));
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+                        w_mma_ts(on, t + L::T_D + ds * N, t + L::T_A + slot * 64 + k16 * 8,
+                                 d_x + ((p * L::XPLANE + (k16 >> 2) * L::XBOX + (k16 & 3) * 32) >> 4), id, kk > 0 || p > 0);
+                    if (k16 % 4 == 3) w_commit(on, a_empty + bar);
                 }
-                if (ok) {
-                    w_commit(on, a_empty + 8 * (half * 2 + slot));
-                    w_commit(on, x_empty + 8 * xs);
-                }
+                if (!ok) break;
+                w_commit(on, d_full + 8 * (half * DS + ds));
             }
-        } else if (warp == 2 || !L::SPLIT) {
-            // ---- copies of codes, of x ----------------------------------------------------------------
-            const bool codes = warp == 2;
-            const uint32_t full = codes ? w_full : x_full, empty = codes ? w_empty : x_empty;
-            const int stages = codes ? WS : XS;
-            int filled = 0;
-            for (; filled < nc; ++filled) {
-                const int st = filled % stages;
-                if (!use_wait(empty + 8 * st, filled + stages, stages, &s_abort)) break;
-                const uint32_t bar = full + 8 * st;
-                if (codes) {
-                    const uint32_t to = base + L::W + st * WSTAGE;
-                    w_expect_tx(on, bar, WSTAGE);
-                    w_tma2d(on, to, &map, (c0 + filled) * (CHUNK / 2), j0, bar);
-                    w_tma2d(on, to + WBOX, &map, (c0 + filled) * (CHUNK / 2), j0 + TILE, bar);
-                } else {
-                    const uint32_t to = base + L::X + st * L::XSTAGE;
-                    w_expect_tx(on, bar, L::XSTAGE);
-                    w_tma2d(on, to, &x_map, (c0 + filled) * CHUNK, i0, bar);
-                    w_tma2d(on, to + L::XBOX, &x_map, (c0 + filled) * CHUNK + 64, i0, bar);
-                }
-            }
-            if (s_abort) {                                      // copies in flight land before the CTA goes on
-                volatile int never = 0;
-                for (int i = max(filled - stages, 0); i < filled; ++i)
-                    bar_wait_slow(full + 8 * (i % stages), (uint32_t)(i / stages) & 1u, &never, nullptr);
-            }
+            if (ok) w_commit(on, x_empty + 8 * xs);
         }
         __syncwarp();
         done();
-    } else if constexpr (L::SPLIT) {
-        // ---- fp32 rows of x ------------------------------------------------------------------------
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::R_X));
-        const T *const x = static_cast<const T *>(a.x) + (long)i0 * a.ldx;
-        const int w = warp - X_0;
-        for (int ci = w; ci < nc && w < XS; ci += XS) {
-            const int slot = ci % XS;
-            if (!w_wait(x_empty + 8 * slot, ((uint32_t)(ci / XS) & 1u) ^ 1u, &s_abort, nullptr)) break;
-            const uint32_t to = base + L::X + slot * L::XSTAGE;
-            const int k0 = (c0 + ci) * CHUNK;
-            constexpr int BATCH = 4;
-            for (int b = 0; b < N / 2; b += BATCH) {
-                Octet<T> o[BATCH];
+    } else {
+        // ---- copies of codes, of x ----------------------------------------------------------------
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::R_COPY));
+        const int w = warp - COPY_0;
+        if constexpr (!L::SPLIT) {
+            // a stage a warp: copied, then each 8 values put into the order of the codes' pairs where they lie
+            static_assert(XS == 4, "");
+            const uint32_t on = elect_one(), at = base + L::X + w * L::XSTAGE;
+            int filled = w;
+            for (; filled < nc; filled += XS) {
+                if (!use_wait(x_empty + 8 * w, filled + XS, XS, &s_abort)) break;
+                w_expect_tx(on, x_raw + 8 * w, L::XSTAGE);
+                w_tma2d(on, at, &x_map, (c0 + filled) * CHUNK, i0, x_raw + 8 * w);
+                w_tma2d(on, at + L::XBOX, &x_map, (c0 + filled) * CHUNK + 64, i0, x_raw + 8 * w);
+                if (!use_wait(x_raw + 8 * w, filled, XS, &s_abort)) break;
+#pragma unroll 1
+                for (int b = 0; b < N / 2; b += 4) {
+                    Octet<T> o[4];
 #pragma unroll
-                for (int i = 0; i < BATCH; ++i) {
-                    const int n = ((b + i) * 32 + lane) >> 4, at = k0 + (lane & 15) * 8;
-                    if (n < rows && at < a.w.k) o[i].load(x + (long)n * a.ldx + at); else o[i].clear();
+                    for (int i = 0; i < 4; ++i) o[i].v = lds16(at + ((b + i) * 32 + lane) * 16);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t v[1][4];
+                        o[i].pairs(v);
+                        sts16(at + ((b + i) * 32 + lane) * 16, v[0]);
+                    }
                 }
-#pragma unroll
-                for (int i = 0; i < BATCH; ++i) {
-                    const int n = ((b + i) * 32 + lane) >> 4, c = lane & 15;
-                    uint32_t v[P][4];
-                    o[i].planes(v);
-#pragma unroll
-                    for (int p = 0; p < P; ++p)
-                        sts16(to + p * L::XPLANE + (c >> 3) * L::XBOX + n * 128 + (((c & 7) ^ (n & 7)) << 4), v[p]);
-                }
+                fence_proxy();
+                __syncwarp();
+                if (lane == 0) bar_arrive(x_full + 8 * w);
             }
-            fence_proxy();
+            if (s_abort && filled < nc) {                       // a copy in flight lands before the CTA goes on
+                volatile int never = 0;
+                bar_wait_slow(x_raw + 8 * w, (uint32_t)(filled / XS) & 1u, &never, nullptr);
+            }
             __syncwarp();
-            if (lane == 0) bar_arrive(x_full + 8 * slot);
+        } else {
+            const T *const x = static_cast<const T *>(a.x) + (long)i0 * a.ldx;
+            for (int ci = w % XS; ci < nc; ci += XS) {
+                const int slot = ci % XS;
+                if (!use_wait(x_empty + 8 * slot, ci + XS, XS, &s_abort)) break;
+                const uint32_t to = base + L::X + slot * L::XSTAGE;
+                const int k0 = (c0 + ci) * CHUNK;
+                constexpr int BATCH = 4;
+                for (int b = w / XS * (N / 2 / L::X_PARTS); b < (w / XS + 1) * (N / 2 / L::X_PARTS); b += BATCH) {
+                    Octet<T> o[BATCH];
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) {
+                        const int n = ((b + i) * 32 + lane) >> 4, at = k0 + (lane & 15) * 8;
+                        if (n < rows && at < a.w.k) o[i].load(x + (long)n * a.ldx + at); else o[i].clear();
+                    }
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) {
+                        const int n = ((b + i) * 32 + lane) >> 4, c = lane & 15;
+                        uint32_t v[P][4];
+                        o[i].pairs(v);
+#pragma unroll
+                        for (int p = 0; p < P; ++p)
+                            sts16(to + p * L::XPLANE + (c >> 3) * L::XBOX + n * 128 + (((c & 7) ^ (n & 7)) << 4), v[p]);
+                    }
+                }
+                fence_proxy();
+                __syncwarp();
+                if (lane == 0) bar_arrive(x_full + 8 * slot);
+            }
         }
         done();
     }
@@ -375,9 +424,9 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     float *const y = a.y + (long)i0 * a.ldy;
     cluster_sync();                                             // totals [N][OUT] of every CTA
     // a part of the rows of x for each CTA, a row for each eight warps
-    for (int i = rank + a.split * (tid / OUT); i < rows; i += a.split * (L::THREADS / OUT)) {
+    for (int i = rank + a.split * (tid / OUT); i < rows; i += a.split * (THREADS / OUT)) {
         const int o = tid % OUT;
-        if (tid >= L::THREADS / OUT * OUT) break;
+        if (tid >= THREADS / OUT * OUT) break;
         float v = 0.f;
         for (int r = 0; r < a.split; ++r) v += peer_value(base + (i * OUT + o) * 4, r);
         if (j0 + o < a.w.o) {
@@ -444,7 +493,7 @@ cudaError_t launch(Args a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3(tiles * a.split, cols);
-    lc.blockDim = L::THREADS;
+    lc.blockDim = THREADS;
     lc.dynamicSmemBytes = smem;
     lc.stream = s;
     cudaLaunchAttribute at[2];
@@ -462,7 +511,10 @@ cudaError_t launch(Args a, cudaStream_t s) {
 
 template <typename T, int GROUP>
 cudaError_t launch_n(const Args &a, cudaStream_t s) {
-    return a.m <= 16 ? launch<T, GROUP, 16>(a, s) : a.m <= 32 ? launch<T, GROUP, 32>(a, s) : launch<T, GROUP, 64>(a, s);
+    if (a.m <= 16) return launch<T, GROUP, 16>(a, s);
+    if constexpr (sizeof(T) == 2)               // (planes of 64 rows would leave room for one stage)
+        if (a.m > 32) return launch<T, GROUP, 64>(a, s);
+    return launch<T, GROUP, 32>(a, s);
 }
 
 }  // namespace
