@@ -211,16 +211,15 @@ template <typename T>
 static cudaError_t launch_few(const T *x, long ldx, int m, const Weight &w, float *y, long ldy, int accumulate, cudaStream_t s) {
     const int align = w.group / 8;              // bytes of a lane's codes of a group
     const bool wide = reinterpret_cast<uintptr_t>(w.codes) % align == 0 && w.k / 2 % align == 0;
-    const int step = m > 8 ? 16 : 8;
+    const int step = m > 8 ? 16 : 8;            // m <= 16
     const FewKernel<T> f = w.group == 128 ? few_kernel<T, 128>(m > 8, wide) : w.group == 64 ? few_kernel<T, 64>(m > 8, wide) : few_kernel<T, 32>(m > 8, wide);
     const size_t sums = (size_t)FEW_WARPS * FEW_OUT * step * 4, beside = (size_t)FEW_OUT * w.groups * 3;
     const bool staged = beside <= 64 * 1024;    // longer rows read them where they are
     const size_t smem = sums + (staged ? beside : 0);
     cudaError_t e = cudaSuccess;
     if (smem > 48 * 1024) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    for (int i = 0; i < m && e == cudaSuccess; i += step) {
-        e = launch_chain(f, (w.o + FEW_OUT - 1) / FEW_OUT, FEW_WARPS * 32, smem, s, x + (long)i * ldx, ldx, std::min(m - i, step), w,
-                         y + (long)i * ldy, ldy, accumulate, (int)staged);
+    if (e == cudaSuccess) {
+        e = launch_chain(f, (w.o + FEW_OUT - 1) / FEW_OUT, FEW_WARPS * 32, smem, s, x, ldx, m, w, y, ldy, accumulate, (int)staged);
         note_launch();
     }
     return e;
@@ -361,6 +360,8 @@ static cudaError_t launch_quantize(const T *x, long ldw, const Weight &w, T *val
     return e;
 }
 
+constexpr int MOST_ROWS = 65535 * 32;           // a grid's height in tiles of 32
+
 static bool take_weight(const msd_weight4 *w, Weight *out) {
     if (!w || !w->codes || !w->scales || w->o < 1 || w->k < 8 || w->k % 8 || reinterpret_cast<uintptr_t>(w->codes) % 4 ||
         reinterpret_cast<uintptr_t>(w->scales) % 2 || (w->group != 32 && w->group != 64 && w->group != 128))
@@ -383,19 +384,17 @@ extern "C" {
 msd_status msd_linear4(const void *x, int64_t ldx, int32_t x_dtype, int32_t m, const msd_weight4 *weight, float *y,
                        int64_t ldy, int32_t accumulate, void *stream) {
     Weight w;
-    if (m < 0 || !take_weight(weight, &w) || (x_dtype != MSD_F32 && x_dtype != MSD_BF16)) return MSD_ERR_INVALID;
+    if (m < 0 || m > MOST_ROWS || !take_weight(weight, &w) || (x_dtype != MSD_F32 && x_dtype != MSD_BF16)) return MSD_ERR_INVALID;
     if (m == 0) return MSD_OK;
     if (bad_rows(x, ldx, x_dtype, w.k) || !y || ldy < w.o || reinterpret_cast<uintptr_t>(y) % 4) return MSD_ERR_INVALID;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     // Which of the two: measured with 1 to 16 rows, k and o of 4096 and 11008. The warps of a few rows win up to 8 rows (fp32: 3, a
     // tile of B operands) while their CTAs of 32 outputs fit the GPU at once (o 4096, k 11008, groups of 128: 12.0 us, 14.6 on
     // tcgen05; 16 rows, k 4096: 7.6 and 9.9), and with one scale for 128 codes of bf16 rows (o 11008: 11.7 and 12.5; with 64 codes 19.2 and 14.0).
-    // Tensor copies take rows of codes that start on 16 bytes.
     const bool f32 = x_dtype == MSD_F32, small = w.o <= 32 * 152;
     const bool few = m <= (f32 ? 3 : 8) ? small || (!f32 && w.group == 128) : !f32 && m <= 16 && (long)w.o * w.k <= 20l << 20;
-    const bool tc = !few && reinterpret_cast<uintptr_t>(w.codes) % 16 == 0 && w.k % 32 == 0;
     const auto run = [&](auto *p) {
-        return tc ? launch_linear4_tc(p, (long)ldx, m, w, y, (long)ldy, accumulate, s) : launch_few(p, (long)ldx, m, w, y, (long)ldy, accumulate, s);
+        return few ? launch_few(p, (long)ldx, m, w, y, (long)ldy, accumulate, s) : launch_linear4_tc(p, (long)ldx, m, w, y, (long)ldy, accumulate, s);
     };
     const cudaError_t e = x_dtype == MSD_F32 ? run(static_cast<const float *>(x)) : run(static_cast<const bf16 *>(x));
     return e == cudaSuccess ? MSD_OK : MSD_ERR_CUDA;

@@ -66,7 +66,7 @@ template <> struct Octet<float> {
     }
 };
 
-// Products on the 5th-generation tensor cores (linear4_tc.cu): rows of codes aligned to 16 bytes.
+// Products on the 5th-generation tensor cores (linear4_tc.cu).
 template <typename T>
 cudaError_t launch_linear4_tc(const T *x, long ldx, int m, const Weight &w, float *y, long ldy, int accumulate, cudaStream_t s);
 

@@ -64,6 +64,7 @@ struct Args {
     long ldx, ldy;
     float *y;
     int m, accumulate, split, staged, slice;                    // slice: groups of a CTA that are staged
+    int direct;                                                 // codes at addresses that tensor copies do not take
 };
 
 __device__ __forceinline__ void cluster_sync() {
@@ -147,7 +148,7 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_abort = 0;
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
+        if (!a.direct) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
         if constexpr (!L::SPLIT) asm volatile("prefetch.tensormap [%0];" ::"l"(&x_map) : "memory");
     }
     if (warp == 0) {
@@ -194,7 +195,7 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         const uint32_t code_row = base + L::W + half * WBOX + row * 64, swz = (uint32_t)(row >> 1 & 3) << 4;
         const uint8_t *const z_at = a.staged ? s_zeros + out : a.w.zeros + (long)(j0 + min(out, outs - 1)) * a.w.groups + g0;
         const int z_step = a.staged ? ZPITCH : 1;
-        const bool copies = warp == CODE_0 || warp == CODE_0 + 4;         // (a warp for the even chunks, one for the odd ones)
+        const bool copies = !a.direct && (warp == CODE_0 || warp == CODE_0 + 4);         // (a warp for the even chunks, one for the odd ones)
         const uint32_t on = elect_one();
         int copied = slot;                                      // chunks copied: slot, slot + 2, ... below this
         const auto copy = [&](int ci) {
@@ -216,16 +217,38 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         for (int ci = slot; ci < nc && ok; ci += 2) {
             const int ws = ci % WS;
             if (copies && ci + AHEAD < nc) copy(ci + AHEAD);
-            ok = use_wait(w_full + 8 * ws, ci, WS, &s_abort);
-            if (!ok) break;
+            uint32_t from = code_row + ws * WSTAGE;
+            if (a.direct) {                                     // the warp's 32 rows, two at a time, by words to where a copy would put them
+                from = code_row + slot * WSTAGE;
+                const int words = a.w.k / 8, at = (c0 + ci) * (CHUNK / 8) + (lane & 15), r0 = half * TILE + (warp & 3) * 32 + (lane >> 4);
+                const uint32_t *const codes = reinterpret_cast<const uint32_t *>(a.w.codes) + at;
+                __syncwarp();                                   // (the last chunk's have been read)
+#pragma unroll 1
+                for (int b = 0; b < 32; b += 16) {
+                    uint32_t v[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        v[i] = at < words ? __ldcs(codes + (long)(j0 + min(r0 + b + 2 * i, outs - 1)) * words) : 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int r = (warp & 3) * 32 + (lane >> 4) + b + 2 * i;
+                        const uint32_t to = base + L::W + slot * WSTAGE + half * WBOX + r * 64 + (((lane & 12) << 2) ^ ((r >> 1 & 3) << 4)) + (lane & 3) * 4;
+                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(v[i]) : "memory");
+                    }
+                }
+                __syncwarp();
+            } else {
+                ok = use_wait(w_full + 8 * ws, ci, WS, &s_abort);
+                if (!ok) break;
+            }
             uint4 q[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) q[i] = lds16(code_row + ws * WSTAGE + ((i << 4) ^ swz));
+            for (int i = 0; i < 4; ++i) q[i] = lds16(from + ((i << 4) ^ swz));
             unsigned z[PER];
 #pragma unroll
             for (int e = 0; e < PER; ++e) z[e] = a.w.zeros && ci * PER + e < gs ? z_at[(long)(ci * PER + e) * z_step] : 8u;
             __syncwarp();
-            if (lane == 0) bar_arrive(w_empty + 8 * ws);
+            if (lane == 0 && !a.direct) bar_arrive(w_empty + 8 * ws);
             // 64 elements at a time, so that the MMAs of the first are done when the next chunk's come
 #pragma unroll
             for (int sub = 0; sub < 2; ++sub) {
@@ -479,7 +502,9 @@ cudaError_t launch(Args a, cudaStream_t s) {
     using L = Lay<T, GROUP, N>;
     CUtensorMap map, x_map;
     memset(&x_map, 0, sizeof x_map);
-    if (!make_map(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.w.codes, a.w.k / 2, a.w.o, a.w.k / 2, CHUNK / 2, TILE, CU_TENSOR_MAP_SWIZZLE_64B) ||
+    a.direct = reinterpret_cast<uintptr_t>(a.w.codes) % 16 != 0 || a.w.k % 32 != 0;
+    memset(&map, 0, sizeof map);
+    if ((!a.direct && !make_map(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.w.codes, a.w.k / 2, a.w.o, a.w.k / 2, CHUNK / 2, TILE, CU_TENSOR_MAP_SWIZZLE_64B)) ||
         (!L::SPLIT && !make_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.x, a.w.k, a.m, a.ldx, 64, N, CU_TENSOR_MAP_SWIZZLE_128B)))
         return cudaErrorUnknown;
     const int chunks = (a.w.k + CHUNK - 1) / CHUNK, tiles = (a.w.o + OUT - 1) / OUT, cols = (a.m + N - 1) / N;
@@ -521,7 +546,7 @@ cudaError_t launch_n(const Args &a, cudaStream_t s) {
 
 template <typename T>
 cudaError_t launch_linear4_tc(const T *x, long ldx, int m, const Weight &w, float *y, long ldy, int accumulate, cudaStream_t s) {
-    const Args a{w, x, ldx, ldy, y, m, accumulate, 1, 0, 0};
+    const Args a{w, x, ldx, ldy, y, m, accumulate, 1, 0, 0, 0};
     return w.group == 128 ? launch_n<T, 128>(a, s) : w.group == 64 ? launch_n<T, 64>(a, s) : launch_n<T, 32>(a, s);
 }
 
