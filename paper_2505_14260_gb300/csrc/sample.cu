@@ -54,6 +54,18 @@ struct Settings {
     const float *top_p, *min_p;
 };
 
+// The settings of a row, as they were given.
+struct RowSettings {
+    float temperature, top_p, min_p;
+    int top_k;
+    __device__ __forceinline__ RowSettings(const Settings &f, int at) {
+        temperature = f.temperature ? f.temperature[at] : 1.f;
+        top_k = f.top_k ? f.top_k[at] : 0;
+        top_p = f.top_p ? f.top_p[at] : 1.f;
+        min_p = f.min_p ? f.min_p[at] : 0.f;
+    }
+};
+
 // What is left of a row: logits above `end`, and of the ids with just this logit the ones up to `tie`.
 struct Left {
     RowScale scale;
@@ -63,7 +75,7 @@ struct Left {
     u64 total;                // its weight; 0: nothing is left
 
     // (NaN and -inf are in no run: it starts at -inf with no id)
-    __device__ __forceinline__ bool has(float x, int id) const { return x > end || (x == end && id <= tie); }
+    __device__ __forceinline__ bool has(float x, int id) const { return x > end | (x == end & id <= tie); }
 };
 
 // Weight of a token of a run, without min-p.
@@ -113,7 +125,7 @@ struct __align__(16) Shared {                   // (the sums and the slice lie b
     u64 above, left;
     double log_total;
     unsigned bucket, own_n[2], list_n[2], base[8];            // (a round may gather twice)
-    unsigned range_lo[2], range_hi[2];          // keys of the tokens gathered
+    unsigned range_lo, range_hi;                // keys of a bucket's tokens
     float end;
     int tie, token;
     int next, gones, gone[MAX_CHILDREN];
@@ -217,6 +229,7 @@ __device__ Extent load_row(const T *row, int V, int ctas, int rank, int slice) {
     T *const data = reinterpret_cast<T *>(g_smem + data_at);
     const T *const from = row + first - mis;                                                // 16-byte aligned
     const int v0 = mis ? 1 : 0, v1 = max((mis + count) / E, v0);                            // whole vectors
+    const uint4 table = reinterpret_cast<const uint4 *>(g_exp_table.pair)[tid];
     float hi = -INFINITY, lo = INFINITY;
     const auto low = [&](float x) { lo = x > -INFINITY ? fminf(lo, x) : lo; };
     for (int v = v0 + tid; v < v1; v += U * ROW_THREADS) {
@@ -249,7 +262,7 @@ __device__ Extent load_row(const T *row, int V, int ctas, int rank, int slice) {
         hi = fmaxf(hi, x);
         low(x);
     }
-    reinterpret_cast<uint4 *>(sh.table)[tid] = reinterpret_cast<const uint4 *>(g_exp_table.pair)[tid];
+    reinterpret_cast<uint4 *>(sh.table)[tid] = table;
     static_assert(EXP_STEPS * 8 == ROW_THREADS * 16, "");
     for (int i = tid; i < BUCKETS; i += ROW_THREADS) sh.all[i] = 0;
     if (tid == 0) {
@@ -525,31 +538,69 @@ __device__ __noinline__ int locate_in_list(int n, u64 goal, int gones) {
 
 enum : int { ONE_TOKEN = 0, IN_LIST = 1, IN_ROW = 2 };        // what is left: l.tie alone; the first CTA's list; add_up's sums
 
-// Tokens of the places from `first` to `last` into the first CTA's list, or (all_lists) every CTA's; their number, which may
-// be more than the list has. `which`: 0 or 1, the counters (zero before the last meeting). Keys' range in sh.range_*.
-template <typename T, typename P>
-__device__ __forceinline__ unsigned gather(int which, P place, unsigned first, unsigned last, bool all_lists) {
+// The bucket of a token of a run, BUCKETS for others: of equal width in the exponent, or (KEYS) in the bits of the keys from
+// k_lo to k_hi. No branches, since a warp's tokens go all ways.
+struct Places {
+    float end, top, scale;
+    int tie, shift;
+    unsigned k_lo, k_hi;
+    template <bool KEYS> __device__ __forceinline__ unsigned of(float x, int id) const {
+        bool in = x > end | (x == end & id <= tie);
+        unsigned b;
+        if constexpr (KEYS) {
+            const unsigned k = key_of(x);
+            in = in & (k >= k_lo) & (k <= k_hi);
+            b = (k_hi - k) >> shift;
+        } else {
+            b = __float_as_uint(fminf((top - x) * scale, (float)(BUCKETS - 1)) + 12582912.f) & (2 * BUCKETS - 1);
+        }
+        return in ? b : BUCKETS;
+    }
+};
+
+// This CTA's histogram of counts or of masses (weights by `scale`).
+template <typename T, bool KEYS, bool MASS>
+__device__ __noinline__ void histogram(const Places p, const RowScale scale) {
     Shared &sh = shared();
-    const int tid = threadIdx.x, lane = tid & 31, ctas = sh.ctas;
-    unsigned lo = ~0u, hi = 0;
     each<T>([&](float x, int id) {
-        const unsigned b = place(x, id);
-        const bool in = b >= first && b <= last;
-        const unsigned all = __ballot_sync(0xffffffffu, in);
-        if (all == 0) return;
-        unsigned slot = 0;
-        if (lane == __ffs(all) - 1) slot = atomicAdd(&sh.own_n[which], __popc(all));
-        slot = __shfl_sync(0xffffffffu, slot, __ffs(all) - 1) + __popc(all & ((1u << lane) - 1u));
-        if (in) {
-            const u64 o = order_of(x, id);
-            lo = min(lo, (unsigned)(o >> 32));
-            hi = max(hi, (unsigned)(o >> 32));
-            if (slot < LIST) sh.own[slot] = o;
+        const unsigned b = p.of<KEYS>(x, id);
+        if constexpr (MASS) {
+            const u64 w = weight_in(scale, x, sh.table);
+            if (b == BUCKETS) return;
+            atomicAdd(&sh.hist[0][b], (unsigned)w & 0x7FFFu);
+            atomicAdd(&sh.hist[1][b], (unsigned)(w >> 15) & 0x7FFFu);
+            atomicAdd(&sh.hist[2][b], (unsigned)(w >> 30));
+        } else {
+            if (b != BUCKETS) atomicAdd(&sh.hist[0][b], 1u);
         }
     });
-    lo = __reduce_min_sync(0xffffffffu, lo);
-    hi = __reduce_max_sync(0xffffffffu, hi);
-    if (hi && lane < ctas) { least(&sh.range_lo[which], lane, lo); most(&sh.range_hi[which], lane, hi); }
+}
+
+// Tokens of the places from `first` to `last` into the first CTA's list, or (all_lists) every CTA's; their number, which may
+// be more than the list has. `which`: 0 or 1, the counters (zero before the last meeting).
+template <typename T, bool KEYS>
+__device__ __noinline__ unsigned gather(int which, const Places p, unsigned first, unsigned last, bool all_lists) {
+    Shared &sh = shared();
+    const int tid = threadIdx.x, lane = tid & 31, ctas = sh.ctas, id0 = sh.first - sh.mis + lane * 4, blocks = sh.blocks;
+#pragma unroll 1
+    for (int b = tid >> 5; b < blocks; b += WARPS) {
+        float x[4];
+        block_logits<T>(b, x);
+        unsigned in = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            in |= (unsigned)(p.of<KEYS>(x[e], id0 + b * BLOCK + e) - first <= last - first) << e;       // (last < BUCKETS)
+        }
+        if (!__any_sync(0xffffffffu, in)) continue;
+        if (in == 0 || *(volatile unsigned *)&sh.own_n[which] > LIST) continue;     // (too many already: how many does not matter)
+        unsigned slot = atomicAdd(&sh.own_n[which], __popc(in));
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (in >> e & 1) {
+                if (slot < LIST) sh.own[slot] = order_of(x[e], id0 + b * BLOCK + e);
+                ++slot;
+            }
+    }
     __syncthreads();
     const unsigned own_n = sh.own_n[which];
     if (own_n && tid < ctas) sh.base[tid] = take(&sh.list_n[which], tid, own_n);
@@ -575,33 +626,14 @@ __device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_e
     const float y_end = fminf((l.scale.top - x_end) * l.scale.c_hi, Y_MOST);
     const float scale = y_end > 0.f ? (float)(BUCKETS - 1) / y_end * l.scale.c_hi : 0.f;
     u64 above = 0;
-    unsigned k_lo = 0, k_hi = ~0u;
-    int shift = -1;
-    const auto place = [&](float x, int id) -> unsigned {                   // BUCKETS: not one of them
-        if (!l.has(x, id)) return BUCKETS;
-        if (shift < 0) return __float_as_uint(fminf((l.scale.top - x) * scale, (float)(BUCKETS - 1)) + 12582912.f) & (2 * BUCKETS - 1);
-        const unsigned k = key_of(x);
-        return k >= k_lo && k <= k_hi ? (k_hi - k) >> shift : BUCKETS;
-    };
+    Places places{l.end, l.scale.top, scale, l.tie, 0, 0, ~0u};
     for (int round = 0;; ++round) {
-        for (int i = tid; i < BUCKETS; i += ROW_THREADS) sh.hist[0][i] = sh.hist[1][i] = sh.hist[2][i] = 0;
-        if (tid < 2) { sh.own_n[tid] = sh.list_n[tid] = 0; sh.range_lo[tid] = ~0u; sh.range_hi[tid] = 0; }
+        for (int i = tid; i < (mass ? 3 : 1) * BUCKETS; i += ROW_THREADS) (&sh.hist[0][0])[i] = 0;
+        if (tid < 2) sh.own_n[tid] = sh.list_n[tid] = 0;
+        if (tid == 2) { sh.range_lo = ~0u; sh.range_hi = 0; }
         __syncthreads();
-        if (mass) {
-            each<T>([&](float x, int id) {
-                const unsigned b = place(x, id);
-                const u64 w = weight_in(l.scale, x, sh.table);
-                if (b == BUCKETS) return;
-                atomicAdd(&sh.hist[0][b], (unsigned)w & 0x7FFFu);
-                atomicAdd(&sh.hist[1][b], (unsigned)(w >> 15) & 0x7FFFu);
-                atomicAdd(&sh.hist[2][b], (unsigned)(w >> 30));
-            });
-        } else {
-            each<T>([&](float x, int id) {
-                const unsigned b = place(x, id);
-                if (b != BUCKETS) atomicAdd(&sh.hist[0][b], 1u);
-            });
-        }
+        if (round == 0) mass ? histogram<T, false, true>(places, l.scale) : histogram<T, false, false>(places, l.scale);
+        else mass ? histogram<T, true, true>(places, l.scale) : histogram<T, true, false>(places, l.scale);
         __syncthreads();
         for (int i = tid; i < BUCKETS; i += ROW_THREADS) {
             const u64 v = mass ? sh.hist[0][i] + ((u64)sh.hist[1][i] << 15) + ((u64)sh.hist[2][i] << 30) : sh.hist[0][i];
@@ -666,7 +698,7 @@ __device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_e
             __syncthreads();
         }
         if (few_before) {
-            const unsigned n = gather<T>(0, place, 0, bucket, false);
+            const unsigned n = gather<T, false>(0, places, 0, bucket, false);
             if (n <= LIST) {
                 l.total = mass ? all : 0;
                 *mode = IN_LIST;
@@ -674,12 +706,24 @@ __device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_e
                 return l;
             }
         }
-        const unsigned n = gather<T>(1, place, bucket, bucket, true);
-        k_lo = sh.range_lo[1];
-        k_hi = sh.range_hi[1];
+        const unsigned n = round == 0 ? gather<T, false>(1, places, bucket, bucket, true) : gather<T, true>(1, places, bucket, bucket, true);
         const bool few = n <= LIST;
-        if (!few && k_lo != k_hi) {
-            shift = max(0, 22 - __clz(k_hi - k_lo));                        // (k_hi - k_lo) >> shift < BUCKETS
+        if (!few) {                                                         // the range of their keys
+            unsigned lo = ~0u, hi = 0;
+            each<T>([&](float x, int id) {
+                if ((round == 0 ? places.of<false>(x, id) : places.of<true>(x, id)) != bucket) return;
+                lo = min(lo, key_of(x));
+                hi = max(hi, key_of(x));
+            });
+            lo = __reduce_min_sync(0xffffffffu, lo);
+            hi = __reduce_max_sync(0xffffffffu, hi);
+            if (hi && lane < ctas) { least(&sh.range_lo, lane, lo); most(&sh.range_hi, lane, hi); }
+            meet();
+            places.k_lo = sh.range_lo;
+            places.k_hi = sh.range_hi;
+        }
+        if (!few && places.k_lo != places.k_hi) {
+            places.shift = max(0, 22 - __clz(places.k_hi - places.k_lo));   // (k_hi - k_lo) >> shift < BUCKETS
             __syncthreads();                                                // all have read the list's length and the range
             continue;
         }
@@ -711,10 +755,10 @@ __device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_e
     }
 }
 
-// What the settings of entry `at` leave: *mode, with IN_LIST in the first CTA alone (the others get a total of 0), *n
+// What a row's settings leave of it: *mode, with IN_LIST in the first CTA alone (the others get a total of 0), *n
 // tokens in its list. whole: every CTA gets to know l in that case too.
 template <typename T>
-__device__ __forceinline__ Left filter_row(const Extent &e, const Settings &f, int at, bool whole, int *mode, unsigned *n) {
+__device__ __forceinline__ Left filter_row(const Extent &e, const RowSettings &f, bool whole, int *mode, unsigned *n) {
     Shared &sh = shared();
     Left l;
     l.total = 0;
@@ -724,9 +768,9 @@ __device__ __forceinline__ Left filter_row(const Extent &e, const Settings &f, i
     l.scale = RowScale{e.top, 0.f, 0.f};
     *mode = ONE_TOKEN;
     if (e.top == -INFINITY) return l;
-    float temp = f.temperature ? f.temperature[at] : 1.f;
-    int k = f.top_k ? f.top_k[at] : 0;
-    const float p = f.top_p ? f.top_p[at] : 1.f, m = f.min_p ? f.min_p[at] : 0.f;
+    float temp = f.temperature;
+    int k = f.top_k;
+    const float p = f.top_p, m = f.min_p;
     if (!(temp >= 0x1p-100f) || m > 1.f || p <= 0.f) k = 1;
     temp = temp > 0.f ? fminf(fmaxf(temp, 0x1p-100f), 0x1p100f) : 1.f;
     // log2(e) / temp as a pair (the remainder of the division is exact): fp64, a few lanes a cycle, took 3 us here
@@ -739,13 +783,13 @@ __device__ __forceinline__ Left filter_row(const Extent &e, const Settings &f, i
             if (x == e.top) id = min(id, (unsigned)i);
         });
         id = __reduce_min_sync(0xffffffffu, id);
-        if (threadIdx.x == 0) sh.range_lo[0] = ~0u;
+        if (threadIdx.x == 0) sh.range_lo = ~0u;
         meet();
         const int lane = threadIdx.x & 31;
-        if (lane < sh.ctas && id != ~0u) least(&sh.range_lo[0], lane, id);
+        if (lane < sh.ctas && id != ~0u) least(&sh.range_lo, lane, id);
         meet();
         l.end = e.top;
-        l.tie = (int)sh.range_lo[0];
+        l.tie = (int)sh.range_lo;
         l.total = 1ull << WEIGHT_BITS;
         return l;
     }
@@ -791,10 +835,11 @@ sample_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int slice,
     Shared &sh = shared();
     const int r = blockIdx.x / ctas, rank = blockIdx.x % ctas;
     const T *row = logits + (long)r * ld;
+    const RowSettings settings(f, r);                   // (requested before the row, which takes longer)
     const Extent e = load_row(row, V, ctas, rank, slice);
     int mode;
     unsigned n = 0;
-    const Left l = filter_row<T>(e, f, r, probs != nullptr, &mode, &n);
+    const Left l = filter_row<T>(e, settings, probs != nullptr, &mode, &n);
     // the thread that knows the token writes it
     if (mode == IN_LIST && rank > 0 && !probs) return;
     if (logp && threadIdx.x == 32) sh.log_total = mode == ONE_TOKEN ? 0.0 : log2((double)l.total) - WEIGHT_BITS;     // (a warp that is free)
@@ -864,10 +909,11 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
     }
     if (d > a.depth) return;                            // never reached (the whole cluster leaves)
     const T *row = logits + (long)r * ld;
+    const RowSettings settings(f, b);
     const Extent e = load_row(row, V, ctas, rank, slice);
     int mode;
     unsigned in_list = 0;
-    const Left l = filter_row<T>(e, f, b, false, &mode, &in_list);
+    const Left l = filter_row<T>(e, settings, false, &mode, &in_list);
     if (mode == IN_LIST) {                              // the first CTA goes on alone
         if (rank > 0) return;
         __syncthreads();
@@ -971,8 +1017,8 @@ __global__ void accept_walk_kernel(TreeArgs a) {
 
 static_assert(data_offset(most_blocks(MAX_VOCAB / 8, 4)) + (size_t)most_blocks(MAX_VOCAB / 8, 4) * BLOCK * 4 <= 227 * 1024, "the largest row fits");
 
-// How many CTAs share a row, and the ids of each: as few as leave room for two CTAs on an SM, more where there are few
-// rows (and 2048 ids for each).
+// How many CTAs share a row, and the ids of each: as few as leave room for two CTAs on an SM, 4 where there are few
+// rows (and 2048 ids for each; 8 are no faster: one row of 32000 takes 13.9 us in 4 parts, 13.5 in 8, 16.6 in 2, 20.7 in 1).
 struct Cut {
     int ctas, slice;
     size_t smem;
@@ -982,7 +1028,7 @@ static Cut cut_rows(int rows, int V, int size) {
     const auto slice_of = [&](int ctas) { return ((V + ctas - 1) / ctas + 7) / 8 * 8; };
     int c = 1;
     while (c < 8 && smem(slice_of(c)) > 112 * 1024) c *= 2;
-    while (c < 8 && (long)rows * c * 2 <= 304 && slice_of(c * 2) >= 2048) c *= 2;
+    while (c < 4 && (long)rows * c * 2 <= 304 && slice_of(c * 2) >= 2048) c *= 2;
     return Cut{c, slice_of(c), smem(slice_of(c))};
 }
 
