@@ -54,15 +54,25 @@ struct Settings {
     const float *top_p, *min_p;
 };
 
-// The settings of a row, as they were given.
+// The settings of a row: what they say, and the scale log2(e) / temperature as a pair.
 struct RowSettings {
-    float temperature, top_p, min_p;
-    int top_k;
-    __device__ __forceinline__ RowSettings(const Settings &f, int at) {
+    float temperature, top_p, min_p, c_hi, c_lo;
+    int top_k;                // 1: the first token alone; 0: off
+    u64 least;
+    __device__ __forceinline__ void request(const Settings &f, int at) {
         temperature = f.temperature ? f.temperature[at] : 1.f;
         top_k = f.top_k ? f.top_k[at] : 0;
         top_p = f.top_p ? f.top_p[at] : 1.f;
         min_p = f.min_p ? f.min_p[at] : 0.f;
+    }
+    __device__ __forceinline__ void prepare() {
+        if (!(temperature >= 0x1p-100f) || min_p > 1.f || top_p <= 0.f) top_k = 1;
+        const float t = temperature > 0.f ? fminf(fmaxf(temperature, 0x1p-100f), 0x1p100f) : 1.f;
+        // (the remainder of the division is exact; in fp64, a few lanes a cycle, it took 3 us)
+        constexpr float LOG2E = 1.44269504088896340736f, LOG2E_LO = (float)(1.44269504088896340736 - (double)1.44269504088896340736f);
+        c_hi = __fdiv_rn(LOG2E, t);
+        c_lo = __fdiv_rn(fmaf(-c_hi, t, LOG2E) + LOG2E_LO, t);
+        least = !(min_p > 0.f) ? 0 : min_p < 1.f ? share_floor(min_p, 1ull << WEIGHT_BITS, true) : 1ull << WEIGHT_BITS;
     }
 };
 
@@ -115,10 +125,7 @@ struct __align__(16) Shared {                   // (the sums and the slice lie b
             u64 own[LIST];
         };
     };
-    union {
-        u64 all[BUCKETS];                       // of the whole row; 0 between uses
-        u64 kid_w[MAX_CHILDREN];
-    };
+    u64 all[BUCKETS];                           // of the whole row; 0 between uses
     u64 red[WARPS + 1];
     u64 total[8];                               // of each CTA of the cluster
     float top[8], low[8];
@@ -129,6 +136,8 @@ struct __align__(16) Shared {                   // (the sums and the slice lie b
     float end;
     int tie, token;
     int next, gones, gone[MAX_CHILDREN];
+    unsigned short kid[MAX_CHILDREN];           // children of a node, and their tokens
+    int kid_token[MAX_CHILDREN];
     // the slice: ids [first, first + count), element i of it at data[mis + i], -inf around it, in whole blocks
     int ctas, rank, first, count, mis, blocks, data_at;
 };
@@ -215,9 +224,9 @@ __device__ __forceinline__ void each(F f) {
     }
 }
 
-// This CTA's slice into shared memory, and the row's extent.
-template <typename T>
-__device__ Extent load_row(const T *row, int V, int ctas, int rank, int slice) {
+// This CTA's slice into shared memory, and the row's extent. meanwhile(): done while the first of it is on its way.
+template <typename T, typename F>
+__device__ __forceinline__ Extent load_row(const T *row, int V, int ctas, int rank, int slice, F meanwhile) {
     constexpr int E = 16 / sizeof(T), U = 4;
     Shared &sh = shared();
     const int tid = threadIdx.x, warp = tid >> 5;
@@ -232,11 +241,33 @@ __device__ Extent load_row(const T *row, int V, int ctas, int rank, int slice) {
     const uint4 table = reinterpret_cast<const uint4 *>(g_exp_table.pair)[tid];
     float hi = -INFINITY, lo = INFINITY;
     const auto low = [&](float x) { lo = x > -INFINITY ? fminf(lo, x) : lo; };
-    for (int v = v0 + tid; v < v1; v += U * ROW_THREADS) {
-        uint4 q[U];
+    uint4 q[U];
+    const auto request = [&](int v) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (v + u * ROW_THREADS < v1) q[u] = __ldcs(reinterpret_cast<const uint4 *>(from) + v + u * ROW_THREADS);
+    };
+    request(v0 + tid);
+    meanwhile();
+    // what a cut starts with
+    for (int i = tid; i < 3 * BUCKETS; i += ROW_THREADS) (&sh.hist[0][0])[i] = 0;
+    for (int i = tid; i < BUCKETS; i += ROW_THREADS) sh.all[i] = 0;
+    if (tid < 2) sh.own_n[tid] = sh.list_n[tid] = 0;
+    if (tid == 0) {
+        sh.ctas = ctas; sh.rank = rank; sh.first = first; sh.count = count; sh.mis = mis; sh.blocks = blocks; sh.data_at = data_at;
+        sh.range_lo = ~0u;
+        sh.range_hi = 0;
+    }
+    // the edges: elements before the first whole vector and behind the last one
+    for (int i = tid; i < v0 * E + blocks * BLOCK - v1 * E; i += ROW_THREADS) {
+        const int at = i < v0 * E ? i : i - v0 * E + v1 * E;
+        const bool is = at >= mis && at < mis + count;
+        const float x = is ? logit_at(from, at) : -INFINITY;
+        data[at] = (T)x;
+        hi = fmaxf(hi, x);
+        low(x);
+    }
+    for (int v = v0 + tid; v < v1;) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (v + u * ROW_THREADS >= v1) break;
@@ -252,25 +283,14 @@ __device__ Extent load_row(const T *row, int V, int ctas, int rank, int slice) {
             }
             if (u == 0) low(__uint_as_float(E == 4 ? w[0] : w[0] & 0xFFFF0000u));
         }
-    }
-    // the edges: elements before the first whole vector and behind the last one
-    for (int i = tid; i < v0 * E + blocks * BLOCK - v1 * E; i += ROW_THREADS) {
-        const int at = i < v0 * E ? i : i - v0 * E + v1 * E;
-        const bool is = at >= mis && at < mis + count;
-        const float x = is ? logit_at(from, at) : -INFINITY;
-        data[at] = (T)x;
-        hi = fmaxf(hi, x);
-        low(x);
+        v += U * ROW_THREADS;
+        request(v);
     }
     reinterpret_cast<uint4 *>(sh.table)[tid] = table;
     static_assert(EXP_STEPS * 8 == ROW_THREADS * 16, "");
-    for (int i = tid; i < BUCKETS; i += ROW_THREADS) sh.all[i] = 0;
-    if (tid == 0) {
-        sh.ctas = ctas; sh.rank = rank; sh.first = first; sh.count = count; sh.mis = mis; sh.blocks = blocks; sh.data_at = data_at;
-    }
     hi = warp_max(hi);
     lo = -warp_max(-lo);
-    float *part = reinterpret_cast<float *>(sh.hist[0]);
+    float *part = reinterpret_cast<float *>(sh.gone);                                       // (not in use yet)
     if ((tid & 31) == 0) { part[warp] = hi; part[32 + warp] = lo; }
     if (ctas > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");               // all CTAs run: their shared memory is there
     __syncthreads();
@@ -429,93 +449,70 @@ __device__ u64 sum_up_to(u64 v, u64 *all) {
     __syncthreads();
     if (lane == 31) sh.red[warp] = v;
     __syncthreads();
-    u64 sum = 0;
-#pragma unroll 4
-    for (int i = 0; i < WARPS; ++i) {
-        if (i == warp) v += sum;
-        sum += sh.red[i];
+    static_assert(WARPS == 16, "");
+    u64 sum = sh.red[lane & 15];                        // every warp adds the warps' sums up
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+        const u64 t = __shfl_up_sync(0xffffffffu, sum, o);
+        if ((lane & 15) >= o) sum += t;
     }
-    *all = sum;
-    return v;
+    *all = __shfl_sync(0xffffffffu, sum, 15);
+    const u64 before = __shfl_sync(0xffffffffu, sum, max(warp - 1, 0));
+    return warp ? v + before : v;
 }
 
-// A token of the list, its rank, and the weight of those before it.
-struct Placed {
-    u64 order, w, ahead;
-    int rank;
-    bool is;                  // this thread has one
-};
-// Places the list's n tokens (weights in it) by order, or by id: up to 256 by comparing all pairs, with all threads, more by
-// sorting (for 64 tokens pairs take 1 us less than sorting, for 512 3 us more).
-// (By order, sorting loses sight of the weights, which are made again: 1 without mass.)
-__device__ __noinline__ Placed place_tokens(int n, bool by_id, bool mass, const RowScale scale) {
+// The list's n tokens by order, or by id: thread i gets the i-th. Up to 256 by counting, with all threads, how many come before each,
+// more by sorting (for 64 tokens counting takes 1 us less, for 512 3 us more). The weights come along only by id.
+template <bool BY_ID>
+__device__ __noinline__ Token ordered(int n) {
     Shared &sh = shared();
     const unsigned tid = threadIdx.x;
-    Placed t{0, 0, 0, 0, false};
-    // by id: the order's lower half is larger for a lower id
     if (n > LIST / 2) {
         const u64 o = tid < (unsigned)n ? sh.list[tid].order : 0;
-        const u64 in_order = sorted(by_id ? o << 32 | tid : o, n);
-        t.is = tid < (unsigned)n;
-        t.rank = (int)tid;
-        if (by_id) {
-            const Token own = t.is ? sh.list[(unsigned)in_order] : Token{0, 0};
-            t.order = own.order;
-            t.w = own.w;
+        if constexpr (BY_ID) {                          // (the order's lower half is larger for a lower id)
+            const u64 at = sorted(o << 32 | tid, n);
+            return tid < (unsigned)n ? sh.list[(unsigned)at] : Token{0, 0};
         } else {
-            t.order = in_order;
-            t.w = !t.is ? 0 : mass ? weight_in(scale, logit_of_order(in_order), sh.table) : 1;
+            return Token{sorted(o, n), 0};
         }
-        u64 all;
-        t.ahead = sum_up_to(t.w, &all) - t.w;
-        return t;
     }
     const int bits = min(5, __clz(max(n - 1, 1)) - 23), per = 1 << bits;    // 512 / per >= n
     const int i = (int)tid >> bits, part = (int)tid & (per - 1);
+    int rank = 0;
+    Token own{0, 0};
     if (i < n) {
-        const Token own = sh.list[i];
-        t.order = own.order;
-        t.w = own.w;
-        const u64 key = by_id ? own.order << 32 : own.order;
+        own = sh.list[i];
 #pragma unroll 4
         for (int j = part; j < n; j += per) {
-            const Token o = sh.list[j];
-            if ((by_id ? o.order << 32 : o.order) > key) {
-                t.ahead += o.w;
-                ++t.rank;
-            }
+            const u64 o = sh.list[j].order;
+            rank += BY_ID ? (unsigned)o > (unsigned)own.order : o > own.order;
         }
     }
-    for (int o = 1; o < per; o *= 2) {
-        t.ahead += __shfl_xor_sync(0xffffffffu, t.ahead, o);
-        t.rank += __shfl_xor_sync(0xffffffffu, t.rank, o);
-    }
-    t.is = i < n && part == 0;
-    return t;
+    for (int o = 1; o < per; o *= 2) rank += __shfl_xor_sync(0xffffffffu, rank, o);
+    __syncthreads();
+    if (i < n && part == 0) sh.list[rank] = own;
+    __syncthreads();
+    return tid < (unsigned)n ? sh.list[tid] : Token{0, 0};
 }
 
 // A run of few tokens, gathered in the first CTA: what top-k, top-p and min-p leave of it. mass: the weight that top-p's
 // share is taken of, where top-k is off. The list's weights become what is left of them.
 __device__ __noinline__ Left rest_of_list(Left l, int n, int k, float p, u64 mass) {
     Shared &sh = shared();
-    const int tid = threadIdx.x;
-    if (tid < n) sh.list[tid].w = weight_in(l.scale, logit_of_order(sh.list[tid].order), sh.table);
-    __syncthreads();
-    Placed t = place_tokens(n, false, true, l.scale);
-    bool in = t.is && (k <= 0 || t.rank < k);
+    const int i = threadIdx.x;
+    const u64 order = ordered<false>(n).order;
+    const u64 w = i < n ? weight_in(l.scale, logit_of_order(order), sh.table) : 0;
+    bool in = i < n && (k <= 0 || i < k);
     if (p < 1.f) {
         u64 all;
-        if (k > 0) {
-            sum_up_to(in ? t.w : 0, &all);
-            mass = all;
-        }
-        in = in && t.ahead < max(share_floor(p, mass, true), 1ull);
+        const u64 before = sum_up_to(in ? w : 0, &all) - w;                 // (of those that top-k leaves; i is one of them or out)
+        in = in && before < max(share_floor(p, k > 0 ? all : mass, true), 1ull);
     }
-    in = in && (t.w >= l.least || t.rank == 0);
-    sum_up_to(in ? t.w : 0, &l.total);
+    in = in && (w >= l.least || i == 0);
+    sum_up_to(in ? w : 0, &l.total);
     const int left = __syncthreads_count(in);
-    if (t.is && t.rank < n) sh.list[t.rank] = Token{t.order, in ? t.w : 0};
-    if (in && t.rank == left - 1) { sh.end = logit_of_order(t.order); sh.tie = id_of_order(t.order); }
+    if (i < n) sh.list[i] = Token{order, in ? w : 0};
+    if (i == left - 1) { sh.end = logit_of_order(order); sh.tie = id_of_order(order); }
     __syncthreads();
     l.end = sh.end;
     l.tie = sh.tie;
@@ -532,8 +529,10 @@ __device__ __noinline__ int locate_in_list(int n, u64 goal, int gones) {
                 if (sh.gone[g] == id_of_order(sh.list[tid].order)) sh.list[tid].w = 0;
         __syncthreads();
     }
-    const Placed t = place_tokens(n, true, true, RowScale{});
-    return t.is && t.ahead <= goal && goal < t.ahead + t.w ? id_of_order(t.order) : -1;
+    const Token t = ordered<true>(n);
+    u64 all;
+    const u64 upto = sum_up_to(t.w, &all);
+    return upto - t.w <= goal && goal < upto ? id_of_order(t.order) : -1;
 }
 
 enum : int { ONE_TOKEN = 0, IN_LIST = 1, IN_ROW = 2 };        // what is left: l.tie alone; the first CTA's list; add_up's sums
@@ -618,8 +617,9 @@ __device__ __noinline__ unsigned gather(int which, const Places p, unsigned firs
 // theirs (mass true): a narrower l. x_end is about its smallest logit. Every CTA finds it by itself from the whole row's
 // histogram and the bucket's tokens, which all are sent. Where few tokens lie before the bucket's end, they are gathered instead
 // (*mode becomes IN_LIST, *n their number) and l.total is the weight that p is a share of; nothing else of l changes then.
+// fresh: the first cut of the row.
 template <typename T>
-__device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_end, int *mode, unsigned *list_n) {
+__device__ __noinline__ Left cut(Left l, bool mass, bool fresh, u64 goal, float p, float x_end, int *mode, unsigned *list_n) {
     Shared &sh = shared();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, ctas = sh.ctas;
     // buckets of equal width in the exponent between the largest logit and x_end; from the second round on, of the keys' bits
@@ -628,10 +628,12 @@ __device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_e
     u64 above = 0;
     Places places{l.end, l.scale.top, scale, l.tie, 0, 0, ~0u};
     for (int round = 0;; ++round) {
-        for (int i = tid; i < (mass ? 3 : 1) * BUCKETS; i += ROW_THREADS) (&sh.hist[0][0])[i] = 0;
-        if (tid < 2) sh.own_n[tid] = sh.list_n[tid] = 0;
-        if (tid == 2) { sh.range_lo = ~0u; sh.range_hi = 0; }
-        __syncthreads();
+        if (round > 0 || !fresh) {
+            for (int i = tid; i < (mass ? 3 : 1) * BUCKETS; i += ROW_THREADS) (&sh.hist[0][0])[i] = 0;
+            if (tid < 2) sh.own_n[tid] = sh.list_n[tid] = 0;
+            if (tid == 2) { sh.range_lo = ~0u; sh.range_hi = 0; }
+            __syncthreads();
+        }
         if (round == 0) mass ? histogram<T, false, true>(places, l.scale) : histogram<T, false, false>(places, l.scale);
         else mass ? histogram<T, true, true>(places, l.scale) : histogram<T, true, false>(places, l.scale);
         __syncthreads();
@@ -652,19 +654,8 @@ __device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_e
             run += v[i];
         }
         const u64 own = run;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const u64 t = __shfl_up_sync(0xffffffffu, run, o);
-            if (lane >= o) run += t;
-        }
-        if (lane == 31) sh.red[warp] = run;
-        __syncthreads();
-        u64 before = above, all = 0;
-#pragma unroll 4
-        for (int i = 0; i < WARPS; ++i) {
-            if (i < warp) before += sh.red[i];
-            all += sh.red[i];
-        }
+        u64 all;
+        run = sum_up_to(run, &all);
         if (round == 0) {
             if (mass) goal = max(share_floor(p, all, true), 1ull);
             else if (all <= goal) {                                         // it has no more tokens than that
@@ -672,7 +663,7 @@ __device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_e
                 return l;
             }
         }
-        u64 at = before + run - own;
+        u64 at = above + run - own;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             if (at < goal && goal <= at + v[i]) { sh.bucket = tid * PER + i; sh.above = at; sh.left = at + v[i]; }
@@ -688,14 +679,9 @@ __device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_e
 #pragma unroll
             for (int i = 0; i < PER; ++i)
                 if (tid * PER + i <= bucket) about += (float)v[i] * exp2f((float)(tid * PER + i) * (y_end / (BUCKETS - 1)) - WEIGHT_BITS);
-            about = warp_sum(about);
-            if (lane == 0) sh.red[warp] = (u64)about;
-            __syncthreads();
-            u64 sum = 0;
-#pragma unroll 4
-            for (int i = 0; i < WARPS; ++i) sum += sh.red[i];
-            few_before = sum < LIST;
-            __syncthreads();
+            u64 sum;
+            sum_up_to((u64)fminf(16.f * about, 1e9f), &sum);
+            few_before = sum < 16 * LIST;
         }
         if (few_before) {
             const unsigned n = gather<T, false>(0, places, 0, bucket, false);
@@ -728,13 +714,11 @@ __device__ __noinline__ Left cut(Left l, bool mass, u64 goal, float p, float x_e
             continue;
         }
         if (few) {                                                          // each token's place among them
-            if (tid < (int)n) sh.list[tid].w = mass ? weight_in(l.scale, logit_of_order(sh.list[tid].order), sh.table) : 1;
-            __syncthreads();
-            const Placed t = place_tokens((int)n, false, mass, l.scale);
-            if (t.is && above + t.ahead < goal && goal <= above + t.ahead + t.w) {
-                sh.end = logit_of_order(t.order);
-                sh.tie = id_of_order(t.order);
-            }
+            const u64 order = ordered<false>((int)n).order;
+            const u64 w = tid >= (int)n ? 0 : mass ? weight_in(l.scale, logit_of_order(order), sh.table) : 1;
+            u64 sum;
+            const u64 upto = above + sum_up_to(w, &sum);
+            if (upto - w < goal && goal <= upto) { sh.end = logit_of_order(order); sh.tie = id_of_order(order); }
         } else {                                                            // equal logits: ids decide
             const float x = logit_of_order(sh.list[0].order);
             const u64 w = !mass ? 1 : max(weight_in(l.scale, x, sh.table), 1ull), need = (goal - above + w - 1) / w;
@@ -768,23 +752,16 @@ __device__ __forceinline__ Left filter_row(const Extent &e, const RowSettings &f
     l.scale = RowScale{e.top, 0.f, 0.f};
     *mode = ONE_TOKEN;
     if (e.top == -INFINITY) return l;
-    float temp = f.temperature;
+    l.scale.c_hi = f.c_hi;
+    l.scale.c_lo = f.c_lo;
     int k = f.top_k;
-    const float p = f.top_p, m = f.min_p;
-    if (!(temp >= 0x1p-100f) || m > 1.f || p <= 0.f) k = 1;
-    temp = temp > 0.f ? fminf(fmaxf(temp, 0x1p-100f), 0x1p100f) : 1.f;
-    // log2(e) / temp as a pair (the remainder of the division is exact): fp64, a few lanes a cycle, took 3 us here
-    constexpr float LOG2E = 1.44269504088896340736f, LOG2E_LO = (float)(1.44269504088896340736 - (double)1.44269504088896340736f);
-    l.scale.c_hi = __fdiv_rn(LOG2E, temp);
-    l.scale.c_lo = __fdiv_rn(fmaf(-l.scale.c_hi, temp, LOG2E) + LOG2E_LO, temp);
+    const float p = f.top_p;
     if (k == 1) {                                                           // the first token alone
         unsigned id = ~0u;
         each<T>([&](float x, int i) {
             if (x == e.top) id = min(id, (unsigned)i);
         });
         id = __reduce_min_sync(0xffffffffu, id);
-        if (threadIdx.x == 0) sh.range_lo = ~0u;
-        meet();
         const int lane = threadIdx.x & 31;
         if (lane < sh.ctas && id != ~0u) least(&sh.range_lo, lane, id);
         meet();
@@ -794,12 +771,14 @@ __device__ __forceinline__ Left filter_row(const Extent &e, const RowSettings &f
         return l;
     }
     *mode = IN_ROW;
-    if (m > 0.f) l.least = m < 1.f ? share_floor(m, 1ull << WEIGHT_BITS, true) : 1ull << WEIGHT_BITS;
+    l.least = f.least;
+    bool fresh = true;
     float x_end = e.low;
 #pragma unroll 1
     for (int by = 0; by < 2 && *mode == IN_ROW; ++by) {                     // top-k, then top-p
         if (by == 0 ? k <= 0 : !(p < 1.f)) continue;
-        l = cut<T>(l, by == 1, (u64)k, p, x_end, mode, n);
+        l = cut<T>(l, by == 1, fresh, (u64)k, p, x_end, mode, n);
+        fresh = false;
         if (*mode == IN_LIST && by == 1) k = 0;                             // (top-k is behind it already)
         if (l.end > -INFINITY) x_end = l.end;
     }
@@ -835,15 +814,17 @@ sample_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int slice,
     Shared &sh = shared();
     const int r = blockIdx.x / ctas, rank = blockIdx.x % ctas;
     const T *row = logits + (long)r * ld;
-    const RowSettings settings(f, r);                   // (requested before the row, which takes longer)
-    const Extent e = load_row(row, V, ctas, rank, slice);
+    RowSettings settings;
+    settings.request(f, r);
+    const float own_u = u[r];
+    const Extent e = load_row(row, V, ctas, rank, slice, [&] { settings.prepare(); });
     int mode;
     unsigned n = 0;
     const Left l = filter_row<T>(e, settings, probs != nullptr, &mode, &n);
     // the thread that knows the token writes it
     if (mode == IN_LIST && rank > 0 && !probs) return;
     if (logp && threadIdx.x == 32) sh.log_total = mode == ONE_TOKEN ? 0.0 : log2((double)l.total) - WEIGHT_BITS;     // (a warp that is free)
-    const u64 goal = share_floor(uniform(u[r]), l.total, false);
+    const u64 goal = share_floor(uniform(own_u), l.total, false);
     int t = -1;
     if (mode == ONE_TOKEN) t = l.tie;
     else if (mode == IN_ROW) t = locate<T>(l, false, goal, 0);
@@ -909,8 +890,27 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
     }
     if (d > a.depth) return;                            // never reached (the whole cluster leaves)
     const T *row = logits + (long)r * ld;
-    const RowSettings settings(f, b);
-    const Extent e = load_row(row, V, ctas, rank, slice);
+    RowSettings settings;
+    settings.request(f, b);
+    const float *u = a.u + ((long)b * (a.depth + 1) + d) * (a.children + 1);
+    const float last_u = u[a.children];
+    int kids = 0;                                       // of the first CTA's first warp
+    const Extent e = load_row(row, V, ctas, rank, slice, [&] {
+        settings.prepare();
+        // the first `children` children, in index order
+        if (rank == 0 && threadIdx.x < 32 && d < a.depth)
+            for (int j0 = node + 1; j0 < n && kids < a.children; j0 += 32) {
+                const int j = j0 + lane;
+                const bool is = j < n && parent[j] == node;
+                const unsigned all = __ballot_sync(0xffffffffu, is);
+                const int slot = kids + __popc(all & ((1u << lane) - 1u));
+                if (is && slot < a.children) {
+                    sh.kid[slot] = (unsigned short)j;
+                    sh.kid_token[slot] = tokens[j];
+                }
+                kids = min(kids + __popc(all), a.children);
+            }
+    });
     int mode;
     unsigned in_list = 0;
     const Left l = filter_row<T>(e, settings, false, &mode, &in_list);
@@ -921,44 +921,33 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
         __syncthreads();
     }
     const int ranks = sh.ctas;
-    const float *u = a.u + ((long)b * (a.depth + 1) + d) * (a.children + 1);
     if (rank == 0 && threadIdx.x < 32) {
-        // the first `children` children, in index order, and their weights; then the decisions one after another
-        u64 *kid_w = sh.kid_w;
-        int *kid = reinterpret_cast<int *>(sh.own), *kid_token = kid + MAX_CHILDREN, kids = 0;
-        if (d < a.depth)
-            for (int j0 = node + 1; j0 < n && kids < a.children; j0 += 32) {
-                const int j = j0 + lane;
-                const bool is = j < n && parent[j] == node;
-                const unsigned all = __ballot_sync(0xffffffffu, is);
-                const int slot = kids + __popc(all & ((1u << lane) - 1u));
-                if (is && slot < a.children) {
-                    const int t = tokens[j];
-                    kid[slot] = j;
-                    kid_token[slot] = t;
-                    kid_w[slot] = t >= 0 && t < V && l.total ? weight_left(l, tame(logit_at(row, t), e.infinite), t, sh.table) : 0;
-                }
-                kids = min(kids + __popc(all), a.children);
-            }
-        __syncwarp();
+        // A child is tried when those before it are rejected, so its odds are known: 32 children at a time. A token that an
+        // earlier child had has no weight left.
         u64 left = l.total;
         int gone = 0, next = -1;
-        for (int c = 0; c < kids; ++c) {
-            const int t = kid_token[c];
-            u64 w = kid_w[c];
-            bool again = false;
-            for (int i = lane; i < gone; i += 32) again |= sh.gone[i] == t;
-            if (__any_sync(0xffffffffu, again)) w = 0;
-            if (share_floor(uniform(u[c]), left, false) < w) {
-                next = kid[c];
-                break;
+        __syncwarp();
+        for (int c0 = 0; c0 < kids && next < 0; c0 += 32) {
+            const int c = c0 + lane, t = c < kids ? sh.kid_token[c] : -1 - lane;
+            const float v = c < kids ? u[c] : 0.f;
+            u64 w = t >= 0 && t < V && l.total ? weight_left(l, tame(logit_at(row, t), e.infinite), t, sh.table) : 0;
+            if (__match_any_sync(0xffffffffu, t) & ((1u << lane) - 1u)) w = 0;
+            for (int i = 0; i < gone; ++i)
+                if (sh.gone[i] == t) w = 0;
+            u64 upto = w;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const u64 before = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += before;
             }
-            if (w) {
-                left -= w;
-                if (lane == 0) sh.gone[gone] = t;
-                ++gone;
-                __syncwarp();
-            }
+            const unsigned yes = __ballot_sync(0xffffffffu, c < kids && share_floor(uniform(v), left - (upto - w), false) < w);
+            const unsigned tried = yes ? (1u << (__ffs(yes) - 1)) - 1u : 0xffffffffu;       // (and rejected)
+            const unsigned less = __ballot_sync(0xffffffffu, w != 0) & tried;
+            if (less >> lane & 1) sh.gone[gone + __popc(less & ((1u << lane) - 1u))] = t;
+            gone += __popc(less);
+            if (yes) next = sh.kid[c0 + __ffs(yes) - 1];
+            left -= __shfl_sync(0xffffffffu, upto, 31);                                     // (not used any more if one is accepted)
+            __syncwarp();
         }
         if (lane < ranks) {
             put(&sh.next, lane, next);
@@ -977,7 +966,7 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
         if (rank == 0 && threadIdx.x == 0) a.drawn[r] = left ? l.tie : -1;
         return;
     }
-    const u64 goal = share_floor(uniform(u[a.children]), left, false);
+    const u64 goal = share_floor(uniform(last_u), left, false);
     if (mode == IN_ROW && gones) {                      // the sums without the rejected tokens
         if (threadIdx.x == 0) {
             u64 less = 0;
