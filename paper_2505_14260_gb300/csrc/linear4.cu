@@ -225,11 +225,11 @@ static cudaError_t launch_few(const T *x, long ldx, int m, const Weight &w, floa
     return e;
 }
 
-// The bf16 nearest to span / n (ties to even), span = hi + lo exactly, n = 7 or 15, span >= 0. The
-// fp32 quotient may sit on the other side of the midpoint of two bf16 values than the true one;
-// n times the midpoint is exact, so the comparison is made there.
+// The bf16 nearest to span / n (ties to even), span = hi + lo exactly, n = 7 or 15, span >= 0. The fp32 product may sit on the
+// other side of a bf16 value or of the midpoint of two than the quotient; n times the midpoint above the lower one is exact, so the
+// comparison is made there, and either neighbour leads to the right one.
 __device__ __forceinline__ float scale_of(float hi, float lo, float n) {
-    const float q = hi / n;
+    const float q = hi * (n == 7.f ? 1.f / 7.f : 1.f / 15.f);
     const unsigned below = __float_as_uint(q) & 0xFFFF0000u;
     const float mid = __uint_as_float(below | 0x8000u);
     const float over = fmaf(-n, mid, hi) + lo;
@@ -237,17 +237,29 @@ __device__ __forceinline__ float scale_of(float hi, float lo, float n) {
     return s >= 0x1p-126f ? s : 0.f;                    // 1 / s is finite
 }
 
-// w / s to the nearest integer, ties to even, |w / s| <= 16. The residual w - q s is exact, so it shows where the
-// rounded product w (1 / s) fell on the wrong side of a border.
-__device__ __forceinline__ float nearest(float w, float s, float inv) {
-    float q = rintf(w * inv);
-    const float r = fmaf(-q, s, w), twice = r + r;
-    if (fabsf(twice) >= s) {
-        const bool odd = (int)q & 1;
-        if (twice > s || (twice == s && odd)) q += 1.f;
-        else if (twice < -s || (twice == -s && odd)) q -= 1.f;
-    }
-    return q;
+// 1 / s to an ulp, s normal and below 2^126.
+__device__ __forceinline__ float reciprocal(float s) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+    return r;
+}
+
+// w / s to the nearest integer, ties to even, |w / s| <= 16, inv about 1 / s, half = s / 2 (0, infinity: 0 for every w). The
+// residual w - q s is exact, so it shows where the rounded product w (1 / s) fell on the wrong side of a border. Adding 1.5 * 2^23
+// rounds to an integer whose lowest bit is the sum's.
+__device__ __forceinline__ float nearest(float w, float s, float inv, float half) {
+    constexpr float MAGIC = 12582912.f;
+    const float t = fmaf(w, inv, MAGIC), q = t - MAGIC;
+    const float r = fmaf(-q, s, w);
+    const bool off = fabsf(r) > half || (fabsf(r) == half && (__float_as_uint(t) & 1u));
+    return off ? q + copysignf(1.f, r) : q;
+}
+
+// The same for a w of bf16 (and s always is): 2 w and an odd multiple of s are whole multiples of a power of two, so w / s is
+// half an integer or at least 2^-11 away from it, and rounding w (1 / s) to multiples of 2^-11 first tells which.
+__device__ __forceinline__ float nearest_bf16(float w, float inv) {
+    constexpr float MAGIC = 12582912.f, FINE = 6144.f;          // 1.5 * 2^23, 1.5 * 2^12
+    return (fmaf(w, inv, FINE) - FINE) + MAGIC - MAGIC;
 }
 
 __device__ __forceinline__ void load8(const float *p, float (&v)[8]) {
@@ -277,28 +289,25 @@ __device__ __forceinline__ void store8(bf16 *p, const float (&v)[8]) {
     __stcs(reinterpret_cast<uint4 *>(p), make_uint4(u[0], u[1], u[2], u[3]));
 }
 
-// Codes of a matrix: 8 consecutive elements a lane, 4, 8 or 16 lanes a group, so a warp has a run of 256 elements of a
+// Codes of a matrix: 8 consecutive elements a lane, 4, 8 or 16 lanes a group, so a warp has runs of 256 elements of a
 // row and reads, and writes codes and values, in whole lines. Each value is read once; what bounds it is memory.
 constexpr int Q_THREADS = 256, Q_RUN = 256;
 template <typename T, int GROUP, bool ZEROS>
 __global__ void __launch_bounds__(Q_THREADS)
-quantize4_kernel(const T *__restrict__ x, long ldw, Weight w, T *__restrict__ values, long ldv, int runs, long tasks) {
-    constexpr int LANES = GROUP / 8, U = 2;                 // U runs in flight a warp
+quantize4_kernel(const T *__restrict__ x, long ldw, Weight w, T *__restrict__ values, long ldv, int runs) {
+    constexpr int LANES = GROUP / 8, U = sizeof(T) == 2 ? 4 : 2;            // U runs in flight a warp
     wait_prior();
     allow_dependents();
     const int lane = threadIdx.x & 31;
-    const long t0 = ((long)blockIdx.x * (Q_THREADS / 32) + (threadIdx.x >> 5)) * U;
+    const unsigned t = blockIdx.x * (Q_THREADS / 32) + (threadIdx.x >> 5);
+    const int j = (int)(t / (unsigned)runs), k0 = (int)(t - (unsigned)j * (unsigned)runs) * (U * Q_RUN) + lane * 8;
+    if (j >= w.o) return;
     float v[U][8];
-    int j[U], k[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const unsigned long t = t0 + u;
-        j[u] = (int)(tasks <= 0x7FFFFFFF ? (unsigned)t / (unsigned)runs : t / (unsigned)runs);
-        k[u] = (int)(t - (unsigned long)j[u] * runs) * Q_RUN + lane * 8;
-        if ((long)t < tasks && k[u] < w.k) {
-            load8(x + (long)j[u] * ldw + k[u], v[u]);
+        if (k0 + u * Q_RUN < w.k) {
+            load8(x + (long)j * ldw + k0 + u * Q_RUN, v[u]);
         } else {
-            k[u] = w.k;
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
         }
@@ -324,38 +333,41 @@ quantize4_kernel(const T *__restrict__ x, long ldw, Weight w, T *__restrict__ va
         if (ZEROS) {
             const float d = hi - lo, b = d - hi;            // d + its rounding error = hi - lo
             s = scale_of(d, (hi - (d - b)) + (-lo - b), 15.f);
-            z = s > 0.f ? fminf(fmaxf(nearest(-lo, s, 1.f / s), 0.f), 15.f) : 0.f;
+            z = s > 0.f ? fminf(fmaxf(nearest(-lo, s, reciprocal(s), 0.5f * s), 0.f), 15.f) : 0.f;
         } else {
             s = scale_of(hi, 0.f, 7.f);
         }
-        if (k[u] >= w.k) continue;
-        const long g = (long)j[u] * w.groups + k[u] / GROUP;
+        const int k = k0 + u * Q_RUN;
+        if (k >= w.k) continue;
+        const long g = (long)j * w.groups + k / GROUP;
         if ((lane & (LANES - 1)) == 0) {
             w.scales[g] = __float2bfloat16(s);
             if (ZEROS) w.zeros[g] = (uint8_t)z;
         }
-        const float inv = s > 0.f ? 1.f / s : 0.f, most = 16.f * s;
+        const float inv = s > 0.f ? reciprocal(s) : 0.f, half = s > 0.f ? 0.5f * s : INFINITY;
         uint32_t word = 0;
         float back[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float c = v[u][i] == v[u][i] ? fminf(fmaxf(v[u][i], -most), most) : 0.f;
-            const float q = s > 0.f ? fminf(fmaxf(nearest(c, s, inv) + z, 0.f), 15.f) : z;
-            word |= (uint32_t)q << (4 * i);
+            const float c = v[u][i] == v[u][i] ? v[u][i] : 0.f;
+            float q = (sizeof(T) == 2 ? nearest_bf16(c, inv) : nearest(c, s, inv, half)) + z;
+            if (ZEROS) q = fminf(q, 15.f);                  // (7.03 steps at most without zeros, none below the zero with them)
+            word |= (__float_as_uint(q + 12582912.f) & 15u) << (4 * i);
             back[i] = s * (q - z);
         }
-        reinterpret_cast<uint32_t *>(w.codes)[(long)j[u] * (w.k / 8) + k[u] / 8] = word;
-        if (values) store8(values + (long)j[u] * ldv + k[u], back);
+        reinterpret_cast<uint32_t *>(w.codes)[(long)j * (w.k / 8) + k / 8] = word;
+        if (values) store8(values + (long)j * ldv + k, back);
     }
 }
 
 template <typename T, int GROUP>
 static cudaError_t launch_quantize(const T *x, long ldw, const Weight &w, T *values, long ldv, cudaStream_t s) {
-    const int runs = (w.k + Q_RUN - 1) / Q_RUN;
-    const long tasks = (long)w.o * runs, ctas = (tasks + Q_THREADS / 32 * 2 - 1) / (Q_THREADS / 32 * 2);
-    if (ctas > 0x7FFFFFFF) return cudaErrorInvalidValue;
-    const cudaError_t e = w.zeros ? launch_chain(quantize4_kernel<T, GROUP, true>, (unsigned)ctas, Q_THREADS, 0, s, x, ldw, w, values, ldv, runs, tasks)
-                                  : launch_chain(quantize4_kernel<T, GROUP, false>, (unsigned)ctas, Q_THREADS, 0, s, x, ldw, w, values, ldv, runs, tasks);
+    constexpr int U = sizeof(T) == 2 ? 4 : 2;
+    const int runs = (w.k + U * Q_RUN - 1) / (U * Q_RUN);
+    const long ctas = ((long)w.o * runs + Q_THREADS / 32 - 1) / (Q_THREADS / 32);
+    if (ctas * (Q_THREADS / 32) > 0x7FFFFFFF) return cudaErrorInvalidValue;
+    const cudaError_t e = w.zeros ? launch_chain(quantize4_kernel<T, GROUP, true>, (unsigned)ctas, Q_THREADS, 0, s, x, ldw, w, values, ldv, runs)
+                                  : launch_chain(quantize4_kernel<T, GROUP, false>, (unsigned)ctas, Q_THREADS, 0, s, x, ldw, w, values, ldv, runs);
     note_launch();
     return e;
 }
