@@ -1,6 +1,7 @@
 """Several questions about one image, decoded from one pool of cache pages.
 
-    python examples/shared_image.py [--questions 4] [--tokens 24] [--dtype bf16]
+    python examples/shared_image.py [--questions 4] [--tokens 24] [--dtype bf16] [--bits 4]
+                                    [--temperature 0.7 --top-p 0.9]
 
 A small decoder of random weights (grouped heads, one layer with a window) whose cache is a
 Pages pool, driven as a serving program drives its own model:
@@ -12,7 +13,11 @@ Pages pool, driven as a serving program drives its own model:
 4. the answers are decoded twice, on forks of their own: token by token, and with a tree of
    drafts a pass that is verified at once and of which the accepted path stays. The drafts
    here are the first decode's tokens, wrong now and then, with random siblings: what counts
-   is that both decodes give the same tokens while the second takes fewer passes.
+   is that both decodes give the same tokens while the second takes fewer passes. (At a
+   temperature both draw from the same distributions, but not the same tokens.)
+
+With --bits 4 every projection and the head are 4-bit weights (msd.Weight4). Tokens come from
+msd.sample, accepted paths from msd.accept.
 """
 from __future__ import annotations
 
@@ -45,7 +50,10 @@ def batch(seqs, counts):
 
 
 def linear(x, w):
-    """x @ w.T in fp32: the library's GEMM for bf16 weights."""
+    """x @ w.T in fp32: the library's GEMM for bf16 weights, its products with 4-bit ones."""
+    if isinstance(w, msd.Weight4):
+        x = x.contiguous()
+        return w.linear(x, torch.empty(x.shape[0], w.o, device="cuda"))
     if w.dtype == torch.float32:
         return x.float() @ w.T
     x, y = x.to(w.dtype).contiguous(), torch.empty(x.shape[0], w.shape[0], device="cuda")
@@ -62,9 +70,13 @@ def norm(x):
 
 
 class Decoder:
-    def __init__(self, pages, dtype, seed=0):
+    def __init__(self, pages, dtype, seed=0, bits=16):
         g = torch.Generator(device="cuda").manual_seed(seed)
-        mat = lambda o, i: (torch.randn(o, i, generator=g, device="cuda") * i ** -0.5).to(dtype)  # noqa: E731
+
+        def mat(o, i):
+            w = (torch.randn(o, i, generator=g, device="cuda") * i ** -0.5).to(dtype)
+            return msd.Weight4.of(w, group=64, zeros=True) if bits == 4 else w
+
         self.pages, self.dtype = pages, dtype
         self.embed = torch.randn(VOCAB, HIDDEN, generator=g, device="cuda")
         width = (HEADS + 2 * KV_HEADS) * HEAD_DIM
@@ -75,16 +87,19 @@ class Decoder:
     def forward(self, b, x, pos, tree=None):
         """Rows x of the batch (their slots reserved) through the layers; the logits."""
         for i, w in enumerate(self.layers):
-            q, k, v = linear(norm(x), w["qkv"]).split([HEADS * HEAD_DIM, KV_HEADS * HEAD_DIM, KV_HEADS * HEAD_DIM], 1)
+            q, k, v = linear(self.cast(norm(x)), w["qkv"]).split([HEADS * HEAD_DIM, KV_HEADS * HEAD_DIM, KV_HEADS * HEAD_DIM], 1)
             turned = torch.empty(b.rows, HEADS, HEAD_DIM, device="cuda", dtype=self.dtype)
             self.pages.rope_append(i, b, q, k, v, pos, turned)
             seen = torch.empty_like(turned)
             narrow = dict(window=WINDOW, sinks=SINKS) if i == 1 else {}
             self.pages.attention(i, b, turned, seen, tree=tree, **narrow)
             x = x + linear(seen.view(b.rows, -1), w["o"])
-            gate, up = linear(norm(x), w["up"]).chunk(2, 1)
-            x = x + linear(torch.nn.functional.silu(gate) * up, w["down"])
-        return linear(norm(x), self.head)
+            gate, up = linear(self.cast(norm(x)), w["up"]).chunk(2, 1)
+            x = x + linear(self.cast(torch.nn.functional.silu(gate) * up), w["down"])
+        return linear(self.cast(norm(x)), self.head)
+
+    def cast(self, x):
+        return x.to(self.dtype)
 
 
 def draft_tree(n, want, nodes, rng, root):
@@ -112,12 +127,20 @@ def draft_tree(n, want, nodes, rng, root):
     return tree, tokens, parents
 
 
-def run(questions=4, tokens=24, dtype="bf16", nodes=16, seed=0, say=print):
+def run(questions=4, tokens=24, dtype="bf16", nodes=16, seed=0, say=print, bits=16, temperature=0.0, top_p=1.0):
     rng = random.Random(seed)
+    uniform = torch.Generator(device="cuda").manual_seed(seed + 2)
+    settings = msd.Filter(temperature=torch.full((questions,), temperature, device="cuda"),
+                          top_p=torch.full((questions,), top_p, device="cuda"))
+
+    def draw(logits):
+        u = torch.rand(questions, generator=uniform, device="cuda")
+        return msd.sample(logits, u, settings, torch.empty(questions, dtype=torch.int32, device="cuda")).long()
+
     page, seqs = 16, 1 + 3 * questions
     pages = msd.Pages(dtype=dtype, layers=LAYERS, heads=HEADS, kv_heads=KV_HEADS, head_dim=HEAD_DIM, page_size=page,
                       n_pages=64 + questions * 24, max_seqs=seqs, max_pages=64, rot_sections=(8, 12, 12))
-    model = Decoder(pages, pages.dtype, seed)
+    model = Decoder(pages, pages.dtype, seed, bits)
 
     # 1. the shared prompt: 8 text tokens, the image, 5 text tokens
     rows, image = 8 + GRID * GRID + 5, GRID * GRID
@@ -141,7 +164,7 @@ def run(questions=4, tokens=24, dtype="bf16", nodes=16, seed=0, say=print):
     pages.positions(b, None, None, pos, place, first=after.expand(questions).contiguous())
     logits = model.forward(b, model.embed[torch.tensor(sum(texts, []), device="cuda")], pos)
     last = b.row_start[1:].long() - 1
-    first = logits[last].argmax(1)
+    first = draw(logits[last])
     say(f"{questions} questions: {int((pages.refs > 0).sum())} pages, {shared} of them the prompt's; "
         f"without sharing {sum(-(-int(n) // page) for n in pages.lens[1:1 + questions])}")
 
@@ -152,7 +175,7 @@ def run(questions=4, tokens=24, dtype="bf16", nodes=16, seed=0, say=print):
     b = batch(plain, [1] * questions)
     for _ in range(tokens):
         pages.reserve(b)
-        token = model.forward(b, model.embed[token], at[None]).argmax(1)
+        token = draw(model.forward(b, model.embed[token], at[None]))
         at += 1
         for s, t in enumerate(token.tolist()):
             got[s].append(t)
@@ -168,19 +191,17 @@ def run(questions=4, tokens=24, dtype="bf16", nodes=16, seed=0, say=print):
         want = [got[s][len(fast[s]):] for s in range(questions)]
         tree, toks, parents = draft_tree(questions, want, nodes, rng, [f[-1] for f in fast])
         pos = (at[:, None] + tree.depth.view(questions, nodes)).view(1, -1)
-        best = model.forward(b, model.embed[torch.tensor(sum(toks, []), device="cuda")], pos, tree).argmax(1)
-        best, keep = best.view(questions, nodes).tolist(), []
-        for s in range(questions):                # follow the child that the target agrees with
-            path, more = [0], True
-            while more:
-                node = path[-1]
-                more = next((i for i in range(1, nodes) if parents[s][i] == node and toks[s][i] == best[s][node]), None)
-                if more:
-                    path.append(more)
-            keep.append(path)
-            fast[s] += [best[s][n] for n in path]
-        n_keep = i32([len(k) for k in keep])
-        pages.compact(b, i32([k + [-1] * (nodes - len(k)) for k in keep]), n_keep)
+        tree.tokens.copy_(i32(sum(toks, [])))
+        tree.parent.copy_(i32(sum(parents, [])))
+        logits = model.forward(b, model.embed[tree.tokens], pos, tree)
+        u = torch.rand(questions, nodes, nodes + 1, generator=uniform, device="cuda")
+        path = torch.empty(questions, nodes, dtype=torch.int32, device="cuda")
+        length, bonus = torch.empty_like(path[:, 0]), torch.empty_like(path[:, 0])
+        msd.accept(logits, b, tree, u, settings, path, length, bonus)
+        n_keep = length + 1
+        pages.compact(b, path, n_keep)
+        for s, (way, n, last_token) in enumerate(zip(path.tolist(), length.tolist(), bonus.tolist())):
+            fast[s] += [toks[s][node] for node in way[1:n + 1]] + [last_token]
         at += n_keep
         passes += 1
     same = [f[: tokens + 1] == g for f, g in zip(fast, got)]
@@ -196,8 +217,11 @@ def main():
     ap.add_argument("--questions", type=int, default=4)
     ap.add_argument("--tokens", type=int, default=24)
     ap.add_argument("--dtype", choices=("bf16", "f32"), default="bf16")
+    ap.add_argument("--bits", type=int, choices=(4, 16), default=16, help="of the weights (16: the dtype's own)")
+    ap.add_argument("--temperature", type=float, default=0.0)
+    ap.add_argument("--top-p", type=float, default=1.0)
     a = ap.parse_args()
-    run(a.questions, a.tokens, a.dtype)
+    run(a.questions, a.tokens, a.dtype, bits=a.bits, temperature=a.temperature, top_p=a.top_p)
 
 
 if __name__ == "__main__":
