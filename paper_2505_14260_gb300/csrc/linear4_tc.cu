@@ -32,16 +32,21 @@
 namespace msd {
 namespace {
 
-constexpr int TILE = 128, CHUNK = 128, OUT = 256;
-constexpr uint32_t WBOX = TILE * CHUNK / 2, WSTAGE = 2 * WBOX;
+constexpr int TILE = 128, CHUNK = 128;
+constexpr uint32_t WBOX = TILE * CHUNK / 2;
 constexpr uint32_t SMEM_MOST = 227 * 1024 - 2048;               // less static shared memory
 constexpr int CODE_WARPS = 16, SUM_WARPS = 8, THREADS = 1024;
-constexpr int AHEAD = 4;                                        // chunks (even, and less than a ring has stages)
+constexpr int AHEAD = 4;                                        // chunks (a multiple of a cycle, and less than a ring has stages)
 constexpr int COPY_0 = 4, SUM_0 = 8, CODE_0 = SUM_0 + SUM_WARPS;                   // first warps of the roles
 
 template <typename T, int GROUP, int N>
 struct Lay {
     static constexpr bool SPLIT = sizeof(T) == 4;               // x in planes
+    // WIDE: 128 outputs and 128 rows of x; the four groups of code warps take every fourth chunk, the two of sum warps half of the rows of x
+    static constexpr bool WIDE = N > 64;
+    static constexpr int OUT = WIDE ? TILE : 2 * TILE, CYCLE = WIDE ? 4 : 2, TOK = WIDE ? N / 2 : N;
+    static constexpr uint32_t WSTAGE = OUT / TILE * WBOX;
+    static constexpr bool IN_ORDER = WIDE;                      // x as copied; else in the order of a word's shifts
     static constexpr int P = Octet<T>::PLANES, PER = CHUNK / GROUP;
     // registers by role: over the eight groups of four warps they are the launch's 64 a thread
     static constexpr int R_CODE = 56, R_SUM = SPLIT ? 96 : 104, R_ISSUE = 40, R_COPY = SPLIT ? 56 : 40;
@@ -49,8 +54,8 @@ struct Lay {
     static constexpr uint32_t XBOX = N * 128, XPLANE = 2 * XBOX, XSTAGE = P * XPLANE;
     static constexpr int XS = SPLIT && N > 16 ? 2 : 4;          // even: a stage's chunks are all even or all odd ones
     static constexpr int X_PARTS = SPLIT ? 4 / XS : 1;          // warps that fill a stage of x
-    static constexpr int WS = 6;
-    static constexpr int DS = 128 / N, HS = DS / 2;             // accumulators of a half, of its even or odd chunks
+    static constexpr int WS = WIDE ? 8 : 6;
+    static constexpr int DS = WIDE ? 2 : 128 / N, HS = DS / 2;  // accumulators of a half (WIDE: in all), of its even or odd chunks
     static constexpr uint32_t X = 0, W = XS * XSTAGE, SCALES = W + WS * WSTAGE;
     static constexpr uint32_t ROOM = SMEM_MOST - 1024 - SCALES; // for scales and zeros
     static constexpr uint32_t T_A = 0, T_D = 128, T_HALF = 256; // columns of a half
@@ -86,6 +91,15 @@ __device__ __forceinline__ void sts16(uint32_t a, const uint32_t *v) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
 
+// Codes 2 i and 2 i + 1 of a word (byte i) less the zero, as a bf16 pair. The even one is put below 128, the odd one, from
+// the word shifted by one bit, at the third bit below 16; off: 128 + zero and 16 + zero.
+__device__ __forceinline__ uint32_t pair_in_order(uint32_t word, int i, __nv_bfloat162 off) {
+    uint32_t v = __byte_perm(word, word >> 1, 0x0400 | i | i << 8);
+    asm("lop3.b32 %0, %0, 0x0078000F, 0x41804300, 0xEA;" : "+r"(v));                     // (a & b) | c
+    const __nv_bfloat162 d = __hsub2(*reinterpret_cast<__nv_bfloat162 *>(&v), off);
+    return *reinterpret_cast<const uint32_t *>(&d);
+}
+
 // A warp waits for the barrier's use-th completion (in laps of `lap` uses). It sleeps in the barrier for up to 20 us at a time: what
 // polls takes issue slots, and they are what the kernel runs out of.
 __device__ __forceinline__ bool use_wait_slow(uint32_t bar, uint32_t parity, volatile int *abort) {
@@ -114,7 +128,9 @@ template <typename T, int GROUP, int N>
 __global__ void __launch_bounds__(THREADS, 1)
 linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap x_map, const Args a) {
     using L = Lay<T, GROUP, N>;
-    constexpr int PER = L::PER, P = L::P, XS = L::XS, WS = L::WS, DS = L::DS, HS = L::HS;
+    constexpr int PER = L::PER, P = L::P, XS = L::XS, WS = L::WS, DS = L::DS, HS = L::HS, OUT = L::OUT, CYCLE = L::CYCLE;
+    constexpr bool WIDE = L::WIDE;
+    constexpr uint32_t WSTAGE = L::WSTAGE;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * WS + 3 * XS + 16 + 4 * DS];
     __shared__ uint32_t s_tmem;
@@ -131,11 +147,11 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     if (tid == 0) {
         for (int i = 0; i < WS; ++i) {
             bar_init(w_full + 8 * i, 1);
-            bar_init(w_empty + 8 * i, 8);
+            bar_init(w_empty + 8 * i, WIDE ? 4 : 8);
         }
         for (int i = 0; i < XS; ++i) {
             bar_init(x_full + 8 * i, L::X_PARTS);
-            bar_init(x_empty + 8 * i, 2);
+            bar_init(x_empty + 8 * i, WIDE ? 1 : 2);
             bar_init(x_raw + 8 * i, 1);
         }
         for (int i = 0; i < 8; ++i) {
@@ -144,7 +160,7 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         }
         for (int i = 0; i < 2 * DS; ++i) {
             bar_init(d_full + 8 * i, 1);
-            bar_init(d_empty + 8 * i, 4);
+            bar_init(d_empty + 8 * i, WIDE ? 8 : 4);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_abort = 0;
@@ -190,31 +206,31 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     if (warp >= CODE_0) {
         // ---- codes to tensor memory ---------------------------------------------------------------
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::R_CODE));
-        const int half = (warp - CODE_0) >> 3, slot = (warp - CODE_0) >> 2 & 1, row = (warp & 3) * 32 + lane, out = half * TILE + row;
-        const uint32_t t_a = tmem + ((uint32_t)(warp & 3) << 21) + half * L::T_HALF + L::T_A + slot * 64;
+        const int g = (warp - CODE_0) >> 2, half = WIDE ? 0 : g >> 1, slot = g % CYCLE, row = (warp & 3) * 32 + lane, out = half * TILE + row;
+        const uint32_t t_a = tmem + ((uint32_t)(warp & 3) << 21) + (g >> 1) * L::T_HALF + L::T_A + (g & 1) * 64;
         const uint32_t code_row = base + L::W + half * WBOX + row * 64, swz = (uint32_t)(row >> 1 & 3) << 4;
         const uint8_t *const z_at = a.staged ? s_zeros + out : a.w.zeros + (long)(j0 + min(out, outs - 1)) * a.w.groups + g0;
         const int z_step = a.staged ? ZPITCH : 1;
-        const bool copies = !a.direct && (warp == CODE_0 || warp == CODE_0 + 4);         // (a warp for the even chunks, one for the odd ones)
+        const bool copies = !a.direct && (warp & 3) == 0 && g < CYCLE;                 // (a warp for each place in the cycle)
         const uint32_t on = elect_one();
-        int copied = slot;                                      // chunks copied: slot, slot + 2, ... below this
+        int copied = slot;                                      // chunks copied: slot, slot + CYCLE, ... below this
         const auto copy = [&](int ci) {
             const int ws = ci % WS;
             if (!use_wait(w_empty + 8 * ws, ci + WS, WS, &s_abort)) return;
             const uint32_t to = base + L::W + ws * WSTAGE, bar = w_full + 8 * ws;
             w_expect_tx(on, bar, WSTAGE);
             w_tma2d(on, to, &map, (c0 + ci) * (CHUNK / 2), j0, bar);
-            w_tma2d(on, to + WBOX, &map, (c0 + ci) * (CHUNK / 2), j0 + TILE, bar);
-            copied = ci + 2;
+            if constexpr (!WIDE) w_tma2d(on, to + WBOX, &map, (c0 + ci) * (CHUNK / 2), j0 + TILE, bar);
+            copied = ci + CYCLE;
         };
         if (copies)
-            for (int ci = slot; ci < min(nc, AHEAD); ci += 2) copy(ci);
+            for (int ci = slot; ci < min(nc, AHEAD); ci += CYCLE) copy(ci);
         if (a.staged && a.w.zeros) {
             stage(s_zeros, a.w.zeros, ZPITCH, tid - CODE_0 * 32, CODE_WARPS * 32);
             asm volatile("bar.sync 1, 512;" ::: "memory");
         }
         bool ok = true;
-        for (int ci = slot; ci < nc && ok; ci += 2) {
+        for (int ci = slot; ci < nc && ok; ci += CYCLE) {
             const int ws = ci % WS;
             if (copies && ci + AHEAD < nc) copy(ci + AHEAD);
             uint32_t from = code_row + ws * WSTAGE;
@@ -252,18 +268,18 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             // 64 elements at a time, so that the MMAs of the first are done when the next chunk's come
 #pragma unroll
             for (int sub = 0; sub < 2; ++sub) {
-                const uint32_t bar = 8 * ((half * 2 + slot) * 2 + sub);
-                ok = ok && use_wait(a_empty + bar, ci + 2, 2, &s_abort);
+                const uint32_t bar = 8 * (g * 2 + sub);
+                ok = ok && use_wait(a_empty + bar, ci + CYCLE, CYCLE, &s_abort);
                 if (!ok) break;
                 fence_after();
 #pragma unroll
                 for (int i = 2 * sub; i < 2 * sub + 2; ++i) {   // 32 elements: 16 columns
-                    const uint32_t both = (0x4300u + z[i * 32 / GROUP]) * 0x10001u;
+                    const uint32_t zero = z[i * 32 / GROUP], both = L::IN_ORDER ? 0x41804300u + zero * 0x00080001u : 0x43004300u + zero * 0x10001u;
                     const __nv_bfloat162 off = *reinterpret_cast<const __nv_bfloat162 *>(&both);
                     const uint32_t f[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
                     uint32_t p[16];
 #pragma unroll
-                    for (int c = 0; c < 16; ++c) p[c] = pair_of(f[c >> 2] >> (4 * (c & 3)), off);
+                    for (int c = 0; c < 16; ++c) p[c] = L::IN_ORDER ? pair_in_order(f[c >> 2], c & 3, off) : pair_of(f[c >> 2] >> (4 * (c & 3)), off);
                     tmem_st16(t_a + 16 * i, p);
                 }
                 tmem_st_wait();
@@ -274,7 +290,7 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         }
         if (copies && s_abort) {                                // copies in flight land before the CTA goes on
             volatile int never = 0;
-            for (int ci = slot; ci < copied; ci += 2)
+            for (int ci = slot; ci < copied; ci += CYCLE)
                 if (ci + WS >= copied) bar_wait_slow(w_full + 8 * (ci % WS), (uint32_t)(ci / WS) & 1u, &never, nullptr);
             __syncwarp();
         }
@@ -282,33 +298,35 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     } else if (warp >= SUM_0) {
         // ---- sums to totals -------------------------------------------------------------------------
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::R_SUM));
-        const int half = (warp - SUM_0) >> 2, out = tid - SUM_0 * 32;
+        const int half = (warp - SUM_0) >> 2, out = (tid - SUM_0 * 32) % OUT, tok0 = WIDE ? half * L::TOK : 0;
         if (a.staged) {
-            stage(s_scales, a.w.scales, SPITCH, out, SUM_WARPS * 32);
+            stage(s_scales, a.w.scales, SPITCH, tid - SUM_0 * 32, SUM_WARPS * 32);
             asm volatile("bar.sync 2, 256;" ::: "memory");
         }
         const bf16 *const s_at = a.staged ? s_scales + out : a.w.scales + (long)(j0 + min(out, outs - 1)) * a.w.groups + g0;
         const int s_step = a.staged ? SPITCH : 1;
-        const uint32_t t_d = tmem + ((uint32_t)(warp & 3) << 21) + half * L::T_HALF + L::T_D;
-        float total[N];
+        const uint32_t t_d = tmem + ((uint32_t)(warp & 3) << 21) + L::T_D + (WIDE ? 0 : half * L::T_HALF);
+        constexpr int TOK = L::TOK;
+        float total[TOK];
 #pragma unroll
-        for (int i = 0; i < N; ++i) total[i] = 0.f;
+        for (int i = 0; i < TOK; ++i) total[i] = 0.f;
         bool ok = true;
         for (int gi = 0; gi < nc * PER; ++gi) {
             const int ci = gi / PER, li = (ci >> 1) * PER + gi % PER, ds = (ci & 1) * HS + li % HS;
             const float s = gi < gs && out < outs ? __bfloat162float(s_at[(long)gi * s_step]) : 0.f;
-            ok = use_wait(d_full + 8 * (half * DS + ds), li, HS, &s_abort);
+            const uint32_t bar = 8 * (WIDE ? ds : half * DS + ds), from = t_d + (WIDE ? ds * L::T_HALF + tok0 : ds * N);
+            ok = use_wait(d_full + bar, li, HS, &s_abort);
             if (!ok) break;
             fence_after();
             constexpr int STEP = 16;
 #pragma unroll
-            for (int i0 = 0; i0 < N; i0 += STEP) {
+            for (int i0 = 0; i0 < TOK; i0 += STEP) {
                 uint32_t d[STEP];
-                tmem_ld16(t_d + ds * N + i0, d);
-                if (i0 + STEP == N) {
+                tmem_ld16(from + i0, d);
+                if (i0 + STEP == TOK) {
                     fence_before();
                     __syncwarp();
-                    if (lane == 0) bar_arrive(d_empty + 8 * (half * DS + ds));
+                    if (lane == 0) bar_arrive(d_empty + bar);
                 }
 #pragma unroll
                 for (int i = 0; i < STEP; ++i) total[i0 + i] = fmaf(s, __uint_as_float(d[i]), total[i0 + i]);
@@ -316,17 +334,17 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         }
         if (!ok || s_abort)
 #pragma unroll
-            for (int i = 0; i < N; ++i) total[i] = NAN;
+            for (int i = 0; i < TOK; ++i) total[i] = NAN;
         done();
         const int j = j0 + out;
         if (a.split > 1) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) reinterpret_cast<float *>(smem)[i * OUT + out] = total[i];
+            for (int i = 0; i < TOK; ++i) reinterpret_cast<float *>(smem)[(tok0 + i) * OUT + out] = total[i];
         } else if (j < a.w.o) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if (i < rows) {
-                    float *at = a.y + (long)(i0 + i) * a.ldy + j;
+            for (int i = 0; i < TOK; ++i) {
+                if (tok0 + i < rows) {
+                    float *at = a.y + (long)(i0 + tok0 + i) * a.ldy + j;
                     *at = a.accumulate ? *at + total[i] : total[i];
                 }
             }
@@ -335,46 +353,69 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         // ---- MMAs ---------------------------------------------------------------------------------
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::R_ISSUE));
         const uint32_t on = elect_one();                        // (whole warps: addresses stay in uniform registers)
-        const int half = warp >> 1, slot = warp & 1;
-        const uint32_t id = idesc(TILE, N, 0), t = tmem + half * L::T_HALF;
-        bool ok = true;
+        // (WIDE: warps 0 and 1, of the even and the odd chunks)
+        const int half = WIDE ? 0 : warp >> 1, slot = warp & 1;
+        const uint32_t id = idesc(TILE, N, 0);
+        bool ok = !WIDE || warp < 2;
         for (int ci = slot; ci < nc && ok; ci += 2) {
+            const int g = WIDE ? ci & 3 : half * 2 + slot;
+            const uint32_t t_a = tmem + (g >> 1) * L::T_HALF + L::T_A + (g & 1) * 64;
             const int xs = ci % XS;
             ok = use_wait(x_full + 8 * xs, ci, XS, &s_abort);
             const uint64_t d_x = sdesc(base + L::X + xs * L::XSTAGE, 16, 1024);
 #pragma unroll
             for (int e = 0; e < PER; ++e) {
                 const int li = (ci >> 1) * PER + e, ds = slot * HS + li % HS;      // (no accumulator is shared by two warps' waits)
-                ok = ok && use_wait(d_empty + 8 * (half * DS + ds), li + HS, HS, &s_abort);
+                const uint32_t d_bar = 8 * (WIDE ? ds : half * DS + ds);
+                const uint32_t t_d = tmem + L::T_D + (WIDE ? ds * L::T_HALF : half * L::T_HALF + ds * N);
+                ok = ok && use_wait(d_empty + d_bar, li + HS, HS, &s_abort);
                 if (!ok) break;
                 fence_after();
 #pragma unroll
                 for (int kk = 0; kk < GROUP / 16; ++kk) {
                     const int k16 = e * (GROUP / 16) + kk;
-                    const uint32_t bar = 8 * ((half * 2 + slot) * 2 + (k16 >> 2));
+                    const uint32_t bar = 8 * (g * 2 + (k16 >> 2));
                     if (k16 % 4 == 0) {
-                        ok = ok && use_wait(a_full + bar, ci, 2, &s_abort);
+                        ok = ok && use_wait(a_full + bar, ci, CYCLE, &s_abort);
                         if (!ok) break;
                         fence_after();
                     }
 #pragma unroll
                     for (int p = 0; p < P; ++p)
-                        w_mma_ts(on, t + L::T_D + ds * N, t + L::T_A + slot * 64 + k16 * 8,
+                        w_mma_ts(on, t_d, t_a + k16 * 8,
                                  d_x + ((p * L::XPLANE + (k16 >> 2) * L::XBOX + (k16 & 3) * 32) >> 4), id, kk > 0 || p > 0);
                     if (k16 % 4 == 3) w_commit(on, a_empty + bar);
                 }
                 if (!ok) break;
-                w_commit(on, d_full + 8 * (half * DS + ds));
+                w_commit(on, d_full + d_bar);
             }
             if (ok) w_commit(on, x_empty + 8 * xs);
         }
         __syncwarp();
         done();
     } else {
-        // ---- copies of codes, of x ----------------------------------------------------------------
+        // ---- x ----------------------------------------------------------------
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::R_COPY));
         const int w = warp - COPY_0;
-        if constexpr (!L::SPLIT) {
+        if constexpr (L::IN_ORDER) {
+            if (w == 0) {
+                const uint32_t on = elect_one();
+                int ci = 0;
+                for (; ci < nc; ++ci) {
+                    const int xs = ci % XS;
+                    if (!use_wait(x_empty + 8 * xs, ci + XS, XS, &s_abort)) break;
+                    const uint32_t to = base + L::X + xs * L::XSTAGE, bar = x_full + 8 * xs;
+                    w_expect_tx(on, bar, L::XSTAGE);
+                    w_tma2d(on, to, &x_map, (c0 + ci) * CHUNK, i0, bar);
+                    w_tma2d(on, to + L::XBOX, &x_map, (c0 + ci) * CHUNK + 64, i0, bar);
+                }
+                if (s_abort) {                                  // copies in flight land before the CTA goes on
+                    volatile int never = 0;
+                    for (int c = max(0, ci - XS); c < ci; ++c) bar_wait_slow(x_full + 8 * (c % XS), (uint32_t)(c / XS) & 1u, &never, nullptr);
+                }
+                __syncwarp();
+            }
+        } else if constexpr (!L::SPLIT) {
             // a stage a warp: copied, then each 8 values put into the order of the codes' pairs where they lie
             static_assert(XS == 4, "");
             const uint32_t on = elect_one(), at = base + L::X + w * L::XSTAGE;
@@ -480,21 +521,26 @@ bool make_map(CUtensorMap *map, CUtensorMapDataType type, int size, const void *
                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Into how many parts K is cut. A part is a CTA that has an SM to itself, so what counts is how many clusters of that size fit the
-// GPU at once (GPCs have 16 to 20 SMs: 152, 76, 46, 36, 28, 23, 15 and 15 were counted) and what a CTA does beside its chunks:
-// about 6 chunks' time to start and to end, 3 more to join.
-int best_split(long tiles, int chunks) {
+// Into how many parts K is cut, and what that costs (in chunks of 256 outputs, 0.74 us). A part is a CTA that has an SM to itself, so
+// what counts is how many clusters of that size fit the GPU at once (GPCs have 16 to 20 SMs: 152, 76, 46, 36, 28, 23, 15 and 15 were
+// counted), a chunk's time and what a CTA does beside its chunks: about 6 chunks' time to start and to end, 3 more to join.
+struct Cut {
+    int split;
+    float cost;
+};
+Cut best_cut(long tiles, int chunks, float chunk) {
     constexpr int fit[8] = {152, 76, 46, 36, 28, 23, 15, 15};
-    int best = 1;
-    long least = -1;
+    Cut best{1, 0.f};
     for (int s = 1; s <= 8 && s <= chunks; ++s) {
-        const long cost = (tiles + fit[s - 1] - 1) / fit[s - 1] * ((chunks + s - 1) / s + 6 + (s > 1 ? 3 : 0));
-        if (least < 0 || cost < least) {
-            least = cost;
-            best = s;
-        }
+        const float cost = (tiles + fit[s - 1] - 1) / fit[s - 1] * (chunk * ((chunks + s - 1) / s) + 6 + (s > 1 ? 3 : 0));
+        if (s == 1 || cost < best.cost) best = {s, cost};
     }
     return best;
+}
+template <typename T, int GROUP, int N>
+Cut cut_of(const Args &a) {
+    using L = Lay<T, GROUP, N>;
+    return best_cut((long)((a.w.o + L::OUT - 1) / L::OUT) * ((a.m + N - 1) / N), (a.w.k + CHUNK - 1) / CHUNK, L::WIDE ? 0.68f : 1.f);
 }
 
 template <typename T, int GROUP, int N>
@@ -507,10 +553,10 @@ cudaError_t launch(Args a, cudaStream_t s) {
     if ((!a.direct && !make_map(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.w.codes, a.w.k / 2, a.w.o, a.w.k / 2, CHUNK / 2, TILE, CU_TENSOR_MAP_SWIZZLE_64B)) ||
         (!L::SPLIT && !make_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.x, a.w.k, a.m, a.ldx, 64, N, CU_TENSOR_MAP_SWIZZLE_128B)))
         return cudaErrorUnknown;
-    const int chunks = (a.w.k + CHUNK - 1) / CHUNK, tiles = (a.w.o + OUT - 1) / OUT, cols = (a.m + N - 1) / N;
-    a.split = best_split(tiles * cols, chunks);
+    const int chunks = (a.w.k + CHUNK - 1) / CHUNK, tiles = (a.w.o + L::OUT - 1) / L::OUT, cols = (a.m + N - 1) / N;
+    a.split = cut_of<T, GROUP, N>(a).split;
     const int slice = (chunks + a.split - 1) / a.split * L::PER;
-    const size_t beside = (size_t)slice * ((OUT + 2) * 2 + (a.w.zeros ? OUT + 4 : 0));
+    const size_t beside = (size_t)slice * ((L::OUT + 2) * 2 + (a.w.zeros ? L::OUT + 4 : 0));
     a.staged = beside <= L::ROOM;
     a.slice = a.staged ? slice : 0;
     const size_t smem = std::max<size_t>(L::SCALES + 1024 + (a.staged ? beside : 0), tmem_smem_floor(512));
@@ -537,8 +583,13 @@ cudaError_t launch(Args a, cudaStream_t s) {
 template <typename T, int GROUP>
 cudaError_t launch_n(const Args &a, cudaStream_t s) {
     if (a.m <= 16) return launch<T, GROUP, 16>(a, s);
-    if constexpr (sizeof(T) == 2)               // (planes of 64 rows would leave room for one stage)
+    if constexpr (sizeof(T) == 2) {             // (planes of 64 rows would leave room for one stage)
+        // 128 rows of x with 128 outputs, or 64 with 256: as many CTAs, and a chunk in 0.50 us instead of 0.74. (645 rows, k 4096,
+        // 11008 outputs: 83 us instead of 112.) Rows just past a multiple of 128 can leave the first with more waves:
+        // 130 rows of the same 41 us instead of 30.
+        if (a.m > 64 && cut_of<T, GROUP, 128>(a).cost < cut_of<T, GROUP, 64>(a).cost) return launch<T, GROUP, 128>(a, s);
         if (a.m > 32) return launch<T, GROUP, 64>(a, s);
+    }
     return launch<T, GROUP, 32>(a, s);
 }
 
