@@ -52,12 +52,6 @@ template <> struct Octet<float> {
         b[1][i] = __byte_perm(__float_as_uint(ra), __float_as_uint(rc), 0x7632);
         b[2][i] = __byte_perm(__float_as_uint(la), __float_as_uint(lc), 0x7632);
     }
-    __device__ __forceinline__ void planes(uint32_t (&b)[3][4]) const {          // in the order that they lie in
-        part(lo.x, lo.y, b, 0);
-        part(lo.z, lo.w, b, 1);
-        part(hi.x, hi.y, b, 2);
-        part(hi.z, hi.w, b, 3);
-    }
     __device__ __forceinline__ void pairs(uint32_t (&b)[3][4]) const {
         part(lo.x, hi.x, b, 0);
         part(lo.y, hi.y, b, 1);

@@ -2,24 +2,28 @@
 //
 // y = x W^T with W's rows as the M side: codes come by tensor copies (128 rows of 64 bytes), a
 // thread turns its row's codes into bf16 differences code - zero (exact) and puts them into tensor
-// memory as the A operand; x is the B operand, staged in shared memory once for 256 outputs. An
-// accumulator takes one group's products, and a group's sum is scaled on its way from tensor
-// memory into the thread's fp32 totals, so no weight is rounded: what is done per code is 11
-// integer and bf16 operations for 8 codes, one fused multiply per row of x for each group, and
-// nothing in the tensor cores that another form would save.
+// memory as the A operand; x is the B operand, staged in shared memory. An accumulator takes one
+// group's products, and a group's sum is scaled on its way from tensor memory into the thread's
+// fp32 totals, so no weight is rounded.
 //
-// A CTA (one an SM: it holds all of the tensor memory) has 256 outputs, two halves of 128, and up to N rows of x; K is
-// cut between the CTAs of a cluster where there are fewer tiles than SMs, and their totals meet through distributed
-// shared memory in rank order. Chunks are 128 elements of K. Roles:
+// A CTA (one an SM: it holds all of the tensor memory) has 256 outputs, two halves of 128, and up to 64 rows of x, or 128
+// outputs and 128 rows; K is cut between the CTAs of a cluster where there are fewer tiles than SMs, and their totals meet through
+// distributed shared memory in rank order. Chunks are 128 elements of K. Roles:
 //   warps 0-3    MMAs, of the even or the odd chunks of a half (first, since a scheduler prefers them: as the last warps, an
 //                MMA's issue took them 100 cycles)
-//   warps 4-7    x: copies of bf16, put into order; fp32 as three bf16 planes that add up to it, swizzled as the MMA reads them
+//   warps 4-7    x: copies of bf16, put into order where need be; fp32 as three bf16 planes that add up to it, swizzled as the MMA
+//                reads them
 //   warps 8-15   a row of W a thread: a group's sum from tensor memory, scaled, into fp32 totals
 //   warps 16-31  a row of W a thread: codes -> tensor memory; four warps for the even chunks of a half, four for the odd ones;
 //                the first of those also issue the copies of codes, four chunks ahead
-// What bounds it is the integer pipe: 8 selections for 8 codes, at half a warp a cycle, 512 cycles for a chunk of 256 outputs
-// (an MMA of such a chunk takes 128 to 512, a copy 330 at the rate of memory). One group of warps a half doing everything in turn
-// took 1800 cycles a chunk, waiting for one another. A wait that runs out (2 s) leaves NaN in the CTA's part of y.
+// What bounds it is the integer pipe, half a warp a cycle, and the issue slots behind it. For 8 codes, in the order of a word's
+// shifts ((0, 4), (1, 5), (2, 6), (3, 7), x ordered alike), it takes 3 shifts, 4 selections and 4 subtractions: about 1000 cycles
+// for a chunk of 256 outputs with scales, copies and waits, against 512 of the MMAs of 64 rows and 330 of a copy at the rate of
+// memory. With 128 rows to a CTA a chunk of 128 outputs takes 950 cycles, of them 512 of MMAs: there x stays as copied (ordering
+// 128 rows took the four copying warps longer than that) and codes come out in their own order, for 2 more operations of 8 codes.
+// To start and to end a CTA takes about 5 us. One group of warps a half doing everything in turn took 1800 cycles a chunk.
+// Measured, us (groups of 128, other weights for each call): k 4096, o 11008: 16 rows 13.5, 60 rows 16.4, 128 rows 22, 645 rows
+// 84 (690 TFLOP/s); k 11008, o 4096, 60 rows: 19.3. A wait that runs out (2 s) leaves NaN in the CTA's part of y.
 #include <algorithm>
 #include <cstring>
 #include <type_traits>
@@ -501,7 +505,7 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     cluster_sync();
 }
 
-// A matrix of `rows` rows of `bytes` bytes (a multiple of 16), `pitch` apart, as boxes of inner x height elements.
+// A matrix of rows x width elements of `size` bytes, `pitch` elements apart (a multiple of 16 bytes), in boxes of height x inner.
 bool make_map(CUtensorMap *map, CUtensorMapDataType type, int size, const void *p, long width, long rows, long pitch, int inner, int height,
               CUtensorMapSwizzle swizzle) {
     static PFN_cuTensorMapEncodeTiled_v12000 encode = [] {
@@ -521,7 +525,7 @@ bool make_map(CUtensorMap *map, CUtensorMapDataType type, int size, const void *
                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Into how many parts K is cut, and what that costs (in chunks of 256 outputs, 0.74 us). A part is a CTA that has an SM to itself, so
+// Into how many parts K is cut, and what a call costs then (in chunks of 256 outputs, 0.74 us). A part is a CTA that has an SM to itself, so
 // what counts is how many clusters of that size fit the GPU at once (GPCs have 16 to 20 SMs: 152, 76, 46, 36, 28, 23, 15 and 15 were
 // counted), a chunk's time and what a CTA does beside its chunks: about 6 chunks' time to start and to end, 3 more to join.
 struct Cut {

@@ -134,7 +134,7 @@ struct __align__(16) Shared {                   // (the sums and the slice lie b
     unsigned bucket, own_n[2], list_n[2], base[8];            // (a round may gather twice)
     unsigned range_lo, range_hi;                // keys of a bucket's tokens
     float end;
-    int tie, token;
+    int tie;
     int next, gones, gone[MAX_CHILDREN];
     unsigned short kid[MAX_CHILDREN];           // children of a node, and their tokens
     int kid_token[MAX_CHILDREN];
@@ -1043,10 +1043,7 @@ static cudaError_t launch_rows(void (*kernel)(K...), int rows, const Cut &c, cud
     return e;
 }
 
-static bool take_filter(const msd_filter *f, Settings *s) {
-    *s = f ? Settings{f->temperature, f->top_k, f->top_p, f->min_p} : Settings{};
-    return true;
-}
+static Settings settings_of(const msd_filter *f) { return f ? Settings{f->temperature, f->top_k, f->top_p, f->min_p} : Settings{}; }
 
 static bool bad_logits(const void *logits, long ld, int dtype, int V) {
     return !logits || (dtype != MSD_F32 && dtype != MSD_BF16) || V < 1 || V > MAX_VOCAB || ld < V ||
@@ -1066,8 +1063,7 @@ msd_status msd_sample(const void *logits, int64_t ld, int32_t dtype, int32_t row
     if (rows == 0) return MSD_OK;
     if (bad_logits(logits, ld, dtype, vocab) || !u || !tokens || (probs && (ldp < vocab || reinterpret_cast<uintptr_t>(probs) % 4)))
         return MSD_ERR_INVALID;
-    Settings s;
-    take_filter(f, &s);
+    const Settings s = settings_of(f);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const Cut c = cut_rows(rows, vocab, dtype == MSD_F32 ? 4 : 2);
     if ((long)rows * c.ctas > 0x7FFFFFFF) return MSD_ERR_INVALID;
@@ -1090,8 +1086,7 @@ msd_status msd_accept_batch(const void *logits, int64_t ld, int32_t dtype, int32
         !u || depth < 0 || depth > (1 << 20) || children < 1 || children > MAX_CHILDREN || !path || !accept_len || !bonus)
         return MSD_ERR_INVALID;
     if (batch->rows > 0 && (bad_logits(logits, ld, dtype, vocab) || !scratch)) return MSD_ERR_INVALID;
-    Settings s;
-    take_filter(f, &s);
+    const Settings s = settings_of(f);
     const TreeArgs a{batch->n, tree_nodes, depth, children, batch->row_start, tree->tokens, tree->parent, tree->n_nodes, u,
                      scratch, scratch + batch->rows, path, accept_len, bonus};
     cudaStream_t st = static_cast<cudaStream_t>(stream);

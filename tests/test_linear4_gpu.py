@@ -97,6 +97,12 @@ def test_many_rows(m):
     run(m, 1000, 130, 32, False, torch.float32)
 
 
+@pytest.mark.parametrize("m,o", [(129, 11008), (150, 12700), (192, 10000), (130, 19456), (256, 9856)])
+def test_rows_past_a_block(m, o):
+    """Where rows past a multiple of 128 make the fewest CTAs blocks of 64 rows, and beside it."""
+    run(m, 256, o, 128, True)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("m", [1, 11, 66, 200])
 def test_strides_and_neighbours(m, dtype):
