@@ -853,42 +853,52 @@ sample_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int slice,
     }
 }
 
-// Per node of the trees: the child that is accepted there, or -1 and the token drawn there.
+// Trees, and what becomes of their nodes: outcome[row] is the child that is accepted there, or -2 - the token drawn there.
 struct TreeArgs {
-    int n, nodes, depth, children;
+    int n, rows, nodes, depth, children;
     const int *row_start, *tokens, *parent, *n_nodes;
     const float *u;
-    int *next, *drawn;        // [rows]
+    int *outcome, *list;      // [rows]: see accept_plan_kernel
     int *path, *accept_len, *bonus;
 };
 
 __device__ __forceinline__ int nodes_of(const TreeArgs &a, int b) {
-    const int rows = min(a.row_start[b + 1] - a.row_start[b], a.nodes);
-    return a.n_nodes ? min(rows, a.n_nodes[b]) : rows;
+    const int start = a.row_start[b], rows = min(min(a.row_start[b + 1], a.rows) - start, a.nodes);
+    return start < 0 ? 0 : a.n_nodes ? min(rows, a.n_nodes[b]) : rows;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(ROW_THREADS, 2)
-accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int slice, Settings f, TreeArgs a) {
-    wait_prior();
-    allow_dependents();
-    Shared &sh = shared();
-    const int r = blockIdx.x / ctas, rank = blockIdx.x % ctas, lane = threadIdx.x & 31;
-    int b = 0;
-    for (int hi = a.n; hi - b > 1;) {                   // the last sequence that starts at or before the row
-        const int mid = (b + hi) >> 1;
-        if (a.row_start[mid] <= r) b = mid; else hi = mid;
+struct Node {
+    int b, node, n, d;        // its sequence, its index among n, drafts accepted there (more than depth: never reached)
+    int first;                // node 0's child above it, or itself
+};
+__device__ __forceinline__ Node node_of(const TreeArgs &a, int r) {
+    Node t{0, 0, 0, 0, 0};
+    for (int hi = a.n; hi - t.b > 1;) {                 // the last sequence that starts at or before the row
+        const int mid = (t.b + hi) >> 1;
+        if (a.row_start[mid] <= r) t.b = mid; else hi = mid;
     }
-    const int node = r - a.row_start[b], n = nodes_of(a, b);
-    const int *parent = a.parent + (long)b * a.nodes, *tokens = a.tokens + (long)b * a.nodes;
-    if (node < 0 || node >= n) return;
-    int d = 0;
-    for (int i = node; i > 0; ++d) {
+    t.node = r - a.row_start[t.b];
+    t.n = nodes_of(a, t.b);
+    if (t.node < 0 || t.node >= t.n) t.d = a.depth + 1;
+    return t;
+}
+__device__ __forceinline__ void find_depth(const TreeArgs &a, Node &t) {
+    const int *parent = a.parent + (long)t.b * a.nodes;
+    for (int i = t.node; i > 0 && t.d <= a.depth; ++t.d) {
         const int up = parent[i];
-        if (up < 0 || up >= i) { d = a.depth + 1; break; }
+        if (up < 0 || up >= i) { t.d = a.depth + 1; break; }
+        t.first = i;
         i = up;
     }
-    if (d > a.depth) return;                            // never reached (the whole cluster leaves)
+}
+
+// What becomes of a node whose parent is accepted.
+template <typename T>
+__device__ __forceinline__ void decide(const T *__restrict__ logits, long ld, int V, int ctas, int rank, int slice, const Settings &f,
+                                       const TreeArgs &a, int r, const Node &t) {
+    Shared &sh = shared();
+    const int lane = threadIdx.x & 31, b = t.b, node = t.node, n = t.n, d = t.d;
+    const int *parent = a.parent + (long)b * a.nodes, *tokens = a.tokens + (long)b * a.nodes;
     const T *row = logits + (long)r * ld;
     RowSettings settings;
     settings.request(f, b);
@@ -958,12 +968,14 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
             for (int i = lane; i < gone; i += 32) put(&sh.gone[i], p, sh.gone[i]);
     }
     meet();
-    if (rank == 0 && threadIdx.x == 0) a.next[r] = sh.next;
-    if (sh.next >= 0) return;
+    if (sh.next >= 0) {
+        if (rank == 0 && threadIdx.x == 0) a.outcome[r] = sh.next;
+        return;
+    }
     const int gones = sh.gones;
     const u64 left = sh.left;
     if (mode == ONE_TOKEN || left == 0) {
-        if (rank == 0 && threadIdx.x == 0) a.drawn[r] = left ? l.tie : -1;
+        if (rank == 0 && threadIdx.x == 0) a.outcome[r] = left ? -2 - l.tie : -1;
         return;
     }
     const u64 goal = share_floor(uniform(last_u), left, false);
@@ -981,8 +993,59 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
         }
         meet();
     }
-    const int t = mode == IN_ROW ? locate<T>(l, false, goal, gones) : locate_in_list((int)in_list, goal, gones);
-    if (t >= 0) a.drawn[r] = t;
+    const int id = mode == IN_ROW ? locate<T>(l, false, goal, gones) : locate_in_list((int)in_list, goal, gones);
+    if (id >= 0) a.outcome[r] = -2 - id;
+}
+
+// Which rows: each of them, a cluster each; the sequences' first ones; those that the plan lists, in turns.
+enum : int { EVERY = 0, ROOTS = 1, LISTED = 2 };
+
+template <typename T>
+__global__ void __launch_bounds__(ROW_THREADS, 2)
+accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int slice, Settings f, TreeArgs a, int which) {
+    wait_prior();
+    allow_dependents();
+    const int rank = blockIdx.x % ctas, count = which == LISTED ? a.list[a.rows - 1] : 0;
+    for (int i = blockIdx.x / ctas;; i += gridDim.x / ctas) {               // (the whole cluster does the same)
+        if (which == LISTED && i >= count) return;
+        const int r = which == EVERY ? i : which == ROOTS ? a.row_start[i] : a.list[i];
+        Node t;
+        if (which == ROOTS) {
+            t = Node{i, 0, nodes_of(a, i), 0, 0};
+            if (t.n < 1) return;
+        } else {
+            t = node_of(a, r);
+            if (which == EVERY) find_depth(a, t); else t.d = a.outcome[r];
+            if (t.d > a.depth) return;
+        }
+        decide(logits, ld, V, ctas, rank, slice, f, a, r, t);
+        if (which != LISTED) return;
+        __syncwarp();
+        // shared memory is free again, and every CTA has read the depth that outcome held
+        if (ctas > 1) asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        else __syncthreads();
+    }
+}
+
+// The rows behind the child that each sequence's first node accepts, in list[0 ..), their number in its last element (a first node
+// is not among them), and the drafts accepted there in outcome.
+__global__ void __launch_bounds__(1024)
+accept_plan_kernel(TreeArgs a) {
+    __shared__ int count;
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+    wait_prior();
+    allow_dependents();
+    for (int r = threadIdx.x; r < a.rows; r += blockDim.x) {
+        Node t = node_of(a, r);
+        if (t.d > a.depth || t.node == 0) continue;
+        find_depth(a, t);
+        if (t.d > a.depth || a.outcome[a.row_start[t.b]] != t.first) continue;
+        a.outcome[r] = t.d;
+        a.list[atomicAdd(&count, 1)] = r;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) a.list[a.rows - 1] = count;
 }
 
 __global__ void accept_walk_kernel(TreeArgs a) {
@@ -995,15 +1058,16 @@ __global__ void accept_walk_kernel(TreeArgs a) {
     const int start = a.row_start[b];
     for (; at >= 0 && d <= a.depth; ++d) {
         path[d] = at;
-        const int next = a.next[start + at];
-        if (next < 0) bonus = a.drawn[start + at];
-        at = next;
+        at = a.outcome[start + at];
+        if (at < 0) bonus = -2 - at;
     }
     a.accept_len[b] = max(d - 1, 0);
-    a.bonus[b] = bonus;
+    a.bonus[b] = max(bonus, -1);
     for (; d <= a.depth; ++d) path[d] = -1;
 }
 
+constexpr int RESIDENT = 2 * 152;               // CTAs that run at a time
+constexpr int STAGED_ABOVE = 2 * RESIDENT;
 static_assert(data_offset(most_blocks(MAX_VOCAB / 8, 4)) + (size_t)most_blocks(MAX_VOCAB / 8, 4) * BLOCK * 4 <= 227 * 1024, "the largest row fits");
 
 // How many CTAs share a row, and the ids of each: as few as leave room for two CTAs on an SM, 4 where there are few
@@ -1017,7 +1081,7 @@ static Cut cut_rows(int rows, int V, int size) {
     const auto slice_of = [&](int ctas) { return ((V + ctas - 1) / ctas + 7) / 8 * 8; };
     int c = 1;
     while (c < 8 && smem(slice_of(c)) > 112 * 1024) c *= 2;
-    while (c < 4 && (long)rows * c * 2 <= 304 && slice_of(c * 2) >= 2048) c *= 2;
+    while (c < 4 && (long)rows * c * 2 <= RESIDENT && slice_of(c * 2) >= 2048) c *= 2;
     return Cut{c, slice_of(c), smem(slice_of(c))};
 }
 
@@ -1087,18 +1151,32 @@ msd_status msd_accept_batch(const void *logits, int64_t ld, int32_t dtype, int32
         return MSD_ERR_INVALID;
     if (batch->rows > 0 && (bad_logits(logits, ld, dtype, vocab) || !scratch)) return MSD_ERR_INVALID;
     const Settings s = settings_of(f);
-    const TreeArgs a{batch->n, tree_nodes, depth, children, batch->row_start, tree->tokens, tree->parent, tree->n_nodes, u,
+    const TreeArgs a{batch->n, batch->rows, tree_nodes, depth, children, batch->row_start, tree->tokens, tree->parent, tree->n_nodes, u,
                      scratch, scratch + batch->rows, path, accept_len, bonus};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (batch->rows > 0) {
-        const Cut c = cut_rows(batch->rows, vocab, dtype == MSD_F32 ? 4 : 2);
-        if ((long)batch->rows * c.ctas > 0x7FFFFFFF) return MSD_ERR_INVALID;
-        const cudaError_t e =
-            dtype == MSD_F32
-                ? launch_rows(accept_rows_kernel<float>, batch->rows, c, st, static_cast<const float *>(logits), (long)ld, vocab, c.ctas,
-                              c.slice, s, a)
-                : launch_rows(accept_rows_kernel<bf16>, batch->rows, c, st, static_cast<const bf16 *>(logits), (long)ld, vocab, c.ctas,
-                              c.slice, s, a);
+        const int size = dtype == MSD_F32 ? 4 : 2;
+        const Cut c = cut_rows(batch->rows, vocab, size), roots = cut_rows(batch->n, vocab, size);
+        if ((long)batch->rows * c.ctas > 0x7FFFFFFF || (long)batch->n * roots.ctas > 0x7FFFFFFF) return MSD_ERR_INVALID;
+        const auto rows = [&](int which, const Cut &cut, int count) {
+            return dtype == MSD_F32 ? launch_rows(accept_rows_kernel<float>, count, cut, st, static_cast<const float *>(logits), (long)ld, vocab,
+                                                  cut.ctas, cut.slice, s, a, which)
+                                    : launch_rows(accept_rows_kernel<bf16>, count, cut, st, static_cast<const bf16 *>(logits), (long)ld, vocab,
+                                                  cut.ctas, cut.slice, s, a, which);
+        };
+        // Where the rows are more than the GPU holds at a time (two CTAs an SM), those of the first nodes go ahead, and of the others
+        // only the ones behind an accepted child follow.
+        cudaError_t e;
+        if ((long)batch->rows * c.ctas <= STAGED_ABOVE || depth == 0) {
+            e = rows(EVERY, c, batch->rows);
+        } else {
+            e = rows(ROOTS, roots, batch->n);
+            if (e == cudaSuccess) {
+                e = launch_chain(accept_plan_kernel, 1, 1024, 0, st, a);
+                note_launch();
+            }
+            if (e == cudaSuccess) e = rows(LISTED, c, std::min(batch->rows, RESIDENT / c.ctas));
+        }
         if (e != cudaSuccess) return MSD_ERR_CUDA;
     }
     if (launch_chain(accept_walk_kernel, (batch->n + 31) / 32, 32, 0, st, a) != cudaSuccess) return MSD_ERR_CUDA;

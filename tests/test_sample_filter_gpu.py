@@ -227,6 +227,20 @@ def test_trees(given, dtype):
         check_accept(x, counts, toks, pars, u, 60, **given)
 
 
+@pytest.mark.parametrize("given", [{}, dict(top_k=20, top_p=0.9), dict(temperature=0.0)], ids=str)
+@pytest.mark.parametrize("vocab,n,dtype", [(900, 40, torch.float32), (32000, 12, torch.float32), (70000, 7, torch.bfloat16), (300, 700, torch.float32)])
+def test_more_rows_than_fit(vocab, n, dtype, given):
+    """The first nodes ahead of the ones behind accepted children; some sequences without rows, of one, with fewer valid nodes."""
+    r = random.Random(n)
+    counts = [r.choice([60, 60, 47, 33, 1, 0]) for _ in range(n)] if n < 100 else [1 + i % 2 for i in range(n)]
+    counts[0] = 60
+    x = logits(sum(counts), vocab, 7, dtype, peaks=6)
+    toks, pars = trees(counts, 60, vocab, x, 7, width=3)
+    u = torch.rand(n, 7, 5, generator=gen(n), device="cuda") * 0.7                # (long paths too)
+    check_accept(x, counts, toks, pars, u, 60, **given)
+    check_accept(x, counts, toks, pars, u, 60, n_nodes=[c - c // 3 for c in counts], **given)
+
+
 def test_trees_with_odd_shapes():
     """Sequences without rows, fewer valid nodes than rows, one child a node at most, no depth, a chain,
     the same token twice among siblings, tokens outside the vocabulary, parents that do not precede."""
