@@ -855,7 +855,7 @@ sample_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int slice,
 
 // Trees, and what becomes of their nodes: outcome[row] is the child that is accepted there, or -2 - the token drawn there.
 struct TreeArgs {
-    int n, rows, nodes, depth, children;
+    int n, rows, nodes, depth, children, ahead;
     const int *row_start, *tokens, *parent, *n_nodes;
     const float *u;
     int *outcome, *list;      // [rows]: see accept_plan_kernel
@@ -869,10 +869,9 @@ __device__ __forceinline__ int nodes_of(const TreeArgs &a, int b) {
 
 struct Node {
     int b, node, n, d;        // its sequence, its index among n, drafts accepted there (more than depth: never reached)
-    int first;                // node 0's child above it, or itself
 };
 __device__ __forceinline__ Node node_of(const TreeArgs &a, int r) {
-    Node t{0, 0, 0, 0, 0};
+    Node t{0, 0, 0, 0};
     for (int hi = a.n; hi - t.b > 1;) {                 // the last sequence that starts at or before the row
         const int mid = (t.b + hi) >> 1;
         if (a.row_start[mid] <= r) t.b = mid; else hi = mid;
@@ -887,7 +886,6 @@ __device__ __forceinline__ void find_depth(const TreeArgs &a, Node &t) {
     for (int i = t.node; i > 0 && t.d <= a.depth; ++t.d) {
         const int up = parent[i];
         if (up < 0 || up >= i) { t.d = a.depth + 1; break; }
-        t.first = i;
         i = up;
     }
 }
@@ -997,8 +995,8 @@ __device__ __forceinline__ void decide(const T *__restrict__ logits, long ld, in
     if (id >= 0) a.outcome[r] = -2 - id;
 }
 
-// Which rows: each of them, a cluster each; the sequences' first ones; those that the plan lists, in turns.
-enum : int { EVERY = 0, ROOTS = 1, LISTED = 2 };
+// Which rows: each of them, a cluster each; the first `ahead` ones of each sequence; those that the plan lists, in turns.
+enum : int { EVERY = 0, AHEAD = 1, LISTED = 2 };
 
 template <typename T>
 __global__ void __launch_bounds__(ROW_THREADS, 2)
@@ -1008,16 +1006,19 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
     const int rank = blockIdx.x % ctas, count = which == LISTED ? a.list[a.rows - 1] : 0;
     for (int i = blockIdx.x / ctas;; i += gridDim.x / ctas) {               // (the whole cluster does the same)
         if (which == LISTED && i >= count) return;
-        const int r = which == EVERY ? i : which == ROOTS ? a.row_start[i] : a.list[i];
+        int r;
         Node t;
-        if (which == ROOTS) {
-            t = Node{i, 0, nodes_of(a, i), 0, 0};
-            if (t.n < 1) return;
+        if (which == AHEAD) {
+            const int b = i % a.n;
+            t = Node{b, i / a.n, nodes_of(a, b), 0};
+            if (t.node >= t.n) return;
+            r = a.row_start[b] + t.node;
         } else {
+            r = which == EVERY ? i : a.list[i];
             t = node_of(a, r);
-            if (which == EVERY) find_depth(a, t); else t.d = a.outcome[r];
-            if (t.d > a.depth) return;
         }
+        if (which == LISTED) t.d = a.outcome[r]; else find_depth(a, t);
+        if (t.d > a.depth) return;
         decide(logits, ld, V, ctas, rank, slice, f, a, r, t);
         if (which != LISTED) return;
         __syncwarp();
@@ -1027,8 +1028,8 @@ accept_rows_kernel(const T *__restrict__ logits, long ld, int V, int ctas, int s
     }
 }
 
-// The rows behind the child that each sequence's first node accepts, in list[0 ..), their number in its last element (a first node
-// is not among them), and the drafts accepted there in outcome.
+// The rows that may still be reached once the first `ahead` ones of each sequence are decided: in list[0 ..), their number in its last
+// element (a first node is not among them), and the drafts accepted there in outcome.
 __global__ void __launch_bounds__(1024)
 accept_plan_kernel(TreeArgs a) {
     __shared__ int count;
@@ -1038,9 +1039,15 @@ accept_plan_kernel(TreeArgs a) {
     allow_dependents();
     for (int r = threadIdx.x; r < a.rows; r += blockDim.x) {
         Node t = node_of(a, r);
-        if (t.d > a.depth || t.node == 0) continue;
+        if (t.d > a.depth || t.node < a.ahead) continue;
         find_depth(a, t);
-        if (t.d > a.depth || a.outcome[a.row_start[t.b]] != t.first) continue;
+        bool may = t.d <= a.depth;
+        for (int i = t.node; may && i > 0;) {
+            const int up = a.parent[(long)t.b * a.nodes + i];
+            may = up >= a.ahead || a.outcome[r - t.node + up] == i;
+            i = up;
+        }
+        if (!may) continue;
         a.outcome[r] = t.d;
         a.list[atomicAdd(&count, 1)] = r;
     }
@@ -1151,31 +1158,36 @@ msd_status msd_accept_batch(const void *logits, int64_t ld, int32_t dtype, int32
         return MSD_ERR_INVALID;
     if (batch->rows > 0 && (bad_logits(logits, ld, dtype, vocab) || !scratch)) return MSD_ERR_INVALID;
     const Settings s = settings_of(f);
-    const TreeArgs a{batch->n, batch->rows, tree_nodes, depth, children, batch->row_start, tree->tokens, tree->parent, tree->n_nodes, u,
+    const int size = dtype == MSD_F32 ? 4 : 2;
+    const Cut c = batch->rows > 0 ? cut_rows(batch->rows, vocab, size) : Cut{1, 0, 0};
+    const int ahead = std::max(1, std::min(tree_nodes, RESIDENT / c.ctas / batch->n));
+    const TreeArgs a{batch->n, batch->rows, tree_nodes, depth, children, ahead, batch->row_start, tree->tokens, tree->parent, tree->n_nodes, u,
                      scratch, scratch + batch->rows, path, accept_len, bonus};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (batch->rows > 0) {
-        const int size = dtype == MSD_F32 ? 4 : 2;
-        const Cut c = cut_rows(batch->rows, vocab, size), roots = cut_rows(batch->n, vocab, size);
-        if ((long)batch->rows * c.ctas > 0x7FFFFFFF || (long)batch->n * roots.ctas > 0x7FFFFFFF) return MSD_ERR_INVALID;
+        if ((long)batch->rows * c.ctas > 0x7FFFFFFF || (long)batch->n * c.ctas > 0x7FFFFFFF) return MSD_ERR_INVALID;
         const auto rows = [&](int which, const Cut &cut, int count) {
             return dtype == MSD_F32 ? launch_rows(accept_rows_kernel<float>, count, cut, st, static_cast<const float *>(logits), (long)ld, vocab,
                                                   cut.ctas, cut.slice, s, a, which)
                                     : launch_rows(accept_rows_kernel<bf16>, count, cut, st, static_cast<const bf16 *>(logits), (long)ld, vocab,
                                                   cut.ctas, cut.slice, s, a, which);
         };
-        // Where the rows are more than the GPU holds at a time (two CTAs an SM), those of the first nodes go ahead, and of the others
-        // only the ones behind an accepted child follow.
+        // Where the rows are more than the GPU holds at a time (two CTAs an SM), the first nodes of each tree go ahead, as many as it
+        // holds, and of the others only those that may be reached then follow. (16 trees of 60 nodes, 32000 tokens:
+        // 53 us, 117 with every row, 80 with the roots alone ahead.)
         cudaError_t e;
         if ((long)batch->rows * c.ctas <= STAGED_ABOVE || depth == 0) {
             e = rows(EVERY, c, batch->rows);
         } else {
-            e = rows(ROOTS, roots, batch->n);
+            const int first = batch->n * ahead;         // (at most n, or what the GPU holds)
+            e = rows(AHEAD, cut_rows(first, vocab, size), first);
             if (e == cudaSuccess) {
                 e = launch_chain(accept_plan_kernel, 1, 1024, 0, st, a);
                 note_launch();
             }
-            if (e == cudaSuccess) e = rows(LISTED, c, std::min(batch->rows, RESIDENT / c.ctas));
+            // (few are expected: the 16 trees with 4 CTAs a row 53 us, with 2 55)
+            const Cut few = cut_rows(std::min(batch->rows, RESIDENT / 4), vocab, size);
+            if (e == cudaSuccess) e = rows(LISTED, few, std::min(batch->rows, RESIDENT / few.ctas));
         }
         if (e != cudaSuccess) return MSD_ERR_CUDA;
     }
