@@ -7,6 +7,7 @@ there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from ctypes import POINTER, c_char_p, c_float, c_int32, c_int64, c_void_p
@@ -738,9 +739,8 @@ def accept(logits: torch.Tensor, batch: Batch, tree: Tree, u: torch.Tensor, sett
     for t in (batch.seqs, tree.tokens):
         if t.device != dev:
             raise ValueError("batch, tree and logits are on one GPU")
-    scratch = torch.empty(2 * rows, dtype=torch.int32, device=dev)
-    if stream is not None:
-        scratch.record_stream(stream)
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):         # memory that this stream may write now
+        scratch = torch.empty(2 * rows, dtype=torch.int32, device=dev)
     st = lib().msd_accept_batch(
         logits.data_ptr(), ld, _TYPES[logits.dtype], logits.shape[1], batch.c(), ctypes.byref(tree.c()), tree.N,
         None if settings is None else settings._for(n, dev), _vector(u, "u", torch.float32, u.numel(), dev),

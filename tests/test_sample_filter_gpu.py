@@ -313,6 +313,31 @@ def test_accept_in_a_graph_and_on_a_stream():
     assert all(torch.equal(a, c) for a, c in zip(out, want[1]))
 
 
+def test_accept_beside_another_stream():
+    """What the current stream still writes into memory that it has given back does not meet a call on another stream."""
+    counts = [60] * 12
+    x = logits(720, 2000, 5, peaks=6)
+    toks, pars = trees(counts, 60, 2000, x, 5)
+    u = torch.rand(12, 7, 5, generator=gen(5), device="cuda") * 0.7
+    want = [t.clone() for t in check_accept(x, counts, toks, pars, u, 60)]
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    b = msd.Batch(torch.arange(12, dtype=torch.int32, device="cuda"), i32([60 * i for i in range(13)]), 720)
+    tree = msd.Tree(12, 60)
+    tree.tokens.copy_(i32(toks).flatten())
+    tree.parent.copy_(i32(pars).flatten())
+    out = [torch.zeros_like(t) for t in want]
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        used = torch.empty(2 * 720, dtype=torch.int32, device="cuda")
+        for _ in range(200):
+            used.fill_(-12345)
+        del used
+        msd.accept(x, b, tree, u, None, *out, stream=s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want))
+
+
 def test_refusals():
     x, u, t = logits(4, 100), uniforms(4), torch.zeros(4, dtype=torch.int32, device="cuda")
     f3 = msd.Filter(temperature=torch.ones(3, device="cuda"))
