@@ -13,7 +13,12 @@
 // in the exponent; counts for top-k, exact masses in three 32-bit pieces for top-p), a look at the
 // one bucket that the bound falls into, and the comparison of its few tokens with one another. A
 // bucket with too many tokens is split again by the logits' bits, down to equal logits, where ids
-// decide; so nothing depends on how logits are spread. Sums of blocks of 128 or 256 ids then lead to the token.
+// decide; so nothing depends on how logits are spread. Where few tokens come before the bucket's end, all are gathered in one
+// CTA, and the rest is done on that list; else sums of blocks of 128 ids lead to the token.
+//
+// What bounds it: for one row its phases in turn, 4 of them meetings of the cluster (a row of 32000 fp32 logits, top-k 50, top-p
+// 0.9: 12.8 us); for many, issue slots, 60 to 70 instructions a token for each pass with exact weights, two of them for top-p of
+// a row that leaves many tokens (64 rows of 100003 bf16 logits, top-p 0.95: 60 us, 61% of slots), 35 for a pass that counts.
 #include <algorithm>
 
 #include "msd.h"
@@ -995,6 +1000,8 @@ __device__ __forceinline__ void decide(const T *__restrict__ logits, long ld, in
     if (id >= 0) a.outcome[r] = -2 - id;
 }
 
+// A tree of 60 nodes, 32000 fp32 logits each, takes 27 us in one wave (and 5 the walk); 16 of them as staged below 53 us.
+//
 // Which rows: each of them, a cluster each; the first `ahead` ones of each sequence; those that the plan lists, in turns.
 enum : int { EVERY = 0, AHEAD = 1, LISTED = 2 };
 
