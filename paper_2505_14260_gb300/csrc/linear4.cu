@@ -15,7 +15,8 @@ namespace msd {
 // three shifts, four selections (code | 0x4300 is the bf16 128 + code) and four subtractions of
 // 128 + zero (exact), 11 for 8 codes of a lane; the products' order within a word is free, so
 // pairs are (0, 4), (1, 5), (2, 6), (3, 7) of it and x is permuted alike. Each mma takes codes of
-// one group, and a group's sum is scaled on the way into the total, so no weight is rounded.
+// one group, and a group's sum is scaled on the way into the total, so no weight is rounded. (A tensor core cuts a sum's last
+// bits at each product added: fp32's later planes have sums of their own, which cost nothing and made 4.6e-7 of 1.1e-7 at groups of 128.)
 //
 // A warp has 32 outputs and every 8th run of groups; the 8 warps' totals meet in shared memory in
 // a fixed order. Weights go from memory to registers, DEPTH chunks of 128 elements ahead; x is
@@ -123,7 +124,7 @@ linear4_few_kernel(const T *__restrict__ x, long ldx, int m, Weight w, float *__
         for (int e = 0; e < PER; ++e) {
             const int group = c * PER + e;
             if (PER > 1 && group >= w.groups) break;
-            float acc[2][NT][4] = {};
+            float acc[P > 1 ? 2 : 1][2][NT][4] = {};                                // fp32: the first planes, the later ones
             __nv_bfloat162 off[4];
             float sc[4];
 #pragma unroll
@@ -155,8 +156,8 @@ linear4_few_kernel(const T *__restrict__ x, long ldx, int m, Weight w, float *__
                     for (int p = 0; p < P; ++p)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            mma_16816(acc[h][n], a[2 * h][0], a[2 * h + 1][0], a[2 * h][1], a[2 * h + 1][1], b[p][0], b[p][1]);
-                            mma_16816(acc[h][n], a[2 * h][2], a[2 * h + 1][2], a[2 * h][3], a[2 * h + 1][3], b[p][2], b[p][3]);
+                            mma_16816(acc[p > 0][h][n], a[2 * h][0], a[2 * h + 1][0], a[2 * h][1], a[2 * h + 1][1], b[p][0], b[p][1]);
+                            mma_16816(acc[p > 0][h][n], a[2 * h][2], a[2 * h + 1][2], a[2 * h][3], a[2 * h + 1][3], b[p][2], b[p][3]);
                         }
                 }
             }
@@ -165,7 +166,10 @@ linear4_few_kernel(const T *__restrict__ x, long ldx, int m, Weight w, float *__
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) total[h][n][i] = fmaf(sc[2 * h + (i >> 1)], acc[h][n][i], total[h][n][i]);
+                    for (int i = 0; i < 4; ++i) {
+                        const float sum = P > 1 ? acc[0][h][n][i] + acc[P > 1][h][n][i] : acc[0][h][n][i];
+                        total[h][n][i] = fmaf(sc[2 * h + (i >> 1)], sum, total[h][n][i]);
+                    }
         }
     };
     for (int c = c0; c < c1; c += FEW_DEPTH) {
@@ -203,8 +207,9 @@ using FewKernel = void (*)(const T *, long, int, Weight, float *, long, int, int
 
 template <typename T, int GROUP>
 static FewKernel<T> few_kernel(bool two, bool wide) {
-    return two ? wide ? linear4_few_kernel<T, GROUP, 2, true> : linear4_few_kernel<T, GROUP, 2, false>
-               : wide ? linear4_few_kernel<T, GROUP, 1, true> : linear4_few_kernel<T, GROUP, 1, false>;
+    if constexpr (sizeof(T) == 2)               // (fp32: 3 rows at most)
+        if (two) return wide ? linear4_few_kernel<T, GROUP, 2, true> : linear4_few_kernel<T, GROUP, 2, false>;
+    return wide ? linear4_few_kernel<T, GROUP, 1, true> : linear4_few_kernel<T, GROUP, 1, false>;
 }
 
 template <typename T>
@@ -290,7 +295,8 @@ __device__ __forceinline__ void store8(bf16 *p, const float (&v)[8]) {
 }
 
 // Codes of a matrix: 8 consecutive elements a lane, 4, 8 or 16 lanes a group, so a warp has runs of 256 elements of a
-// row and reads, and writes codes and values, in whole lines. Each value is read once; what bounds it is memory.
+// row and reads, and writes codes and values, in whole lines. Each value is read once; what bounds it is memory: 32000 x 5120 fp32 with
+// zeros and values take 205 us, 6.9 TB/s; 4096 x 4096 bf16 15.7 us, of them 13 the kernel's (issue slots 75% busy).
 constexpr int Q_THREADS = 256, Q_RUN = 256;
 template <typename T, int GROUP, bool ZEROS>
 __global__ void __launch_bounds__(Q_THREADS)

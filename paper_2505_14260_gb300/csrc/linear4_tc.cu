@@ -375,20 +375,26 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
                 ok = ok && use_wait(d_empty + d_bar, li + HS, HS, &s_abort);
                 if (!ok) break;
                 fence_after();
+                // (fp32's later planes first: a tensor core cuts a sum's last bits at each product added, and they are smaller. At groups
+                // of 128 that makes errors 8e-8 of 4.4e-7, in 4% more time; at 32 they are 1.5e-7 plane after plane)
+                constexpr bool LATER_FIRST = P > 1 && GROUP > 32;
 #pragma unroll
-                for (int kk = 0; kk < GROUP / 16; ++kk) {
-                    const int k16 = e * (GROUP / 16) + kk;
-                    const uint32_t bar = 8 * (g * 2 + (k16 >> 2));
-                    if (k16 % 4 == 0) {
-                        ok = ok && use_wait(a_full + bar, ci, CYCLE, &s_abort);
-                        if (!ok) break;
-                        fence_after();
+                for (int part = LATER_FIRST ? 0 : 1; part < 2 && ok; ++part) {
+#pragma unroll
+                    for (int kk = 0; kk < GROUP / 16; ++kk) {
+                        const int k16 = e * (GROUP / 16) + kk;
+                        const uint32_t bar = 8 * (g * 2 + (k16 >> 2));
+                        if ((!LATER_FIRST || part == 0) && k16 % 4 == 0) {
+                            ok = ok && use_wait(a_full + bar, ci, CYCLE, &s_abort);
+                            if (!ok) break;
+                            fence_after();
+                        }
+#pragma unroll
+                        for (int p = LATER_FIRST && part == 1 ? 0 : P - 1; p >= (part == 0 ? 1 : 0); --p)
+                            w_mma_ts(on, t_d, t_a + k16 * 8, d_x + ((p * L::XPLANE + (k16 >> 2) * L::XBOX + (k16 & 3) * 32) >> 4), id,
+                                     kk > 0 || p < (LATER_FIRST && part == 1 ? P : P - 1));
+                        if (part == 1 && k16 % 4 == 3) w_commit(on, a_empty + bar);
                     }
-#pragma unroll
-                    for (int p = 0; p < P; ++p)
-                        w_mma_ts(on, t_d, t_a + k16 * 8,
-                                 d_x + ((p * L::XPLANE + (k16 >> 2) * L::XBOX + (k16 & 3) * 32) >> 4), id, kk > 0 || p > 0);
-                    if (k16 % 4 == 3) w_commit(on, a_empty + bar);
                 }
                 if (!ok) break;
                 w_commit(on, d_full + d_bar);
