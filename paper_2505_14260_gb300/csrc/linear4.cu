@@ -207,7 +207,7 @@ using FewKernel = void (*)(const T *, long, int, Weight, float *, long, int, int
 
 template <typename T, int GROUP>
 static FewKernel<T> few_kernel(bool two, bool wide) {
-    if constexpr (sizeof(T) == 2)               // (fp32: 3 rows at most)
+    if constexpr (sizeof(T) == 2)               // (fp32: 8 rows at most)
         if (two) return wide ? linear4_few_kernel<T, GROUP, 2, true> : linear4_few_kernel<T, GROUP, 2, false>;
     return wide ? linear4_few_kernel<T, GROUP, 1, true> : linear4_few_kernel<T, GROUP, 1, false>;
 }
@@ -228,6 +228,20 @@ static cudaError_t launch_few(const T *x, long ldx, int m, const Weight &w, floa
         note_launch();
     }
     return e;
+}
+
+// Whether these kernels take less time than the ones on tcgen05: a CTA of 32 outputs takes 2.5 us and a time for each element of a row
+// (1, 8 and 16 rows, k 1024 to 11008, groups of 32, 64 and 128), and 152 of them run at a time; two on an SM, as those of up to 8 bf16
+// rows do, take about as long as one after the other. (One row, groups of 128: k and o 4096 6.3 us here, 9.7 there; k 11008 12.3 and
+// 15.2; o 32000 25.5 and 25.0. Groups of 32: k 1024 4.5 and 7.6, o 11008 31 and 19. 16 rows, o 11008, groups of 128: 21 and 13.5.)
+template <typename T>
+static bool few_rows(int m, const Weight &w) {
+    constexpr bool f32 = sizeof(T) == 4;
+    if (m > (f32 ? 8 : 16)) return false;
+    constexpr float us[3][3] = {{2.4e-3f, 1.3e-3f, 0.9e-3f}, {2.6e-3f, 1.6e-3f, 1.2e-3f}, {2.8e-3f, 1.7e-3f, 1.5e-3f}};
+    const float each = us[f32 ? 2 : m > 8][w.group == 32 ? 0 : w.group == 64 ? 1 : 2];
+    const float waves = !f32 && m <= 8 ? std::max(1.f, 1.1f / (FEW_OUT * 152) * w.o) : (float)((w.o + FEW_OUT * 152 - 1) / (FEW_OUT * 152));
+    return 2.5f + each * w.k * waves < linear4_tc_us<T>(w);
 }
 
 // The bf16 nearest to span / n (ties to even), span = hi + lo exactly, n = 7 or 15, span >= 0. The fp32 product may sit on the
@@ -406,13 +420,10 @@ msd_status msd_linear4(const void *x, int64_t ldx, int32_t x_dtype, int32_t m, c
     if (m == 0) return MSD_OK;
     if (bad_rows(x, ldx, x_dtype, w.k) || !y || ldy < w.o || reinterpret_cast<uintptr_t>(y) % 4) return MSD_ERR_INVALID;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    // Which of the two: measured with 1 to 16 rows, k and o of 4096 and 11008. The warps of a few rows win up to 8 rows (fp32: 3, a
-    // tile of B operands) while their CTAs of 32 outputs fit the GPU at once (o 4096, k 11008, groups of 128: 12.0 us, 14.6 on
-    // tcgen05; 16 rows, k 4096: 7.6 and 9.9), and with one scale for 128 codes of bf16 rows (o 11008: 11.7 and 12.5; with 64 codes 19.2 and 14.0).
-    const bool f32 = x_dtype == MSD_F32, small = w.o <= 32 * 152;
-    const bool few = m <= (f32 ? 3 : 8) ? small || (!f32 && w.group == 128) : !f32 && m <= 16 && (long)w.o * w.k <= 20l << 20;
     const auto run = [&](auto *p) {
-        return few ? launch_few(p, (long)ldx, m, w, y, (long)ldy, accumulate, s) : launch_linear4_tc(p, (long)ldx, m, w, y, (long)ldy, accumulate, s);
+        using T = std::remove_const_t<std::remove_pointer_t<decltype(p)>>;
+        return few_rows<T>(m, w) ? launch_few(p, (long)ldx, m, w, y, (long)ldy, accumulate, s)
+                                 : launch_linear4_tc(p, (long)ldx, m, w, y, (long)ldy, accumulate, s);
     };
     const cudaError_t e = x_dtype == MSD_F32 ? run(static_cast<const float *>(x)) : run(static_cast<const bf16 *>(x));
     return e == cudaSuccess ? MSD_OK : MSD_ERR_CUDA;

@@ -64,4 +64,7 @@ template <> struct Octet<float> {
 template <typename T>
 cudaError_t launch_linear4_tc(const T *x, long ldx, int m, const Weight &w, float *y, long ldy, int accumulate, cudaStream_t s);
 
+// About how long up to 16 rows take there.
+template <typename T> float linear4_tc_us(const Weight &w);
+
 }  // namespace msd

@@ -531,26 +531,30 @@ bool make_map(CUtensorMap *map, CUtensorMapDataType type, int size, const void *
                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Into how many parts K is cut, and what a call costs then (in chunks of 256 outputs, 0.74 us). A part is a CTA that has an SM to itself, so
-// what counts is how many clusters of that size fit the GPU at once (GPCs have 16 to 20 SMs: 152, 76, 46, 36, 28, 23, 15 and 15 were
-// counted), a chunk's time and what a CTA does beside its chunks: about 6 chunks' time to start and to end, 3 more to join.
+// Into how many parts K is cut, and about how long a call takes then. A part is a CTA that has an SM to itself, so what counts is how
+// many clusters of that size fit the GPU at once (GPCs have 16 to 20 SMs: 152, 76, 46, 36, 28, 23, 15 and 15 were counted), a
+// chunk's time, and what a CTA does beside its chunks: 3.8 us to start and to end, 1.9 more to join.
 struct Cut {
     int split;
-    float cost;
+    float us;
 };
-Cut best_cut(long tiles, int chunks, float chunk) {
+Cut best_cut(long tiles, int chunks, float chunk_us) {
     constexpr int fit[8] = {152, 76, 46, 36, 28, 23, 15, 15};
     Cut best{1, 0.f};
     for (int s = 1; s <= 8 && s <= chunks; ++s) {
-        const float cost = (tiles + fit[s - 1] - 1) / fit[s - 1] * (chunk * ((chunks + s - 1) / s) + 6 + (s > 1 ? 3 : 0));
-        if (s == 1 || cost < best.cost) best = {s, cost};
+        const float us = (tiles + fit[s - 1] - 1) / fit[s - 1] * (chunk_us * ((chunks + s - 1) / s) + (s > 1 ? 5.7f : 3.8f));
+        if (s == 1 || us < best.us) best = {s, us};
     }
     return best;
 }
+// (a chunk's time: measured with 1, 16, 32, 60 and 128 rows, groups of 32, 64 and 128)
 template <typename T, int GROUP, int N>
-Cut cut_of(const Args &a) {
+Cut cut_of(int m, const Weight &w) {
     using L = Lay<T, GROUP, N>;
-    return best_cut((long)((a.w.o + L::OUT - 1) / L::OUT) * ((a.m + N - 1) / N), (a.w.k + CHUNK - 1) / CHUNK, L::WIDE ? 0.68f : 1.f);
+    constexpr float us[5][3] = {{1.25f, 0.98f, 0.82f}, {2.0f, 1.57f, 1.35f},                            // fp32: 16 and 32 rows
+                                {1.15f, 0.75f, 0.65f}, {2.1f, 1.25f, 0.85f}, {1.76f, 1.03f, 0.57f}};    // bf16: up to 32, 64, 128
+    constexpr int row = L::SPLIT ? (N > 16 ? 1 : 0) : L::WIDE ? 4 : N > 32 ? 3 : 2;
+    return best_cut((long)((w.o + L::OUT - 1) / L::OUT) * ((m + N - 1) / N), (w.k + CHUNK - 1) / CHUNK, us[row][GROUP == 32 ? 0 : GROUP == 64 ? 1 : 2]);
 }
 
 template <typename T, int GROUP, int N>
@@ -564,7 +568,7 @@ cudaError_t launch(Args a, cudaStream_t s) {
         (!L::SPLIT && !make_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.x, a.w.k, a.m, a.ldx, 64, N, CU_TENSOR_MAP_SWIZZLE_128B)))
         return cudaErrorUnknown;
     const int chunks = (a.w.k + CHUNK - 1) / CHUNK, tiles = (a.w.o + L::OUT - 1) / L::OUT, cols = (a.m + N - 1) / N;
-    a.split = cut_of<T, GROUP, N>(a).split;
+    a.split = cut_of<T, GROUP, N>(a.m, a.w).split;
     const int slice = (chunks + a.split - 1) / a.split * L::PER;
     const size_t beside = (size_t)slice * ((L::OUT + 2) * 2 + (a.w.zeros ? L::OUT + 4 : 0));
     a.staged = beside <= L::ROOM;
@@ -594,10 +598,10 @@ template <typename T, int GROUP>
 cudaError_t launch_n(const Args &a, cudaStream_t s) {
     if (a.m <= 16) return launch<T, GROUP, 16>(a, s);
     if constexpr (sizeof(T) == 2) {             // (planes of 64 rows would leave room for one stage)
-        // 128 rows of x with 128 outputs, or 64 with 256: as many CTAs, and a chunk in 0.50 us instead of 0.74. (645 rows, k 4096,
-        // 11008 outputs: 83 us instead of 112.) Rows just past a multiple of 128 can leave the first with more waves:
+        // 128 rows of x with 128 outputs, or 64 with 256: as many CTAs, and chunks that take less. (645 rows, k 4096, 11008
+        // outputs: 82 us instead of 112.) Rows just past a multiple of 128 can leave the first with more waves:
         // 130 rows of the same 41 us instead of 30.
-        if (a.m > 64 && cut_of<T, GROUP, 128>(a).cost < cut_of<T, GROUP, 64>(a).cost) return launch<T, GROUP, 128>(a, s);
+        if (a.m > 64 && cut_of<T, GROUP, 128>(a.m, a.w).us < cut_of<T, GROUP, 64>(a.m, a.w).us) return launch<T, GROUP, 128>(a, s);
         if (a.m > 32) return launch<T, GROUP, 64>(a, s);
     }
     return launch<T, GROUP, 32>(a, s);
@@ -611,6 +615,13 @@ cudaError_t launch_linear4_tc(const T *x, long ldx, int m, const Weight &w, floa
     return w.group == 128 ? launch_n<T, 128>(a, s) : w.group == 64 ? launch_n<T, 64>(a, s) : launch_n<T, 32>(a, s);
 }
 
+template <typename T>
+float linear4_tc_us(const Weight &w) {
+    return (w.group == 128 ? cut_of<T, 128, 16>(1, w) : w.group == 64 ? cut_of<T, 64, 16>(1, w) : cut_of<T, 32, 16>(1, w)).us;
+}
+
+template float linear4_tc_us<float>(const Weight &);
+template float linear4_tc_us<bf16>(const Weight &);
 template cudaError_t launch_linear4_tc<float>(const float *, long, int, const Weight &, float *, long, int, cudaStream_t);
 template cudaError_t launch_linear4_tc<bf16>(const bf16 *, long, int, const Weight &, float *, long, int, cudaStream_t);
 

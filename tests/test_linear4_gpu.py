@@ -97,6 +97,15 @@ def test_many_rows(m):
     run(m, 1000, 130, 32, False, torch.float32)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("m", [1, 3, 8, 12, 16, 30])
+def test_few_rows_of_long_ones(m, group, dtype):
+    """Few rows on either side of the choice between the kernels; codes that tensor copies take and ones they do not."""
+    for k, o, zeros in ((11000, 150, True), (9984, 300, False), (11008, 40, True), (2048, 9000, True), (1000, 20000, False)):
+        run(m, k, o, group, zeros, dtype, seed=m + k)
+
+
 @pytest.mark.parametrize("m,o", [(129, 11008), (150, 12700), (192, 10000), (130, 19456), (256, 9856)])
 def test_rows_past_a_block(m, o):
     """Where rows past a multiple of 128 make the fewest CTAs blocks of 64 rows, and beside it."""
