@@ -219,10 +219,12 @@ static cudaError_t launch_few(const T *x, long ldx, int m, const Weight &w, floa
     const int step = m > 8 ? 16 : 8;            // m <= 16
     const FewKernel<T> f = w.group == 128 ? few_kernel<T, 128>(m > 8, wide) : w.group == 64 ? few_kernel<T, 64>(m > 8, wide) : few_kernel<T, 32>(m > 8, wide);
     const size_t sums = (size_t)FEW_WARPS * FEW_OUT * step * 4, beside = (size_t)FEW_OUT * w.groups * 3;
-    const bool staged = beside <= 64 * 1024;    // longer rows read them where they are
+    constexpr size_t BESIDE = 64 * 1024;        // longer rows read them where they are
+    const bool staged = beside <= BESIDE;
     const size_t smem = sums + (staged ? beside : 0);
     cudaError_t e = cudaSuccess;
-    if (smem > 48 * 1024) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    // (one value, whatever the call: another thread may be between this and its launch)
+    if (smem > 48 * 1024) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sums + BESIDE));
     if (e == cudaSuccess) {
         e = launch_chain(f, (w.o + FEW_OUT - 1) / FEW_OUT, FEW_WARPS * 32, smem, s, x, ldx, m, w, y, ldy, accumulate, (int)staged);
         note_launch();
