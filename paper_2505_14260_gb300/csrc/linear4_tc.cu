@@ -7,23 +7,24 @@
 // fp32 totals, so no weight is rounded.
 //
 // A CTA (one an SM: it holds all of the tensor memory) has 256 outputs, two halves of 128, and up to 64 rows of x, or 128
-// outputs and 128 rows; K is cut between the CTAs of a cluster where there are fewer tiles than SMs, and their totals meet through
-// distributed shared memory in rank order. Chunks are 128 elements of K. Roles:
-//   warps 0-3    MMAs, of the even or the odd chunks of a half (first, since a scheduler prefers them: as the last warps, an
+// outputs and up to 128 rows; K is cut between the CTAs of a cluster where there are fewer tiles than SMs, and their totals meet
+// through distributed shared memory in rank order. Chunks are 128 elements of K. Roles:
+//   warps 0-3    MMAs, of the even or the odd chunks (of a half; first, since a scheduler prefers them: as the last warps, an
 //                MMA's issue took them 100 cycles)
 //   warps 4-7    x: copies of bf16, put into order where need be; fp32 as three bf16 planes that add up to it, swizzled as the MMA
 //                reads them
-//   warps 8-15   a row of W a thread: a group's sum from tensor memory, scaled, into fp32 totals
-//   warps 16-31  a row of W a thread: codes -> tensor memory; four warps for the even chunks of a half, four for the odd ones;
-//                the first of those also issue the copies of codes, four chunks ahead
+//   warps 8-15   a row of W a thread: a group's sum from tensor memory, scaled, into fp32 totals (of half the rows of x, with 128
+//                outputs)
+//   warps 16-31  a row of W a thread: codes -> tensor memory; four warps for the even chunks of a half and four for the odd ones, or
+//                four for every fourth chunk; the first of the four also issue the copies of codes, four chunks ahead
 // What bounds it is the integer pipe, half a warp a cycle, and the issue slots behind it. For 8 codes, in the order of a word's
 // shifts ((0, 4), (1, 5), (2, 6), (3, 7), x ordered alike), it takes 3 shifts, 4 selections and 4 subtractions: about 1000 cycles
 // for a chunk of 256 outputs with scales, copies and waits, against 512 of the MMAs of 64 rows and 330 of a copy at the rate of
 // memory. With 128 rows to a CTA a chunk of 128 outputs takes 950 cycles, of them 512 of MMAs: there x stays as copied (ordering
 // 128 rows took the four copying warps longer than that) and codes come out in their own order, for 2 more operations of 8 codes.
-// To start and to end a CTA takes about 5 us. One group of warps a half doing everything in turn took 1800 cycles a chunk.
-// Measured, us (groups of 128, other weights for each call): k 4096, o 11008: 16 rows 13.5, 60 rows 16.4, 128 rows 22, 645 rows
-// 84 (690 TFLOP/s); k 11008, o 4096, 60 rows: 19.3. A wait that runs out (2 s) leaves NaN in the CTA's part of y.
+// To start and to end a CTA takes about 4 us, to join 2 to 3.5. One group of warps a half doing everything in turn took 1800 cycles
+// a chunk. Measured, us (groups of 128, other weights for each call): k 4096, o 11008: 16 rows 13.5, 60 rows 16.4, 128 rows 22, 645
+// rows 83 (700 TFLOP/s); k 11008, o 4096, 60 rows 18.2. A wait that runs out (2 s) leaves NaN in the CTA's part of y.
 #include <algorithm>
 #include <cstring>
 #include <type_traits>
@@ -43,14 +44,15 @@ constexpr int CODE_WARPS = 16, SUM_WARPS = 8, THREADS = 1024;
 constexpr int AHEAD = 4;                                        // chunks (a multiple of a cycle, and less than a ring has stages)
 constexpr int COPY_0 = 4, SUM_0 = 8, CODE_0 = SUM_0 + SUM_WARPS;                   // first warps of the roles
 
-template <typename T, int GROUP, int N>
+template <typename T, int GROUP, int N, int OUTPUTS>
 struct Lay {
     static constexpr bool SPLIT = sizeof(T) == 4;               // x in planes
-    // WIDE: 128 outputs and 128 rows of x; the four groups of code warps take every fourth chunk, the two of sum warps half of the rows of x
-    static constexpr bool WIDE = N > 64;
-    static constexpr int OUT = WIDE ? TILE : 2 * TILE, CYCLE = WIDE ? 4 : 2, TOK = WIDE ? N / 2 : N;
+    // 256 outputs, two halves; or HALF of that: the four groups of code warps take every fourth chunk, the two of sum warps half of the
+    // rows of x
+    static constexpr bool HALF = OUTPUTS == TILE;
+    static constexpr int OUT = OUTPUTS, CYCLE = HALF ? 4 : 2, TOK = HALF ? N / 2 : N;
     static constexpr uint32_t WSTAGE = OUT / TILE * WBOX;
-    static constexpr bool IN_ORDER = WIDE;                      // x as copied; else in the order of a word's shifts
+    static constexpr bool IN_ORDER = N > 64;                     // x as copied; else in the order of a word's shifts
     static constexpr int P = Octet<T>::PLANES, PER = CHUNK / GROUP;
     // registers by role: over the eight groups of four warps they are the launch's 64 a thread
     static constexpr int R_CODE = 56, R_SUM = SPLIT ? 96 : 104, R_ISSUE = 40, R_COPY = SPLIT ? 56 : 40;
@@ -58,8 +60,8 @@ struct Lay {
     static constexpr uint32_t XBOX = N * 128, XPLANE = 2 * XBOX, XSTAGE = P * XPLANE;
     static constexpr int XS = SPLIT && N > 16 ? 2 : 4;          // even: a stage's chunks are all even or all odd ones
     static constexpr int X_PARTS = SPLIT ? 4 / XS : 1;          // warps that fill a stage of x
-    static constexpr int WS = WIDE ? 8 : 6;
-    static constexpr int DS = WIDE ? 2 : 128 / N, HS = DS / 2;  // accumulators of a half (WIDE: in all), of its even or odd chunks
+    static constexpr int WS = HALF ? 8 : 6;
+    static constexpr int DS = (HALF ? 256 : 128) / N, HS = DS / 2;          // accumulators (of a half), of even or odd chunks
     static constexpr uint32_t X = 0, W = XS * XSTAGE, SCALES = W + WS * WSTAGE;
     static constexpr uint32_t ROOM = SMEM_MOST - 1024 - SCALES; // for scales and zeros
     static constexpr uint32_t T_A = 0, T_D = 128, T_HALF = 256; // columns of a half
@@ -128,12 +130,12 @@ __device__ __forceinline__ bool use_wait(uint32_t bar, int use, int lap, volatil
     return __all_sync(0xffffffffu, bar_try(bar, parity)) || use_wait_slow(bar, parity, abort);
 }
 
-template <typename T, int GROUP, int N>
+template <typename T, int GROUP, int N, int OUTPUTS>
 __global__ void __launch_bounds__(THREADS, 1)
 linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap x_map, const Args a) {
-    using L = Lay<T, GROUP, N>;
+    using L = Lay<T, GROUP, N, OUTPUTS>;
     constexpr int PER = L::PER, P = L::P, XS = L::XS, WS = L::WS, DS = L::DS, HS = L::HS, OUT = L::OUT, CYCLE = L::CYCLE;
-    constexpr bool WIDE = L::WIDE;
+    constexpr bool HALF = L::HALF;
     constexpr uint32_t WSTAGE = L::WSTAGE;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * WS + 3 * XS + 16 + 4 * DS];
@@ -151,11 +153,11 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     if (tid == 0) {
         for (int i = 0; i < WS; ++i) {
             bar_init(w_full + 8 * i, 1);
-            bar_init(w_empty + 8 * i, WIDE ? 4 : 8);
+            bar_init(w_empty + 8 * i, HALF ? 4 : 8);
         }
         for (int i = 0; i < XS; ++i) {
             bar_init(x_full + 8 * i, L::X_PARTS);
-            bar_init(x_empty + 8 * i, WIDE ? 1 : 2);
+            bar_init(x_empty + 8 * i, HALF ? 1 : 2);
             bar_init(x_raw + 8 * i, 1);
         }
         for (int i = 0; i < 8; ++i) {
@@ -164,7 +166,7 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         }
         for (int i = 0; i < 2 * DS; ++i) {
             bar_init(d_full + 8 * i, 1);
-            bar_init(d_empty + 8 * i, WIDE ? 8 : 4);
+            bar_init(d_empty + 8 * i, HALF ? 8 : 4);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_abort = 0;
@@ -210,7 +212,7 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     if (warp >= CODE_0) {
         // ---- codes to tensor memory ---------------------------------------------------------------
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::R_CODE));
-        const int g = (warp - CODE_0) >> 2, half = WIDE ? 0 : g >> 1, slot = g % CYCLE, row = (warp & 3) * 32 + lane, out = half * TILE + row;
+        const int g = (warp - CODE_0) >> 2, half = HALF ? 0 : g >> 1, slot = g % CYCLE, row = (warp & 3) * 32 + lane, out = half * TILE + row;
         const uint32_t t_a = tmem + ((uint32_t)(warp & 3) << 21) + (g >> 1) * L::T_HALF + L::T_A + (g & 1) * 64;
         const uint32_t code_row = base + L::W + half * WBOX + row * 64, swz = (uint32_t)(row >> 1 & 3) << 4;
         const uint8_t *const z_at = a.staged ? s_zeros + out : a.w.zeros + (long)(j0 + min(out, outs - 1)) * a.w.groups + g0;
@@ -224,7 +226,7 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             const uint32_t to = base + L::W + ws * WSTAGE, bar = w_full + 8 * ws;
             w_expect_tx(on, bar, WSTAGE);
             w_tma2d(on, to, &map, (c0 + ci) * (CHUNK / 2), j0, bar);
-            if constexpr (!WIDE) w_tma2d(on, to + WBOX, &map, (c0 + ci) * (CHUNK / 2), j0 + TILE, bar);
+            if constexpr (!HALF) w_tma2d(on, to + WBOX, &map, (c0 + ci) * (CHUNK / 2), j0 + TILE, bar);
             copied = ci + CYCLE;
         };
         if (copies)
@@ -302,14 +304,14 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     } else if (warp >= SUM_0) {
         // ---- sums to totals -------------------------------------------------------------------------
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::R_SUM));
-        const int half = (warp - SUM_0) >> 2, out = (tid - SUM_0 * 32) % OUT, tok0 = WIDE ? half * L::TOK : 0;
+        const int half = (warp - SUM_0) >> 2, out = (tid - SUM_0 * 32) % OUT, tok0 = HALF ? half * L::TOK : 0;
         if (a.staged) {
             stage(s_scales, a.w.scales, SPITCH, tid - SUM_0 * 32, SUM_WARPS * 32);
             asm volatile("bar.sync 2, 256;" ::: "memory");
         }
         const bf16 *const s_at = a.staged ? s_scales + out : a.w.scales + (long)(j0 + min(out, outs - 1)) * a.w.groups + g0;
         const int s_step = a.staged ? SPITCH : 1;
-        const uint32_t t_d = tmem + ((uint32_t)(warp & 3) << 21) + L::T_D + (WIDE ? 0 : half * L::T_HALF);
+        const uint32_t t_d = tmem + ((uint32_t)(warp & 3) << 21) + L::T_D + (HALF ? 0 : half * L::T_HALF);
         constexpr int TOK = L::TOK;
         float total[TOK];
 #pragma unroll
@@ -318,15 +320,15 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         for (int gi = 0; gi < nc * PER; ++gi) {
             const int ci = gi / PER, li = (ci >> 1) * PER + gi % PER, ds = (ci & 1) * HS + li % HS;
             const float s = gi < gs && out < outs ? __bfloat162float(s_at[(long)gi * s_step]) : 0.f;
-            const uint32_t bar = 8 * (WIDE ? ds : half * DS + ds), from = t_d + (WIDE ? ds * L::T_HALF + tok0 : ds * N);
+            const uint32_t bar = 8 * (HALF ? ds : half * DS + ds), from = t_d + (HALF ? ds / HS * L::T_HALF + ds % HS * N + tok0 : ds * N);
             ok = use_wait(d_full + bar, li, HS, &s_abort);
             if (!ok) break;
             fence_after();
-            constexpr int STEP = 16;
+            constexpr int STEP = TOK < 16 ? TOK : 16;
 #pragma unroll
             for (int i0 = 0; i0 < TOK; i0 += STEP) {
                 uint32_t d[STEP];
-                tmem_ld16(from + i0, d);
+                if constexpr (STEP == 16) tmem_ld16(from + i0, d); else tmem_ld8(from + i0, d);
                 if (i0 + STEP == TOK) {
                     fence_before();
                     __syncwarp();
@@ -357,12 +359,12 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         // ---- MMAs ---------------------------------------------------------------------------------
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::R_ISSUE));
         const uint32_t on = elect_one();                        // (whole warps: addresses stay in uniform registers)
-        // (WIDE: warps 0 and 1, of the even and the odd chunks)
-        const int half = WIDE ? 0 : warp >> 1, slot = warp & 1;
+        // (HALF: warps 0 and 1, of the even and the odd chunks)
+        const int half = HALF ? 0 : warp >> 1, slot = warp & 1;
         const uint32_t id = idesc(TILE, N, 0);
-        bool ok = !WIDE || warp < 2;
+        bool ok = !HALF || warp < 2;
         for (int ci = slot; ci < nc && ok; ci += 2) {
-            const int g = WIDE ? ci & 3 : half * 2 + slot;
+            const int g = HALF ? ci & 3 : half * 2 + slot;
             const uint32_t t_a = tmem + (g >> 1) * L::T_HALF + L::T_A + (g & 1) * 64;
             const int xs = ci % XS;
             ok = use_wait(x_full + 8 * xs, ci, XS, &s_abort);
@@ -370,8 +372,8 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
 #pragma unroll
             for (int e = 0; e < PER; ++e) {
                 const int li = (ci >> 1) * PER + e, ds = slot * HS + li % HS;      // (no accumulator is shared by two warps' waits)
-                const uint32_t d_bar = 8 * (WIDE ? ds : half * DS + ds);
-                const uint32_t t_d = tmem + L::T_D + (WIDE ? ds * L::T_HALF : half * L::T_HALF + ds * N);
+                const uint32_t d_bar = 8 * (HALF ? ds : half * DS + ds);
+                const uint32_t t_d = tmem + L::T_D + (HALF ? ds / HS * L::T_HALF + ds % HS * N : half * L::T_HALF + ds * N);
                 ok = ok && use_wait(d_empty + d_bar, li + HS, HS, &s_abort);
                 if (!ok) break;
                 fence_after();
@@ -533,33 +535,36 @@ bool make_map(CUtensorMap *map, CUtensorMapDataType type, int size, const void *
 
 // Into how many parts K is cut, and about how long a call takes then. A part is a CTA that has an SM to itself, so what counts is how
 // many clusters of that size fit the GPU at once (GPCs have 16 to 20 SMs: 152, 76, 46, 36, 28, 23, 15 and 15 were counted), a
-// chunk's time, and what a CTA does beside its chunks: 3.8 us to start and to end, 1.9 more to join.
+// chunk's time, and what a CTA does beside its chunks: 3.8 us to start and to end, and to join 2.2 with 128 outputs or 16 rows, 3.5
+// with 256 and 64 rows.
 struct Cut {
     int split;
     float us;
 };
-Cut best_cut(long tiles, int chunks, float chunk_us) {
+Cut best_cut(long tiles, int chunks, float chunk_us, float join_us) {
     constexpr int fit[8] = {152, 76, 46, 36, 28, 23, 15, 15};
     Cut best{1, 0.f};
     for (int s = 1; s <= 8 && s <= chunks; ++s) {
-        const float us = (tiles + fit[s - 1] - 1) / fit[s - 1] * (chunk_us * ((chunks + s - 1) / s) + (s > 1 ? 5.7f : 3.8f));
+        const float us = (tiles + fit[s - 1] - 1) / fit[s - 1] * (chunk_us * ((chunks + s - 1) / s) + 3.8f + (s > 1 ? join_us : 0.f));
         if (s == 1 || us < best.us) best = {s, us};
     }
     return best;
 }
-// (a chunk's time: measured with 1, 16, 32, 60 and 128 rows, groups of 32, 64 and 128)
-template <typename T, int GROUP, int N>
+template <typename T, int GROUP, int N, int OUTPUTS>
 Cut cut_of(int m, const Weight &w) {
-    using L = Lay<T, GROUP, N>;
-    constexpr float us[5][3] = {{1.25f, 0.98f, 0.82f}, {2.0f, 1.57f, 1.35f},                            // fp32: 16 and 32 rows
-                                {1.15f, 0.75f, 0.65f}, {2.1f, 1.25f, 0.85f}, {1.76f, 1.03f, 0.57f}};    // bf16: up to 32, 64, 128
-    constexpr int row = L::SPLIT ? (N > 16 ? 1 : 0) : L::WIDE ? 4 : N > 32 ? 3 : 2;
-    return best_cut((long)((w.o + L::OUT - 1) / L::OUT) * ((m + N - 1) / N), (w.k + CHUNK - 1) / CHUNK, us[row][GROUP == 32 ? 0 : GROUP == 64 ? 1 : 2]);
+    using L = Lay<T, GROUP, N, OUTPUTS>;
+    // a chunk's time with groups of 32, 64 and 128: fp32, 16 and 32 rows; bf16, 16, 32, 64 and 128
+    constexpr float us[2][6][3] = {{{1.30f, 1.04f, 0.87f}, {1.90f, 1.70f, 1.45f}, {1.20f, 0.80f, 0.67f}, {1.53f, 0.93f, 0.77f}, {2.05f, 1.18f, 0.84f}, {}},
+                                   {{0.87f, 0.70f, 0.61f}, {1.30f, 1.20f, 1.13f}, {0.79f, 0.50f, 0.40f}, {0.85f, 0.56f, 0.44f}, {1.10f, 0.65f, 0.56f},
+                                    {1.74f, 0.90f, 0.57f}}};
+    constexpr int row = (L::SPLIT ? 0 : 2) + (N > 64 ? 3 : N > 32 ? 2 : N > 16 ? 1 : 0);
+    return best_cut((long)((w.o + L::OUT - 1) / L::OUT) * ((m + N - 1) / N), (w.k + CHUNK - 1) / CHUNK,
+                    us[L::HALF][row][GROUP == 32 ? 0 : GROUP == 64 ? 1 : 2], L::HALF ? 2.2f : 1.6f + 0.03f * N);
 }
 
-template <typename T, int GROUP, int N>
+template <typename T, int GROUP, int N, int OUTPUTS>
 cudaError_t launch(Args a, cudaStream_t s) {
-    using L = Lay<T, GROUP, N>;
+    using L = Lay<T, GROUP, N, OUTPUTS>;
     CUtensorMap map, x_map;
     memset(&x_map, 0, sizeof x_map);
     a.direct = reinterpret_cast<uintptr_t>(a.w.codes) % 16 != 0 || a.w.k % 32 != 0;
@@ -568,13 +573,13 @@ cudaError_t launch(Args a, cudaStream_t s) {
         (!L::SPLIT && !make_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.x, a.w.k, a.m, a.ldx, 64, N, CU_TENSOR_MAP_SWIZZLE_128B)))
         return cudaErrorUnknown;
     const int chunks = (a.w.k + CHUNK - 1) / CHUNK, tiles = (a.w.o + L::OUT - 1) / L::OUT, cols = (a.m + N - 1) / N;
-    a.split = cut_of<T, GROUP, N>(a.m, a.w).split;
+    a.split = cut_of<T, GROUP, N, OUTPUTS>(a.m, a.w).split;
     const int slice = (chunks + a.split - 1) / a.split * L::PER;
     const size_t beside = (size_t)slice * ((L::OUT + 2) * 2 + (a.w.zeros ? L::OUT + 4 : 0));
     a.staged = beside <= L::ROOM;
     a.slice = a.staged ? slice : 0;
     const size_t smem = std::max<size_t>(L::SCALES + 1024 + (a.staged ? beside : 0), tmem_smem_floor(512));
-    cudaError_t e = cudaFuncSetAttribute(linear4_tc_kernel<T, GROUP, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_MOST);
+    cudaError_t e = cudaFuncSetAttribute(linear4_tc_kernel<T, GROUP, N, OUTPUTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_MOST);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3(tiles * a.split, cols);
@@ -589,22 +594,34 @@ cudaError_t launch(Args a, cudaStream_t s) {
     at[1].val.programmaticStreamSerializationAllowed = 1;
     lc.attrs = at;
     lc.numAttrs = programmatic(s) ? 2 : 1;
-    e = cudaLaunchKernelEx(&lc, linear4_tc_kernel<T, GROUP, N>, map, x_map, a);
+    e = cudaLaunchKernelEx(&lc, linear4_tc_kernel<T, GROUP, N, OUTPUTS>, map, x_map, a);
     note_launch();
     return e;
 }
 
-template <typename T, int GROUP>
+// 128 outputs to a CTA where that fills the GPU better: 60 rows, k and o 4096, groups of 128 10.7 us, with 256 12.9; o 11008 21.6 and
+// 16.6; 16 fp32 rows, k 8192, o 1024 10.5 and 12.2.
+template <typename T, int GROUP, int N>
+float best_us(int m, const Weight &w) {
+    return std::min(cut_of<T, GROUP, N, 128>(m, w).us, cut_of<T, GROUP, N, 256>(m, w).us);
+}
+template <typename T, int GROUP, int N>
 cudaError_t launch_n(const Args &a, cudaStream_t s) {
-    if (a.m <= 16) return launch<T, GROUP, 16>(a, s);
+    if (cut_of<T, GROUP, N, 128>(a.m, a.w).us < cut_of<T, GROUP, N, 256>(a.m, a.w).us) return launch<T, GROUP, N, 128>(a, s);
+    return launch<T, GROUP, N, 256>(a, s);
+}
+
+template <typename T, int GROUP>
+cudaError_t launch_m(const Args &a, cudaStream_t s) {
+    if (a.m <= 16) return launch_n<T, GROUP, 16>(a, s);
     if constexpr (sizeof(T) == 2) {             // (planes of 64 rows would leave room for one stage)
-        // 128 rows of x with 128 outputs, or 64 with 256: as many CTAs, and chunks that take less. (645 rows, k 4096, 11008
-        // outputs: 82 us instead of 112.) Rows just past a multiple of 128 can leave the first with more waves:
-        // 130 rows of the same 41 us instead of 30.
-        if (a.m > 64 && cut_of<T, GROUP, 128>(a.m, a.w).us < cut_of<T, GROUP, 64>(a.m, a.w).us) return launch<T, GROUP, 128>(a, s);
-        if (a.m > 32) return launch<T, GROUP, 64>(a, s);
+        // 128 rows of x with 128 outputs: chunks that take less than those of 64 rows and 256 outputs. (645 rows, k 4096, 11008
+        // outputs: 82 us instead of 112.) Rows just past a multiple of 128 can leave the first with more waves: 130 rows of the
+        // same 41 us instead of 30.
+        if (a.m > 64 && cut_of<T, GROUP, 128, 128>(a.m, a.w).us < best_us<T, GROUP, 64>(a.m, a.w)) return launch<T, GROUP, 128, 128>(a, s);
+        if (a.m > 32) return launch_n<T, GROUP, 64>(a, s);
     }
-    return launch<T, GROUP, 32>(a, s);
+    return launch_n<T, GROUP, 32>(a, s);
 }
 
 }  // namespace
@@ -612,12 +629,12 @@ cudaError_t launch_n(const Args &a, cudaStream_t s) {
 template <typename T>
 cudaError_t launch_linear4_tc(const T *x, long ldx, int m, const Weight &w, float *y, long ldy, int accumulate, cudaStream_t s) {
     const Args a{w, x, ldx, ldy, y, m, accumulate, 1, 0, 0, 0};
-    return w.group == 128 ? launch_n<T, 128>(a, s) : w.group == 64 ? launch_n<T, 64>(a, s) : launch_n<T, 32>(a, s);
+    return w.group == 128 ? launch_m<T, 128>(a, s) : w.group == 64 ? launch_m<T, 64>(a, s) : launch_m<T, 32>(a, s);
 }
 
 template <typename T>
 float linear4_tc_us(const Weight &w) {
-    return (w.group == 128 ? cut_of<T, 128, 16>(1, w) : w.group == 64 ? cut_of<T, 64, 16>(1, w) : cut_of<T, 32, 16>(1, w)).us;
+    return w.group == 128 ? best_us<T, 128, 16>(1, w) : w.group == 64 ? best_us<T, 64, 16>(1, w) : best_us<T, 32, 16>(1, w);
 }
 
 template float linear4_tc_us<float>(const Weight &);
