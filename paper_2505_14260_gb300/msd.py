@@ -594,15 +594,23 @@ class Pages:
 
 
 _TYPES = {torch.float32: MSD_F32, torch.bfloat16: MSD_BF16}
+_F32 = (torch.float32,)
 
 
 def _matrix(t: torch.Tensor, what: str, types=_TYPES) -> int:
     """The row stride of a 2-D tensor on the current GPU whose rows are contiguous."""
-    if t.dim() != 2 or t.dtype not in types or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: a matrix with contiguous rows on the GPU, {' or '.join(str(d) for d in types)}")
-    if t.device.index != torch._C._cuda_getDevice():
+    if t.dim() != 2 or t.dtype not in types or not t.is_cuda:
+        _refuse_matrix(what, types)
+    (rows, width), (ld, step) = t.shape, t.stride()
+    if step != 1 and width > 1:
+        _refuse_matrix(what, types)
+    if t.get_device() != torch._C._cuda_getDevice():
         raise ValueError(f"{what} is not on the current GPU")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return ld if rows > 1 else width
+
+
+def _refuse_matrix(what: str, types):
+    raise ValueError(f"{what}: a matrix with contiguous rows on the GPU, {' or '.join(str(d) for d in types)}")
 
 
 def _vector(t: torch.Tensor | None, what: str, dtype: torch.dtype, n: int, device) -> int | None:
@@ -615,7 +623,7 @@ def _vector(t: torch.Tensor | None, what: str, dtype: torch.dtype, n: int, devic
 
 
 def _raw_stream(stream, device) -> int:
-    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device if type(device) is int else device.index) if stream is None else stream.cuda_stream
 
 
 def _call(st: int, call: str):
@@ -634,7 +642,7 @@ class Weight4:
         if group not in (32, 64, 128):
             raise ValueError("group is 32, 64 or 128")
         self.o, self.k, self.group = codes.shape[0], 2 * codes.shape[1], group
-        self.codes, self.scales, self.zeros = codes, scales, zeros
+        self.codes, self.scales, self.zeros, self._device = codes, scales, zeros, codes.get_device()
         n = self.o * -(-self.k // group)
         self._c = msd_weight4(codes.data_ptr(), _vector(scales, "scales", torch.bfloat16, n, codes.device),
                               _vector(zeros, "zeros", torch.uint8, n, codes.device), self.o, self.k, group)
@@ -669,12 +677,13 @@ class Weight4:
 
     def linear(self, x: torch.Tensor, y: torch.Tensor, accumulate: bool = False, stream=None) -> torch.Tensor:
         """y (=|+=) x w^T (msd_linear4): x [m, in] bf16 or fp32, y [m, out] fp32."""
-        ldx, ldy = _matrix(x, "x"), _matrix(y, "y", (torch.float32,))
-        if x.shape[1] != self.k or y.shape != (x.shape[0], self.o):
+        ldx, ldy, m, device = _matrix(x, "x"), _matrix(y, "y", _F32), len(x), x.get_device()
+        if x.shape[1] != self.k or y.shape != (m, self.o):
             raise ValueError(f"x is [m, {self.k}] and y [m, {self.o}]")
-        self._on(x)
-        st = lib().msd_linear4(x.data_ptr(), ldx, _TYPES[x.dtype], x.shape[0], self._ref, y.data_ptr(), ldy,
-                               int(accumulate), _raw_stream(stream, x.device))
+        if device != self._device:
+            raise ValueError("the weight is on another GPU")
+        st = lib().msd_linear4(x.data_ptr(), ldx, _TYPES[x.dtype], m, self._ref, y.data_ptr(), ldy, int(accumulate),
+                               _raw_stream(stream, device))
         if st:
             _call(st, "msd_linear4")
         return y
@@ -714,7 +723,7 @@ def sample(logits: torch.Tensor, u: torch.Tensor, settings: Filter | None, token
     ld, dev, (rows, vocab) = _matrix(logits, "logits"), logits.device, logits.shape
     ldp = 0
     if probs is not None:
-        ldp = _matrix(probs, "probs", (torch.float32,))
+        ldp = _matrix(probs, "probs", _F32)
         if probs.shape != logits.shape:
             raise ValueError("probs has the logits' shape")
     st = lib().msd_sample(logits.data_ptr(), ld, _TYPES[logits.dtype], rows, vocab,
