@@ -338,6 +338,35 @@ def test_accept_beside_another_stream():
         assert all(torch.equal(p, q) for p, q in zip(out, want))
 
 
+def test_many_trees_in_a_graph():
+    """The launches of more rows than fit, replayed on other logits, links and numbers of nodes; rows past the last sequence's."""
+    n, nodes = 14, 60
+    counts = [nodes] * n
+    xs = [logits(n * nodes + 7, 1500, s, peaks=6) for s in (1, 2, 3)]
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    u = torch.rand(n, 8, 5, generator=gen(1), device="cuda") * 0.7
+    b = msd.Batch(torch.arange(n, dtype=torch.int32, device="cuda"), i32([nodes * i for i in range(n + 1)]), n * nodes + 7)
+    tree, f = msd.Tree(n, nodes), settings(n, top_p=0.9)[0]
+    x = xs[0].clone()
+    out = [torch.zeros(n, 8, dtype=torch.int32, device="cuda")] + [torch.zeros(n, dtype=torch.int32, device="cuda") for _ in range(2)]
+    g = torch.cuda.CUDAGraph()
+    msd.accept(x, b, tree, u, f, *out)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        msd.accept(x, b, tree, u, f, *out)
+    for s, src in enumerate(xs):
+        live = [nodes - (s * 13 + i) % 50 for i in range(n)]
+        toks, pars = trees(counts, nodes, 1500, src[:n * nodes], s, width=3)
+        want = check_accept(src[:n * nodes], counts, toks, pars, u, nodes, n_nodes=live, top_p=0.9)
+        x.copy_(src)
+        tree.tokens.copy_(i32(toks).flatten())
+        tree.parent.copy_(i32(pars).flatten())
+        tree.n_nodes.copy_(i32(live))
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want))
+
+
 def test_refusals():
     x, u, t = logits(4, 100), uniforms(4), torch.zeros(4, dtype=torch.int32, device="cuda")
     f3 = msd.Filter(temperature=torch.ones(3, device="cuda"))
