@@ -626,6 +626,11 @@ def _raw_stream(stream, device) -> int:
     return torch._C._cuda_getCurrentRawStream(device if type(device) is int else device.index) if stream is None else stream.cuda_stream
 
 
+def _memory_of(stream):
+    """Tensors made inside are memory that a call on `stream` (None: the current one) may write now."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def _call(st: int, call: str):
     if st != MSD_OK:
         raise MsdError(st, call, "bad sizes, strides or alignment" if st == MSD_ERR_INVALID else "launch failed")
@@ -650,15 +655,17 @@ class Weight4:
 
     @classmethod
     def of(cls, w: torch.Tensor, group: int = 128, zeros: bool = False, stream=None) -> "Weight4":
-        """w [out, in] in 4 bits (msd_quantize4)."""
+        """w [out, in] in 4 bits (msd_quantize4). Codes, scales and zeros are memory of the stream that the call runs
+        on, as tensors made there are: another stream uses them behind that one, and as long as they are held."""
         _matrix(w, "w")
         if group not in (32, 64, 128):
             raise ValueError("group is 32, 64 or 128")
         o, k = w.shape
         n = -(-k // group)
-        self = cls(torch.empty(o, k // 2, dtype=torch.uint8, device=w.device),
-                   torch.empty(o, n, dtype=torch.bfloat16, device=w.device),
-                   torch.empty(o, n, dtype=torch.uint8, device=w.device) if zeros else None, group)
+        with _memory_of(stream):
+            self = cls(torch.empty(o, k // 2, dtype=torch.uint8, device=w.device),
+                       torch.empty(o, n, dtype=torch.bfloat16, device=w.device),
+                       torch.empty(o, n, dtype=torch.uint8, device=w.device) if zeros else None, group)
         return self.quantize(w, stream=stream)
 
     def quantize(self, w: torch.Tensor, values: torch.Tensor | None = None, stream=None) -> "Weight4":
@@ -748,7 +755,7 @@ def accept(logits: torch.Tensor, batch: Batch, tree: Tree, u: torch.Tensor, sett
     for t in (batch.seqs, tree.tokens):
         if t.device != dev:
             raise ValueError("batch, tree and logits are on one GPU")
-    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):         # memory that this stream may write now
+    with _memory_of(stream):
         scratch = torch.empty(2 * rows, dtype=torch.int32, device=dev)
     st = lib().msd_accept_batch(
         logits.data_ptr(), ld, _TYPES[logits.dtype], logits.shape[1], batch.c(), ctypes.byref(tree.c()), tree.N,

@@ -306,6 +306,25 @@ def test_codes_of_strided_rows():
     check_codes(wide[:1, 4:4 + 16], 32, False, with_values=False)
 
 
+def test_of_beside_another_stream():
+    """What the current stream still writes into memory that it has given back does not meet codes made on another stream."""
+    w = 0.05 * torch.randn(512, 1024, generator=gen(8), device="cuda")
+    want = msd.Weight4.of(w, group=64, zeros=True)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        used = [torch.empty_like(t) for t in (want.codes, want.scales, want.zeros)]
+        for _ in range(200):
+            for t in used:
+                t.fill_(77)
+        del used, t
+        got = msd.Weight4.of(w, group=64, zeros=True, stream=s)
+        torch.cuda.synchronize()
+        for a, b in ((got.codes, want.codes), (got.scales, want.scales), (got.zeros, want.zeros)):
+            assert torch.equal(a, b)
+        del got, a
+
+
 def test_of_and_linear_together():
     """A projection brought to 4 bits: its products are those of the values it stands for."""
     w = 0.05 * torch.randn(688, 256, generator=gen(6), device="cuda")
