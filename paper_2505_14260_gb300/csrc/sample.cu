@@ -513,9 +513,10 @@ __device__ __noinline__ Left rest_of_list(Left l, int n, int k, float p, u64 mas
         const u64 before = sum_up_to(in ? w : 0, &all) - w;                 // (of those that top-k leaves; i is one of them or out)
         in = in && before < max(share_floor(p, k > 0 ? all : mass, true), 1ull);
     }
-    in = in && (w >= l.least || i == 0);
-    sum_up_to(in ? w : 0, &l.total);
+    // the run's end: min-p, which goes by weights, may leave a hole in it (a lower logit's weight can be the larger one by a unit)
     const int left = __syncthreads_count(in);
+    in = in && w >= l.least;
+    sum_up_to(in ? w : 0, &l.total);
     if (i < n) sh.list[i] = Token{order, in ? w : 0};
     if (i == left - 1) { sh.end = logit_of_order(order); sh.tie = id_of_order(order); }
     __syncthreads();

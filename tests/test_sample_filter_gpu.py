@@ -144,6 +144,34 @@ def test_strides_and_neighbours():
     assert torch.allclose(probs[:, 5:1026].sum(1), torch.ones(4, device="cuda"), atol=1e-4)
 
 
+def test_min_p_between_two_logits_whose_weights_are_the_other_way_round():
+    """Weights are taken to 2^-44, so of two logits the lower one's may be the larger by a unit. Where min_p lies between them,
+    what is drawn, its probability and what a tree accepts go by the weights alike, through lists (top_k) and without."""
+    for top, low in (("0x1.c2f09p+3", "0x1.7ffffep-20"), ("0x1.c646bap+3", "-0x1.800002p-20"), ("0x1.b5f74ep+3", "-0x1.2p-18")):
+        top, low = float.fromhex(top), float.fromhex(low)
+        high = torch.nextafter(torch.tensor(low), torch.tensor(INF)).item()
+        x = torch.tensor([[top, high, low] + [-50.0] * 5], device="cuda")
+        p = torch.tensor(math.exp(low - top)).nextafter(torch.tensor(0.0)).item()
+        u = torch.tensor([1.0], device="cuda")                       # the last id that is left
+        for min_p in (p, math.exp(low - top), torch.tensor(math.exp(low - top)).nextafter(torch.tensor(1.0)).item()):
+            for top_k in (0, 3):
+                f, _ = settings(1, top_k=top_k, min_p=min_p)
+                t, lp, probs = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(1, device="cuda"), torch.zeros(1, 8, device="cuda")
+                msd.sample(x, u, f, t, logp=lp, probs=probs)
+                share = probs[0, int(t)].item()
+                # half a step of a logarithm of 14 is 2^-21; the probability's own 2^-21; a unit of a weight of 10^7
+                assert share > 0 and abs(share - math.exp(lp.item())) <= 2.0 ** -19 * share, (top, min_p, top_k, share, lp.item())
+                assert not bool((probs[0, int(t) + 1:] > 0).any())
+                # a child with the token that was drawn is accepted where u is 0
+                b = msd.Batch(torch.zeros(1, dtype=torch.int32, device="cuda"), torch.tensor([0, 2], dtype=torch.int32, device="cuda"), 2)
+                tree = msd.Tree(1, 2)
+                tree.tokens.copy_(torch.cat([torch.zeros_like(t), t]))
+                tree.parent.copy_(torch.tensor([-1, 0], dtype=torch.int32, device="cuda"))
+                path, n, bonus = (torch.zeros(1, c, dtype=torch.int32, device="cuda") for c in (2, 1, 1))
+                msd.accept(x.repeat(2, 1), b, tree, torch.zeros(1, 2, 2, device="cuda"), f, path, n.view(1), bonus.view(1))
+                assert path.tolist() == [[0, 1]] and n.item() == 1, (top, min_p, top_k)
+
+
 def test_no_rows():
     msd.sample(torch.empty(0, 100, device="cuda"), torch.empty(0, device="cuda"), None,
                torch.empty(0, dtype=torch.int32, device="cuda"))
