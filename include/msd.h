@@ -511,7 +511,7 @@ msd_status msd_pages_attention(msd_pages *p, int32_t layer, const msd_batch *bat
 
 /* A weight matrix [o][k] in 4 bits: code c stands for scale * (c - zero) with the scale
  * and zero of its group, `group` consecutive elements of a row (the last group of a row
- * may be shorter). k is a multiple of 8; group is 32, 64 or 128. */
+ * may be shorter). k is a multiple of 8; group is 32, 64 or 128; o and k are 2^30 at most. */
 typedef struct {
     uint8_t *codes;             /* [o][k / 2], 4-byte aligned: element 2 i in the low half of byte i,
                                    2 i + 1 in the high half */

@@ -395,10 +395,11 @@ static cudaError_t launch_quantize(const T *x, long ldw, const Weight &w, T *val
 }
 
 constexpr int MOST_ROWS = 65535 * 32;           // a grid's height in tiles of 32
+constexpr int MOST_SIZE = 1 << 30;              // of o and k: they are rounded up to groups, chunks and tiles in 32 bits
 
 static bool take_weight(const msd_weight4 *w, Weight *out) {
-    if (!w || !w->codes || !w->scales || w->o < 1 || w->k < 8 || w->k % 8 || reinterpret_cast<uintptr_t>(w->codes) % 4 ||
-        reinterpret_cast<uintptr_t>(w->scales) % 2 || (w->group != 32 && w->group != 64 && w->group != 128))
+    if (!w || !w->codes || !w->scales || w->o < 1 || w->o > MOST_SIZE || w->k < 8 || w->k > MOST_SIZE || w->k % 8 ||
+        reinterpret_cast<uintptr_t>(w->codes) % 4 || reinterpret_cast<uintptr_t>(w->scales) % 2 || (w->group != 32 && w->group != 64 && w->group != 128))
         return false;
     *out = Weight{w->codes, static_cast<bf16 *>(w->scales), w->zeros, w->o, w->k, w->group, (w->k + w->group - 1) / w->group};
     return true;

@@ -29,6 +29,18 @@ def test_linear4_refuses(lib, bad):
     assert linear(lib, **bad) == msd.MSD_ERR_INVALID
 
 
+@pytest.mark.parametrize("bad", [dict(k=2**31 - 8, ldx=2**31 - 8), dict(k=2**30 + 8, ldx=2**30 + 8), dict(o=2**31 - 1, ldy=2**31 - 1),
+                                 dict(o=2**30 + 1, ldy=2**30 + 1)], ids=str)
+def test_weights_whose_indices_would_pass_32_bits(lib, bad):
+    """Sizes are rounded up to groups, chunks and tiles in 32 bits."""
+    for group in (32, 64, 128):
+        assert linear(lib, group=group, **bad) == msd.MSD_ERR_INVALID
+        a = dict(o=8, k=64)
+        a.update({n: v for n, v in bad.items() if n in a})
+        w = msd.msd_weight4(A, A, None, a["o"], a["k"], group)
+        assert lib.msd_quantize4(A, a["k"], msd.MSD_F32, ctypes.byref(w), None, 0, None) == msd.MSD_ERR_INVALID
+
+
 def test_linear4_without_rows_or_weight(lib):
     assert linear(lib, m=0) == msd.MSD_OK
     assert lib.msd_linear4(A, 64, 1, 1, None, A, 8, 0, None) == msd.MSD_ERR_INVALID
