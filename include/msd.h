@@ -577,8 +577,8 @@ msd_status msd_sample(const void *logits_dev, int64_t ld, int32_t dtype, int32_t
  * path[i * (depth + 1) + d]: the nodes accepted, node 0 first, then -1; accept_len[i]: their
  * number less one. path and accept_len + 1 are what msd_pages_compact takes. A sequence without
  * rows gives -1, 0 and a bonus of -1; a row without any weight a bonus of -1.
- * scratch: [2 * rows] int32, any contents, not used by another call at the same time. depth >= 0,
- * children 1 .. 256, tree_nodes <= 1024. */
+ * scratch: [2 * rows] int32, any contents, not used by another call at the same time. depth 0 .. 2^20,
+ * children 1 .. 256, tree_nodes <= 1024; at most 2^30 rows and sequences. */
 msd_status msd_accept_batch(const void *logits_dev, int64_t ld, int32_t dtype, int32_t vocab, const msd_batch *batch,
                             const msd_tree *tree, int32_t tree_nodes, const msd_filter *f, const float *u_dev,
                             int32_t depth, int32_t children, int32_t *scratch_dev, int32_t *path_dev,

@@ -36,6 +36,8 @@ constexpr float Y_MOST = 46.f;                  // exponents from here on have w
 constexpr int MAX_VOCAB = 393216;
 constexpr int MAX_CHILDREN = 256;
 constexpr int MAX_TREE_NODES = 1024;
+constexpr int MAX_DEPTH = 1 << 20;
+constexpr int MAX_TREE_ROWS = 1 << 30;          // and sequences: a loop's next index, and the sum of two, stay in 32 bits
 
 __device__ __forceinline__ float logit_at(const float *row, int i) { return row[i]; }
 __device__ __forceinline__ float logit_at(const bf16 *row, int i) { return __bfloat162float(row[i]); }
@@ -1159,10 +1161,10 @@ msd_status msd_accept_batch(const void *logits, int64_t ld, int32_t dtype, int32
                             const msd_tree *tree, int32_t tree_nodes, const msd_filter *f, const float *u,
                             int32_t depth, int32_t children, int32_t *scratch, int32_t *path, int32_t *accept_len,
                             int32_t *bonus, void *stream) {
-    if (!batch || batch->n < 0 || batch->rows < 0) return MSD_ERR_INVALID;
+    if (!batch || batch->n < 0 || batch->n > MAX_TREE_ROWS || batch->rows < 0 || batch->rows > MAX_TREE_ROWS) return MSD_ERR_INVALID;
     if (batch->n == 0) return MSD_OK;
     if (!batch->row_start || !tree || !tree->tokens || !tree->parent || tree_nodes < 1 || tree_nodes > MAX_TREE_NODES ||
-        !u || depth < 0 || depth > (1 << 20) || children < 1 || children > MAX_CHILDREN || !path || !accept_len || !bonus)
+        !u || depth < 0 || depth > MAX_DEPTH || children < 1 || children > MAX_CHILDREN || !path || !accept_len || !bonus)
         return MSD_ERR_INVALID;
     if (batch->rows > 0 && (bad_logits(logits, ld, dtype, vocab) || !scratch)) return MSD_ERR_INVALID;
     const Settings s = settings_of(f);

@@ -76,6 +76,16 @@ def test_accept_refuses(lib, bad):
                                 a["children"], a["scratch"], a["path"], a["len_"], a["bonus"], None) == msd.MSD_ERR_INVALID
 
 
+@pytest.mark.parametrize("bad", [dict(rows=2**31 - 1), dict(rows=2**30 + 1), dict(n=2**31 - 1), dict(n=2**30 + 1)], ids=str)
+def test_trees_whose_indices_would_pass_32_bits(lib, bad):
+    """Rows are taken 1024 at a time, sequences halved and 32 at a time, in 32 bits."""
+    a = dict(n=2, rows=4)
+    a.update(bad)
+    b = msd.msd_batch(a["n"], A, A, a["rows"])
+    t = msd.msd_tree(A, A, None, None, None)
+    assert lib.msd_accept_batch(A, 1, msd.MSD_BF16, 1, ctypes.byref(b), ctypes.byref(t), 4, None, A, 2, 3, A, A, A, A, None) == msd.MSD_ERR_INVALID
+
+
 def test_nothing_to_do_needs_no_gpu(lib):
     assert lib.msd_sample(None, 0, 0, 0, 100, None, None, None, None, None, 0, None) == msd.MSD_OK
     b, t = msd.msd_batch(0, None, None, 0), msd.msd_tree()
