@@ -529,6 +529,17 @@ typedef struct {
 msd_status msd_linear4(const void *x_dev, int64_t ldx, int32_t x_dtype, int32_t m, const msd_weight4 *w,
                        float *y_dev, int64_t ldy, int32_t accumulate, void *stream);
 
+/* Test hook of its launch rules (host only, needs no GPU; addresses of *w are looked at for their alignment, not read). */
+typedef struct {
+    int32_t few;                /* 1: the kernel of few rows, on mma.sync; 0: the one on tcgen05 */
+    int32_t rows, outputs;      /* of a CTA, at most */
+    int32_t split;              /* CTAs that share K */
+    int32_t staged;             /* scales and zeros are brought to shared memory first */
+    int32_t direct;             /* codes are read by words, their address or row being aligned to less */
+    int32_t smem_bytes;
+} msd_linear4_shape;
+msd_status msd_test_linear4_shape(int32_t x_dtype, int32_t m, const msd_weight4 *w, msd_linear4_shape *out);
+
 /* Writes the codes, scales and (unless null) zeros of *out from w [o][ldw], bf16 or fp32 with
  * 16-byte aligned rows. Per group, without zeros: scale = max|w| / 7 rounded to bf16; with zeros:
  * scale = (max(w, 0) - min(w, 0)) / 15 rounded to bf16, zero = -min(w, 0) / scale to the nearest

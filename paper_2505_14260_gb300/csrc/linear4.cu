@@ -23,6 +23,7 @@ namespace msd {
 // read from the caches (16 bytes a lane and word).
 // ---------------------------------------------------------------------------
 constexpr int FEW_WARPS = 8, FEW_OUT = 32, FEW_DEPTH = 3;
+constexpr size_t FEW_BESIDE = 64 * 1024;        // room for scales and zeros; longer rows read them where they are
 
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                           uint32_t b1) {
@@ -213,20 +214,27 @@ static FewKernel<T> few_kernel(bool two, bool wide) {
 }
 
 template <typename T>
-static cudaError_t launch_few(const T *x, long ldx, int m, const Weight &w, float *y, long ldy, int accumulate, cudaStream_t s) {
+static Linear4Shape few_shape(int m, const Weight &w) {
     const int align = w.group / 8;              // bytes of a lane's codes of a group
     const bool wide = reinterpret_cast<uintptr_t>(w.codes) % align == 0 && w.k / 2 % align == 0;
     const int step = m > 8 ? 16 : 8;            // m <= 16
-    const FewKernel<T> f = w.group == 128 ? few_kernel<T, 128>(m > 8, wide) : w.group == 64 ? few_kernel<T, 64>(m > 8, wide) : few_kernel<T, 32>(m > 8, wide);
     const size_t sums = (size_t)FEW_WARPS * FEW_OUT * step * 4, beside = (size_t)FEW_OUT * w.groups * 3;
-    constexpr size_t BESIDE = 64 * 1024;        // longer rows read them where they are
-    const bool staged = beside <= BESIDE;
-    const size_t smem = sums + (staged ? beside : 0);
+    const bool staged = beside <= FEW_BESIDE;
+    return Linear4Shape{step, FEW_OUT, 1, staged, !wide, w.groups, sums + (staged ? beside : 0)};
+}
+
+template <typename T>
+static cudaError_t launch_few(const T *x, long ldx, int m, const Weight &w, float *y, long ldy, int accumulate, cudaStream_t s) {
+    const Linear4Shape c = few_shape<T>(m, w);
+    const bool wide = !c.direct;
+    const FewKernel<T> f = w.group == 128 ? few_kernel<T, 128>(m > 8, wide) : w.group == 64 ? few_kernel<T, 64>(m > 8, wide) : few_kernel<T, 32>(m > 8, wide);
+    const size_t smem = c.smem;
+    constexpr size_t most = (size_t)FEW_WARPS * FEW_OUT * 16 * 4 + FEW_BESIDE;
     cudaError_t e = cudaSuccess;
     // (one value, whatever the call: another thread may be between this and its launch)
-    if (smem > 48 * 1024) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sums + BESIDE));
+    if (smem > 48 * 1024) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
     if (e == cudaSuccess) {
-        e = launch_chain(f, (w.o + FEW_OUT - 1) / FEW_OUT, FEW_WARPS * 32, smem, s, x, ldx, m, w, y, ldy, accumulate, (int)staged);
+        e = launch_chain(f, (w.o + FEW_OUT - 1) / FEW_OUT, FEW_WARPS * 32, smem, s, x, ldx, m, w, y, ldy, accumulate, (int)c.staged);
         note_launch();
     }
     return e;
@@ -430,6 +438,19 @@ msd_status msd_linear4(const void *x, int64_t ldx, int32_t x_dtype, int32_t m, c
     };
     const cudaError_t e = x_dtype == MSD_F32 ? run(static_cast<const float *>(x)) : run(static_cast<const bf16 *>(x));
     return e == cudaSuccess ? MSD_OK : MSD_ERR_CUDA;
+}
+
+msd_status msd_test_linear4_shape(int32_t x_dtype, int32_t m, const msd_weight4 *weight, msd_linear4_shape *out) {
+    Weight w;
+    if (m < 1 || m > MOST_ROWS || !take_weight(weight, &w) || (x_dtype != MSD_F32 && x_dtype != MSD_BF16) || !out) return MSD_ERR_INVALID;
+    const auto shape = [&](auto v) {
+        using T = decltype(v);
+        const bool few = few_rows<T>(m, w);
+        const Linear4Shape c = few ? few_shape<T>(m, w) : linear4_tc_shape<T>(m, w);
+        *out = msd_linear4_shape{few, c.rows, c.outputs, c.split, c.staged, c.direct, (int32_t)c.smem};
+    };
+    x_dtype == MSD_F32 ? shape(float()) : shape(bf16());
+    return MSD_OK;
 }
 
 msd_status msd_quantize4(const void *x, int64_t ldw, int32_t dtype, const msd_weight4 *out, void *values, int64_t ldv,

@@ -64,6 +64,16 @@ template <> struct Octet<float> {
 template <typename T>
 cudaError_t launch_linear4_tc(const T *x, long ldx, int m, const Weight &w, float *y, long ldy, int accumulate, cudaStream_t s);
 
+// How they are launched: rows and outputs to a CTA, parts of K, whether scales and zeros are staged (`slice` groups of them) and codes
+// read without tensor copies.
+struct Linear4Shape {
+    int rows, outputs, split;
+    bool staged, direct;
+    int slice;
+    size_t smem;
+};
+template <typename T> Linear4Shape linear4_tc_shape(int m, const Weight &w);
+
 // About how long up to 16 rows take there.
 template <typename T> float linear4_tc_us(const Weight &w);
 

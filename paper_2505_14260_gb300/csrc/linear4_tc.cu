@@ -562,29 +562,39 @@ Cut cut_of(int m, const Weight &w) {
                     us[L::HALF][row][GROUP == 32 ? 0 : GROUP == 64 ? 1 : 2], L::HALF ? 2.2f : 1.6f + 0.03f * N);
 }
 
+// How a call is launched with blocks of N rows and OUTPUTS outputs: the parts of K, and what of scales and zeros a CTA stages.
+template <typename T, int GROUP, int N, int OUTPUTS>
+Linear4Shape shape_of(int m, const Weight &w) {
+    using L = Lay<T, GROUP, N, OUTPUTS>;
+    const int chunks = (w.k + CHUNK - 1) / CHUNK, split = cut_of<T, GROUP, N, OUTPUTS>(m, w).split;
+    const int slice = (chunks + split - 1) / split * L::PER;
+    const size_t beside = (size_t)slice * ((L::OUT + 2) * 2 + (w.zeros ? L::OUT + 4 : 0));
+    const bool staged = beside <= L::ROOM, direct = reinterpret_cast<uintptr_t>(w.codes) % 16 != 0 || w.k % 32 != 0;
+    const size_t smem = std::max<size_t>(L::SCALES + 1024 + (staged ? beside : 0), tmem_smem_floor(512));
+    return Linear4Shape{N, OUTPUTS, split, staged, direct, staged ? slice : 0, smem};
+}
+
 template <typename T, int GROUP, int N, int OUTPUTS>
 cudaError_t launch(Args a, cudaStream_t s) {
     using L = Lay<T, GROUP, N, OUTPUTS>;
+    const Linear4Shape c = shape_of<T, GROUP, N, OUTPUTS>(a.m, a.w);
     CUtensorMap map, x_map;
     memset(&x_map, 0, sizeof x_map);
-    a.direct = reinterpret_cast<uintptr_t>(a.w.codes) % 16 != 0 || a.w.k % 32 != 0;
+    a.direct = c.direct;
     memset(&map, 0, sizeof map);
     if ((!a.direct && !make_map(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.w.codes, a.w.k / 2, a.w.o, a.w.k / 2, CHUNK / 2, TILE, CU_TENSOR_MAP_SWIZZLE_64B)) ||
         (!L::SPLIT && !make_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.x, a.w.k, a.m, a.ldx, 64, N, CU_TENSOR_MAP_SWIZZLE_128B)))
         return cudaErrorUnknown;
-    const int chunks = (a.w.k + CHUNK - 1) / CHUNK, tiles = (a.w.o + L::OUT - 1) / L::OUT, cols = (a.m + N - 1) / N;
-    a.split = cut_of<T, GROUP, N, OUTPUTS>(a.m, a.w).split;
-    const int slice = (chunks + a.split - 1) / a.split * L::PER;
-    const size_t beside = (size_t)slice * ((L::OUT + 2) * 2 + (a.w.zeros ? L::OUT + 4 : 0));
-    a.staged = beside <= L::ROOM;
-    a.slice = a.staged ? slice : 0;
-    const size_t smem = std::max<size_t>(L::SCALES + 1024 + (a.staged ? beside : 0), tmem_smem_floor(512));
+    const int tiles = (a.w.o + L::OUT - 1) / L::OUT, cols = (a.m + N - 1) / N;
+    a.split = c.split;
+    a.staged = c.staged;
+    a.slice = c.slice;
     cudaError_t e = cudaFuncSetAttribute(linear4_tc_kernel<T, GROUP, N, OUTPUTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_MOST);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3(tiles * a.split, cols);
     lc.blockDim = THREADS;
-    lc.dynamicSmemBytes = smem;
+    lc.dynamicSmemBytes = c.smem;
     lc.stream = s;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -599,29 +609,37 @@ cudaError_t launch(Args a, cudaStream_t s) {
     return e;
 }
 
+template <int N> using Rows = std::integral_constant<int, N>;
+template <int N> using Outs = std::integral_constant<int, N>;
+
+// f of the rows and outputs that a CTA of this call has.
+//
 // 128 outputs to a CTA where that fills the GPU better: 60 rows, k and o 4096, groups of 128 10.7 us, with 256 12.9; o 11008 21.6 and
 // 16.6; 16 fp32 rows, k 8192, o 1024 10.5 and 12.2.
 template <typename T, int GROUP, int N>
 float best_us(int m, const Weight &w) {
     return std::min(cut_of<T, GROUP, N, 128>(m, w).us, cut_of<T, GROUP, N, 256>(m, w).us);
 }
-template <typename T, int GROUP, int N>
-cudaError_t launch_n(const Args &a, cudaStream_t s) {
-    if (cut_of<T, GROUP, N, 128>(a.m, a.w).us < cut_of<T, GROUP, N, 256>(a.m, a.w).us) return launch<T, GROUP, N, 128>(a, s);
-    return launch<T, GROUP, N, 256>(a, s);
+template <typename T, int GROUP, int N, typename F>
+auto with_outputs(int m, const Weight &w, F f) {
+    if (cut_of<T, GROUP, N, 128>(m, w).us < cut_of<T, GROUP, N, 256>(m, w).us) return f(Rows<N>(), Outs<128>());
+    return f(Rows<N>(), Outs<256>());
 }
-
-template <typename T, int GROUP>
-cudaError_t launch_m(const Args &a, cudaStream_t s) {
-    if (a.m <= 16) return launch_n<T, GROUP, 16>(a, s);
+template <typename T, int GROUP, typename F>
+auto with_blocks(int m, const Weight &w, F f) {
+    if (m <= 16) return with_outputs<T, GROUP, 16>(m, w, f);
     if constexpr (sizeof(T) == 2) {             // (planes of 64 rows would leave room for one stage)
         // 128 rows of x with 128 outputs: chunks that take less than those of 64 rows and 256 outputs. (645 rows, k 4096, 11008
         // outputs: 82 us instead of 112.) Rows just past a multiple of 128 can leave the first with more waves: 130 rows of the
         // same 41 us instead of 30.
-        if (a.m > 64 && cut_of<T, GROUP, 128, 128>(a.m, a.w).us < best_us<T, GROUP, 64>(a.m, a.w)) return launch<T, GROUP, 128, 128>(a, s);
-        if (a.m > 32) return launch_n<T, GROUP, 64>(a, s);
+        if (m > 64 && cut_of<T, GROUP, 128, 128>(m, w).us < best_us<T, GROUP, 64>(m, w)) return f(Rows<128>(), Outs<128>());
+        if (m > 32) return with_outputs<T, GROUP, 64>(m, w, f);
     }
-    return launch_n<T, GROUP, 32>(a, s);
+    return with_outputs<T, GROUP, 32>(m, w, f);
+}
+template <typename F>
+auto with_group(const Weight &w, F f) {
+    return w.group == 128 ? f(std::integral_constant<int, 128>()) : w.group == 64 ? f(std::integral_constant<int, 64>()) : f(std::integral_constant<int, 32>());
 }
 
 }  // namespace
@@ -629,16 +647,29 @@ cudaError_t launch_m(const Args &a, cudaStream_t s) {
 template <typename T>
 cudaError_t launch_linear4_tc(const T *x, long ldx, int m, const Weight &w, float *y, long ldy, int accumulate, cudaStream_t s) {
     const Args a{w, x, ldx, ldy, y, m, accumulate, 1, 0, 0, 0};
-    return w.group == 128 ? launch_m<T, 128>(a, s) : w.group == 64 ? launch_m<T, 64>(a, s) : launch_m<T, 32>(a, s);
+    return with_group(w, [&](auto group) {
+        return with_blocks<T, decltype(group)::value>(
+            m, w, [&](auto rows, auto outs) { return launch<T, decltype(group)::value, decltype(rows)::value, decltype(outs)::value>(a, s); });
+    });
+}
+
+template <typename T>
+Linear4Shape linear4_tc_shape(int m, const Weight &w) {
+    return with_group(w, [&](auto group) {
+        return with_blocks<T, decltype(group)::value>(
+            m, w, [&](auto rows, auto outs) { return shape_of<T, decltype(group)::value, decltype(rows)::value, decltype(outs)::value>(m, w); });
+    });
 }
 
 template <typename T>
 float linear4_tc_us(const Weight &w) {
-    return w.group == 128 ? best_us<T, 128, 16>(1, w) : w.group == 64 ? best_us<T, 64, 16>(1, w) : best_us<T, 32, 16>(1, w);
+    return with_group(w, [&](auto group) { return best_us<T, decltype(group)::value, 16>(1, w); });
 }
 
 template float linear4_tc_us<float>(const Weight &);
 template float linear4_tc_us<bf16>(const Weight &);
+template Linear4Shape linear4_tc_shape<float>(int, const Weight &);
+template Linear4Shape linear4_tc_shape<bf16>(int, const Weight &);
 template cudaError_t launch_linear4_tc<float>(const float *, long, int, const Weight &, float *, long, int, cudaStream_t);
 template cudaError_t launch_linear4_tc<bf16>(const bf16 *, long, int, const Weight &, float *, long, int, cudaStream_t);
 

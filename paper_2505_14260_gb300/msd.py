@@ -97,6 +97,11 @@ class msd_weight4(ctypes.Structure):
                 ("group", c_int32)]
 
 
+class msd_linear4_shape(ctypes.Structure):
+    _fields_ = [("few", c_int32), ("rows", c_int32), ("outputs", c_int32), ("split", c_int32), ("staged", c_int32),
+                ("direct", c_int32), ("smem_bytes", c_int32)]
+
+
 class msd_filter(ctypes.Structure):
     _fields_ = [("temperature", c_void_p), ("top_k", c_void_p), ("top_p", c_void_p), ("min_p", c_void_p)]
 
@@ -145,6 +150,7 @@ _SIGNATURES = {
                                       c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p]),
     "msd_linear4": (c_int32, [c_void_p, c_int64, c_int32, c_int32, POINTER(msd_weight4), c_void_p, c_int64, c_int32,
                               c_void_p]),
+    "msd_test_linear4_shape": (c_int32, [c_int32, c_int32, POINTER(msd_weight4), POINTER(msd_linear4_shape)]),
     "msd_quantize4": (c_int32, [c_void_p, c_int64, c_int32, POINTER(msd_weight4), c_void_p, c_int64, c_void_p]),
     "msd_sample": (c_int32, [c_void_p, c_int64, c_int32, c_int32, c_int32, POINTER(msd_filter), c_void_p, c_void_p,
                              c_void_p, c_void_p, c_int64, c_void_p]),

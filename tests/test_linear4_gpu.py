@@ -8,6 +8,7 @@ import pytest
 import torch
 
 from paper_2505_14260_gb300 import build, msd
+from tests.tokens_support import LINEAR4, linear4_shape
 
 pytestmark = pytest.mark.gpu
 
@@ -112,6 +113,35 @@ def test_rows_past_a_block(m, o):
     run(m, 256, o, 128, True)
 
 
+@pytest.mark.parametrize("case", LINEAR4, ids=lambda c: "-".join(str(v) for v in c[:6]))
+def test_every_kernel(case):
+    """Each kernel that there is, with its scales and zeros staged and read where they are, and the sizes of large layers. Relative to the
+    norm of y: a group's sum is rounded (or cut) once for each 16 elements and plane that are added to it, its share of the total once,
+    by 2^-24 of the sum on average, alike within a group at worst and at random over the groups; 4 for the rest."""
+    dtype, group, m, k, o, zeros, few, rows, outputs, staged = case
+    w = weight(o, k, group, zeros, m)
+    c = linear4_shape(dtype, group, m, k, o, zeros, w.codes.data_ptr())
+    assert (c.few, c.rows, c.outputs, c.staged) == (few, rows, outputs, staged)
+    x = torch.randn(m, k, generator=gen(m + 1), device="cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    y = w.linear(x, torch.full((m, o), math.nan, device="cuda"))
+    torch.cuda.synchronize()
+    ref = x.double() @ values(w).T
+    adds = group // 16 * (3 if dtype == "f32" else 1)
+    assert float((y.double() - ref).norm() / ref.norm()) <= 2.0 ** -24 * (adds + (k / group) ** 0.5 + 4)
+    assert float((y.double() - ref).abs().max() / ref.abs().max()) <= 2.0 ** -20 * (adds + (k / group) ** 0.5 + 4)
+
+
+@pytest.mark.parametrize("group", [64, 128])
+@pytest.mark.parametrize("m", [5, 12, 60])
+def test_later_planes_of_fp32_x_keep_their_bits(m, group):
+    """With sums of their own, or first: errors of 8e-8 of the norm of y where plane after plane made 4.4e-7. The bound lies between."""
+    w = weight(300, 2048, group, True, m)
+    x = torch.randn(m, 2048, generator=gen(m), device="cuda")
+    y = w.linear(x, torch.empty(m, 300, device="cuda")).double()
+    ref = x.double() @ values(w).T
+    assert float((y - ref).norm() / ref.norm()) <= 2.0 ** -22
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("m", [1, 11, 66, 200])
 def test_strides_and_neighbours(m, dtype):
@@ -158,6 +188,23 @@ def test_fp32_x_is_not_rounded():
     want = w.scales[:, 0].double() * 2.0 ** -23
     for i, f in enumerate((1.0, 2.0 ** 60, 2.0 ** -60)):
         assert torch.equal(y[i].double(), want * f)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("m,o", [(8, 300), (12, 300), (12, 20000), (60, 300), (60, 20000)])
+def test_fp32_x_is_not_rounded_in_any_kernel(m, o, group):
+    """The same of every kernel of fp32 x: rows of one value that needs 24 bits, with another of the opposite sign or not."""
+    w = weight(o, 256, group, False)
+    w.codes[:, 0] = 0x99
+    x = torch.zeros(m, 256, device="cuda")
+    x[:, 0] = (1 + 2.0 ** -23) * 2.0 ** torch.arange(m, device="cuda")
+    x[::2, 1] = -(2.0 ** torch.arange(0, m, 2, device="cuda"))
+    y = torch.empty(m, o, device="cuda")
+    w.linear(x, y)
+    torch.cuda.synchronize()
+    s = w.scales[:, 0].double()
+    for i in range(m):
+        assert torch.equal(y[i], (s * float(x[i, 0].double() + x[i, 1].double())).float())
 
 
 @pytest.mark.parametrize("dtype", TYPES)

@@ -1,11 +1,14 @@
 """Filtered sampling, tree acceptance and 4-bit products: arguments that are refused before
 anything touches a GPU, and the sums behind the fixed-point weights."""
 import ctypes
+import itertools
+import random
 
 import pytest
 import torch
 
 from paper_2505_14260_gb300 import build, msd
+from tests.tokens_support import LINEAR4, linear4_shape
 
 P = ctypes.c_void_p
 A = 1 << 20                      # an address that nothing reads: every call here is refused
@@ -39,6 +42,38 @@ def test_weights_whose_indices_would_pass_32_bits(lib, bad):
         a.update({n: v for n, v in bad.items() if n in a})
         w = msd.msd_weight4(A, A, None, a["o"], a["k"], group)
         assert lib.msd_quantize4(A, a["k"], msd.MSD_F32, ctypes.byref(w), None, 0, None) == msd.MSD_ERR_INVALID
+
+
+def test_every_kernel_of_a_product_is_among_the_tested_ones(lib):
+    """The list that the GPU tests run has each kernel, with scales and zeros staged and not, whatever the times that choose between
+    them become; sizes from a token's to long prompts' lead to no other."""
+    for dtype, group, m, k, o, zeros, few, rows, outputs, staged in LINEAR4:
+        c = linear4_shape(dtype, group, m, k, o, zeros)
+        assert (c.few, c.rows, c.outputs, c.staged) == (few, rows, outputs, staged), (dtype, group, m, k, o, zeros)
+    tested = {(c[0], c[1], *c[6:]) for c in LINEAR4}
+    blocks = {"bf16": [(1, 8, 32), (1, 16, 32), (0, 16, 128), (0, 16, 256), (0, 32, 128), (0, 32, 256), (0, 64, 128), (0, 64, 256), (0, 128, 128)],
+              "f32": [(1, 8, 32), (0, 16, 128), (0, 16, 256), (0, 32, 128), (0, 32, 256)]}
+    for dtype in blocks:
+        for group, b in itertools.product((32, 64, 128), blocks[dtype]):
+            assert (dtype, group, *b, 1) in tested, (dtype, group, b)
+    rng, rare = random.Random(3), set()
+    for _ in range(20000):
+        dtype, group = rng.choice(("bf16", "f32")), rng.choice((32, 64, 128))
+        m, k, o = int(2 ** rng.uniform(0, 12)), 8 * int(2 ** rng.uniform(0, 12)), int(2 ** rng.uniform(0, 17))
+        c = linear4_shape(dtype, group, m, k, o, rng.random() < 0.5)
+        assert c.smem_bytes <= 227 * 1024 and 1 <= c.split <= 8
+        assert c.few or c.smem_bytes >= 193 * 1024          # (all of an SM's tensor memory: no second CTA that waits for some fits beside it)
+        if (dtype, group, c.few, c.rows, c.outputs, c.staged) not in tested:
+            rare.add((dtype, group, c.few, c.rows, c.outputs, c.staged))
+    assert all(not staged and not few for _, _, few, _, _, staged in rare) and len(rare) <= 4, rare
+
+
+def test_the_shape_hook_refuses_bad_arguments(lib):
+    w, out = msd.msd_weight4(A, A, None, 8, 64, 32), msd.msd_linear4_shape()
+    for dtype, m, weight in ((2, 1, w), (1, 0, w), (1, -1, w), (1, 1, msd.msd_weight4(A, A, None, 8, 60, 32)), (1, 1, msd.msd_weight4(A, A, None, 0, 64, 32))):
+        assert lib.msd_test_linear4_shape(dtype, m, ctypes.byref(weight), ctypes.byref(out)) == msd.MSD_ERR_INVALID
+    assert lib.msd_test_linear4_shape(1, 1, None, ctypes.byref(out)) == msd.MSD_ERR_INVALID
+    assert lib.msd_test_linear4_shape(1, 1, ctypes.byref(w), None) == msd.MSD_ERR_INVALID
 
 
 def test_linear4_without_rows_or_weight(lib):

@@ -1,11 +1,100 @@
 """Helpers for the tests of filtered sampling and tree acceptance: the definitions in 64 bits,
 row by row, and calls of the binding on host data."""
+import ctypes
 import math
 
 import numpy as np
 import torch
 
 from paper_2505_14260_gb300 import msd
+
+# A product for each kernel that msd_linear4 has, with scales and zeros staged and (where such sizes exist) not, and the sizes
+# of large models' layers: type, group, m, k, o, zeros; few, rows and outputs of a CTA, staged (msd_test_linear4_shape).
+LINEAR4 = [
+    ("bf16", 32, 1, 98776, 134, True, 0, 16, 128, 0),
+    ("bf16", 32, 11, 2040, 132, True, 0, 16, 128, 1),
+    ("bf16", 32, 1, 37984, 3053, True, 0, 16, 256, 0),
+    ("bf16", 32, 10, 1192, 4911, True, 0, 16, 256, 1),
+    ("bf16", 32, 19, 88664, 138, True, 0, 32, 128, 0),
+    ("bf16", 32, 19, 1088, 132, True, 0, 32, 128, 1),
+    ("bf16", 32, 21, 4160, 24002, True, 0, 32, 256, 0),
+    ("bf16", 32, 17, 1048, 6680, True, 0, 32, 256, 1),
+    ("bf16", 32, 33, 65504, 143, True, 0, 64, 128, 0),
+    ("bf16", 32, 38, 1056, 130, True, 0, 64, 128, 1),
+    ("bf16", 32, 907, 22280, 147, True, 0, 64, 256, 0),
+    ("bf16", 32, 36, 1032, 6374, True, 0, 64, 256, 1),
+    ("bf16", 32, 765, 23968, 132, True, 0, 128, 128, 0),
+    ("bf16", 32, 741, 1936, 135, True, 0, 128, 128, 1),
+    ("bf16", 32, 1, 1032, 131, True, 1, 8, 32, 1),
+    ("bf16", 32, 9, 1032, 131, True, 1, 16, 32, 1),
+    ("bf16", 64, 11, 3488, 137, True, 0, 16, 128, 1),
+    ("bf16", 64, 2, 78256, 2949, True, 0, 16, 256, 0),
+    ("bf16", 64, 9, 1912, 4928, True, 0, 16, 256, 1),
+    ("bf16", 64, 22, 1056, 131, True, 0, 32, 128, 1),
+    ("bf16", 64, 19, 49936, 4611, True, 0, 32, 256, 0),
+    ("bf16", 64, 18, 1160, 4639, False, 0, 32, 256, 1),
+    ("bf16", 64, 51, 130072, 140, True, 0, 64, 128, 0),
+    ("bf16", 64, 36, 1040, 141, True, 0, 64, 128, 1),
+    ("bf16", 64, 947, 65336, 142, False, 0, 64, 256, 0),
+    ("bf16", 64, 40, 1840, 6082, True, 0, 64, 256, 1),
+    ("bf16", 64, 912, 32664, 130, True, 0, 128, 128, 0),
+    ("bf16", 64, 453, 1656, 144, True, 0, 128, 128, 1),
+    ("bf16", 64, 1, 1136, 136, True, 1, 8, 32, 1),
+    ("bf16", 64, 10, 1088, 136, True, 1, 16, 32, 1),
+    ("bf16", 128, 9, 4824, 136, True, 0, 16, 128, 1),
+    ("bf16", 128, 13, 2280, 5127, True, 0, 16, 256, 1),
+    ("bf16", 128, 20, 1088, 142, True, 0, 32, 128, 1),
+    ("bf16", 128, 19, 1224, 6067, True, 0, 32, 256, 1),
+    ("bf16", 128, 37, 1056, 132, False, 0, 64, 128, 1),
+    ("bf16", 128, 145, 11104, 10036, True, 0, 64, 256, 0),
+    ("bf16", 128, 35, 1568, 6462, True, 0, 64, 256, 1),
+    ("bf16", 128, 468, 89184, 139, True, 0, 128, 128, 0),
+    ("bf16", 128, 458, 1760, 135, True, 0, 128, 128, 1),
+    ("bf16", 128, 1, 1088, 131, True, 1, 8, 32, 1),
+    ("bf16", 128, 15, 1056, 131, True, 1, 16, 32, 1),
+    ("f32", 32, 1, 78688, 131, True, 0, 16, 128, 0),
+    ("f32", 32, 11, 1040, 136, True, 0, 16, 128, 1),
+    ("f32", 32, 4, 26648, 3010, True, 0, 16, 256, 0),
+    ("f32", 32, 9, 1568, 1944, False, 0, 16, 256, 1),
+    ("f32", 32, 20, 77088, 133, True, 0, 32, 128, 0),
+    ("f32", 32, 19, 1048, 138, True, 0, 32, 128, 1),
+    ("f32", 32, 355, 31688, 130, True, 0, 32, 256, 0),
+    ("f32", 32, 473, 1576, 132, True, 0, 32, 256, 1),
+    ("f32", 32, 1, 1056, 131, True, 1, 8, 32, 1),
+    ("f32", 64, 2, 113936, 1944, True, 0, 16, 128, 0),
+    ("f32", 64, 9, 1064, 132, True, 0, 16, 128, 1),
+    ("f32", 64, 1, 41664, 3877, True, 0, 16, 256, 0),
+    ("f32", 64, 10, 1544, 1984, True, 0, 16, 256, 1),
+    ("f32", 64, 228, 118032, 139, True, 0, 32, 128, 0),
+    ("f32", 64, 19, 1040, 140, True, 0, 32, 128, 1),
+    ("f32", 64, 355, 64776, 131, True, 0, 32, 256, 0),
+    ("f32", 64, 595, 1216, 140, True, 0, 32, 256, 1),
+    ("f32", 64, 2, 1072, 131, True, 1, 8, 32, 1),
+    ("f32", 128, 10, 1056, 137, True, 0, 16, 128, 1),
+    ("f32", 128, 12, 1728, 2004, True, 0, 16, 256, 1),
+    ("f32", 128, 751, 78096, 301, True, 0, 32, 128, 0),
+    ("f32", 128, 20, 1088, 133, True, 0, 32, 128, 1),
+    ("f32", 128, 249, 110280, 149, True, 0, 32, 256, 0),
+    ("f32", 128, 242, 1608, 144, False, 0, 32, 256, 1),
+    ("f32", 128, 3, 1088, 133, True, 1, 8, 32, 1),
+    ("bf16", 64, 645, 4096, 11008, True, 0, 128, 128, 1),
+    ("bf16", 32, 645, 11008, 4096, False, 0, 128, 128, 0),
+    ("bf16", 32, 60, 4096, 11008, False, 0, 64, 256, 1),
+    ("bf16", 128, 645, 11008, 11008, True, 0, 128, 128, 0),
+    ("bf16", 128, 60, 13824, 32000, True, 0, 64, 256, 0),
+    ("f32", 32, 16, 5120, 32000, False, 0, 16, 256, 0),
+    ("f32", 32, 16, 5120, 32000, True, 0, 16, 256, 0),
+    ("f32", 64, 60, 4096, 11008, True, 0, 32, 256, 1),
+    ("f32", 128, 200, 11008, 4096, False, 0, 32, 256, 1),
+]
+
+
+def linear4_shape(dtype, group, m, k, o, zeros, codes=1 << 20):
+    """How msd_linear4 launches a product whose codes lie at this address."""
+    a = 1 << 20                       # (an address that nothing reads)
+    w, out = msd.msd_weight4(codes, a, a if zeros else None, o, k, group), msd.msd_linear4_shape()
+    assert msd.lib().msd_test_linear4_shape(msd.MSD_BF16 if dtype == "bf16" else msd.MSD_F32, m, ctypes.byref(w), ctypes.byref(out)) == msd.MSD_OK
+    return out
 
 
 class Row:
