@@ -524,7 +524,9 @@ typedef struct {
  * but with a weight in 4 bits. x [m][ldx] is bf16 (x_dtype MSD_BF16) or fp32 (MSD_F32), its rows
  * 16-byte aligned; y [m][ldy] is fp32. Differences c - zero are exact, sums are fp32, and a
  * group's sum is multiplied by its scale: no weight is rounded on the way. fp32 x enters as three
- * bf16 values that add up to it exactly. A value of x that is not finite makes its row of y so.
+ * bf16 values that add up to it exactly (below 2^-110 to a multiple of 2^-133, bf16's smallest
+ * step). A value of x that is not finite makes its row of y so; finite ones may too above 2^117,
+ * where a group's sum before its scale can leave the range of fp32.
  * m <= 65535 * 32. The kernel's waits are bounded (2 s): one that runs out leaves NaN in its part of y. */
 msd_status msd_linear4(const void *x_dev, int64_t ldx, int32_t x_dtype, int32_t m, const msd_weight4 *w,
                        float *y_dev, int64_t ldy, int32_t accumulate, void *stream);

@@ -44,7 +44,7 @@ template <> struct Octet<float> {
     }
     __device__ __forceinline__ void clear() { lo = hi = make_float4(0.f, 0.f, 0.f, 0.f); }
     // A value's upper 16 bits, those of what is left, and the 8 bits left then: truncations, so the three parts add
-    // up to it and none overflows. What is not finite leaves NaN in the later parts.
+    // up to it (but for what lies below 2^-133) and none overflows. What is not finite leaves NaN in the later parts.
     static __device__ __forceinline__ void part(float a, float c, uint32_t (&b)[3][4], int i) {
         const auto upper = [](float v) { return __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); };
         const float ra = a - upper(a), rc = c - upper(c), la = ra - upper(ra), lc = rc - upper(rc);

@@ -208,6 +208,38 @@ def test_fp32_x_is_not_rounded_in_any_kernel(m, o, group):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("m", [2, 10, 66, 200])
+def test_the_largest_values(m, group, dtype):
+    """Up to 2^117: a group's sum, 128 products with up to 15, stays finite before it is scaled."""
+    w = weight(40, 256, group, True)
+    x = torch.randn(m, 256, generator=gen(1), device="cuda").sign() * 2.0 ** 117
+    x[1::2] = x[1::2].abs()
+    x = x.to(dtype)
+    y = w.linear(x, torch.empty(m, 40, device="cuda"))
+    torch.cuda.synchronize()
+    check(w, x, y)
+
+
+@pytest.mark.parametrize("m,o", [(8, 64), (12, 64), (40, 64), (12, 20000)])
+def test_the_smallest_values(m, o):
+    """fp32 down to 2^-110 exactly, below it less what lies under bf16's smallest step, 2^-133; bf16 as it is. Scales of 2^100."""
+    ones = torch.full((o, 128), 0x99, dtype=torch.uint8, device="cuda")
+    w = msd.Weight4(ones, torch.full((o, 8), 2.0 ** 100, dtype=torch.bfloat16, device="cuda"), None, 32)
+    v = torch.tensor([(1 + 2.0 ** -23) * 2.0 ** e for e in (-100, -109, -110)] + [2.0 ** -126, 2.0 ** -133, 0.0, -0.0, 0.0], dtype=torch.float64)
+    small = torch.tensor([(1 + 2.0 ** -23) * 2.0 ** e for e in (-111, -112, -120, -126, -127, -133, -134, -149)], dtype=torch.float64)
+    for values_, room in ((v, 0.0), (small, 2.0 ** -33)):
+        x = torch.zeros(m, 256, device="cuda")
+        x[:8, 0] = values_.float().cuda()
+        y = w.linear(x, torch.empty(m, o, device="cuda")).double().cpu()
+        assert bool(((y[:8] - 2.0 ** 100 * values_.float().double()[:, None]).abs() <= room).all())
+    x = torch.zeros(m, 256, dtype=torch.bfloat16, device="cuda")
+    x[:2, 0] = torch.tensor([2.0 ** -126, 2.0 ** -133], device="cuda").bfloat16()
+    y = w.linear(x, torch.empty(m, o, device="cuda")).double()
+    assert bool((y[0] == 2.0 ** -26).all()) and bool((y[1] == 2.0 ** -33).all()) and bool((y[2:] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("m", [2, 10, 66, 200])
 def test_values_that_are_not_finite(m, dtype):
     """They reach their own rows of y alone; so do the largest finite ones."""
