@@ -23,7 +23,7 @@ namespace msd {
 // read from the caches (16 bytes a lane and word).
 // ---------------------------------------------------------------------------
 constexpr int FEW_WARPS = 8, FEW_OUT = 32, FEW_DEPTH = 3;
-constexpr size_t FEW_BESIDE = 64 * 1024;        // room for scales and zeros; longer rows read them where they are
+constexpr size_t FEW_BESIDE = 64 * 1024;        // room for scales and zeros
 
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                           uint32_t b1) {
@@ -36,8 +36,7 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
 // rows of x. WIDE: the codes of a lane and group are aligned to their size.
 template <typename T, int GROUP, int NT, bool WIDE>
 __global__ void __launch_bounds__(FEW_WARPS * 32)
-linear4_few_kernel(const T *__restrict__ x, long ldx, int m, Weight w, float *__restrict__ y, long ldy, int accumulate,
-                   int staged) {
+linear4_few_kernel(const T *__restrict__ x, long ldx, int m, Weight w, float *__restrict__ y, long ldy, int accumulate) {
     constexpr int WORDS = GROUP / 32;           // words of a lane, row and group
     constexpr int PER = 128 / GROUP;            // groups of a chunk
     constexpr int P = Octet<T>::PLANES;
@@ -85,9 +84,7 @@ linear4_few_kernel(const T *__restrict__ x, long ldx, int m, Weight w, float *__
     for (int d = 0; d < FEW_DEPTH; ++d)
         if (c0 + d < c1) fetch(c0 + d, q[d]);
 
-    const bf16 *sc_at = w.scales + (long)j0 * w.groups;
-    const uint8_t *z_at = w.zeros + (long)j0 * w.groups;
-    if (staged) {   // scales and zeros of the tile: one run of each, in 16-byte pieces where they lie so
+    {   // scales and zeros of the tile: one run of each, in 16-byte pieces where they lie so
         const auto copy = [&](uint8_t *to, const uint8_t *from, int bytes) {
             constexpr int T = FEW_WARPS * 32, U = 4;
             int done = 0;
@@ -105,10 +102,8 @@ linear4_few_kernel(const T *__restrict__ x, long ldx, int m, Weight w, float *__
             }
             for (int i = done + tid; i < bytes; i += T) to[i] = from[i];
         };
-        copy(reinterpret_cast<uint8_t *>(scales), reinterpret_cast<const uint8_t *>(sc_at), outs * w.groups * 2);
-        if (w.zeros) copy(zeros, z_at, outs * w.groups);
-        sc_at = scales;
-        z_at = zeros;
+        copy(reinterpret_cast<uint8_t *>(scales), reinterpret_cast<const uint8_t *>(w.scales + (long)j0 * w.groups), outs * w.groups * 2);
+        if (w.zeros) copy(zeros, w.zeros + (long)j0 * w.groups, outs * w.groups);
     }
     __syncthreads();
 
@@ -131,10 +126,10 @@ linear4_few_kernel(const T *__restrict__ x, long ldx, int m, Weight w, float *__
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int at = min(g + 8 * r, outs - 1) * w.groups + group;
-                const unsigned o = 0x4300u + (w.zeros ? z_at[at] : 8u);             // 128 + zero
+                const unsigned o = 0x4300u + (w.zeros ? zeros[at] : 8u);             // 128 + zero
                 const uint32_t both = o | o << 16;
                 off[r] = *reinterpret_cast<const __nv_bfloat162 *>(&both);
-                sc[r] = __bfloat162float(sc_at[at]);
+                sc[r] = __bfloat162float(scales[at]);
             }
 #pragma unroll
             for (int v = 0; v < WORDS; ++v) {
@@ -204,7 +199,7 @@ linear4_few_kernel(const T *__restrict__ x, long ldx, int m, Weight w, float *__
 }
 
 template <typename T>
-using FewKernel = void (*)(const T *, long, int, Weight, float *, long, int, int);
+using FewKernel = void (*)(const T *, long, int, Weight, float *, long, int);
 
 template <typename T, int GROUP>
 static FewKernel<T> few_kernel(bool two, bool wide) {
@@ -213,19 +208,18 @@ static FewKernel<T> few_kernel(bool two, bool wide) {
     return wide ? linear4_few_kernel<T, GROUP, 1, true> : linear4_few_kernel<T, GROUP, 1, false>;
 }
 
-template <typename T>
+static size_t few_beside(const Weight &w) { return (size_t)FEW_OUT * w.groups * 3; }
+
 static Linear4Shape few_shape(int m, const Weight &w) {
     const int align = w.group / 8;              // bytes of a lane's codes of a group
     const bool wide = reinterpret_cast<uintptr_t>(w.codes) % align == 0 && w.k / 2 % align == 0;
     const int step = m > 8 ? 16 : 8;            // m <= 16
-    const size_t sums = (size_t)FEW_WARPS * FEW_OUT * step * 4, beside = (size_t)FEW_OUT * w.groups * 3;
-    const bool staged = beside <= FEW_BESIDE;
-    return Linear4Shape{step, FEW_OUT, 1, staged, !wide, w.groups, sums + (staged ? beside : 0)};
+    return Linear4Shape{step, FEW_OUT, 1, true, !wide, w.groups, (size_t)FEW_WARPS * FEW_OUT * step * 4 + few_beside(w)};
 }
 
 template <typename T>
 static cudaError_t launch_few(const T *x, long ldx, int m, const Weight &w, float *y, long ldy, int accumulate, cudaStream_t s) {
-    const Linear4Shape c = few_shape<T>(m, w);
+    const Linear4Shape c = few_shape(m, w);
     const bool wide = !c.direct;
     const FewKernel<T> f = w.group == 128 ? few_kernel<T, 128>(m > 8, wide) : w.group == 64 ? few_kernel<T, 64>(m > 8, wide) : few_kernel<T, 32>(m > 8, wide);
     const size_t smem = c.smem;
@@ -234,7 +228,7 @@ static cudaError_t launch_few(const T *x, long ldx, int m, const Weight &w, floa
     // (one value, whatever the call: another thread may be between this and its launch)
     if (smem > 48 * 1024) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
     if (e == cudaSuccess) {
-        e = launch_chain(f, (w.o + FEW_OUT - 1) / FEW_OUT, FEW_WARPS * 32, smem, s, x, ldx, m, w, y, ldy, accumulate, (int)c.staged);
+        e = launch_chain(f, (w.o + FEW_OUT - 1) / FEW_OUT, FEW_WARPS * 32, smem, s, x, ldx, m, w, y, ldy, accumulate);
         note_launch();
     }
     return e;
@@ -244,10 +238,11 @@ static cudaError_t launch_few(const T *x, long ldx, int m, const Weight &w, floa
 // (1, 8 and 16 rows, k 1024 to 11008, groups of 32, 64 and 128), and 152 of them run at a time; two on an SM, as those of up to 8 bf16
 // rows do, take about as long as one after the other. (One row, groups of 128: k and o 4096 6.3 us here, 9.7 there; k 11008 12.3 and
 // 15.2; o 32000 25.5 and 25.0. Groups of 32: k 1024 4.5 and 7.6, o 11008 31 and 19. 16 rows, o 11008, groups of 128: 21 and 13.5.)
+// Rows whose scales would not fit beside the sums (k past 21824, 43648 and 87296) take less time there in any case.
 template <typename T>
 static bool few_rows(int m, const Weight &w) {
     constexpr bool f32 = sizeof(T) == 4;
-    if (m > (f32 ? 8 : 16)) return false;
+    if (m > (f32 ? 8 : 16) || few_beside(w) > FEW_BESIDE) return false;
     constexpr float us[3][3] = {{2.4e-3f, 1.3e-3f, 0.9e-3f}, {2.6e-3f, 1.6e-3f, 1.2e-3f}, {2.8e-3f, 1.7e-3f, 1.5e-3f}};
     const float each = us[f32 ? 2 : m > 8][w.group == 32 ? 0 : w.group == 64 ? 1 : 2];
     const float waves = !f32 && m <= 8 ? std::max(1.f, 1.1f / (FEW_OUT * 152) * w.o) : (float)((w.o + FEW_OUT * 152 - 1) / (FEW_OUT * 152));
@@ -446,7 +441,7 @@ msd_status msd_test_linear4_shape(int32_t x_dtype, int32_t m, const msd_weight4 
     const auto shape = [&](auto v) {
         using T = decltype(v);
         const bool few = few_rows<T>(m, w);
-        const Linear4Shape c = few ? few_shape<T>(m, w) : linear4_tc_shape<T>(m, w);
+        const Linear4Shape c = few ? few_shape(m, w) : linear4_tc_shape<T>(m, w);
         *out = msd_linear4_shape{few, c.rows, c.outputs, c.split, c.staged, c.direct, (int32_t)c.smem};
     };
     x_dtype == MSD_F32 ? shape(float()) : shape(bf16());
