@@ -542,6 +542,12 @@ typedef struct {
 } msd_linear4_shape;
 msd_status msd_test_linear4_shape(int32_t x_dtype, int32_t m, const msd_weight4 *w, msd_linear4_shape *out);
 
+/* Test hook of its failure detection: the product on tcgen05, whatever m, whose CTAs get no codes from the chunk-th 128 elements of
+ * k on (where tensor copies bring them: codes 16-byte aligned, k a multiple of 32). Their waits run out, what is in flight ends,
+ * and their part of y is NaN, as msd_linear4 says; nothing else is disturbed. */
+msd_status msd_test_linear4_timeout(const void *x_dev, int64_t ldx, int32_t x_dtype, int32_t m, const msd_weight4 *w,
+                                    float *y_dev, int64_t ldy, int32_t chunk, void *stream);
+
 /* Writes the codes, scales and (unless null) zeros of *out from w [o][ldw], bf16 or fp32 with
  * 16-byte aligned rows. Per group, without zeros: scale = max|w| / 7 rounded to bf16; with zeros:
  * scale = (max(w, 0) - min(w, 0)) / 15 rounded to bf16, zero = -min(w, 0) / scale to the nearest

@@ -413,6 +413,22 @@ static bool bad_rows(const void *p, long ld, int dtype, int width) {
     return !p || ld < width || reinterpret_cast<uintptr_t>(p) % 16 || ld * size % 16;
 }
 
+static msd_status linear4(const void *x, long ldx, int x_dtype, int m, const msd_weight4 *weight, float *y, long ldy, int accumulate,
+                          void *stream, int stall) {
+    Weight w;
+    if (m < 0 || m > MOST_ROWS || !take_weight(weight, &w) || (x_dtype != MSD_F32 && x_dtype != MSD_BF16)) return MSD_ERR_INVALID;
+    if (m == 0) return MSD_OK;
+    if (bad_rows(x, ldx, x_dtype, w.k) || !y || ldy < w.o || reinterpret_cast<uintptr_t>(y) % 4) return MSD_ERR_INVALID;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const auto run = [&](auto *p) {
+        using T = std::remove_const_t<std::remove_pointer_t<decltype(p)>>;
+        if (stall == NO_STALL && few_rows<T>(m, w)) return launch_few(p, ldx, m, w, y, ldy, accumulate, s);
+        return launch_linear4_tc(p, ldx, m, w, y, ldy, accumulate, s, stall);
+    };
+    const cudaError_t e = x_dtype == MSD_F32 ? run(static_cast<const float *>(x)) : run(static_cast<const bf16 *>(x));
+    return e == cudaSuccess ? MSD_OK : MSD_ERR_CUDA;
+}
+
 }  // namespace msd
 
 using namespace msd;
@@ -421,18 +437,13 @@ extern "C" {
 
 msd_status msd_linear4(const void *x, int64_t ldx, int32_t x_dtype, int32_t m, const msd_weight4 *weight, float *y,
                        int64_t ldy, int32_t accumulate, void *stream) {
-    Weight w;
-    if (m < 0 || m > MOST_ROWS || !take_weight(weight, &w) || (x_dtype != MSD_F32 && x_dtype != MSD_BF16)) return MSD_ERR_INVALID;
-    if (m == 0) return MSD_OK;
-    if (bad_rows(x, ldx, x_dtype, w.k) || !y || ldy < w.o || reinterpret_cast<uintptr_t>(y) % 4) return MSD_ERR_INVALID;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const auto run = [&](auto *p) {
-        using T = std::remove_const_t<std::remove_pointer_t<decltype(p)>>;
-        return few_rows<T>(m, w) ? launch_few(p, (long)ldx, m, w, y, (long)ldy, accumulate, s)
-                                 : launch_linear4_tc(p, (long)ldx, m, w, y, (long)ldy, accumulate, s);
-    };
-    const cudaError_t e = x_dtype == MSD_F32 ? run(static_cast<const float *>(x)) : run(static_cast<const bf16 *>(x));
-    return e == cudaSuccess ? MSD_OK : MSD_ERR_CUDA;
+    return linear4(x, ldx, x_dtype, m, weight, y, ldy, accumulate, stream, NO_STALL);
+}
+
+msd_status msd_test_linear4_timeout(const void *x, int64_t ldx, int32_t x_dtype, int32_t m, const msd_weight4 *weight, float *y,
+                                    int64_t ldy, int32_t chunk, void *stream) {
+    if (chunk < 0 || chunk == NO_STALL || !weight || reinterpret_cast<uintptr_t>(weight->codes) % 16 || weight->k % 32) return MSD_ERR_INVALID;
+    return linear4(x, ldx, x_dtype, m, weight, y, ldy, 0, stream, chunk);
 }
 
 msd_status msd_test_linear4_shape(int32_t x_dtype, int32_t m, const msd_weight4 *weight, msd_linear4_shape *out) {

@@ -60,9 +60,12 @@ template <> struct Octet<float> {
     }
 };
 
-// Products on the 5th-generation tensor cores (linear4_tc.cu).
+// Products on the 5th-generation tensor cores (linear4_tc.cu). stall: chunks of 128 elements of K from this one on never get
+// their codes, so that the waits for them run out (a test).
+constexpr int NO_STALL = 0x7FFFFFFF;
 template <typename T>
-cudaError_t launch_linear4_tc(const T *x, long ldx, int m, const Weight &w, float *y, long ldy, int accumulate, cudaStream_t s);
+cudaError_t launch_linear4_tc(const T *x, long ldx, int m, const Weight &w, float *y, long ldy, int accumulate, cudaStream_t s,
+                              int stall = NO_STALL);
 
 // How they are launched: rows and outputs to a CTA, parts of K, whether scales and zeros are staged (`slice` groups of them) and codes
 // read without tensor copies.

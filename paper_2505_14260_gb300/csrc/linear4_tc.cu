@@ -76,6 +76,7 @@ struct Args {
     float *y;
     int m, accumulate, split, staged, slice;                    // slice: groups of a CTA that are staged
     int direct;                                                 // codes at addresses that tensor copies do not take
+    int stall;                                                  // chunks of K from this one on get no codes (a test's waits run out)
 };
 
 __device__ __forceinline__ void cluster_sync() {
@@ -138,14 +139,14 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     constexpr bool HALF = L::HALF;
     constexpr uint32_t WSTAGE = L::WSTAGE;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * WS + 3 * XS + 16 + 4 * DS];
+    __shared__ __align__(8) uint64_t bars[2 * WS + 3 * XS + 16 + 4 * DS + 4];
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_abort;
     const uint32_t base = (su32(smem_raw) + 1023u) & ~1023u;
     uint8_t *const smem = smem_raw + (base - su32(smem_raw));
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t w_full = su32(bars), w_empty = w_full + 8 * WS, x_full = w_empty + 8 * WS, x_empty = x_full + 8 * XS,
-                   a_full = x_empty + 8 * XS, a_empty = a_full + 64, d_full = a_empty + 64, d_empty = d_full + 16 * DS, x_raw = d_empty + 16 * DS;
+                   a_full = x_empty + 8 * XS, a_empty = a_full + 64, d_full = a_empty + 64, d_empty = d_full + 16 * DS, x_raw = d_empty + 16 * DS, drained = x_raw + 8 * XS;
     const int rank = (int)(blockIdx.x % a.split), tile = (int)(blockIdx.x / a.split);
     const int j0 = tile * OUT, i0 = (int)blockIdx.y * N, rows = min(N, a.m - i0);
     const int chunks = (a.w.k + CHUNK - 1) / CHUNK;
@@ -168,6 +169,7 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             bar_init(d_full + 8 * i, 1);
             bar_init(d_empty + 8 * i, HALF ? 8 : 4);
         }
+        for (int i = 0; i < 4; ++i) bar_init(drained + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_abort = 0;
         if (!a.direct) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
@@ -222,7 +224,7 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         int copied = slot;                                      // chunks copied: slot, slot + CYCLE, ... below this
         const auto copy = [&](int ci) {
             const int ws = ci % WS;
-            if (!use_wait(w_empty + 8 * ws, ci + WS, WS, &s_abort)) return;
+            if (c0 + ci >= a.stall || !use_wait(w_empty + 8 * ws, ci + WS, WS, &s_abort)) return;
             const uint32_t to = base + L::W + ws * WSTAGE, bar = w_full + 8 * ws;
             w_expect_tx(on, bar, WSTAGE);
             w_tma2d(on, to, &map, (c0 + ci) * (CHUNK / 2), j0, bar);
@@ -403,6 +405,11 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             }
             if (ok) w_commit(on, x_empty + 8 * xs);
         }
+        if (__any_sync(0xffffffffu, s_abort)) {                 // MMAs in flight end before their operands and tensor memory go
+            volatile int never = 0;
+            w_commit(on, drained + 8 * warp);
+            bar_wait_slow(drained + 8 * warp, 0, &never, nullptr);
+        }
         __syncwarp();
         done();
     } else {
@@ -431,9 +438,10 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             // a stage a warp: copied, then each 8 values put into the order of the codes' pairs where they lie
             static_assert(XS == 4, "");
             const uint32_t on = elect_one(), at = base + L::X + w * L::XSTAGE;
-            int filled = w;
-            for (; filled < nc; filled += XS) {
+            int copied = -1;
+            for (int filled = w; filled < nc; filled += XS) {
                 if (!use_wait(x_empty + 8 * w, filled + XS, XS, &s_abort)) break;
+                copied = filled;
                 w_expect_tx(on, x_raw + 8 * w, L::XSTAGE);
                 w_tma2d(on, at, &x_map, (c0 + filled) * CHUNK, i0, x_raw + 8 * w);
                 w_tma2d(on, at + L::XBOX, &x_map, (c0 + filled) * CHUNK + 64, i0, x_raw + 8 * w);
@@ -454,9 +462,9 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
                 __syncwarp();
                 if (lane == 0) bar_arrive(x_full + 8 * w);
             }
-            if (s_abort && filled < nc) {                       // a copy in flight lands before the CTA goes on
+            if (s_abort && copied >= 0) {                       // a copy in flight lands before the CTA goes on
                 volatile int never = 0;
-                bar_wait_slow(x_raw + 8 * w, (uint32_t)(filled / XS) & 1u, &never, nullptr);
+                bar_wait_slow(x_raw + 8 * w, (uint32_t)(copied / XS) & 1u, &never, nullptr);
             }
             __syncwarp();
         } else {
@@ -645,8 +653,8 @@ auto with_group(const Weight &w, F f) {
 }  // namespace
 
 template <typename T>
-cudaError_t launch_linear4_tc(const T *x, long ldx, int m, const Weight &w, float *y, long ldy, int accumulate, cudaStream_t s) {
-    const Args a{w, x, ldx, ldy, y, m, accumulate, 1, 0, 0, 0};
+cudaError_t launch_linear4_tc(const T *x, long ldx, int m, const Weight &w, float *y, long ldy, int accumulate, cudaStream_t s, int stall) {
+    const Args a{w, x, ldx, ldy, y, m, accumulate, 1, 0, 0, 0, stall};
     return with_group(w, [&](auto group) {
         return with_blocks<T, decltype(group)::value>(
             m, w, [&](auto rows, auto outs) { return launch<T, decltype(group)::value, decltype(rows)::value, decltype(outs)::value>(a, s); });
@@ -670,7 +678,7 @@ template float linear4_tc_us<float>(const Weight &);
 template float linear4_tc_us<bf16>(const Weight &);
 template Linear4Shape linear4_tc_shape<float>(int, const Weight &);
 template Linear4Shape linear4_tc_shape<bf16>(int, const Weight &);
-template cudaError_t launch_linear4_tc<float>(const float *, long, int, const Weight &, float *, long, int, cudaStream_t);
-template cudaError_t launch_linear4_tc<bf16>(const bf16 *, long, int, const Weight &, float *, long, int, cudaStream_t);
+template cudaError_t launch_linear4_tc<float>(const float *, long, int, const Weight &, float *, long, int, cudaStream_t, int);
+template cudaError_t launch_linear4_tc<bf16>(const bf16 *, long, int, const Weight &, float *, long, int, cudaStream_t, int);
 
 }  // namespace msd

@@ -151,6 +151,8 @@ _SIGNATURES = {
     "msd_linear4": (c_int32, [c_void_p, c_int64, c_int32, c_int32, POINTER(msd_weight4), c_void_p, c_int64, c_int32,
                               c_void_p]),
     "msd_test_linear4_shape": (c_int32, [c_int32, c_int32, POINTER(msd_weight4), POINTER(msd_linear4_shape)]),
+    "msd_test_linear4_timeout": (c_int32, [c_void_p, c_int64, c_int32, c_int32, POINTER(msd_weight4), c_void_p, c_int64, c_int32,
+                                           c_void_p]),
     "msd_quantize4": (c_int32, [c_void_p, c_int64, c_int32, POINTER(msd_weight4), c_void_p, c_int64, c_void_p]),
     "msd_sample": (c_int32, [c_void_p, c_int64, c_int32, c_int32, c_int32, POINTER(msd_filter), c_void_p, c_void_p,
                              c_void_p, c_void_p, c_int64, c_void_p]),

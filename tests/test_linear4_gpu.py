@@ -261,6 +261,26 @@ def test_values_that_are_not_finite(m, dtype):
     assert torch.equal(y[~bad.cuda()], clean[~bad.cuda()])
 
 
+@pytest.mark.parametrize("m,k,o,group,dtype,chunk", [(1, 5120, 300, 128, torch.bfloat16, 13), (60, 1024, 300, 64, torch.bfloat16, 0),
+                                                     (60, 640, 20000, 32, torch.bfloat16, 3), (458, 3520, 135, 128, torch.bfloat16, 7),
+                                                     (30, 4096, 300, 64, torch.float32, 2)])
+def test_a_wait_that_runs_out(m, k, o, group, dtype, chunk):
+    """Codes that never come: after 2 s every role gives up, y is NaN, nothing beside it is written and the next call is as ever."""
+    w = weight(o, k, group, True)
+    x = torch.randn(m, k, generator=gen(1), device="cuda").to(dtype)
+    wide = torch.full((m, o + 3), 7.0, device="cuda")
+    start = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    start[0].record()
+    assert msd.lib().msd_test_linear4_timeout(x.data_ptr(), k, msd.MSD_BF16 if dtype == torch.bfloat16 else msd.MSD_F32, m, w._ref,
+                                              wide.data_ptr(), o + 3, chunk, torch.cuda.current_stream().cuda_stream) == msd.MSD_OK
+    start[1].record()
+    y = w.linear(x, torch.empty(m, o, device="cuda"))
+    torch.cuda.synchronize()
+    assert bool(wide[:, :o].isnan().all()) and bool((wide[:, o:] == 7).all())
+    assert 1900 < start[0].elapsed_time(start[1]) < 3000
+    check(w, x, y)
+
+
 def test_no_rows():
     weight(8, 64, 32, False).linear(torch.empty(0, 64, device="cuda"), torch.empty(0, 8, device="cuda"))
 

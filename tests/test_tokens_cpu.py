@@ -76,6 +76,13 @@ def test_the_shape_hook_refuses_bad_arguments(lib):
     assert lib.msd_test_linear4_shape(1, 1, ctypes.byref(w), None) == msd.MSD_ERR_INVALID
 
 
+def test_the_timeout_hook_refuses_what_it_cannot_hold_back(lib):
+    for codes, k, chunk in ((A, 64, -1), (A, 64, 2**31 - 1), (A + 4, 64, 0), (A, 72, 0)):
+        w = msd.msd_weight4(codes, A, None, 8, k, 32)
+        assert lib.msd_test_linear4_timeout(A, k, 1, 1, ctypes.byref(w), A, 8, chunk, None) == msd.MSD_ERR_INVALID
+    assert lib.msd_test_linear4_timeout(A, 64, 1, 1, None, A, 8, 0, None) == msd.MSD_ERR_INVALID
+
+
 def test_linear4_without_rows_or_weight(lib):
     assert linear(lib, m=0) == msd.MSD_OK
     assert lib.msd_linear4(A, 64, 1, 1, None, A, 8, 0, None) == msd.MSD_ERR_INVALID
