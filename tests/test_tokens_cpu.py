@@ -2,7 +2,11 @@
 anything touches a GPU, and the sums behind the fixed-point weights."""
 import ctypes
 import itertools
+import os
 import random
+import re
+import shutil
+import subprocess
 
 import pytest
 import torch
@@ -145,3 +149,64 @@ def test_the_binding_refuses_host_tensors(lib):
     with pytest.raises(ValueError):
         msd.Filter(temperature=torch.ones(2))
     assert msd.Filter().n is None
+
+
+# weight_exp.cuh compiled for the host: single operations of fp32 are the same there (no contraction, fmaf exact)
+SHIM = """
+#include <cmath>
+#include <cstdint>
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+#define __device__
+#define __forceinline__ inline
+struct float2 { float x, y; };
+static float2 make_float2(float x, float y) { return {x, y}; }
+static unsigned __float_as_uint(float f) { unsigned u; memcpy(&u, &f, 4); return u; }
+static float __uint_as_float(unsigned u) { float f; memcpy(&f, &u, 4); return f; }
+static float __fmul_rn(float a, float b) { return a * b; }
+static float __fdiv_rn(float a, float b) { return a / b; }
+"""
+MAIN = """
+int main() {
+    static const msd::ExpTable table;
+    const float2 *pairs = reinterpret_cast<const float2 *>(table.pair);
+    const float temperatures[] = {1.f, 0.7f, 0.05f, 1e-3f, 3.f, 30.f, 1e4f, 0x1p-100f, 0x1p100f};
+    double worst = 0;
+    uint64_t seed = 1;
+    for (float t : temperatures) {
+        const float log2e = 1.44269504088896340736f, rest = (float)(1.44269504088896340736 - (double)log2e);
+        msd::RowScale r;
+        r.c_hi = __fdiv_rn(log2e, t);
+        r.c_lo = __fdiv_rn(fmaf(-r.c_hi, t, log2e) + rest, t);
+        for (int i = 0; i < 200000; ++i) {
+            seed = seed * 6364136223846793005ull + 1442695040888963407ull;
+            const double spread = 33.0 * (double)(seed >> 40) / (1 << 24);
+            seed = seed * 6364136223846793005ull + 1442695040888963407ull;
+            r.top = (float)(((double)(seed >> 40) / (1 << 24) - 0.5) * 60.0 * (t < 100.f ? t : 100.f));
+            const float x = i % 16 == 0 ? r.top : (float)(r.top - spread * t);
+            const long double want = ldexpl(expl(((long double)x - (long double)r.top) / (long double)t), msd::WEIGHT_BITS);
+            const unsigned long long w = msd::weight_of(msd::exponent_of(x, r), pairs);
+            if (i % 16 == 0 && w != 1ull << msd::WEIGHT_BITS) return puts("the largest is not 2^44"), 1;
+            const double off = (double)fabsl((long double)w - want);
+            if (off > worst) worst = off;
+        }
+    }
+    printf("%.4f\\n", worst);
+    return 0;
+}
+"""
+
+
+def test_weights_are_exponentials_to_a_unit_or_two(tmp_path):
+    """2^44 exp((logit - max) / T) of 1.8 million logits at 9 temperatures against long double: half a unit for rounding to an integer,
+    and what the exponent (a pair of fp32 values) and the series leave, which weight_exp.cuh puts below another one and a half."""
+    if shutil.which("g++") is None:
+        pytest.skip("no host compiler")
+    text = open(os.path.join(os.path.dirname(msd.__file__), "csrc", "weight_exp.cuh")).read()
+    text = re.sub(r'#pragma once|#include "common.cuh"', "", text)
+    src = tmp_path / "weights.cpp"
+    src.write_text(SHIM + text + MAIN)
+    subprocess.run(["g++", "-O1", "-std=c++17", "-ffp-contract=off", str(src), "-o", str(tmp_path / "weights")], check=True)
+    out = subprocess.run([str(tmp_path / "weights")], check=True, capture_output=True, text=True).stdout
+    assert float(out) <= 2.0, out
