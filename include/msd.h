@@ -577,7 +577,7 @@ typedef struct {
  * and the others none. A row without any weight gives -1. logp (nullable): the natural logarithm of
  * the token's share of the weight, -inf for a token of -1. probs (nullable) [rows][ldp] fp32: every
  * id's share. Weights are taken to 2^-44 of the largest and summed exactly, so tokens do not depend on the
- * grid and agree with an exact evaluation unless u or top_p lies within vocab * 2^-44 of a border.
+ * grid and agree with an exact evaluation unless u, top_p or min_p lies within vocab * 2^-44 of a border.
  * f: null, or the rows' settings. vocab <= 393216. */
 msd_status msd_sample(const void *logits_dev, int64_t ld, int32_t dtype, int32_t rows, int32_t vocab,
                       const msd_filter *f, const float *u_dev, int32_t *tokens_dev, float *logp_dev,

@@ -16,7 +16,7 @@ namespace msd {
 // 128 + zero (exact), 11 for 8 codes of a lane; the products' order within a word is free, so
 // pairs are (0, 4), (1, 5), (2, 6), (3, 7) of it and x is permuted alike. Each mma takes codes of
 // one group, and a group's sum is scaled on the way into the total, so no weight is rounded. (A tensor core cuts a sum's last
-// bits at each product added: fp32's later planes have sums of their own, which cost nothing and made 4.6e-7 of 1.1e-7 at groups of 128.)
+// bits at each product added: fp32's later planes have sums of their own, which cost nothing. Groups of 128: errors of 8e-8, not 4.4e-7.)
 //
 // A warp has 32 outputs and every 8th run of groups; the 8 warps' totals meet in shared memory in
 // a fixed order. Weights go from memory to registers, DEPTH chunks of 128 elements ahead; x is

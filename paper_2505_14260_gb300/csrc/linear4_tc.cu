@@ -17,14 +17,22 @@
 //                outputs)
 //   warps 16-31  a row of W a thread: codes -> tensor memory; four warps for the even chunks of a half and four for the odd ones, or
 //                four for every fourth chunk; the first of the four also issue the copies of codes, four chunks ahead
-// What bounds it is the integer pipe, half a warp a cycle, and the issue slots behind it. For 8 codes, in the order of a word's
-// shifts ((0, 4), (1, 5), (2, 6), (3, 7), x ordered alike), it takes 3 shifts, 4 selections and 4 subtractions: about 1000 cycles
-// for a chunk of 256 outputs with scales, copies and waits, against 512 of the MMAs of 64 rows and 330 of a copy at the rate of
-// memory. With 128 rows to a CTA a chunk of 128 outputs takes 950 cycles, of them 512 of MMAs: there x stays as copied (ordering
-// 128 rows took the four copying warps longer than that) and codes come out in their own order, for 2 more operations of 8 codes.
+// For 8 codes, in the order of a word's shifts ((0, 4), (1, 5), (2, 6), (3, 7), x ordered alike), the integer pipe, half a warp a
+// cycle, takes 3 shifts, 4 selections and 4 subtractions: 704 cycles for a chunk of 256 outputs, against 512 of the MMAs of 64 rows and
+// 330 of a copy at the rate of memory. With 128 rows to a CTA x stays as copied (ordering 128 rows took the four copying warps
+// longer than a chunk) and codes come out in their own order, for 2 more operations of 8 codes.
+//
+// What bounds it (clocks around the roles' waits in a scratch build, which itself takes 5 to 10% longer): no pipe alone, the integer one
+// is busy 37 to 54% and issue 50 to 65% of the time.
+//   groups of 128   60 rows, 256 outputs: 1350 cycles a chunk, the code warps busy 84% of them, MMAs waiting for x 28, codes 25 and
+//                   accumulators 19%. 128 rows and outputs: 900, 512 of them MMAs; the code warps wait 40% for their buffer, the sum warps
+//                   51% for sums. 16 rows, 128 outputs: 720; a code warp waits 27% for its buffer, the sum warps 65%
+//   groups of 64, 32   MMAs wait for accumulators that the sum warps have not read: 66 and 78% of the time with 128 rows (1550 and 2300
+//                   cycles a chunk of 128 outputs), 75% with 64 (groups of 32)
+//   fp32, 32 rows   MMAs wait for x 64% of the time (groups of 128, 2600 cycles for 256 outputs): the copying warps split it in planes
 // To start and to end a CTA takes about 4 us, to join 2 to 3.5. One group of warps a half doing everything in turn took 1800 cycles
-// a chunk. Measured, us (groups of 128, other weights for each call): k 4096, o 11008: 16 rows 13.5, 60 rows 16.4, 128 rows 22, 645
-// rows 83 (700 TFLOP/s); k 11008, o 4096, 60 rows 18.2. A wait that runs out (2 s) leaves NaN in the CTA's part of y.
+// a chunk. Measured, us (groups of 128, other weights for each call): k 4096, o 11008: 16 rows 13.5, 60 rows 16.7, 128 rows 22, 645
+// rows 84 (690 TFLOP/s); k 11008, o 4096, 60 rows 18.2. A wait that runs out (2 s) leaves NaN in the CTA's part of y.
 #include <algorithm>
 #include <cstring>
 #include <type_traits>
@@ -146,7 +154,8 @@ linear4_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     uint8_t *const smem = smem_raw + (base - su32(smem_raw));
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t w_full = su32(bars), w_empty = w_full + 8 * WS, x_full = w_empty + 8 * WS, x_empty = x_full + 8 * XS,
-                   a_full = x_empty + 8 * XS, a_empty = a_full + 64, d_full = a_empty + 64, d_empty = d_full + 16 * DS, x_raw = d_empty + 16 * DS, drained = x_raw + 8 * XS;
+                   a_full = x_empty + 8 * XS, a_empty = a_full + 64, d_full = a_empty + 64, d_empty = d_full + 16 * DS, x_raw = d_empty + 16 * DS,
+                   drained = x_raw + 8 * XS;
     const int rank = (int)(blockIdx.x % a.split), tile = (int)(blockIdx.x / a.split);
     const int j0 = tile * OUT, i0 = (int)blockIdx.y * N, rows = min(N, a.m - i0);
     const int chunks = (a.w.k + CHUNK - 1) / CHUNK;
@@ -636,7 +645,9 @@ auto with_outputs(int m, const Weight &w, F f) {
 template <typename T, int GROUP, typename F>
 auto with_blocks(int m, const Weight &w, F f) {
     if (m <= 16) return with_outputs<T, GROUP, 16>(m, w, f);
-    if constexpr (sizeof(T) == 2) {             // (planes of 64 rows would leave room for one stage)
+    // (fp32: 32 rows at most. With 256 outputs the 64 totals of 64 rows would leave the copying warps too few registers; with 128
+    // outputs two stages of x and the codes' ring would fit: not built)
+    if constexpr (sizeof(T) == 2) {
         // 128 rows of x with 128 outputs: chunks that take less than those of 64 rows and 256 outputs. (645 rows, k 4096, 11008
         // outputs: 82 us instead of 112.) Rows just past a multiple of 128 can leave the first with more waves: 130 rows of the
         // same 41 us instead of 30.

@@ -17,8 +17,8 @@
 // CTA, and the rest is done on that list; else sums of blocks of 128 ids lead to the token.
 //
 // What bounds it: for one row its phases in turn, 4 of them meetings of the cluster (a row of 32000 fp32 logits, top-k 50, top-p
-// 0.9: 12.8 us); for many, issue slots, 60 to 70 instructions a token for each pass with exact weights, two of them for top-p of
-// a row that leaves many tokens (64 rows of 100003 bf16 logits, top-p 0.95: 60 us, 61% of slots), 35 for a pass that counts.
+// 0.9: 12 to 13 us); for many, issue slots, 60 to 70 instructions a token for each pass with exact weights, two of them for top-p of
+// a row that leaves many tokens (64 rows of 100003 bf16 logits, top-p 0.95: 60 us in a graph, 61% of slots), 35 for a pass that counts.
 #include <algorithm>
 
 #include "msd.h"
@@ -1088,7 +1088,7 @@ constexpr int STAGED_ABOVE = 2 * RESIDENT;
 static_assert(data_offset(most_blocks(MAX_VOCAB / 8, 4)) + (size_t)most_blocks(MAX_VOCAB / 8, 4) * BLOCK * 4 <= 227 * 1024, "the largest row fits");
 
 // How many CTAs share a row, and the ids of each: as few as leave room for two CTAs on an SM, 4 where there are few
-// rows (and 2048 ids for each; 8 are no faster: one row of 32000 takes 13.9 us in 4 parts, 13.5 in 8, 16.6 in 2, 20.7 in 1).
+// rows (and 2048 ids for each; 8 are no faster: one row of 32000 in a graph takes 11.9 us in 4 parts, 12.0 in 8, 13.3 in 2, 15.7 in 1).
 struct Cut {
     int ctas, slice;
     size_t smem;
