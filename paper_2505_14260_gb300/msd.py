@@ -760,9 +760,11 @@ def accept(logits: torch.Tensor, batch: Batch, tree: Tree, u: torch.Tensor, sett
         raise ValueError("a row of logits per row of the batch, a tree per sequence")
     if u.dim() != 3 or u.shape[0] != n or path.shape != (n, u.shape[1]):
         raise ValueError("u is [n, depth + 1, children + 1], path [n, depth + 1]")
-    for t in (batch.seqs, tree.tokens):
+    for t in (batch.seqs, batch.row_start):
         if t.device != dev:
             raise ValueError("batch, tree and logits are on one GPU")
+    for what, t, size in (("tokens", tree.tokens, n * tree.N), ("parent", tree.parent, n * tree.N), ("n_nodes", tree.n_nodes, n)):
+        _vector(t, f"the tree's {what}", torch.int32, size, dev)
     with _memory_of(stream):
         scratch = torch.empty(2 * rows, dtype=torch.int32, device=dev)
     st = lib().msd_accept_batch(

@@ -419,3 +419,20 @@ def test_refusals():
             bad()
     with pytest.raises(msd.MsdError):
         msd.accept(x, b, tree, torch.rand(2, 3, 258, device="cuda"), None, path, v, v)
+
+
+def test_trees_whose_arrays_do_not_fit_are_refused():
+    """Arrays of a tree that a program has put in place of the ones that it was made with: host memory, other types, fewer entries."""
+    x, b = logits(4, 100), msd.Batch(torch.arange(2, dtype=torch.int32, device="cuda"), torch.tensor([0, 2, 4], dtype=torch.int32, device="cuda"), 4)
+    path, v, u = torch.zeros(2, 3, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda"), torch.rand(2, 3, 4, device="cuda")
+    for name, change in (("tokens", torch.Tensor.cpu), ("parent", torch.Tensor.cpu), ("n_nodes", torch.Tensor.cpu), ("tokens", torch.Tensor.long),
+                         ("parent", torch.Tensor.float), ("tokens", lambda t: t[:3]), ("parent", lambda t: t[:1]), ("n_nodes", lambda t: t[:1]),
+                         ("parent", lambda t: t.repeat(2)[::2])):
+        tree = msd.Tree(2, 2)
+        setattr(tree, name, change(getattr(tree, name)))
+        with pytest.raises(ValueError):
+            msd.accept(x, b, tree, u, None, path, v, v)
+    tree = msd.Tree(2, 2)
+    tree.n_nodes = None                    # (as many as rows)
+    msd.accept(x, b, tree, u, None, path, v, v.clone())
+    torch.cuda.synchronize()
